@@ -1,0 +1,52 @@
+// What the operators of ssd_ops.h share: element types, loads, reductions and
+// the host's error reporting.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "../../include/ssd_ops.h"
+
+namespace ssd {
+
+// records the message for ssd_last_error and returns the status (runtime.hip)
+ssd_status op_fail(ssd_status st, const char* msg) noexcept;
+
+#define OP_REQUIRE(cond, status, msg) \
+  do {                                \
+    if (!(cond)) return ssd::op_fail(status, msg); \
+  } while (0)
+// after a launch: its status
+#define OP_LAUNCHED()                                                                   \
+  do {                                                                                  \
+    hipError_t e_ = hipGetLastError();                                                  \
+    if (e_ != hipSuccess) return ssd::op_fail(SSD_E_DEVICE, hipGetErrorString(e_));     \
+  } while (0)
+
+inline bool op_dtype(int t) { return t == SSD_F32 || t == SSD_BF16; }
+inline int op_size(int t) { return t == SSD_F32 ? 4 : 2; }
+// whether [a, a + na) and [b, b + nb) share a byte
+inline bool op_overlap(const void* a, size_t na, const void* b, size_t nb) {
+  return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
+// bytes from a matrix's first element to past its last
+inline size_t op_span(int64_t rows, int64_t ld, int64_t cols, int size) {
+  return rows > 0 ? ((size_t)(rows - 1) * ld + cols) * size : 0;
+}
+
+struct bf16_t {
+  uint16_t bits;
+};
+
+__device__ __forceinline__ float op_ld(const float* p, size_t i) { return p[i]; }
+__device__ __forceinline__ float op_ld(const bf16_t* p, size_t i) {
+  return __uint_as_float((uint32_t)p[i].bits << 16);
+}
+// (to bfloat16: nearest, ties to even)
+__device__ __forceinline__ void op_st(float* p, size_t i, float v) { p[i] = v; }
+__device__ __forceinline__ void op_st(bf16_t* p, size_t i, float v) {
+  p[i].bits = __builtin_bit_cast(uint16_t, (__bf16)v);
+}
+
+}  // namespace ssd

@@ -1,0 +1,565 @@
+// Embedding rows and the table's gradient (ssd_embed, ssd_embed_grad of
+// ssd_ops.h).
+//
+//   out[n] = s W[tok_n],   dW[v] = s sum_{n: tok_n = v} g[n].
+//
+// The gradient sorts the positions by token (stable, so a token's terms are added
+// in a fixed order), then walks the merged sequence
+//   rows of token 0, end of 0, rows of token 1, end of 1, ...
+// in which a position is a row of g to read and an end a row of dW to write.  It is cut
+// into equal pieces whatever the tokens' frequencies; a piece that begins or
+// ends inside a token's rows leaves a partial sum, and a second kernel adds
+// these up.  Bound: memory (g read once, dW written once).
+#include "ops_common.h"
+
+namespace ssd {
+namespace {
+
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+// callers' rows begin at any element
+typedef unsigned u32x2_a2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
+
+// four columns of a row from column c on; the last ones of a row where fewer are left
+__device__ __forceinline__ f32x4 load4(const float* row, int c, int d) {
+  if (c + 4 <= d) return *(const f32x4_a4*)(row + c);
+  f32x4 r = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < 3; ++i)
+    if (c + i < d) r[i] = row[c + i];
+  return r;
+}
+__device__ __forceinline__ f32x4 load4(const bf16_t* row, int c, int d) {
+  if (c + 4 <= d) {
+    const u32x2 r = *(const u32x2_a2*)(row + c);
+    return (f32x4){__uint_as_float(r[0] << 16), __uint_as_float(r[0] & 0xffff0000u), __uint_as_float(r[1] << 16),
+                   __uint_as_float(r[1] & 0xffff0000u)};
+  }
+  f32x4 r = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < 3; ++i)
+    if (c + i < d) r[i] = op_ld(row, c + i);
+  return r;
+}
+__device__ __forceinline__ void store4(float* row, int c, int d, f32x4 v) {
+  if (c + 4 <= d) {
+    *(f32x4_a4*)(row + c) = v;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      if (c + i < d) row[c + i] = v[i];
+  }
+}
+__device__ __forceinline__ void store4(bf16_t* row, int c, int d, f32x4 v) {
+  typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+  if (c + 4 <= d) {
+    *(u32x2_a2*)(row + c) = __builtin_bit_cast(u32x2, __builtin_convertvector(v, b4));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      if (c + i < d) op_st(row, c + i, v[i]);
+  }
+}
+
+// ---------------------------------------------------------------- lookup
+
+// a thread per four columns of a row
+template <typename T, typename O>
+__global__ __launch_bounds__(256) void embed_rows_kernel(const int* __restrict__ tokens, int64_t quads, int per,
+                                                         const T* __restrict__ table, int64_t ld_table, int V, int d,
+                                                         float scale, O* __restrict__ out, int64_t ld_out) {
+  const int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (q >= quads) return;
+  const int64_t n = q / per;
+  const int c = 4 * (int)(q - n * per), tok = tokens[n];
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  if (tok >= 0 && tok < V) v = scale * load4(table + (size_t)tok * ld_table, c, d);
+  store4(out + (size_t)n * ld_out, c, d, v);
+}
+
+// ---------------------------------------------------------------- sort by token
+
+// a token and its position; tokens outside the vocabulary sort last, as V
+struct Entry {
+  int key, pos;
+};
+
+__device__ __forceinline__ int key_of(int token, int V) { return token >= 0 && token < V ? token : V; }
+
+// Up to kRankMax positions: every position's rank is the number of those before
+// it in the order, counted by comparing all with all.  A workgroup ranks 64
+// positions (one per lane); its waves share out the others.
+constexpr int kRankMax = 8192, kRankThreads = 1024;
+__global__ __launch_bounds__(kRankThreads) void rank_kernel(const int* __restrict__ tokens, int N, int V,
+                                                            Entry* __restrict__ sorted) {
+  constexpr int W = kRankThreads / 64;
+  __shared__ __align__(16) int keys[kRankMax];
+  __shared__ int count[W][64];
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+  const int n4 = (N + 3) / 4;
+  for (int j = t; j < 4 * n4; j += kRankThreads) keys[j] = j < N ? key_of(tokens[j], V) : 0x7fffffff;
+  __syncthreads();
+  const int i0 = blockIdx.x * 64, i = i0 + lane, key = i < N ? keys[i] : 0;
+  const int per = (n4 + W - 1) / W, from = w * per, to = min(n4, from + per);
+  int c = 0;
+  for (int j4 = from; j4 < to; ++j4) {
+    const int4 k = ((const int4*)keys)[j4];
+    const int j = 4 * j4;
+    if (j + 4 <= i0) {  // all before this workgroup's
+      c += (k.x <= key) + (k.y <= key) + (k.z <= key) + (k.w <= key);
+    } else if (j >= i0 + 64) {
+      c += (k.x < key) + (k.y < key) + (k.z < key) + (k.w < key);
+    } else {
+      c += (k.x < key || (k.x == key && j < i)) + (k.y < key || (k.y == key && j + 1 < i)) +
+           (k.z < key || (k.z == key && j + 2 < i)) + (k.w < key || (k.w == key && j + 3 < i));
+    }
+  }
+  count[w][lane] = c;
+  __syncthreads();
+  if (w == 0 && i < N) {
+    int r = 0;
+#pragma unroll
+    for (int k = 0; k < W; ++k) r += count[k][lane];
+    sorted[r] = (Entry){key, i};
+  }
+}
+
+// More positions: a stable radix sort from the lowest digit up.  At most
+// kSortBlocks workgroups each own a run of positions; a pass counts every
+// run's digits, and a run's entries of digit x go behind all lower digits and
+// the earlier runs' x.  The counts of a later pass are taken while the pass before
+// it places its entries.
+constexpr int kDigitBits = 9, kBins = 1 << kDigitBits, kSortThreads = 1024, kSortBlocks = 256;
+
+// positions of a run: as few sub-tiles of 2 per thread as keep the runs within kSortBlocks
+constexpr int kSubTile = 2 * kSortThreads;
+inline int sort_run(int N) {
+  const int tiles = (N + kSubTile - 1) / kSubTile;
+  return kSubTile * ((tiles + kSortBlocks - 1) / kSortBlocks);
+}
+inline int sort_passes(int V) {  // keys 0 .. V
+  int bits = 1;
+  while (V >> bits) ++bits;
+  return (bits + kDigitBits - 1) / kDigitBits;
+}
+
+// counts of the first pass; clears those of the others
+__global__ __launch_bounds__(kSortThreads) void count_kernel(const int* __restrict__ tokens, int N, int V, int run,
+                                                             int passes, int* __restrict__ counts) {
+  __shared__ int bins[kBins];
+  const int t = threadIdx.x, b = blockIdx.x, blocks = gridDim.x;
+  if (t < kBins) bins[t] = 0;
+  __syncthreads();
+  const int to = min((int64_t)N, (int64_t)(b + 1) * run);
+  for (int j = b * run + t; j < to; j += kSortThreads) atomicAdd(&bins[key_of(tokens[j], V) & (kBins - 1)], 1);
+  __syncthreads();
+  if (t < kBins) {
+    counts[(size_t)b * kBins + t] = bins[t];
+    for (int p = 1; p < passes; ++p) counts[((size_t)p * blocks + b) * kBins + t] = 0;
+  }
+}
+
+// one pass: from the tokens (in == nullptr) or entries, to entries
+__global__ __launch_bounds__(kSortThreads) void place_kernel(const int* __restrict__ tokens,
+                                                             const Entry* __restrict__ in, int N, int V, int run,
+                                                             int pass, const int* __restrict__ counts,
+                                                             Entry* __restrict__ out, int* __restrict__ next_counts) {
+  constexpr int W = kSortThreads / 64;
+  __shared__ int base[kBins];       // where the run's next entry of a digit goes
+  __shared__ int cnt[W][kBins];     // a sub-tile's entries of a digit, by wave; then their offsets
+  __shared__ int wsum[kBins / 64];
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6, b = blockIdx.x, blocks = gridDim.x;
+  const int shift = pass * kDigitBits;
+  // base: all lower digits, then the earlier runs' entries of this one
+  int total = 0, before = 0;
+  if (t < kBins) {
+    for (int k = 0; k < blocks; ++k) {
+      const int c = counts[(size_t)k * kBins + t];
+      before += k < b ? c : 0;
+      total += c;
+    }
+    int s = total;  // inclusive over the wave
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int u = __shfl_up(s, o);
+      if (lane >= o) s += u;
+    }
+    if (lane == 63) wsum[w] = s;
+    base[t] = s - total + before;
+  }
+  __syncthreads();
+  if (t < kBins)
+    for (int k = 0; k < w; ++k) base[t] += wsum[k];
+  const int end = min((int64_t)N, (int64_t)(b + 1) * run);
+  for (int j0 = b * run; j0 < end; j0 += kSubTile) {
+    for (int k = t; k < W * kBins; k += kSortThreads) ((int*)cnt)[k] = 0;
+    __syncthreads();
+    // wave w has 2 x 64 consecutive positions; equal digits of a wave find each other by ballots
+    Entry e[2];
+    int rank[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const int j = j0 + w * 128 + r * 64 + lane;
+      const bool in_run = j < end;
+      if (in_run) e[r] = in ? in[j] : (Entry){key_of(tokens[j], V), j};
+      else e[r] = (Entry){0, 0};
+      const int dg = (e[r].key >> shift) & (kBins - 1);
+      unsigned long long same = __builtin_amdgcn_ballot_w64(in_run);
+#pragma unroll
+      for (int k = 0; k < kDigitBits; ++k) {
+        const unsigned long long m = __builtin_amdgcn_ballot_w64(dg >> k & 1);
+        same &= dg >> k & 1 ? m : ~m;
+      }
+      const int lower = __builtin_popcountll(same & ((1ull << lane) - 1));
+      rank[r] = cnt[w][dg] + lower;
+      __builtin_amdgcn_wave_barrier();
+      if (in_run && lower == 0) cnt[w][dg] += __builtin_popcountll(same);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();
+    if (t < kBins) {
+      int s = base[t];
+      for (int k = 0; k < W; ++k) {
+        const int c = cnt[k][t];
+        cnt[k][t] = s;
+        s += c;
+      }
+      base[t] = s;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const int j = j0 + w * 128 + r * 64 + lane;
+      if (j < end) {
+        const int to = cnt[w][(e[r].key >> shift) & (kBins - 1)] + rank[r];
+        out[to] = e[r];
+        if (next_counts)
+          atomicAdd(&next_counts[(size_t)(to / run) * kBins + ((e[r].key >> (shift + kDigitBits)) & (kBins - 1))], 1);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------- sums of the sorted rows
+
+struct GradArgs {
+  const Entry* sorted;
+  int N, V, d, items, pieces;  // items of the merged sequence per piece
+  const void* grad;
+  int64_t ld_grad;
+  void* dtable;
+  int64_t ld_table;
+  float scale;
+  float *head, *tail;  // [pieces][d] partial sums
+  int* open;           // [pieces]: the token whose earlier terms are in the pieces before and that ends here, or -1
+};
+
+// The merged sequence without the ends (accumulate): a piece is a run of entries.
+// With them (ACC false): entry j comes at j + key_j, as many ends before it as
+// there are lower tokens.  first(t): the entries before place t.
+template <bool ACC>
+__device__ __forceinline__ int first(const Entry* __restrict__ s, int N, int64_t t) {
+  if (ACC) return (int)min((int64_t)N, t);
+  int lo = 0, hi = N;  // the answer is in [lo, hi]
+  const int lane = threadIdx.x & 63;
+  while (lo < hi) {  // the wave looks at 64 places at a time
+    const int step = (hi - lo + 63) / 64, j = lo + lane * step;
+    const bool before = j < hi && (int64_t)s[j].key + j < t;
+    const int k = __builtin_popcountll(__builtin_amdgcn_ballot_w64(before));  // (a prefix of the lanes)
+    if (k == 0) return lo;
+    const int at = lo + (k - 1) * step;
+    hi = min(hi, at + step);
+    lo = at + 1;
+  }
+  return lo;
+}
+
+template <typename G, typename T, bool ACC>
+__global__ __launch_bounds__(1024) void embed_grad_kernel(GradArgs a) {
+  constexpr int U = 8;     // rows in flight
+  constexpr int L = 512;   // entries staged at a time
+  __shared__ Entry es[L];
+  const int g = blockIdx.x, c = 4 * (blockIdx.y * blockDim.x + threadIdx.x);
+  const int64_t t0 = (int64_t)g * a.items, t1 = min(t0 + a.items, ACC ? (int64_t)a.N : (int64_t)a.N + a.V);
+  const int i0 = __builtin_amdgcn_readfirstlane(first<ACC>(a.sorted, a.N, t0));
+  const int i1 = __builtin_amdgcn_readfirstlane(first<ACC>(a.sorted, a.N, t1));
+  const bool col = c < a.d;
+  const G* grad = (const G*)a.grad;
+  T* table = (T*)a.dtable;
+  // v: the token whose end comes next; v1: ends from it on lie in later pieces
+  int v = ACC ? (i0 < i1 ? a.sorted[i0].key : a.V) : (int)(t0 - i0);
+  int v1;
+  if (ACC) {  // the last entry's token ends here unless the next piece goes on with it
+    v1 = i0 < i1 ? a.sorted[i1 - 1].key + 1 : 0;
+    if (i0 < i1 && i1 < a.N && a.sorted[i1].key == v1 - 1) v1 -= 1;
+  } else {
+    v1 = (int)(t1 - i1);
+  }
+  v = __builtin_amdgcn_readfirstlane(v);
+  v1 = __builtin_amdgcn_readfirstlane(min(v1, a.V));
+  bool cont = i0 > 0 && v < a.V && a.sorted[i0 - 1].key == v;  // earlier terms of v lie in pieces before
+  int opened = -1;
+  int terms = 0;  // of v in this piece
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+
+  auto end = [&]() {  // the end of token v
+    if (cont) {
+      opened = v;
+      if (col) store4(a.head + (size_t)g * a.d, c, a.d, acc);
+    } else if (col && (!ACC || terms)) {
+      T* row = table + (size_t)v * a.ld_table;
+      f32x4 r = a.scale * acc;
+      if (ACC) r += load4(row, c, a.d);
+      store4(row, c, a.d, r);
+    }
+    cont = false;
+    terms = 0;
+    acc = (f32x4){0.f, 0.f, 0.f, 0.f};
+  };
+
+  for (int b0 = i0; b0 < i1; b0 += L) {
+    const int nb = min(L, i1 - b0);
+    __syncthreads();
+    for (int j = threadIdx.x; j < nb; j += blockDim.x) es[j] = a.sorted[b0 + j];
+    __syncthreads();
+    for (int j0 = 0; j0 < nb; j0 += U) {
+      f32x4 r[U];
+      int key[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int j = min(j0 + u, nb - 1);
+        key[u] = j0 + u < nb ? __builtin_amdgcn_readfirstlane(es[j].key) : a.V;
+        const int pos = __builtin_amdgcn_readfirstlane(es[j].pos);
+        r[u] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        if (col && key[u] < a.V) r[u] = load4(grad + (size_t)pos * a.ld_grad, c, a.d);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (key[u] >= a.V) continue;
+        if (ACC) {
+          if (key[u] != v) {
+            end();
+            v = key[u];
+          }
+        } else {
+          for (; v < key[u]; ++v) end();
+        }
+        acc += r[u];
+        ++terms;
+      }
+    }
+  }
+  if (ACC) {
+    if (v < v1) {
+      end();
+      v = v1;
+    }
+  } else {
+    for (; v < v1; ++v) end();
+  }
+  if (terms && col) store4(a.tail + (size_t)g * a.d, c, a.d, acc);
+  if (blockIdx.y == 0 && threadIdx.x == 0) a.open[g] = opened;
+}
+
+// adds up the partial sums of a token that ends in piece g and began before it
+template <typename T, bool ACC>
+__global__ __launch_bounds__(1024) void embed_join_kernel(GradArgs a) {
+  const int g = blockIdx.x, v = a.open[g];
+  if (v < 0) return;
+  int lo = 0, hi = a.N;  // the first entry of v
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (a.sorted[mid].key < v) lo = mid + 1;
+    else hi = mid;
+  }
+  const int from = (int)((ACC ? (int64_t)lo : (int64_t)lo + v) / a.items);
+  const int c = 4 * (blockIdx.y * blockDim.x + threadIdx.x);
+  if (c >= a.d) return;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int k = from; k < g; ++k) acc += load4(a.tail + (size_t)k * a.d, c, a.d);
+  acc += load4(a.head + (size_t)g * a.d, c, a.d);
+  T* row = (T*)a.dtable + (size_t)v * a.ld_table;
+  f32x4 r = a.scale * acc;
+  if (ACC) r += load4(row, c, a.d);
+  store4(row, c, a.d, r);
+}
+
+constexpr int kMaxPieces = 2048;
+
+// pieces of the merged sequence: 8 a CU, fewer where a piece would have under 16 places
+int grad_pieces(int64_t places) {
+  const int64_t p = (places + 15) / 16;
+  return (int)(p < 1 ? 1 : p > kMaxPieces ? kMaxPieces : p);
+}
+
+size_t round256(size_t x) { return (x + 255) / 256 * 256; }
+
+struct Layout {
+  size_t entries[2], counts, head, tail, open, bytes;
+  int pieces, blocks, run, passes;
+};
+Layout layout(int n, int vocab, int d) {
+  Layout l{};
+  size_t at = 0;
+  auto take = [&](size_t b) {
+    const size_t o = at;
+    at += round256(b);
+    return o;
+  };
+  l.pieces = grad_pieces((int64_t)n + vocab);  // (no fewer than without the ends)
+  l.entries[0] = take((size_t)n * sizeof(Entry));
+  if (n > kRankMax) {
+    l.run = sort_run(n);
+    l.blocks = (n + l.run - 1) / l.run;
+    l.passes = sort_passes(vocab);
+    l.entries[1] = take((size_t)n * sizeof(Entry));
+    l.counts = take((size_t)l.passes * l.blocks * kBins * 4);
+  }
+  l.head = take((size_t)l.pieces * d * 4);
+  l.tail = take((size_t)l.pieces * d * 4);
+  l.open = take((size_t)l.pieces * 4);
+  l.bytes = at;
+  return l;
+}
+
+template <typename G, typename T, bool ACC>
+void launch_grad(const GradArgs& a, hipStream_t s) {
+  // threads of four columns each: whole waves, at most 1024
+  const int quads = (a.d + 3) / 4, threads = quads >= 1024 ? 1024 : (quads + 63) / 64 * 64;
+  const dim3 grid(a.pieces, (quads + threads - 1) / threads);
+  embed_grad_kernel<G, T, ACC><<<grid, threads, 0, s>>>(a);
+  embed_join_kernel<T, ACC><<<grid, threads, 0, s>>>(a);
+}
+template <typename G, typename T>
+void launch_grad(const GradArgs& a, bool acc, hipStream_t s) {
+  if (acc) launch_grad<G, T, true>(a, s);
+  else launch_grad<G, T, false>(a, s);
+}
+template <typename G>
+void launch_grad(const GradArgs& a, int table_dtype, bool acc, hipStream_t s) {
+  if (table_dtype == SSD_F32) launch_grad<G, float>(a, acc, s);
+  else launch_grad<G, bf16_t>(a, acc, s);
+}
+
+ssd_status check(int32_t n, int32_t vocab, int32_t d) {
+  OP_REQUIRE(n >= 0 && n <= 1 << 24, SSD_E_INVALID_ARG, "n outside [0, 2^24]");
+  OP_REQUIRE(vocab >= 1 && vocab <= 1 << 24, SSD_E_INVALID_ARG, "vocab outside [1, 2^24]");
+  OP_REQUIRE(d >= 1 && d <= 65536, SSD_E_INVALID_ARG, "d outside [1, 65536]");
+  return SSD_OK;
+}
+
+template <typename T>
+void launch_embed_rows(int out_dtype, const int* tokens, int n, const void* table, int64_t ld_table, int V, int d,
+                       float scale, void* out, int64_t ld_out, hipStream_t s) {
+  const int per = (d + 3) / 4;
+  const int64_t quads = (int64_t)n * per;
+  const unsigned grid = (unsigned)((quads + 255) / 256);
+  if (out_dtype == SSD_F32)
+    embed_rows_kernel<<<grid, 256, 0, s>>>(tokens, quads, per, (const T*)table, ld_table, V, d, scale, (float*)out,
+                                           ld_out);
+  else
+    embed_rows_kernel<<<grid, 256, 0, s>>>(tokens, quads, per, (const T*)table, ld_table, V, d, scale, (bf16_t*)out,
+                                           ld_out);
+}
+
+}  // namespace
+}  // namespace ssd
+
+using namespace ssd;
+
+extern "C" ssd_status ssd_embed(ssd_dtype table_dtype, ssd_dtype out_dtype, const int32_t* tokens, int32_t n,
+                                const void* table, int64_t ld_table, int32_t vocab, int32_t d, float scale, void* out,
+                                int64_t ld_out, void* stream) {
+  OP_REQUIRE(op_dtype(table_dtype) && op_dtype(out_dtype), SSD_E_INVALID_ARG, "dtype must be SSD_F32 or SSD_BF16");
+  ssd_status st = check(n, vocab, d);
+  if (st != SSD_OK) return st;
+  OP_REQUIRE(ld_table >= d && ld_out >= d, SSD_E_INVALID_ARG, "a row stride is below d");
+  if (n == 0) return SSD_OK;
+  OP_REQUIRE(tokens && table && out, SSD_E_INVALID_ARG, "null argument");
+  OP_REQUIRE((uintptr_t)table % op_size(table_dtype) == 0 && (uintptr_t)out % op_size(out_dtype) == 0,
+             SSD_E_INVALID_ARG, "a pointer is not aligned to its type");
+  OP_REQUIRE(!op_overlap(table, op_span(vocab, ld_table, d, op_size(table_dtype)), out,
+                         op_span(n, ld_out, d, op_size(out_dtype))),
+             SSD_E_INVALID_ARG, "out overlaps the table");
+  if (table_dtype == SSD_F32)
+    launch_embed_rows<float>(out_dtype, tokens, n, table, ld_table, vocab, d, scale, out, ld_out, (hipStream_t)stream);
+  else
+    launch_embed_rows<bf16_t>(out_dtype, tokens, n, table, ld_table, vocab, d, scale, out, ld_out,
+                              (hipStream_t)stream);
+  OP_LAUNCHED();
+  return SSD_OK;
+}
+
+extern "C" ssd_status ssd_embed_grad_workspace(int32_t n, int32_t vocab, int32_t d, size_t* bytes) {
+  OP_REQUIRE(bytes, SSD_E_INVALID_ARG, "null argument");
+  ssd_status st = check(n, vocab, d);
+  if (st != SSD_OK) return st;
+  *bytes = layout(n, vocab, d).bytes;
+  return SSD_OK;
+}
+
+extern "C" ssd_status ssd_embed_grad(ssd_dtype grad_dtype, ssd_dtype table_dtype, const int32_t* tokens, int32_t n,
+                                     const void* grad, int64_t ld_grad, int32_t vocab, int32_t d, float scale,
+                                     int32_t accumulate, void* dtable, int64_t ld_table, void* workspace,
+                                     size_t workspace_bytes, void* stream) {
+  OP_REQUIRE(op_dtype(grad_dtype) && op_dtype(table_dtype), SSD_E_INVALID_ARG, "dtype must be SSD_F32 or SSD_BF16");
+  size_t need = 0;
+  ssd_status st = ssd_embed_grad_workspace(n, vocab, d, &need);
+  if (st != SSD_OK) return st;
+  OP_REQUIRE(ld_grad >= d && ld_table >= d, SSD_E_INVALID_ARG, "a row stride is below d");
+  OP_REQUIRE(dtable && workspace && (n == 0 || (tokens && grad)), SSD_E_INVALID_ARG, "null argument");
+  OP_REQUIRE((uintptr_t)grad % op_size(grad_dtype) == 0 && (uintptr_t)dtable % op_size(table_dtype) == 0,
+             SSD_E_INVALID_ARG, "a pointer is not aligned to its type");
+  OP_REQUIRE(workspace_bytes >= need && (uintptr_t)workspace % 16 == 0, SSD_E_CAPACITY,
+             "workspace below ssd_embed_grad_workspace's bytes or not 16-byte aligned");
+  OP_REQUIRE(!op_overlap(grad, op_span(n, ld_grad, d, op_size(grad_dtype)), dtable,
+                         op_span(vocab, ld_table, d, op_size(table_dtype))),
+             SSD_E_INVALID_ARG, "dtable overlaps grad");
+  if (n == 0 && accumulate) return SSD_OK;
+  const Layout l = layout(n, vocab, d);
+  char* ws = (char*)workspace;
+  hipStream_t s = (hipStream_t)stream;
+  Entry *sorted = (Entry*)(ws + l.entries[0]), *other = (Entry*)(ws + l.entries[1]);
+  if (n > kRankMax) {
+    int* counts = (int*)(ws + l.counts);
+    count_kernel<<<l.blocks, kSortThreads, 0, s>>>(tokens, n, vocab, l.run, l.passes, counts);
+    OP_LAUNCHED();
+    const size_t step = (size_t)l.blocks * kBins;
+    for (int p = 0; p < l.passes; ++p) {
+      Entry* to = (l.passes - p) & 1 ? sorted : other;  // (the last pass ends in sorted)
+      const Entry* from = p == 0 ? nullptr : to == sorted ? other : sorted;
+      place_kernel<<<l.blocks, kSortThreads, 0, s>>>(tokens, from, n, vocab, l.run, p, counts + p * step, to,
+                                                     p + 1 < l.passes ? counts + (p + 1) * step : nullptr);
+      OP_LAUNCHED();
+    }
+  } else if (n > 0) {
+    rank_kernel<<<(n + 63) / 64, kRankThreads, 0, s>>>(tokens, n, vocab, sorted);
+    OP_LAUNCHED();
+  }
+  const int64_t places = accumulate ? (int64_t)n : (int64_t)n + vocab;
+  GradArgs a{};
+  a.sorted = sorted;
+  a.N = n;
+  a.V = vocab;
+  a.d = d;
+  a.pieces = grad_pieces(places);
+  a.items = (int)((places + a.pieces - 1) / a.pieces);
+  a.pieces = (int)((places + a.items - 1) / a.items);
+  a.grad = grad;
+  a.ld_grad = ld_grad;
+  a.dtable = dtable;
+  a.ld_table = ld_table;
+  a.scale = scale;
+  a.head = (float*)(ws + l.head);
+  a.tail = (float*)(ws + l.tail);
+  a.open = (int*)(ws + l.open);
+  if (grad_dtype == SSD_F32) launch_grad<float>(a, table_dtype, accumulate != 0, s);
+  else launch_grad<bf16_t>(a, table_dtype, accumulate != 0, s);
+  OP_LAUNCHED();
+  return SSD_OK;
+}

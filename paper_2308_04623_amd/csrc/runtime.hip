@@ -17,6 +17,7 @@
 #include <vector>
 
 #include "../../include/ssd.h"
+#include "ops_common.h"
 #include "ssd_internal.h"
 
 using namespace ssd;
@@ -46,6 +47,17 @@ ssd_status fail(ssd_status st, const std::string& msg) {
 int round_up(int a, int b) { return (a + b - 1) / b * b; }
 
 }  // namespace
+
+namespace ssd {
+ssd_status op_fail(ssd_status st, const char* msg) noexcept {
+  try {
+    g_last_error = msg;
+  } catch (...) {  // (no memory for the message: the status still tells)
+    g_last_error.clear();
+  }
+  return st;
+}
+}  // namespace ssd
 
 struct ssd_model {
   ssd_config cfg;

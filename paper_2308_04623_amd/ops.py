@@ -1,0 +1,294 @@
+"""Operators for training a draft on its oracle (include/ssd_ops.h) on torch
+tensors: attention of a batch over a shared prompt, distillation from top
+logits, embedding rows and their table's gradient.
+
+As in ssd.py, the library does the work and PyTorch supplies device memory
+and streams.  Outputs and scratch come from torch's allocator on the stream of
+the call (the current one, or `stream`), so calls may run on any streams that
+are ordered with the tensors' own use.  Every function takes its outputs from
+the caller where `out` is given.  Arguments are checked, here for what a pointer
+no longer tells (devices, types, shapes) and in the library for the rest.
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes as C
+import math
+from typing import Optional
+
+import torch
+
+from . import ssd
+from .ssd import SSDError
+
+# every function include/ssd_ops.h declares
+EXPORTS = ("ssd_prefix_attn_workspace", "ssd_prefix_attn", "ssd_distill_forward", "ssd_distill_backward",
+           "ssd_distill_step", "ssd_embed", "ssd_embed_grad_workspace", "ssd_embed_grad")
+
+_DTYPES = {torch.float32: ssd.F32, torch.bfloat16: ssd.BF16}
+
+
+class _PrefixAttnDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_seq", C.c_int32), ("n_query", C.c_int32), ("n_head", C.c_int32),
+                ("n_kv_head", C.c_int32), ("head_dim", C.c_int32), ("prefix_len", C.c_int32),
+                ("own_rows", C.c_int32), ("scale", C.c_float)] + \
+               [(n, C.c_int64) for n in ("q_seq", "q_row", "q_head", "out_seq", "out_row", "out_head", "prefix_head",
+                                         "prefix_row", "own_seq", "own_head", "own_row")]
+
+
+_lib = None
+
+
+def _ops():
+    global _lib
+    if _lib is None:
+        L = ssd.lib()
+        i32, i64, f32, vp, sz = C.c_int32, C.c_int64, C.c_float, C.c_void_p, C.c_size_t
+        logits = [i32, vp, i64, i32, i32, vp, vp, i32]
+        sig = {
+            "ssd_prefix_attn_workspace": [C.POINTER(_PrefixAttnDesc), C.POINTER(sz)],
+            "ssd_prefix_attn": [C.POINTER(_PrefixAttnDesc)] + [vp] * 9 + [sz, vp],
+            "ssd_distill_forward": logits + [vp, f32, vp, vp, vp],
+            "ssd_distill_backward": logits + [vp, vp, f32, vp, i64, vp],
+            "ssd_distill_step": logits + [vp, f32, vp, vp, vp, i64, vp],
+            "ssd_embed": [i32, i32, vp, i32, vp, i64, i32, i32, f32, vp, i64, vp],
+            "ssd_embed_grad_workspace": [i32, i32, i32, C.POINTER(sz)],
+            "ssd_embed_grad": [i32, i32, vp, i32, vp, i64, i32, i32, f32, i32, vp, i64, vp, sz, vp],
+        }
+        for name, args in sig.items():
+            f = getattr(L, name)
+            f.argtypes = args
+            f.restype = C.c_int
+        _lib = L
+    return _lib
+
+
+def _refuse(what: str, why: str, status: int = ssd.E_INVALID_ARG):
+    raise SSDError(status, what, why)
+
+
+def _check(status: int, what: str):
+    if status != ssd.OK:
+        raise SSDError(status, what, _lib.ssd_last_error().decode())
+
+
+def _tensor(what, name, t, dtypes, dims, like=None):
+    """t is a device tensor of one of the dtypes with `dims` dimensions, on like's device."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        _refuse(what, f"{name} must be a tensor on the GPU")
+    if t.dtype not in dtypes:
+        _refuse(what, f"{name} must be {' or '.join(str(d) for d in dtypes)}, not {t.dtype}")
+    if t.dim() != dims:
+        _refuse(what, f"{name} must have {dims} dimensions, not {t.dim()}")
+    if like is not None and t.device != like.device:
+        _refuse(what, f"{name} is on {t.device}, not {like.device}")
+
+
+def _rows(what, name, t):
+    """The row stride of a matrix whose rows' elements lie side by side."""
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        _refuse(what, f"{name}'s last dimension must be contiguous")
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+
+
+def _vector(what, name, t, dtype, n, like):
+    _tensor(what, name, t, (dtype,), 1, like)
+    if t.shape[0] != n:
+        _refuse(what, f"{name} has {t.shape[0]} entries, not {n}")
+    if n > 1 and t.stride(0) != 1:
+        _refuse(what, f"{name} must be contiguous")
+
+
+@contextlib.contextmanager
+def _on(t, stream):
+    """The stream's handle, with t's device and the stream current (what is allocated inside belongs to it)."""
+    if stream is None:
+        if t.device.index == torch.cuda.current_device():
+            yield torch.cuda.current_stream().cuda_stream
+        else:
+            with torch.cuda.device(t.device):
+                yield torch.cuda.current_stream().cuda_stream
+    else:
+        with torch.cuda.stream(stream):
+            yield stream.cuda_stream
+
+
+# ---------------------------------------------------------------- attention
+
+def prefix_attention(q, k_prefix, v_prefix, k_own, v_own, own_len, scale: Optional[float] = None, out=None,
+                     return_lse: bool = False, stream=None):
+    """ssd_prefix_attn: attention of sequences that share a prefix.
+
+    q [B][T][H][D] (a sequence's last T positions); k_prefix, v_prefix
+    [G][P][D]; k_own, v_own [B][G][R][D]; own_len int32 [B].  float32 or
+    bfloat16, any strides that are multiples of 16 bytes with D contiguous (K and
+    V alike).  scale defaults to 1 / sqrt(D).  Returns out [B][T][H][D], or (out,
+    lse float32 [B][T][H])."""
+    what = "ssd_prefix_attn"
+    kinds = (torch.float32, torch.bfloat16)
+    _tensor(what, "q", q, kinds, 4)
+    for name, t, dims in (("k_prefix", k_prefix, 3), ("v_prefix", v_prefix, 3), ("k_own", k_own, 4),
+                          ("v_own", v_own, 4)):
+        _tensor(what, name, t, (q.dtype,), dims, q)
+    b, t, h, d = q.shape
+    g, p = k_prefix.shape[:2]
+    r = k_own.shape[2]
+    if k_prefix.shape != v_prefix.shape or k_prefix.shape[2] != d:
+        _refuse(what, f"k_prefix {tuple(k_prefix.shape)} and v_prefix {tuple(v_prefix.shape)} must be [G][P][{d}]")
+    if k_own.shape != v_own.shape or tuple(k_own.shape) != (b, g, r, d):
+        _refuse(what, f"k_own {tuple(k_own.shape)} and v_own {tuple(v_own.shape)} must be [{b}][{g}][R][{d}]")
+    if k_prefix.stride() != v_prefix.stride() or k_own.stride() != v_own.stride():
+        _refuse(what, "keys and values must have the same strides")
+    _vector(what, "own_len", own_len, torch.int32, b, q)
+    if out is not None:
+        _tensor(what, "out", out, (q.dtype,), 4, q)
+        if out.shape != q.shape:
+            _refuse(what, f"out {tuple(out.shape)} must be {tuple(q.shape)}")
+    for name, x in (("q", q), ("k_prefix", k_prefix), ("k_own", k_own), ("out", out)):
+        if x is not None and x.numel() and x.stride(-1) != 1:
+            _refuse(what, f"{name}'s last dimension must be contiguous")
+    lib = _ops()
+    with _on(q, stream) as s:
+        if out is None:
+            out = torch.empty((b, t, h, d), dtype=q.dtype, device=q.device)
+        lse = torch.empty((b, t, h), dtype=torch.float32, device=q.device) if return_lse else None
+        # (a dimension of one entry has no stride to speak of)
+        step = lambda x, i: x.stride(i) if x.shape[i] > 1 else 0  # noqa: E731
+        a = _PrefixAttnDesc(_DTYPES[q.dtype], b, t, h, g, d, p, r, 1.0 / math.sqrt(d) if scale is None else scale,
+                            step(q, 0), step(q, 1), step(q, 2), step(out, 0), step(out, 1), step(out, 2),
+                            step(k_prefix, 0), step(k_prefix, 1), step(k_own, 0), step(k_own, 1), step(k_own, 2))
+        need = C.c_size_t(0)
+        _check(lib.ssd_prefix_attn_workspace(C.byref(a), C.byref(need)), what)
+        work = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+        _check(lib.ssd_prefix_attn(C.byref(a), q.data_ptr(), k_prefix.data_ptr(), v_prefix.data_ptr(),
+                                   k_own.data_ptr(), v_own.data_ptr(), own_len.data_ptr(), out.data_ptr(),
+                                   lse.data_ptr() if lse is not None else None, work.data_ptr(), need.value, s), what)
+    return (out, lse) if return_lse else out
+
+
+# ---------------------------------------------------------------- distillation
+
+def _logits(what, logits, ids, vals, weight):
+    _tensor(what, "logits", logits, (torch.float32, torch.bfloat16), 2)
+    n, v = logits.shape
+    ld = _rows(what, "logits", logits)
+    _tensor(what, "ids", ids, (torch.int32,), 2, logits)
+    _tensor(what, "vals", vals, (torch.float32,), 2, logits)
+    if ids.shape != vals.shape or ids.shape[0] != n:
+        _refuse(what, f"ids {tuple(ids.shape)} and vals {tuple(vals.shape)} must be [{n}][k]")
+    if not ids.is_contiguous() or not vals.is_contiguous():
+        _refuse(what, "ids and vals must be contiguous")
+    if weight is not None:
+        _vector(what, "weight", weight, torch.float32, n, logits)
+    return [_DTYPES[logits.dtype], logits.data_ptr(), ld, n, v, ids.data_ptr(), vals.data_ptr(), ids.shape[1]]
+
+
+def _grad_out(what, logits, out):
+    if out is None:
+        return torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    _tensor(what, "out", out, (logits.dtype,), 2, logits)
+    if out.shape != logits.shape:
+        _refuse(what, f"out {tuple(out.shape)} must be {tuple(logits.shape)}")
+    return out
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
+def distill_forward(logits, ids, vals, weight=None, temperature: float = 1.0, stream=None):
+    """ssd_distill_forward: (loss float32 [N], lse float32 [N]) of logits
+    [N][V] (float32 or bfloat16) against the teacher's ids int32 [N][k] and
+    their logits vals float32 [N][k]; weight float32 [N] or None."""
+    what = "ssd_distill_forward"
+    args = _logits(what, logits, ids, vals, weight)
+    lib = _ops()
+    with _on(logits, stream) as s:
+        loss, lse = torch.empty((2, logits.shape[0]), dtype=torch.float32, device=logits.device).unbind(0)
+        _check(lib.ssd_distill_forward(*args, _ptr(weight), temperature, loss.data_ptr(), lse.data_ptr(), s), what)
+    return loss, lse
+
+
+def distill_backward(logits, ids, vals, lse, weight=None, temperature: float = 1.0, out=None, stream=None):
+    """ssd_distill_backward: the gradient [N][V] of sum(weight * divergence)
+    in the logits' type, from distill_forward's lse.  out may be logits."""
+    what = "ssd_distill_backward"
+    args = _logits(what, logits, ids, vals, weight)
+    _vector(what, "lse", lse, torch.float32, logits.shape[0], logits)
+    lib = _ops()
+    with _on(logits, stream) as s:
+        out = _grad_out(what, logits, out)
+        _check(lib.ssd_distill_backward(*args, lse.data_ptr(), _ptr(weight), temperature, out.data_ptr(),
+                                        _rows(what, "out", out), s), what)
+    return out
+
+
+def distill_step(logits, ids, vals, weight=None, temperature: float = 1.0, out=None, stream=None):
+    """ssd_distill_step: (loss, lse, gradient) in one call.  out may be logits."""
+    what = "ssd_distill_step"
+    args = _logits(what, logits, ids, vals, weight)
+    lib = _ops()
+    with _on(logits, stream) as s:
+        loss, lse = torch.empty((2, logits.shape[0]), dtype=torch.float32, device=logits.device).unbind(0)
+        out = _grad_out(what, logits, out)
+        _check(lib.ssd_distill_step(*args, _ptr(weight), temperature, loss.data_ptr(), lse.data_ptr(), out.data_ptr(),
+                                    _rows(what, "out", out), s), what)
+    return loss, lse, out
+
+
+# ---------------------------------------------------------------- embedding
+
+def embed(tokens, table, scale: float = 1.0, dtype=None, out=None, stream=None):
+    """ssd_embed: scale * table[tokens] as [N][d] of `dtype` (default: the
+    table's); tokens int32 [N], those outside the table give zeros."""
+    what = "ssd_embed"
+    kinds = (torch.float32, torch.bfloat16)
+    _tensor(what, "table", table, kinds, 2)
+    _tensor(what, "tokens", tokens, (torch.int32,), 1, table)
+    n = tokens.shape[0]
+    _vector(what, "tokens", tokens, torch.int32, n, table)
+    lib = _ops()
+    with _on(table, stream) as s:
+        if out is None:
+            dtype = dtype or table.dtype
+            if dtype not in kinds:
+                _refuse(what, f"dtype must be torch.float32 or torch.bfloat16, not {dtype}")
+            out = torch.empty((n, table.shape[1]), dtype=dtype, device=table.device)
+        _tensor(what, "out", out, kinds, 2, table)
+        if tuple(out.shape) != (n, table.shape[1]) or (dtype is not None and out.dtype != dtype):
+            _refuse(what, f"out must be [{n}][{table.shape[1]}] of the type asked for")
+        _check(lib.ssd_embed(_DTYPES[table.dtype], _DTYPES[out.dtype], tokens.data_ptr(), n, table.data_ptr(),
+                             _rows(what, "table", table), table.shape[0], table.shape[1], scale, out.data_ptr(),
+                             _rows(what, "out", out), s), what)
+    return out
+
+
+def embed_grad(tokens, grad, vocab: int, scale: float = 1.0, dtype=None, out=None, accumulate: bool = False,
+               stream=None):
+    """ssd_embed_grad: the gradient [vocab][d] of embed's table from grad
+    [N][d], of `dtype` (default: grad's).  accumulate adds to `out`."""
+    what = "ssd_embed_grad"
+    kinds = (torch.float32, torch.bfloat16)
+    _tensor(what, "grad", grad, kinds, 2)
+    n, d = grad.shape
+    _vector(what, "tokens", tokens, torch.int32, n, grad)
+    if accumulate and out is None:
+        _refuse(what, "accumulate needs out")
+    lib = _ops()
+    with _on(grad, stream) as s:
+        if out is None:
+            dtype = dtype or grad.dtype
+            if dtype not in kinds:
+                _refuse(what, f"dtype must be torch.float32 or torch.bfloat16, not {dtype}")
+        need = C.c_size_t(0)
+        _check(lib.ssd_embed_grad_workspace(n, vocab, d, C.byref(need)), what)
+        if out is None:
+            out = torch.empty((vocab, d), dtype=dtype, device=grad.device)
+        _tensor(what, "out", out, kinds, 2, grad)
+        if tuple(out.shape) != (vocab, d) or (dtype is not None and out.dtype != dtype):
+            _refuse(what, f"out must be [{vocab}][{d}] of the type asked for")
+        work = torch.empty(need.value, dtype=torch.uint8, device=grad.device)
+        _check(lib.ssd_embed_grad(_DTYPES[grad.dtype], _DTYPES[out.dtype], tokens.data_ptr(), n, grad.data_ptr(),
+                                  _rows(what, "grad", grad), vocab, d, scale, int(accumulate), out.data_ptr(),
+                                  _rows(what, "out", out), work.data_ptr(), need.value, s), what)
+    return out

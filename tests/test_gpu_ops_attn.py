@@ -1,0 +1,289 @@
+"""ops.prefix_attention against the definition in 64 bits on the host.
+
+Tolerances, set from the arithmetic: a score is a float32 sum of D products,
+so it is off by at most (D + 4) eps S with S the largest sum of |q_i k_i|
+scale; a softmax weight by twice that, relatively, and the weighted sum of the
+values (whose absolute maximum is vmax) by that times vmax, plus the few
+roundings of the sums and rescalings (64 eps).  bfloat16: the weights for the
+value product and the output are rounded to 8 bits each, 2^-9 vmax apiece."""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+EPS = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def env():
+    import torch
+    from paper_2308_04623_amd import ops
+    assert torch.cuda.is_available()
+    return torch, ops
+
+
+def make(torch, dtype, b, t, h, g, d, p, r, seed=0, lens=None):
+    gen = torch.Generator().manual_seed(seed)
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    rn = lambda *s: torch.randn(s, generator=gen).to(dt)  # noqa: E731
+    x = {"q": rn(b, t, h, d) * 2, "kp": rn(g, p, d), "vp": rn(g, p, d), "ko": rn(b, g, r, d), "vo": rn(b, g, r, d)}
+    if lens is None:
+        lens = torch.randint(0, r + 1, (b,), generator=gen).tolist()
+    return x, lens
+
+
+def reference(x, lens, scale=None):
+    """(out, lse, S, vmax) in 64 bits."""
+    q, kp, vp, ko, vo = (x[k].double().numpy() for k in ("q", "kp", "vp", "ko", "vo"))
+    b, t, h, d = q.shape
+    g, p, r = kp.shape[0], kp.shape[1], ko.shape[2]
+    scale = 1.0 / math.sqrt(d) if scale is None else scale
+    out, lse, big = np.zeros(q.shape), np.full((b, t, h), -np.inf), 0.0
+    vmax = 0.0
+    for i in range(b):
+        n = min(lens[i], r)
+        if lens[i] < 0:
+            continue
+        for j in range(t):
+            own = max(0, n - t + 1 + j)
+            for hh in range(h):
+                kv = hh // (h // g)
+                k = np.concatenate([kp[kv], ko[i, kv, :own]])
+                v = np.concatenate([vp[kv], vo[i, kv, :own]])
+                if not len(k):
+                    continue
+                s = k @ q[i, j, hh] * scale
+                m = s.max()
+                e = np.exp(s - m)
+                out[i, j, hh] = e @ v / e.sum()
+                lse[i, j, hh] = m + math.log(e.sum())
+                big = max(big, (np.abs(k) @ np.abs(q[i, j, hh])).max() * abs(scale))
+                vmax = max(vmax, np.abs(v).max())
+    return out, lse, big, vmax
+
+
+def tolerance(dtype, d, big, vmax):
+    tol = vmax * (2 * EPS * (d + 4) * big + 64 * EPS)
+    return tol + (2.0 ** -8 * vmax if dtype == "bf16" else 0.0)
+
+
+def check(torch, ops, dtype, x, lens, scale=None, put=None, **kw):
+    put = put or (lambda name, t: t.cuda())
+    dev = {k: put(k, v) for k, v in x.items()}
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    out, lse = ops.prefix_attention(dev["q"], dev["kp"], dev["vp"], dev["ko"], dev["vo"], n, scale=scale,
+                                    return_lse=True, **kw)
+    torch.cuda.synchronize()
+    ref, rl, big, vmax = reference(x, lens, scale)
+    d = x["q"].shape[3]
+    got = out.double().cpu().numpy()
+    assert np.isfinite(got).all()
+    assert np.abs(got - ref).max() <= tolerance(dtype, d, big, vmax)
+    got_l = lse.double().cpu().numpy()
+    assert np.array_equal(np.isneginf(got_l), np.isneginf(rl))
+    live = np.isfinite(rl)
+    if live.any():
+        assert np.abs(got_l[live] - rl[live]).max() <= (d + 4) * EPS * big + 64 * EPS * (1 + np.abs(rl[live]).max())
+    return out
+
+
+SHAPES = [
+    # b, t, h, g, d, p, r
+    (1, 1, 1, 1, 32, 1, 1), (1, 1, 4, 4, 32, 64, 24), (6, 1, 4, 4, 32, 65, 7), (3, 2, 6, 2, 64, 31, 33),
+    (5, 1, 20, 20, 64, 130, 40), (2, 5, 8, 2, 128, 257, 100), (17, 3, 4, 1, 64, 500, 9), (33, 1, 2, 2, 128, 129, 65),
+    (2, 64, 2, 1, 64, 96, 70), (70, 8, 4, 2, 32, 200, 12), (1, 1, 25, 25, 64, 3000, 5), (4, 17, 3, 3, 64, 1, 300),
+    (260, 1, 2, 1, 64, 513, 3)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_against_64_bits(env, dtype, shape):
+    torch, ops = env
+    print(dtype, shape, flush=True)
+    x, lens = make(torch, dtype, *shape)
+    check(torch, ops, dtype, x, lens)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("p", [1, 15, 16, 17, 32, 33, 63, 64, 127, 128, 129, 255, 1023])
+def test_prefix_lengths(env, dtype, p):
+    torch, ops = env
+    x, lens = make(torch, dtype, 3, 2, 4, 2, 64, p, 20, seed=p)
+    check(torch, ops, dtype, x, lens)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_no_prefix_no_own_rows_and_empty_slots(env, dtype):
+    torch, ops = env
+    # no prefix: sequences of length 0 see nothing, length 1 one row; a slot that is off
+    x, lens = make(torch, dtype, 6, 1, 4, 2, 64, 0, 40, lens=[0, 1, -1, 40, 41, 17])
+    out = check(torch, ops, dtype, x, lens)
+    assert not out[0].any() and not out[2].any()
+    # queries before a sequence's first row
+    x, lens = make(torch, dtype, 4, 5, 4, 2, 64, 0, 40, lens=[0, 2, 5, -3])
+    out = check(torch, ops, dtype, x, lens)
+    assert not out[1, :3].any() and out[1, 3:].any() and not out[3].any()
+    # no own rows at all
+    x, lens = make(torch, dtype, 4, 2, 4, 2, 64, 77, 0, lens=[0, 0, -1, 3])
+    check(torch, ops, dtype, x, lens)
+    # nothing to look at
+    x, lens = make(torch, dtype, 2, 2, 4, 2, 64, 0, 0, lens=[0, -1])
+    assert not check(torch, ops, dtype, x, lens).any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_that_are_not_seen_may_hold_anything(env, dtype):
+    torch, ops = env
+    x, lens = make(torch, dtype, 5, 3, 4, 2, 64, 70, 48, lens=[0, 1, 20, 47, -1])
+    want = check(torch, ops, dtype, x, lens)
+    for i, n in enumerate(lens):
+        for name in ("ko", "vo"):
+            x[name][i, :, max(0, n):] = float("nan") if name == "vo" else float("inf")
+
+    def put(name, t):  # and beyond the prefix, within the same buffer
+        if name in ("kp", "vp"):
+            room = torch.full((t.shape[0], t.shape[1] + 64, t.shape[2]), float("nan"), dtype=t.dtype, device="cuda")
+            room[:, :t.shape[1]] = t.cuda()
+            return room[:, :t.shape[1]]
+        return t.cuda()
+
+    dev = {k: put(k, v) for k, v in x.items()}
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    got = ops.prefix_attention(dev["q"], dev["kp"], dev["vp"], dev["ko"], dev["vo"], n)
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_values_of_infinite_size_stay_with_their_rows(env, dtype):
+    """A NaN value that is seen reaches its own sequence alone, a shared one every one."""
+    torch, ops = env
+    x, lens = make(torch, dtype, 4, 1, 2, 2, 64, 40, 30, lens=[10, 30, 1, -1])
+    x["vo"][1, 0, 5, 3] = float("nan")
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    run = lambda: ops.prefix_attention(*(x[k].cuda() for k in ("q", "kp", "vp", "ko", "vo")), n)  # noqa: E731
+    bad = torch.isnan(run())
+    assert bad[1, 0, 0, 3] and bad.sum() == 1
+    x["vp"][1, 7, 9] = float("nan")
+    bad = torch.isnan(run())
+    assert bad[:3, 0, 1, 9].all() and bad.sum() == 4
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_scores_far_apart_and_equal(env, dtype):
+    torch, ops = env
+    x, lens = make(torch, dtype, 3, 1, 2, 2, 64, 200, 50, lens=[50, 3, 0])
+    x["q"] = x["q"] * 20  # one key takes nearly everything
+    check(torch, ops, dtype, x, lens)
+    x["q"] = x["q"] * 0  # all alike
+    check(torch, ops, dtype, x, lens)
+    x, lens = make(torch, dtype, 3, 1, 2, 2, 64, 200, 50, lens=[50, 3, 0])
+    check(torch, ops, dtype, x, lens, scale=-0.3)
+    check(torch, ops, dtype, x, lens, scale=0.0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_strides(env, dtype):
+    """Keys and values with the tokens outside the heads, queries inside a wider
+    projection, an output inside a wider buffer."""
+    torch, ops = env
+    x, lens = make(torch, dtype, 5, 3, 4, 2, 64, 90, 21)
+
+    def put(name, t):
+        if name in ("kp", "vp"):
+            return t.cuda().transpose(0, 1).contiguous().transpose(0, 1)
+        if name in ("ko", "vo"):
+            return t.cuda().transpose(1, 2).contiguous().transpose(1, 2)
+        wide = torch.full((5, 3, 3 * 4 * 64), 7.0, dtype=t.dtype, device="cuda")
+        q = wide[:, :, :256].unflatten(2, (4, 64))
+        q.copy_(t)
+        return q
+
+    room = torch.full((5, 3, 6, 64), 3.0, dtype=x["q"].dtype, device="cuda")
+    check(torch, ops, dtype, x, lens, put=put, out=room[:, :, 1:5])
+    assert (room[:, :, 0] == 3).all() and (room[:, :, 5] == 3).all()
+    plain = check(torch, ops, dtype, x, lens)
+    assert torch.equal(plain, room[:, :, 1:5])
+
+
+def test_broadcast_queries(env):
+    torch, ops = env
+    x, lens = make(torch, "bf16", 4, 1, 4, 4, 64, 50, 16)
+    x["q"] = x["q"][:1].expand(4, 1, 4, 64)
+    check(torch, ops, "bf16", x, lens, put=lambda k, t: t[:1].cuda().expand(4, 1, 4, 64) if k == "q" else t.cuda())
+
+
+def test_offsets_past_32_bits(env):
+    """Rows 2^26 elements apart: the last ones lie 5 GB into the buffer."""
+    torch, ops = env
+    p, d, step = 45, 64, 1 << 26
+    x, lens = make(torch, "bf16", 3, 1, 2, 1, d, p, 4)
+    big = torch.empty(p * step, dtype=torch.bfloat16, device="cuda")
+    kp = big.as_strided((1, p, d), (0, step, 1))
+    vp = big[4096:].as_strided((1, p, d), (0, step, 1))
+
+    def put(name, t):
+        if name == "kp":
+            return kp.copy_(t)
+        return vp.copy_(t) if name == "vp" else t.cuda()
+
+    check(torch, ops, "bf16", x, lens, put=put)
+
+
+def test_a_sequence_does_not_depend_on_the_batch_around_it(env):
+    """Bitwise, from run to run and on another stream."""
+    torch, ops = env
+    x, lens = make(torch, "bf16", 9, 2, 4, 2, 64, 777, 64)
+    args = [x[k].cuda() for k in ("q", "kp", "vp", "ko", "vo")] + [torch.tensor(lens, dtype=torch.int32, device="cuda")]
+    a = ops.prefix_attention(*args)
+    for _ in range(3):
+        assert torch.equal(a, ops.prefix_attention(*args))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    b = ops.prefix_attention(*args, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(a, b)
+
+
+def test_captured_in_a_graph(env):
+    torch, ops = env
+    x, lens = make(torch, "bf16", 9, 1, 4, 2, 64, 777, 64)
+    args = [x[k].cuda() for k in ("q", "kp", "vp", "ko", "vo")] + [torch.tensor(lens, dtype=torch.int32, device="cuda")]
+    out = torch.empty_like(args[0])
+    ops.prefix_attention(*args, out=out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ops.prefix_attention(*args, out=out)
+    for i in range(3):
+        args[0].add_(0.25)
+        args[5].fill_(10 * i)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, ops.prefix_attention(*args))
+
+
+def test_refusals_of_the_binding(env):
+    torch, ops = env
+    from paper_2308_04623_amd.ssd import SSDError
+    x, lens = make(torch, "bf16", 2, 1, 4, 2, 64, 8, 4)
+    a = [x[k].cuda() for k in ("q", "kp", "vp", "ko", "vo")] + [torch.tensor(lens, dtype=torch.int32, device="cuda")]
+
+    def refused(i, t):
+        b = list(a)
+        b[i] = t
+        with pytest.raises(SSDError):
+            ops.prefix_attention(*b)
+
+    refused(0, a[0].float())
+    refused(0, a[0][0])
+    refused(1, a[1][:, :, :32])
+    refused(2, a[2][:, :4])
+    refused(3, a[3][:1])
+    refused(4, a[4].transpose(1, 2).contiguous().transpose(1, 2))
+    refused(5, a[5].long())
+    refused(5, a[5].cpu())
+    refused(0, torch.zeros(2, 1, 4, 128, dtype=torch.bfloat16, device="cuda")[..., ::2])
+    with pytest.raises(SSDError):
+        ops.prefix_attention(*a, out=torch.empty(2, 1, 4, 32, dtype=torch.bfloat16, device="cuda"))

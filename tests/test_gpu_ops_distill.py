@@ -1,0 +1,275 @@
+"""ops.distill_forward / _backward / _step against the definition in 64 bits.
+
+Tolerances, set from the arithmetic (eps = 2^-24): x = z / T carries |x| eps; an
+exponential of an argument up to |x| apart is then off by a few |x| eps
+relatively, the sum's error is that plus the roundings of a chain of at most
+some hundred additions.  So lse is off by at most eps (4 X + 256) with X the
+largest |x| of the row or its teacher, a probability relatively by the same,
+the loss by twice that per unit of weight; bfloat16 gradients are rounded once,
+2^-9 of themselves."""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+EPS = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def env():
+    import torch
+    from paper_2308_04623_amd import ops
+    assert torch.cuda.is_available()
+    return torch, ops
+
+
+def make(torch, dtype, n, v, k, seed=0):
+    gen = torch.Generator().manual_seed(seed)
+    z = (torch.randn(n, v, generator=gen) * 2.5).to(torch.float32 if dtype == "f32" else torch.bfloat16)
+    teacher = z.float() + torch.randn(n, v, generator=gen)
+    top = teacher.topk(min(k, v), 1)
+    w = torch.rand(n, generator=gen) + 0.25
+    return z, top.indices.int().contiguous(), top.values.contiguous(), w
+
+
+def reference(z, ids, vals, w, T, lse=None):
+    """loss, lse, gradient and X in 64 bits."""
+    z, ids = z.double().numpy(), ids.numpy()
+    vals, w = vals.double().numpy(), w.double().numpy()
+    n, v = z.shape
+    loss, ls, g, X = np.zeros(n), np.zeros(n), np.zeros((n, v)), np.zeros(n)
+    with np.errstate(all="ignore"):
+        for i in range(n):
+            x = z[i] / T
+            m = x.max()
+            l = m + math.log(np.exp(x - m).sum())
+            ls[i] = l
+            if lse is not None:
+                l = float(lse[i])
+            ok = (ids[i] >= 0) & (ids[i] < v) & ~np.isneginf(vals[i])
+            fin = x[np.isfinite(x)]
+            X[i] = max(np.abs(fin).max(initial=0.0), np.abs(vals[i][ok] / T).max(initial=0.0))
+            if w[i] == 0 or not ok.any():
+                continue
+            t = vals[i][ok] / T
+            p = np.exp(t - t.max())
+            p /= p.sum()
+            q = np.exp(x - l)
+            logq = x[ids[i][ok]] - l
+            live = p > 0
+            loss[i] = w[i] * (p[live] * (np.log(p[live]) - logq[live])).sum()
+            np.subtract.at(q, ids[i][ok], p)
+            g[i] = w[i] / T * q
+    return loss, ls, g, X
+
+
+def close(dtype, got, ref, tol):
+    assert (np.abs(got - ref) <= tol + (2.0 ** -8 * np.abs(ref) if dtype == "bf16" else 0.0) + 1e-37).all()
+
+
+def check(torch, ops, dtype, z, ids, vals, w, T=1.0, put=lambda t: t.cuda(), **kw):
+    dz, di, dv, dw = put(z), ids.cuda(), vals.cuda(), w.cuda()
+    rloss, rlse, rg, X = reference(z, ids, vals, w, T)
+    unit = EPS * (4 * X + 256)
+    wn = w.double().numpy()
+    loss, lse = ops.distill_forward(dz, di, dv, dw, temperature=T)
+    back = ops.distill_backward(dz, di, dv, lse, dw, temperature=T)
+    loss2, lse2, grad = ops.distill_step(dz, di, dv, dw, temperature=T, **kw)
+    torch.cuda.synchronize()
+    scale = (np.abs(wn) / T * unit)[:, None]
+    mag = np.abs(rg) * T / np.maximum(np.abs(wn), 1e-30)[:, None]
+    for i in range(z.shape[0]):  # p + q where p is
+        for j in range(ids.shape[1]):
+            if 0 <= ids[i, j] < z.shape[1]:
+                mag[i, ids[i, j]] += 2
+    for a, b in ((loss, lse), (loss2, lse2)):
+        assert (np.abs(a.double().cpu().numpy() - rloss) <= 2 * wn * unit).all()
+        assert (np.abs(b.double().cpu().numpy() - rlse) <= unit).all()
+    close(dtype, grad.double().cpu().numpy(), rg, scale * mag)
+    rb = reference(z, ids, vals, w, T, lse=lse.cpu())[2]
+    close(dtype, back.double().cpu().numpy(), rb, scale * mag)
+    return loss2, lse2, grad
+
+
+SHAPES = [(1, 1, 1), (1, 2, 1), (3, 7, 3), (15, 512, 8), (5, 511, 8), (4, 1000, 64), (3, 1025, 65), (2, 4097, 128),
+          (2, 8193, 16), (3, 16411, 50), (2, 50257, 8), (3, 65536, 8), (2, 65537, 50), (1, 131072, 100),
+          (2, 131075, 128), (1, 200003, 7), (700, 33, 2)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,v,k", SHAPES)
+def test_against_64_bits(env, dtype, n, v, k):
+    torch, ops = env
+    print(dtype, n, v, k, flush=True)
+    check(torch, ops, dtype, *make(torch, dtype, n, v, k, seed=v))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("v", [100, 20000, 131072])
+@pytest.mark.parametrize("T", [0.5, 3.0])
+def test_temperatures(env, dtype, v, T):
+    torch, ops = env
+    check(torch, ops, dtype, *make(torch, dtype, 4, v, 20), T=T)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("v", [300, 40001, 140000])
+def test_slots_and_rows_that_are_left_out(env, dtype, v):
+    torch, ops = env
+    z, ids, vals, w = make(torch, dtype, 7, v, 9)
+    w[0] = 0.0                        # a row of weight 0
+    ids[1] = -1                       # no token at all
+    vals[2] = -math.inf               # no probability at all
+    ids[3, 2], ids[3, 5] = v, -7      # outside the vocabulary
+    vals[4, 1] = -math.inf
+    ids[5] = ids[5, 0]                # one token in every slot
+    vals[6] = -300.0                  # far below, all alike
+    loss, lse, grad = check(torch, ops, dtype, z, ids, vals, w)
+    assert not loss[:3].any() and not grad[:3].any()
+    z[:3] = float("nan")              # such rows may hold anything
+    loss, lse, grad = ops.distill_step(z.cuda(), ids.cuda(), vals.cuda(), w.cuda())
+    assert not loss[:3].any() and not grad[:3].any()
+    assert torch.isfinite(grad).all() and torch.isfinite(loss).all()
+    back = ops.distill_backward(z.cuda(), ids.cuda(), vals.cuda(), lse, w.cuda())
+    assert not back[:3].any() and torch.isfinite(back).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("v", [300, 40001, 140000])
+def test_infinities(env, dtype, v):
+    torch, ops = env
+    z, ids, vals, w = make(torch, dtype, 4, v, 5)
+    keep = torch.zeros(4, v, dtype=torch.bool).scatter_(1, ids.long(), True)
+    z[0][~keep[0]] = -math.inf        # the student allows the teacher's tokens only
+    z[1][~keep[1]] = torch.finfo(z.dtype).min
+    loss, lse, grad = check(torch, ops, dtype, z, ids, vals, w)
+    assert not grad[0][~keep[0].cuda()].any()
+    z[2, ids[2, 1]] = -math.inf       # it forbids one of them
+    loss, _, grad = ops.distill_step(z.cuda(), ids.cuda(), vals.cuda(), w.cuda())
+    assert math.isinf(loss[2]) and loss[2] > 0 and torch.isfinite(grad[2]).all()
+    z[3, v // 2] = math.nan
+    loss, lse, grad = ops.distill_step(z.cuda(), ids.cuda(), vals.cuda(), w.cuda())
+    assert torch.isnan(loss[3]) and torch.isnan(lse[3]) and torch.isnan(grad[3]).all()
+    assert torch.isfinite(grad[:3]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_logits(env, dtype):
+    torch, ops = env
+    z, ids, vals, w = make(torch, dtype, 3, 5000, 8)
+    z[0] += 1e4
+    z[1] *= 30
+    check(torch, ops, dtype, z, ids, vals, w)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("v", [333, 50257, 131200])
+def test_strides_and_alignment(env, dtype, v):
+    """Rows at any element; what lies between them is left alone."""
+    torch, ops = env
+    z, ids, vals, w = make(torch, dtype, 4, v, 8)
+    for off in (0, 1, 3):
+        room = torch.full((4 * (v + 5) + off,), 7.0, dtype=z.dtype, device="cuda")
+        view = room[off:].view(4, v + 5)[:, :v]
+        view.copy_(z)
+        dest = torch.full((4 * (v + 9) + off,), 5.0, dtype=z.dtype, device="cuda")
+        dview = dest[off:].view(4, v + 9)[:, :v]
+        check(torch, ops, dtype, z, ids, vals, w, put=lambda t: view, out=dview)
+        assert (dest[off:].view(4, v + 9)[:, v:] == 5).all() and (dest[:off] == 5).all()
+        assert (room[off:].view(4, v + 5)[:, v:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("v", [90, 50257, 140001])
+def test_in_place(env, dtype, v):
+    torch, ops = env
+    z, ids, vals, w = (t.cuda() for t in make(torch, dtype, 5, v, 12))
+    loss, lse, grad = ops.distill_step(z, ids, vals, w)
+    back = ops.distill_backward(z, ids, vals, lse, w)
+    a, b = z.clone(), z.clone()
+    l2, s2, g2 = ops.distill_step(a, ids, vals, w, out=a)
+    assert g2 is a and torch.equal(a, grad) and torch.equal(l2, loss) and torch.equal(s2, lse)
+    ops.distill_backward(b, ids, vals, lse, w, out=b)
+    assert torch.equal(b, back)
+
+
+def test_without_weights_and_again(env):
+    torch, ops = env
+    z, ids, vals, w = (t.cuda() for t in make(torch, "f32", 6, 3001, 8))
+    a = ops.distill_step(z, ids, vals)
+    b = ops.distill_step(z, ids, vals, torch.ones_like(w))
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    c = ops.distill_step(z, ids, vals, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(x, y) for x, y in zip(a, c))
+    assert ops.distill_forward(z[:0], ids[:0], vals[:0])[0].shape == (0,)
+
+
+def test_gradient_against_differences(env):
+    """Central differences of the loss, step h: the loss is off by at most the
+    tolerance above (twice, over 2h), and the remainder is h^2 / 6 times the
+    third derivative of a log-sum-exp, at most 0.1 / T^3 w."""
+    torch, ops = env
+    v, k, T, h = 11, 4, 0.8, 2e-2
+    z, ids, vals, w = make(torch, "f32", 1, v, k)
+    loss, lse, grad = ops.distill_step(z.cuda(), ids.cuda(), vals.cuda(), w.cuda(), temperature=T)
+    up, down = z.repeat(v, 1) + h * torch.eye(v), z.repeat(v, 1) - h * torch.eye(v)
+    many = lambda t: t.repeat(v, *([1] * (t.dim() - 1))).cuda()  # noqa: E731
+    lu = ops.distill_forward(up.cuda(), many(ids), many(vals), many(w), temperature=T)[0].double()
+    ld = ops.distill_forward(down.cuda(), many(ids), many(vals), many(w), temperature=T)[0].double()
+    step = (up.double() - down.double()).diagonal().cuda()
+    X = max(float(z.abs().max()), float(vals.abs().max())) / T
+    tol = 2 * 2 * float(w[0]) * EPS * (4 * X + 256) / (2 * h) + h * h / 6 * 0.1 * float(w[0]) / T ** 3
+    assert float(((lu - ld) / step - grad[0].double()).abs().max()) <= tol
+
+
+def test_offsets_past_32_bits(env):
+    torch, ops = env
+    z, ids, vals, w = make(torch, "bf16", 3, 700, 5)
+    step = 1500000000
+    room = torch.empty(2 * step + 700, dtype=torch.bfloat16, device="cuda")
+    view = room.as_strided((3, 700), (step, 1))
+    view.copy_(z)
+    check(torch, ops, "bf16", z, ids, vals, w, put=lambda t: view)
+    a = ops.distill_step(z.cuda(), ids.cuda(), vals.cuda(), w.cuda())[2]
+    ops.distill_step(view, ids.cuda(), vals.cuda(), w.cuda(), out=view)
+    assert torch.equal(view, a)
+
+
+def test_captured_in_a_graph(env):
+    torch, ops = env
+    z, ids, vals, w = (t.cuda() for t in make(torch, "bf16", 40, 5001, 8))
+    out = torch.empty_like(z)
+    ops.distill_step(z, ids, vals, w, out=out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        loss, lse, _ = ops.distill_step(z, ids, vals, w, out=out)
+    for _ in range(3):
+        z.mul_(0.9)
+        graph.replay()
+        torch.cuda.synchronize()
+        a = ops.distill_step(z, ids, vals, w)
+        assert torch.equal(a[0], loss) and torch.equal(a[1], lse) and torch.equal(a[2], out)
+
+
+def test_refusals_of_the_binding(env):
+    torch, ops = env
+    from paper_2308_04623_amd.ssd import SSDError
+    z, ids, vals, w = (t.cuda() for t in make(torch, "f32", 4, 100, 6))
+    for bad in ((z.half(), ids, vals, w), (z, ids.long(), vals, w), (z, ids, vals.double(), w), (z, ids[:3], vals, w),
+                (z, ids, vals, w[:3]), (z, ids, vals, w.cpu()), (z.t(), ids, vals, w), (z[0], ids, vals, w),
+                (z, ids[:, ::2], vals[:, ::2], w)):
+        with pytest.raises(SSDError):
+            ops.distill_forward(*bad)
+    with pytest.raises(SSDError):
+        ops.distill_step(z, ids, vals, w, temperature=0.0)
+    with pytest.raises(SSDError):
+        ops.distill_step(z, ids, vals, w, out=z.bfloat16())
+    both = torch.zeros(5, 100, device="cuda")
+    with pytest.raises(SSDError):
+        ops.distill_step(both[:4], ids, vals, w, out=both[1:])

@@ -1,0 +1,258 @@
+"""ops.embed and ops.embed_grad against the definition in 64 bits.
+
+Tolerances, set from the arithmetic (eps = 2^-24): a lookup is one product; a
+row of the gradient is a float32 sum of c terms in some order, off by at most
+c eps times the sum of their magnitudes, times the scale; bfloat16 results are
+rounded once, 2^-9 of themselves."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+EPS = 2.0 ** -24
+KINDS = [("f32", "f32"), ("bf16", "f32"), ("f32", "bf16"), ("bf16", "bf16")]
+
+
+@pytest.fixture(scope="module")
+def env():
+    import torch
+    from paper_2308_04623_amd import ops
+    assert torch.cuda.is_available()
+    return torch, ops
+
+
+def dt(torch, name):
+    return torch.float32 if name == "f32" else torch.bfloat16
+
+
+def draw_tokens(gen, torch, n, v, kind):
+    if kind == "even":
+        return torch.randint(0, v, (n,), generator=gen, dtype=torch.int32)
+    if kind == "one":
+        return torch.full((n,), v // 2, dtype=torch.int32)
+    if kind == "few":
+        return (torch.randint(0, 3, (n,), generator=gen) * (v - 1) // 2).int()
+    t = (torch.exp(torch.rand(n, generator=gen) * float(np.log(v + 1.0))).long() - 1).clamp(0, v - 1).int()
+    t[torch.rand(n, generator=gen) < 0.1] = -1
+    if n > 2:
+        t[n // 2], t[n - 1] = v, 2 ** 31 - 1
+        t[0] = -2 ** 31
+    return t
+
+
+@pytest.mark.parametrize("td,od", KINDS)
+@pytest.mark.parametrize("n,v,d", [(1, 1, 1), (5, 7, 3), (32, 512, 128), (33, 1000, 1280), (3, 50, 1027), (260, 9, 66)])
+def test_lookup(env, td, od, n, v, d):
+    torch, ops = env
+    gen = torch.Generator().manual_seed(n)
+    table, tokens = torch.randn(v, d, generator=gen).to(dt(torch, td)), draw_tokens(gen, torch, n, v, "zipf")
+    got = ops.embed(tokens.cuda(), table.cuda(), scale=1.7, dtype=dt(torch, od)).double().cpu()
+    ok = (tokens >= 0) & (tokens < v)
+    ref = torch.zeros(n, d, dtype=torch.float64)
+    ref[ok] = table.double()[tokens[ok].long()] * float(np.float32(1.7))
+    assert ((got - ref).abs() <= ref.abs() * (2 * EPS + (2.0 ** -8 if od == "bf16" else 0))).all()
+
+
+def grad_reference(tokens, grad, v, scale, base=None):
+    """(gradient, its tolerance before the last rounding) in 64 bits."""
+    g, t = grad.double().numpy() * float(np.float32(scale)), tokens.numpy()
+    ok = (t >= 0) & (t < v)
+    ref, mag = np.zeros((v, g.shape[1])), np.zeros((v, g.shape[1]))
+    np.add.at(ref, t[ok], g[ok])
+    np.add.at(mag, t[ok], np.abs(g[ok]))
+    c = np.bincount(t[ok], minlength=v)[:, None]
+    if base is not None:
+        ref += base
+        mag += np.abs(base)
+    return ref, (c + 4) * EPS * mag
+
+
+def check_grad(torch, ops, gd, td, tokens, grad, v, scale=0.6):
+    got = ops.embed_grad(tokens.cuda(), grad.cuda(), v, scale=scale, dtype=dt(torch, td)).double().cpu().numpy()
+    ref, tol = grad_reference(tokens, grad, v, scale)
+    assert (np.abs(got - ref) <= tol + (2.0 ** -8 * np.abs(ref) if td == "bf16" else 0)).all()
+    base = torch.randn(v, grad.shape[1], generator=torch.Generator().manual_seed(3)).to(dt(torch, td))
+    out = base.cuda()
+    assert ops.embed_grad(tokens.cuda(), grad.cuda(), v, scale=scale, out=out, accumulate=True) is out
+    ref, tol = grad_reference(tokens, grad, v, scale, base.double().numpy())
+    got = out.double().cpu()
+    assert (np.abs(got.numpy() - ref) <= tol + (2.0 ** -8 * np.abs(ref) if td == "bf16" else 0)).all()
+    absent = torch.ones(v, dtype=torch.bool)
+    absent[tokens[(tokens >= 0) & (tokens < v)].long()] = False
+    assert torch.equal(out.cpu()[absent], base[absent])
+
+
+@pytest.mark.parametrize("gd,td", KINDS)
+@pytest.mark.parametrize("n,v,d", [(1, 1, 1), (1, 40, 16), (2, 3, 5), (64, 64, 64), (65, 1000, 130), (200, 512, 128),
+                                   (1000, 100, 36), (3000, 5000, 20), (9000, 700, 12), (20000, 50257, 8)])
+@pytest.mark.parametrize("kind", ["even", "zipf"])
+def test_gradient(env, gd, td, n, v, d, kind):
+    torch, ops = env
+    print(gd, td, n, v, d, kind, flush=True)
+    gen = torch.Generator().manual_seed(n + d)
+    check_grad(torch, ops, gd, td, draw_tokens(gen, torch, n, v, kind),
+               torch.randn(n, d, generator=gen).to(dt(torch, gd)), v)
+
+
+@pytest.mark.parametrize("kind", ["one", "few"])
+@pytest.mark.parametrize("n,v,d", [(70, 9, 33), (5000, 300, 64), (12000, 50257, 16)])
+def test_gradient_of_very_frequent_tokens(env, kind, n, v, d):
+    torch, ops = env
+    gen = torch.Generator().manual_seed(n)
+    check_grad(torch, ops, "f32", "f32", draw_tokens(gen, torch, n, v, kind), torch.randn(n, d, generator=gen), v)
+
+
+@pytest.mark.parametrize("d", [1, 2, 4, 63, 64, 255, 256, 257, 1024, 1280, 1600, 4100, 5000])
+def test_gradient_widths(env, d):
+    torch, ops = env
+    gen = torch.Generator().manual_seed(d)
+    for gd, td in KINDS:
+        check_grad(torch, ops, gd, td, draw_tokens(gen, torch, 150, 60, "zipf"),
+                   torch.randn(150, d, generator=gen).to(dt(torch, gd)), 60)
+
+
+def test_wide_vocabulary(env):
+    """More than 2^18 tokens, and the largest the call takes."""
+    torch, ops = env
+    gen = torch.Generator().manual_seed(1)
+    for n, v in ((5000, 300000), (20000, 1 << 24)):
+        tokens = draw_tokens(gen, torch, n, v, "even")
+        tokens[::7] = v - 1
+        grad = torch.randn(n, 2, generator=gen)
+        got = ops.embed_grad(tokens.cuda(), grad.cuda(), v).double().cpu().numpy()
+        ref, tol = grad_reference(tokens, grad, v, 1.0)
+        assert (np.abs(got - ref) <= tol).all()
+
+
+def test_no_tokens(env):
+    torch, ops = env
+    none, grad = torch.zeros(0, dtype=torch.int32, device="cuda"), torch.zeros(0, 24, device="cuda")
+    assert not ops.embed_grad(none, grad, 100).any()
+    out = torch.randn(100, 24, device="cuda")
+    keep = out.clone()
+    ops.embed_grad(none, grad, 100, out=out, accumulate=True)
+    assert torch.equal(out, keep)
+    assert ops.embed(none, out).shape == (0, 24)
+    # padding alone
+    pad = torch.full((50,), -1, dtype=torch.int32, device="cuda")
+    assert not ops.embed_grad(pad, torch.randn(50, 24, device="cuda"), 100).any()
+    assert not ops.embed(pad, out).any()
+
+
+def test_padding_may_hold_anything(env):
+    torch, ops = env
+    gen = torch.Generator().manual_seed(5)
+    tokens, grad = draw_tokens(gen, torch, 400, 90, "zipf").cuda(), torch.randn(400, 32, generator=gen).cuda()
+    want = ops.embed_grad(tokens, grad, 90)
+    grad[(tokens < 0) | (tokens >= 90)] = float("nan")
+    assert torch.equal(ops.embed_grad(tokens, grad, 90), want)
+
+
+@pytest.mark.parametrize("gd,td", KINDS)
+def test_strides_and_alignment(env, gd, td):
+    """Rows at any element; what lies between them is left alone."""
+    torch, ops = env
+    gen = torch.Generator().manual_seed(9)
+    for d, pad, off in ((64, 1, 0), (64, 8, 1), (61, 3, 2), (128, 16, 0)):
+        tokens = draw_tokens(gen, torch, 300, 80, "zipf")
+        grad = torch.randn(300, d, generator=gen).to(dt(torch, gd))
+        want = ops.embed_grad(tokens.cuda(), grad.cuda(), 80, dtype=dt(torch, td))
+        room = torch.full((300 * (d + pad) + off,), 9.0, dtype=grad.dtype, device="cuda")
+        g = room[off:].view(300, d + pad)[:, :d]
+        g.copy_(grad)
+        dest = torch.full((80 * (d + pad) + off,), 5.0, dtype=dt(torch, td), device="cuda")
+        out = dest[off:].view(80, d + pad)[:, :d]
+        ops.embed_grad(tokens.cuda(), g, 80, out=out)
+        assert torch.equal(out, want) and (dest[:off] == 5).all() and (dest[off:].view(80, d + pad)[:, d:] == 5).all()
+        rows = ops.embed(tokens.cuda(), out, scale=2.0, dtype=torch.float32)
+        assert torch.equal(rows, ops.embed(tokens.cuda(), want, scale=2.0, dtype=torch.float32))
+        back = room[off:].view(300, d + pad)[:, :d]
+        back.fill_(0)
+        ops.embed(tokens.cuda(), want, out=back)
+        assert torch.equal(back, ops.embed(tokens.cuda(), want, dtype=back.dtype))
+
+
+def test_the_gradient_is_the_lookups_adjoint_and_difference(env):
+    """<embed(W), G> = <W, embed_grad(G)>, and a step of W along E changes
+    <embed(W), G> by <E, embed_grad(G)> (both are linear in W)."""
+    torch, ops = env
+    gen = torch.Generator().manual_seed(2)
+    tokens = draw_tokens(gen, torch, 500, 70, "zipf").cuda()
+    w, e = (torch.randn(70, 48, generator=gen).cuda() for _ in range(2))
+    g = torch.randn(500, 48, generator=gen).cuda()
+    grad = ops.embed_grad(tokens, g, 70, scale=1.3)
+    val = lambda t: float((ops.embed(tokens, t, scale=1.3).double() * g.double()).sum())  # noqa: E731
+    size = float((ops.embed(tokens, w.abs(), scale=1.3).double() * g.double().abs()).sum())
+    assert abs(val(w) - float((w.double() * grad.double()).sum())) <= 600 * EPS * size
+    size += float((ops.embed(tokens, e.abs(), scale=1.3).double() * g.double().abs()).sum())
+    assert abs(val(w + e) - val(w) - float((e.double() * grad.double()).sum())) <= 1200 * EPS * size
+
+
+def test_the_same_bits_again_and_on_another_stream(env):
+    torch, ops = env
+    gen = torch.Generator().manual_seed(4)
+    tokens, grad = draw_tokens(gen, torch, 30000, 2000, "zipf").cuda(), torch.randn(30000, 64, generator=gen).cuda()
+    a = ops.embed_grad(tokens, grad, 2000)
+    for _ in range(4):
+        assert torch.equal(a, ops.embed_grad(tokens, grad, 2000))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    b = ops.embed_grad(tokens, grad, 2000, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(a, b)
+
+
+def test_offsets_past_32_bits(env):
+    torch, ops = env
+    gen = torch.Generator().manual_seed(6)
+    step, d = 1 << 28, 40
+    tokens, grad = draw_tokens(gen, torch, 9, 11, "even"), torch.randn(9, d, generator=gen)
+    room = torch.empty(10 * step + d, device="cuda")
+    g, out = room.as_strided((9, d), (step, 1)), room[4096:].as_strided((10, d), (step, 1))
+    g.copy_(grad)
+    tokens = tokens.clamp(max=9)
+    want = ops.embed_grad(tokens.cuda(), grad.cuda(), 10)
+    got = torch.empty(10 * step, device="cuda").as_strided((10, d), (step, 1))
+    ops.embed_grad(tokens.cuda(), g, 10, out=got)
+    assert torch.equal(got, want)
+    out.copy_(want)
+    assert torch.equal(ops.embed(tokens.cuda(), out), ops.embed(tokens.cuda(), want))
+
+
+def test_captured_in_a_graph(env):
+    torch, ops = env
+    gen = torch.Generator().manual_seed(8)
+    for n in (300, 20000):
+        tokens, grad = draw_tokens(gen, torch, n, 900, "zipf").cuda(), torch.randn(n, 32, generator=gen).cuda()
+        out = torch.empty(900, 32, device="cuda")
+        ops.embed_grad(tokens, grad, 900, out=out)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            ops.embed_grad(tokens, grad, 900, out=out)
+        for i in range(3):
+            tokens.copy_(torch.roll(tokens, 17))
+            out.fill_(float("nan"))
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, ops.embed_grad(tokens, grad, 900))
+
+
+def test_refusals_of_the_binding(env):
+    torch, ops = env
+    from paper_2308_04623_amd.ssd import SSDError
+    tokens, grad = torch.zeros(4, dtype=torch.int32, device="cuda"), torch.zeros(4, 8, device="cuda")
+    for bad in ((tokens.long(), grad, 9), (tokens[:3], grad, 9), (tokens, grad.half(), 9), (tokens, grad.t(), 9),
+                (tokens, grad, 0), (tokens.cpu(), grad, 9)):
+        with pytest.raises(SSDError):
+            ops.embed_grad(*bad)
+    with pytest.raises(SSDError):
+        ops.embed_grad(tokens, grad, 9, accumulate=True)
+    with pytest.raises(SSDError):
+        ops.embed_grad(tokens, grad, 9, out=torch.zeros(8, 8, device="cuda"))
+    with pytest.raises(SSDError):
+        ops.embed_grad(tokens, grad, 9, dtype=torch.float16)
+    with pytest.raises(SSDError):
+        ops.embed(tokens, grad, dtype=torch.float64)
+    with pytest.raises(SSDError):
+        ops.embed(tokens, grad, out=torch.zeros(4, 9, device="cuda"))

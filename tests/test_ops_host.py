@@ -1,0 +1,142 @@
+"""The operators of include/ssd_ops.h without a GPU: exports, workspace sizes
+and the refusals of the C entry points (every check runs before anything is
+enqueued, so none of these calls reaches a device)."""
+import ctypes as C
+import os
+import re
+
+import pytest
+
+from paper_2308_04623_amd import ops, ssd
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+BUF = 1 << 20  # stands for an aligned device address
+
+
+def _desc(**kw):
+    v = dict(dtype=ssd.BF16, n_seq=2, n_query=3, n_head=8, n_kv_head=4, head_dim=64, prefix_len=100, own_rows=16,
+             scale=0.125, q_seq=3 * 512, q_row=512, q_head=64, out_seq=3 * 512, out_row=512, out_head=64,
+             prefix_head=6400, prefix_row=64, own_seq=4096, own_head=1024, own_row=64)
+    v.update(kw)
+    return ops._PrefixAttnDesc(**v)
+
+
+def _attn(d, q=BUF, kp=BUF, vp=BUF, ko=BUF, vo=BUF, lens=BUF, out=8 * BUF, work=16 * BUF, size=0):
+    return ops._ops().ssd_prefix_attn(C.byref(d), q, kp, vp, ko, vo, lens, out, None, work, size, None)
+
+
+def test_library_exports_every_declared_operator():
+    txt = open(os.path.join(ROOT, "include", "ssd_ops.h")).read()
+    names = sorted(set(re.findall(r"\b(ssd_[a-z_0-9]+)\s*\(", re.sub(r"/\*.*?\*/", "", txt, flags=re.S))))
+    assert names == sorted(ops.EXPORTS)
+    for n in names:
+        assert hasattr(ops._ops(), n), n
+
+
+def test_prefix_attn_workspace_grows_with_the_call():
+    L = ops._ops()
+    small, large = C.c_size_t(0), C.c_size_t(0)
+    assert L.ssd_prefix_attn_workspace(C.byref(_desc()), C.byref(small)) == ssd.OK and small.value > 0
+    assert L.ssd_prefix_attn_workspace(C.byref(_desc(n_seq=64, prefix_len=100000)), C.byref(large)) == ssd.OK
+    assert large.value >= small.value
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dtype=2), ssd.E_INVALID_ARG), (dict(head_dim=48), ssd.E_UNSUPPORTED),
+    (dict(head_dim=256), ssd.E_UNSUPPORTED), (dict(n_seq=0), ssd.E_INVALID_ARG),
+    (dict(n_seq=4097), ssd.E_INVALID_ARG), (dict(n_query=0), ssd.E_INVALID_ARG),
+    (dict(n_query=65), ssd.E_INVALID_ARG), (dict(n_kv_head=3), ssd.E_INVALID_ARG),
+    (dict(n_kv_head=0), ssd.E_INVALID_ARG), (dict(n_kv_head=16), ssd.E_INVALID_ARG),
+    (dict(prefix_len=-1), ssd.E_INVALID_ARG), (dict(own_rows=1 << 30), ssd.E_INVALID_ARG),
+    (dict(scale=float("nan")), ssd.E_INVALID_ARG), (dict(scale=float("inf")), ssd.E_INVALID_ARG),
+    (dict(q_row=516), ssd.E_UNSUPPORTED), (dict(prefix_row=65), ssd.E_UNSUPPORTED),
+    (dict(own_row=-64), ssd.E_INVALID_ARG), (dict(out_head=0), ssd.E_INVALID_ARG),
+    (dict(out_head=32), ssd.E_INVALID_ARG)])
+def test_prefix_attn_refuses_shapes(kw, status):
+    assert _attn(_desc(**kw), size=1 << 40) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(q=None), ssd.E_INVALID_ARG), (dict(kp=None), ssd.E_INVALID_ARG), (dict(vo=None), ssd.E_INVALID_ARG),
+    (dict(lens=None), ssd.E_INVALID_ARG), (dict(out=None), ssd.E_INVALID_ARG), (dict(work=None), ssd.E_INVALID_ARG),
+    (dict(q=BUF + 8), ssd.E_UNSUPPORTED), (dict(vp=BUF + 2), ssd.E_UNSUPPORTED),
+    (dict(size=8), ssd.E_CAPACITY), (dict(work=BUF + 4), ssd.E_CAPACITY)])
+def test_prefix_attn_refuses_buffers(kw, status):
+    assert _attn(_desc(), **{"size": 1 << 40, **kw}) == status
+
+
+def _distill(which, **kw):
+    v = dict(dtype=ssd.F32, logits=BUF, ld=100, n=4, vocab=100, ids=BUF, vals=BUF, k=8, weight=None, t=1.0,
+             loss=BUF, lse=BUF, grad=8 * BUF, ld_d=100)
+    v.update(kw)
+    L = ops._ops()
+    head = [v[x] for x in ("dtype", "logits", "ld", "n", "vocab", "ids", "vals", "k")]
+    if which == "forward":
+        return L.ssd_distill_forward(*head, v["weight"], v["t"], v["loss"], v["lse"], None)
+    if which == "backward":
+        return L.ssd_distill_backward(*head, v["lse"], v["weight"], v["t"], v["grad"], v["ld_d"], None)
+    return L.ssd_distill_step(*head, v["weight"], v["t"], v["loss"], v["lse"], v["grad"], v["ld_d"], None)
+
+
+@pytest.mark.parametrize("which", ["forward", "backward", "step"])
+@pytest.mark.parametrize("kw", [dict(dtype=7), dict(n=-1), dict(vocab=0), dict(vocab=(1 << 24) + 1, ld=1 << 25),
+                                dict(k=0), dict(k=129), dict(t=0.0), dict(t=-1.0), dict(t=float("nan")),
+                                dict(t=float("inf")), dict(ld=99), dict(logits=None), dict(ids=None),
+                                dict(vals=None), dict(lse=None), dict(logits=BUF + 2)])
+def test_distill_refuses(which, kw):
+    assert _distill(which, **kw) == ssd.E_INVALID_ARG
+
+
+@pytest.mark.parametrize("which", ["backward", "step"])
+@pytest.mark.parametrize("kw", [dict(grad=None), dict(ld_d=99), dict(grad=8 * BUF + 1), dict(grad=BUF + 400),
+                                dict(grad=BUF, ld_d=101)])
+def test_distill_refuses_gradients(which, kw):
+    assert _distill(which, **kw) == ssd.E_INVALID_ARG
+
+
+def test_calls_over_no_rows_do_nothing():
+    for which in ("forward", "backward", "step"):
+        assert _distill(which, n=0, logits=None, ids=None, vals=None, loss=None, lse=None, grad=None) == ssd.OK
+    assert ops._ops().ssd_embed(ssd.F32, ssd.F32, None, 0, None, 8, 4, 8, 1.0, None, 8, None) == ssd.OK
+
+
+@pytest.mark.parametrize("kw", [dict(td=3), dict(od=-1), dict(n=-1), dict(vocab=0), dict(d=0), dict(d=65537),
+                                dict(ld=7), dict(ldo=7), dict(tokens=None), dict(table=None), dict(out=None),
+                                dict(table=BUF + 1), dict(out=BUF + 8)])
+def test_embed_refuses(kw):
+    v = dict(td=ssd.F32, od=ssd.F32, tokens=BUF, n=3, table=BUF, ld=8, vocab=10, d=8, out=8 * BUF, ldo=8)
+    v.update(kw)
+    assert ops._ops().ssd_embed(v["td"], v["od"], v["tokens"], v["n"], v["table"], v["ld"], v["vocab"], v["d"], 1.0,
+                                v["out"], v["ldo"], None) == ssd.E_INVALID_ARG
+
+
+@pytest.mark.parametrize("kw,status", [(dict(gd=5), ssd.E_INVALID_ARG), (dict(n=-1), ssd.E_INVALID_ARG),
+                                       (dict(n=(1 << 24) + 1), ssd.E_INVALID_ARG), (dict(vocab=0), ssd.E_INVALID_ARG),
+                                       (dict(d=0), ssd.E_INVALID_ARG), (dict(ldg=7), ssd.E_INVALID_ARG),
+                                       (dict(ldt=7), ssd.E_INVALID_ARG), (dict(tokens=None), ssd.E_INVALID_ARG),
+                                       (dict(grad=None), ssd.E_INVALID_ARG), (dict(out=None), ssd.E_INVALID_ARG),
+                                       (dict(work=None), ssd.E_INVALID_ARG), (dict(out=BUF + 16), ssd.E_INVALID_ARG),
+                                       (dict(out=8 * BUF + 1), ssd.E_INVALID_ARG), (dict(size=1), ssd.E_CAPACITY),
+                                       (dict(work=16 * BUF + 8), ssd.E_CAPACITY)])
+def test_embed_grad_refuses(kw, status):
+    v = dict(gd=ssd.F32, td=ssd.F32, tokens=BUF, n=3, grad=BUF, ldg=8, vocab=10, d=8, out=8 * BUF, ldt=8,
+             work=16 * BUF, size=1 << 40)
+    v.update(kw)
+    assert ops._ops().ssd_embed_grad(v["gd"], v["td"], v["tokens"], v["n"], v["grad"], v["ldg"], v["vocab"], v["d"],
+                                     1.0, 0, v["out"], v["ldt"], v["work"], v["size"], None) == status
+
+
+def test_refusals_carry_a_message():
+    assert _distill("step", k=200) == ssd.E_INVALID_ARG
+    assert b"128" in ops._ops().ssd_last_error()
+
+
+def test_the_binding_refuses_host_tensors():
+    torch = pytest.importorskip("torch")
+    x = torch.zeros(2, 8)
+    with pytest.raises(ssd.SSDError):
+        ops.distill_forward(x, torch.zeros(2, 1, dtype=torch.int32), torch.zeros(2, 1))
+    with pytest.raises(ssd.SSDError):
+        ops.embed(torch.zeros(2, dtype=torch.int32), x)
+    with pytest.raises(ssd.SSDError):
+        ops.embed_grad(torch.zeros(2, dtype=torch.int32), x, 4)
