@@ -7,7 +7,7 @@
 //   dz_i = w / T (exp(x_i - lse) - sum_{j: id_j = i} p_j).
 // Bound: memory.  The forward pass has to read the row, the step to read and to
 // write it.
-#include <type_traits>
+#include <limits.h>
 
 #include "ops_common.h"
 
@@ -15,9 +15,11 @@ namespace ssd {
 namespace {
 
 constexpr int kMaxSlots = 128;  // teacher slots of a row
+constexpr int kCUs = 256;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-// rows begin where the caller's stride puts them: at any element
+// for outputs that lie differently from the logits
 typedef unsigned u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
 
 template <typename T> struct Vec;  // 16 bytes of elements
@@ -46,35 +48,36 @@ template <> struct Vec<bf16_t> {
   }
 };
 
-// chunk c of a row (elements c E .. c E + E - 1); -infinity past its end
+// A row's body is its 16-byte chunks at multiples of 16 bytes; up to E - 1
+// elements lie before it and after it.  (Rows of an odd number of elements begin
+// anywhere.)  Thread t < 2 E also takes edge element t, the ones before the
+// body, then the ones after it.
 template <typename T>
-__device__ __forceinline__ u32x4 load_chunk(const T* row, int c, int V) {
-  constexpr int E = Vec<T>::E;
-  u32x4 r = {Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone};
-  const int at = c * E;
-  if (at + E <= V) {
-    r = *(const u32x4_a2*)(row + at);
-  } else if (at < V) {
-    float v[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = at + e < V ? op_ld(row, at + e) : -INFINITY;
-    r = Vec<T>::pack(v);
+struct Row {
+  static constexpr int E = Vec<T>::E;
+  int head, chunks, tail, V;
+  __device__ __forceinline__ Row(const T* row, int V_) : V(V_) {
+    head = min((int)((16 - (uintptr_t)row % 16) % 16 / sizeof(T)), V);
+    chunks = (V - head) / E;
+    tail = V - head - chunks * E;
   }
-  return r;
-}
-
-template <typename T>
-__device__ __forceinline__ void store_chunk(T* row, int c, int V, const float (&v)[Vec<T>::E]) {
-  constexpr int E = Vec<T>::E;
-  const int at = c * E;
-  if (at + E <= V) {
-    *(u32x4_a2*)(row + at) = Vec<T>::pack(v);
-  } else {
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-      if (at + e < V) op_st(row, at + e, v[e]);
+  // chunk c0 + thread; -infinity where there is none.  LAST: it is not read
+  // again, and need not stay in the caches.
+  template <bool LAST>
+  __device__ __forceinline__ u32x4 load(const T* row, int c0) const {
+    u32x4 r = {Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone, Vec<T>::kNone};
+    if (c0 + (int)threadIdx.x < chunks) {
+      const u32x4* at = (const u32x4*)((const char*)(row + head + (size_t)c0 * E) + 16u * threadIdx.x);
+      r = LAST ? __builtin_nontemporal_load(at) : *at;
+    }
+    return r;
   }
-}
+  // the index of edge element t, or -1
+  __device__ __forceinline__ int edge(int t) const {
+    if (t < E) return t < head ? t : -1;
+    return t - E < tail ? V - tail + t - E : -1;
+  }
+};
 
 __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
@@ -106,149 +109,353 @@ struct DistillArgs {
 struct Slots {
   int id[kMaxSlots];
   float p[kMaxSlots];
-  int live;  // whether the row counts
+  float sum[kMaxSlots];  // of the p of all slots that name this one's token, in the first of them; 0 in the others
+  float z[kMaxSlots];    // the token's logit
+  int live;              // whether the row counts
 };
 
-// By one wave; lane l has slots l and l + 64.  lp: their log p.
-__device__ __forceinline__ void teacher(const DistillArgs& a, int n, Slots& s, float (&lp)[2]) {
-  const int lane = threadIdx.x & 63;
+// Lane l of the first wave has slots l and l + 64: their tokens (-1: left out),
+// the teacher's logits and the student's, and log p.
+struct Mine {
   int id[2];
-  float x[2];
+  float x[2], z[2], lp[2];
+};
+
+template <typename T>
+__device__ __forceinline__ void fetch(const DistillArgs& a, int n, const T* row, Mine& m) {
+  const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int j = lane + 64 * i;
-    id[i] = -1;
-    x[i] = -INFINITY;
+    m.id[i] = -1;
+    m.x[i] = -INFINITY;
     if (j < a.K) {
       const int t = a.ids[(size_t)n * a.K + j];
       const float v = a.vals[(size_t)n * a.K + j];
       if (t >= 0 && t < a.V && !(v == -INFINITY)) {
-        id[i] = t;
-        x[i] = v * a.inv_t;
+        m.id[i] = t;
+        m.x[i] = v;
       }
     }
   }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) m.z[i] = m.id[i] >= 0 ? op_ld(row, m.id[i]) : 0.f;
+}
+
+// the teacher's probabilities, by the wave that fetched
+__device__ __forceinline__ void teacher(const DistillArgs& a, int n, Mine& mine, Slots& s) {
+  const int lane = threadIdx.x & 63;
+  const int(&id)[2] = mine.id;
+  const float(&x)[2] = mine.x;
   const bool any = __builtin_amdgcn_ballot_w64(id[0] >= 0 || id[1] >= 0) != 0;
   const float m = any ? wave_max(fmaxf(x[0], x[1])) : 0.f;
-  const float e0 = __expf(x[0] - m), e1 = __expf(x[1] - m);
+  const float c = a.inv_t * kLog2e;
+  const float e0 = __builtin_amdgcn_exp2f((x[0] - m) * c), e1 = __builtin_amdgcn_exp2f((x[1] - m) * c);
   const float total = wave_sum(e0 + e1), ls = logf(total);
   const float w = a.weight ? a.weight[n] : 1.f;
-  lp[0] = x[0] - m - ls;
-  lp[1] = x[1] - m - ls;
+  mine.lp[0] = (x[0] - m) * a.inv_t - ls;
+  mine.lp[1] = (x[1] - m) * a.inv_t - ls;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int j = lane + 64 * i;
     s.id[j] = id[i];
+    s.z[j] = mine.z[i];
     s.p[j] = id[i] >= 0 ? (i ? e1 : e0) / total : 0.f;
   }
   if (lane == 0) s.live = any && w != 0.f;
-}
-
-// marks, for every thread, which of its chunks (bit i: chunk c0 + i TPB + t)
-// hold a teacher's token; by the wave that ran teacher(), after the marks are 0
-template <int E, int TPB>
-__device__ __forceinline__ void mark(const Slots& s, int K, int c0, int C, unsigned* marks) {
-  for (int j = threadIdx.x & 63; j < K; j += 64) {
-    const int c = s.id[j] / E - c0;
-    if (s.id[j] >= 0 && c >= 0 && c < C * TPB) atomicOr(&marks[c % TPB], 1u << (c / TPB));
-  }
-}
-
-// subtracts the teacher's probabilities of a marked chunk's tokens, in the slots' order
-template <int E>
-__device__ __forceinline__ void subtract(const Slots& s, int K, int c, float (&g)[E]) {
-  for (int j = 0; j < K; ++j) {
-    const int at = s.id[j] - c * E;
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-      if (at == e) g[e] -= s.p[j];
-  }
-}
-
-template <int TPB, bool MAX>
-__device__ __forceinline__ float block_reduce(float v, float* red) {
-  constexpr int W = TPB / 64;
-  v = MAX ? wave_max(v) : wave_sum(v);
-  if (W == 1) return v;
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = red[0];
-#pragma unroll
-  for (int i = 1; i < W; ++i) v = MAX ? fmaxf(v, red[i]) : v + red[i];
-  return v;
-}
-
-// One workgroup per row, two sweeps over it: the running maximum and sum, then
-// the gradient.
-template <typename T, bool GRAD>
-__global__ __launch_bounds__(1024) void distill_sweep_kernel(DistillArgs a) {
-  constexpr int TPB = 1024, E = Vec<T>::E, SEG = 32;
-  __shared__ Slots slots;
-  __shared__ unsigned marks[TPB];
-  __shared__ float red[TPB / 64];
-  const int n = blockIdx.x, t = threadIdx.x;
-  const T* row = (const T*)a.logits + (size_t)n * a.ld;
-  const int chunks = (a.V + E - 1) / E;
-  float lp[2] = {0.f, 0.f}, z[2] = {0.f, 0.f};
-  if (t < 64) {
-    teacher(a, n, slots, lp);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  float sum[2] = {s.p[lane], s.p[lane + 64]};
+  for (int k = 0; k < a.K; ++k) {
+    const int ik = s.id[k];
+    const float pk = s.p[k];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-      if (slots.id[t + 64 * i] >= 0) z[i] = op_ld(row, slots.id[t + 64 * i]);
+      if (ik == id[i] && k != lane + 64 * i) sum[i] = k < lane + 64 * i ? -INFINITY : sum[i] + pk;
   }
-  float m = -INFINITY, s = 0.f;
-  for (int c = t; c < chunks; c += TPB) {
-    const u32x4 r = load_chunk(row, c, a.V);
-    float top = m;
+  // (a token named before: -infinity, whatever was added)
 #pragma unroll
-    for (int e = 0; e < E; ++e) top = fmaxf(top, Vec<T>::get(r, e) * a.inv_t);
-    const float ref = top == -INFINITY ? 0.f : top;
-    s *= __expf(m - ref);
+  for (int i = 0; i < 2; ++i) s.sum[lane + 64 * i] = sum[i] == -INFINITY ? 0.f : sum[i];
+}
+
+// Every thread's list of the teacher's tokens among its elements of a run: the
+// edge element it has, and chunks c0 + i TPB + t.
+template <int TPB>
+struct __align__(16) Lists {
+  int head[TPB];
+  int next[kMaxSlots];
+
+  // By the wave that ran teacher().  A list's order does not matter, its tokens differ.
+  template <typename T>
+  __device__ __forceinline__ void fill(const Slots& s, int K, const Row<T>& body, int c0, int C) {
+    constexpr int E = Vec<T>::E;
 #pragma unroll
-    for (int e = 0; e < E; ++e) s += __expf(Vec<T>::get(r, e) * a.inv_t - ref);
-    m = top;
+    for (int i = 0; i < TPB / 256; ++i) ((int4*)head)[64 * i + threadIdx.x] = make_int4(-1, -1, -1, -1);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    for (int j = threadIdx.x; j < K; j += 64) {
+      const int id = s.id[j];
+      if (id < 0 || s.sum[j] == 0.f) continue;
+      int t;
+      if (id < body.head || id >= body.V - body.tail) {
+        if (c0) continue;
+        t = id < body.head ? id : E + id - (body.V - body.tail);
+      } else {
+        const int c = (id - body.head) / E - c0;
+        if (c < 0 || c >= C * TPB) continue;
+        t = c % TPB;
+      }
+      next[j] = atomicExch(&head[t], j);
+    }
   }
-  const float top = block_reduce<TPB, true>(m, red), ref = top == -INFINITY ? 0.f : top;
-  const float total = block_reduce<TPB, false>(s * __expf(m - ref), red);
-  const float lse = top + logf(total);
+};
+
+// A reference m and the sum of 2^(c z - m), c = log2 e / T: with m the largest
+// c z for the sums of one thread, which agree on one later.
+struct Stat {
+  float m, s;
+};
+// References beyond this are not used: 2^(c z - m) by one rounding (fmaf) fails
+// where c z overflows, as for rows of the type's lowest value.  Such a row is
+// found by its reference and done again by sweep().
+constexpr float kFar = 1e30f;
+__device__ __forceinline__ float near_(float x) { return fminf(fmaxf(x, -kFar), kFar); }
+
+// Keeps the compiler from holding the chunk's elements unpacked from one use
+// to the next (twice the registers for bfloat16).
+__device__ __forceinline__ void repack(u32x4& r) { asm volatile("" : "+v"(r)); }
+
+// Adds a row's chunks, four at a time as their loads arrive: the arithmetic of a
+// row takes about as long as its loads.
+template <typename T, int FROM, int N>
+__device__ __forceinline__ void add_all(Stat& a, u32x4 (&r)[N], float c) {
+  if constexpr (FROM < N) {
+    constexpr int E = Vec<T>::E, TO = FROM + 4 < N ? FROM + 4 : N;
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = FROM; i < TO; ++i) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) top = fmaxf(top, Vec<T>::get(r[i], e));
+      repack(r[i]);
+    }
+    const float m = fmaxf(a.m, near_(top * c));
+    float s = a.s * __builtin_amdgcn_exp2f(a.m - m);
+#pragma unroll
+    for (int i = FROM; i < TO; ++i) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f(fmaf(Vec<T>::get(r[i], e), c, -m));
+      repack(r[i]);
+    }
+    a.m = m;
+    a.s = s;
+    __builtin_amdgcn_sched_barrier(0);
+    add_all<T, TO>(a, r, c);
+  }
+}
+
+// Joins the workgroup's; one barrier.  c: 1, or the factor of sums whose
+// references are not in units of log 2 yet.
+template <int TPB>
+__device__ __forceinline__ Stat block_stat(Stat a, float c, Stat* red) {
+  constexpr int W = TPB / 64;
+  const float top = wave_max(a.m);
+  // (a thread, or a wave, all of whose entries are -infinity adds 0)
+  a.s = wave_sum(a.m == -INFINITY ? a.s : a.s * __builtin_amdgcn_exp2f((a.m - top) * c));
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = (Stat){top, a.s};
+  __syncthreads();
+  Stat r = red[0];
+#pragma unroll
+  for (int i = 1; i < W; ++i) r.m = fmaxf(r.m, red[i].m);
+  float t = 0.f;
+#pragma unroll
+  for (int i = 0; i < W; ++i)
+    t += red[i].m == -INFINITY ? red[i].s : red[i].s * __builtin_amdgcn_exp2f((red[i].m - r.m) * c);
+  r.s = t;
+  return r;
+}
+
+// Chunk c0 + thread of the gradient, mul q' with q' its exponentials, as if the teacher had
+// none of its tokens; aligned: whether out's chunks begin at multiples of 16 bytes
+// as the logits' do.  The stores pass by the caches (512 float32 rows of
+// 131072, step: 152 us with plain ones, 127 with these).
+template <typename T>
+__device__ __forceinline__ void put_chunk(T* out, const Row<T>& body, int c0, bool aligned, float mul,
+                                          float (&q)[Vec<T>::E]) {
+  constexpr int E = Vec<T>::E;
+#pragma unroll
+  for (int e = 0; e < E; ++e) q[e] *= mul;
+  const u32x4 r = Vec<T>::pack(q);
+  char* at = (char*)(out + body.head + (size_t)c0 * E) + 16u * threadIdx.x;
+  if (aligned) __builtin_nontemporal_store(r, (u32x4*)at);
+  else *(u32x4_a2*)at = r;
+}
+
+// The gradient of the thread's tokens, mul q' - f p, over what its own stores
+// have put there; q(z): q' of a logit.
+template <typename T, int TPB, typename Q>
+__device__ __forceinline__ void put_tokens(T* out, const Slots& s, const Lists<TPB>& lists, float mul, float f, Q q) {
+  for (int j = lists.head[threadIdx.x]; j >= 0; j = lists.next[j])
+    op_st(out, s.id[j], q(s.z[j]) * mul - s.sum[j] * f);
+}
+
+// the gradient of a row that does not count: chunks c0 .. c1 - 1, and edge element `edge`
+template <typename T, int TPB>
+__device__ __forceinline__ void put_zeros(T* out, const Row<T>& row, int c0, int c1, int edge) {
+  for (int c = c0 + threadIdx.x; c < min(c1, row.chunks); c += TPB)
+    *(u32x4_a2*)(out + row.head + (size_t)c * Vec<T>::E) = (u32x4){0, 0, 0, 0};
+  if (edge >= 0) op_st(out, edge, 0.f);
+}
+
+// the row's loss, by the wave that ran teacher()
+__device__ __forceinline__ void put_loss(const DistillArgs& a, int n, const Slots& s, const Mine& m, float lse) {
+  const int lane = threadIdx.x & 63;
+  float l = 0.f;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float p = s.p[lane + 64 * i];
+    if (p != 0.f) l += p * (m.lp[i] - (m.z[i] * a.inv_t - lse));
+  }
+  l = wave_sum(l);
+  if (lane == 0) {
+    a.loss[n] = s.live ? l * (a.weight ? a.weight[n] : 1.f) : 0.f;
+    a.lse[n] = lse;
+  }
+}
+
+// what is taken from z: the maximum, or 0 where all entries are -infinity
+__device__ __forceinline__ float ref_of(float m) { return m == -INFINITY ? 0.f : m; }
+
+// A row by two sweeps over it: the maximum and sum, then the gradient.  The
+// difference z - maximum comes before the factor c, for logits of any size.
+// The first wave has run teacher().
+template <typename T, int TPB, bool GRAD>
+__device__ void sweep(const DistillArgs& a, int n, const Row<T>& body, int edge, float ze, const Slots& slots,
+                      Lists<TPB>& lists, Stat* red, const Mine& mine) {
+  constexpr int E = Vec<T>::E, U = 4, SEG = 64;
+  const int t = threadIdx.x, chunks = body.chunks;
+  const T* row = (const T*)a.logits + (size_t)n * a.ld;
+  const float c2 = a.inv_t * kLog2e;
+  Stat st = {ze, edge >= 0 && ze != -INFINITY ? 1.f : 0.f};
+  for (int c = 0; c < chunks; c += U * TPB) {
+    u32x4 r[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) r[i] = body.template load<!GRAD>(row, c + i * TPB);
+    float top = st.m;
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+      for (int e = 0; e < E; ++e) top = fmaxf(top, Vec<T>::get(r[i], e));
+    const float ref = ref_of(top);
+    float s = st.s * __builtin_amdgcn_exp2f((st.m - ref) * c2);
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+      for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f((Vec<T>::get(r[i], e) - ref) * c2);
+    st.m = top;
+    st.s = s;
+  }
+  __syncthreads();  // (red may still be read)
+  st = block_stat<TPB>(st, c2, red);
+  const float ref = ref_of(st.m);
+  if (GRAD) {
+    T* out = (T*)a.grad + (size_t)n * a.ld_d;
+    const bool aligned = (uintptr_t)out % 16 == (uintptr_t)row % 16;
+    const float f = (a.weight ? a.weight[n] : 1.f) * a.inv_t, mul = f / st.s;
+    if (!slots.live) put_zeros<T, TPB>(out, body, 0, chunks, edge);
+    else
+      for (int c0 = 0; c0 == 0 || c0 < chunks; c0 += SEG * TPB) {
+        __syncthreads();
+        if (t < 64) lists.fill(slots, a.K, body, c0, SEG);
+        __syncthreads();
+        auto q1 = [&](float x) { return __builtin_amdgcn_exp2f((x - ref) * c2); };
+        if (c0 == 0 && edge >= 0) op_st(out, edge, q1(ze) * mul);
+        for (int i0 = 0; i0 < SEG && c0 + i0 * TPB < chunks; i0 += U) {
+          u32x4 r[U];
+#pragma unroll
+          for (int i = 0; i < U; ++i) r[i] = body.template load<true>(row, c0 + (i0 + i) * TPB);
+#pragma unroll
+          for (int i = 0; i < U; ++i) {
+            const int c = c0 + (i0 + i) * TPB;
+            if (c + t >= chunks) continue;
+            float q[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) q[e] = q1(Vec<T>::get(r[i], e));
+            put_chunk(out, body, c, aligned, mul, q);
+          }
+        }
+        put_tokens(out, slots, lists, mul, f, q1);
+      }
+  }
+  if (t < 64) put_loss(a, n, slots, mine, ref * a.inv_t + logf(st.s));
+}
+
+template <typename T, bool GRAD>
+__global__ __launch_bounds__(1024) void distill_sweep_kernel(DistillArgs a) {
+  constexpr int TPB = 1024, E = Vec<T>::E;
+  __shared__ Slots slots;
+  __shared__ Lists<TPB> lists;
+  __shared__ Stat red[TPB / 64];
+  const int n = blockIdx.x, t = threadIdx.x;
+  const T* row = (const T*)a.logits + (size_t)n * a.ld;
+  const Row<T> body(row, a.V);
+  const int edge = t < 2 * E ? body.edge(t) : -1;
+  const float ze = edge >= 0 ? op_ld(row, edge) : -INFINITY;
+  Mine mine;
   if (t < 64) {
-    float l = 0.f;
+    fetch(a, n, row, mine);
+    teacher(a, n, mine, slots);
+  }
+  sweep<T, TPB, GRAD>(a, n, body, edge, ze, slots, lists, red, mine);
+}
+
+// One workgroup per row, which its registers hold: C chunks a thread.
+// W: waves per SIMD that its registers leave room for.
+template <typename T, int TPB, int C, int W, bool GRAD>
+__global__ __launch_bounds__(TPB, W) void distill_row_kernel(DistillArgs a) {
+  constexpr int E = Vec<T>::E;
+  __shared__ Slots slots;
+  __shared__ Lists<TPB> lists;
+  __shared__ Stat red[TPB / 64];
+  const int n = blockIdx.x, t = threadIdx.x;
+  const T* row = (const T*)a.logits + (size_t)n * a.ld;
+  const Row<T> body(row, a.V);
+  const int edge = t < 2 * E ? body.edge(t) : -1;
+  const float ze = edge >= 0 ? op_ld(row, edge) : -INFINITY;
+  Mine mine;
+  if (t < 64) fetch(a, n, row, mine);  // (first: all else waits for it less long than it would for the row)
+  u32x4 r[C];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float p = slots.p[t + 64 * i];
-      if (p != 0.f) l += p * (lp[i] - (z[i] * a.inv_t - lse));
-    }
-    l = wave_sum(l);
-    if (t == 0) {
-      a.loss[n] = slots.live ? l * (a.weight ? a.weight[n] : 1.f) : 0.f;
-      a.lse[n] = lse;
+  for (int i = 0; i < C; ++i) r[i] = body.template load<true>(row, i * TPB);
+  if (t < 64) {
+    teacher(a, n, mine, slots);
+    if (GRAD) lists.fill(slots, a.K, body, 0, C);
+  }
+  const float c2 = a.inv_t * kLog2e;
+  Stat st;
+  st.m = near_(ze * c2);
+  st.s = __builtin_amdgcn_exp2f(fmaf(ze, c2, -st.m));
+  add_all<T, 0>(st, r, c2);
+  st = block_stat<TPB>(st, 1.f, red);
+  if (!(fabsf(st.m) < kFar)) return sweep<T, TPB, GRAD>(a, n, body, edge, ze, slots, lists, red, mine);
+  if (GRAD) {
+    T* out = (T*)a.grad + (size_t)n * a.ld_d;
+    const float f = (a.weight ? a.weight[n] : 1.f) * a.inv_t, mul = f / st.s;
+    if (slots.live) {
+      const bool aligned = (uintptr_t)out % 16 == (uintptr_t)row % 16;
+      auto q1 = [&](float x) { return __builtin_amdgcn_exp2f(fmaf(x, c2, -st.m)); };
+      if (edge >= 0) op_st(out, edge, q1(ze) * mul);
+#pragma unroll
+      for (int i = 0; i < C; ++i) {
+        if (i * TPB + t >= body.chunks) continue;
+        float q[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) q[e] = q1(Vec<T>::get(r[i], e));
+        put_chunk(out, body, i * TPB, aligned, mul, q);
+      }
+      put_tokens(out, slots, lists, mul, f, q1);
+    } else {
+      put_zeros<T, TPB>(out, body, 0, body.chunks, edge);
     }
   }
-  if (!GRAD) return;
-  T* out = (T*)a.grad + (size_t)n * a.ld_d;
-  const bool live = slots.live;
-  const float f = (a.weight ? a.weight[n] : 1.f) * a.inv_t, inv = 1.f / total;
-  for (int c0 = 0; c0 < chunks; c0 += SEG * TPB) {
-    __syncthreads();
-    marks[t] = 0;
-    __syncthreads();
-    if (t < 64) mark<E, TPB>(slots, a.K, c0, SEG, marks);
-    __syncthreads();
-    const unsigned mk = marks[t];
-    for (int i = 0; i < SEG; ++i) {
-      const int c = c0 + i * TPB + t;
-      if (c >= chunks) break;
-      const u32x4 r = load_chunk(row, c, a.V);
-      float g[E];
-#pragma unroll
-      for (int e = 0; e < E; ++e) g[e] = __expf(Vec<T>::get(r, e) * a.inv_t - top) * inv;
-      if (mk >> i & 1) subtract<E>(slots, a.K, c, g);
-#pragma unroll
-      for (int e = 0; e < E; ++e) g[e] = live ? g[e] * f : 0.f;
-      store_chunk(out, c, a.V, g);
-    }
-  }
+  if (t < 64) put_loss(a, n, slots, mine, (st.m + __log2f(st.s)) * kLn2);
 }
 
 // The gradient from a known log-sum-exp: a workgroup per row and 8 chunks a thread.
@@ -256,34 +463,40 @@ template <typename T>
 __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a) {
   constexpr int TPB = 256, E = Vec<T>::E, C = 8;
   __shared__ Slots slots;
-  __shared__ unsigned marks[TPB];
+  __shared__ Lists<TPB> lists;
   const int n = blockIdx.x, c0 = blockIdx.y * (C * TPB), t = threadIdx.x;
   const T* row = (const T*)a.logits + (size_t)n * a.ld;
   T* out = (T*)a.grad + (size_t)n * a.ld_d;
-  const int chunks = (a.V + E - 1) / E;
+  const Row<T> body(row, a.V);
+  const int chunks = body.chunks, edge = blockIdx.y == 0 && t < 2 * E ? body.edge(t) : -1;
+  if (c0 >= chunks && blockIdx.y) return;
+  const float ze = edge >= 0 ? op_ld(row, edge) : 0.f;
+  Mine mine;
+  if (t < 64) fetch(a, n, row, mine);
   u32x4 r[C];
 #pragma unroll
-  for (int i = 0; i < C; ++i) r[i] = load_chunk(row, c0 + i * TPB + t, a.V);
-  marks[t] = 0;
-  float lp[2];
-  if (t < 64) teacher(a, n, slots, lp);
+  for (int i = 0; i < C; ++i) r[i] = body.template load<true>(row, c0 + i * TPB);
+  if (t < 64) {
+    teacher(a, n, mine, slots);
+    lists.fill(slots, a.K, body, c0, C);
+  }
   __syncthreads();
-  if (t < 64) mark<E, TPB>(slots, a.K, c0, C, marks);
-  __syncthreads();
-  const unsigned mk = marks[t];
-  const bool live = slots.live;
+  const bool aligned = (uintptr_t)out % 16 == (uintptr_t)row % 16;
   const float f = (a.weight ? a.weight[n] : 1.f) * a.inv_t, lse = a.lse[n];
+  if (!slots.live) return put_zeros<T, TPB>(out, body, c0, c0 + C * TPB, edge);
+  // (the difference before the factor log2 e: 2^(c z - lse log2 e) would carry the rounding of two large numbers)
+  auto q1 = [&](float x) { return __expf(fmaf(x, a.inv_t, -lse)); };
+  if (edge >= 0) op_st(out, edge, q1(ze) * f);
 #pragma unroll
   for (int i = 0; i < C; ++i) {
-    const int c = c0 + i * TPB + t;
-    float g[E];
+    const int c = c0 + i * TPB;
+    if (c + t >= chunks) continue;
+    float q[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) g[e] = __expf(Vec<T>::get(r[i], e) * a.inv_t - lse);
-    if (mk >> i & 1) subtract<E>(slots, a.K, c, g);
-#pragma unroll
-    for (int e = 0; e < E; ++e) g[e] = live ? g[e] * f : 0.f;
-    if (c < chunks) store_chunk(out, c, a.V, g);
+    for (int e = 0; e < E; ++e) q[e] = q1(Vec<T>::get(r[i], e));
+    put_chunk(out, body, c, aligned, f, q);
   }
+  put_tokens(out, slots, lists, f, f, q1);
 }
 
 ssd_status check(int dtype, const void* logits, int64_t ld, int n, int V, const int* ids, const float* vals, int k,
@@ -309,10 +522,31 @@ ssd_status check_grad(int dtype, const void* logits, int64_t ld, int n, int V, c
   return SSD_OK;
 }
 
-template <typename T>
-void launch_rows(const DistillArgs& a, int n, bool grad, hipStream_t s) {
-  if (grad) distill_sweep_kernel<T, true><<<n, 1024, 0, s>>>(a);
-  else distill_sweep_kernel<T, false><<<n, 1024, 0, s>>>(a);
+// How a row is held: TPB threads with up to C chunks each.  With at least a row
+// for every CU, few threads with many chunks: two to four rows are on a CU, and one's
+// loads and stores run beside another's arithmetic and waits (2048 float32
+// rows of 50257, step: 149 us with 256 threads, 170 with 512, 167 with 1024).
+// With fewer rows a CU has one, and more threads are sooner done with it (64
+// rows: 15.2, 13.6, 12.7 us).
+template <typename T, bool GRAD>
+void launch_rows(const DistillArgs& a, int n, hipStream_t s) {
+  const int chunks = a.inv_t < 1e6f ? a.V / Vec<T>::E : INT_MAX;  // (see kFar)
+#define ROWS(TPB, C, W) \
+  if (chunks <= TPB * C) return distill_row_kernel<T, TPB, C, W, GRAD><<<n, TPB, 0, s>>>(a);
+  ROWS(256, 4, 6)
+  if (n < kCUs) {
+    ROWS(1024, 4, 4)
+    ROWS(1024, 7, 4)
+    ROWS(1024, 13, 4)
+  }
+  ROWS(256, 10, 4)
+  ROWS(256, 16, 4)
+  ROWS(256, 25, 3)
+  ROWS(256, 50, 2)
+  ROWS(512, 32, 2)
+  ROWS(512, 48, 2)
+#undef ROWS
+  return distill_sweep_kernel<T, GRAD><<<n, 1024, 0, s>>>(a);
 }
 
 }  // namespace
@@ -329,8 +563,8 @@ extern "C" ssd_status ssd_distill_forward(ssd_dtype dtype, const void* logits, i
   if (n_rows == 0) return SSD_OK;
   OP_REQUIRE(loss && lse, SSD_E_INVALID_ARG, "null argument");
   DistillArgs a{logits, ld, vocab, ids, vals, k, weight, 1.f / temperature, loss, lse, nullptr, 0};
-  if (dtype == SSD_F32) launch_rows<float>(a, n_rows, false, (hipStream_t)stream);
-  else launch_rows<bf16_t>(a, n_rows, false, (hipStream_t)stream);
+  if (dtype == SSD_F32) launch_rows<float, false>(a, n_rows, (hipStream_t)stream);
+  else launch_rows<bf16_t, false>(a, n_rows, (hipStream_t)stream);
   OP_LAUNCHED();
   return SSD_OK;
 }
@@ -345,8 +579,8 @@ extern "C" ssd_status ssd_distill_step(ssd_dtype dtype, const void* logits, int6
   if (n_rows == 0) return SSD_OK;
   OP_REQUIRE(loss && lse, SSD_E_INVALID_ARG, "null argument");
   DistillArgs a{logits, ld, vocab, ids, vals, k, weight, 1.f / temperature, loss, lse, dlogits, ld_d};
-  if (dtype == SSD_F32) launch_rows<float>(a, n_rows, true, (hipStream_t)stream);
-  else launch_rows<bf16_t>(a, n_rows, true, (hipStream_t)stream);
+  if (dtype == SSD_F32) launch_rows<float, true>(a, n_rows, (hipStream_t)stream);
+  else launch_rows<bf16_t, true>(a, n_rows, (hipStream_t)stream);
   OP_LAUNCHED();
   return SSD_OK;
 }
