@@ -13,6 +13,7 @@
 // chunk's blocks of rows in turn and never wait for each other until the end: a
 // wave copies its blocks' keys and values into LDS of its own, one block ahead.
 #include <algorithm>
+#include <atomic>
 
 #include "ops_common.h"
 
@@ -632,9 +633,18 @@ Plan plan(const ssd_prefix_attn_desc* a) {
 template <typename T, int D, int MP, int MO>
 hipError_t launch(const PrefixAttnArgs& a, int64_t blocks, hipStream_t s) {
   constexpr int lds = kWaves * 2 * 2 * Block<T, D>::BYTES;
-  hipError_t e = hipFuncSetAttribute((const void*)prefix_attn_kernel<T, D, MP, MO>,
-                                     hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  // once per device: raises the kernel's limit of dynamic LDS
+  static std::atomic<uint64_t> ready{0};
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return e;
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (!(ready.load(std::memory_order_acquire) & bit)) {
+    e = hipFuncSetAttribute((const void*)prefix_attn_kernel<T, D, MP, MO>,
+                            hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+    ready.fetch_or(bit, std::memory_order_release);
+  }
   if (blocks > 0) prefix_attn_kernel<T, D, MP, MO><<<(unsigned)blocks, 64 * kWaves, lds, s>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;

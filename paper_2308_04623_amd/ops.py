@@ -11,8 +11,8 @@ no longer tells (devices, types, shapes) and in the library for the rest.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
+import functools
 import math
 from typing import Optional
 
@@ -36,6 +36,7 @@ class _PrefixAttnDesc(C.Structure):
                                          "prefix_row", "own_seq", "own_head", "own_row")]
 
 
+_KINDS = (torch.float32, torch.bfloat16)
 _lib = None
 
 
@@ -74,6 +75,9 @@ def _check(status: int, what: str):
 
 def _tensor(what, name, t, dtypes, dims, like=None):
     """t is a device tensor of one of the dtypes with `dims` dimensions, on like's device."""
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in dtypes and t.dim() == dims and \
+            (like is None or t.get_device() == like.get_device()):
+        return
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         _refuse(what, f"{name} must be a tensor on the GPU")
     if t.dtype not in dtypes:
@@ -99,34 +103,35 @@ def _vector(what, name, t, dtype, n, like):
         _refuse(what, f"{name} must be contiguous")
 
 
-@contextlib.contextmanager
-def _on(t, stream):
-    """The stream's handle, with t's device and the stream current (what is allocated inside belongs to it)."""
-    if stream is None:
-        if t.device.index == torch.cuda.current_device():
-            yield torch.cuda.current_stream().cuda_stream
-        else:
-            with torch.cuda.device(t.device):
-                yield torch.cuda.current_stream().cuda_stream
-    else:
-        with torch.cuda.stream(stream):
-            yield stream.cuda_stream
+def _elsewhere(dev: int, stream):
+    """None where the call's stream and device are the current ones, else the
+    context that makes them so (what is allocated inside belongs to the stream)."""
+    if stream is not None:
+        return torch.cuda.stream(stream)
+    return None if dev == torch.cuda.current_device() else torch.cuda.device(dev)
+
+
+# the current stream's handle (torch.cuda.current_stream() builds an object each
+# time, 2.7 us where this takes 0.1; a call of these operators takes 5 to 10)
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
+    lambda dev: torch.cuda.current_stream(dev).cuda_stream
 
 
 # ---------------------------------------------------------------- attention
 
-def prefix_attention(q, k_prefix, v_prefix, k_own, v_own, own_len, scale: Optional[float] = None, out=None,
-                     return_lse: bool = False, stream=None):
-    """ssd_prefix_attn: attention of sequences that share a prefix.
+@functools.lru_cache(maxsize=256)
+def _attn_plan(dtype, b, t, h, d, g, p, r, scale, *strides):
+    """The description of a call's shapes and its workspace's bytes."""
+    a = _PrefixAttnDesc(_DTYPES[dtype], b, t, h, g, d, p, r, 1.0 / math.sqrt(d) if scale is None else scale, *strides)
+    need = C.c_size_t(0)
+    _check(_ops().ssd_prefix_attn_workspace(C.byref(a), C.byref(need)), "ssd_prefix_attn")
+    return C.byref(a), need.value
 
-    q [B][T][H][D] (a sequence's last T positions); k_prefix, v_prefix
-    [G][P][D]; k_own, v_own [B][G][R][D]; own_len int32 [B].  float32 or
-    bfloat16, any strides that are multiples of 16 bytes with D contiguous (K and
-    V alike).  scale defaults to 1 / sqrt(D).  Returns out [B][T][H][D], or (out,
-    lse float32 [B][T][H])."""
+
+def _refuse_attn(q, k_prefix, v_prefix, k_own, v_own, own_len, out):
+    """Says what is wrong with prefix_attention's tensors, if anything is."""
     what = "ssd_prefix_attn"
-    kinds = (torch.float32, torch.bfloat16)
-    _tensor(what, "q", q, kinds, 4)
+    _tensor(what, "q", q, _KINDS, 4)
     for name, t, dims in (("k_prefix", k_prefix, 3), ("v_prefix", v_prefix, 3), ("k_own", k_own, 4),
                           ("v_own", v_own, 4)):
         _tensor(what, name, t, (q.dtype,), dims, q)
@@ -147,29 +152,48 @@ def prefix_attention(q, k_prefix, v_prefix, k_own, v_own, own_len, scale: Option
     for name, x in (("q", q), ("k_prefix", k_prefix), ("k_own", k_own), ("out", out)):
         if x is not None and x.numel() and x.stride(-1) != 1:
             _refuse(what, f"{name}'s last dimension must be contiguous")
-    lib = _ops()
-    with _on(q, stream) as s:
-        if out is None:
-            out = torch.empty((b, t, h, d), dtype=q.dtype, device=q.device)
-        lse = torch.empty((b, t, h), dtype=torch.float32, device=q.device) if return_lse else None
-        # (a dimension of one entry has no stride to speak of)
-        step = lambda x, i: x.stride(i) if x.shape[i] > 1 else 0  # noqa: E731
-        a = _PrefixAttnDesc(_DTYPES[q.dtype], b, t, h, g, d, p, r, 1.0 / math.sqrt(d) if scale is None else scale,
-                            step(q, 0), step(q, 1), step(q, 2), step(out, 0), step(out, 1), step(out, 2),
-                            step(k_prefix, 0), step(k_prefix, 1), step(k_own, 0), step(k_own, 1), step(k_own, 2))
-        need = C.c_size_t(0)
-        _check(lib.ssd_prefix_attn_workspace(C.byref(a), C.byref(need)), what)
-        work = torch.empty(need.value, dtype=torch.uint8, device=q.device)
-        _check(lib.ssd_prefix_attn(C.byref(a), q.data_ptr(), k_prefix.data_ptr(), v_prefix.data_ptr(),
-                                   k_own.data_ptr(), v_own.data_ptr(), own_len.data_ptr(), out.data_ptr(),
-                                   lse.data_ptr() if lse is not None else None, work.data_ptr(), need.value, s), what)
+
+
+def prefix_attention(q, k_prefix, v_prefix, k_own, v_own, own_len, scale: Optional[float] = None, out=None,
+                     return_lse: bool = False, stream=None):
+    """ssd_prefix_attn: attention of sequences that share a prefix.
+
+    q [B][T][H][D] (a sequence's last T positions); k_prefix, v_prefix
+    [G][P][D]; k_own, v_own [B][G][R][D]; own_len int32 [B].  float32 or
+    bfloat16, any strides that are multiples of 16 bytes with D contiguous (K and
+    V alike).  scale defaults to 1 / sqrt(D).  Returns out [B][T][H][D], or (out,
+    lse float32 [B][T][H])."""
+    _refuse_attn(q, k_prefix, v_prefix, k_own, v_own, own_len, out)
+    dev = q.get_device()
+    where = _elsewhere(dev, stream)
+    if where is not None:
+        with where:
+            return prefix_attention(q, k_prefix, v_prefix, k_own, v_own, own_len, scale, out, return_lse)
+    if out is None:
+        out = q.new_empty(q.shape)
+    b, t, h, d = q.shape
+    g, p, _ = k_prefix.shape
+    r = k_own.shape[2]
+    lse = torch.empty((b, t, h), dtype=torch.float32, device=q.device) if return_lse else None
+    # (a dimension of one entry has no stride to speak of)
+    qs, os, ps, ks = q.stride(), out.stride(), k_prefix.stride(), k_own.stride()
+    a, need = _attn_plan(q.dtype, b, t, h, d, g, p, r, scale, qs[0] if b > 1 else 0, qs[1] if t > 1 else 0,
+                         qs[2] if h > 1 else 0, os[0] if b > 1 else 0, os[1] if t > 1 else 0, os[2] if h > 1 else 0,
+                         ps[0] if g > 1 else 0, ps[1] if p > 1 else 0, ks[0] if b > 1 else 0, ks[1] if g > 1 else 0,
+                         ks[2] if r > 1 else 0)
+    work = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _check(_ops().ssd_prefix_attn(a, q.data_ptr(), k_prefix.data_ptr(), v_prefix.data_ptr(), k_own.data_ptr(),
+                                  v_own.data_ptr(), own_len.data_ptr(), out.data_ptr(),
+                                  lse.data_ptr() if return_lse else None, work.data_ptr(), need, _raw_stream(dev)),
+           "ssd_prefix_attn")
     return (out, lse) if return_lse else out
 
 
 # ---------------------------------------------------------------- distillation
 
 def _logits(what, logits, ids, vals, weight):
-    _tensor(what, "logits", logits, (torch.float32, torch.bfloat16), 2)
+    """Checks what the calls share and gives the library's first arguments."""
+    _tensor(what, "logits", logits, _KINDS, 2)
     n, v = logits.shape
     ld = _rows(what, "logits", logits)
     _tensor(what, "ids", ids, (torch.int32,), 2, logits)
@@ -180,7 +204,7 @@ def _logits(what, logits, ids, vals, weight):
         _refuse(what, "ids and vals must be contiguous")
     if weight is not None:
         _vector(what, "weight", weight, torch.float32, n, logits)
-    return [_DTYPES[logits.dtype], logits.data_ptr(), ld, n, v, ids.data_ptr(), vals.data_ptr(), ids.shape[1]]
+    return _DTYPES[logits.dtype], logits.data_ptr(), ld, n, v, ids.data_ptr(), vals.data_ptr(), ids.shape[1]
 
 
 def _grad_out(what, logits, out):
@@ -196,16 +220,26 @@ def _ptr(t):
     return t.data_ptr() if t is not None else None
 
 
+def _loss_lse(logits):
+    n = logits.shape[0]
+    return (torch.empty(n, dtype=torch.float32, device=logits.device),
+            torch.empty(n, dtype=torch.float32, device=logits.device))
+
+
 def distill_forward(logits, ids, vals, weight=None, temperature: float = 1.0, stream=None):
     """ssd_distill_forward: (loss float32 [N], lse float32 [N]) of logits
     [N][V] (float32 or bfloat16) against the teacher's ids int32 [N][k] and
     their logits vals float32 [N][k]; weight float32 [N] or None."""
     what = "ssd_distill_forward"
     args = _logits(what, logits, ids, vals, weight)
-    lib = _ops()
-    with _on(logits, stream) as s:
-        loss, lse = torch.empty((2, logits.shape[0]), dtype=torch.float32, device=logits.device).unbind(0)
-        _check(lib.ssd_distill_forward(*args, _ptr(weight), temperature, loss.data_ptr(), lse.data_ptr(), s), what)
+    dev = logits.get_device()
+    where = _elsewhere(dev, stream)
+    if where is not None:
+        with where:
+            return distill_forward(logits, ids, vals, weight, temperature)
+    loss, lse = _loss_lse(logits)
+    _check(_ops().ssd_distill_forward(*args, _ptr(weight), temperature, loss.data_ptr(), lse.data_ptr(),
+                                      _raw_stream(dev)), what)
     return loss, lse
 
 
@@ -215,11 +249,14 @@ def distill_backward(logits, ids, vals, lse, weight=None, temperature: float = 1
     what = "ssd_distill_backward"
     args = _logits(what, logits, ids, vals, weight)
     _vector(what, "lse", lse, torch.float32, logits.shape[0], logits)
-    lib = _ops()
-    with _on(logits, stream) as s:
-        out = _grad_out(what, logits, out)
-        _check(lib.ssd_distill_backward(*args, lse.data_ptr(), _ptr(weight), temperature, out.data_ptr(),
-                                        _rows(what, "out", out), s), what)
+    dev = logits.get_device()
+    where = _elsewhere(dev, stream)
+    if where is not None:
+        with where:
+            return distill_backward(logits, ids, vals, lse, weight, temperature, out)
+    out = _grad_out(what, logits, out)
+    _check(_ops().ssd_distill_backward(*args, lse.data_ptr(), _ptr(weight), temperature, out.data_ptr(),
+                                       _rows(what, "out", out), _raw_stream(dev)), what)
     return out
 
 
@@ -227,40 +264,58 @@ def distill_step(logits, ids, vals, weight=None, temperature: float = 1.0, out=N
     """ssd_distill_step: (loss, lse, gradient) in one call.  out may be logits."""
     what = "ssd_distill_step"
     args = _logits(what, logits, ids, vals, weight)
-    lib = _ops()
-    with _on(logits, stream) as s:
-        loss, lse = torch.empty((2, logits.shape[0]), dtype=torch.float32, device=logits.device).unbind(0)
-        out = _grad_out(what, logits, out)
-        _check(lib.ssd_distill_step(*args, _ptr(weight), temperature, loss.data_ptr(), lse.data_ptr(), out.data_ptr(),
-                                    _rows(what, "out", out), s), what)
+    dev = logits.get_device()
+    where = _elsewhere(dev, stream)
+    if where is not None:
+        with where:
+            return distill_step(logits, ids, vals, weight, temperature, out)
+    loss, lse = _loss_lse(logits)
+    out = _grad_out(what, logits, out)
+    _check(_ops().ssd_distill_step(*args, _ptr(weight), temperature, loss.data_ptr(), lse.data_ptr(), out.data_ptr(),
+                                   _rows(what, "out", out), _raw_stream(dev)), what)
     return loss, lse, out
 
 
 # ---------------------------------------------------------------- embedding
 
+def _rows_out(what, like, shape, dtype, out):
+    """`out`, checked, or a new tensor of the type asked for."""
+    if out is None:
+        if dtype not in _DTYPES:
+            _refuse(what, f"dtype must be torch.float32 or torch.bfloat16, not {dtype}")
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    _tensor(what, "out", out, _KINDS, 2, like)
+    if tuple(out.shape) != shape or (dtype is not None and out.dtype != dtype):
+        _refuse(what, f"out must be {list(shape)} of the type asked for")
+    return out
+
+
 def embed(tokens, table, scale: float = 1.0, dtype=None, out=None, stream=None):
     """ssd_embed: scale * table[tokens] as [N][d] of `dtype` (default: the
     table's); tokens int32 [N], those outside the table give zeros."""
     what = "ssd_embed"
-    kinds = (torch.float32, torch.bfloat16)
-    _tensor(what, "table", table, kinds, 2)
+    _tensor(what, "table", table, _KINDS, 2)
     _tensor(what, "tokens", tokens, (torch.int32,), 1, table)
     n = tokens.shape[0]
     _vector(what, "tokens", tokens, torch.int32, n, table)
-    lib = _ops()
-    with _on(table, stream) as s:
-        if out is None:
-            dtype = dtype or table.dtype
-            if dtype not in kinds:
-                _refuse(what, f"dtype must be torch.float32 or torch.bfloat16, not {dtype}")
-            out = torch.empty((n, table.shape[1]), dtype=dtype, device=table.device)
-        _tensor(what, "out", out, kinds, 2, table)
-        if tuple(out.shape) != (n, table.shape[1]) or (dtype is not None and out.dtype != dtype):
-            _refuse(what, f"out must be [{n}][{table.shape[1]}] of the type asked for")
-        _check(lib.ssd_embed(_DTYPES[table.dtype], _DTYPES[out.dtype], tokens.data_ptr(), n, table.data_ptr(),
-                             _rows(what, "table", table), table.shape[0], table.shape[1], scale, out.data_ptr(),
-                             _rows(what, "out", out), s), what)
+    dev = table.get_device()
+    where = _elsewhere(dev, stream)
+    if where is not None:
+        with where:
+            return embed(tokens, table, scale, dtype, out)
+    v, d = table.shape
+    out = _rows_out(what, table, (n, d), dtype or (None if out is not None else table.dtype), out)
+    _check(_ops().ssd_embed(_DTYPES[table.dtype], _DTYPES[out.dtype], tokens.data_ptr(), n, table.data_ptr(),
+                            _rows(what, "table", table), v, d, scale, out.data_ptr(), _rows(what, "out", out),
+                            _raw_stream(dev)), what)
     return out
+
+
+@functools.lru_cache(maxsize=256)
+def _embed_grad_bytes(n, vocab, d):
+    need = C.c_size_t(0)
+    _check(_ops().ssd_embed_grad_workspace(n, vocab, d, C.byref(need)), "ssd_embed_grad")
+    return need.value
 
 
 def embed_grad(tokens, grad, vocab: int, scale: float = 1.0, dtype=None, out=None, accumulate: bool = False,
@@ -268,27 +323,20 @@ def embed_grad(tokens, grad, vocab: int, scale: float = 1.0, dtype=None, out=Non
     """ssd_embed_grad: the gradient [vocab][d] of embed's table from grad
     [N][d], of `dtype` (default: grad's).  accumulate adds to `out`."""
     what = "ssd_embed_grad"
-    kinds = (torch.float32, torch.bfloat16)
-    _tensor(what, "grad", grad, kinds, 2)
+    _tensor(what, "grad", grad, _KINDS, 2)
     n, d = grad.shape
     _vector(what, "tokens", tokens, torch.int32, n, grad)
     if accumulate and out is None:
         _refuse(what, "accumulate needs out")
-    lib = _ops()
-    with _on(grad, stream) as s:
-        if out is None:
-            dtype = dtype or grad.dtype
-            if dtype not in kinds:
-                _refuse(what, f"dtype must be torch.float32 or torch.bfloat16, not {dtype}")
-        need = C.c_size_t(0)
-        _check(lib.ssd_embed_grad_workspace(n, vocab, d, C.byref(need)), what)
-        if out is None:
-            out = torch.empty((vocab, d), dtype=dtype, device=grad.device)
-        _tensor(what, "out", out, kinds, 2, grad)
-        if tuple(out.shape) != (vocab, d) or (dtype is not None and out.dtype != dtype):
-            _refuse(what, f"out must be [{vocab}][{d}] of the type asked for")
-        work = torch.empty(need.value, dtype=torch.uint8, device=grad.device)
-        _check(lib.ssd_embed_grad(_DTYPES[grad.dtype], _DTYPES[out.dtype], tokens.data_ptr(), n, grad.data_ptr(),
-                                  _rows(what, "grad", grad), vocab, d, scale, int(accumulate), out.data_ptr(),
-                                  _rows(what, "out", out), work.data_ptr(), need.value, s), what)
+    dev = grad.get_device()
+    where = _elsewhere(dev, stream)
+    if where is not None:
+        with where:
+            return embed_grad(tokens, grad, vocab, scale, dtype, out, accumulate)
+    need = _embed_grad_bytes(n, vocab, d)
+    out = _rows_out(what, grad, (vocab, d), dtype or (None if out is not None else grad.dtype), out)
+    work = torch.empty(need, dtype=torch.uint8, device=grad.device)
+    _check(_ops().ssd_embed_grad(_DTYPES[grad.dtype], _DTYPES[out.dtype], tokens.data_ptr(), n, grad.data_ptr(),
+                                 _rows(what, "grad", grad), vocab, d, scale, int(accumulate), out.data_ptr(),
+                                 _rows(what, "out", out), work.data_ptr(), need, _raw_stream(dev)), what)
     return out
