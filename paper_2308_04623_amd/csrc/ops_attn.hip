@@ -41,10 +41,10 @@ struct PrefixAttnArgs {
   float* lse;
   float2* ml;   // [query][parts] (m, l) with query = (sequence, position, head)
   float* o;     // [query][parts][head_dim]
-  int p_tiles, p_chunks, p_chunk, p_blocks;  // query tiles and chunks of the prefix, its rows per chunk, its workgroups
+  int p_cols, p_tiles, p_chunks, p_chunk, p_blocks;  // of the prefix: queries per tile, tiles, chunks, rows per chunk, workgroups
   int o_tiles, o_chunks, o_chunk;            // of a sequence's own rows
   int parts;                                 // p_chunks + o_chunks
-  float scale2;                              // scale times log2 e
+  float scale2;                              // |scale| log2 e
 };
 
 constexpr int kWaves = 4;
@@ -67,24 +67,23 @@ struct Block {
   }
 };
 
-// Copies rows kb .. kb + KB - 1 of a range (those from `end` on: row end - 1
-// again) into the wave's LDS at dst.  By a whole wave; 2 LOADS copies in flight.
+// Copies the q-th KB of a block of keys (half 0) or values (1), rows kb .. of a
+// matrix (those from `end` on: row end - 1 again), into LDS at dst.  By a whole wave.
 template <typename T, int D>
-__device__ __forceinline__ void issue(const Range& s, int kb, int end, unsigned char* dst) {
+__device__ __forceinline__ void copy_1k(const char* base, int half, int q, int64_t row, int kb, int end,
+                                        unsigned char* dst, int lane) {
   typedef Block<T, D> B;
-  const int lane = threadIdx.x & 63;
+  const int p = q * 64 + lane, r = p / B::CH, c = (p % B::CH) ^ (half ? B::swz_v(r) : B::swz_k(r));
+  const char* src = base + (int64_t)min(kb + r, end - 1) * row + 16 * c;
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                   (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+}
+// the whole block; LOADS copies in flight
+template <typename T, int D, int HALF>
+__device__ __forceinline__ void issue(const Range& s, int kb, int end, unsigned char* dst) {
 #pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    const char* base = half ? s.v : s.k;
-#pragma unroll
-    for (int i = 0; i < B::LOADS; ++i) {
-      const int p = i * 64 + lane, r = p / B::CH, c = (p % B::CH) ^ (half ? B::swz_v(r) : B::swz_k(r));
-      const char* src = base + (int64_t)min(kb + r, end - 1) * s.row + 16 * c;
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
-                                       (__attribute__((address_space(3))) void*)(dst + half * B::BYTES + i * 1024), 16,
-                                       0, 0);
-    }
-  }
+  for (int i = 0; i < Block<T, D>::LOADS; ++i)
+    copy_1k<T, D>(HALF ? s.v : s.k, HALF, i, s.row, kb, end, dst + i * 1024, threadIdx.x & 63);
 }
 
 // the wave's copies but the last N are in LDS
@@ -281,8 +280,8 @@ __device__ __forceinline__ float value_at(const unsigned char* v, int r, int i) 
   return op_ld((const T*)(v + r * Block<T, D>::ROW + 16 * (c ^ Block<T, D>::swz_v(r))), i % (16 / (int)sizeof(T)));
 }
 
-// The queries of a tile of MT x 16 columns from `first` on: of the prefix, all
-// (sequence, position, group member) of kv head h; of own rows, sequence b's.
+// The queries of a tile from `first` on: of the prefix, all (sequence,
+// position, group member) of kv head h; of own rows, sequence b's.
 struct Queries {
   int h, b;     // b < 0: of every sequence
   int first, count;
@@ -295,61 +294,43 @@ struct Queries {
   }
 };
 
-// One workgroup's work: queries against rows [k0, k1) of a range, the part left
-// in slot `part`.  own: query t sees rows below len - n_query + 1 + t.
+// MT x 16 queries of a wave and what it has of their attention.
 template <typename T, int D, int MT>
-__device__ __forceinline__ void attend(const PrefixAttnArgs& a, const Queries& qs, const Range& range, int k0, int k1,
-                                       int len, int part, unsigned char* lds) {
+struct Wave {
   typedef Block<T, D> B;
   typedef Math<T, D, MT> M;
-  constexpr int KB = B::KB, KT = M::KT, KK = M::KK, DT = M::DT, STAGE = 2 * B::BYTES;
-  const ssd_prefix_attn_desc& d = a.d;
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
-  unsigned char* ring = lds + w * (2 * STAGE);
-  int kb = k0 + w * KB;
-  if (kb < k1) issue<T, D>(range, kb, k1, ring);
-  if (kb + kWaves * KB < k1) issue<T, D>(range, kb + kWaves * KB, k1, ring + STAGE);
-
+  static constexpr int KB = B::KB, KT = M::KT, KK = M::KK, DT = M::DT;
   u32x4 q[MT][KK];
-  int lim[MT];  // rows this lane's queries see end here
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt) {
-    int seq, t, head;
-    qs.split(d, min(qs.first + 16 * mt + n, qs.count - 1), seq, t, head);
-    const T* row = (const T*)a.q + (int64_t)seq * d.q_seq + (int64_t)t * d.q_row + (int64_t)head * d.q_head;
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk) q[mt][kk] = *((const u32x4*)row + 4 * kk + g);
-    lim[mt] = qs.b < 0 ? k1 : min(k1, len - d.n_query + 1 + t);
-  }
-  const int all = qs.b < 0 ? k1 : min(k1, len - d.n_query + 1);  // rows below are seen by every query
-
   f32x4 o[MT][DT];
   float m[MT], l[MT];
+  int pos[MT];  // of this lane's queries
+
+  __device__ __forceinline__ void load(const PrefixAttnArgs& a, const Queries& qs) {
+    const ssd_prefix_attn_desc& d = a.d;
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    // (a negative scale goes into the queries' signs: the largest score is then that of the largest product)
+    const unsigned sign = d.scale < 0.f ? (sizeof(T) == 2 ? 0x80008000u : 0x80000000u) : 0u;
 #pragma unroll
-  for (int mt = 0; mt < MT; ++mt) {
-    m[mt] = -INFINITY;
-    l[mt] = 0.f;
+    for (int mt = 0; mt < MT; ++mt) {
+      int seq, t, head;
+      qs.split(d, min(qs.first + 16 * mt + n, qs.count - 1), seq, t, head);
+      pos[mt] = t;
+      const T* row = (const T*)a.q + (int64_t)seq * d.q_seq + (int64_t)t * d.q_row + (int64_t)head * d.q_head;
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) o[mt][dt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+      for (int kk = 0; kk < KK; ++kk) q[mt][kk] = *((const u32x4*)row + 4 * kk + g) ^ sign;
+      m[mt] = -INFINITY;
+      l[mt] = 0.f;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[mt][dt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
   }
 
-  int buf = 0;
-  for (; kb < k1; kb += kWaves * KB, buf ^= 1) {
-    if (kb + kWaves * KB < k1) copies_landed<2 * B::LOADS>();
-    else copies_landed<0>();
-    const unsigned char *k = ring + buf * STAGE, *v = k + B::BYTES;
-    f32x4 s[MT][KT];
-    M::scores(k, q, s);
+  // the weights of rows kb .. of a block from their raw scores; lane's query mt
+  // sees rows below lim[mt], and every query those below `all`
+  __device__ __forceinline__ void weigh(f32x4 (&s)[MT][KT], int kb, int all, const int (&lim)[MT], float scale2,
+                                        typename M::P& p) {
+    const int g = (threadIdx.x & 63) >> 4;
     const bool masked = kb + KB > all;
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt) {
-        // (read here, in the products' own block: read past a branch, float32
-        // products of two tiles were taken before they were complete)
-        s[mt][kt] *= a.scale2;
-        asm volatile("" : "+v"(s[mt][kt]));
-      }
     if (masked) {
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
@@ -359,25 +340,23 @@ __device__ __forceinline__ void attend(const PrefixAttnArgs& a, const Queries& q
           for (int r = 0; r < 4; ++r)
             if (kb + 16 * kt + 4 * g + r >= lim[mt]) s[mt][kt][r] = -INFINITY;
     }
+    float top[MT];
     bool above = false;
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int mt = 0; mt < MT; ++mt) {
+      top[mt] = s[mt][0][0];
 #pragma unroll
-      for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) above |= s[mt][kt][r] > m[mt] + kSlack;
+      for (int i = 1; i < 4 * KT; ++i) top[mt] = fmaxf(top[mt], s[mt][i / 4][i % 4]);
+      above |= top[mt] * scale2 > m[mt] + kSlack;
+    }
     if (__builtin_amdgcn_ballot_w64(above)) {  // a new reference: the largest score so far
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
-        float top = m[mt];
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) top = fmaxf(top, s[mt][kt][r]);
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float c = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[mt] - top);
-        m[mt] = top;
+        float x = top[mt] == -INFINITY ? m[mt] : fmaxf(m[mt], top[mt] * scale2);
+        x = fmaxf(x, __shfl_xor(x, 16));
+        x = fmaxf(x, __shfl_xor(x, 32));
+        const float c = x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[mt] - x);
+        m[mt] = x;
         l[mt] *= c;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[mt][dt] *= c;
@@ -389,21 +368,46 @@ __device__ __forceinline__ void attend(const PrefixAttnArgs& a, const Queries& q
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          s[mt][kt][r] = __builtin_amdgcn_exp2f(s[mt][kt][r] - ref);
-          l[mt] += s[mt][kt][r];
-        }
+        for (int r = 0; r < 4; ++r) s[mt][kt][r] = __builtin_amdgcn_exp2f(fmaf(s[mt][kt][r], scale2, -ref));
     }
-    typename M::P p;
+    if (masked) {  // (whatever came of -infinity times a scale of 0)
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (kb + 16 * kt + 4 * g + r >= lim[mt]) s[mt][kt][r] = 0.f;
+    }
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) l[mt] += s[mt][kt][r];
     M::weights(s, p);
-    typename M::V x;
-    M::values(v, x);
+  }
+
+  __device__ __forceinline__ void scores(const unsigned char* k, f32x4 (&s)[MT][KT]) const {
+    M::scores(k, q, s);
+    // (read here, in the products' own block: read past a branch, float32
+    // products of two tiles were taken before they were complete)
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) asm volatile("" : "+v"(s[mt][kt]));
+  }
+
+  // adds the values of a block, x read from v.  A weight of 0 does not silence
+  // an infinity or NaN: in blocks that some query does not see to the end those
+  // values are added to the queries that see their rows.
+  __device__ __forceinline__ void add(typename M::V& x, const unsigned char* v, const typename M::P& p, int kb,
+                                      bool masked, const int (&lim)[MT]) {
     bool bad = false;
     if (masked) bad = M::clear(x);
     M::add(x, p, o);
     if (masked && __builtin_amdgcn_ballot_w64(bad)) {
-      // weights of 0 do not silence an infinity or NaN: those values are added to
-      // the queries that see their rows
+      const int g = (threadIdx.x & 63) >> 4;
       for (int r = 0; r < KB; ++r)
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
@@ -417,64 +421,219 @@ __device__ __forceinline__ void attend(const PrefixAttnArgs& a, const Queries& q
             }
           }
     }
-    if (kb + 2 * kWaves * KB < k1) {
-      // (the block's reads are over: their results went into the products above)
-      __builtin_amdgcn_sched_barrier(0);
-      __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
-      asm volatile("" ::: "memory");
-      issue<T, D>(range, kb + 2 * kWaves * KB, k1, ring + buf * STAGE);
-    }
   }
 
-  // the four waves' sums, through LDS: a wave's area of the ring holds its o
-  // (columns of D floats), as large as it needs with 4 query tiles
-  static_assert(MT * 16 * D * 4 <= 2 * STAGE, "a wave's outputs fit its part of the ring");
-  __shared__ float ref_s[kWaves][MT * 16], sum_s[kWaves][MT * 16];
+  // the sums of l over the lanes of a query
+  __device__ __forceinline__ void close() {
 #pragma unroll
-  for (int mt = 0; mt < MT; ++mt) {
-    l[mt] += __shfl_xor(l[mt], 16);
-    l[mt] += __shfl_xor(l[mt], 32);
-    if (g == 0) {
-      ref_s[w][16 * mt + n] = m[mt];
-      sum_s[w][16 * mt + n] = l[mt];
+    for (int mt = 0; mt < MT; ++mt) {
+      l[mt] += __shfl_xor(l[mt], 16);
+      l[mt] += __shfl_xor(l[mt], 32);
     }
   }
+};
+
+// a query's place among all (sequence, position, head)
+__device__ __forceinline__ size_t query_of(const ssd_prefix_attn_desc& d, int seq, int t, int head) {
+  return ((size_t)seq * d.n_query + t) * d.n_head + head;
+}
+
+__device__ __forceinline__ void reads_over() {
+  // the wave's LDS reads so far are complete: what they read may be overwritten
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// ---- few queries: the waves of a workgroup take the blocks of rows in turn
+
+// A wave's share of rows [k0, k1) of a range: blocks w, w + kWaves, ...  One
+// block of keys and one of values are in LDS; the next keys are fetched when this
+// block's scores are there, the next values when its values are in registers.
+// own: query t sees rows below len - n_query + 1 + t.
+template <typename T, int D, int MT>
+__device__ __forceinline__ void walk(Wave<T, D, MT>& s, const Range& range, int k0, int k1, bool own, int len,
+                                     int n_query, float scale2, unsigned char* lds) {
+  typedef Wave<T, D, MT> W;
+  typedef Block<T, D> B;
+  constexpr int KB = W::KB, STEP = kWaves * KB;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  unsigned char *k = lds + w * (2 * B::BYTES), *v = k + B::BYTES;
+  int lim[MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) lim[mt] = own ? min(k1, len - n_query + 1 + s.pos[mt]) : k1;
+  const int all = own ? min(k1, len - n_query + 1) : k1;
+  int kb = k0 + w * KB;
+  if (kb < k1) {
+    issue<T, D, 0>(range, kb, k1, k);
+    issue<T, D, 1>(range, kb, k1, v);
+  }
+  for (; kb < k1; kb += STEP) {
+    const bool more = kb + STEP < k1;
+    copies_landed<B::LOADS>();  // (the values may be under way)
+    f32x4 x[MT][W::KT];
+    s.scores(k, x);
+    if (more) {
+      reads_over();
+      issue<T, D, 0>(range, kb + STEP, k1, k);
+    }
+    typename W::M::P p;
+    s.weigh(x, kb, all, lim, scale2, p);
+    if (more) copies_landed<B::LOADS>();  // (the next keys may be)
+    else copies_landed<0>();
+    typename W::M::V f;
+    W::M::values(v, f);
+    s.add(f, v, p, kb, kb + KB > all, lim);
+    if (more) {
+      reads_over();
+      issue<T, D, 1>(range, kb + STEP, k1, v);
+    }
+  }
+}
+
+// Joins the four waves' sums through LDS (a wave's blocks are over): calls
+// put(column, dim / 4, four dims, reference, sum) once for each.
+template <typename T, int D, int MT, typename Put>
+__device__ __forceinline__ void join_waves(Wave<T, D, MT>& s, const Queries& qs, unsigned char* lds, Put put) {
+  typedef Wave<T, D, MT> W;
+  constexpr int AREA = 2 * Block<T, D>::BYTES, Q4 = D / 4;
+  static_assert(MT * 16 * D * 4 <= AREA, "a wave's outputs fit its part of the LDS");
+  __shared__ float ref_s[kWaves][MT * 16], sum_s[kWaves][MT * 16];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
+  s.close();
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+    if (g == 0) {
+      ref_s[w][16 * mt + n] = s.m[mt];
+      sum_s[w][16 * mt + n] = s.l[mt];
+    }
   __syncthreads();
-  float* mine = (float*)ring;
+  float* mine = (float*)(lds + w * AREA);
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) {
     float top = ref_s[0][16 * mt + n];
 #pragma unroll
     for (int i = 1; i < kWaves; ++i) top = fmaxf(top, ref_s[i][16 * mt + n]);
-    const float c = m[mt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[mt] - top);
+    const float c = s.m[mt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.m[mt] - top);
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) *(f32x4*)(mine + (16 * mt + n) * D + 16 * dt + 4 * g) = o[mt][dt] * c;
+    for (int dt = 0; dt < W::DT; ++dt) *(f32x4*)(mine + (16 * mt + n) * D + 16 * dt + 4 * g) = s.o[mt][dt] * c;
   }
   __syncthreads();
-  constexpr int Q4 = D / 4;
   for (int i = threadIdx.x; i < MT * 16 * Q4; i += 64 * kWaves) {
     const int col = i / Q4, x = i - col * Q4;
     if (qs.first + col >= qs.count) break;
-    int seq, t, head;
-    qs.split(d, qs.first + col, seq, t, head);
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    float top = ref_s[0][col], total = 0.f;
 #pragma unroll
-    for (int j = 0; j < kWaves; ++j) sum += *(const f32x4*)(lds + j * (2 * STAGE) + (size_t)(col * D + 4 * x) * 4);
-    const size_t slot = ((size_t)((size_t)seq * d.n_query + t) * d.n_head + head) * a.parts + part;
-    *(f32x4*)(a.o + slot * D + 4 * x) = sum;
-    if (x == 0) {
-      float top = ref_s[0][col], total = 0.f;
+    for (int j = 1; j < kWaves; ++j) top = fmaxf(top, ref_s[j][col]);
 #pragma unroll
-      for (int j = 1; j < kWaves; ++j) top = fmaxf(top, ref_s[j][col]);
-#pragma unroll
-      for (int j = 0; j < kWaves; ++j)
-        total += ref_s[j][col] == -INFINITY ? 0.f : sum_s[j][col] * __builtin_amdgcn_exp2f(ref_s[j][col] - top);
-      a.ml[slot] = make_float2(top, total);
+    for (int j = 0; j < kWaves; ++j) {
+      sum += *(const f32x4*)(lds + j * AREA + (size_t)(col * D + 4 * x) * 4);
+      total += ref_s[j][col] == -INFINITY ? 0.f : sum_s[j][col] * __builtin_amdgcn_exp2f(ref_s[j][col] - top);
     }
+    put(col, x, sum, top, total);
   }
 }
 
-template <typename T, int D, int MP, int MO>
+// One part: queries against rows [k0, k1) of a range.
+template <typename T, int D, int MT>
+__device__ __forceinline__ void part_by_rows(const PrefixAttnArgs& a, const Queries& qs, const Range& range, int k0,
+                                             int k1, int len, int part, unsigned char* lds) {
+  Wave<T, D, MT> s;
+  s.load(a, qs);
+  walk(s, range, k0, k1, qs.b >= 0, len, a.d.n_query, a.scale2, lds);
+  join_waves(s, qs, lds, [&](int col, int x, f32x4 sum, float top, float total) {
+    int seq, t, head;
+    qs.split(a.d, qs.first + col, seq, t, head);
+    const size_t slot = query_of(a.d, seq, t, head) * a.parts + part;
+    *(f32x4*)(a.o + slot * D + 4 * x) = sum;
+    if (x == 0) a.ml[slot] = make_float2(top, total);
+  });
+}
+
+// ---- many queries: the waves take MT x 16 of them each and share the blocks
+
+constexpr int kStages = 3;
+// A stage of kStageBytes holds SUB blocks; each wave copies a quarter of it.
+template <typename T, int D>
+struct Stage {
+  typedef Block<T, D> B;
+  static constexpr int SUB = 128 / D, ROWS = SUB * B::KB, BYTES = SUB * 2 * B::BYTES, PER = BYTES / 1024 / kWaves;
+  static_assert(BYTES == 16384 && PER == 4, "four copies a wave");
+  static __device__ __forceinline__ void issue(const Range& s, int kb, int end, unsigned char* dst) {
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int j = w * PER + i, sub = j / (2 * B::LOADS), half = j / B::LOADS % 2, q = j % B::LOADS;
+      copy_1k<T, D>(half ? s.v : s.k, half, q, s.row, kb + sub * B::KB, end, dst + j * 1024, lane);
+    }
+  }
+};
+
+template <typename T, int D, int MT>
+__device__ __forceinline__ void part_by_queries(const PrefixAttnArgs& a, Queries qs, const Range& range, int k0, int k1,
+                                                int part, unsigned char* lds) {
+  typedef Wave<T, D, MT> W;
+  typedef Block<T, D> B;
+  typedef Stage<T, D> S;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+  qs.first += w * (MT * 16);
+  const bool work = qs.first < qs.count;  // (a wave without queries still copies its share)
+  S::issue(range, k0, k1, lds);
+  if (k0 + S::ROWS < k1) S::issue(range, k0 + S::ROWS, k1, lds + S::BYTES);
+  W s;
+  s.load(a, qs);
+  int lim[MT];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) lim[mt] = k1;
+  int slot = 0;
+  for (int kb = k0; kb < k1; kb += S::ROWS) {
+    // this wave's copies of the stage are there; behind the barrier all waves'
+    // are, and no wave still reads the stage before, whose place the next copies take
+    if (kb + S::ROWS < k1) copies_landed<S::PER>();
+    else copies_landed<0>();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    int ahead = slot + 2;
+    if (ahead >= kStages) ahead -= kStages;
+    if (kb + 2 * S::ROWS < k1) S::issue(range, kb + 2 * S::ROWS, k1, lds + ahead * S::BYTES);
+    if (work) {
+#pragma unroll
+      for (int sub = 0; sub < S::SUB; ++sub) {
+        const int kr = kb + sub * B::KB;
+        if (sub && kr >= k1) break;
+        const unsigned char *k = lds + slot * S::BYTES + sub * (2 * B::BYTES), *v = k + B::BYTES;
+        f32x4 x[MT][W::KT];
+        s.scores(k, x);
+        typename W::M::P p;
+        s.weigh(x, kr, k1, lim, a.scale2, p);
+        typename W::M::V f;
+        W::M::values(v, f);
+        s.add(f, v, p, kr, kr + B::KB > k1, lim);
+      }
+      reads_over();
+    }
+    slot = slot + 1 == kStages ? 0 : slot + 1;
+  }
+  if (!work) return;
+  s.close();
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) {
+    const int i = qs.first + 16 * mt + n;
+    if (i >= qs.count) continue;
+    int seq, t, head;
+    qs.split(a.d, i, seq, t, head);
+    const size_t at = query_of(a.d, seq, t, head) * a.parts + part;
+#pragma unroll
+    for (int dt = 0; dt < W::DT; ++dt) *(f32x4*)(a.o + at * D + 16 * dt + 4 * g) = s.o[mt][dt];
+    if (g == 0) a.ml[at] = make_float2(s.m[mt], s.l[mt]);
+  }
+}
+
+// BYQ: the prefix's workgroups share their blocks among the waves (part_by_queries)
+template <typename T, int D, int MP, int MO, bool BYQ>
 __global__ __launch_bounds__(64 * kWaves) void prefix_attn_kernel(PrefixAttnArgs a) {
   extern __shared__ __align__(512) unsigned char lds[];  // (a block's rows lie at multiples of their size)
   const ssd_prefix_attn_desc& d = a.d;
@@ -494,7 +653,7 @@ __global__ __launch_bounds__(64 * kWaves) void prefix_attn_kernel(PrefixAttnArgs
     k1 = min(k0 + a.p_chunk, d.prefix_len);
     at = (int64_t)h * d.prefix_head;
     row = d.prefix_row;
-    qs = {h, -1, tile * MP * 16, d.n_seq * d.n_query * G};
+    qs = {h, -1, tile * a.p_cols, d.n_seq * d.n_query * G};
   } else {
     i -= a.p_blocks;
     const int c = i % a.o_chunks, tile = i / a.o_chunks % a.o_tiles, bh = i / (a.o_chunks * a.o_tiles);
@@ -510,8 +669,9 @@ __global__ __launch_bounds__(64 * kWaves) void prefix_attn_kernel(PrefixAttnArgs
   }
   const Range r = {(const char*)(shared ? a.kp : a.ko) + at * (int)sizeof(T),
                    (const char*)(shared ? a.vp : a.vo) + at * (int)sizeof(T), row * (int)sizeof(T)};
-  if (MP == MO || shared) attend<T, D, MP>(a, qs, r, k0, k1, len, part, lds);
-  else attend<T, D, MO>(a, qs, r, k0, k1, len, part, lds);
+  if (BYQ && shared) return part_by_queries<T, D, MP>(a, qs, r, k0, k1, part, lds);
+  if (BYQ || MP == MO || !shared) part_by_rows<T, D, MO>(a, qs, r, k0, k1, len, part, lds);
+  else part_by_rows<T, D, MP>(a, qs, r, k0, k1, len, part, lds);
 }
 
 // A wave per query adds its parts: lane l has dims 4 (l % (D / 4)) .. + 3 and every
@@ -588,14 +748,16 @@ ssd_status check_strides(const ssd_prefix_attn_desc* a) {
   return SSD_OK;
 }
 
-// How a call is cut up: query tiles of 16, 32 or 64 columns, as few as hold the
-// queries; chunks of the shared rows so that there are about kTarget workgroups
-// (several a CU: the last to finish leave little idle), none below a block for each wave.
+// How a call is cut up.  Up to 32 queries of a kv head: one tile, the waves
+// split the rows.  More: tiles of 64 or 128, the waves split the queries.  Chunks of
+// rows so that there are about kTarget workgroups (several a CU), none
+// below a block for each wave.
 constexpr int kTarget = 1024;
 
 struct Plan {
-  int mp, mo;  // matrix tiles per query tile
-  int p_tiles, p_chunks, p_chunk, p_blocks, o_tiles, o_chunks, o_chunk;
+  bool byq;    // see prefix_attn_kernel
+  int mp, mo;  // matrix tiles per wave
+  int p_cols, p_tiles, p_chunks, p_chunk, p_blocks, o_tiles, o_chunks, o_chunk;
   int64_t blocks;
   size_t o_bytes, bytes;
 };
@@ -611,9 +773,11 @@ Plan plan(const ssd_prefix_attn_desc* a) {
   Plan p{};
   const int G = a->n_head / a->n_kv_head, step = kWaves * (a->dtype == SSD_F32 ? 16 : 32);
   const int64_t cols = (int64_t)a->n_seq * a->n_query * G, own_cols = (int64_t)a->n_query * G;
-  p.mp = tile_of(cols, a->dtype == SSD_F32 ? 2 : 4);
+  p.byq = cols > 32;
+  p.mp = p.byq ? (cols > 64 ? 2 : 1) : tile_of(cols, 2);
   p.mo = tile_of(own_cols, 2);
-  p.p_tiles = (int)div_up(cols, 16 * p.mp);
+  p.p_cols = 16 * p.mp * (p.byq ? kWaves : 1);
+  p.p_tiles = (int)div_up(cols, p.p_cols);
   p.o_tiles = (int)div_up(own_cols, 16 * p.mo);
   auto cut = [&](int64_t rows, int64_t sets, int& chunks, int& chunk) {
     const int64_t want = std::min(std::max<int64_t>(kTarget / sets, 1), std::max<int64_t>(div_up(rows, step), 1));
@@ -630,35 +794,37 @@ Plan plan(const ssd_prefix_attn_desc* a) {
   return p;
 }
 
-template <typename T, int D, int MP, int MO>
+template <typename T, int D, int MP, int MO, bool BYQ>
 hipError_t launch(const PrefixAttnArgs& a, int64_t blocks, hipStream_t s) {
-  constexpr int lds = kWaves * 2 * 2 * Block<T, D>::BYTES;
-  // once per device: raises the kernel's limit of dynamic LDS
+  constexpr int rows = kWaves * 2 * Block<T, D>::BYTES, queries = kStages * Stage<T, D>::BYTES;
+  constexpr int lds = BYQ && queries > rows ? queries : rows;
+  // (once per device: more than 64 KB of LDS, with the kernel's own, has to be asked for)
   static std::atomic<uint64_t> ready{0};
   int dev = 0;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return e;
   const uint64_t bit = dev < 64 ? 1ull << dev : 0;
   if (!(ready.load(std::memory_order_acquire) & bit)) {
-    e = hipFuncSetAttribute((const void*)prefix_attn_kernel<T, D, MP, MO>,
+    e = hipFuncSetAttribute((const void*)prefix_attn_kernel<T, D, MP, MO, BYQ>,
                             hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
     ready.fetch_or(bit, std::memory_order_release);
   }
-  if (blocks > 0) prefix_attn_kernel<T, D, MP, MO><<<(unsigned)blocks, 64 * kWaves, lds, s>>>(a);
+  if (blocks > 0) prefix_attn_kernel<T, D, MP, MO, BYQ><<<(unsigned)blocks, 64 * kWaves, lds, s>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int queries = a.d.n_seq * a.d.n_query * a.d.n_head;
-  merge_kernel<T, D><<<(queries + 3) / 4, 256, 0, s>>>(a, queries);
+  const int n = a.d.n_seq * a.d.n_query * a.d.n_head;
+  merge_kernel<T, D><<<(n + 3) / 4, 256, 0, s>>>(a, n);
   return hipGetLastError();
 }
 template <typename T, int D>
 hipError_t launch(const PrefixAttnArgs& a, const Plan& p, hipStream_t s) {
-  if constexpr (sizeof(T) == 2) {
-    if (p.mp == 4) return p.mo == 2 ? launch<T, D, 4, 2>(a, p.blocks, s) : launch<T, D, 4, 1>(a, p.blocks, s);
+  if (p.byq) {
+    if (p.mp == 2) return p.mo == 2 ? launch<T, D, 2, 2, true>(a, p.blocks, s) : launch<T, D, 2, 1, true>(a, p.blocks, s);
+    return p.mo == 2 ? launch<T, D, 1, 2, true>(a, p.blocks, s) : launch<T, D, 1, 1, true>(a, p.blocks, s);
   }
-  if (p.mp >= 2) return p.mo == 2 ? launch<T, D, 2, 2>(a, p.blocks, s) : launch<T, D, 2, 1>(a, p.blocks, s);
-  return launch<T, D, 1, 1>(a, p.blocks, s);  // (a sequence has no more queries than all)
+  if (p.mp == 2) return p.mo == 2 ? launch<T, D, 2, 2, false>(a, p.blocks, s) : launch<T, D, 2, 1, false>(a, p.blocks, s);
+  return launch<T, D, 1, 1, false>(a, p.blocks, s);  // (a sequence has no more queries than all)
 }
 template <typename T>
 hipError_t launch(const PrefixAttnArgs& a, const Plan& p, hipStream_t s) {
@@ -713,6 +879,7 @@ extern "C" ssd_status ssd_prefix_attn(const ssd_prefix_attn_desc* a, const void*
   x.lse = lse;
   x.o = (float*)workspace;
   x.ml = (float2*)((char*)workspace + p.o_bytes);
+  x.p_cols = p.p_cols;
   x.p_tiles = p.p_tiles;
   x.p_chunks = p.p_chunks;
   x.p_chunk = p.p_chunk;
@@ -721,7 +888,7 @@ extern "C" ssd_status ssd_prefix_attn(const ssd_prefix_attn_desc* a, const void*
   x.o_chunks = p.o_chunks;
   x.o_chunk = p.o_chunk;
   x.parts = p.p_chunks + p.o_chunks;
-  x.scale2 = a->scale * 1.4426950408889634f;
+  x.scale2 = fabsf(a->scale) * 1.4426950408889634f;
   const hipError_t e = a->dtype == SSD_F32 ? launch<float>(x, p, (hipStream_t)stream) : launch<bf16_t>(x, p, (hipStream_t)stream);
   if (e != hipSuccess) return op_fail(SSD_E_DEVICE, hipGetErrorString(e));
   return SSD_OK;
