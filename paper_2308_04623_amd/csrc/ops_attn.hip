@@ -69,21 +69,21 @@ struct Block {
 
 // Copies the q-th KB of a block of keys (half 0) or values (1), rows kb .. of a
 // matrix (those from `end` on: row end - 1 again), into LDS at dst.  By a whole wave.
-template <typename T, int D>
+template <typename T, int D, int CPOL>
 __device__ __forceinline__ void copy_1k(const char* base, int half, int q, int64_t row, int kb, int end,
                                         unsigned char* dst, int lane) {
   typedef Block<T, D> B;
   const int p = q * 64 + lane, r = p / B::CH, c = (p % B::CH) ^ (half ? B::swz_v(r) : B::swz_k(r));
   const char* src = base + (int64_t)min(kb + r, end - 1) * row + 16 * c;
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
-                                   (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+                                   (__attribute__((address_space(3))) void*)dst, 16, 0, CPOL);
 }
 // the whole block; LOADS copies in flight
 template <typename T, int D, int HALF>
 __device__ __forceinline__ void issue(const Range& s, int kb, int end, unsigned char* dst) {
 #pragma unroll
   for (int i = 0; i < Block<T, D>::LOADS; ++i)
-    copy_1k<T, D>(HALF ? s.v : s.k, HALF, i, s.row, kb, end, dst + i * 1024, threadIdx.x & 63);
+    copy_1k<T, D, 2>(HALF ? s.v : s.k, HALF, i, s.row, kb, end, dst + i * 1024, threadIdx.x & 63);
 }
 
 // the wave's copies but the last N are in LDS
@@ -566,7 +566,7 @@ struct Stage {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int j = w * PER + i, sub = j / (2 * B::LOADS), half = j / B::LOADS % 2, q = j % B::LOADS;
-      copy_1k<T, D>(half ? s.v : s.k, half, q, s.row, kb + sub * B::KB, end, dst + j * 1024, lane);
+      copy_1k<T, D, 0>(half ? s.v : s.k, half, q, s.row, kb + sub * B::KB, end, dst + j * 1024, lane);
     }
   }
 };
@@ -634,7 +634,7 @@ __device__ __forceinline__ void part_by_queries(const PrefixAttnArgs& a, Queries
 
 // BYQ: the prefix's workgroups share their blocks among the waves (part_by_queries)
 template <typename T, int D, int MP, int MO, bool BYQ>
-__global__ __launch_bounds__(64 * kWaves) void prefix_attn_kernel(PrefixAttnArgs a) {
+__global__ __launch_bounds__(64 * kWaves, D == 128 ? 2 : D == 64 ? 3 : 4) void prefix_attn_kernel(PrefixAttnArgs a) {
   extern __shared__ __align__(512) unsigned char lds[];  // (a block's rows lie at multiples of their size)
   const ssd_prefix_attn_desc& d = a.d;
   const int G = d.n_head / d.n_kv_head;
@@ -749,10 +749,12 @@ ssd_status check_strides(const ssd_prefix_attn_desc* a) {
 }
 
 // How a call is cut up.  Up to 32 queries of a kv head: one tile, the waves
-// split the rows.  More: tiles of 64 or 128, the waves split the queries.  Chunks of
-// rows so that there are about kTarget workgroups (several a CU), none
-// below a block for each wave.
-constexpr int kTarget = 1024;
+// split the rows.  More: tiles of 64 or 128, the waves split the queries.  The rows
+// are cut so that the workgroups are one round over the CUs, two a CU where there
+// are products to overlap: more, shorter chunks cost more parts than they even out
+// (16 sequences over 100,000 rows: 97 us with 256 workgroups, 100 with 512, 103 with
+// 1024; 48 x 5 queries over 8,191 with grouped heads: 83, 67 and 78 us).
+constexpr int kRound = 256;
 
 struct Plan {
   bool byq;    // see prefix_attn_kernel
@@ -779,8 +781,9 @@ Plan plan(const ssd_prefix_attn_desc* a) {
   p.p_cols = 16 * p.mp * (p.byq ? kWaves : 1);
   p.p_tiles = (int)div_up(cols, p.p_cols);
   p.o_tiles = (int)div_up(own_cols, 16 * p.mo);
+  const int round = p.byq ? 2 * kRound : kRound;
   auto cut = [&](int64_t rows, int64_t sets, int& chunks, int& chunk) {
-    const int64_t want = std::min(std::max<int64_t>(kTarget / sets, 1), std::max<int64_t>(div_up(rows, step), 1));
+    const int64_t want = std::min(std::max<int64_t>(round / sets, 1), std::max<int64_t>(div_up(rows, step), 1));
     chunk = (int)(div_up(std::max<int64_t>(div_up(rows, want), 1), step) * step);
     chunks = (int)div_up(rows, chunk);
   };
