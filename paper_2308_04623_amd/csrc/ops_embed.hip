@@ -43,19 +43,25 @@ __device__ __forceinline__ f32x4 load4(const bf16_t* row, int c, int d) {
     if (c + i < d) r[i] = op_ld(row, c + i);
   return r;
 }
+// LAST: the row is not used again here and need not stay in the caches
+template <bool LAST = false>
 __device__ __forceinline__ void store4(float* row, int c, int d, f32x4 v) {
   if (c + 4 <= d) {
-    *(f32x4_a4*)(row + c) = v;
+    if (LAST) __builtin_nontemporal_store(v, (f32x4_a4*)(row + c));
+    else *(f32x4_a4*)(row + c) = v;
   } else {
 #pragma unroll
     for (int i = 0; i < 3; ++i)
       if (c + i < d) row[c + i] = v[i];
   }
 }
+template <bool LAST = false>
 __device__ __forceinline__ void store4(bf16_t* row, int c, int d, f32x4 v) {
   typedef __bf16 b4 __attribute__((ext_vector_type(4)));
   if (c + 4 <= d) {
-    *(u32x2_a2*)(row + c) = __builtin_bit_cast(u32x2, __builtin_convertvector(v, b4));
+    const u32x2 r = __builtin_bit_cast(u32x2, __builtin_convertvector(v, b4));
+    if (LAST) __builtin_nontemporal_store(r, (u32x2_a2*)(row + c));
+    else *(u32x2_a2*)(row + c) = r;
   } else {
 #pragma unroll
     for (int i = 0; i < 3; ++i)
@@ -88,42 +94,72 @@ struct Entry {
 
 __device__ __forceinline__ int key_of(int token, int V) { return token >= 0 && token < V ? token : V; }
 
-// Up to kRankMax positions: every position's rank is the number of those before
-// it in the order, counted by comparing all with all.  A workgroup ranks 64
-// positions (one per lane); its waves share out the others.
-constexpr int kRankMax = 8192, kRankThreads = 1024;
-__global__ __launch_bounds__(kRankThreads) void rank_kernel(const int* __restrict__ tokens, int N, int V,
-                                                            Entry* __restrict__ sorted) {
+// Up to kRunsMax positions: sorted runs, then every entry's place among all.
+// Within a run (all positions up to kOneRun, else kRun) an entry's rank is the number
+// of those before it, counted by comparing all with all: a workgroup ranks 64
+// positions, one per lane, and its waves share out the others.
+constexpr int kOneRun = 4096, kRun = 2048, kRunsMax = 131072, kRankThreads = 512;
+__global__ __launch_bounds__(kRankThreads) void rank_kernel(const int* __restrict__ tokens, int N, int V, int run,
+                                                            Entry* __restrict__ out) {
   constexpr int W = kRankThreads / 64;
-  __shared__ __align__(16) int keys[kRankMax];
+  __shared__ __align__(16) int keys[kOneRun];
   __shared__ int count[W][64];
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-  const int n4 = (N + 3) / 4;
-  for (int j = t; j < 4 * n4; j += kRankThreads) keys[j] = j < N ? key_of(tokens[j], V) : 0x7fffffff;
+  const int b = blockIdx.x * 64 / run * run, n = min(run, N - b), n4 = (n + 3) / 4;  // the run
+  for (int j = t; j < 4 * n4; j += kRankThreads) keys[j] = j < n ? key_of(tokens[b + j], V) : 0x7fffffff;
   __syncthreads();
-  const int i0 = blockIdx.x * 64, i = i0 + lane, key = i < N ? keys[i] : 0;
-  const int per = (n4 + W - 1) / W, from = w * per, to = min(n4, from + per);
+  const int i0 = blockIdx.x * 64 - b, i = i0 + lane, key = i < n ? keys[i] : 0;
+  const int per = (n4 + W - 1) / W, from = min(n4, w * per), to = min(n4, from + per);
+  const int first4 = min(to, max(from, i0 / 4)), last4 = max(from, min(to, i0 / 4 + 16));
+  const int4* k4 = (const int4*)keys;
   int c = 0;
-  for (int j4 = from; j4 < to; ++j4) {
-    const int4 k = ((const int4*)keys)[j4];
+#pragma unroll 4
+  for (int j4 = from; j4 < first4; ++j4) {  // all before this workgroup's positions
+    const int4 k = k4[j4];
+    c += (k.x <= key) + (k.y <= key) + (k.z <= key) + (k.w <= key);
+  }
+  for (int j4 = first4; j4 < last4; ++j4) {
+    const int4 k = k4[j4];
     const int j = 4 * j4;
-    if (j + 4 <= i0) {  // all before this workgroup's
-      c += (k.x <= key) + (k.y <= key) + (k.z <= key) + (k.w <= key);
-    } else if (j >= i0 + 64) {
-      c += (k.x < key) + (k.y < key) + (k.z < key) + (k.w < key);
-    } else {
-      c += (k.x < key || (k.x == key && j < i)) + (k.y < key || (k.y == key && j + 1 < i)) +
-           (k.z < key || (k.z == key && j + 2 < i)) + (k.w < key || (k.w == key && j + 3 < i));
-    }
+    c += (k.x < key || (k.x == key && j < i)) + (k.y < key || (k.y == key && j + 1 < i)) +
+         (k.z < key || (k.z == key && j + 2 < i)) + (k.w < key || (k.w == key && j + 3 < i));
+  }
+#pragma unroll 4
+  for (int j4 = last4; j4 < to; ++j4) {  // all after
+    const int4 k = k4[j4];
+    c += (k.x < key) + (k.y < key) + (k.z < key) + (k.w < key);
   }
   count[w][lane] = c;
   __syncthreads();
-  if (w == 0 && i < N) {
+  if (w == 0 && i < n) {
     int r = 0;
 #pragma unroll
     for (int k = 0; k < W; ++k) r += count[k][lane];
-    sorted[r] = (Entry){key, i};
+    out[b + r] = (Entry){key, b + i};
   }
+}
+
+// An entry's place: its own in its run, and in every other run the number of
+// lower keys, equal ones included in the runs before.  Eight threads an entry take
+// the runs in turn.
+__global__ __launch_bounds__(256) void merge_runs_kernel(const Entry* __restrict__ in, int N, Entry* __restrict__ out) {
+  const int e = (blockIdx.x * 256 + threadIdx.x) >> 3, sub = threadIdx.x & 7;
+  const int i = min(e, N - 1), mine = i / kRun, runs = (N + kRun - 1) / kRun;
+  const Entry x = in[i];
+  int place = 0;
+#pragma unroll 4
+  for (int r = sub; r < runs; r += 8) {
+    const Entry* s = in + (size_t)r * kRun;
+    const int n = min(kRun, N - r * kRun), key = r < mine ? x.key : x.key - 1;  // entries up to key come before
+    int lo = 0;
+#pragma unroll
+    for (int step = kRun; step > 0; step >>= 1)
+      if (lo + step <= n && s[lo + step - 1].key <= key) lo += step;
+    place += r == mine ? i - r * kRun : lo;
+  }
+#pragma unroll
+  for (int o = 1; o < 8; o <<= 1) place += __shfl_xor(place, o);
+  if (e < N && sub == 0) out[place] = x;
 }
 
 // More positions: a stable radix sort from the lowest digit up.  At most
@@ -258,24 +294,29 @@ struct GradArgs {
   int* open;           // [pieces]: the token whose earlier terms are in the pieces before and that ends here, or -1
 };
 
-// The merged sequence without the ends (accumulate): a piece is a run of entries.
-// With them (ACC false): entry j comes at j + key_j, as many ends before it as
-// there are lower tokens.  first(t): the entries before place t.
-template <bool ACC>
-__device__ __forceinline__ int first(const Entry* __restrict__ s, int N, int64_t t) {
-  if (ACC) return (int)min((int64_t)N, t);
+// The first of N entries for which `before` (true up to some entry) is false; by
+// a whole wave, which looks at 64 places at a time.
+template <typename P>
+__device__ __forceinline__ int search(int N, P before) {
   int lo = 0, hi = N;  // the answer is in [lo, hi]
   const int lane = threadIdx.x & 63;
-  while (lo < hi) {  // the wave looks at 64 places at a time
+  while (lo < hi) {
     const int step = (hi - lo + 63) / 64, j = lo + lane * step;
-    const bool before = j < hi && (int64_t)s[j].key + j < t;
-    const int k = __builtin_popcountll(__builtin_amdgcn_ballot_w64(before));  // (a prefix of the lanes)
+    const int k = __builtin_popcountll(__builtin_amdgcn_ballot_w64(j < hi && before(j)));
     if (k == 0) return lo;
     const int at = lo + (k - 1) * step;
     hi = min(hi, at + step);
     lo = at + 1;
   }
   return lo;
+}
+// The merged sequence without the ends (accumulate): a piece is a run of entries.
+// With them (ACC false): entry j comes at j + key_j, as many ends before it as
+// there are lower tokens.  first(t): the entries before place t.
+template <bool ACC>
+__device__ __forceinline__ int first(const Entry* __restrict__ s, int N, int64_t t) {
+  if (ACC) return (int)min((int64_t)N, t);
+  return search(N, [&](int j) { return (int64_t)s[j].key + j < t; });
 }
 
 template <typename G, typename T, bool ACC>
@@ -314,7 +355,7 @@ __global__ __launch_bounds__(1024) void embed_grad_kernel(GradArgs a) {
       T* row = table + (size_t)v * a.ld_table;
       f32x4 r = a.scale * acc;
       if (ACC) r += load4(row, c, a.d);
-      store4(row, c, a.d, r);
+      store4<true>(row, c, a.d, r);
     }
     cont = false;
     terms = 0;
@@ -370,12 +411,7 @@ template <typename T, bool ACC>
 __global__ __launch_bounds__(1024) void embed_join_kernel(GradArgs a) {
   const int g = blockIdx.x, v = a.open[g];
   if (v < 0) return;
-  int lo = 0, hi = a.N;  // the first entry of v
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (a.sorted[mid].key < v) lo = mid + 1;
-    else hi = mid;
-  }
+  const int lo = search(a.N, [&](int j) { return a.sorted[j].key < v; });  // the first entry of v
   const int from = (int)((ACC ? (int64_t)lo : (int64_t)lo + v) / a.items);
   const int c = 4 * (blockIdx.y * blockDim.x + threadIdx.x);
   if (c >= a.d) return;
@@ -413,11 +449,11 @@ Layout layout(int n, int vocab, int d) {
   };
   l.pieces = grad_pieces((int64_t)n + vocab);  // (no fewer than without the ends)
   l.entries[0] = take((size_t)n * sizeof(Entry));
-  if (n > kRankMax) {
+  if (n > kOneRun) l.entries[1] = take((size_t)n * sizeof(Entry));
+  if (n > kRunsMax) {
     l.run = sort_run(n);
     l.blocks = (n + l.run - 1) / l.run;
     l.passes = sort_passes(vocab);
-    l.entries[1] = take((size_t)n * sizeof(Entry));
     l.counts = take((size_t)l.passes * l.blocks * kBins * 4);
   }
   l.head = take((size_t)l.pieces * d * 4);
@@ -525,7 +561,7 @@ extern "C" ssd_status ssd_embed_grad(ssd_dtype grad_dtype, ssd_dtype table_dtype
   char* ws = (char*)workspace;
   hipStream_t s = (hipStream_t)stream;
   Entry *sorted = (Entry*)(ws + l.entries[0]), *other = (Entry*)(ws + l.entries[1]);
-  if (n > kRankMax) {
+  if (n > kRunsMax) {
     int* counts = (int*)(ws + l.counts);
     count_kernel<<<l.blocks, kSortThreads, 0, s>>>(tokens, n, vocab, l.run, l.passes, counts);
     OP_LAUNCHED();
@@ -538,8 +574,13 @@ extern "C" ssd_status ssd_embed_grad(ssd_dtype grad_dtype, ssd_dtype table_dtype
       OP_LAUNCHED();
     }
   } else if (n > 0) {
-    rank_kernel<<<(n + 63) / 64, kRankThreads, 0, s>>>(tokens, n, vocab, sorted);
+    const bool one = n <= kOneRun;
+    rank_kernel<<<(n + 63) / 64, kRankThreads, 0, s>>>(tokens, n, vocab, one ? kOneRun : kRun, one ? sorted : other);
     OP_LAUNCHED();
+    if (!one) {
+      merge_runs_kernel<<<(n + 31) / 32, 256, 0, s>>>(other, n, sorted);
+      OP_LAUNCHED();
+    }
   }
   const int64_t places = accumulate ? (int64_t)n : (int64_t)n + vocab;
   GradArgs a{};

@@ -124,6 +124,15 @@ def test_wide_vocabulary(env):
         assert (np.abs(got - ref) <= tol).all()
 
 
+@pytest.mark.parametrize("kind", ["even", "zipf", "one"])
+@pytest.mark.parametrize("n", [4095, 4096, 4097, 8191, 8193, 32769, 131072, 131073, 200001])
+def test_lengths_around_the_sorts(env, n, kind):
+    torch, ops = env
+    print(n, kind, flush=True)
+    gen = torch.Generator().manual_seed(n)
+    check_grad(torch, ops, "f32", "f32", draw_tokens(gen, torch, n, 3000, kind), torch.randn(n, 3, generator=gen), 3000)
+
+
 def test_no_tokens(env):
     torch, ops = env
     none, grad = torch.zeros(0, dtype=torch.int32, device="cuda"), torch.zeros(0, 24, device="cuda")
