@@ -20,6 +20,7 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 // callers' rows begin at any element
 typedef unsigned u32x2_a2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef unsigned u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
 
 // four columns of a row from column c on; the last ones of a row where fewer are left
@@ -71,18 +72,53 @@ __device__ __forceinline__ void store4(bf16_t* row, int c, int d, f32x4 v) {
 
 // ---------------------------------------------------------------- lookup
 
-// a thread per four columns of a row
+// eight columns of a row from column c on, as floats
+__device__ __forceinline__ void load8(const float* row, int c, int d, f32x4 (&v)[2]) {
+  v[0] = load4(row, c, d);
+  v[1] = load4(row, c + 4, d);
+}
+__device__ __forceinline__ void load8(const bf16_t* row, int c, int d, f32x4 (&v)[2]) {
+  if (c + 8 <= d) {
+    const u32x4 r = *(const u32x4_a2*)(row + c);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = __uint_as_float(i & 1 ? r[i >> 1] & 0xffff0000u : r[i >> 1] << 16);
+  } else {
+    v[0] = load4(row, c, d);
+    v[1] = load4(row, c + 4, d);
+  }
+}
+__device__ __forceinline__ void store8(float* row, int c, int d, const f32x4 (&v)[2]) {
+  store4(row, c, d, v[0]);
+  store4(row, c + 4, d, v[1]);
+}
+__device__ __forceinline__ void store8(bf16_t* row, int c, int d, const f32x4 (&v)[2]) {
+  typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+  if (c + 8 <= d) {
+    const u32x2 a = __builtin_bit_cast(u32x2, __builtin_convertvector(v[0], b4));
+    const u32x2 b = __builtin_bit_cast(u32x2, __builtin_convertvector(v[1], b4));
+    *(u32x4_a2*)(row + c) = (u32x4){a[0], a[1], b[0], b[1]};
+  } else {
+    store4(row, c, d, v[0]);
+    store4(row, c + 4, d, v[1]);
+  }
+}
+
+// a thread per eight columns of a row
 template <typename T, typename O>
-__global__ __launch_bounds__(256) void embed_rows_kernel(const int* __restrict__ tokens, int64_t quads, int per,
+__global__ __launch_bounds__(256) void embed_rows_kernel(const int* __restrict__ tokens, int64_t parts, int per,
                                                          const T* __restrict__ table, int64_t ld_table, int V, int d,
                                                          float scale, O* __restrict__ out, int64_t ld_out) {
   const int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (q >= quads) return;
+  if (q >= parts) return;
   const int64_t n = q / per;
-  const int c = 4 * (int)(q - n * per), tok = tokens[n];
-  f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  if (tok >= 0 && tok < V) v = scale * load4(table + (size_t)tok * ld_table, c, d);
-  store4(out + (size_t)n * ld_out, c, d, v);
+  const int c = 8 * (int)(q - n * per), tok = tokens[n];
+  f32x4 v[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+  if (tok >= 0 && tok < V) {
+    load8(table + (size_t)tok * ld_table, c, d, v);
+    v[0] *= scale;
+    v[1] *= scale;
+  }
+  store8(out + (size_t)n * ld_out, c, d, v);
 }
 
 // ---------------------------------------------------------------- sort by token
@@ -294,11 +330,10 @@ struct GradArgs {
   int* open;           // [pieces]: the token whose earlier terms are in the pieces before and that ends here, or -1
 };
 
-// The first of N entries for which `before` (true up to some entry) is false; by
-// a whole wave, which looks at 64 places at a time.
+// The first of entries lo .. hi - 1 for which `before` (true up to some entry) is
+// false, or hi; by a whole wave, which looks at 64 places at a time.
 template <typename P>
-__device__ __forceinline__ int search(int N, P before) {
-  int lo = 0, hi = N;  // the answer is in [lo, hi]
+__device__ __forceinline__ int search(int lo, int hi, P before) {
   const int lane = threadIdx.x & 63;
   while (lo < hi) {
     const int step = (hi - lo + 63) / 64, j = lo + lane * step;
@@ -310,52 +345,39 @@ __device__ __forceinline__ int search(int N, P before) {
   }
   return lo;
 }
-// The merged sequence without the ends (accumulate): a piece is a run of entries.
-// With them (ACC false): entry j comes at j + key_j, as many ends before it as
-// there are lower tokens.  first(t): the entries before place t.
-template <bool ACC>
-__device__ __forceinline__ int first(const Entry* __restrict__ s, int N, int64_t t) {
-  if (ACC) return (int)min((int64_t)N, t);
-  return search(N, [&](int j) { return (int64_t)s[j].key + j < t; });
+// Entry j comes at place j + key_j of the merged sequence, after as many ends as
+// there are lower tokens.  The entries before place t, known to be lo to hi.
+__device__ __forceinline__ int entries_before(const Entry* __restrict__ s, int lo, int hi, int64_t t) {
+  return search(lo, hi, [&](int j) { return (int64_t)s[j].key + j < t; });
 }
 
-template <typename G, typename T, bool ACC>
+constexpr int kInFlight = 8, kStaged = 512;  // rows in flight, entries in LDS at a time
+
+template <typename G, typename T>
 __global__ __launch_bounds__(1024) void embed_grad_kernel(GradArgs a) {
-  constexpr int U = 8;     // rows in flight
-  constexpr int L = 512;   // entries staged at a time
+  constexpr int U = kInFlight, L = kStaged;
   __shared__ Entry es[L];
   const int g = blockIdx.x, c = 4 * (blockIdx.y * blockDim.x + threadIdx.x);
-  const int64_t t0 = (int64_t)g * a.items, t1 = min(t0 + a.items, ACC ? (int64_t)a.N : (int64_t)a.N + a.V);
-  const int i0 = __builtin_amdgcn_readfirstlane(first<ACC>(a.sorted, a.N, t0));
-  const int i1 = __builtin_amdgcn_readfirstlane(first<ACC>(a.sorted, a.N, t1));
+  const int64_t t0 = (int64_t)g * a.items, t1 = min(t0 + a.items, (int64_t)a.N + a.V);
+  const int i0 = __builtin_amdgcn_readfirstlane(entries_before(a.sorted, 0, a.N, t0));
+  const int i1 =
+      __builtin_amdgcn_readfirstlane(entries_before(a.sorted, i0, (int)min((int64_t)a.N, i0 + (t1 - t0)), t1));
   const bool col = c < a.d;
   const G* grad = (const G*)a.grad;
   T* table = (T*)a.dtable;
   // v: the token whose end comes next; v1: ends from it on lie in later pieces
-  int v = ACC ? (i0 < i1 ? a.sorted[i0].key : a.V) : (int)(t0 - i0);
-  int v1;
-  if (ACC) {  // the last entry's token ends here unless the next piece goes on with it
-    v1 = i0 < i1 ? a.sorted[i1 - 1].key + 1 : 0;
-    if (i0 < i1 && i1 < a.N && a.sorted[i1].key == v1 - 1) v1 -= 1;
-  } else {
-    v1 = (int)(t1 - i1);
-  }
-  v = __builtin_amdgcn_readfirstlane(v);
-  v1 = __builtin_amdgcn_readfirstlane(min(v1, a.V));
+  int v = (int)(t0 - i0);
+  const int v1 = min((int)(t1 - i1), a.V);
   bool cont = i0 > 0 && v < a.V && a.sorted[i0 - 1].key == v;  // earlier terms of v lie in pieces before
-  int opened = -1;
-  int terms = 0;  // of v in this piece
+  int opened = -1, terms = 0;  // terms: of v in this piece
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 
   auto end = [&]() {  // the end of token v
     if (cont) {
       opened = v;
       if (col) store4(a.head + (size_t)g * a.d, c, a.d, acc);
-    } else if (col && (!ACC || terms)) {
-      T* row = table + (size_t)v * a.ld_table;
-      f32x4 r = a.scale * acc;
-      if (ACC) r += load4(row, c, a.d);
-      store4<true>(row, c, a.d, r);
+    } else if (col) {
+      store4<true>(table + (size_t)v * a.ld_table, c, a.d, a.scale * acc);
     }
     cont = false;
     terms = 0;
@@ -381,26 +403,70 @@ __global__ __launch_bounds__(1024) void embed_grad_kernel(GradArgs a) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         if (key[u] >= a.V) continue;
-        if (ACC) {
-          if (key[u] != v) {
-            end();
-            v = key[u];
-          }
-        } else {
-          for (; v < key[u]; ++v) end();
-        }
+        for (; v < key[u]; ++v) end();
         acc += r[u];
         ++terms;
       }
     }
   }
-  if (ACC) {
-    if (v < v1) {
-      end();
-      v = v1;
+  for (; v < v1; ++v) end();
+  if (terms && col) store4(a.tail + (size_t)g * a.d, c, a.d, acc);
+  if (blockIdx.y == 0 && threadIdx.x == 0) a.open[g] = opened;
+}
+
+// The same, added to the table: a piece is a run of entries, and the rows of the
+// table that end in it are loaded with the rows of the gradient.
+template <typename G, typename T>
+__global__ __launch_bounds__(1024) void embed_grad_add_kernel(GradArgs a) {
+  constexpr int U = kInFlight, L = kStaged;
+  __shared__ Entry es[L + 1];
+  const int g = blockIdx.x, c = 4 * (blockIdx.y * blockDim.x + threadIdx.x);
+  const int i0 = (int)min((int64_t)a.N, (int64_t)g * a.items), i1 = min(a.N, i0 + a.items);
+  const bool col = c < a.d;
+  const G* grad = (const G*)a.grad;
+  T* table = (T*)a.dtable;
+  bool cont = i0 > 0 && i0 < i1 && a.sorted[i0 - 1].key == a.sorted[i0].key;  // see embed_grad_kernel
+  int opened = -1, terms = 0;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int b0 = i0; b0 < i1; b0 += L) {
+    const int nb = min(L, i1 - b0);
+    __syncthreads();
+    // (and the entry after: the last one's token may end with it)
+    for (int j = threadIdx.x; j <= nb; j += blockDim.x) es[j] = b0 + j < a.N ? a.sorted[b0 + j] : (Entry){a.V, 0};
+    __syncthreads();
+    for (int j0 = 0; j0 < nb; j0 += U) {
+      f32x4 r[U], old[U];
+      int key[U];
+      bool ends[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int j = min(j0 + u, nb - 1);
+        key[u] = j0 + u < nb ? __builtin_amdgcn_readfirstlane(es[j].key) : a.V;
+        ends[u] = key[u] != __builtin_amdgcn_readfirstlane(es[j + 1].key);
+        const int pos = __builtin_amdgcn_readfirstlane(es[j].pos);
+        r[u] = old[u] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        if (col && key[u] < a.V) {
+          r[u] = load4(grad + (size_t)pos * a.ld_grad, c, a.d);
+          if (ends[u]) old[u] = load4(table + (size_t)key[u] * a.ld_table, c, a.d);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (key[u] >= a.V) continue;
+        acc += r[u];
+        ++terms;
+        if (!ends[u]) continue;
+        if (cont) {
+          opened = key[u];
+          if (col) store4(a.head + (size_t)g * a.d, c, a.d, acc);
+        } else if (col) {
+          store4(table + (size_t)key[u] * a.ld_table, c, a.d, old[u] + a.scale * acc);
+        }
+        cont = false;
+        terms = 0;
+        acc = (f32x4){0.f, 0.f, 0.f, 0.f};
+      }
     }
-  } else {
-    for (; v < v1; ++v) end();
   }
   if (terms && col) store4(a.tail + (size_t)g * a.d, c, a.d, acc);
   if (blockIdx.y == 0 && threadIdx.x == 0) a.open[g] = opened;
@@ -411,7 +477,7 @@ template <typename T, bool ACC>
 __global__ __launch_bounds__(1024) void embed_join_kernel(GradArgs a) {
   const int g = blockIdx.x, v = a.open[g];
   if (v < 0) return;
-  const int lo = search(a.N, [&](int j) { return a.sorted[j].key < v; });  // the first entry of v
+  const int lo = search(0, a.N, [&](int j) { return a.sorted[j].key < v; });  // the first entry of v
   const int from = (int)((ACC ? (int64_t)lo : (int64_t)lo + v) / a.items);
   const int c = 4 * (blockIdx.y * blockDim.x + threadIdx.x);
   if (c >= a.d) return;
@@ -427,9 +493,9 @@ __global__ __launch_bounds__(1024) void embed_join_kernel(GradArgs a) {
 
 constexpr int kMaxPieces = 2048;
 
-// pieces of the merged sequence: 8 a CU, fewer where a piece would have under 16 places
+// pieces of the merged sequence: 8 a CU, fewer where a piece would have under 4 places
 int grad_pieces(int64_t places) {
-  const int64_t p = (places + 15) / 16;
+  const int64_t p = (places + 3) / 4;
   return (int)(p < 1 ? 1 : p > kMaxPieces ? kMaxPieces : p);
 }
 
@@ -468,7 +534,8 @@ void launch_grad(const GradArgs& a, hipStream_t s) {
   // threads of four columns each: whole waves, at most 1024
   const int quads = (a.d + 3) / 4, threads = quads >= 1024 ? 1024 : (quads + 63) / 64 * 64;
   const dim3 grid(a.pieces, (quads + threads - 1) / threads);
-  embed_grad_kernel<G, T, ACC><<<grid, threads, 0, s>>>(a);
+  if (ACC) embed_grad_add_kernel<G, T><<<grid, threads, 0, s>>>(a);
+  else embed_grad_kernel<G, T><<<grid, threads, 0, s>>>(a);
   embed_join_kernel<T, ACC><<<grid, threads, 0, s>>>(a);
 }
 template <typename G, typename T>
@@ -492,14 +559,14 @@ ssd_status check(int32_t n, int32_t vocab, int32_t d) {
 template <typename T>
 void launch_embed_rows(int out_dtype, const int* tokens, int n, const void* table, int64_t ld_table, int V, int d,
                        float scale, void* out, int64_t ld_out, hipStream_t s) {
-  const int per = (d + 3) / 4;
-  const int64_t quads = (int64_t)n * per;
-  const unsigned grid = (unsigned)((quads + 255) / 256);
+  const int per = (d + 7) / 8;
+  const int64_t parts = (int64_t)n * per;
+  const unsigned grid = (unsigned)((parts + 255) / 256);
   if (out_dtype == SSD_F32)
-    embed_rows_kernel<<<grid, 256, 0, s>>>(tokens, quads, per, (const T*)table, ld_table, V, d, scale, (float*)out,
+    embed_rows_kernel<<<grid, 256, 0, s>>>(tokens, parts, per, (const T*)table, ld_table, V, d, scale, (float*)out,
                                            ld_out);
   else
-    embed_rows_kernel<<<grid, 256, 0, s>>>(tokens, quads, per, (const T*)table, ld_table, V, d, scale, (bf16_t*)out,
+    embed_rows_kernel<<<grid, 256, 0, s>>>(tokens, parts, per, (const T*)table, ld_table, V, d, scale, (bf16_t*)out,
                                            ld_out);
 }
 
