@@ -7,9 +7,12 @@
 // in a fixed order), then walks the merged sequence
 //   rows of token 0, end of 0, rows of token 1, end of 1, ...
 // in which a position is a row of g to read and an end a row of dW to write.  It is cut
-// into equal pieces whatever the tokens' frequencies; a piece that begins or
-// ends inside a token's rows leaves a partial sum, and a second kernel adds
-// these up.  Bound: memory (g read once, dW written once).
+// into equal pieces whatever the tokens' frequencies.  A cut inside the rows of a
+// token with few of them is moved behind its end; the rows of a frequent token
+// are cut, its pieces leave partial sums, and a second kernel adds these up.
+// Bound: memory (g read once, dW written once).
+#include <algorithm>
+
 #include "ops_common.h"
 
 namespace ssd {
@@ -330,45 +333,94 @@ struct GradArgs {
   int* open;           // [pieces]: the token whose earlier terms are in the pieces before and that ends here, or -1
 };
 
-// The first of entries lo .. hi - 1 for which `before` (true up to some entry) is
-// false, or hi; by a whole wave, which looks at 64 places at a time.
+// The first of lo .. hi - 1 for which `before` (true up to some place) is false, or
+// hi; by a whole wave, which looks at 64 places at a time.  Stops with a range
+// of at most `near` places that holds it (or its end).
 template <typename P>
-__device__ __forceinline__ int search(int lo, int hi, P before) {
+__device__ __forceinline__ void narrow(int& lo, int& hi, int near, P before) {
   const int lane = threadIdx.x & 63;
-  while (lo < hi) {
+  while (hi - lo > near) {
     const int step = (hi - lo + 63) / 64, j = lo + lane * step;
     const int k = __builtin_popcountll(__builtin_amdgcn_ballot_w64(j < hi && before(j)));
-    if (k == 0) return lo;
-    const int at = lo + (k - 1) * step;
-    hi = min(hi, at + step);
-    lo = at + 1;
+    if (k == 0) {
+      hi = lo;
+    } else {
+      const int at = lo + (k - 1) * step;
+      hi = min(hi, at + step);
+      lo = at + 1;
+    }
   }
-  return lo;
-}
-// Entry j comes at place j + key_j of the merged sequence, after as many ends as
-// there are lower tokens.  The entries before place t, known to be lo to hi.
-__device__ __forceinline__ int entries_before(const Entry* __restrict__ s, int lo, int hi, int64_t t) {
-  return search(lo, hi, [&](int j) { return (int64_t)s[j].key + j < t; });
 }
 
-constexpr int kInFlight = 8, kStaged = 512;  // rows in flight, entries in LDS at a time
+constexpr int kInFlight = 8;  // rows in flight
+// Entries in LDS, from place `base` on; others are read where they are.
+constexpr int kStaged = 512;
+struct Staged {
+  const Entry* all;
+  Entry* lds;
+  int base, n;
+  __device__ __forceinline__ Entry at(int j) const {
+    const int k = j - base;
+    return (unsigned)k < (unsigned)n ? lds[k] : all[j];
+  }
+  // by the whole workgroup
+  __device__ __forceinline__ void stage(int from, int to) {
+    base = from;
+    n = min(kStaged, to - from);
+    __syncthreads();
+    for (int k = threadIdx.x; k < n; k += blockDim.x) lds[k] = all[from + k];
+    __syncthreads();
+  }
+};
+
+// A cut before entry i among the rows of token v, some of which come before it: if
+// v has no more than kShort rows, how many come after it; else -1.  By a whole wave.
+constexpr int kShort = 32;
+__device__ __forceinline__ int rows_after(const Staged& s, int N, int i, int v) {
+  const int j = i - 32 + (int)(threadIdx.x & 63);
+  const unsigned long long same = __builtin_amdgcn_ballot_w64(j >= 0 && j < N && s.at(j).key == v);
+  const int n = __builtin_popcountll(same);
+  // (with kShort rows at most and one of them before the cut, all are seen)
+  const bool more = i + 32 < N && same >> 63 && s.at(i + 32).key == v;
+  const bool less = i > 32 && (same & 1) && s.at(i - 33).key == v;
+  return n <= kShort && !more && !less ? __builtin_popcountll(same >> 32) : -1;
+}
 
 template <typename G, typename T>
 __global__ __launch_bounds__(1024) void embed_grad_kernel(GradArgs a) {
-  constexpr int U = kInFlight, L = kStaged;
-  __shared__ Entry es[L];
-  const int g = blockIdx.x, c = 4 * (blockIdx.y * blockDim.x + threadIdx.x);
+  constexpr int U = kInFlight;
+  __shared__ Entry lds[kStaged];
+  Staged es = {a.sorted, lds, 0, 0};
+  const int g = blockIdx.x, c = 4 * (blockIdx.y * blockDim.x + threadIdx.x), lane = threadIdx.x & 63;
+  // The piece is places t0 .. t1 - 1: entry j comes at place j + key_j, after as
+  // many ends as there are lower tokens.  i0, v: the entries and ends before it;
+  // i1, v1: before the next.  What is looked at around them is staged at once, the
+  // entries themselves included unless they are many.
   const int64_t t0 = (int64_t)g * a.items, t1 = min(t0 + a.items, (int64_t)a.N + a.V);
-  const int i0 = __builtin_amdgcn_readfirstlane(entries_before(a.sorted, 0, a.N, t0));
-  const int i1 =
-      __builtin_amdgcn_readfirstlane(entries_before(a.sorted, i0, (int)min((int64_t)a.N, i0 + (t1 - t0)), t1));
+  int lo = 0, hi = a.N;
+  narrow(lo, hi, 64, [&](int j) { return (int64_t)a.sorted[j].key + j < t0; });
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  hi = __builtin_amdgcn_readfirstlane(hi);
+  es.stage(max(0, lo - 33), (int)min((int64_t)a.N, (int64_t)hi + a.items + 34));
+  auto before = [&](int from, int to, int64_t t) {  // the first of from .. to at place t or behind
+    narrow(from, to, 0, [&](int j) { return (int64_t)es.at(j).key + j < t; });
+    return __builtin_amdgcn_readfirstlane(from);
+  };
+  int i0 = before(lo, hi, t0), v = (int)(t0 - i0);
+  int i1 = before(i0, (int)min((int64_t)a.N, i0 + (t1 - t0)), t1), v1 = min((int)(t1 - i1), a.V);
+  auto move = [&](int& i, int& end) {
+    if (i == 0 || end >= a.V || __builtin_amdgcn_readfirstlane(es.at(i - 1).key) != end) return false;
+    const int n = __builtin_amdgcn_readfirstlane(rows_after(es, a.N, i, end));
+    if (n < 0) return true;  // the token's rows are cut here
+    i += n;
+    end += 1;
+    return false;
+  };
+  bool cont = move(i0, v);  // earlier terms of v lie in pieces before
+  move(i1, v1);
   const bool col = c < a.d;
   const G* grad = (const G*)a.grad;
   T* table = (T*)a.dtable;
-  // v: the token whose end comes next; v1: ends from it on lie in later pieces
-  int v = (int)(t0 - i0);
-  const int v1 = min((int)(t1 - i1), a.V);
-  bool cont = i0 > 0 && v < a.V && a.sorted[i0 - 1].key == v;  // earlier terms of v lie in pieces before
   int opened = -1, terms = 0;  // terms: of v in this piece
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 
@@ -384,29 +436,25 @@ __global__ __launch_bounds__(1024) void embed_grad_kernel(GradArgs a) {
     acc = (f32x4){0.f, 0.f, 0.f, 0.f};
   };
 
-  for (int b0 = i0; b0 < i1; b0 += L) {
-    const int nb = min(L, i1 - b0);
-    __syncthreads();
-    for (int j = threadIdx.x; j < nb; j += blockDim.x) es[j] = a.sorted[b0 + j];
-    __syncthreads();
-    for (int j0 = 0; j0 < nb; j0 += U) {
-      f32x4 r[U];
-      int key[U];
+  for (int j0 = i0; j0 < i1; j0 += U) {
+    if (min(j0 + U, i1) > es.base + es.n) es.stage(j0, i1);
+    f32x4 r[U];
+    int key[U];
+    // (the entries first, a lane each: one read)
+    const Entry e = es.at(min(j0 + (lane & (U - 1)), i1 - 1));
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int j = min(j0 + u, nb - 1);
-        key[u] = j0 + u < nb ? __builtin_amdgcn_readfirstlane(es[j].key) : a.V;
-        const int pos = __builtin_amdgcn_readfirstlane(es[j].pos);
-        r[u] = (f32x4){0.f, 0.f, 0.f, 0.f};
-        if (col && key[u] < a.V) r[u] = load4(grad + (size_t)pos * a.ld_grad, c, a.d);
-      }
+    for (int u = 0; u < U; ++u) {
+      key[u] = j0 + u < i1 ? __builtin_amdgcn_readlane(e.key, u) : a.V;
+      const int pos = __builtin_amdgcn_readlane(e.pos, u);
+      r[u] = (f32x4){0.f, 0.f, 0.f, 0.f};
+      if (col && key[u] < a.V) r[u] = load4(grad + (size_t)pos * a.ld_grad, c, a.d);
+    }
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (key[u] >= a.V) continue;
-        for (; v < key[u]; ++v) end();
-        acc += r[u];
-        ++terms;
-      }
+    for (int u = 0; u < U; ++u) {
+      if (key[u] >= a.V) continue;
+      for (; v < key[u]; ++v) end();
+      acc += r[u];
+      ++terms;
     }
   }
   for (; v < v1; ++v) end();
@@ -418,85 +466,125 @@ __global__ __launch_bounds__(1024) void embed_grad_kernel(GradArgs a) {
 // table that end in it are loaded with the rows of the gradient.
 template <typename G, typename T>
 __global__ __launch_bounds__(1024) void embed_grad_add_kernel(GradArgs a) {
-  constexpr int U = kInFlight, L = kStaged;
-  __shared__ Entry es[L + 1];
-  const int g = blockIdx.x, c = 4 * (blockIdx.y * blockDim.x + threadIdx.x);
-  const int i0 = (int)min((int64_t)a.N, (int64_t)g * a.items), i1 = min(a.N, i0 + a.items);
+  constexpr int U = kInFlight;
+  __shared__ Entry lds[kStaged];
+  Staged es = {a.sorted, lds, 0, 0};
+  const int g = blockIdx.x, c = 4 * (blockIdx.y * blockDim.x + threadIdx.x), lane = threadIdx.x & 63;
+  int i0 = (int)min((int64_t)a.N, (int64_t)g * a.items), i1 = min(a.N, i0 + a.items);
+  es.stage(max(0, i0 - 33), (int)min((int64_t)a.N, (int64_t)i1 + 34));
+  auto move = [&](int& i) {  // see embed_grad_kernel
+    if (i == 0 || i >= a.N) return false;
+    const int key = __builtin_amdgcn_readfirstlane(es.at(i).key);
+    if (key >= a.V || __builtin_amdgcn_readfirstlane(es.at(i - 1).key) != key) return false;
+    const int n = __builtin_amdgcn_readfirstlane(rows_after(es, a.N, i, key));
+    if (n < 0) return true;
+    i += n;
+    return false;
+  };
+  bool cont = move(i0);
+  move(i1);
   const bool col = c < a.d;
   const G* grad = (const G*)a.grad;
   T* table = (T*)a.dtable;
-  bool cont = i0 > 0 && i0 < i1 && a.sorted[i0 - 1].key == a.sorted[i0].key;  // see embed_grad_kernel
   int opened = -1, terms = 0;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int b0 = i0; b0 < i1; b0 += L) {
-    const int nb = min(L, i1 - b0);
-    __syncthreads();
+  for (int j0 = i0; j0 < i1; j0 += U) {
     // (and the entry after: the last one's token may end with it)
-    for (int j = threadIdx.x; j <= nb; j += blockDim.x) es[j] = b0 + j < a.N ? a.sorted[b0 + j] : (Entry){a.V, 0};
-    __syncthreads();
-    for (int j0 = 0; j0 < nb; j0 += U) {
-      f32x4 r[U], old[U];
-      int key[U];
-      bool ends[U];
+    if (min(min(j0 + U, i1) + 1, a.N) > es.base + es.n) es.stage(j0, min(a.N, i1 + 1));
+    f32x4 r[U], old[U];
+    int key[U];
+    bool ends[U];
+    const int j = j0 + (lane & (2 * U - 1));
+    const Entry e = j <= i1 && j < a.N ? es.at(j) : (Entry){a.V, 0};
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int j = min(j0 + u, nb - 1);
-        key[u] = j0 + u < nb ? __builtin_amdgcn_readfirstlane(es[j].key) : a.V;
-        ends[u] = key[u] != __builtin_amdgcn_readfirstlane(es[j + 1].key);
-        const int pos = __builtin_amdgcn_readfirstlane(es[j].pos);
-        r[u] = old[u] = (f32x4){0.f, 0.f, 0.f, 0.f};
-        if (col && key[u] < a.V) {
-          r[u] = load4(grad + (size_t)pos * a.ld_grad, c, a.d);
-          if (ends[u]) old[u] = load4(table + (size_t)key[u] * a.ld_table, c, a.d);
-        }
+    for (int u = 0; u < U; ++u) {
+      key[u] = j0 + u < i1 ? __builtin_amdgcn_readlane(e.key, u) : a.V;
+      ends[u] = key[u] != __builtin_amdgcn_readlane(e.key, u + 1);
+      const int pos = __builtin_amdgcn_readlane(e.pos, u);
+      r[u] = old[u] = (f32x4){0.f, 0.f, 0.f, 0.f};
+      if (col && key[u] < a.V) {
+        r[u] = load4(grad + (size_t)pos * a.ld_grad, c, a.d);
+        if (ends[u]) old[u] = load4(table + (size_t)key[u] * a.ld_table, c, a.d);
       }
+    }
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (key[u] >= a.V) continue;
-        acc += r[u];
-        ++terms;
-        if (!ends[u]) continue;
-        if (cont) {
-          opened = key[u];
-          if (col) store4(a.head + (size_t)g * a.d, c, a.d, acc);
-        } else if (col) {
-          store4(table + (size_t)key[u] * a.ld_table, c, a.d, old[u] + a.scale * acc);
-        }
-        cont = false;
-        terms = 0;
-        acc = (f32x4){0.f, 0.f, 0.f, 0.f};
+    for (int u = 0; u < U; ++u) {
+      if (key[u] >= a.V) continue;
+      acc += r[u];
+      ++terms;
+      if (!ends[u]) continue;
+      if (cont) {
+        opened = key[u];
+        if (col) store4(a.head + (size_t)g * a.d, c, a.d, acc);
+      } else if (col) {
+        store4(table + (size_t)key[u] * a.ld_table, c, a.d, old[u] + a.scale * acc);
       }
+      cont = false;
+      terms = 0;
+      acc = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
   }
   if (terms && col) store4(a.tail + (size_t)g * a.d, c, a.d, acc);
   if (blockIdx.y == 0 && threadIdx.x == 0) a.open[g] = opened;
 }
 
-// adds up the partial sums of a token that ends in piece g and began before it
+// Adds up the partial sums of the tokens that end in a piece and began before
+// it.  A workgroup looks at kJoined pieces; the pieces of one token are shared
+// out over groups of threads that cover a row.
+constexpr int kJoined = 16, kJoinThreads = 1024;
 template <typename T, bool ACC>
-__global__ __launch_bounds__(1024) void embed_join_kernel(GradArgs a) {
-  const int g = blockIdx.x, v = a.open[g];
-  if (v < 0) return;
-  const int lo = search(0, a.N, [&](int j) { return a.sorted[j].key < v; });  // the first entry of v
-  const int from = (int)((ACC ? (int64_t)lo : (int64_t)lo + v) / a.items);
-  const int c = 4 * (blockIdx.y * blockDim.x + threadIdx.x);
-  if (c >= a.d) return;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+__global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(GradArgs a) {
+  __shared__ f32x4 part[kJoinThreads];
+  const int t = threadIdx.x, lane = t & 63, g0 = blockIdx.x * kJoined;
+  unsigned long long open =
+      __builtin_amdgcn_ballot_w64(lane < kJoined && g0 + lane < a.pieces && a.open[g0 + lane] >= 0);
+  const int quads = (a.d + 3) / 4;
+  for (; open; open &= open - 1) {
+    const int g = g0 + __builtin_ctzll(open), v = a.open[g];
+    int lo = 0, hi = a.N;  // the first entry of v
+    narrow(lo, hi, 0, [&](int j) { return a.sorted[j].key < v; });
+    const int from = (int)((ACC ? (int64_t)lo : (int64_t)lo + v) / a.items), n = g - from;
+    for (int q0 = 0; q0 < quads; q0 += kJoinThreads) {
+      const int nq = min(kJoinThreads, quads - q0), groups = kJoinThreads / nq, k = t / nq, c = 4 * (q0 + t - k * nq);
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+      if (k < groups) {
+        const int to = from + (int)((int64_t)n * (k + 1) / groups);
 #pragma unroll 8
-  for (int k = from; k < g; ++k) acc += load4(a.tail + (size_t)k * a.d, c, a.d);
-  acc += load4(a.head + (size_t)g * a.d, c, a.d);
-  T* row = (T*)a.dtable + (size_t)v * a.ld_table;
-  f32x4 r = a.scale * acc;
-  if (ACC) r += load4(row, c, a.d);
-  store4(row, c, a.d, r);
+        for (int i = from + (int)((int64_t)n * k / groups); i < to; ++i)
+          acc += load4(a.tail + (size_t)i * a.d, c, a.d);
+      }
+      __syncthreads();
+      part[t] = acc;
+      __syncthreads();
+      if (k == 0) {
+        for (int i = 1; i < groups; ++i) acc += part[i * nq + t];
+        acc += load4(a.head + (size_t)g * a.d, c, a.d);
+        T* row = (T*)a.dtable + (size_t)v * a.ld_table;
+        f32x4 r = a.scale * acc;
+        if (ACC) r += load4(row, c, a.d);
+        store4(row, c, a.d, r);
+      }
+    }
+  }
 }
 
-constexpr int kMaxPieces = 2048;
+// threads of four columns each: whole waves, at most 1024
+int grad_threads(int d) {
+  const int quads = (d + 3) / 4;
+  return quads >= 1024 ? 1024 : (quads + 63) / 64 * 64;
+}
 
-// pieces of the merged sequence: 8 a CU, fewer where a piece would have under 4 places
-int grad_pieces(int64_t places) {
-  const int64_t p = (places + 3) / 4;
-  return (int)(p < 1 ? 1 : p > kMaxPieces ? kMaxPieces : p);
+// Pieces of the merged sequence: one round of workgroups over the CUs (32 waves on
+// each), or more where the table's rows are most of the traffic, a piece for every
+// 32 KB of them: those at work then write to one stretch of the table that moves
+// along (16384 tokens to 257 MB of float32: 64 us with 1536 pieces, 53 with 4096, 48
+// with 8192; to 129 MB of bfloat16: 37 with 2048, 45 with 8192).  Fewer where a
+// piece would have under 4 places or the partial sums over 64 MB.
+int grad_pieces(int64_t places, int64_t table_bytes, int d) {
+  const int64_t round = 256 * (32 * 64 / grad_threads(d));
+  const int64_t most = std::min<int64_t>(8192, std::max<int64_t>(1024, (64 << 20) / (8 * (int64_t)d)));
+  const int64_t want = std::min(std::max(round, table_bytes >> 15), most);
+  return (int)std::min(want, std::max<int64_t>((places + 3) / 4, 1));
 }
 
 size_t round256(size_t x) { return (x + 255) / 256 * 256; }
@@ -513,7 +601,7 @@ Layout layout(int n, int vocab, int d) {
     at += round256(b);
     return o;
   };
-  l.pieces = grad_pieces((int64_t)n + vocab);  // (no fewer than without the ends)
+  l.pieces = grad_pieces((int64_t)n + vocab, (int64_t)vocab * d * 4, d);  // (no fewer than a call has)
   l.entries[0] = take((size_t)n * sizeof(Entry));
   if (n > kOneRun) l.entries[1] = take((size_t)n * sizeof(Entry));
   if (n > kRunsMax) {
@@ -531,12 +619,11 @@ Layout layout(int n, int vocab, int d) {
 
 template <typename G, typename T, bool ACC>
 void launch_grad(const GradArgs& a, hipStream_t s) {
-  // threads of four columns each: whole waves, at most 1024
-  const int quads = (a.d + 3) / 4, threads = quads >= 1024 ? 1024 : (quads + 63) / 64 * 64;
+  const int quads = (a.d + 3) / 4, threads = grad_threads(a.d);
   const dim3 grid(a.pieces, (quads + threads - 1) / threads);
   if (ACC) embed_grad_add_kernel<G, T><<<grid, threads, 0, s>>>(a);
   else embed_grad_kernel<G, T><<<grid, threads, 0, s>>>(a);
-  embed_join_kernel<T, ACC><<<grid, threads, 0, s>>>(a);
+  embed_join_kernel<T, ACC><<<(a.pieces + kJoined - 1) / kJoined, kJoinThreads, 0, s>>>(a);
 }
 template <typename G, typename T>
 void launch_grad(const GradArgs& a, bool acc, hipStream_t s) {
@@ -655,7 +742,7 @@ extern "C" ssd_status ssd_embed_grad(ssd_dtype grad_dtype, ssd_dtype table_dtype
   a.N = n;
   a.V = vocab;
   a.d = d;
-  a.pieces = grad_pieces(places);
+  a.pieces = grad_pieces(places, accumulate ? 0 : (int64_t)vocab * d * op_size(table_dtype), d);
   a.items = (int)((places + a.pieces - 1) / a.pieces);
   a.pieces = (int)((places + a.items - 1) / a.items);
   a.grad = grad;
