@@ -133,18 +133,19 @@ struct Entry {
 
 __device__ __forceinline__ int key_of(int token, int V) { return token >= 0 && token < V ? token : V; }
 
-// Up to kRunsMax positions: sorted runs, then every entry's place among all.
-// Within a run (all positions up to kOneRun, else kRun) an entry's rank is the number
-// of those before it, counted by comparing all with all: a workgroup ranks 64
-// positions, one per lane, and its waves share out the others.
-constexpr int kOneRun = 4096, kRun = 2048, kRunsMax = 131072, kRankThreads = 512;
-__global__ __launch_bounds__(kRankThreads) void rank_kernel(const int* __restrict__ tokens, int N, int V, int run,
+// Up to kRunsMax positions: sorted runs of kRun, then every entry's place among
+// all.  Within a run an entry's rank is the number of those before it, counted by
+// comparing all with all: a workgroup ranks 64 positions, one per lane, and its
+// waves share out the others.  (16384 positions: 6.5 and 5.0 us, where the radix
+// sort below takes 25; 65536: 14 and 23 us; 131072: 26 and 82, the radix sort 75.)
+constexpr int kRun = 2048, kRunsMax = 65536, kRankThreads = 1024;
+__global__ __launch_bounds__(kRankThreads) void rank_kernel(const int* __restrict__ tokens, int N, int V,
                                                             Entry* __restrict__ out) {
   constexpr int W = kRankThreads / 64;
-  __shared__ __align__(16) int keys[kOneRun];
+  __shared__ __align__(16) int keys[kRun];
   __shared__ int count[W][64];
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-  const int b = blockIdx.x * 64 / run * run, n = min(run, N - b), n4 = (n + 3) / 4;  // the run
+  const int b = blockIdx.x * 64 / kRun * kRun, n = min(kRun, N - b), n4 = (n + 3) / 4;  // the run
   for (int j = t; j < 4 * n4; j += kRankThreads) keys[j] = j < n ? key_of(tokens[b + j], V) : 0x7fffffff;
   __syncthreads();
   const int i0 = blockIdx.x * 64 - b, i = i0 + lane, key = i < n ? keys[i] : 0;
@@ -603,7 +604,7 @@ Layout layout(int n, int vocab, int d) {
   };
   l.pieces = grad_pieces((int64_t)n + vocab, (int64_t)vocab * d * 4, d);  // (no fewer than a call has)
   l.entries[0] = take((size_t)n * sizeof(Entry));
-  if (n > kOneRun) l.entries[1] = take((size_t)n * sizeof(Entry));
+  if (n > kRun) l.entries[1] = take((size_t)n * sizeof(Entry));
   if (n > kRunsMax) {
     l.run = sort_run(n);
     l.blocks = (n + l.run - 1) / l.run;
@@ -728,8 +729,8 @@ extern "C" ssd_status ssd_embed_grad(ssd_dtype grad_dtype, ssd_dtype table_dtype
       OP_LAUNCHED();
     }
   } else if (n > 0) {
-    const bool one = n <= kOneRun;
-    rank_kernel<<<(n + 63) / 64, kRankThreads, 0, s>>>(tokens, n, vocab, one ? kOneRun : kRun, one ? sorted : other);
+    const bool one = n <= kRun;
+    rank_kernel<<<(n + 63) / 64, kRankThreads, 0, s>>>(tokens, n, vocab, one ? sorted : other);
     OP_LAUNCHED();
     if (!one) {
       merge_runs_kernel<<<(n + 31) / 32, 256, 0, s>>>(other, n, sorted);

@@ -125,7 +125,7 @@ def test_wide_vocabulary(env):
 
 
 @pytest.mark.parametrize("kind", ["even", "zipf", "one"])
-@pytest.mark.parametrize("n", [4095, 4096, 4097, 8191, 8193, 32769, 131072, 131073, 200001])
+@pytest.mark.parametrize("n", [2047, 2048, 2049, 4095, 4097, 8193, 32769, 65536, 65537, 131073, 200001])
 def test_lengths_around_the_sorts(env, n, kind):
     torch, ops = env
     print(n, kind, flush=True)
