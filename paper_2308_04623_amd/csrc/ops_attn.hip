@@ -669,9 +669,14 @@ __global__ __launch_bounds__(64 * kWaves, D == 128 ? 2 : D == 64 ? 3 : 4) void p
   }
   const Range r = {(const char*)(shared ? a.kp : a.ko) + at * (int)sizeof(T),
                    (const char*)(shared ? a.vp : a.vo) + at * (int)sizeof(T), row * (int)sizeof(T)};
-  if (BYQ && shared) return part_by_queries<T, D, MP>(a, qs, r, k0, k1, part, lds);
-  if (BYQ || MP == MO || !shared) part_by_rows<T, D, MO>(a, qs, r, k0, k1, len, part, lds);
-  else part_by_rows<T, D, MP>(a, qs, r, k0, k1, len, part, lds);
+  if constexpr (BYQ)
+    if (shared) return part_by_queries<T, D, MP>(a, qs, r, k0, k1, part, lds);
+  if constexpr (BYQ || MP == MO) {
+    part_by_rows<T, D, MO>(a, qs, r, k0, k1, len, part, lds);
+  } else {
+    if (shared) part_by_rows<T, D, MP>(a, qs, r, k0, k1, len, part, lds);
+    else part_by_rows<T, D, MO>(a, qs, r, k0, k1, len, part, lds);
+  }
 }
 
 // A wave per query adds its parts: lane l has dims 4 (l % (D / 4)) .. + 3 and every
