@@ -66,7 +66,7 @@ ssd_status ssd_prefix_attn_workspace(const ssd_prefix_attn_desc *a, size_t *byte
  *   dtype SSD_F32 or SSD_BF16; head_dim 32, 64 or 128; n_head a multiple of
  * n_kv_head; 1 <= n_seq <= 4096, 1 <= n_query <= 64, prefix_len, own_rows >= 0
  * and below 2^30.  Pointers are 16-byte aligned and strides multiples of 16
- * bytes, prefix_row and own_row at most 2^27 bytes; out's rows do not overlap.  k_prefix and v_prefix may be NULL when
+ * bytes; out's rows do not overlap.  k_prefix and v_prefix may be NULL when
  * prefix_len is 0, k_own and v_own when own_rows is 0.  Scores and sums are
  * float32; bfloat16 calls round the weights exp(x - max) to bfloat16 for the
  * product with the values.
@@ -103,8 +103,8 @@ ssd_status ssd_distill_backward(ssd_dtype dtype, const void *logits, int64_t ld,
                                 const int32_t *ids, const float *vals, int32_t k, const float *lse,
                                 const float *weight, float temperature, void *dlogits, int64_t ld_d, void *stream);
 /* Both at once, for weights known beforehand: the logits are read once where a
- * row fits the registers of a compute unit (float32: 65,536 entries, bfloat16:
- * 131,072). */
+ * row fits the registers of a compute unit (float32: 98,304 entries, bfloat16:
+ * 196,608). */
 ssd_status ssd_distill_step(ssd_dtype dtype, const void *logits, int64_t ld, int32_t n_rows, int32_t vocab,
                             const int32_t *ids, const float *vals, int32_t k, const float *weight, float temperature,
                             float *loss, float *lse, void *dlogits, int64_t ld_d, void *stream);
