@@ -9,7 +9,8 @@
 //
 // A workgroup of four waves takes a tile of queries (16 per matrix tile) and a
 // chunk of rows, either of the prefix or of one sequence's own, and leaves one
-// part (m, l, o) per query; merge_kernel adds a query's parts.  Its waves take the
+// part (m, l, o) per query; merge_kernel adds a query's parts.  (Where the prefix is
+// short for the batch, short_attn_kernel does all for a sequence.)  Its waves take the
 // chunk's blocks of rows in turn and never wait for each other until the end: a
 // wave copies its blocks' keys and values into LDS of its own, one block ahead.
 #include <algorithm>
@@ -438,6 +439,19 @@ __device__ __forceinline__ size_t query_of(const ssd_prefix_attn_desc& d, int se
   return ((size_t)seq * d.n_query + t) * d.n_head + head;
 }
 
+// Four dims of a query's attention from its sums, and its log of the sum.
+template <typename T>
+__device__ __forceinline__ void put_query(const PrefixAttnArgs& a, int seq, int t, int head, int x, f32x4 sum, float top,
+                                          float total) {
+  const ssd_prefix_attn_desc& d = a.d;
+  T* out = (T*)a.out + (int64_t)seq * d.out_seq + (int64_t)t * d.out_row + (int64_t)head * d.out_head;
+  const float inv = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) op_st(out, 4 * x + i, sum[i] * inv);
+  if (a.lse && x == 0)
+    a.lse[query_of(d, seq, t, head)] = total == 0.f ? -INFINITY : top * 0.6931471805599453f + logf(total);
+}
+
 __device__ __forceinline__ void reads_over() {
   // the wave's LDS reads so far are complete: what they read may be overwritten
   __builtin_amdgcn_sched_barrier(0);
@@ -679,6 +693,34 @@ __global__ __launch_bounds__(64 * kWaves, D == 128 ? 2 : D == 64 ? 3 : 4) void p
   }
 }
 
+// Prefixes that are short for the batch: a workgroup takes a tile of one
+// sequence's queries over the prefix and its own rows, and writes their attention.
+// One launch, no parts to write, read and join (6 sequences of 4 float32 heads of 32,
+// 64 + 24 rows: 7.4 us by parts, 5.1 by this; bound by latency, two blocks a wave).
+template <typename T, int D, int MO>
+__global__ __launch_bounds__(64 * kWaves, D == 128 ? 2 : D == 64 ? 3 : 4) void short_attn_kernel(PrefixAttnArgs a) {
+  extern __shared__ __align__(512) unsigned char lds[];
+  const ssd_prefix_attn_desc& d = a.d;
+  const int tile = blockIdx.x % a.o_tiles, bh = blockIdx.x / a.o_tiles, b = bh / d.n_kv_head, h = bh - b * d.n_kv_head;
+  const int len = min(a.own_len[b], d.own_rows);
+  const Queries qs = {h, b, tile * MO * 16, d.n_query * (d.n_head / d.n_kv_head)};
+  const int64_t ap = (int64_t)h * d.prefix_head, ao = (int64_t)b * d.own_seq + (int64_t)h * d.own_head;
+  constexpr int ES = sizeof(T);
+  Wave<T, D, MO> s;
+  s.load(a, qs);
+  if (len >= 0)
+    walk(s, (Range){(const char*)a.kp + ap * ES, (const char*)a.vp + ap * ES, d.prefix_row * ES}, 0, d.prefix_len, false,
+         0, d.n_query, a.scale2, lds);
+  reads_over();
+  walk(s, (Range){(const char*)a.ko + ao * ES, (const char*)a.vo + ao * ES, d.own_row * ES}, 0, len, true, len, d.n_query,
+       a.scale2, lds);
+  join_waves(s, qs, lds, [&](int col, int x, f32x4 sum, float top, float total) {
+    int seq, t, head;
+    qs.split(d, qs.first + col, seq, t, head);
+    put_query<T>(a, seq, t, head, x, sum, top, total);
+  });
+}
+
 // A wave per query adds its parts: lane l has dims 4 (l % (D / 4)) .. + 3 and every
 // (256 / D)-th part.
 template <typename T, int D>
@@ -713,13 +755,7 @@ __global__ __launch_bounds__(256) void merge_kernel(PrefixAttnArgs a, int querie
 #pragma unroll
     for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], o);
   }
-  if (lane < LD) {
-    T* out = (T*)a.out + (int64_t)b * d.out_seq + (int64_t)t * d.out_row + (int64_t)h * d.out_head;
-    const float inv = total == 0.f ? 0.f : 1.f / total;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) op_st(out, 4 * x + i, acc[i] * inv);
-    if (a.lse && lane == 0) a.lse[q] = total == 0.f ? -INFINITY : top * 0.6931471805599453f + logf(total);
-  }
+  if (lane < LD) put_query<T>(a, b, t, h, x, acc, top, total);
 }
 
 constexpr int kMaxRows = 1 << 30;
@@ -753,15 +789,28 @@ ssd_status check_strides(const ssd_prefix_attn_desc* a) {
   return SSD_OK;
 }
 
-// How a call is cut up.  Up to 32 queries of a kv head: one tile, the waves
-// split the rows.  More: tiles of 64 or 128, the waves split the queries.  The rows
-// are cut so that the workgroups are one round over the CUs, two a CU where there
+// How a call is cut up.
+//   Alone (short_attn_kernel): a sequence's queries take the prefix and their own rows
+// in one workgroup, where the prefix is short for the number of workgroups that
+// read it again: up to 2 steps of the four waves (a step: 128 rows of bfloat16, 64
+// of float32), and where a tile's 32 columns are more than half used, 1 more per 16
+// workgroups up to 16 steps; and where a sequence's own rows would be one chunk, or
+// both are 4 steps.  Measured, split and alone (us): 1 sequence of 20 heads of 64, 256 rows
+// and 64 of its own 7.7 and 6.1, 1024 rows 9.0 and 11.3; 128 sequences of it, 128
+// rows 22.4 and 20.1, 512 rows 24.3 and 32.7; 8 queries, 16 heads on 4 of 128: 8
+// sequences, 512 rows 14.3 and 13.8, 1024 rows 15.3 and 18.2; 64 sequences, 2048 rows 39.9
+// and 28.1; float32, 512 rows 49 and 34.  48 x 5 queries, 32 heads on 8 of 128:
+// 2048 rows 50 and 43, 4096 rows 58 and 69.
+//   Else the prefix is read once for all.  Up to 32 queries of a kv head: one
+// tile, the waves split the rows.  More: tiles of 64 or 128, the waves split the
+// queries.  The rows are cut so that the workgroups are one round over the CUs, two a CU where there
 // are products to overlap: more, shorter chunks cost more parts than they even out
 // (16 sequences over 100,000 rows: 97 us with 256 workgroups, 100 with 512, 103 with
 // 1024; 48 x 5 queries over 8,191 with grouped heads: 83, 67 and 78 us).
 constexpr int kRound = 256;
 
 struct Plan {
+  bool alone;  // see short_attn_kernel
   bool byq;    // see prefix_attn_kernel
   int mp, mo;  // matrix tiles per wave
   int p_cols, p_tiles, p_chunks, p_chunk, p_blocks, o_tiles, o_chunks, o_chunk;
@@ -792,32 +841,44 @@ Plan plan(const ssd_prefix_attn_desc* a) {
     chunk = (int)(div_up(std::max<int64_t>(div_up(rows, want), 1), step) * step);
     chunks = (int)div_up(rows, chunk);
   };
+  const int64_t own_blocks = (int64_t)a->n_seq * a->n_kv_head * p.o_tiles;
+  cut(a->own_rows, own_blocks, p.o_chunks, p.o_chunk);
+  const int64_t again = 2 + (p.mo == 2 ? std::min<int64_t>(own_blocks / 16, 14) : 0);
+  p.alone = a->prefix_len <= again * step && (p.o_chunks <= 1 || (int64_t)a->prefix_len + a->own_rows <= 4 * step);
+  if (p.alone) {
+    p.blocks = own_blocks;
+    p.bytes = 16;  // (not used)
+    return p;
+  }
   cut(a->prefix_len, (int64_t)a->n_kv_head * p.p_tiles, p.p_chunks, p.p_chunk);
-  cut(a->own_rows, (int64_t)a->n_seq * a->n_kv_head * p.o_tiles, p.o_chunks, p.o_chunk);
   p.p_blocks = (int)(div_up((int64_t)a->n_kv_head * p.p_chunks, 8) * 8 * p.p_tiles);
-  p.blocks = p.p_blocks + (int64_t)a->n_seq * a->n_kv_head * p.o_tiles * p.o_chunks;
+  p.blocks = p.p_blocks + own_blocks * p.o_chunks;
   const int64_t slots = (int64_t)a->n_seq * a->n_query * a->n_head * std::max(1, p.p_chunks + p.o_chunks);
   p.o_bytes = (size_t)slots * a->head_dim * 4;
   p.bytes = p.o_bytes + (size_t)slots * sizeof(float2);
   return p;
 }
 
-template <typename T, int D, int MP, int MO, bool BYQ>
-hipError_t launch(const PrefixAttnArgs& a, int64_t blocks, hipStream_t s) {
-  constexpr int rows = kWaves * 2 * Block<T, D>::BYTES, queries = kStages * Stage<T, D>::BYTES;
-  constexpr int lds = BYQ && queries > rows ? queries : rows;
-  // (once per device: more than 64 KB of LDS, with the kernel's own, has to be asked for)
+// Once per kernel and device: more than 64 KB of LDS, with the kernel's own, has
+// to be asked for.
+template <auto kernel>
+hipError_t ask_for_lds(int bytes) {
   static std::atomic<uint64_t> ready{0};
   int dev = 0;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return e;
   const uint64_t bit = dev < 64 ? 1ull << dev : 0;
-  if (!(ready.load(std::memory_order_acquire) & bit)) {
-    e = hipFuncSetAttribute((const void*)prefix_attn_kernel<T, D, MP, MO, BYQ>,
-                            hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    if (e != hipSuccess) return e;
-    ready.fetch_or(bit, std::memory_order_release);
-  }
+  if (ready.load(std::memory_order_acquire) & bit) return hipSuccess;
+  e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == hipSuccess) ready.fetch_or(bit, std::memory_order_release);
+  return e;
+}
+template <typename T, int D, int MP, int MO, bool BYQ>
+hipError_t launch(const PrefixAttnArgs& a, int64_t blocks, hipStream_t s) {
+  constexpr int rows = kWaves * 2 * Block<T, D>::BYTES, queries = kStages * Stage<T, D>::BYTES;
+  constexpr int lds = BYQ && queries > rows ? queries : rows;
+  hipError_t e = ask_for_lds<prefix_attn_kernel<T, D, MP, MO, BYQ>>(lds);
+  if (e != hipSuccess) return e;
   if (blocks > 0) prefix_attn_kernel<T, D, MP, MO, BYQ><<<(unsigned)blocks, 64 * kWaves, lds, s>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
@@ -825,8 +886,17 @@ hipError_t launch(const PrefixAttnArgs& a, int64_t blocks, hipStream_t s) {
   merge_kernel<T, D><<<(n + 3) / 4, 256, 0, s>>>(a, n);
   return hipGetLastError();
 }
+template <typename T, int D, int MO>
+hipError_t launch_short(const PrefixAttnArgs& a, int64_t blocks, hipStream_t s) {
+  constexpr int lds = kWaves * 2 * Block<T, D>::BYTES;
+  const hipError_t e = ask_for_lds<short_attn_kernel<T, D, MO>>(lds);
+  if (e != hipSuccess) return e;
+  short_attn_kernel<T, D, MO><<<(unsigned)blocks, 64 * kWaves, lds, s>>>(a);
+  return hipGetLastError();
+}
 template <typename T, int D>
 hipError_t launch(const PrefixAttnArgs& a, const Plan& p, hipStream_t s) {
+  if (p.alone) return p.mo == 2 ? launch_short<T, D, 2>(a, p.blocks, s) : launch_short<T, D, 1>(a, p.blocks, s);
   if (p.byq) {
     if (p.mp == 2) return p.mo == 2 ? launch<T, D, 2, 2, true>(a, p.blocks, s) : launch<T, D, 2, 1, true>(a, p.blocks, s);
     return p.mo == 2 ? launch<T, D, 1, 2, true>(a, p.blocks, s) : launch<T, D, 1, 1, true>(a, p.blocks, s);

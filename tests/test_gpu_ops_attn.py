@@ -287,3 +287,34 @@ def test_refusals_of_the_binding(env):
     refused(0, torch.zeros(2, 1, 4, 128, dtype=torch.bfloat16, device="cuda")[..., ::2])
     with pytest.raises(SSDError):
         ops.prefix_attention(*a, out=torch.empty(2, 1, 4, 32, dtype=torch.bfloat16, device="cuda"))
+
+
+# a prefix that one workgroup takes with the sequence's own rows, and one that is cut
+# into parts: 128 bfloat16 (64 float32) rows are a step, two steps the limit with few queries
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("steps,more", [(2, 0), (2, 1), (5, 13), (18, 1)])
+@pytest.mark.parametrize("b,t,h,g,d", [(3, 1, 4, 4, 64), (6, 2, 6, 2, 32), (40, 3, 2, 1, 128), (9, 16, 4, 2, 64)])
+def test_short_and_long_prefixes(env, dtype, steps, more, b, t, h, g, d):
+    """Unseen rows hold NaN; sequences are off, empty, shorter than their queries, full."""
+    torch, ops = env
+    p = steps * (64 if dtype == "f32" else 128) + more
+    lens = [(-1, 0, 1, 37, 5)[i % 5] for i in range(b)]
+    x, lens = make(torch, dtype, b, t, h, g, d, p, 37, seed=p + b, lens=lens)
+    for i, n in enumerate(lens):
+        x["ko"][i, :, max(0, n):] = 0.0
+        x["vo"][i, :, max(0, n):] = 0.0
+    want = check(torch, ops, dtype, x, lens)
+    for i, n in enumerate(lens):
+        x["ko"][i, :, max(0, n):] = float("inf")
+        x["vo"][i, :, max(0, n):] = float("nan")
+    args = [x[k].cuda() for k in ("q", "kp", "vp", "ko", "vo")]
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    assert torch.equal(ops.prefix_attention(*args, n), want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("b,p", [(2, 0), (2, 300), (40, 64), (1, 1500)])
+def test_long_own_rows(env, dtype, b, p):
+    torch, ops = env
+    x, lens = make(torch, dtype, b, 2, 4, 2, 64, p, 1333, seed=p, lens=[1333 - 700 * (i % 2) for i in range(b)])
+    check(torch, ops, dtype, x, lens)
