@@ -9,7 +9,8 @@
 // in which a position is a row of g to read and an end a row of dW to write.  It is cut
 // into equal pieces whatever the tokens' frequencies.  A cut inside the rows of a
 // token with few of them is moved behind its end; the rows of a frequent token
-// are cut, its pieces leave partial sums, and a second kernel adds these up.
+// are cut, its pieces leave partial sums, and a second kernel adds these up.  (Few
+// positions of a small table: embed_grad_few_kernel, without the sort.)
 // Bound: memory (g read once, dW written once).
 #include <algorithm>
 
@@ -26,9 +27,15 @@ typedef unsigned u32x2_a2 __attribute__((ext_vector_type(2), aligned(2)));
 typedef unsigned u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
 typedef float f32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
 
+__device__ __forceinline__ f32x4 quad(const float* p) { return *(const f32x4_a4*)p; }
+__device__ __forceinline__ f32x4 quad(const bf16_t* p) {
+  const u32x2 r = *(const u32x2_a2*)p;
+  return (f32x4){__uint_as_float(r[0] << 16), __uint_as_float(r[0] & 0xffff0000u), __uint_as_float(r[1] << 16),
+                 __uint_as_float(r[1] & 0xffff0000u)};
+}
 // four columns of a row from column c on; the last ones of a row where fewer are left
 __device__ __forceinline__ f32x4 load4(const float* row, int c, int d) {
-  if (c + 4 <= d) return *(const f32x4_a4*)(row + c);
+  if (c + 4 <= d) return quad(row + c);
   f32x4 r = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < 3; ++i)
@@ -36,11 +43,7 @@ __device__ __forceinline__ f32x4 load4(const float* row, int c, int d) {
   return r;
 }
 __device__ __forceinline__ f32x4 load4(const bf16_t* row, int c, int d) {
-  if (c + 4 <= d) {
-    const u32x2 r = *(const u32x2_a2*)(row + c);
-    return (f32x4){__uint_as_float(r[0] << 16), __uint_as_float(r[0] & 0xffff0000u), __uint_as_float(r[1] << 16),
-                   __uint_as_float(r[1] & 0xffff0000u)};
-  }
+  if (c + 4 <= d) return quad(row + c);
   f32x4 r = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < 3; ++i)
@@ -569,6 +572,62 @@ __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(GradArgs a) {
   }
 }
 
+// ---------------------------------------------------------------- few positions
+
+// Up to kFew positions and a small table: a wave per row of it and 256 columns looks
+// all tokens through and adds the row's positions in their order.  One launch, no sort,
+// nothing to join; bound by latency (200 tokens of 512 x 128 float32: 4.2 us).
+constexpr int kFew = 256;
+template <typename G, typename T, bool ACC>
+__global__ __launch_bounds__(256) void embed_grad_few_kernel(GradArgs a, const int* __restrict__ tokens) {
+  const int lane = threadIdx.x & 63, v = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+  if (v >= a.V) return;
+  unsigned long long here[kFew / 64], any = 0;
+#pragma unroll
+  for (int g = 0; g < kFew / 64; ++g) {
+    const int i = 64 * g + lane;
+    any |= here[g] = __builtin_amdgcn_ballot_w64(i < a.N && tokens[min(i, a.N - 1)] == v);
+  }
+  if (ACC && !any) return;
+  // (a row's last columns: its last four, of which the new ones are written)
+  const int c = 4 * ((int)blockIdx.y * 64 + lane), at = min(c, a.d - 4);
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int g = 0; g < kFew / 64; ++g) {
+    const G* rows = (const G*)a.grad + (size_t)(64 * g) * a.ld_grad + at;
+    unsigned long long m = here[g];
+    if (m && !(m & (m - 1))) {
+      sum += quad(rows + (size_t)__builtin_ctzll(m) * a.ld_grad);
+      continue;
+    }
+    while (m) {  // eight in flight; past the last: the last again, not added
+      f32x4 x[8];
+      bool more[8];
+      int n = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        more[j] = m != 0;
+        n = m ? __builtin_ctzll(m) : n;
+        m &= m - 1;  // (0 stays 0)
+        x[j] = quad(rows + (size_t)n * a.ld_grad);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (more[j]) sum += x[j];
+    }
+  }
+  T* row = (T*)a.dtable + (size_t)v * a.ld_table;
+  sum *= a.scale;
+  if (ACC) sum += quad(row + at);
+  if (at == c) {
+    store4<!ACC>(row, c, c + 4, sum);
+  } else {
+#pragma unroll
+    for (int i = 1; i < 4; ++i)
+      if (at + i >= c) op_st(row, at + i, sum[i]);
+  }
+}
+
 // threads of four columns each: whole waves, at most 1024
 int grad_threads(int d) {
   const int quads = (d + 3) / 4;
@@ -618,8 +677,21 @@ Layout layout(int n, int vocab, int d) {
   return l;
 }
 
+// Whether embed_grad_few_kernel takes a call.  A wave per row has to be less work than
+// the sort saves: tables of up to 65536 waves.  Sorted and few (us), 200 tokens of
+// Zipf frequencies, float32: 512 x 128 10.5 and 4.2, 8192 x 1024 12.8 and 9.8, 50257 x 128 12.9
+// and 11.8; accumulated 10.6 and 4.4, 9.6 and 6.5, but 50257 x 1280 9.7 and 19.5.  256
+// times one token, the worst: 512 x 128 12 and 16.
+bool few(int n, int V, int d) {
+  return n > 0 && n <= kFew && d >= 4 && (int64_t)V * ((d + 255) / 256) <= 65536;
+}
+
 template <typename G, typename T, bool ACC>
-void launch_grad(const GradArgs& a, hipStream_t s) {
+void launch_grad(const GradArgs& a, const int* tokens, hipStream_t s) {
+  if (few(a.N, a.V, a.d)) {
+    embed_grad_few_kernel<G, T, ACC><<<dim3((a.V + 3) / 4, (a.d + 255) / 256), 256, 0, s>>>(a, tokens);
+    return;
+  }
   const int quads = (a.d + 3) / 4, threads = grad_threads(a.d);
   const dim3 grid(a.pieces, (quads + threads - 1) / threads);
   if (ACC) embed_grad_add_kernel<G, T><<<grid, threads, 0, s>>>(a);
@@ -627,14 +699,14 @@ void launch_grad(const GradArgs& a, hipStream_t s) {
   embed_join_kernel<T, ACC><<<(a.pieces + kJoined - 1) / kJoined, kJoinThreads, 0, s>>>(a);
 }
 template <typename G, typename T>
-void launch_grad(const GradArgs& a, bool acc, hipStream_t s) {
-  if (acc) launch_grad<G, T, true>(a, s);
-  else launch_grad<G, T, false>(a, s);
+void launch_grad(const GradArgs& a, bool acc, const int* tokens, hipStream_t s) {
+  if (acc) launch_grad<G, T, true>(a, tokens, s);
+  else launch_grad<G, T, false>(a, tokens, s);
 }
 template <typename G>
-void launch_grad(const GradArgs& a, int table_dtype, bool acc, hipStream_t s) {
-  if (table_dtype == SSD_F32) launch_grad<G, float>(a, acc, s);
-  else launch_grad<G, bf16_t>(a, acc, s);
+void launch_grad(const GradArgs& a, int table_dtype, bool acc, const int* tokens, hipStream_t s) {
+  if (table_dtype == SSD_F32) launch_grad<G, float>(a, acc, tokens, s);
+  else launch_grad<G, bf16_t>(a, acc, tokens, s);
 }
 
 ssd_status check(int32_t n, int32_t vocab, int32_t d) {
@@ -728,7 +800,7 @@ extern "C" ssd_status ssd_embed_grad(ssd_dtype grad_dtype, ssd_dtype table_dtype
                                                      p + 1 < l.passes ? counts + (p + 1) * step : nullptr);
       OP_LAUNCHED();
     }
-  } else if (n > 0) {
+  } else if (n > 0 && !few(n, vocab, d)) {
     const bool one = n <= kRun;
     rank_kernel<<<(n + 63) / 64, kRankThreads, 0, s>>>(tokens, n, vocab, one ? sorted : other);
     OP_LAUNCHED();
@@ -754,8 +826,8 @@ extern "C" ssd_status ssd_embed_grad(ssd_dtype grad_dtype, ssd_dtype table_dtype
   a.head = (float*)(ws + l.head);
   a.tail = (float*)(ws + l.tail);
   a.open = (int*)(ws + l.open);
-  if (grad_dtype == SSD_F32) launch_grad<float>(a, table_dtype, accumulate != 0, s);
-  else launch_grad<bf16_t>(a, table_dtype, accumulate != 0, s);
+  if (grad_dtype == SSD_F32) launch_grad<float>(a, table_dtype, accumulate != 0, tokens, s);
+  else launch_grad<bf16_t>(a, table_dtype, accumulate != 0, tokens, s);
   OP_LAUNCHED();
   return SSD_OK;
 }

@@ -209,7 +209,7 @@ def _logits(what, logits, ids, vals, weight):
 
 def _grad_out(what, logits, out):
     if out is None:
-        return torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        return logits.new_empty(logits.shape)
     _tensor(what, "out", out, (logits.dtype,), 2, logits)
     if out.shape != logits.shape:
         _refuse(what, f"out {tuple(out.shape)} must be {tuple(logits.shape)}")

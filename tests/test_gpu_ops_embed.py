@@ -265,3 +265,44 @@ def test_refusals_of_the_binding(env):
         ops.embed(tokens, grad, dtype=torch.float64)
     with pytest.raises(SSDError):
         ops.embed(tokens, grad, out=torch.zeros(4, 9, device="cuda"))
+
+
+@pytest.mark.parametrize("gd,td", KINDS)
+@pytest.mark.parametrize("n,v,d", [(255, 300, 4), (256, 300, 5), (257, 300, 5), (256, 70001, 9), (100, 40000, 300),
+                                   (40, 22000, 514), (256, 7, 1283), (3, 65536, 256), (3, 65537, 256), (8, 100, 3)])
+@pytest.mark.parametrize("kind", ["zipf", "one"])
+def test_few_positions(env, gd, td, n, v, d, kind):
+    """Both sides of the sizes (256 positions, 65536 waves of 256 columns) up to which nothing is sorted."""
+    torch, ops = env
+    gen = torch.Generator().manual_seed(n + v)
+    check_grad(torch, ops, gd, td, draw_tokens(gen, torch, n, v, kind),
+               torch.randn(n, d, generator=gen).to(dt(torch, gd)), v)
+
+
+@pytest.mark.parametrize("d", [1, 2, 3, 4, 63, 64, 255, 256, 257, 1024, 1283, 4100])
+def test_gradient_widths_of_sorted_positions(env, d):
+    torch, ops = env
+    gen = torch.Generator().manual_seed(d)
+    for gd, td in KINDS:
+        check_grad(torch, ops, gd, td, draw_tokens(gen, torch, 300, 60, "zipf"),
+                   torch.randn(300, d, generator=gen).to(dt(torch, gd)), 60)
+
+
+@pytest.mark.parametrize("gd,td", KINDS)
+@pytest.mark.parametrize("n", [37, 300])
+def test_gradient_between_other_columns(env, gd, td, n):
+    """Rows inside wider buffers at odd elements: what lies beside them stays, and is not read."""
+    torch, ops = env
+    v, d = 50, 261
+    gen = torch.Generator().manual_seed(n)
+    tokens, grad = draw_tokens(gen, torch, n, v, "zipf"), torch.randn(n, d, generator=gen).to(dt(torch, gd))
+    wide = torch.full((n, d + 6), float("nan"), dtype=grad.dtype, device="cuda")
+    wide[:, 1:1 + d] = grad.cuda()
+    table = torch.full((v, d + 9), 3.0, dtype=dt(torch, td), device="cuda")
+    for accumulate in (False, True):
+        ops.embed_grad(tokens.cuda(), wide[:, 1:1 + d], v, out=table[:, 3:3 + d], accumulate=accumulate)
+        assert (table[:, :3] == 3).all() and (table[:, 3 + d:] == 3).all()
+        base = torch.zeros(v, d, dtype=table.dtype, device="cuda") if not accumulate else before
+        want = ops.embed_grad(tokens.cuda(), grad.cuda(), v, out=base, accumulate=accumulate)
+        assert torch.equal(table[:, 3:3 + d], want)
+        before = want.clone()
