@@ -275,7 +275,7 @@ __device__ __forceinline__ Stat block_stat(Stat a, float c, Stat* red) {
 // Chunk c0 + thread of the gradient, mul q' with q' its exponentials, as if the teacher had
 // none of its tokens; aligned: whether out's chunks begin at multiples of 16 bytes
 // as the logits' do.  The stores pass by the caches (512 float32 rows of
-// 131072, step: 152 us with plain ones, 127 with these).
+// 131072, step: 151 us with plain ones, 121 with these).
 template <typename T>
 __device__ __forceinline__ void put_chunk(T* out, const Row<T>& body, int c0, bool aligned, float mul,
                                           float (&q)[Vec<T>::E]) {
@@ -522,29 +522,38 @@ ssd_status check_grad(int dtype, const void* logits, int64_t ld, int n, int V, c
   return SSD_OK;
 }
 
-// How a row is held: TPB threads with up to C chunks each.  With at least a row
-// for every CU, few threads with many chunks: two to four rows are on a CU, and one's
-// loads and stores run beside another's arithmetic and waits (2048 float32
-// rows of 50257, step: 149 us with 256 threads, 170 with 512, 167 with 1024).
-// With fewer rows a CU has one, and more threads are sooner done with it (64
-// rows: 15.2, 13.6, 12.7 us).
+// How a row is held: TPB threads with up to C chunks each.  One row a CU at most:
+// more threads are sooner done with it (64 float32 rows of 50257, step: 15.5 us with
+// 256 threads, 11.9 with 512, 11.1 with 1024).  More rows: few threads with many
+// chunks, so that two to four rows are on a CU and one's loads and stores run beside
+// another's arithmetic and waits (4096 bfloat16 rows of 32000, step: 98 us with 256
+// threads, 101 with 512, 147 with 1024), up to what their registers hold without
+// spilling (of 50257: 170, 157, 197; 4096 float32 rows of 50257: 332, 325, 316).  The
+// step of longer rows keeps them in 512 threads (4096 float32 rows of 65000: 427 us,
+// 465 in two sweeps).  The loss alone reads a row once either way: long rows are swept
+// (4096 float32 rows of 65000: 193 us with 512 threads, 159 swept; of 20000: 54 with 256, 68).
 template <typename T, bool GRAD>
 void launch_rows(const DistillArgs& a, int n, hipStream_t s) {
   const int chunks = a.inv_t < 1e6f ? a.V / Vec<T>::E : INT_MAX;  // (see kFar)
 #define ROWS(TPB, C, W) \
   if (chunks <= TPB * C) return distill_row_kernel<T, TPB, C, W, GRAD><<<n, TPB, 0, s>>>(a);
   ROWS(256, 4, 6)
-  if (n < kCUs) {
+  if (n <= kCUs) {
     ROWS(1024, 4, 4)
     ROWS(1024, 7, 4)
     ROWS(1024, 13, 4)
   }
   ROWS(256, 10, 4)
   ROWS(256, 16, 4)
-  ROWS(256, 25, 3)
-  ROWS(256, 50, 2)
-  ROWS(512, 32, 2)
-  ROWS(512, 48, 2)
+  if constexpr (GRAD) {
+    ROWS(512, 13, 4)
+    ROWS(512, 16, 4)
+    ROWS(1024, 13, 4)
+    ROWS(512, 32, 2)
+    ROWS(512, 48, 2)
+  } else {
+    ROWS(256, 25, 3)
+  }
 #undef ROWS
   return distill_sweep_kernel<T, GRAD><<<n, 1024, 0, s>>>(a);
 }

@@ -273,3 +273,37 @@ def test_refusals_of_the_binding(env):
     both = torch.zeros(5, 100, device="cuda")
     with pytest.raises(SSDError):
         ops.distill_step(both[:4], ids, vals, w, out=both[1:])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("chunks", [900, 1024, 1025, 2560, 2561, 4096, 4097, 6400, 6401, 6656, 6657, 8192, 8193, 13312,
+                                    13313, 16384, 16385, 24576, 24577])
+@pytest.mark.parametrize("odd", [0, 3])
+def test_many_rows_of_every_length(env, dtype, chunks, odd):
+    """More rows than compute units, five of them distinct, of as many 16-byte chunks as
+    the registers hold and one more; odd: rows that begin at any element."""
+    torch, ops = env
+    v = chunks * (4 if dtype == "f32" else 8) + odd
+    z, ids, vals, w = make(torch, dtype, 5, v, 9, seed=chunks)
+    rows = torch.arange(260) % 5
+    wide = torch.empty(260, v + odd, dtype=z.dtype, device="cuda")
+    many = wide[:, :v]
+    many.copy_(z.cuda()[rows.cuda()])
+    args = [x.cuda()[rows.cuda()] for x in (ids, vals, w)]
+    rloss, rlse, rg, X = reference(z, ids, vals, w, 1.0)
+    unit, wn = EPS * (4 * X + 256), w.double().numpy()
+    mag = np.abs(rg) / wn[:, None]
+    np.put_along_axis(mag, ids.numpy().astype(np.int64), np.take_along_axis(mag, ids.numpy().astype(np.int64), 1) + 2, 1)
+    forward = ops.distill_forward(many, *args)
+    back = ops.distill_backward(many, *args[:2], forward[1], args[2])
+    step = ops.distill_step(many, *args, out=many)  # in place
+    assert step[2].data_ptr() == many.data_ptr()
+    for loss, lse in (forward, step[:2]):
+        assert (np.abs(loss[:5].double().cpu().numpy() - rloss) <= 2 * wn * unit).all()
+        assert (np.abs(lse[:5].double().cpu().numpy() - rlse) <= unit).all()
+    rb = reference(z, ids, vals, w, 1.0, lse=forward[1][:5].cpu())[2]
+    close(dtype, many[:5].double().cpu().numpy(), rg, (wn * unit)[:, None] * mag)
+    close(dtype, back[:5].double().cpu().numpy(), rb, (wn * unit)[:, None] * mag)
+    if not odd:  # rows alike give the same, wherever they stand
+        for x in (*forward, back, *step):
+            assert torch.equal(x[5:10], x[:5]) and torch.equal(x[255:], x[:5])
