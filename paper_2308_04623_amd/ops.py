@@ -90,16 +90,18 @@ def _tensor(what, name, t, dtypes, dims, like=None):
 
 def _rows(what, name, t):
     """The row stride of a matrix whose rows' elements lie side by side."""
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    (n, d), (ld, step) = t.shape, t.stride()
+    if step != 1 and d > 1:
         _refuse(what, f"{name}'s last dimension must be contiguous")
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+    return ld if n > 1 else max(d, ld)
 
 
 def _vector(what, name, t, dtype, n, like):
+    """t is a contiguous vector of n entries (None: of any number)."""
     _tensor(what, name, t, (dtype,), 1, like)
-    if t.shape[0] != n:
+    if n is not None and t.shape[0] != n:
         _refuse(what, f"{name} has {t.shape[0]} entries, not {n}")
-    if n > 1 and t.stride(0) != 1:
+    if not t.is_contiguous():
         _refuse(what, f"{name} must be contiguous")
 
 
@@ -295,9 +297,8 @@ def embed(tokens, table, scale: float = 1.0, dtype=None, out=None, stream=None):
     table's); tokens int32 [N], those outside the table give zeros."""
     what = "ssd_embed"
     _tensor(what, "table", table, _KINDS, 2)
-    _tensor(what, "tokens", tokens, (torch.int32,), 1, table)
+    _vector(what, "tokens", tokens, torch.int32, None, table)
     n = tokens.shape[0]
-    _vector(what, "tokens", tokens, torch.int32, n, table)
     dev = table.get_device()
     where = _elsewhere(dev, stream)
     if where is not None:
