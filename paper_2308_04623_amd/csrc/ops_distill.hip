@@ -458,10 +458,14 @@ __global__ __launch_bounds__(TPB, W) void distill_row_kernel(DistillArgs a) {
   if (t < 64) put_loss(a, n, slots, mine, (st.m + __log2f(st.s)) * kLn2);
 }
 
-// The gradient from a known log-sum-exp: a workgroup per row and 8 chunks a thread.
-template <typename T>
-__global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a) {
-  constexpr int TPB = 256, E = Vec<T>::E, C = 8;
+// The gradient from a known log-sum-exp: a workgroup per row and C chunks a thread.
+// Rows of more than one part: 512 threads (3000 bfloat16 rows of 50257: 127 us with
+// 256 threads, 117 with 512; 1500 float32 rows 127 and 125), shorter ones 256 (4096
+// bfloat16 rows of 8000: 30 and 39).
+constexpr int kGradChunks = 8;
+template <typename T, int TPB>
+__global__ __launch_bounds__(TPB) void distill_grad_kernel(DistillArgs a) {
+  constexpr int E = Vec<T>::E, C = kGradChunks;
   __shared__ Slots slots;
   __shared__ Lists<TPB> lists;
   const int n = blockIdx.x, c0 = blockIdx.y * (C * TPB), t = threadIdx.x;
@@ -505,7 +509,8 @@ ssd_status check(int dtype, const void* logits, int64_t ld, int n, int V, const 
   OP_REQUIRE(n >= 0, SSD_E_INVALID_ARG, "n_rows is negative");
   OP_REQUIRE(V >= 1 && V <= 1 << 24, SSD_E_INVALID_ARG, "vocab outside [1, 2^24]");
   OP_REQUIRE(k >= 1 && k <= kMaxSlots, SSD_E_INVALID_ARG, "k outside [1, 128]");
-  OP_REQUIRE(temperature > 0.f && temperature < INFINITY, SSD_E_INVALID_ARG, "temperature must be positive and finite");
+  OP_REQUIRE(temperature > 0.f && temperature < INFINITY && 1.f / temperature < INFINITY, SSD_E_INVALID_ARG,
+             "temperature and its reciprocal must be positive and finite");
   OP_REQUIRE(ld >= V, SSD_E_INVALID_ARG, "the logits' row stride is below vocab");
   OP_REQUIRE(n == 0 || (logits && ids && vals), SSD_E_INVALID_ARG, "null argument");
   OP_REQUIRE((uintptr_t)logits % op_size(dtype) == 0, SSD_E_INVALID_ARG, "logits not aligned to their type");
@@ -558,6 +563,13 @@ void launch_rows(const DistillArgs& a, int n, hipStream_t s) {
   return distill_sweep_kernel<T, GRAD><<<n, 1024, 0, s>>>(a);
 }
 
+template <typename T>
+void launch_grad(const DistillArgs& a, int n, hipStream_t s) {
+  constexpr int per = kGradChunks * Vec<T>::E;  // elements a thread
+  if (a.V <= 256 * per) distill_grad_kernel<T, 256><<<dim3(n, 1), 256, 0, s>>>(a);
+  else distill_grad_kernel<T, 512><<<dim3(n, (a.V + 512 * per - 1) / (512 * per)), 512, 0, s>>>(a);
+}
+
 }  // namespace
 }  // namespace ssd
 
@@ -604,10 +616,8 @@ extern "C" ssd_status ssd_distill_backward(ssd_dtype dtype, const void* logits, 
   if (n_rows == 0) return SSD_OK;
   OP_REQUIRE(lse, SSD_E_INVALID_ARG, "null argument");
   DistillArgs a{logits, ld, vocab, ids, vals, k, weight, 1.f / temperature, nullptr, (float*)lse, dlogits, ld_d};
-  const int per = 8 * 256 * (16 / op_size(dtype));
-  const dim3 grid(n_rows, (vocab + per - 1) / per);
-  if (dtype == SSD_F32) distill_grad_kernel<float><<<grid, 256, 0, (hipStream_t)stream>>>(a);
-  else distill_grad_kernel<bf16_t><<<grid, 256, 0, (hipStream_t)stream>>>(a);
+  if (dtype == SSD_F32) launch_grad<float>(a, n_rows, (hipStream_t)stream);
+  else launch_grad<bf16_t>(a, n_rows, (hipStream_t)stream);
   OP_LAUNCHED();
   return SSD_OK;
 }

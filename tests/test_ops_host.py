@@ -140,3 +140,9 @@ def test_the_binding_refuses_host_tensors():
         ops.embed(torch.zeros(2, dtype=torch.int32), x)
     with pytest.raises(ssd.SSDError):
         ops.embed_grad(torch.zeros(2, dtype=torch.int32), x, 4)
+
+
+@pytest.mark.parametrize("which", ["forward", "backward", "step"])
+@pytest.mark.parametrize("t", [1e-39, 1e-45])
+def test_distill_refuses_temperatures_without_a_reciprocal(which, t):
+    assert _distill(which, t=t) == ssd.E_INVALID_ARG
