@@ -109,7 +109,8 @@ __device__ __forceinline__ void store8(bf16_t* row, int c, int d, const f32x4 (&
   }
 }
 
-// a thread per eight columns of a row
+// A thread per eight columns of a row.  Bound: memory (32768 rows of 1280 float32:
+// 63 us, 5.3 TB/s).
 template <typename T, typename O>
 __global__ __launch_bounds__(256) void embed_rows_kernel(const int* __restrict__ tokens, int64_t parts, int per,
                                                          const T* __restrict__ table, int64_t ld_table, int V, int d,
@@ -185,7 +186,7 @@ __global__ __launch_bounds__(kRankThreads) void rank_kernel(const int* __restric
 
 // An entry's place: its own in its run, and in every other run the number of
 // lower keys, equal ones included in the runs before.  Eight threads an entry take
-// the runs in turn.
+// the runs in turn.  (32768 positions: 9.2 us to rank, 8.7 to place.)
 __global__ __launch_bounds__(256) void merge_runs_kernel(const Entry* __restrict__ in, int N, Entry* __restrict__ out) {
   const int e = (blockIdx.x * 256 + threadIdx.x) >> 3, sub = threadIdx.x & 7;
   const int i = min(e, N - 1), mine = i / kRun, runs = (N + kRun - 1) / kRun;
@@ -241,7 +242,8 @@ __global__ __launch_bounds__(kSortThreads) void count_kernel(const int* __restri
   }
 }
 
-// one pass: from the tokens (in == nullptr) or entries, to entries
+// one pass: from the tokens (in == nullptr) or entries, to entries (200000 positions:
+// 51 us, bound by the ranks within a run and the counts of the runs before)
 __global__ __launch_bounds__(kSortThreads) void place_kernel(const int* __restrict__ tokens,
                                                              const Entry* __restrict__ in, int N, int V, int run,
                                                              int pass, const int* __restrict__ counts,
@@ -391,6 +393,8 @@ __device__ __forceinline__ int rows_after(const Staged& s, int N, int i, int v) 
   return n <= kShort && !more && !less ? __builtin_popcountll(same >> 32) : -1;
 }
 
+// The table written whole: a workgroup per piece, a thread per four columns (16384
+// bfloat16 rows of 1280 to 50257 of float32: 52 us, 5.8 TB/s).
 template <typename G, typename T>
 __global__ __launch_bounds__(1024) void embed_grad_kernel(GradArgs a) {
   constexpr int U = kInFlight;
@@ -468,7 +472,8 @@ __global__ __launch_bounds__(1024) void embed_grad_kernel(GradArgs a) {
 }
 
 // The same, added to the table: a piece is a run of entries, and the rows of the
-// table that end in it are loaded with the rows of the gradient.
+// table that end in it are loaded with the rows of the gradient (32768 bfloat16 rows of
+// 1280 to 50257 of float32: 75 us).
 template <typename G, typename T>
 __global__ __launch_bounds__(1024) void embed_grad_add_kernel(GradArgs a) {
   constexpr int U = kInFlight;
@@ -534,41 +539,41 @@ __global__ __launch_bounds__(1024) void embed_grad_add_kernel(GradArgs a) {
 }
 
 // Adds up the partial sums of the tokens that end in a piece and began before
-// it.  A workgroup looks at kJoined pieces; the pieces of one token are shared
-// out over groups of threads that cover a row.
-constexpr int kJoined = 16, kJoinThreads = 1024;
+// it.  A workgroup looks at kJoined pieces and 4 kJoinQuads columns; the pieces of
+// one token are shared out over groups of threads that cover these.  Bound by the
+// chain of loads for the most frequent token (the whole gradient of 16384 tokens of
+// 50257 x 1280: 70 us, with rows whole in 1024 threads 73; of 200000 368 and 373).
+constexpr int kJoined = 16, kJoinThreads = 512, kJoinQuads = 64;
 template <typename T, bool ACC>
 __global__ __launch_bounds__(kJoinThreads) void embed_join_kernel(GradArgs a) {
   __shared__ f32x4 part[kJoinThreads];
   const int t = threadIdx.x, lane = t & 63, g0 = blockIdx.x * kJoined;
   unsigned long long open =
       __builtin_amdgcn_ballot_w64(lane < kJoined && g0 + lane < a.pieces && a.open[g0 + lane] >= 0);
-  const int quads = (a.d + 3) / 4;
+  const int q0 = blockIdx.y * kJoinQuads, nq = min(kJoinQuads, (a.d + 3) / 4 - q0), groups = kJoinThreads / nq,
+            k = t / nq, c = 4 * (q0 + t - k * nq);
   for (; open; open &= open - 1) {
     const int g = g0 + __builtin_ctzll(open), v = a.open[g];
     int lo = 0, hi = a.N;  // the first entry of v
     narrow(lo, hi, 0, [&](int j) { return a.sorted[j].key < v; });
     const int from = (int)((ACC ? (int64_t)lo : (int64_t)lo + v) / a.items), n = g - from;
-    for (int q0 = 0; q0 < quads; q0 += kJoinThreads) {
-      const int nq = min(kJoinThreads, quads - q0), groups = kJoinThreads / nq, k = t / nq, c = 4 * (q0 + t - k * nq);
-      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-      if (k < groups) {
-        const int to = from + (int)((int64_t)n * (k + 1) / groups);
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    if (k < groups) {
+      const int to = from + (int)((int64_t)n * (k + 1) / groups);
 #pragma unroll 8
-        for (int i = from + (int)((int64_t)n * k / groups); i < to; ++i)
-          acc += load4(a.tail + (size_t)i * a.d, c, a.d);
-      }
-      __syncthreads();
-      part[t] = acc;
-      __syncthreads();
-      if (k == 0) {
-        for (int i = 1; i < groups; ++i) acc += part[i * nq + t];
-        acc += load4(a.head + (size_t)g * a.d, c, a.d);
-        T* row = (T*)a.dtable + (size_t)v * a.ld_table;
-        f32x4 r = a.scale * acc;
-        if (ACC) r += load4(row, c, a.d);
-        store4(row, c, a.d, r);
-      }
+      for (int i = from + (int)((int64_t)n * k / groups); i < to; ++i)
+        acc += load4(a.tail + (size_t)i * a.d, c, a.d);
+    }
+    __syncthreads();
+    part[t] = acc;
+    __syncthreads();
+    if (k == 0) {
+      for (int i = 1; i < groups; ++i) acc += part[i * nq + t];
+      acc += load4(a.head + (size_t)g * a.d, c, a.d);
+      T* row = (T*)a.dtable + (size_t)v * a.ld_table;
+      f32x4 r = a.scale * acc;
+      if (ACC) r += load4(row, c, a.d);
+      store4(row, c, a.d, r);
     }
   }
 }
@@ -697,7 +702,8 @@ void launch_grad(const GradArgs& a, const int* tokens, hipStream_t s) {
   const dim3 grid(a.pieces, (quads + threads - 1) / threads);
   if (ACC) embed_grad_add_kernel<G, T><<<grid, threads, 0, s>>>(a);
   else embed_grad_kernel<G, T><<<grid, threads, 0, s>>>(a);
-  embed_join_kernel<T, ACC><<<(a.pieces + kJoined - 1) / kJoined, kJoinThreads, 0, s>>>(a);
+  embed_join_kernel<T, ACC><<<dim3((a.pieces + kJoined - 1) / kJoined, (quads + kJoinQuads - 1) / kJoinQuads),
+                              kJoinThreads, 0, s>>>(a);
 }
 template <typename G, typename T>
 void launch_grad(const GradArgs& a, bool acc, const int* tokens, hipStream_t s) {
