@@ -137,13 +137,11 @@ struct Entry {
 
 __device__ __forceinline__ int key_of(int token, int V) { return token >= 0 && token < V ? token : V; }
 
-// Up to kRunsMax positions: sorted runs of kRun, then every entry's place among
-// all.  Within a run an entry's rank is the number of those before it, counted by
+// Not too many positions (see by_runs): sorted runs of kRun, then every entry's place
+// among all.  Within a run an entry's rank is the number of those before it, counted by
 // comparing all with all: a workgroup ranks 64 positions, one per lane, and its
-// waves share out the others.  (16384 positions: 6.5 and 5.0 us.  The whole gradient
-// of 50257 x 768, with this and with the radix sort below: 16384 positions 57 and 77
-// us, 65536 119 and 134, 131072 218 and 175.)
-constexpr int kRun = 2048, kRunsMax = 65536, kRankThreads = 1024;
+// waves share out the others.  (16384 positions: 6.5 and 5.0 us.)
+constexpr int kRun = 2048, kRankThreads = 1024;
 __global__ __launch_bounds__(kRankThreads) void rank_kernel(const int* __restrict__ tokens, int N, int V,
                                                             Entry* __restrict__ out) {
   constexpr int W = kRankThreads / 64;
@@ -210,8 +208,9 @@ __global__ __launch_bounds__(256) void merge_runs_kernel(const Entry* __restrict
 // More positions: a stable radix sort from the lowest digit up.  At most
 // kSortBlocks workgroups each own a run of positions; a pass counts every
 // run's digits, and a run's entries of digit x go behind all lower digits and
-// the earlier runs' x.  The counts of a later pass are taken while the pass before
-// it places its entries.
+// the earlier runs' x.  Every pass counts by itself: counts taken while the pass
+// before places its entries are atomics that a frequent token sends to one address
+// (200000 positions, one in 16 the same token: 51 us a pass, 5 and 9 by itself).
 constexpr int kDigitBits = 9, kBins = 1 << kDigitBits, kSortThreads = 1024, kSortBlocks = 256;
 
 // positions of a run: as few sub-tiles of 2 per thread as keep the runs within kSortBlocks
@@ -226,28 +225,37 @@ inline int sort_passes(int V) {  // keys 0 .. V
   return (bits + kDigitBits - 1) / kDigitBits;
 }
 
-// counts of the first pass; clears those of the others
-__global__ __launch_bounds__(kSortThreads) void count_kernel(const int* __restrict__ tokens, int N, int V, int run,
-                                                             int passes, int* __restrict__ counts) {
+// Whether positions are sorted by runs.  The radix sort's time is its passes', two
+// launches each; the runs' grows with the square of their number.  The whole gradient by
+// runs and by radix (us): 50257 x 768, two passes, 16384 positions 57 and 65, 32768
+// 66 and 66, 65536 118 and 101; 300000 x 128, three, 32768 48 and 57, 50000 69 and 66;
+// 500 x 128, one, 3000 27 and 24.
+inline bool by_runs(int N, int V) {
+  const int passes = sort_passes(V);
+  return N <= (passes == 1 ? kRun : 16384 * passes);
+}
+
+// every run's digits of a pass, from the tokens (in == nullptr) or entries
+__global__ __launch_bounds__(kSortThreads) void count_kernel(const int* __restrict__ tokens,
+                                                             const Entry* __restrict__ in, int N, int V, int run,
+                                                             int pass, int* __restrict__ counts) {
   __shared__ int bins[kBins];
-  const int t = threadIdx.x, b = blockIdx.x, blocks = gridDim.x;
+  const int t = threadIdx.x, b = blockIdx.x, shift = pass * kDigitBits;
   if (t < kBins) bins[t] = 0;
   __syncthreads();
   const int to = min((int64_t)N, (int64_t)(b + 1) * run);
-  for (int j = b * run + t; j < to; j += kSortThreads) atomicAdd(&bins[key_of(tokens[j], V) & (kBins - 1)], 1);
+  for (int j = b * run + t; j < to; j += kSortThreads)
+    atomicAdd(&bins[((in ? in[j].key : key_of(tokens[j], V)) >> shift) & (kBins - 1)], 1);
   __syncthreads();
-  if (t < kBins) {
-    counts[(size_t)b * kBins + t] = bins[t];
-    for (int p = 1; p < passes; ++p) counts[((size_t)p * blocks + b) * kBins + t] = 0;
-  }
+  if (t < kBins) counts[(size_t)b * kBins + t] = bins[t];
 }
 
 // one pass: from the tokens (in == nullptr) or entries, to entries (200000 positions:
-// 51 us, bound by the ranks within a run and the counts of the runs before)
+// 9.4 us, bound by the latency of its steps)
 __global__ __launch_bounds__(kSortThreads) void place_kernel(const int* __restrict__ tokens,
                                                              const Entry* __restrict__ in, int N, int V, int run,
                                                              int pass, const int* __restrict__ counts,
-                                                             Entry* __restrict__ out, int* __restrict__ next_counts) {
+                                                             Entry* __restrict__ out) {
   constexpr int W = kSortThreads / 64;
   __shared__ int base[kBins];       // where the run's next entry of a digit goes
   __shared__ int cnt[W][kBins];     // a sub-tile's entries of a digit, by wave; then their offsets
@@ -257,6 +265,7 @@ __global__ __launch_bounds__(kSortThreads) void place_kernel(const int* __restri
   // base: all lower digits, then the earlier runs' entries of this one
   int total = 0, before = 0;
   if (t < kBins) {
+#pragma unroll 16
     for (int k = 0; k < blocks; ++k) {
       const int c = counts[(size_t)k * kBins + t];
       before += k < b ? c : 0;
@@ -318,8 +327,6 @@ __global__ __launch_bounds__(kSortThreads) void place_kernel(const int* __restri
       if (j < end) {
         const int to = cnt[w][(e[r].key >> shift) & (kBins - 1)] + rank[r];
         out[to] = e[r];
-        if (next_counts)
-          atomicAdd(&next_counts[(size_t)(to / run) * kBins + ((e[r].key >> (shift + kDigitBits)) & (kBins - 1))], 1);
       }
     }
     __syncthreads();
@@ -670,11 +677,11 @@ Layout layout(int n, int vocab, int d) {
   l.pieces = grad_pieces((int64_t)n + vocab, (int64_t)vocab * d * 4, d);  // (no fewer than a call has)
   l.entries[0] = take((size_t)n * sizeof(Entry));
   if (n > kRun) l.entries[1] = take((size_t)n * sizeof(Entry));
-  if (n > kRunsMax) {
+  if (!by_runs(n, vocab)) {
     l.run = sort_run(n);
     l.blocks = (n + l.run - 1) / l.run;
     l.passes = sort_passes(vocab);
-    l.counts = take((size_t)l.passes * l.blocks * kBins * 4);
+    l.counts = take((size_t)l.blocks * kBins * 4);
   }
   l.head = take((size_t)l.pieces * d * 4);
   l.tail = take((size_t)l.pieces * d * 4);
@@ -795,16 +802,14 @@ extern "C" ssd_status ssd_embed_grad(ssd_dtype grad_dtype, ssd_dtype table_dtype
   char* ws = (char*)workspace;
   hipStream_t s = (hipStream_t)stream;
   Entry *sorted = (Entry*)(ws + l.entries[0]), *other = (Entry*)(ws + l.entries[1]);
-  if (n > kRunsMax) {
+  if (!by_runs(n, vocab)) {
     int* counts = (int*)(ws + l.counts);
-    count_kernel<<<l.blocks, kSortThreads, 0, s>>>(tokens, n, vocab, l.run, l.passes, counts);
-    OP_LAUNCHED();
-    const size_t step = (size_t)l.blocks * kBins;
     for (int p = 0; p < l.passes; ++p) {
       Entry* to = (l.passes - p) & 1 ? sorted : other;  // (the last pass ends in sorted)
       const Entry* from = p == 0 ? nullptr : to == sorted ? other : sorted;
-      place_kernel<<<l.blocks, kSortThreads, 0, s>>>(tokens, from, n, vocab, l.run, p, counts + p * step, to,
-                                                     p + 1 < l.passes ? counts + (p + 1) * step : nullptr);
+      count_kernel<<<l.blocks, kSortThreads, 0, s>>>(tokens, from, n, vocab, l.run, p, counts);
+      OP_LAUNCHED();
+      place_kernel<<<l.blocks, kSortThreads, 0, s>>>(tokens, from, n, vocab, l.run, p, counts, to);
       OP_LAUNCHED();
     }
   } else if (n > 0 && !few(n, vocab, d)) {

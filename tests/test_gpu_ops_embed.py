@@ -306,3 +306,12 @@ def test_gradient_between_other_columns(env, gd, td, n):
         want = ops.embed_grad(tokens.cuda(), grad.cuda(), v, out=base, accumulate=accumulate)
         assert torch.equal(table[:, 3:3 + d], want)
         before = want.clone()
+
+
+@pytest.mark.parametrize("kind", ["zipf", "one", "even"])
+@pytest.mark.parametrize("n,v", [(2048, 511), (2049, 511), (70000, 511), (32768, 512), (32769, 512), (32769, 262143),
+                                 (49152, 262144), (49153, 262144), (100001, 300000), (600001, 1000)])
+def test_sorts_of_one_two_and_three_digits(env, n, v, kind):
+    torch, ops = env
+    gen = torch.Generator().manual_seed(n + v)
+    check_grad(torch, ops, "f32", "f32", draw_tokens(gen, torch, n, v, kind), torch.randn(n, 5, generator=gen), v)
