@@ -66,7 +66,8 @@ ssd_status ssd_prefix_attn_workspace(const ssd_prefix_attn_desc *a, size_t *byte
  *   dtype SSD_F32 or SSD_BF16; head_dim 32, 64 or 128; n_head a multiple of
  * n_kv_head; 1 <= n_seq <= 4096, 1 <= n_query <= 64, prefix_len, own_rows >= 0
  * and below 2^30.  Pointers are 16-byte aligned and strides multiples of 16
- * bytes; out's rows do not overlap.  k_prefix and v_prefix may be NULL when
+ * bytes; out's rows do not overlap, nor does out share an element with an
+ * input.  k_prefix and v_prefix may be NULL when
  * prefix_len is 0, k_own and v_own when own_rows is 0.  Scores and sums are
  * float32; bfloat16 calls round the weights exp(x - max) to bfloat16 for the
  * product with the values.

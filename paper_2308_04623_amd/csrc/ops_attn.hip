@@ -729,10 +729,10 @@ __global__ __launch_bounds__(64 * kWaves, D == 128 ? 2 : D == 64 ? 3 : 4) void s
 // (256 / D)-th part.  Bound: memory (7680 queries of 128, 9 parts each: 8.4 us, 4.4 TB/s)
 // or, for few, the launch (4 us).
 template <typename T, int D>
-__global__ __launch_bounds__(256) void merge_kernel(PrefixAttnArgs a, int queries) {
+__global__ __launch_bounds__(256) void merge_kernel(PrefixAttnArgs a, int first, int queries) {
   constexpr int LD = D / 4, PAR = 64 / LD;
   const ssd_prefix_attn_desc& d = a.d;
-  const int lane = threadIdx.x & 63, q = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, q = first + blockIdx.x * 4 + (threadIdx.x >> 6);
   if (q >= queries) return;
   const int h = q % d.n_head, bt = q / d.n_head, t = bt % d.n_query, b = bt / d.n_query, len = min(a.own_len[b], d.own_rows);
   const int np = len < 0 ? 0 : a.p_chunks, no = len > 0 ? (len + a.o_chunk - 1) / a.o_chunk : 0, n = np + no;
@@ -764,6 +764,7 @@ __global__ __launch_bounds__(256) void merge_kernel(PrefixAttnArgs a, int querie
 }
 
 constexpr int kMaxRows = 1 << 30;
+constexpr int kMergeQueries = 1 << 25;  // of a launch: a grid holds fewer than 2^32 threads
 
 ssd_status check(const ssd_prefix_attn_desc* a) {
   OP_REQUIRE(a, SSD_E_INVALID_ARG, "null argument");
@@ -888,8 +889,11 @@ hipError_t launch(const PrefixAttnArgs& a, int64_t blocks, hipStream_t s) {
   e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int n = a.d.n_seq * a.d.n_query * a.d.n_head;
-  merge_kernel<T, D><<<(n + 3) / 4, 256, 0, s>>>(a, n);
-  return hipGetLastError();
+  for (int first = 0; first < n && e == hipSuccess; first += kMergeQueries) {
+    merge_kernel<T, D><<<(std::min(n - first, kMergeQueries) + 3) / 4, 256, 0, s>>>(a, first, n);
+    e = hipGetLastError();
+  }
+  return e;
 }
 template <typename T, int D, int MO>
 hipError_t launch_short(const PrefixAttnArgs& a, int64_t blocks, hipStream_t s) {
@@ -944,6 +948,7 @@ extern "C" ssd_status ssd_prefix_attn(const ssd_prefix_attn_desc* a, const void*
   OP_REQUIRE(q && own_len && out && workspace, SSD_E_INVALID_ARG, "null argument");
   OP_REQUIRE(a->prefix_len == 0 || (k_prefix && v_prefix), SSD_E_INVALID_ARG, "null prefix");
   OP_REQUIRE(a->own_rows == 0 || (k_own && v_own), SSD_E_INVALID_ARG, "null own rows");
+  OP_REQUIRE(out != q, SSD_E_INVALID_ARG, "out is the queries");
   const void* pointers[] = {q, k_prefix, v_prefix, k_own, v_own, out};
   for (const void* x : pointers)
     OP_REQUIRE((uintptr_t)x % 16 == 0, SSD_E_UNSUPPORTED, "a pointer is not 16-byte aligned");

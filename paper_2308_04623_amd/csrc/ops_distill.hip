@@ -573,6 +573,36 @@ void launch_grad(const DistillArgs& a, int n, hipStream_t s) {
   else distill_grad_kernel<T, 512><<<dim3(n, (a.V + 512 * per - 1) / (512 * per)), 512, 0, s>>>(a);
 }
 
+// Calls launch(arguments, rows) for at most kSlice rows at a time: a grid holds
+// fewer than 2^32 threads.
+constexpr int kSlice = 1 << 21;
+template <typename T, typename Launch>
+hipError_t by_slices(DistillArgs a, int n, Launch launch) {
+  for (;;) {
+    const int rows = n < kSlice ? n : kSlice;
+    launch(a, rows);
+    const hipError_t e = hipGetLastError();
+    n -= rows;
+    if (e != hipSuccess || n == 0) return e;
+    a.logits = (const T*)a.logits + (size_t)rows * a.ld;
+    a.ids += (size_t)rows * a.K;
+    a.vals += (size_t)rows * a.K;
+    a.lse += rows;
+    if (a.weight) a.weight += rows;
+    if (a.loss) a.loss += rows;
+    if (a.grad) a.grad = (T*)a.grad + (size_t)rows * a.ld_d;
+  }
+}
+
+template <typename T, bool GRAD>
+hipError_t rows(const DistillArgs& a, int n, hipStream_t s) {
+  return by_slices<T>(a, n, [s](const DistillArgs& x, int m) { launch_rows<T, GRAD>(x, m, s); });
+}
+template <typename T>
+hipError_t gradient(const DistillArgs& a, int n, hipStream_t s) {
+  return by_slices<T>(a, n, [s](const DistillArgs& x, int m) { launch_grad<T>(x, m, s); });
+}
+
 }  // namespace
 }  // namespace ssd
 
@@ -587,9 +617,9 @@ extern "C" ssd_status ssd_distill_forward(ssd_dtype dtype, const void* logits, i
   if (n_rows == 0) return SSD_OK;
   OP_REQUIRE(loss && lse, SSD_E_INVALID_ARG, "null argument");
   DistillArgs a{logits, ld, vocab, ids, vals, k, weight, 1.f / temperature, loss, lse, nullptr, 0};
-  if (dtype == SSD_F32) launch_rows<float, false>(a, n_rows, (hipStream_t)stream);
-  else launch_rows<bf16_t, false>(a, n_rows, (hipStream_t)stream);
-  OP_LAUNCHED();
+  const hipError_t e = dtype == SSD_F32 ? rows<float, false>(a, n_rows, (hipStream_t)stream)
+                                        : rows<bf16_t, false>(a, n_rows, (hipStream_t)stream);
+  if (e != hipSuccess) return op_fail(SSD_E_DEVICE, hipGetErrorString(e));
   return SSD_OK;
 }
 
@@ -603,9 +633,9 @@ extern "C" ssd_status ssd_distill_step(ssd_dtype dtype, const void* logits, int6
   if (n_rows == 0) return SSD_OK;
   OP_REQUIRE(loss && lse, SSD_E_INVALID_ARG, "null argument");
   DistillArgs a{logits, ld, vocab, ids, vals, k, weight, 1.f / temperature, loss, lse, dlogits, ld_d};
-  if (dtype == SSD_F32) launch_rows<float, true>(a, n_rows, (hipStream_t)stream);
-  else launch_rows<bf16_t, true>(a, n_rows, (hipStream_t)stream);
-  OP_LAUNCHED();
+  const hipError_t e = dtype == SSD_F32 ? rows<float, true>(a, n_rows, (hipStream_t)stream)
+                                        : rows<bf16_t, true>(a, n_rows, (hipStream_t)stream);
+  if (e != hipSuccess) return op_fail(SSD_E_DEVICE, hipGetErrorString(e));
   return SSD_OK;
 }
 
@@ -619,8 +649,8 @@ extern "C" ssd_status ssd_distill_backward(ssd_dtype dtype, const void* logits, 
   if (n_rows == 0) return SSD_OK;
   OP_REQUIRE(lse, SSD_E_INVALID_ARG, "null argument");
   DistillArgs a{logits, ld, vocab, ids, vals, k, weight, 1.f / temperature, nullptr, (float*)lse, dlogits, ld_d};
-  if (dtype == SSD_F32) launch_grad<float>(a, n_rows, (hipStream_t)stream);
-  else launch_grad<bf16_t>(a, n_rows, (hipStream_t)stream);
-  OP_LAUNCHED();
+  const hipError_t e = dtype == SSD_F32 ? gradient<float>(a, n_rows, (hipStream_t)stream)
+                                        : gradient<bf16_t>(a, n_rows, (hipStream_t)stream);
+  if (e != hipSuccess) return op_fail(SSD_E_DEVICE, hipGetErrorString(e));
   return SSD_OK;
 }

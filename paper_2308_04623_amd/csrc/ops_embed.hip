@@ -733,15 +733,19 @@ ssd_status check(int32_t n, int32_t vocab, int32_t d) {
 template <typename T>
 void launch_embed_rows(int out_dtype, const int* tokens, int n, const void* table, int64_t ld_table, int V, int d,
                        float scale, void* out, int64_t ld_out, hipStream_t s) {
-  const int per = (d + 7) / 8;
-  const int64_t parts = (int64_t)n * per;
-  const unsigned grid = (unsigned)((parts + 255) / 256);
-  if (out_dtype == SSD_F32)
-    embed_rows_kernel<<<grid, 256, 0, s>>>(tokens, parts, per, (const T*)table, ld_table, V, d, scale, (float*)out,
-                                           ld_out);
-  else
-    embed_rows_kernel<<<grid, 256, 0, s>>>(tokens, parts, per, (const T*)table, ld_table, V, d, scale, (bf16_t*)out,
-                                           ld_out);
+  const int per = (d + 7) / 8, slice = (1 << 30) / per;  // (a grid holds fewer than 2^32 threads)
+  for (int first = 0; first < n; first += slice) {
+    const int rows = std::min(n - first, slice);
+    const int64_t parts = (int64_t)rows * per;
+    const unsigned grid = (unsigned)((parts + 255) / 256);
+    char* to = (char*)out + (size_t)first * ld_out * op_size(out_dtype);
+    if (out_dtype == SSD_F32)
+      embed_rows_kernel<<<grid, 256, 0, s>>>(tokens + first, parts, per, (const T*)table, ld_table, V, d, scale,
+                                             (float*)to, ld_out);
+    else
+      embed_rows_kernel<<<grid, 256, 0, s>>>(tokens + first, parts, per, (const T*)table, ld_table, V, d, scale,
+                                             (bf16_t*)to, ld_out);
+  }
 }
 
 }  // namespace

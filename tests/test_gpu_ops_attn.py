@@ -318,3 +318,24 @@ def test_long_own_rows(env, dtype, b, p):
     torch, ops = env
     x, lens = make(torch, dtype, b, 2, 4, 2, 64, p, 1333, seed=p, lens=[1333 - 700 * (i % 2) for i in range(b)])
     check(torch, ops, dtype, x, lens)
+
+
+def test_more_queries_than_a_launch_joins(env):
+    torch, ops = env
+    x, _ = make(torch, "bf16", 2, 64, 136, 8, 32, 2060, 2)  # 4096 x 64 x 136 queries, 2^25 a launch
+    ref, _, big, vmax = reference(x, [2, 0])
+    q, ko, vo = (x[k].cuda().repeat(2048, 1, 1, 1) for k in ("q", "ko", "vo"))
+    n = torch.tensor([2, 0], dtype=torch.int32, device="cuda").repeat(2048)
+    out = ops.prefix_attention(q, x["kp"].cuda(), x["vp"].cuda(), ko, vo, n)
+    ref = torch.from_numpy(ref).cuda()
+    for i in range(0, 4096, 2):
+        assert float((out[i:i + 2].double() - ref).abs().max()) <= tolerance("bf16", 32, big, vmax)
+
+
+def test_out_is_not_the_queries(env):
+    torch, ops = env
+    from paper_2308_04623_amd.ssd import SSDError
+    x, lens = make(torch, "bf16", 2, 1, 4, 2, 64, 8, 4)
+    a = [x[k].cuda() for k in ("q", "kp", "vp", "ko", "vo")] + [torch.tensor(lens, dtype=torch.int32, device="cuda")]
+    with pytest.raises(SSDError):
+        ops.prefix_attention(*a, out=a[0])

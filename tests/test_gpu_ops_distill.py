@@ -307,3 +307,24 @@ def test_many_rows_of_every_length(env, dtype, chunks, odd):
     if not odd:  # rows alike give the same, wherever they stand
         for x in (*forward, back, *step):
             assert torch.equal(x[5:10], x[:5]) and torch.equal(x[255:], x[:5])
+
+
+# more rows than one launch takes (2^21): rows of both sides of the cut and of the ends
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_more_rows_than_a_launch(env, dtype):
+    torch, ops = env
+    cut, v, k, T = 1 << 21, 24, 2, 1.25
+    z, ids, vals, w = make(torch, dtype, 64, v, k)
+    n = cut + 77
+    big = [torch.cat([t.cuda()] * (n // 64 + 1))[:n].contiguous() for t in (z, ids, vals, w)]
+    loss, lse, grad = ops.distill_step(*big, temperature=T)
+    loss2, lse2 = ops.distill_forward(*big, temperature=T)
+    back = ops.distill_backward(*big[:3], lse, big[3], temperature=T)
+    small = [t.cuda() for t in (z, ids, vals, w)]
+    a = ops.distill_step(*small, temperature=T)
+    b = ops.distill_backward(*small[:3], a[1], small[3], temperature=T)
+    assert torch.equal(loss, loss2) and torch.equal(lse, lse2)
+    for got, want in ((loss, a[0]), (lse, a[1]), (grad, a[2]), (back, b)):
+        want = torch.cat([want] * (n // 64 + 1))[:n]
+        assert torch.equal(got, want)
+    check(torch, ops, dtype, z, ids, vals, w, T=T)

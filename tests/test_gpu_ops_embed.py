@@ -315,3 +315,14 @@ def test_sorts_of_one_two_and_three_digits(env, n, v, kind):
     torch, ops = env
     gen = torch.Generator().manual_seed(n + v)
     check_grad(torch, ops, "f32", "f32", draw_tokens(gen, torch, n, v, kind), torch.randn(n, 5, generator=gen), v)
+
+
+def test_more_rows_than_a_launch(env):
+    torch, ops = env
+    d, n = 65536, (1 << 30) // 8192 + 5  # 2^30 threads of eight columns a launch
+    gen = torch.Generator().manual_seed(8)
+    table = torch.randn(7, d, generator=gen).bfloat16().cuda()
+    tokens = draw_tokens(gen, torch, n, 7, "even").cuda()
+    out = ops.embed(tokens, table, scale=2.0)
+    for i in list(range(0, n, 8192)) + [n - 64]:  # (twice a bfloat16 number is exact)
+        assert torch.equal(out[i:i + 8192], 2.0 * table[tokens[i:i + 8192].long()])
