@@ -68,23 +68,31 @@ struct Block {
   }
 };
 
-// Copies the q-th KB of a block of keys (half 0) or values (1), rows kb .. of a
-// matrix (those from `end` on: row end - 1 again), into LDS at dst.  By a whole wave.
-template <typename T, int D, int CPOL>
-__device__ __forceinline__ void copy_1k(const char* base, int half, int q, int64_t row, int kb, int end,
-                                        unsigned char* dst, int lane) {
+// The q-th KB of a block of keys (half 0) or values (1) is copied by a wave, 16 bytes a
+// lane: bytes lane_at .. of the block's row lane_row.
+template <typename T, int D>
+__device__ __forceinline__ int lane_row(int q) {
+  return (q * 64 + (int)(threadIdx.x & 63)) / Block<T, D>::CH;
+}
+template <typename T, int D>
+__device__ __forceinline__ int lane_at(int half, int q) {
   typedef Block<T, D> B;
-  const int p = q * 64 + lane, r = p / B::CH, c = (p % B::CH) ^ (half ? B::swz_v(r) : B::swz_k(r));
-  const char* src = base + (int64_t)min(kb + r, end - 1) * row + 16 * c;
+  const int p = q * 64 + (int)(threadIdx.x & 63), r = p / B::CH;
+  return 16 * (p % B::CH ^ (half ? B::swz_v(r) : B::swz_k(r)));
+}
+template <int CPOL>
+__device__ __forceinline__ void copy_1k(const char* src, unsigned char* dst) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
                                    (__attribute__((address_space(3))) void*)dst, 16, 0, CPOL);
 }
-// the whole block; LOADS copies in flight
+// The whole block, rows kb .. of a matrix (those from `end` on: row end - 1 again), into
+// LDS at dst; LOADS copies in flight.
 template <typename T, int D, int HALF>
 __device__ __forceinline__ void issue(const Range& s, int kb, int end, unsigned char* dst) {
 #pragma unroll
   for (int i = 0; i < Block<T, D>::LOADS; ++i)
-    copy_1k<T, D, 2>(HALF ? s.v : s.k, HALF, i, s.row, kb, end, dst + i * 1024, threadIdx.x & 63);
+    copy_1k<2>((HALF ? s.v : s.k) + (int64_t)min(kb + lane_row<T, D>(i), end - 1) * s.row + lane_at<T, D>(HALF, i),
+               dst + i * 1024);
 }
 
 // the wave's copies but the last N are in LDS
@@ -131,6 +139,49 @@ __device__ __forceinline__ void read_transposed(unsigned a0, unsigned a1, unsign
       : "memory");
 }
 
+// The same, and 2^x of eight numbers while the reads are under way.
+template <int OFF>
+__device__ __forceinline__ void read_transposed(unsigned a0, unsigned a1, unsigned a2, unsigned a3, u32x2 (&f0)[2],
+                                                u32x2 (&f1)[2], u32x2 (&f2)[2], u32x2 (&f3)[2], f32x4 (&x)[2]) {
+  float e0 = x[0][0], e1 = x[0][1], e2 = x[0][2], e3 = x[0][3], e4 = x[1][0], e5 = x[1][1], e6 = x[1][2], e7 = x[1][3];
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %16\n"
+      "ds_read_b64_tr_b16 %1, %16 offset:%20\n"
+      "ds_read_b64_tr_b16 %2, %17\n"
+      "ds_read_b64_tr_b16 %3, %17 offset:%20\n"
+      "ds_read_b64_tr_b16 %4, %18\n"
+      "ds_read_b64_tr_b16 %5, %18 offset:%20\n"
+      "ds_read_b64_tr_b16 %6, %19\n"
+      "ds_read_b64_tr_b16 %7, %19 offset:%20\n"
+      "v_exp_f32 %8, %8\n"
+      "v_exp_f32 %9, %9\n"
+      "v_exp_f32 %10, %10\n"
+      "v_exp_f32 %11, %11\n"
+      "v_exp_f32 %12, %12\n"
+      "v_exp_f32 %13, %13\n"
+      "v_exp_f32 %14, %14\n"
+      "v_exp_f32 %15, %15\n"
+      "s_waitcnt lgkmcnt(0)\n"
+      "s_nop 0"
+      : "=&v"(f0[0]), "=&v"(f0[1]), "=&v"(f1[0]), "=&v"(f1[1]), "=&v"(f2[0]), "=&v"(f2[1]), "=&v"(f3[0]),
+        "=&v"(f3[1]), "+v"(e0), "+v"(e1), "+v"(e2), "+v"(e3), "+v"(e4), "+v"(e5), "+v"(e6), "+v"(e7)
+      : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "n"(OFF)
+      : "memory");
+  x[0] = (f32x4){e0, e1, e2, e3};
+  x[1] = (f32x4){e4, e5, e6, e7};
+}
+
+// 2^x of the tiles from FROM on
+template <int FROM, int MT, int KT>
+__device__ __forceinline__ void exp2_all(f32x4 (&s)[MT][KT]) {
+#pragma unroll
+  for (int mt = FROM; mt < MT; ++mt)
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s[mt][kt][r] = __builtin_amdgcn_exp2f(s[mt][kt][r]);
+}
+
 // the operands and products of one type: S^T (keys x queries) and O^T (dims x queries)
 template <typename T, int D, int MT>
 struct Math;
@@ -142,18 +193,24 @@ struct Math<bf16_t, D, MT> {
   // lane l: keys 4 (l / 16) + r of each 16-key tile, query l % 16
   static __device__ __forceinline__ void scores(const unsigned char* k, const u32x4 (&q)[MT][KK], f32x4 (&s)[MT][KT]) {
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    u32x4 f[KT][KK];
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) {
         const int r = 16 * kt + n;
-        const u32x4 f = *(const u32x4*)(k + r * B::ROW + 16 * ((4 * kk + g) ^ B::swz_k(r)));
+        f[kt][kk] = *(const u32x4*)(k + r * B::ROW + 16 * ((4 * kk + g) ^ B::swz_k(r)));
+      }
+    __builtin_amdgcn_sched_barrier(0);  // (all reads under way before the first product; 128 dims 339 us, 350 without)
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
-          s[mt][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f),
+          s[mt][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f[kt][kk]),
                                                               __builtin_bit_cast(bf16x8, q[mt][kk]),
                                                               kk ? s[mt][kt] : (f32x4){0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-      }
   }
   struct P {
     u32x4 w[MT];
@@ -173,17 +230,27 @@ struct Math<bf16_t, D, MT> {
   struct V {
     u32x2 f[DT][2];
   };
-  static __device__ __forceinline__ void values(const unsigned char* v, V& x) {
+  // EXP: the weights are made of their exponents on the way
+  template <bool EXP>
+  static __device__ __forceinline__ void values(const unsigned char* v, V& x, f32x4 (&s)[MT][KT]) {
     // a 16-lane group reads four rows of 16 dims and gets them transposed
     const int lane = threadIdx.x & 63, r = 4 * (lane >> 4) + ((lane & 15) >> 2);
     const unsigned at = (unsigned)(size_t)(lds_byte*)v + r * B::ROW + 16 * (((lane & 3) >> 1) ^ B::swz_v(r)) +
                         8 * (lane & 1);
-    if constexpr (DT == 2) read_transposed<16 * B::ROW>(at, at ^ 32, x.f[0], x.f[1]);
-    else
+    if constexpr (DT == 2) {
+      read_transposed<16 * B::ROW>(at, at ^ 32, x.f[0], x.f[1]);
+      if (EXP) exp2_all<0>(s);
+    } else {
 #pragma unroll
       for (int dt = 0; dt < DT; dt += 4)
-        read_transposed<16 * B::ROW>(at ^ (32 * dt), at ^ (32 * (dt + 1)), at ^ (32 * (dt + 2)), at ^ (32 * (dt + 3)),
-                                     x.f[dt], x.f[dt + 1], x.f[dt + 2], x.f[dt + 3]);
+        if (EXP && dt / 4 < MT)
+          read_transposed<16 * B::ROW>(at ^ (32 * dt), at ^ (32 * (dt + 1)), at ^ (32 * (dt + 2)), at ^ (32 * (dt + 3)),
+                                       x.f[dt], x.f[dt + 1], x.f[dt + 2], x.f[dt + 3], s[dt / 4]);
+        else
+          read_transposed<16 * B::ROW>(at ^ (32 * dt), at ^ (32 * (dt + 1)), at ^ (32 * (dt + 2)), at ^ (32 * (dt + 3)),
+                                       x.f[dt], x.f[dt + 1], x.f[dt + 2], x.f[dt + 3]);
+      if (EXP) exp2_all<DT / 4>(s);
+    }
   }
   // clears infinities and NaNs; whether there were any
   static __device__ __forceinline__ bool clear(V& x) {
@@ -241,8 +308,10 @@ struct Math<float, D, MT> {
   struct V {
     f32x4 f[DT];
   };
-  static __device__ __forceinline__ void values(const unsigned char* v, V& x) {
+  template <bool EXP>
+  static __device__ __forceinline__ void values(const unsigned char* v, V& x, f32x4 (&s)[MT][KT]) {
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    if (EXP) exp2_all<0>(s);
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -326,20 +395,27 @@ struct Wave {
     }
   }
 
-  // the weights of rows kb .. of a block from their raw scores; lane's query mt
-  // sees rows below lim[mt], and every query those below `all`
-  __device__ __forceinline__ void weigh(f32x4 (&s)[MT][KT], int kb, int all, const int (&lim)[MT], float scale2,
-                                        typename M::P& p) {
-    const int g = (threadIdx.x & 63) >> 4;
-    const bool masked = kb + KB > all;
+  // The first row of a block that the lane has scores of.  (Opaque: its comparisons
+  // are not to be prepared in blocks that are not masked.)
+  static __device__ __forceinline__ int lane_key(int kb) {
+    int row = kb + 4 * (int)((threadIdx.x & 63) >> 4);
+    asm volatile("" : "+v"(row));
+    return row;
+  }
+
+  // The exponents of the weights of rows kb .. of a block from their raw scores.
+  // masked: lane's query mt sees rows below lim[mt]; else all see all.
+  __device__ __forceinline__ void exponents(f32x4 (&s)[MT][KT], int kb, bool masked, const int (&lim)[MT],
+                                            float scale2) {
     if (masked) {
+      const int row = lane_key(kb);
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (kb + 16 * kt + 4 * g + r >= lim[mt]) s[mt][kt][r] = -INFINITY;
+            if (row + 16 * kt + r >= lim[mt]) s[mt][kt][r] = -INFINITY;
     }
     float top[MT];
     bool above = false;
@@ -369,16 +445,22 @@ struct Wave {
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) s[mt][kt][r] = __builtin_amdgcn_exp2f(fmaf(s[mt][kt][r], scale2, -ref));
+        for (int r = 0; r < 4; ++r) s[mt][kt][r] = fmaf(s[mt][kt][r], scale2, -ref);
     }
+  }
+
+  // takes the weights into the sums
+  __device__ __forceinline__ void sums(f32x4 (&s)[MT][KT], int kb, bool masked, const int (&lim)[MT],
+                                       typename M::P& p) {
     if (masked) {  // (whatever came of -infinity times a scale of 0)
+      const int row = lane_key(kb);
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (kb + 16 * kt + 4 * g + r >= lim[mt]) s[mt][kt][r] = 0.f;
+            if (row + 16 * kt + r >= lim[mt]) s[mt][kt][r] = 0.f;
     }
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
@@ -409,6 +491,7 @@ struct Wave {
     M::add(x, p, o);
     if (masked && __builtin_amdgcn_ballot_w64(bad)) {
       const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll 1
       for (int r = 0; r < KB; ++r)
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
@@ -422,6 +505,23 @@ struct Wave {
             }
           }
     }
+  }
+
+  // All that a block's scores and values add.  Values under way are waited for
+  // by landed(), behind the exponentials; those THERE are read while they are taken.
+  template <bool THERE, typename Landed>
+  __device__ __forceinline__ void take(f32x4 (&x)[MT][KT], const unsigned char* v, int kb, bool masked,
+                                       const int (&lim)[MT], float scale2, Landed landed) {
+    exponents(x, kb, masked, lim, scale2);
+    if (!THERE) {
+      exp2_all<0>(x);
+      landed();
+    }
+    typename M::V f;
+    M::template values<THERE>(v, f, x);
+    typename M::P p;
+    sums(x, kb, masked, lim, p);
+    add(f, v, p, kb, masked, lim);
   }
 
   // the sums of l over the lanes of a query
@@ -492,13 +592,11 @@ __device__ __forceinline__ void walk(Wave<T, D, MT>& s, const Range& range, int 
       reads_over();
       issue<T, D, 0>(range, kb + STEP, k1, k);
     }
-    typename W::M::P p;
-    s.weigh(x, kb, all, lim, scale2, p);
-    if (more) copies_landed<B::LOADS>();  // (the next keys may be)
-    else copies_landed<0>();
-    typename W::M::V f;
-    W::M::values(v, f);
-    s.add(f, v, p, kb, kb + KB > all, lim);
+    auto landed = [&] {
+      if (more) copies_landed<B::LOADS>();  // (the next keys may be)
+      else copies_landed<0>();
+    };
+    s.template take<false>(x, v, kb, kb + KB > all, lim, scale2, landed);
     if (more) {
       reads_over();
       issue<T, D, 1>(range, kb + STEP, k1, v);
@@ -575,13 +673,45 @@ struct Stage {
   typedef Block<T, D> B;
   static constexpr int SUB = 128 / D, ROWS = SUB * B::KB, BYTES = SUB * 2 * B::BYTES, PER = BYTES / 1024 / kWaves;
   static_assert(BYTES == 16384 && PER == 4, "four copies a wave");
-  static __device__ __forceinline__ void issue(const Range& s, int kb, int end, unsigned char* dst) {
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  typedef uint64_t u64x4 __attribute__((ext_vector_type(4)));
+  u64x4 at;  // where the lane's copies of the next stage begin
+
+  static __device__ __forceinline__ void place(int i, int& half, int& q, int& sub) {
+    const int j = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * PER + i;
+    sub = j / (2 * B::LOADS);
+    half = j / B::LOADS % 2;
+    q = j % B::LOADS;
+  }
+  __device__ __forceinline__ void start(const Range& s, int kb) {
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int j = w * PER + i, sub = j / (2 * B::LOADS), half = j / B::LOADS % 2, q = j % B::LOADS;
-      copy_1k<T, D, 0>(half ? s.v : s.k, half, q, s.row, kb + sub * B::KB, end, dst + j * 1024, lane);
+      int half, q, sub;
+      place(i, half, q, sub);
+      at[i] = (uint64_t)((half ? s.v : s.k) + (int64_t)(kb + sub * B::KB + lane_row<T, D>(q)) * s.row +
+                         lane_at<T, D>(half, q));
     }
+  }
+  // The stage of rows kb .., the next after the last one issued; rows from `end` on: row
+  // end - 1 again.  (Whole stages from addresses kept: a row's product for each copy was a
+  // third of the instructions around the matrix products, 303 us for 65536 rows, 350 with it.)
+  __device__ __forceinline__ void issue(const Range& s, int kb, int end, unsigned char* dst) {
+    dst += __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * (PER * 1024);
+    if (kb + ROWS <= end) {
+      copy_1k<0>((const char*)at[0], dst);
+      copy_1k<0>((const char*)at[1], dst + 1024);
+      copy_1k<0>((const char*)at[2], dst + 2048);
+      copy_1k<0>((const char*)at[3], dst + 3072);
+    } else {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        int half, q, sub;
+        place(i, half, q, sub);
+        copy_1k<0>((half ? s.v : s.k) + (int64_t)min(kb + sub * B::KB + lane_row<T, D>(q), end - 1) * s.row +
+                       lane_at<T, D>(half, q),
+                   dst + i * 1024);
+      }
+    }
+    at += (uint64_t)(ROWS * s.row);
   }
 };
 
@@ -594,8 +724,10 @@ __device__ __forceinline__ void part_by_queries(const PrefixAttnArgs& a, Queries
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   qs.first += w * (MT * 16);
   const bool work = qs.first < qs.count;  // (a wave without queries still copies its share)
-  S::issue(range, k0, k1, lds);
-  if (k0 + S::ROWS < k1) S::issue(range, k0 + S::ROWS, k1, lds + S::BYTES);
+  S copies;
+  copies.start(range, k0);
+  copies.issue(range, k0, k1, lds);
+  if (k0 + S::ROWS < k1) copies.issue(range, k0 + S::ROWS, k1, lds + S::BYTES);
   W s;
   s.load(a, qs);
   int lim[MT];
@@ -612,7 +744,7 @@ __device__ __forceinline__ void part_by_queries(const PrefixAttnArgs& a, Queries
     __builtin_amdgcn_sched_barrier(0);
     int ahead = slot + 2;
     if (ahead >= kStages) ahead -= kStages;
-    if (kb + 2 * S::ROWS < k1) S::issue(range, kb + 2 * S::ROWS, k1, lds + ahead * S::BYTES);
+    if (kb + 2 * S::ROWS < k1) copies.issue(range, kb + 2 * S::ROWS, k1, lds + ahead * S::BYTES);
     if (work) {
 #pragma unroll
       for (int sub = 0; sub < S::SUB; ++sub) {
@@ -621,11 +753,7 @@ __device__ __forceinline__ void part_by_queries(const PrefixAttnArgs& a, Queries
         const unsigned char *k = lds + slot * S::BYTES + sub * (2 * B::BYTES), *v = k + B::BYTES;
         f32x4 x[MT][W::KT];
         s.scores(k, x);
-        typename W::M::P p;
-        s.weigh(x, kr, k1, lim, a.scale2, p);
-        typename W::M::V f;
-        W::M::values(v, f);
-        s.add(f, v, p, kr, kr + B::KB > k1, lim);
+        s.template take<true>(x, v, kr, kr + B::KB > k1, lim, a.scale2, [] {});
       }
       reads_over();
     }
@@ -650,7 +778,7 @@ __device__ __forceinline__ void part_by_queries(const PrefixAttnArgs& a, Queries
 // Few queries are bound by memory (16 sequences of 20 heads of 64 over 100,000 rows: 82
 // to 86 us, 6.1 TB/s), many by the matrix products and the LDS reads that feed them, which
 // take alike with 32 queries a wave (48 x 5 queries, 32 heads on 8 of 128, over 8191 rows: 57
-// us and 8 to join; 65536 rows: 348 us, 741 TFLOP/s).
+// us and 8 to join; 65536 rows: 303 us, 850 TFLOP/s).
 template <typename T, int D, int MP, int MO, bool BYQ>
 __global__ __launch_bounds__(64 * kWaves, D == 128 ? 2 : D == 64 ? 3 : 4) void prefix_attn_kernel(PrefixAttnArgs a) {
   extern __shared__ __align__(512) unsigned char lds[];  // (a block's rows lie at multiples of their size)
