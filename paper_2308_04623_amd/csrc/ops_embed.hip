@@ -130,6 +130,39 @@ __global__ __launch_bounds__(256) void embed_rows_kernel(const int* __restrict__
 
 // ---------------------------------------------------------------- sort by token
 
+// The sort leaves most of the chip's bandwidth alone, and most rows of a table are zeros
+// whatever the sort finds: its launches carry workgroups that clear the table's first
+// rows (see fill_bytes), and embed_grad_kernel skips those of tokens that do not occur.
+struct Fill {
+  void* table;
+  int64_t ld;      // bytes from row to row
+  int row;         // bytes of a row
+  int wide;        // rows begin and end at multiples of 16 bytes, else of 4
+  int first, last; // rows
+  int blocks;      // workgroups
+};
+// by a workgroup of `threads`, number b of f.blocks
+template <typename U>
+__device__ __forceinline__ void clear_by(const Fill& f, int b, int threads) {
+  const int per = f.row / (int)sizeof(U), rows = (f.last - f.first + f.blocks - 1) / f.blocks;
+  const int r0 = f.first + b * rows, n = min(rows, f.last - r0);
+  char* table = (char*)f.table + (size_t)r0 * f.ld;
+  const int down = threads / per, right = threads - down * per;
+  for (int r = (int)threadIdx.x / per, c = (int)threadIdx.x - r * per; r < n;) {
+    __builtin_nontemporal_store(U{}, (U*)(table + (size_t)r * f.ld) + c);
+    r += down;
+    c += right;
+    if (c >= per) {
+      c -= per;
+      ++r;
+    }
+  }
+}
+__device__ __forceinline__ void clear_rows(const Fill& f, int b, int threads) {
+  if (f.wide) clear_by<u32x4>(f, b, threads);
+  else clear_by<unsigned>(f, b, threads);
+}
+
 // a token and its position; tokens outside the vocabulary sort last, as V
 struct Entry {
   int key, pos;
@@ -143,8 +176,10 @@ __device__ __forceinline__ int key_of(int token, int V) { return token >= 0 && t
 // waves share out the others.  (16384 positions: 6.5 and 5.0 us.)
 constexpr int kRun = 2048, kRankThreads = 1024;
 __global__ __launch_bounds__(kRankThreads) void rank_kernel(const int* __restrict__ tokens, int N, int V,
-                                                            Entry* __restrict__ out) {
+                                                            Entry* __restrict__ out, Fill fill) {
   constexpr int W = kRankThreads / 64;
+  const int blocks = (N + 63) / 64;
+  if ((int)blockIdx.x >= blocks) return clear_rows(fill, blockIdx.x - blocks, kRankThreads);
   __shared__ __align__(16) int keys[kRun];
   __shared__ int count[W][64];
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
@@ -185,7 +220,10 @@ __global__ __launch_bounds__(kRankThreads) void rank_kernel(const int* __restric
 // An entry's place: its own in its run, and in every other run the number of
 // lower keys, equal ones included in the runs before.  Eight threads an entry take
 // the runs in turn.  (32768 positions: 9.2 us to rank, 8.7 to place.)
-__global__ __launch_bounds__(256) void merge_runs_kernel(const Entry* __restrict__ in, int N, Entry* __restrict__ out) {
+__global__ __launch_bounds__(256) void merge_runs_kernel(const Entry* __restrict__ in, int N, Entry* __restrict__ out,
+                                                         Fill fill) {
+  const int blocks = (N + 31) / 32;
+  if ((int)blockIdx.x >= blocks) return clear_rows(fill, blockIdx.x - blocks, 256);
   const int e = (blockIdx.x * 256 + threadIdx.x) >> 3, sub = threadIdx.x & 7;
   const int i = min(e, N - 1), mine = i / kRun, runs = (N + kRun - 1) / kRun;
   const Entry x = in[i];
@@ -238,7 +276,9 @@ inline bool by_runs(int N, int V) {
 // every run's digits of a pass, from the tokens (in == nullptr) or entries
 __global__ __launch_bounds__(kSortThreads) void count_kernel(const int* __restrict__ tokens,
                                                              const Entry* __restrict__ in, int N, int V, int run,
-                                                             int pass, int* __restrict__ counts) {
+                                                             int pass, int* __restrict__ counts, int blocks,
+                                                             Fill fill) {
+  if ((int)blockIdx.x >= blocks) return clear_rows(fill, blockIdx.x - blocks, kSortThreads);
   __shared__ int bins[kBins];
   const int t = threadIdx.x, b = blockIdx.x, shift = pass * kDigitBits;
   if (t < kBins) bins[t] = 0;
@@ -255,12 +295,13 @@ __global__ __launch_bounds__(kSortThreads) void count_kernel(const int* __restri
 __global__ __launch_bounds__(kSortThreads) void place_kernel(const int* __restrict__ tokens,
                                                              const Entry* __restrict__ in, int N, int V, int run,
                                                              int pass, const int* __restrict__ counts,
-                                                             Entry* __restrict__ out) {
+                                                             Entry* __restrict__ out, int blocks, Fill fill) {
+  if ((int)blockIdx.x >= blocks) return clear_rows(fill, blockIdx.x - blocks, kSortThreads);
   constexpr int W = kSortThreads / 64;
   __shared__ int base[kBins];       // where the run's next entry of a digit goes
   __shared__ int cnt[W][kBins];     // a sub-tile's entries of a digit, by wave; then their offsets
   __shared__ int wsum[kBins / 64];
-  const int t = threadIdx.x, lane = t & 63, w = t >> 6, b = blockIdx.x, blocks = gridDim.x;
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6, b = blockIdx.x;
   const int shift = pass * kDigitBits;
   // base: all lower digits, then the earlier runs' entries of this one
   int total = 0, before = 0;
@@ -344,6 +385,7 @@ struct GradArgs {
   int64_t ld_table;
   float scale;
   float *head, *tail;  // [pieces][d] partial sums
+  int zeroed;          // the table's rows below are zeros already
   int* open;           // [pieces]: the token whose earlier terms are in the pieces before and that ends here, or -1
 };
 
@@ -402,7 +444,8 @@ __device__ __forceinline__ int rows_after(const Staged& s, int N, int i, int v) 
 
 // The table written whole: a workgroup per piece, a thread per four columns (16384
 // bfloat16 rows of 1280 to 50257 of float32: 52 us, 5.8 TB/s).
-template <typename G, typename T>
+// CLEARED: rows below a.zeroed are zeros already.
+template <typename G, typename T, bool CLEARED>
 __global__ __launch_bounds__(1024) void embed_grad_kernel(GradArgs a) {
   constexpr int U = kInFlight;
   __shared__ Entry lds[kStaged];
@@ -452,6 +495,11 @@ __global__ __launch_bounds__(1024) void embed_grad_kernel(GradArgs a) {
     acc = (f32x4){0.f, 0.f, 0.f, 0.f};
   };
 
+  // from v, or behind it: the next token up to `to` whose row is not zeros already
+  auto skip = [&](int to) {
+    if (CLEARED) v = max(v, min(to, a.zeroed));
+  };
+
   for (int j0 = i0; j0 < i1; j0 += U) {
     if (min(j0 + U, i1) > es.base + es.n) es.stage(j0, i1);
     f32x4 r[U];
@@ -468,12 +516,20 @@ __global__ __launch_bounds__(1024) void embed_grad_kernel(GradArgs a) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (key[u] >= a.V) continue;
-      for (; v < key[u]; ++v) end();
+      if (CLEARED && !cont && terms == 0) skip(key[u]);
+      for (; v < key[u]; skip(key[u])) {
+        end();
+        ++v;
+      }
       acc += r[u];
       ++terms;
     }
   }
-  for (; v < v1; ++v) end();
+  if (CLEARED && !cont && terms == 0) skip(v1);
+  for (; v < v1; skip(v1)) {
+    end();
+    ++v;
+  }
   if (terms && col) store4(a.tail + (size_t)g * a.d, c, a.d, acc);
   if (blockIdx.y == 0 && threadIdx.x == 0) a.open[g] = opened;
 }
@@ -662,6 +718,16 @@ int grad_pieces(int64_t places, int64_t table_bytes, int d) {
 
 size_t round256(size_t x) { return (x + 255) / 256 * 256; }
 
+// Bytes of the table that a launch of the sort clears: what it has time for.  Ranks of up to
+// 8192 positions leave half of the CUs idle, the radix sort's launches wait for memory;
+// the ranks of more positions need the whole chip, and small tables are soon written.  The
+// whole gradient, bfloat16 to float32 without and with (us): 50257 x 1280, 1000
+// positions 58 and 54, 16384 71.4 and 70.6 (not taken: 58.5 and 60 to bfloat16); 50257 x 768, 3000
+// positions 49 and 43; 131072 x 450, 5000 positions 92 and 82; 131072 x 280 bfloat16, 70000
+// positions 79 and 74 (24 MB a launch: 75).
+constexpr int64_t kFillTable = 32 << 20, kFillBlock = 64 << 10;  // least table; bytes of a workgroup
+int64_t fill_bytes(int n, int V) { return by_runs(n, V) ? (n <= 8192 ? 32 << 20 : 0) : 12 << 20; }
+
 struct Layout {
   size_t entries[2], counts, head, tail, open, bytes;
   int pieces, blocks, run, passes;
@@ -708,7 +774,8 @@ void launch_grad(const GradArgs& a, const int* tokens, hipStream_t s) {
   const int quads = (a.d + 3) / 4, threads = grad_threads(a.d);
   const dim3 grid(a.pieces, (quads + threads - 1) / threads);
   if (ACC) embed_grad_add_kernel<G, T><<<grid, threads, 0, s>>>(a);
-  else embed_grad_kernel<G, T><<<grid, threads, 0, s>>>(a);
+  else if (a.zeroed) embed_grad_kernel<G, T, true><<<grid, threads, 0, s>>>(a);
+  else embed_grad_kernel<G, T, false><<<grid, threads, 0, s>>>(a);
   embed_join_kernel<T, ACC><<<dim3((a.pieces + kJoined - 1) / kJoined, (quads + kJoinQuads - 1) / kJoinQuads),
                               kJoinThreads, 0, s>>>(a);
 }
@@ -806,22 +873,42 @@ extern "C" ssd_status ssd_embed_grad(ssd_dtype grad_dtype, ssd_dtype table_dtype
   char* ws = (char*)workspace;
   hipStream_t s = (hipStream_t)stream;
   Entry *sorted = (Entry*)(ws + l.entries[0]), *other = (Entry*)(ws + l.entries[1]);
+  int zeroed = 0;
+  auto share = [&](int64_t bytes) {  // of the table for the next launch to clear
+    Fill f{};
+    const int es = op_size(table_dtype);
+    const uintptr_t at = (uintptr_t)dtable | (uintptr_t)(ld_table * es) | (uintptr_t)(d * es);
+    if (accumulate || at % 4 != 0 || (int64_t)vocab * d * es < kFillTable) return f;
+    f.table = dtable;
+    f.ld = ld_table * es;
+    f.row = d * es;
+    f.wide = at % 16 == 0;
+    f.first = zeroed;
+    f.last = zeroed = (int)std::min<int64_t>(vocab, zeroed + bytes / f.row);
+    f.blocks = (int)std::min<int64_t>(f.last - f.first, (int64_t)(f.last - f.first) * f.row / kFillBlock + 1);
+    return f;
+  };
   if (!by_runs(n, vocab)) {
     int* counts = (int*)(ws + l.counts);
     for (int p = 0; p < l.passes; ++p) {
       Entry* to = (l.passes - p) & 1 ? sorted : other;  // (the last pass ends in sorted)
       const Entry* from = p == 0 ? nullptr : to == sorted ? other : sorted;
-      count_kernel<<<l.blocks, kSortThreads, 0, s>>>(tokens, from, n, vocab, l.run, p, counts);
+      Fill f = share(fill_bytes(n, vocab));
+      count_kernel<<<l.blocks + f.blocks, kSortThreads, 0, s>>>(tokens, from, n, vocab, l.run, p, counts, l.blocks, f);
       OP_LAUNCHED();
-      place_kernel<<<l.blocks, kSortThreads, 0, s>>>(tokens, from, n, vocab, l.run, p, counts, to);
+      f = share(fill_bytes(n, vocab));
+      place_kernel<<<l.blocks + f.blocks, kSortThreads, 0, s>>>(tokens, from, n, vocab, l.run, p, counts, to, l.blocks,
+                                                                f);
       OP_LAUNCHED();
     }
   } else if (n > 0 && !few(n, vocab, d)) {
     const bool one = n <= kRun;
-    rank_kernel<<<(n + 63) / 64, kRankThreads, 0, s>>>(tokens, n, vocab, one ? sorted : other);
+    Fill f = share(fill_bytes(n, vocab));
+    rank_kernel<<<(n + 63) / 64 + f.blocks, kRankThreads, 0, s>>>(tokens, n, vocab, one ? sorted : other, f);
     OP_LAUNCHED();
     if (!one) {
-      merge_runs_kernel<<<(n + 31) / 32, 256, 0, s>>>(other, n, sorted);
+      f = share(fill_bytes(n, vocab));
+      merge_runs_kernel<<<(n + 31) / 32 + f.blocks, 256, 0, s>>>(other, n, sorted, f);
       OP_LAUNCHED();
     }
   }
@@ -839,6 +926,7 @@ extern "C" ssd_status ssd_embed_grad(ssd_dtype grad_dtype, ssd_dtype table_dtype
   a.dtable = dtable;
   a.ld_table = ld_table;
   a.scale = scale;
+  a.zeroed = zeroed;
   a.head = (float*)(ws + l.head);
   a.tail = (float*)(ws + l.tail);
   a.open = (int*)(ws + l.open);

@@ -326,3 +326,27 @@ def test_more_rows_than_a_launch(env):
     out = ops.embed(tokens, table, scale=2.0)
     for i in list(range(0, n, 8192)) + [n - 64]:  # (twice a bfloat16 number is exact)
         assert torch.equal(out[i:i + 8192], 2.0 * table[tokens[i:i + 8192].long()])
+
+
+# tables of which the sort's launches clear some rows, all of them or none; what lies
+# between the rows stays
+@pytest.mark.parametrize("td", ["f32", "bf16"])
+@pytest.mark.parametrize("n,v,d,pad", [(300, 40000, 256, 0), (5000, 40000, 512, 0), (5000, 40000, 510, 6),
+                                       (8192, 9000, 1100, 3), (8193, 40000, 512, 0), (60000, 131072, 256, 8),
+                                       (300, 16777216, 4, 0), (2049, 30011, 1027, 1)])
+def test_rows_cleared_beside_the_sort(env, td, n, v, d, pad):
+    torch, ops = env
+    gen = torch.Generator().manual_seed(n)
+    tokens, grad = draw_tokens(gen, torch, n, v, "zipf").cuda(), torch.randn(n, d, generator=gen).bfloat16().cuda()
+    room = torch.full((v, d + pad), float("nan"), dtype=dt(torch, td), device="cuda")
+    out = ops.embed_grad(tokens, grad, v, scale=0.5, out=room[:, :d])
+    ok = (tokens >= 0) & (tokens < v)
+    ref = torch.zeros(v, d, dtype=torch.float64, device="cuda")
+    mag = torch.zeros(v, d, dtype=torch.float64, device="cuda")
+    count = torch.bincount(tokens[ok].long(), minlength=v)
+    ref.index_add_(0, tokens[ok].long(), 0.5 * grad[ok].double())
+    mag.index_add_(0, tokens[ok].long(), 0.5 * grad[ok].double().abs())
+    tol = (count + 1).double()[:, None] * EPS * mag + (2.0 ** -8 * ref.abs() if td == "bf16" else 0.0)
+    assert bool(((out.double() - ref).abs() <= tol).all())
+    assert pad == 0 or bool(room[:, d:].isnan().all())
+    assert torch.equal(ops.embed_grad(tokens, grad, v, scale=0.5, dtype=dt(torch, td)), out)
