@@ -109,6 +109,8 @@ def _elsewhere(dev: int, stream):
     """None where the call's stream and device are the current ones, else the
     context that makes them so (what is allocated inside belongs to the stream)."""
     if stream is not None:
+        if stream.device_index != dev:
+            _refuse("stream", f"the stream is on device {stream.device_index}, the tensors on {dev}")
         return torch.cuda.stream(stream)
     return None if dev == torch.cuda.current_device() else torch.cuda.device(dev)
 
@@ -121,13 +123,42 @@ _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_get
 
 # ---------------------------------------------------------------- attention
 
-@functools.lru_cache(maxsize=256)
-def _attn_plan(dtype, b, t, h, d, g, p, r, scale, *strides):
-    """The description of a call's shapes and its workspace's bytes."""
-    a = _PrefixAttnDesc(_DTYPES[dtype], b, t, h, g, d, p, r, 1.0 / math.sqrt(d) if scale is None else scale, *strides)
+def _layout(t):
+    return t.dtype, t.shape, t.stride(), t.get_device()
+
+
+# calls' descriptions and workspaces' bytes by their tensors' layouts: what was found in order
+# is not looked at again (5 of a short call's 13 us)
+_attn_plans = {}
+
+
+def _attn_plan(q, k_prefix, v_prefix, k_own, v_own, own_len, scale, out):
+    """The description of a call's shapes (out None: contiguous) and its workspace's bytes."""
+    try:
+        key = (_layout(q), _layout(k_prefix), _layout(v_prefix), _layout(k_own), _layout(v_own), _layout(own_len), scale,
+               None if out is None else _layout(out))
+        plan = _attn_plans.get(key)
+    except (AttributeError, TypeError):  # (not all tensors: refused below)
+        key = plan = None
+    if plan is not None:
+        return plan
+    _refuse_attn(q, k_prefix, v_prefix, k_own, v_own, own_len, out)
+    b, t, h, d = q.shape
+    g, p, _ = k_prefix.shape
+    r = k_own.shape[2]
+    # (a dimension of one entry has no stride to speak of)
+    by = lambda strides, sizes: [x if n > 1 else 0 for x, n in zip(strides, sizes)]  # noqa: E731
+    a = _PrefixAttnDesc(_DTYPES[q.dtype], b, t, h, g, d, p, r, 1.0 / math.sqrt(d) if scale is None else scale,
+                        *by(q.stride(), (b, t, h)), *by((t * h * d, h * d, d) if out is None else out.stride(), (b, t, h)),
+                        *by(k_prefix.stride(), (g, p)), *by(k_own.stride(), (b, g, r)))
     need = C.c_size_t(0)
     _check(_ops().ssd_prefix_attn_workspace(C.byref(a), C.byref(need)), "ssd_prefix_attn")
-    return C.byref(a), need.value
+    plan = C.byref(a), need.value
+    if key is not None:
+        if len(_attn_plans) >= 256:
+            _attn_plans.clear()
+        _attn_plans[key] = plan
+    return plan
 
 
 def _refuse_attn(q, k_prefix, v_prefix, k_own, v_own, own_len, out):
@@ -165,24 +196,15 @@ def prefix_attention(q, k_prefix, v_prefix, k_own, v_own, own_len, scale: Option
     bfloat16, any strides that are multiples of 16 bytes with D contiguous (K and
     V alike).  scale defaults to 1 / sqrt(D).  Returns out [B][T][H][D], or (out,
     lse float32 [B][T][H])."""
-    _refuse_attn(q, k_prefix, v_prefix, k_own, v_own, own_len, out)
+    a, need = _attn_plan(q, k_prefix, v_prefix, k_own, v_own, own_len, scale, out)
     dev = q.get_device()
     where = _elsewhere(dev, stream)
     if where is not None:
         with where:
             return prefix_attention(q, k_prefix, v_prefix, k_own, v_own, own_len, scale, out, return_lse)
     if out is None:
-        out = q.new_empty(q.shape)
-    b, t, h, d = q.shape
-    g, p, _ = k_prefix.shape
-    r = k_own.shape[2]
-    lse = torch.empty((b, t, h), dtype=torch.float32, device=q.device) if return_lse else None
-    # (a dimension of one entry has no stride to speak of)
-    qs, os, ps, ks = q.stride(), out.stride(), k_prefix.stride(), k_own.stride()
-    a, need = _attn_plan(q.dtype, b, t, h, d, g, p, r, scale, qs[0] if b > 1 else 0, qs[1] if t > 1 else 0,
-                         qs[2] if h > 1 else 0, os[0] if b > 1 else 0, os[1] if t > 1 else 0, os[2] if h > 1 else 0,
-                         ps[0] if g > 1 else 0, ps[1] if p > 1 else 0, ks[0] if b > 1 else 0, ks[1] if g > 1 else 0,
-                         ks[2] if r > 1 else 0)
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device) if return_lse else None
     work = torch.empty(need, dtype=torch.uint8, device=q.device)
     _check(_ops().ssd_prefix_attn(a, q.data_ptr(), k_prefix.data_ptr(), v_prefix.data_ptr(), k_own.data_ptr(),
                                   v_own.data_ptr(), own_len.data_ptr(), out.data_ptr(),
@@ -211,7 +233,7 @@ def _logits(what, logits, ids, vals, weight):
 
 def _grad_out(what, logits, out):
     if out is None:
-        return logits.new_empty(logits.shape)
+        return torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
     _tensor(what, "out", out, (logits.dtype,), 2, logits)
     if out.shape != logits.shape:
         _refuse(what, f"out {tuple(out.shape)} must be {tuple(logits.shape)}")
