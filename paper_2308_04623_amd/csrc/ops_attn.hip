@@ -854,41 +854,66 @@ __global__ __launch_bounds__(64 * kWaves, D == 128 ? 2 : D == 64 ? 3 : 4) void s
 }
 
 // A wave per query adds its parts: lane l has dims 4 (l % (D / 4)) .. + 3 and every
-// (256 / D)-th part.  Bound: memory (7680 queries of 128, 9 parts each: 8.4 us, 4.4 TB/s)
-// or, for few, the launch (4 us).
+// (256 / D)-th part.  All parts' places are read, without waiting for the sequence's length to
+// tell which of them were written (32 sequences over 2048 rows, both kernels: 15.3 us with the
+// length first and a pass for the maximum, 14.5 so).  Bound: memory (7680 queries of 128,
+// 9 parts each: 8.4 us, 4.4 TB/s) or, for few, the launch (4 us).
 template <typename T, int D>
 __global__ __launch_bounds__(256) void merge_kernel(PrefixAttnArgs a, int first, int queries) {
-  constexpr int LD = D / 4, PAR = 64 / LD;
+  constexpr int LD = D / 4, PAR = 64 / LD, U = 4;
   const ssd_prefix_attn_desc& d = a.d;
   const int lane = threadIdx.x & 63, q = first + blockIdx.x * 4 + (threadIdx.x >> 6);
   if (q >= queries) return;
   const int h = q % d.n_head, bt = q / d.n_head, t = bt % d.n_query, b = bt / d.n_query, len = min(a.own_len[b], d.own_rows);
-  const int np = len < 0 ? 0 : a.p_chunks, no = len > 0 ? (len + a.o_chunk - 1) / a.o_chunk : 0, n = np + no;
   const float2* ml = a.ml + (size_t)q * a.parts;
   const float* po = a.o + (size_t)q * a.parts * D;
-  float top = -INFINITY;
-  for (int i = lane; i < n; i += 64) top = fmaxf(top, ml[i < np ? i : i - np + a.p_chunks].x);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  float total = 0.f;
   const int x = lane % LD;
-#pragma unroll 4
-  for (int i = lane / LD; i < n; i += PAR) {
-    const int s = i < np ? i : i - np + a.p_chunks;
-    const float2 p = ml[s];
-    const f32x4 v = *(const f32x4*)(po + (size_t)s * D + 4 * x);
-    const float c = p.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(p.x - top);
-    acc += c * v;
-    total += c * p.y;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  float top = -INFINITY, total = 0.f;
+  for (int i = lane / LD; i < a.parts; i += U * PAR) {
+    float2 p[U];
+    f32x4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int s = i + u * PAR;
+      p[u].x = -INFINITY;
+      if (s < a.parts) {
+        p[u] = ml[s];
+        v[u] = *(const f32x4*)(po + (size_t)s * D + 4 * x);
+      }
+    }
+    float m = top;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int s = i + u * PAR;
+      if (s < a.p_chunks ? len < 0 : (s - a.p_chunks) * a.o_chunk >= len) p[u].x = -INFINITY;
+      m = fmaxf(m, p[u].x);
+    }
+    const float c = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - m);
+    acc *= c;
+    total *= c;
+    top = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (p[u].x != -INFINITY) {
+        const float w = __builtin_amdgcn_exp2f(p[u].x - m);
+        acc += w * v[u];
+        total += w * p[u].y;
+      }
   }
+  float all = top;
+#pragma unroll
+  for (int o = 32; o >= LD; o >>= 1) all = fmaxf(all, __shfl_xor(all, o));
+  const float c = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - all);
+  acc *= c;
+  total *= c;
 #pragma unroll
   for (int o = 32; o >= LD; o >>= 1) {
     total += __shfl_xor(total, o);
 #pragma unroll
     for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], o);
   }
-  if (lane < LD) put_query<T>(a, b, t, h, x, acc, top, total);
+  if (lane < LD) put_query<T>(a, b, t, h, x, acc, all, total);
 }
 
 constexpr int kMaxRows = 1 << 30;
