@@ -952,21 +952,25 @@ ssd_status check_strides(const ssd_prefix_attn_desc* a) {
 //   Alone (short_attn_kernel): a sequence's queries take the prefix and their own rows
 // in one workgroup, where the prefix is short for the number of workgroups that
 // read it again: up to 2 steps of the four waves (a step: 128 rows of bfloat16, 64
-// of float32), and where a tile's 32 columns are more than half used, 1 more per 16
+// of float32), and where a tile's 32 columns are more than half used, 1 and 1 more per 16
 // workgroups up to 16 steps; and where a sequence's own rows would be one chunk, or
 // both are 4 steps.  Measured, split and alone (us): 1 sequence of 20 heads of 64, 256 rows
-// and 64 of its own 7.7 and 6.1, 1024 rows 9.0 and 11.3; 128 sequences of it, 128
-// rows 22.4 and 20.1, 512 rows 24.3 and 32.7; 8 queries, 16 heads on 4 of 128: 8
-// sequences, 512 rows 14.3 and 13.8, 1024 rows 15.3 and 18.2; 64 sequences, 2048 rows 39.9
-// and 28.1; float32, 512 rows 49 and 34.  48 x 5 queries, 32 heads on 8 of 128:
-// 2048 rows 50 and 43, 4096 rows 58 and 69.
+// and 64 of its own 7.2 and 5.8, 1024 rows 7.5 and 9.0; 128 sequences of it, 128
+// rows 22 and 20, 512 rows 24 and 32; 8 queries, 16 heads on 4 of 128: 8
+// sequences, 256 rows 12.3 and 11.9, 512 rows 12.8 and 14.1; 64 sequences, 2048 rows 38
+// and 28; float32, 512 rows 49 and 33.  48 x 5 queries, 32 heads on 8 of 128:
+// 2048 rows 39 and 34, 4096 rows 46 and 55.
 //   Else the prefix is read once for all.  Up to 32 queries of a kv head: one
 // tile, the waves split the rows.  More: tiles of 64 or 128, the waves split the
-// queries.  The rows are cut so that the workgroups are one round over the CUs, two a CU where there
-// are products to overlap: more, shorter chunks cost more parts than they even out
-// (16 sequences over 100,000 rows: 97 us with 256 workgroups, 100 with 512, 103 with
-// 1024; 48 x 5 queries over 8,191 with grouped heads: 83, 67 and 78 us).
+// queries.  The rows are cut so that the workgroups are one round over the CUs, and two a CU where
+// there are products to overlap, in chunks longer than kOverlap rows: more, shorter chunks cost
+// more parts than they even out (16 sequences over 100,000 rows: 97 us with 256
+// workgroups, 100 with 512, 103 with 1024; 48 x 5 queries with grouped heads, with 256, 512
+// and 1024: 65,536 rows 426, 298 and 310 us, 8,191 rows 71, 71 and 83, 4,096 rows 43, 46 and
+// 57; 33 x 2, 20 heads of 64 over 3000 rows 16.5, 19.4 and 19.4; 20 x 8 float32, 32 heads on
+// 8 of 128 over 3000 rows 92, 89 and 99).
 constexpr int kRound = 256;
+constexpr int kOverlap = 1024, kOverlapF32 = 256;  // (products of float32 take four times as long)
 
 struct Plan {
   bool alone;  // see short_attn_kernel
@@ -994,15 +998,17 @@ Plan plan(const ssd_prefix_attn_desc* a) {
   p.p_cols = 16 * p.mp * (p.byq ? kWaves : 1);
   p.p_tiles = (int)div_up(cols, p.p_cols);
   p.o_tiles = (int)div_up(own_cols, 16 * p.mo);
-  const int round = p.byq ? 2 * kRound : kRound;
   auto cut = [&](int64_t rows, int64_t sets, int& chunks, int& chunk) {
+    const bool twice = p.byq && div_up(rows, std::max<int64_t>(kRound / sets, 1)) >
+                                    (a->dtype == SSD_F32 ? kOverlapF32 : kOverlap);
+    const int round = twice ? 2 * kRound : kRound;
     const int64_t want = std::min(std::max<int64_t>(round / sets, 1), std::max<int64_t>(div_up(rows, step), 1));
     chunk = (int)(div_up(std::max<int64_t>(div_up(rows, want), 1), step) * step);
     chunks = (int)div_up(rows, chunk);
   };
   const int64_t own_blocks = (int64_t)a->n_seq * a->n_kv_head * p.o_tiles;
   cut(a->own_rows, own_blocks, p.o_chunks, p.o_chunk);
-  const int64_t again = 2 + (p.mo == 2 ? std::min<int64_t>(own_blocks / 16, 14) : 0);
+  const int64_t again = p.mo == 2 ? std::clamp<int64_t>(1 + own_blocks / 16, 2, 16) : 2;
   p.alone = a->prefix_len <= again * step && (p.o_chunks <= 1 || (int64_t)a->prefix_len + a->own_rows <= 4 * step);
   if (p.alone) {
     p.blocks = own_blocks;
