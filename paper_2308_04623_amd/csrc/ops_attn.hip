@@ -776,9 +776,9 @@ __device__ __forceinline__ void part_by_queries(const PrefixAttnArgs& a, Queries
 
 // BYQ: the prefix's workgroups share their blocks among the waves (part_by_queries).
 // Few queries are bound by memory (16 sequences of 20 heads of 64 over 100,000 rows: 82
-// to 86 us, 6.1 TB/s), many by the matrix products and the LDS reads that feed them, which
-// take alike with 32 queries a wave (48 x 5 queries, 32 heads on 8 of 128, over 8191 rows: 57
-// us and 8 to join; 65536 rows: 303 us, 850 TFLOP/s).
+// us, 6.1 TB/s), many by the softmax's vector instructions and the matrix products, which
+// follow each other with 32 queries a wave (48 x 5 queries, 32 heads on 8 of 128, over 8191
+// rows: 52 us and 8 to join; 65536 rows: 303 us, 850 TFLOP/s).
 template <typename T, int D, int MP, int MO, bool BYQ>
 __global__ __launch_bounds__(64 * kWaves, D == 128 ? 2 : D == 64 ? 3 : 4) void prefix_attn_kernel(PrefixAttnArgs a) {
   extern __shared__ __align__(512) unsigned char lds[];  // (a block's rows lie at multiples of their size)
