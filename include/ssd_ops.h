@@ -60,7 +60,9 @@ ssd_status ssd_prefix_attn_workspace(const ssd_prefix_attn_desc *a, size_t *byte
  * softmax of scale q.k over the seen rows times their values; rows that are
  * not seen are never looked at and may hold anything.  A query that sees no
  * row gives 0, and so do the queries of a sequence with own_len[b] < 0 (an
- * unused slot of the batch); lengths past own_rows count as own_rows.
+ * unused slot of the batch); lengths past own_rows count as own_rows.  A row whose
+ * score is -infinity counts as one that is not seen; a score of NaN makes the
+ * query's out and lse NaN.
  * lse, if not NULL: float32 [n_seq][n_query][n_head], the log of the sum of
  * exponentials of the seen scores (-infinity where there are none).
  *   dtype SSD_F32 or SSD_BF16; head_dim 32, 64 or 128; n_head a multiple of

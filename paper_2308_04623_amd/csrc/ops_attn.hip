@@ -524,12 +524,14 @@ struct Wave {
     add(f, v, p, kb, masked, lim);
   }
 
-  // the sums of l over the lanes of a query
+  // The sums of l over the lanes of a query.  A reference of -infinity says that no row
+  // was seen; NaN scores do not raise it, so a sum of theirs takes 0 and is joined as any other.
   __device__ __forceinline__ void close() {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       l[mt] += __shfl_xor(l[mt], 16);
       l[mt] += __shfl_xor(l[mt], 32);
+      if (m[mt] == -INFINITY && l[mt] != l[mt]) m[mt] = 0.f;
     }
   }
 };

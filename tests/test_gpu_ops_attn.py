@@ -374,3 +374,58 @@ def test_more_layouts_than_are_remembered(env):
             if p % 60 == 0:
                 w = torch.softmax((q[0, 0, :, None].double() * k[:, :p].double()).sum(2) / 32 ** 0.5, 1)
                 assert float((out[0, 0] - (w[:, :, None] * k[:, :p].double()).sum(1)).abs().max()) < 1e-5
+
+
+# how a call is cut: one launch, the waves split the rows, the waves split the queries (one and two tiles each)
+FORMS = {"alone": (4, 1, 4, 2, 60), "rows": (4, 1, 4, 2, 3000), "queries": (21, 2, 4, 4, 3000),
+         "many": (24, 3, 6, 2, 3000)}
+
+
+def check_with_nan(torch, ops, dtype, x, lens):
+    """As check, where some results are NaN: the same ones, out and lse."""
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    out, lse = ops.prefix_attention(*(x[k].cuda() for k in ("q", "kp", "vp", "ko", "vo")), n, return_lse=True)
+    clean = {k: torch.nan_to_num(v) for k, v in x.items()}
+    ref, rl, _, _ = reference(x, lens)
+    _, _, big, vmax = reference(clean, lens)
+    d = x["q"].shape[3]
+    for got, want, tol in ((out, ref, tolerance(dtype, d, big, vmax)),
+                           (lse, rl, (d + 4) * EPS * big + 64 * EPS * (1 + np.abs(rl[np.isfinite(rl)]).max()))):
+        got = got.double().cpu().numpy()
+        assert np.array_equal(np.isnan(got), np.isnan(want))
+        assert np.array_equal(np.isneginf(got), np.isneginf(want))
+        live = np.isfinite(want)
+        assert np.abs(got[live] - want[live]).max() <= tol
+    return ref
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("form", list(FORMS))
+def test_nan_scores_are_not_lost(env, dtype, d, form):
+    """A NaN in a query, in the only row of a sequence's own, in all keys of a stretch
+    of the prefix: the queries that see it are NaN, with their lse, and no others."""
+    torch, ops = env
+    b, t, h, g, p = FORMS[form]
+    # (the longest own rows are one chunk: a part of their own where the prefix is cut)
+    lens = [(20, 1, -1, 0)[i % 4] for i in range(b)]
+    nan = float("nan")
+    x, lens = make(torch, dtype, b, t, h, g, d, p, 20, seed=d, lens=lens)
+    x["q"][1, 0, 2, 5] = nan
+    x["q"][2, t - 1, 0, 0] = nan  # of a slot that is off
+    assert np.isnan(check_with_nan(torch, ops, dtype, x, lens)).all(3).sum() == 1
+    x, lens = make(torch, dtype, b, t, h, g, d, p, 20, seed=d, lens=lens)
+    x["ko"][1, 0, 0, 7] = nan
+    assert np.isnan(check_with_nan(torch, ops, dtype, x, lens)).all(3).sum() == h // g  # (the last query alone sees it)
+    x, lens = make(torch, dtype, b, t, h, g, d, p, 20, seed=d, lens=lens)
+    x["kp"][g - 1, p // 3:2 * p // 3, 1] = nan
+    x["kp"][0, 0, 0] = nan if g > 2 else 0.0
+    assert np.isnan(check_with_nan(torch, ops, dtype, x, lens)).any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_query_of_nan_that_sees_no_row(env, dtype):
+    torch, ops = env
+    x, lens = make(torch, dtype, 3, 2, 4, 2, 64, 0, 20, lens=[0, 1, 20])
+    x["q"][:2] = float("nan")
+    check_with_nan(torch, ops, dtype, x, lens)
