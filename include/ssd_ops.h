@@ -102,7 +102,8 @@ ssd_status ssd_distill_forward(ssd_dtype dtype, const void *logits, int64_t ld, 
                                const int32_t *ids, const float *vals, int32_t k, const float *weight,
                                float temperature, float *loss, float *lse, void *stream);
 /* The gradient from lse as ssd_distill_forward left it; weight[n] is the
- * derivative of the objective with respect to row n's unweighted divergence. */
+ * derivative of the objective with respect to row n's unweighted divergence.
+ * (q is exp(logits / T - lse) here and carries lse's rounding, 2^-24 |lse| of itself.) */
 ssd_status ssd_distill_backward(ssd_dtype dtype, const void *logits, int64_t ld, int32_t n_rows, int32_t vocab,
                                 const int32_t *ids, const float *vals, int32_t k, const float *lse,
                                 const float *weight, float temperature, void *dlogits, int64_t ld_d, void *stream);

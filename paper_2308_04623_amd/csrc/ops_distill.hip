@@ -304,14 +304,16 @@ __device__ __forceinline__ void put_zeros(T* out, const Row<T>& row, int c0, int
   if (edge >= 0) op_st(out, edge, 0.f);
 }
 
-// the row's loss, by the wave that ran teacher()
-__device__ __forceinline__ void put_loss(const DistillArgs& a, int n, const Slots& s, const Mine& m, float lse) {
+// The row's loss, by the wave that ran teacher().  logq(z): log q of a logit, from its
+// difference to the reference (log q = z / T - lse would carry the rounding of two large numbers).
+template <typename Q>
+__device__ __forceinline__ void put_loss(const DistillArgs& a, int n, const Slots& s, const Mine& m, float lse, Q logq) {
   const int lane = threadIdx.x & 63;
   float l = 0.f;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const float p = s.p[lane + 64 * i];
-    if (p != 0.f) l += p * (m.lp[i] - (m.z[i] * a.inv_t - lse));
+    if (p != 0.f) l += p * (m.lp[i] - logq(m.z[i]));
   }
   l = wave_sum(l);
   if (lane == 0) {
@@ -384,7 +386,8 @@ __device__ void sweep(const DistillArgs& a, int n, const Row<T>& body, int edge,
         put_tokens(out, slots, lists, mul, f, q1);
       }
   }
-  if (t < 64) put_loss(a, n, slots, mine, ref * a.inv_t + logf(st.s));
+  const float ls = logf(st.s);
+  if (t < 64) put_loss(a, n, slots, mine, ref * a.inv_t + ls, [&](float z) { return (z - ref) * a.inv_t - ls; });
 }
 
 // One workgroup per row of any length, read twice for the gradient (512 float32 rows of
@@ -458,7 +461,8 @@ __global__ __launch_bounds__(TPB, W) void distill_row_kernel(DistillArgs a) {
       put_zeros<T, TPB>(out, body, 0, body.chunks, edge);
     }
   }
-  if (t < 64) put_loss(a, n, slots, mine, (st.m + __log2f(st.s)) * kLn2);
+  const float ls = __log2f(st.s);
+  if (t < 64) put_loss(a, n, slots, mine, (st.m + ls) * kLn2, [&](float z) { return (fmaf(z, c2, -st.m) - ls) * kLn2; });
 }
 
 // The gradient from a known log-sum-exp: a workgroup per row and C chunks a thread.

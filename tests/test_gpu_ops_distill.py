@@ -328,3 +328,59 @@ def test_more_rows_than_a_launch(env, dtype):
         want = torch.cat([want] * (n // 64 + 1))[:n]
         assert torch.equal(got, want)
     check(torch, ops, dtype, z, ids, vals, w, T=T)
+
+
+def far_rows(torch, dtype, v, k, sizes):
+    """Rows of one value each, then two of ordinary spread around one whose maximum is the
+    teacher's first token."""
+    z, ids, vals, w = make(torch, dtype, len(sizes) + 2, v, k, seed=v)
+    for i, c in enumerate(sizes):
+        z[i] = c
+    ids[-2:, 0] = v // 2
+    z[-2, v // 2] = max(sizes) / 2
+    z[-1] -= max(sizes)
+    z[-1, v // 2] = -max(sizes) / 2
+    return z, ids, vals, w
+
+
+# Against 64 bits with tolerances that do not grow with the logits: an entry z enters by
+# (z - max) / T alone, off by a few eps of itself, so everything but lse, which is rounded as a
+# number of its size, is off by EPS (4 Y + 256) with Y the largest such difference that matters: of the
+# entries whose exponential is not 0 (120 and a little), and of the teacher's tokens for the loss.
+# Exponentials below 2^-126 are 0.
+def far_check(torch, ops, dtype, z, ids, vals, w, T):
+    dev = [x.cuda() for x in (z, ids, vals, w)]
+    T = float(np.float32(T))
+    forward = ops.distill_forward(*dev, temperature=T)
+    step = ops.distill_step(*dev, temperature=T)
+    zz, tv, wn = z.double().numpy(), vals.double().numpy(), w.double().numpy()
+    x = (zz - zz.max(1, keepdims=True)) / T
+    total = np.exp(x).sum(1)
+    lse = zz.max(1) / T + np.log(total)
+    p = np.exp((tv - tv.max(1, keepdims=True)) / T)
+    p /= p.sum(1, keepdims=True)
+    at = ids.long().numpy()
+    logq = np.take_along_axis(x, at, 1) - np.log(total)[:, None]
+    loss = wn * np.where(p > 0, p * (np.log(np.where(p > 0, p, 1)) - logq), 0).sum(1)
+    q = np.exp(x) / total[:, None]
+    grad = q.copy()
+    for i in range(len(at)):
+        np.subtract.at(grad[i], at[i], p[i])
+    grad *= (wn / T)[:, None]
+    spread = np.abs(tv - tv.max(1, keepdims=True)).max(1) / T
+    unit = EPS * (4 * (120 + spread) + 256)
+    unit_loss = EPS * (4 * (np.abs(np.take_along_axis(x, at, 1)).max(1) + spread) + 256)
+    mag = q
+    np.put_along_axis(mag, at, np.take_along_axis(mag, at, 1) + 2, 1)
+    for l, s in (forward, step[:2]):
+        assert (np.abs(l.double().cpu().numpy() - loss) <= 2 * wn * unit_loss).all()
+        assert (np.abs(s.double().cpu().numpy() - lse) <= EPS * (8 * np.abs(lse) + 256)).all()
+    close(dtype, step[2].double().cpu().numpy(), grad, (wn / T)[:, None] * (unit[:, None] * mag + 2.0 ** -125))
+
+
+# below 2^23 everywhere, beyond in rows that no registers hold
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("v,sizes", [(300, (-1e6, 5e6)), (40001, (-5e6, 1e6)), (200003, (-1e6, 1e10, -1e20))])
+def test_the_loss_does_not_carry_the_logits_rounding(env, dtype, v, sizes):
+    torch, ops = env
+    far_check(torch, ops, dtype, *far_rows(torch, dtype, v, 6, sizes), 1.0)
