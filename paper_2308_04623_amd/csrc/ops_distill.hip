@@ -7,8 +7,6 @@
 //   dz_i = w / T (exp(x_i - lse) - sum_{j: id_j = i} p_j).
 // Bound: memory.  The forward pass has to read the row, the step to read and to
 // write it.
-#include <limits.h>
-
 #include "ops_common.h"
 
 namespace ssd {
@@ -213,10 +211,11 @@ struct __align__(16) Lists {
 struct Stat {
   float m, s;
 };
-// References beyond this are not used: 2^(c z - m) by one rounding (fmaf) fails
-// where c z overflows, as for rows of the type's lowest value.  Such a row is
-// found by its reference and done again by sweep().
-constexpr float kFar = 1e30f;
+// References from here on are not used: 2^(c z - m) by one rounding (fmaf) leaves the
+// row's largest entry 2^r with r the rounding of m, below 1/2 here, 2^128 for m around
+// 2^32, and c z itself may overflow.  Such a row is found by its reference and
+// done again by sweep().
+constexpr float kFar = 16777216.f;
 __device__ __forceinline__ float near_(float x) { return fminf(fmaxf(x, -kFar), kFar); }
 
 // Keeps the compiler from holding the chunk's elements unpacked from one use
@@ -546,7 +545,7 @@ ssd_status check_grad(int dtype, const void* logits, int64_t ld, int n, int V, c
 // (4096 float32 rows of 65000: 193 us with 512 threads, 159 swept; of 20000: 54 with 256, 68).
 template <typename T, bool GRAD>
 void launch_rows(const DistillArgs& a, int n, hipStream_t s) {
-  const int chunks = a.inv_t < 1e6f ? a.V / Vec<T>::E : INT_MAX;  // (see kFar)
+  const int chunks = a.V / Vec<T>::E;
 #define ROWS(TPB, C, W) \
   if (chunks <= TPB * C) return distill_row_kernel<T, TPB, C, W, GRAD><<<n, TPB, 0, s>>>(a);
   ROWS(256, 4, 6)

@@ -384,3 +384,29 @@ def far_check(torch, ops, dtype, z, ids, vals, w, T):
 def test_the_loss_does_not_carry_the_logits_rounding(env, dtype, v, sizes):
     torch, ops = env
     far_check(torch, ops, dtype, *far_rows(torch, dtype, v, 6, sizes), 1.0)
+
+
+# both sides of 2^24 (in units of log 2), where a row is done again by sweeps
+SIZES = (-1e6, 1.1e7, 1.2e7, -1.2e7, 5e8, -1e9, 1e10, -1e10, -3e10, 1e20, -1e20, -1e29, 1e38)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("v", [300, 5000, 40001, 70001, 140000, 200003])
+@pytest.mark.parametrize("T", [1.0, 0.5])
+def test_logits_of_any_size(env, dtype, v, T):
+    torch, ops = env
+    far_check(torch, ops, dtype, *far_rows(torch, dtype, v, 6, SIZES), T)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("v", [300, 40001, 200003])
+@pytest.mark.parametrize("T", [1e-5, 2.0 ** -17, 1e-7])
+def test_small_temperatures(env, dtype, v, T):
+    """Masks of -65504 and logits around 5e4."""
+    torch, ops = env
+    z, ids, vals, w = make(torch, dtype, 4, v, 6, seed=3)
+    z[0] = -65504.0
+    z[1, v // 3] = 5e4
+    z[2] += 5e4
+    vals = vals * T  # (the teacher's distribution stays one)
+    far_check(torch, ops, dtype, z, ids, vals, w, T)
