@@ -96,7 +96,7 @@ ssd_status ssd_prefix_attn(const ssd_prefix_attn_desc *a, const void *q, const v
  * row; any alignment of the element's.  dlogits may be logits itself (with the
  * same row stride) and overlaps it in no other way.  ids, vals: [n_rows][k].
  * n_rows >= 0, 1 <= vocab <= 2^24, 1 <= k <= 128, temperature and
- * 1 / temperature positive and finite.
+ * log2(e) / temperature positive and finite.
  * Errors: SSD_E_INVALID_ARG, SSD_E_DEVICE. */
 ssd_status ssd_distill_forward(ssd_dtype dtype, const void *logits, int64_t ld, int32_t n_rows, int32_t vocab,
                                const int32_t *ids, const float *vals, int32_t k, const float *weight,

@@ -515,8 +515,8 @@ ssd_status check(int dtype, const void* logits, int64_t ld, int n, int V, const 
   OP_REQUIRE(n >= 0, SSD_E_INVALID_ARG, "n_rows is negative");
   OP_REQUIRE(V >= 1 && V <= 1 << 24, SSD_E_INVALID_ARG, "vocab outside [1, 2^24]");
   OP_REQUIRE(k >= 1 && k <= kMaxSlots, SSD_E_INVALID_ARG, "k outside [1, 128]");
-  OP_REQUIRE(temperature > 0.f && temperature < INFINITY && 1.f / temperature < INFINITY, SSD_E_INVALID_ARG,
-             "temperature and its reciprocal must be positive and finite");
+  OP_REQUIRE(temperature > 0.f && temperature < INFINITY && 1.f / temperature * kLog2e < INFINITY, SSD_E_INVALID_ARG,
+             "temperature and its reciprocal, times log2 e, must be positive and finite");
   OP_REQUIRE(ld >= V, SSD_E_INVALID_ARG, "the logits' row stride is below vocab");
   OP_REQUIRE(n == 0 || (logits && ids && vals), SSD_E_INVALID_ARG, "null argument");
   OP_REQUIRE((uintptr_t)logits % op_size(dtype) == 0, SSD_E_INVALID_ARG, "logits not aligned to their type");

@@ -146,3 +146,10 @@ def test_the_binding_refuses_host_tensors():
 @pytest.mark.parametrize("t", [1e-39, 1e-45])
 def test_distill_refuses_temperatures_without_a_reciprocal(which, t):
     assert _distill(which, t=t) == ssd.E_INVALID_ARG
+
+
+@pytest.mark.parametrize("which", ["forward", "backward", "step"])
+@pytest.mark.parametrize("t", [3e-39, 4.2e-39])  # 1 / t is finite, its multiples by log2 e are not
+def test_distill_refuses_temperatures_without_a_factor_of_their_exponents(which, t):
+    assert 1 / t < 3.4e38 < 1.4427 / t
+    assert _distill(which, t=t) == ssd.E_INVALID_ARG
