@@ -71,7 +71,8 @@ ssd_status ssd_prefix_attn_workspace(const ssd_prefix_attn_desc *a, size_t *byte
  * bytes; out's rows do not overlap, nor does out share an element with an
  * input.  k_prefix and v_prefix may be NULL when
  * prefix_len is 0, k_own and v_own when own_rows is 0.  Scores and sums are
- * float32; bfloat16 calls round the weights exp(x - max) to bfloat16 for the
+ * float32: q.k and |scale| q.k have to lie below 2^127 in size, and are infinite
+ * beyond.  bfloat16 calls round the weights exp(x - max) to bfloat16 for the
  * product with the values.
  * Errors: SSD_E_INVALID_ARG, SSD_E_CAPACITY (workspace too small),
  * SSD_E_UNSUPPORTED (head_dim, alignment), SSD_E_DEVICE. */

@@ -50,6 +50,10 @@ struct PrefixAttnArgs {
 
 constexpr int kWaves = 4;
 constexpr float kSlack = 8.f;  // how far a score may lie above the reference before the sums are rescaled
+// From references of this size on, scaled scores are rounded before the reference is taken from
+// them: by one rounding (fmaf) the largest score's weight is 2^r with r the rounding of the
+// reference, below 1/2 here, 2^128 for references around 2^32.
+constexpr float kFar = 16777216.f;
 
 // A block of rows in LDS: KB rows of keys, then of values, CH 16-byte chunks each.
 // Chunk c of row r lies at place c ^ swizzle(r), so that the lanes of one read
@@ -373,6 +377,7 @@ struct Wave {
   u32x4 q[MT][KK];
   f32x4 o[MT][DT];
   float m[MT], l[MT];
+  float limit[MT];  // a scaled score above it takes the way of a new reference
   int pos[MT];  // of this lane's queries
 
   __device__ __forceinline__ void load(const PrefixAttnArgs& a, const Queries& qs) {
@@ -388,7 +393,7 @@ struct Wave {
       const T* row = (const T*)a.q + (int64_t)seq * d.q_seq + (int64_t)t * d.q_row + (int64_t)head * d.q_head;
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) q[mt][kk] = *((const u32x4*)row + 4 * kk + g) ^ sign;
-      m[mt] = -INFINITY;
+      m[mt] = limit[mt] = -INFINITY;
       l[mt] = 0.f;
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) o[mt][dt] = (f32x4){0.f, 0.f, 0.f, 0.f};
@@ -424,9 +429,10 @@ struct Wave {
       top[mt] = s[mt][0][0];
 #pragma unroll
       for (int i = 1; i < 4 * KT; ++i) top[mt] = fmaxf(top[mt], s[mt][i / 4][i % 4]);
-      above |= top[mt] * scale2 > m[mt] + kSlack;
+      above |= top[mt] * scale2 > limit[mt];
     }
     if (__builtin_amdgcn_ballot_w64(above)) {  // a new reference: the largest score so far
+      bool beyond = false;
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
         float x = top[mt] == -INFINITY ? m[mt] : fmaxf(m[mt], top[mt] * scale2);
@@ -434,9 +440,25 @@ struct Wave {
         x = fmaxf(x, __shfl_xor(x, 32));
         const float c = x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[mt] - x);
         m[mt] = x;
+        limit[mt] = x + kSlack;
+        beyond |= x != -INFINITY && fabsf(x) >= kFar;
         l[mt] *= c;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[mt][dt] *= c;
+      }
+      if (__builtin_amdgcn_ballot_w64(beyond)) {
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) limit[mt] = -INFINITY;  // (the next block's, too: no test of its own in the loop)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              s[mt][kt][r] *= scale2;
+              asm volatile("" : "+v"(s[mt][kt][r]));  // (rounded here: not to be made one operation with what follows)
+            }
+        scale2 = 1.f;
       }
     }
 #pragma unroll

@@ -429,3 +429,50 @@ def test_a_query_of_nan_that_sees_no_row(env, dtype):
     x, lens = make(torch, dtype, 3, 2, 4, 2, 64, 0, 20, lens=[0, 1, 20])
     x["q"][:2] = float("nan")
     check_with_nan(torch, ops, dtype, x, lens)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("form", list(FORMS))
+@pytest.mark.parametrize("power", [10, 22, 24, 27, 31, 34, 60, 115])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_scores_of_any_size(env, dtype, form, power, sign):
+    """Scores that are exact, whole multiples of 2^power up to 2^(power + 7), and whose
+    largest a few rows share: out is the mean of these rows' values, by the roundings of sums
+    and output alone, and lse the score and the logarithm of their number."""
+    torch, ops = env
+    b, t, h, g, p = FORMS[form]
+    d, r = 64, 20
+    lens = [(20, 1, -1, 0)[i % 4] for i in range(b)]
+    x, lens = make(torch, dtype, b, t, h, g, d, p, r, seed=power, lens=lens)
+    gen = torch.Generator().manual_seed(power)
+    x["q"].zero_()
+    half = power // 2
+    x["q"][..., 3] = sign * 8 * 2.0 ** half  # (1 / sqrt(64) = 1 / 8)
+    for name in ("kp", "ko"):
+        x[name][..., 3] = torch.randint(-100, 101, x[name].shape[:-1], generator=gen).to(x[name].dtype) * 2.0 ** (power - half)
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    out, lse = ops.prefix_attention(*(x[k].cuda() for k in ("q", "kp", "vp", "ko", "vo")), n, return_lse=True)
+    ref, rl, _, vmax = reference(x, lens)
+    tol = vmax * (64 * EPS + (2.0 ** -8 if dtype == "bf16" else 0))
+    assert np.abs(out.double().cpu().numpy() - ref).max() <= tol
+    got = lse.double().cpu().numpy()
+    assert np.array_equal(np.isneginf(got), np.isneginf(rl))
+    live = np.isfinite(rl)
+    assert (np.abs(got[live] - rl[live]) <= 8 * EPS * np.abs(rl[live]) + 64 * EPS).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("form", list(FORMS))
+def test_scores_of_very_different_sizes_in_one_tile(env, dtype, form):
+    """Queries of ordinary size beside ones with scores of 2^40: each as if alone."""
+    torch, ops = env
+    b, t, h, g, p = FORMS[form]
+    x, lens = make(torch, dtype, b, t, h, g, 64, p, 20, seed=9, lens=[(20, 1, 7, 0)[i % 4] for i in range(b)])
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    big = {k: v.clone() for k, v in x.items()}
+    big["q"][1::2] *= 2.0 ** 40
+    out = ops.prefix_attention(*(big[k].cuda() for k in ("q", "kp", "vp", "ko", "vo")), n)
+    assert torch.isfinite(out).all()
+    ref, _, s, vmax = reference(x, lens)
+    got = out.double().cpu().numpy()[::2]
+    assert np.abs(got - ref[::2]).max() <= tolerance(dtype, 64, s, vmax)
