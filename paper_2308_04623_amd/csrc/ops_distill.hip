@@ -109,14 +109,15 @@ struct Slots {
   float p[kMaxSlots];
   float sum[kMaxSlots];  // of the p of all slots that name this one's token, in the first of them; 0 in the others
   float z[kMaxSlots];    // the token's logit
+  float lp[kMaxSlots];   // log p
   int live;              // whether the row counts
 };
 
 // Lane l of the first wave has slots l and l + 64: their tokens (-1: left out),
-// the teacher's logits and the student's, and log p.
+// the teacher's logits and the student's.
 struct Mine {
   int id[2];
-  float x[2], z[2], lp[2];
+  float x[2], z[2];
 };
 
 template <typename T>
@@ -141,7 +142,7 @@ __device__ __forceinline__ void fetch(const DistillArgs& a, int n, const T* row,
 }
 
 // the teacher's probabilities, by the wave that fetched
-__device__ __forceinline__ void teacher(const DistillArgs& a, int n, Mine& mine, Slots& s) {
+__device__ __forceinline__ void teacher(const DistillArgs& a, int n, const Mine& mine, Slots& s) {
   const int lane = threadIdx.x & 63;
   const int(&id)[2] = mine.id;
   const float(&x)[2] = mine.x;
@@ -151,13 +152,12 @@ __device__ __forceinline__ void teacher(const DistillArgs& a, int n, Mine& mine,
   const float e0 = __builtin_amdgcn_exp2f((x[0] - m) * c), e1 = __builtin_amdgcn_exp2f((x[1] - m) * c);
   const float total = wave_sum(e0 + e1), ls = logf(total);
   const float w = a.weight ? a.weight[n] : 1.f;
-  mine.lp[0] = (x[0] - m) * a.inv_t - ls;
-  mine.lp[1] = (x[1] - m) * a.inv_t - ls;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int j = lane + 64 * i;
     s.id[j] = id[i];
     s.z[j] = mine.z[i];
+    s.lp[j] = (x[i] - m) * a.inv_t - ls;
     s.p[j] = id[i] >= 0 ? (i ? e1 : e0) / total : 0.f;
   }
   if (lane == 0) s.live = any && w != 0.f;
@@ -306,13 +306,13 @@ __device__ __forceinline__ void put_zeros(T* out, const Row<T>& row, int c0, int
 // The row's loss, by the wave that ran teacher().  logq(z): log q of a logit, from its
 // difference to the reference (log q = z / T - lse would carry the rounding of two large numbers).
 template <typename Q>
-__device__ __forceinline__ void put_loss(const DistillArgs& a, int n, const Slots& s, const Mine& m, float lse, Q logq) {
+__device__ __forceinline__ void put_loss(const DistillArgs& a, int n, const Slots& s, float lse, Q logq) {
   const int lane = threadIdx.x & 63;
   float l = 0.f;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const float p = s.p[lane + 64 * i];
-    if (p != 0.f) l += p * (m.lp[i] - logq(m.z[i]));
+    if (p != 0.f) l += p * (s.lp[lane + 64 * i] - logq(s.z[lane + 64 * i]));
   }
   l = wave_sum(l);
   if (lane == 0) {
@@ -329,7 +329,7 @@ __device__ __forceinline__ float ref_of(float m) { return m == -INFINITY ? 0.f :
 // The first wave has run teacher().
 template <typename T, int TPB, bool GRAD>
 __device__ void sweep(const DistillArgs& a, int n, const Row<T>& body, int edge, float ze, const Slots& slots,
-                      Lists<TPB>& lists, Stat* red, const Mine& mine) {
+                      Lists<TPB>& lists, Stat* red) {
   constexpr int E = Vec<T>::E, U = 4, SEG = 64;
   const int t = threadIdx.x, chunks = body.chunks;
   const T* row = (const T*)a.logits + (size_t)n * a.ld;
@@ -386,7 +386,7 @@ __device__ void sweep(const DistillArgs& a, int n, const Row<T>& body, int edge,
       }
   }
   const float ls = logf(st.s);
-  if (t < 64) put_loss(a, n, slots, mine, ref * a.inv_t + ls, [&](float z) { return (z - ref) * a.inv_t - ls; });
+  if (t < 64) put_loss(a, n, slots, ref * a.inv_t + ls, [&](float z) { return (z - ref) * a.inv_t - ls; });
 }
 
 // One workgroup per row of any length, read twice for the gradient (512 float32 rows of
@@ -407,7 +407,7 @@ __global__ __launch_bounds__(1024) void distill_sweep_kernel(DistillArgs a) {
     fetch(a, n, row, mine);
     teacher(a, n, mine, slots);
   }
-  sweep<T, TPB, GRAD>(a, n, body, edge, ze, slots, lists, red, mine);
+  sweep<T, TPB, GRAD>(a, n, body, edge, ze, slots, lists, red);
 }
 
 // One workgroup per row, which its registers hold: C chunks a thread.
@@ -439,7 +439,7 @@ __global__ __launch_bounds__(TPB, W) void distill_row_kernel(DistillArgs a) {
   st.s = __builtin_amdgcn_exp2f(fmaf(ze, c2, -st.m));
   add_all<T, 0>(st, r, c2);
   st = block_stat<TPB>(st, 1.f, red);
-  if (!(fabsf(st.m) < kFar)) return sweep<T, TPB, GRAD>(a, n, body, edge, ze, slots, lists, red, mine);
+  if (!(fabsf(st.m) < kFar)) return sweep<T, TPB, GRAD>(a, n, body, edge, ze, slots, lists, red);
   if (GRAD) {
     T* out = (T*)a.grad + (size_t)n * a.ld_d;
     const float f = (a.weight ? a.weight[n] : 1.f) * a.inv_t, mul = f / st.s;
@@ -461,7 +461,7 @@ __global__ __launch_bounds__(TPB, W) void distill_row_kernel(DistillArgs a) {
     }
   }
   const float ls = __log2f(st.s);
-  if (t < 64) put_loss(a, n, slots, mine, (st.m + ls) * kLn2, [&](float z) { return (fmaf(z, c2, -st.m) - ls) * kLn2; });
+  if (t < 64) put_loss(a, n, slots, (st.m + ls) * kLn2, [&](float z) { return (fmaf(z, c2, -st.m) - ls) * kLn2; });
 }
 
 // The gradient from a known log-sum-exp: a workgroup per row and C chunks a thread.
