@@ -66,16 +66,16 @@ ssd_status ssd_prefix_attn_workspace(const ssd_prefix_attn_desc *a, size_t *byte
  * lse, if not NULL: float32 [n_seq][n_query][n_head], the log of the sum of
  * exponentials of the seen scores (-infinity where there are none).
  *   dtype SSD_F32 or SSD_BF16; head_dim 32, 64 or 128; n_head a multiple of
- * n_kv_head; 1 <= n_seq <= 4096, 1 <= n_query <= 64, prefix_len, own_rows >= 0
- * and below 2^30.  Pointers are 16-byte aligned and strides multiples of 16
- * bytes; out's rows do not overlap, nor does out share an element with an
- * input.  k_prefix and v_prefix may be NULL when
- * prefix_len is 0, k_own and v_own when own_rows is 0.  Scores and sums are
- * float32: q.k and |scale| q.k have to lie below 2^127 in size, and are infinite
+ * n_kv_head and at most 1024; 1 <= n_seq <= 4096, 1 <= n_query <= 64, prefix_len,
+ * own_rows >= 0 and below 2^30.  Pointers are 16-byte aligned and strides multiples
+ * of 16 bytes, not negative; out's rows do not overlap, nor does out share an
+ * element with an input.  k_prefix and v_prefix may be NULL when prefix_len is 0,
+ * k_own and v_own when own_rows is 0.  Scores and sums are float32: q.k and |scale| q.k have to lie below 2^127 in size, and are infinite
  * beyond.  bfloat16 calls round the weights exp(x - max) to bfloat16 for the
  * product with the values.
- * Errors: SSD_E_INVALID_ARG, SSD_E_CAPACITY (workspace too small),
- * SSD_E_UNSUPPORTED (head_dim, alignment), SSD_E_DEVICE. */
+ * Errors: SSD_E_INVALID_ARG, SSD_E_CAPACITY (workspace too small, or queries and
+ * chunks of rows for 2^24 workgroups), SSD_E_UNSUPPORTED (head_dim, alignment),
+ * SSD_E_DEVICE. */
 ssd_status ssd_prefix_attn(const ssd_prefix_attn_desc *a, const void *q, const void *k_prefix, const void *v_prefix,
                            const void *k_own, const void *v_own, const int32_t *own_len, void *out, float *lse,
                            void *workspace, size_t workspace_bytes, void *stream);

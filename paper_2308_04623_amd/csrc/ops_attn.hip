@@ -941,7 +941,9 @@ __global__ __launch_bounds__(256) void merge_kernel(PrefixAttnArgs a, int first,
 }
 
 constexpr int kMaxRows = 1 << 30;
-constexpr int kMergeQueries = 1 << 25;  // of a launch: a grid holds fewer than 2^32 threads
+// a grid holds fewer than 2^32 threads
+constexpr int kMaxBlocks = (1 << 24) - 1;  // of 64 kWaves threads
+constexpr int kMergeQueries = 1 << 25;     // of a launch
 
 ssd_status check(const ssd_prefix_attn_desc* a) {
   OP_REQUIRE(a, SSD_E_INVALID_ARG, "null argument");
@@ -1115,7 +1117,7 @@ extern "C" ssd_status ssd_prefix_attn_workspace(const ssd_prefix_attn_desc* a, s
   ssd_status st = check(a);
   if (st != SSD_OK) return st;
   const Plan p = plan(a);
-  OP_REQUIRE(p.blocks <= 0x7fffffff, SSD_E_CAPACITY, "too many workgroups");
+  OP_REQUIRE(p.blocks <= kMaxBlocks, SSD_E_CAPACITY, "more workgroups than a grid holds");
   *bytes = p.bytes;
   return SSD_OK;
 }

@@ -153,3 +153,13 @@ def test_distill_refuses_temperatures_without_a_reciprocal(which, t):
 def test_distill_refuses_temperatures_without_a_factor_of_their_exponents(which, t):
     assert 1 / t < 3.4e38 < 1.4427 / t
     assert _distill(which, t=t) == ssd.E_INVALID_ARG
+
+
+def test_prefix_attn_refuses_more_workgroups_than_a_grid_holds():
+    """A grid holds fewer than 2^32 threads: 2^24 - 1 workgroups of 256."""
+    need = C.c_size_t(0)
+    large = dict(n_seq=4096, n_query=64, n_head=1024, n_kv_head=1, prefix_len=100000, q_seq=64 * 65536, q_row=65536,
+                 out_seq=64 * 65536, out_row=65536)
+    assert ops._ops().ssd_prefix_attn_workspace(C.byref(_desc(**large)), C.byref(need)) == ssd.E_CAPACITY
+    assert _attn(_desc(**large), size=1 << 60) == ssd.E_CAPACITY
+    assert ops._ops().ssd_prefix_attn_workspace(C.byref(_desc(**{**large, "n_head": 256})), C.byref(need)) == ssd.OK
