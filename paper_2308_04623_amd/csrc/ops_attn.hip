@@ -974,6 +974,27 @@ ssd_status check_strides(const ssd_prefix_attn_desc* a) {
   return SSD_OK;
 }
 
+// whether out shares an element with an input
+bool out_overlaps(const ssd_prefix_attn_desc& a, const void* q, const void* kp, const void* vp, const void* ko,
+                  const void* vo, const int32_t* own_len, const void* out) {
+  const int64_t es = op_size(a.dtype);
+  const OpView::Dim row = {a.head_dim, es};
+  auto queries = [&](const void* p, int64_t seq, int64_t pos, int64_t head) {
+    return OpView{p, {{a.n_seq, seq * es}, {a.n_query, pos * es}, {a.n_head, head * es}, row}};
+  };
+  auto prefix = [&](const void* p) {
+    return OpView{p, {{1, 0}, {a.n_kv_head, a.prefix_head * es}, {a.prefix_len, a.prefix_row * es}, row}};
+  };
+  auto own = [&](const void* p) {
+    return OpView{p, {{a.n_seq, a.own_seq * es}, {a.n_kv_head, a.own_head * es}, {a.own_rows, a.own_row * es}, row}};
+  };
+  const OpView o = queries(out, a.out_seq, a.out_row, a.out_head);
+  for (const OpView& in : {queries(q, a.q_seq, a.q_row, a.q_head), prefix(kp), prefix(vp), own(ko), own(vo),
+                           OpView{own_len, {{1, 0}, {1, 0}, {1, 0}, {a.n_seq, 4}}}})
+    if (!op_apart(o, in)) return true;
+  return false;
+}
+
 // How a call is cut up.
 //   Alone (short_attn_kernel): a sequence's queries take the prefix and their own rows
 // in one workgroup, where the prefix is short for the number of workgroups that
@@ -1133,10 +1154,11 @@ extern "C" ssd_status ssd_prefix_attn(const ssd_prefix_attn_desc* a, const void*
   OP_REQUIRE(q && own_len && out && workspace, SSD_E_INVALID_ARG, "null argument");
   OP_REQUIRE(a->prefix_len == 0 || (k_prefix && v_prefix), SSD_E_INVALID_ARG, "null prefix");
   OP_REQUIRE(a->own_rows == 0 || (k_own && v_own), SSD_E_INVALID_ARG, "null own rows");
-  OP_REQUIRE(out != q, SSD_E_INVALID_ARG, "out is the queries");
   const void* pointers[] = {q, k_prefix, v_prefix, k_own, v_own, out};
   for (const void* x : pointers)
     OP_REQUIRE((uintptr_t)x % 16 == 0, SSD_E_UNSUPPORTED, "a pointer is not 16-byte aligned");
+  OP_REQUIRE(!out_overlaps(*a, q, k_prefix, v_prefix, k_own, v_own, own_len, out), SSD_E_INVALID_ARG,
+             "out overlaps an input");
   OP_REQUIRE(workspace_bytes >= need && (uintptr_t)workspace % 16 == 0, SSD_E_CAPACITY,
              "workspace below ssd_prefix_attn_workspace's bytes or not 16-byte aligned");
   const Plan p = plan(a);

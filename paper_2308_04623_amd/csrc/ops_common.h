@@ -30,6 +30,40 @@ inline int op_size(int t) { return t == SSD_F32 ? 4 : 2; }
 inline bool op_overlap(const void* a, size_t na, const void* b, size_t nb) {
   return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
 }
+// Elements in memory, those of up to four dimensions.
+struct OpView {
+  const void* p;
+  struct Dim {
+    int64_t n, step;  // in bytes, not negative
+  } dims[4];          // (the last: the elements that lie side by side)
+};
+// Whether two views are sure to share no byte: their bytes lie apart, or, modulo a step that divides all
+// larger ones, what either has of smaller steps does (parts of the rows, heads or
+// tokens of one buffer).  Others count as overlapping.
+inline bool op_apart(const OpView& a, const OpView& b) {
+  // bytes from the first to past the last, of dimensions whose steps are below `most`
+  auto extent = [](const OpView& v, int64_t most) {
+    int64_t e = 0;
+    for (const auto& d : v.dims) {
+      if (d.n <= 0) return (int64_t)0;
+      if (d.step < most) e += (d.n - 1) * d.step;
+    }
+    return e + v.dims[3].step;
+  };
+  const int64_t ea = extent(a, INT64_MAX), eb = extent(b, INT64_MAX);
+  if (ea == 0 || eb == 0 || !op_overlap(a.p, (size_t)ea, b.p, (size_t)eb)) return true;
+  auto proves = [&](int64_t step) {
+    for (const OpView* v : {&a, &b})
+      for (const auto& d : v->dims)
+        if (d.n > 1 && d.step >= step && d.step % step != 0) return false;
+    const int64_t from = (((int64_t)((intptr_t)b.p - (intptr_t)a.p)) % step + step) % step;
+    return extent(a, step) <= from && from + extent(b, step) <= step;
+  };
+  for (const OpView* v : {&a, &b})
+    for (const auto& d : v->dims)
+      if (d.n > 1 && d.step > 0 && proves(d.step)) return true;
+  return false;
+}
 // bytes from a matrix's first element to past its last
 inline size_t op_span(int64_t rows, int64_t ld, int64_t cols, int size) {
   return rows > 0 ? ((size_t)(rows - 1) * ld + cols) * size : 0;

@@ -476,3 +476,33 @@ def test_scores_of_very_different_sizes_in_one_tile(env, dtype, form):
     ref, _, s, vmax = reference(x, lens)
     got = out.double().cpu().numpy()[::2]
     assert np.abs(got - ref[::2]).max() <= tolerance(dtype, 64, s, vmax)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("where", ["queries", "cache", "own rows"])
+def test_an_out_between_its_inputs_elements(env, dtype, where):
+    """Beside the queries in one projection's rows, in a cache's rows behind the prefix, in
+    the heads of own rows that are not read: no element is shared, none but out's is written."""
+    torch, ops = env
+    b, t, h, g, d, p, r = 5, 3, 4, 4, 64, 300, 21
+    x, lens = make(torch, dtype, b, t, h, g, d, p, r)
+    want = check(torch, ops, dtype, x, lens)
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    a = {k: v.cuda() for k, v in x.items()}
+    zeros = lambda *s: torch.zeros(s, dtype=x["q"].dtype, device="cuda")  # noqa: E731
+    if where == "queries":
+        room = zeros(b, t, 2, h, d)
+        a["q"], out = room[:, :, 0].copy_(a["q"]), room[:, :, 1]
+    elif where == "cache":
+        room = zeros(g, p + b * t, d)
+        a["kp"], out = room[:, :p].copy_(a["kp"]), room[:, p:].unflatten(1, (b, t)).permute(1, 2, 0, 3)
+        a["vp"] = zeros(g, p + b * t, d)[:, :p].copy_(a["vp"])
+    else:
+        room = zeros(b, 2, g, r, d)
+        a["ko"], out = room[:, 0].copy_(a["ko"]), room[:, 1, :, :t].transpose(1, 2)
+        a["vo"] = zeros(b, 2, g, r, d)[:, 0].copy_(a["vo"])
+    before = room.clone()
+    ops.prefix_attention(a["q"], a["kp"], a["vp"], a["ko"], a["vo"], n, out=out)
+    assert torch.equal(out, want)
+    out.zero_()
+    assert torch.equal(room, before)

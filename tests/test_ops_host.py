@@ -163,3 +163,20 @@ def test_prefix_attn_refuses_more_workgroups_than_a_grid_holds():
     assert ops._ops().ssd_prefix_attn_workspace(C.byref(_desc(**large)), C.byref(need)) == ssd.E_CAPACITY
     assert _attn(_desc(**large), size=1 << 60) == ssd.E_CAPACITY
     assert ops._ops().ssd_prefix_attn_workspace(C.byref(_desc(**{**large, "n_head": 256})), C.byref(need)) == ssd.OK
+
+
+# (q: 3 x 512 elements a sequence, 6 KB in all; the prefix 51,200 bytes, own rows 16,384)
+@pytest.mark.parametrize("kw", [
+    dict(out=BUF + 16), dict(out=BUF - 16), dict(out=BUF + 6128), dict(out=8 * BUF, kp=8 * BUF - 51184),
+    dict(kp=8 * BUF + 6128), dict(vp=8 * BUF + 16), dict(ko=8 * BUF - 16368), dict(vo=8 * BUF + 4096),
+    dict(lens=8 * BUF), dict(lens=8 * BUF + 6140)])
+def test_prefix_attn_refuses_an_out_that_shares_elements_with_an_input(kw):
+    assert _attn(_desc(), **{"size": 1 << 40, **kw}) == ssd.E_INVALID_ARG
+    assert b"overlaps" in ops._ops().ssd_last_error()
+
+
+@pytest.mark.parametrize("at", [0, 16, 1008, 1040, 2048, 4096 + 1008])
+def test_prefix_attn_refuses_an_out_between_the_queries_rows_that_reaches_into_them(at):
+    d = _desc(q_row=1024, q_seq=3072, out_row=1024, out_seq=3072)
+    assert _attn(d, out=BUF + at, kp=8 * BUF, vp=8 * BUF, ko=8 * BUF, vo=8 * BUF, lens=8 * BUF,
+                 size=1 << 40) == ssd.E_INVALID_ARG
