@@ -15,6 +15,7 @@
 // wave copies its blocks' keys and values into LDS of its own, one block ahead.
 #include <algorithm>
 #include <atomic>
+#include <cstdlib>
 
 #include "ops_common.h"
 
@@ -960,6 +961,36 @@ ssd_status check(const ssd_prefix_attn_desc* a) {
   return SSD_OK;
 }
 
+// whether rows of out share an element
+bool out_rows_overlap(const ssd_prefix_attn_desc& a) {
+  struct Dim {
+    int64_t n, step;
+  } d[3] = {{a.n_seq, a.out_seq}, {a.n_query, a.out_row}, {a.n_head, a.out_head}};
+  for (Dim& x : d) {
+    if (x.n == 1) x.step = a.head_dim;
+    if (x.step < a.head_dim) return true;
+  }
+  std::sort(d, d + 3, [](const Dim& x, const Dim& y) { return x.step < y.step; });
+  // steps that pass by all that the smaller ones reach
+  int64_t reach = a.head_dim;
+  bool nested = true;
+  for (const Dim& x : d) {
+    nested &= x.n == 1 || x.step >= reach;
+    reach += (x.n - 1) * x.step;
+  }
+  if (nested) return false;
+  // else every difference of two rows, that of the longest dimension the nearest to the others'
+  std::sort(d, d + 3, [](const Dim& x, const Dim& y) { return x.n < y.n; });
+  for (int64_t i = 0; i < d[0].n; ++i)
+    for (int64_t j = i ? 1 - d[1].n : 0; j < d[1].n; ++j) {
+      const int64_t by = i * d[0].step + j * d[1].step;
+      const int64_t near = -by / d[2].step;
+      for (int64_t k = std::max(near - 1, 1 - d[2].n); k <= std::min(near + 1, d[2].n - 1); ++k)
+        if ((i || j || k) && std::abs(by + k * d[2].step) < a.head_dim) return true;
+    }
+  return false;
+}
+
 ssd_status check_strides(const ssd_prefix_attn_desc* a) {
   const int64_t s[] = {a->q_seq, a->q_row, a->q_head, a->prefix_head, a->prefix_row, a->own_seq, a->own_head,
                        a->own_row, a->out_seq, a->out_row, a->out_head};
@@ -968,9 +999,7 @@ ssd_status check_strides(const ssd_prefix_attn_desc* a) {
     OP_REQUIRE(x >= 0, SSD_E_INVALID_ARG, "a stride is negative");
     OP_REQUIRE(x % unit == 0, SSD_E_UNSUPPORTED, "a stride is not a multiple of 16 bytes");
   }
-  OP_REQUIRE((a->n_seq == 1 || a->out_seq >= a->head_dim) && (a->n_query == 1 || a->out_row >= a->head_dim) &&
-                 (a->n_head == 1 || a->out_head >= a->head_dim),
-             SSD_E_INVALID_ARG, "out's rows overlap");
+  OP_REQUIRE(!out_rows_overlap(*a), SSD_E_INVALID_ARG, "out's rows overlap");
   return SSD_OK;
 }
 

@@ -506,3 +506,18 @@ def test_an_out_between_its_inputs_elements(env, dtype, where):
     assert torch.equal(out, want)
     out.zero_()
     assert torch.equal(room, before)
+
+
+@pytest.mark.parametrize("heads,rows,seqs", [(192, 128, 512), (64, 128, 384), (384, 64, 192), (64, 136, 1000)])
+def test_an_out_of_any_order(env, heads, rows, seqs):
+    """2 heads, 3 queries, 2 sequences of 64 elements: one with strides that do not nest."""
+    torch, ops = env
+    x, lens = make(torch, "bf16", 2, 3, 2, 2, 64, 100, 9)
+    want = check(torch, ops, "bf16", x, lens)
+    room = torch.full((8192,), 7.0, dtype=torch.bfloat16, device="cuda")
+    out = room.as_strided(want.shape, (seqs, rows, heads, 1))
+    args = [x[k].cuda() for k in ("q", "kp", "vp", "ko", "vo")] + [torch.tensor(lens, dtype=torch.int32, device="cuda")]
+    ops.prefix_attention(*args, out=out)
+    assert torch.equal(out, want)
+    out.fill_(7.0)
+    assert (room == 7).all()

@@ -180,3 +180,14 @@ def test_prefix_attn_refuses_an_out_between_the_queries_rows_that_reaches_into_t
     d = _desc(q_row=1024, q_seq=3072, out_row=1024, out_seq=3072)
     assert _attn(d, out=BUF + at, kp=8 * BUF, vp=8 * BUF, ko=8 * BUF, vo=8 * BUF, lens=8 * BUF,
                  size=1 << 40) == ssd.E_INVALID_ARG
+
+
+# 2 sequences, 3 queries, 8 heads of 64
+@pytest.mark.parametrize("kw", [
+    dict(out_row=64), dict(out_row=128), dict(out_row=448), dict(out_head=1536, out_row=1536, out_seq=64),
+    dict(out_seq=512), dict(out_seq=1024), dict(out_seq=504), dict(out_head=512, out_row=64, out_seq=128),
+    dict(out_head=320, out_row=1280, out_seq=4096), dict(out_head=192, out_row=576, out_seq=4096),
+    dict(out_head=128, out_row=2048, out_seq=72)])
+def test_prefix_attn_refuses_an_out_whose_rows_overlap(kw):
+    assert _attn(_desc(**kw), size=1 << 40) == ssd.E_INVALID_ARG
+    assert b"rows overlap" in ops._ops().ssd_last_error()
