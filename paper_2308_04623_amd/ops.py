@@ -14,6 +14,7 @@ from __future__ import annotations
 import ctypes as C
 import functools
 import math
+import operator
 from typing import Optional
 
 import torch
@@ -196,6 +197,8 @@ def prefix_attention(q, k_prefix, v_prefix, k_own, v_own, own_len, scale: Option
     bfloat16, any strides that are multiples of 16 bytes with D contiguous (K and
     V alike).  scale defaults to 1 / sqrt(D).  Returns out [B][T][H][D], or (out,
     lse float32 [B][T][H])."""
+    if scale is not None and type(scale) is not float:
+        scale = float(scale)  # (by its value: what is remembered of a call must not go by a tensor's identity)
     a, need = _attn_plan(q, k_prefix, v_prefix, k_own, v_own, own_len, scale, out)
     dev = q.get_device()
     where = _elsewhere(dev, stream)
@@ -356,6 +359,7 @@ def embed_grad(tokens, grad, vocab: int, scale: float = 1.0, dtype=None, out=Non
     if where is not None:
         with where:
             return embed_grad(tokens, grad, vocab, scale, dtype, out, accumulate)
+    vocab = operator.index(vocab)
     need = _embed_grad_bytes(n, vocab, d)
     out = _rows_out(what, grad, (vocab, d), dtype or (None if out is not None else grad.dtype), out)
     work = torch.empty(need, dtype=torch.uint8, device=grad.device)

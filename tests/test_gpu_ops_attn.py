@@ -521,3 +521,13 @@ def test_an_out_of_any_order(env, heads, rows, seqs):
     assert torch.equal(out, want)
     out.fill_(7.0)
     assert (room == 7).all()
+
+
+def test_a_scale_that_changes_in_place(env):
+    torch, ops = env
+    x, lens = make(torch, "f32", 3, 1, 2, 2, 64, 40, 8, lens=[8, 3, 0])
+    scale = torch.tensor(0.1)
+    args = [x[k].cuda() for k in ("q", "kp", "vp", "ko", "vo")] + [torch.tensor(lens, dtype=torch.int32, device="cuda")]
+    for _ in range(2):
+        assert torch.equal(ops.prefix_attention(*args, scale=scale), ops.prefix_attention(*args, scale=float(scale)))
+        scale.mul_(3)

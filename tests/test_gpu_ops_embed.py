@@ -350,3 +350,12 @@ def test_rows_cleared_beside_the_sort(env, td, n, v, d, pad):
     assert bool(((out.double() - ref).abs() <= tol).all())
     assert pad == 0 or bool(room[:, d:].isnan().all())
     assert torch.equal(ops.embed_grad(tokens, grad, v, scale=0.5, dtype=dt(torch, td)), out)
+
+
+def test_a_vocabulary_that_changes_in_place(env):
+    torch, ops = env
+    vocab, tokens, grad = torch.tensor(40), torch.arange(40, dtype=torch.int32, device="cuda"), torch.ones(40, 8, device="cuda")
+    for _ in range(3):
+        got = ops.embed_grad(tokens, grad, vocab)
+        assert got.shape == (int(vocab), 8) and float(got.sum()) == 320
+        vocab.mul_(100)
