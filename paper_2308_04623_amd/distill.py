@@ -44,8 +44,10 @@ class Rollout:
         """float32 logits [n_seq][vocab] after each sequence's token number
         `step` (int32 [n_seq]), whose keys and values join the sequence's."""
         cfg, w, b = self.cfg, self.model.tensors, self.n_seq
-        if prefix_len + step >= cfg.n_pos or step >= self.max_new:
-            raise ValueError(f"position {prefix_len + step}, token {step}: past the model's or the rollout's end")
+        if prefix_len + step >= cfg.n_pos or not 0 <= step < self.max_new:
+            raise ValueError(f"position {prefix_len + step}, token {step}: outside the model's or the rollout's rows")
+        if not 0 <= prefix_len <= self.session.max_ctx:
+            raise ValueError(f"a prefix of {prefix_len} rows in a cache of {self.session.max_ctx}")
         own_len = torch.full((b,), step + 1, dtype=torch.int32, device=self.model.device)
         x = ops.embed(tokens, w["wte"], dtype=torch.float32) + w["wpe"][prefix_len + step].float()
         norm = lambda g, bias: F.layer_norm(x, (cfg.d_model,), g.float(), bias.float(), cfg.ln_eps)  # noqa: E731

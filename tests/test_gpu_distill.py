@@ -103,3 +103,13 @@ def test_successors_feed_the_staged_loop(env):
     for p in parents[1:]:
         depth.append(depth[p] + 1)
     assert ssd.validate_tree(tokens, parents, 512) == max(depth)  # (raises on a tree that is none)
+
+
+@pytest.mark.parametrize("prefix,step", [(129, 0), (200, 3), (-1, 0), (20, -1), (20, 12)])
+def test_a_rollout_refuses_places_outside_its_caches(env, prefix, step):
+    """The session's cache has 128 rows, the rollout's 12, the model 256 positions."""
+    torch, distill, *_ = env
+    session, root = oracle_at(env, "f32", 20)
+    rollout = distill.Rollout(session, 2, 12)
+    with pytest.raises(ValueError):
+        rollout.logits(prefix, torch.zeros(2, dtype=torch.int32, device="cuda"), step)
