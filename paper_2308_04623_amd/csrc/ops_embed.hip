@@ -488,7 +488,8 @@ __global__ __launch_bounds__(1024) void embed_grad_kernel(GradArgs a) {
       opened = v;
       if (col) store4(a.head + (size_t)g * a.d, c, a.d, acc);
     } else if (col) {
-      store4<true>(table + (size_t)v * a.ld_table, c, a.d, a.scale * acc);
+      // (a token that does not occur: 0 whatever the scale)
+      store4<true>(table + (size_t)v * a.ld_table, c, a.d, terms ? a.scale * acc : acc);
     }
     cont = false;
     terms = 0;
@@ -686,7 +687,7 @@ __global__ __launch_bounds__(256) void embed_grad_few_kernel(GradArgs a, const i
     }
   }
   T* row = (T*)a.dtable + (size_t)v * a.ld_table;
-  sum *= a.scale;
+  if (any) sum *= a.scale;  // (else 0 whatever the scale)
   if (ACC) sum += quad(row + at);
   if (at == c) {
     store4<!ACC>(row, c, c + 4, sum);

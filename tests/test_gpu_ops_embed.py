@@ -359,3 +359,17 @@ def test_a_vocabulary_that_changes_in_place(env):
         got = ops.embed_grad(tokens, grad, vocab)
         assert got.shape == (int(vocab), 8) and float(got.sum()) == 320
         vocab.mul_(100)
+
+
+# (a table with a wave per row, a sorted one, one whose rows the sort's launches clear)
+@pytest.mark.parametrize("td", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [float("inf"), float("nan")])
+@pytest.mark.parametrize("n,v,d", [(40, 300, 64), (700, 3000, 64), (500, 40000, 512)])
+def test_a_scale_that_is_no_number_leaves_absent_tokens_at_zero(env, td, scale, n, v, d):
+    torch, ops = env
+    gen = torch.Generator().manual_seed(n)
+    tokens, grad = draw_tokens(gen, torch, n, v, "even"), torch.randn(n, d, generator=gen) + 5.0
+    got = ops.embed_grad(tokens.cuda(), grad.cuda(), v, scale=scale, dtype=dt(torch, td))
+    there = torch.zeros(v, dtype=torch.bool).index_fill_(0, tokens.long(), True).cuda()
+    assert not got[~there].any()
+    assert not torch.isfinite(got[there]).any()
