@@ -531,3 +531,31 @@ def test_a_scale_that_changes_in_place(env):
     for _ in range(2):
         assert torch.equal(ops.prefix_attention(*args, scale=scale), ops.prefix_attention(*args, scale=float(scale)))
         scale.mul_(3)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("form", list(FORMS))
+@pytest.mark.parametrize("kind", ["nan-queries", "large-queries", "nan-rows", "off", "other-lengths"])
+def test_other_sequences_of_the_batch(env, dtype, form, kind):
+    """Every second sequence is replaced: the others' results stay right (not bitwise, the
+    columns of a tile take new references together)."""
+    torch, ops = env
+    b, t, h, g, p = FORMS[form]
+    x, lens = make(torch, dtype, b, t, h, g, 64, p, 20, seed=4, lens=[(20, 13, 7, 1)[i % 4] for i in range(b)])
+    ref, rl, big, vmax = reference(x, lens)
+    if kind == "nan-queries":
+        x["q"][1::2] = float("nan")
+    elif kind == "large-queries":
+        x["q"][1::2] *= 2.0 ** 33
+    elif kind == "nan-rows":
+        x["ko"][1::2] = x["vo"][1::2] = float("nan")
+    else:
+        lens = [n if i % 2 == 0 else -1 if kind == "off" else 20 - n for i, n in enumerate(lens)]
+    n = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    out, lse = ops.prefix_attention(*(x[k].cuda() for k in ("q", "kp", "vp", "ko", "vo")), n, return_lse=True)
+    assert np.abs(out[::2].double().cpu().numpy() - ref[::2]).max() <= tolerance(dtype, 64, big, vmax)
+    assert np.abs(lse[::2].double().cpu().numpy() - rl[::2]).max() <= 68 * EPS * big + 64 * EPS * (1 + np.abs(rl).max())
+    if kind == "off":
+        assert not out[1::2].any() and torch.isneginf(lse[1::2]).all()
+    if kind == "nan-queries":
+        assert torch.isnan(out[1::2]).all() and torch.isnan(lse[1::2]).all()
