@@ -64,9 +64,8 @@ inline bool op_apart(const OpView& a, const OpView& b) {
       if (d.n > 1 && d.step > 0 && proves(d.step)) return true;
   return false;
 }
-// bytes from a matrix's first element to past its last
-inline size_t op_span(int64_t rows, int64_t ld, int64_t cols, int size) {
-  return rows > 0 ? ((size_t)(rows - 1) * ld + cols) * size : 0;
+inline OpView op_matrix(const void* p, int64_t rows, int64_t ld, int64_t cols, int size) {
+  return {p, {{1, 0}, {1, 0}, {rows, ld * size}, {cols, size}}};
 }
 
 struct bf16_t {

@@ -527,8 +527,8 @@ ssd_status check_grad(int dtype, const void* logits, int64_t ld, int n, int V, c
   OP_REQUIRE(ld_d >= V, SSD_E_INVALID_ARG, "dlogits' row stride is below vocab");
   OP_REQUIRE(n == 0 || grad, SSD_E_INVALID_ARG, "null argument");
   OP_REQUIRE((uintptr_t)grad % op_size(dtype) == 0, SSD_E_INVALID_ARG, "dlogits not aligned to their type");
-  OP_REQUIRE((grad == logits && ld == ld_d) || !op_overlap(logits, op_span(n, ld, V, op_size(dtype)), grad,
-                                                           op_span(n, ld_d, V, op_size(dtype))),
+  OP_REQUIRE((grad == logits && ld == ld_d) || op_apart(op_matrix(logits, n, ld, V, op_size(dtype)),
+                                                        op_matrix(grad, n, ld_d, V, op_size(dtype))),
              SSD_E_INVALID_ARG, "dlogits overlaps the logits without being them");
   return SSD_OK;
 }

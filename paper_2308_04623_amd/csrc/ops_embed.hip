@@ -832,8 +832,8 @@ extern "C" ssd_status ssd_embed(ssd_dtype table_dtype, ssd_dtype out_dtype, cons
   OP_REQUIRE(tokens && table && out, SSD_E_INVALID_ARG, "null argument");
   OP_REQUIRE((uintptr_t)table % op_size(table_dtype) == 0 && (uintptr_t)out % op_size(out_dtype) == 0,
              SSD_E_INVALID_ARG, "a pointer is not aligned to its type");
-  OP_REQUIRE(!op_overlap(table, op_span(vocab, ld_table, d, op_size(table_dtype)), out,
-                         op_span(n, ld_out, d, op_size(out_dtype))),
+  OP_REQUIRE(op_apart(op_matrix(table, vocab, ld_table, d, op_size(table_dtype)),
+                      op_matrix(out, n, ld_out, d, op_size(out_dtype))),
              SSD_E_INVALID_ARG, "out overlaps the table");
   if (table_dtype == SSD_F32)
     launch_embed_rows<float>(out_dtype, tokens, n, table, ld_table, vocab, d, scale, out, ld_out, (hipStream_t)stream);
@@ -866,8 +866,8 @@ extern "C" ssd_status ssd_embed_grad(ssd_dtype grad_dtype, ssd_dtype table_dtype
              SSD_E_INVALID_ARG, "a pointer is not aligned to its type");
   OP_REQUIRE(workspace_bytes >= need && (uintptr_t)workspace % 16 == 0, SSD_E_CAPACITY,
              "workspace below ssd_embed_grad_workspace's bytes or not 16-byte aligned");
-  OP_REQUIRE(!op_overlap(grad, op_span(n, ld_grad, d, op_size(grad_dtype)), dtable,
-                         op_span(vocab, ld_table, d, op_size(table_dtype))),
+  OP_REQUIRE(op_apart(op_matrix(grad, n, ld_grad, d, op_size(grad_dtype)),
+                      op_matrix(dtable, vocab, ld_table, d, op_size(table_dtype))),
              SSD_E_INVALID_ARG, "dtable overlaps grad");
   if (n == 0 && accumulate) return SSD_OK;
   const Layout l = layout(n, vocab, d);

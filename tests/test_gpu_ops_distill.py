@@ -410,3 +410,18 @@ def test_small_temperatures(env, dtype, v, T):
     z[2] += 5e4
     vals = vals * T  # (the teacher's distribution stays one)
     far_check(torch, ops, dtype, z, ids, vals, w, T)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("v", [200, 5001])
+def test_a_gradient_beside_the_logits_rows(env, dtype, v):
+    """Columns of one buffer: no element is shared."""
+    torch, ops = env
+    z, ids, vals, w = (t.cuda() for t in make(torch, dtype, 5, v, 12))
+    loss, lse, grad = ops.distill_step(z, ids, vals, w)
+    room = torch.zeros(5, 2 * v, dtype=z.dtype, device="cuda")
+    left, right = room[:, :v].copy_(z), room[:, v:]
+    assert torch.equal(ops.distill_step(left, ids, vals, w, out=right)[2], grad)
+    assert torch.equal(left, z)
+    back = ops.distill_backward(z, ids, vals, lse, w)
+    assert torch.equal(ops.distill_backward(left, ids, vals, lse, w, out=right), back)

@@ -373,3 +373,26 @@ def test_a_scale_that_is_no_number_leaves_absent_tokens_at_zero(env, td, scale, 
     there = torch.zeros(v, dtype=torch.bool).index_fill_(0, tokens.long(), True).cuda()
     assert not got[~there].any()
     assert not torch.isfinite(got[there]).any()
+
+
+@pytest.mark.parametrize("td,od", KINDS)
+def test_results_beside_their_inputs_rows(env, td, od):
+    """Table and out, gradient and table's gradient as columns of one buffer: no element is shared."""
+    torch, ops = env
+    n, v, d = 40, 60, 24
+    gen = torch.Generator().manual_seed(2)
+    tokens = draw_tokens(gen, torch, n, v, "zipf").cuda()
+
+    def halves(a, x, b, y):  # [rows][a] of type x and [rows][b] of type y, row beside row
+        size = [{"f32": 4, "bf16": 2}[k] * d for k in (x, y)]
+        room = torch.zeros(max(a, b), sum(size), dtype=torch.uint8, device="cuda")
+        return room, room[:a, :size[0]].view(dt(torch, x)), room[:b, size[0]:].view(dt(torch, y))
+
+    room, table, out = halves(v, td, n, od)
+    table.copy_(torch.randn(v, d, generator=gen))
+    want = ops.embed(tokens, table.clone(), dtype=dt(torch, od))
+    assert torch.equal(ops.embed(tokens, table, out=out), want)
+    room, grad, dtable = halves(n, od, v, td)
+    grad.copy_(torch.randn(n, d, generator=gen))
+    want = ops.embed_grad(tokens, grad.clone(), v, dtype=dt(torch, td))
+    assert torch.equal(ops.embed_grad(tokens, grad, v, out=dtable), want)
