@@ -176,6 +176,26 @@ __device__ __forceinline__ void read_transposed(unsigned a0, unsigned a1, unsign
   x[1] = (f32x4){e4, e5, e6, e7};
 }
 
+// The N results are complete.  A vector instruction may read a matrix product's result 8
+// (bfloat16) or 10 (float32) instructions' time after it and not sooner; nothing in the
+// hardware holds it back, and the compiler, which puts the waits, does not count reliably
+// across the end of a block (without this, scores of float32 were read one instruction after
+// the last product, where a branch lay between).  So results that are read behind a
+// branch are waited for here first.
+template <int N>
+__device__ __forceinline__ void complete(f32x4* x) {
+  static_assert(N == 1 || N == 2 || N == 4 || N == 8, "one statement for all: its wait comes after every product");
+  if constexpr (N == 1)
+    asm volatile("s_nop 9" : "+v"(x[0]));
+  else if constexpr (N == 2)
+    asm volatile("s_nop 9" : "+v"(x[0]), "+v"(x[1]));
+  else if constexpr (N == 4)
+    asm volatile("s_nop 9" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]));
+  else
+    asm volatile("s_nop 9"
+                 : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]), "+v"(x[4]), "+v"(x[5]), "+v"(x[6]), "+v"(x[7]));
+}
+
 // 2^x of the tiles from FROM on
 template <int FROM, int MT, int KT>
 __device__ __forceinline__ void exp2_all(f32x4 (&s)[MT][KT]) {
@@ -442,6 +462,7 @@ struct Wave {
         const float c = x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[mt] - x);
         m[mt] = x;
         limit[mt] = x + kSlack;
+        complete<DT>(o[mt]);
         beyond |= x != -INFINITY && fabsf(x) >= kFar;
         l[mt] *= c;
 #pragma unroll
@@ -496,12 +517,7 @@ struct Wave {
 
   __device__ __forceinline__ void scores(const unsigned char* k, f32x4 (&s)[MT][KT]) const {
     M::scores(k, q, s);
-    // (read here, in the products' own block: read past a branch, float32
-    // products of two tiles were taken before they were complete)
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt) asm volatile("" : "+v"(s[mt][kt]));
+    complete<MT * KT>(&s[0][0]);
   }
 
   // adds the values of a block, x read from v.  A weight of 0 does not silence
@@ -514,6 +530,8 @@ struct Wave {
     M::add(x, p, o);
     if (masked && __builtin_amdgcn_ballot_w64(bad)) {
       const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) complete<DT>(o[mt]);
 #pragma unroll 1
       for (int r = 0; r < KB; ++r)
 #pragma unroll
@@ -552,6 +570,7 @@ struct Wave {
   __device__ __forceinline__ void close() {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
+      complete<DT>(o[mt]);
       l[mt] += __shfl_xor(l[mt], 16);
       l[mt] += __shfl_xor(l[mt], 32);
       if (m[mt] == -INFINITY && l[mt] != l[mt]) m[mt] = 0.f;
