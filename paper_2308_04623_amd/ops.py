@@ -147,11 +147,10 @@ def _attn_plan(q, k_prefix, v_prefix, k_own, v_own, own_len, scale, out):
     b, t, h, d = q.shape
     g, p, _ = k_prefix.shape
     r = k_own.shape[2]
-    # (a dimension of one entry has no stride to speak of)
-    by = lambda strides, sizes: [x if n > 1 else 0 for x, n in zip(strides, sizes)]  # noqa: E731
+    out_strides = (t * h * d, h * d, d) if out is None else out.stride()
     a = _PrefixAttnDesc(_DTYPES[q.dtype], b, t, h, g, d, p, r, 1.0 / math.sqrt(d) if scale is None else scale,
-                        *by(q.stride(), (b, t, h)), *by((t * h * d, h * d, d) if out is None else out.stride(), (b, t, h)),
-                        *by(k_prefix.stride(), (g, p)), *by(k_own.stride(), (b, g, r)))
+                        *_strides(q.stride(), (b, t, h)), *_strides(out_strides, (b, t, h)),
+                        *_strides(k_prefix.stride(), (g, p)), *_strides(k_own.stride(), (b, g, r)))
     need = C.c_size_t(0)
     _check(_ops().ssd_prefix_attn_workspace(C.byref(a), C.byref(need)), "ssd_prefix_attn")
     plan = C.byref(a), need.value
@@ -160,6 +159,11 @@ def _attn_plan(q, k_prefix, v_prefix, k_own, v_own, own_len, scale, out):
             _attn_plans.clear()
         _attn_plans[key] = plan
     return plan
+
+
+def _strides(strides, sizes):
+    """The strides, 0 for a dimension of one entry, which has none to speak of."""
+    return [x if n > 1 else 0 for x, n in zip(strides, sizes)]
 
 
 def _refuse_attn(q, k_prefix, v_prefix, k_own, v_own, own_len, out):
@@ -176,8 +180,9 @@ def _refuse_attn(q, k_prefix, v_prefix, k_own, v_own, own_len, out):
         _refuse(what, f"k_prefix {tuple(k_prefix.shape)} and v_prefix {tuple(v_prefix.shape)} must be [G][P][{d}]")
     if k_own.shape != v_own.shape or tuple(k_own.shape) != (b, g, r, d):
         _refuse(what, f"k_own {tuple(k_own.shape)} and v_own {tuple(v_own.shape)} must be [{b}][{g}][R][{d}]")
-    if k_prefix.stride() != v_prefix.stride() or k_own.stride() != v_own.stride():
-        _refuse(what, "keys and values must have the same strides")
+    for k, v in ((k_prefix, v_prefix), (k_own, v_own)):
+        if _strides(k.stride(), k.shape) != _strides(v.stride(), v.shape):
+            _refuse(what, "keys and values must have the same strides")
     _vector(what, "own_len", own_len, torch.int32, b, q)
     if out is not None:
         _tensor(what, "out", out, (q.dtype,), 4, q)

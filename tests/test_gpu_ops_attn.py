@@ -559,3 +559,21 @@ def test_other_sequences_of_the_batch(env, dtype, form, kind):
         assert not out[1::2].any() and torch.isneginf(lse[1::2]).all()
     if kind == "nan-queries":
         assert torch.isnan(out[1::2]).all() and torch.isnan(lse[1::2]).all()
+
+
+def test_strides_of_dimensions_of_one_entry_do_not_matter(env):
+    """One kv head or one sequence: keys from one cache, values from a longer one."""
+    torch, ops = env
+
+    def inside(t, dim):  # t in a buffer with more entries of a dimension
+        shape = list(t.shape)
+        shape[dim] += 3
+        room = torch.full(shape, float("nan"), dtype=t.dtype, device="cuda")
+        return room[tuple(slice(n) for n in t.shape)].copy_(t)
+
+    x, lens = make(torch, "bf16", 3, 1, 4, 1, 64, 40, 8)
+    check(torch, ops, "bf16", x, lens, put=lambda name, t: inside(t, 1) if name == "vp" else t.cuda())
+    x, lens = make(torch, "bf16", 1, 1, 4, 2, 64, 40, 8)
+    check(torch, ops, "bf16", x, lens, put=lambda name, t: inside(t, 1) if name == "vo" else t.cuda())
+    x, lens = make(torch, "bf16", 1, 1, 4, 1, 64, 1, 1, lens=[1])
+    check(torch, ops, "bf16", x, lens, put=lambda name, t: inside(t, 1) if name in ("vp", "vo") else t.cuda())
