@@ -3,9 +3,11 @@
  *
  * Staged speculative decoding (Sec. 2.3, 3.2 of arXiv 2308.04623) is only as
  * fast as its draft agrees with the oracle.  A draft is brought nearer by
- * sampling a batch of continuations of one prompt, and fitting the draft's
- * distribution to the oracle's on them.  The operators here are what that
- * takes beside the verification pass and the top-k of ssd.h:
+ * sampling a batch of continuations of one prompt from the oracle, and fitting
+ * the draft's distribution to the oracle's on them.  The operators here are what
+ * that takes beside the verification pass and the top-k of ssd.h, for a draft
+ * whose layers between embedding and logits have their gradients elsewhere (or
+ * are none, as a bigram model's); attention has no backward pass:
  *   ssd_prefix_attn      attention of a batch of sequences over the keys and
  *                        values of a prompt they share and over their own;
  *   ssd_distill_*        the divergence of the draft's logits from the
@@ -69,7 +71,8 @@ ssd_status ssd_prefix_attn_workspace(const ssd_prefix_attn_desc *a, size_t *byte
  * n_kv_head and at most 1024; 1 <= n_seq <= 4096, 1 <= n_query <= 64, prefix_len,
  * own_rows >= 0 and below 2^30.  Pointers are 16-byte aligned and strides multiples
  * of 16 bytes, not negative; out's rows do not overlap, nor does out share an
- * element with an input.  k_prefix and v_prefix may be NULL when prefix_len is 0,
+ * element with an input (it may lie between its rows, heads or tokens, where a
+ * step that divides the larger ones of both tells them apart).  k_prefix and v_prefix may be NULL when prefix_len is 0,
  * k_own and v_own when own_rows is 0.  Scores and sums are float32: q.k and |scale| q.k have to lie below 2^127 in size, and are infinite
  * beyond.  bfloat16 calls round the weights exp(x - max) to bfloat16 for the
  * product with the values.

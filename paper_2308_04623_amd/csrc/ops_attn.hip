@@ -240,7 +240,10 @@ struct Math<bf16_t, D, MT> {
   struct P {
     u32x4 w[MT];
   };
-  // the weights as the second product's operand: its lane needs the keys it holds already
+  // The weights as the second product's operand: its lane needs the keys it holds already.
+  // They are rounded to bfloat16, 2^-9 of themselves at most, as a product with a float32 operand
+  // takes sixteen times as long; their sum takes them unrounded, for which they need not be
+  // unpacked again.  (Error against 64 bits 0.0023 relative; of the output's rounding alone 0.0016.)
   static __device__ __forceinline__ void weights(const f32x4 (&s)[MT][KT], P& p) {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
@@ -822,7 +825,9 @@ __device__ __forceinline__ void part_by_queries(const PrefixAttnArgs& a, Queries
 // Few queries are bound by memory (16 sequences of 20 heads of 64 over 100,000 rows: 82
 // us, 6.1 TB/s), many by the softmax's vector instructions and the matrix products, which
 // follow each other with 32 queries a wave (48 x 5 queries, 32 heads on 8 of 128, over 8191
-// rows: 52 us and 8 to join; 65536 rows: 303 us, 850 TFLOP/s).
+// rows: 56 us and 8 to join, 65 and 8 with up to 512 own rows a sequence; 65536 rows: 286 to 299
+// us with the join, 860 to 900 TFLOP/s; 64 dims, the same vector work for half the products: 64 x 8
+// queries of 20 heads over 5000 rows 36 us, 360 TFLOP/s).
 template <typename T, int D, int MP, int MO, bool BYQ>
 __global__ __launch_bounds__(64 * kWaves, D == 128 ? 2 : D == 64 ? 3 : 4) void prefix_attn_kernel(PrefixAttnArgs a) {
   extern __shared__ __align__(512) unsigned char lds[];  // (a block's rows lie at multiples of their size)
@@ -872,7 +877,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 128 ? 2 : D == 64 ? 3 : 4) void p
 // Prefixes that are short for the batch: a workgroup takes a tile of one
 // sequence's queries over the prefix and its own rows, and writes their attention.
 // One launch, no parts to write, read and join (6 sequences of 4 float32 heads of 32,
-// 64 + 24 rows: 7.4 us by parts, 5.1 by this; bound by latency, two blocks a wave).
+// 64 + 24 rows: 7.4 us by parts, 5.2 by this; bound by latency, two blocks a wave).
 template <typename T, int D, int MO>
 __global__ __launch_bounds__(64 * kWaves, D == 128 ? 2 : D == 64 ? 3 : 4) void short_attn_kernel(PrefixAttnArgs a) {
   extern __shared__ __align__(512) unsigned char lds[];

@@ -412,7 +412,7 @@ __global__ __launch_bounds__(1024) void distill_sweep_kernel(DistillArgs a) {
 
 // One workgroup per row, which its registers hold: C chunks a thread.
 // W: waves per SIMD that its registers leave room for.  Bound: memory (4096 bfloat16
-// rows of 50257, step: 158 us, 5.2 TB/s).
+// rows of 50257, step: 162 us, 5.1 TB/s).
 template <typename T, int TPB, int C, int W, bool GRAD>
 __global__ __launch_bounds__(TPB, W) void distill_row_kernel(DistillArgs a) {
   constexpr int E = Vec<T>::E;
@@ -538,10 +538,12 @@ ssd_status check_grad(int dtype, const void* logits, int64_t ld, int n, int V, c
 // 256 threads, 11.9 with 512, 11.1 with 1024).  More rows: few threads with many
 // chunks, so that two to four rows are on a CU and one's loads and stores run beside
 // another's arithmetic and waits (4096 bfloat16 rows of 32000, step: 98 us with 256
-// threads, 101 with 512, 147 with 1024), up to what their registers hold without
-// spilling (of 50257: 170, 157, 197; 4096 float32 rows of 50257: 332, 325, 316).  The
-// step of longer rows keeps them in 512 threads (4096 float32 rows of 65000: 427 us,
-// 465 in two sweeps).  The loss alone reads a row once either way: long rows are swept
+// threads, 101 with 512, 147 with 1024), up to what their registers hold with few
+// spilled (the step's instances of 13 chunks and more than 512 threads, of 16 and of 48
+// spill 3 to 10 each, 256 threads of 16 chunks of float32 none; 4096 bfloat16 rows of
+// 50257: 170, 157, 197; float32: 332, 325, 316).  The step of longer rows keeps them in 512
+// threads, few rows too (4096 float32 rows of 65000: 427 us, 465 in two sweeps; 256 rows
+// 29, 4.6 TB/s, of 90000 36, 5.1).  The loss alone reads a row once either way: long rows are swept
 // (4096 float32 rows of 65000: 193 us with 512 threads, 159 swept; of 20000: 54 with 256, 68).
 template <typename T, bool GRAD>
 void launch_rows(const DistillArgs& a, int n, hipStream_t s) {

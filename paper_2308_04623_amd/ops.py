@@ -8,6 +8,10 @@ the call (the current one, or `stream`), so calls may run on any streams that
 are ordered with the tensors' own use.  Every function takes its outputs from
 the caller where `out` is given.  Arguments are checked, here for what a pointer
 no longer tells (devices, types, shapes) and in the library for the rest.
+
+Nothing here is recorded for autograd: results are plain tensors whatever their
+inputs' requires_grad, and the gradients are the functions that say so
+(distill_backward, distill_step, embed_grad).  prefix_attention has none.
 """
 from __future__ import annotations
 
