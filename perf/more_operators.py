@@ -1,0 +1,727 @@
+"""The operators of a paged cache in 8 bits for a batch of sequences, as measurable cases.
+
+A case is a dict of plain values; its "kind" says which operators it goes
+through (paper_2308_04623_amd.paged):
+
+  attn     attention of each sequence's new rows (a chain, or a tree's nodes) over
+           its pages, its open page's rows and each other, all rows or a window of
+           them with the first few                      paged.paged_attention
+  admit    a prompt's keys and values become a sequence: pages are taken, its rows
+           stored in them and read back as the values that they stand for now
+                          paged.pages_take, .pages_store, .pages_load
+  commit   the accepted path of every sequence's new rows joins the sequence; pages
+           that got full are stored (and read back)   paged.pages_commit
+  fork     slots of the batch become copies of others, or are freed
+                                                        paged.pages_fork
+  compact  the pages in use move to the front of the pool
+                                                        paged.pages_compact
+
+Sizes are those of the package's models (the toy: 4 heads of 32, 2 layers;
+GPT-2-Large: 20 heads of 64, 36 layers) and, for grouped heads, generic ones.
+
+A page holds R0 rows of every layer and head: data uint8 [layer][page][head][2][R0 D]
+(keys, values), scale float32 [layer][page][head][2]; element = scale * code.
+Bytes are code + 128 ("int8") or a float of 4 exponent and 3 mantissa bits ("e4m3").
+Their order, with rows 32 a + 16 b + m of the keys and 32 a + 16 b + 4 g + r of the values:
+  keys, D >= 64   [a][b][D / 64: c][g: 4][m: 16][i: 16], dim 64 c + 16 g + i
+  keys, D = 32    [a][g: 4][m: 16][b][i: 8],              dim 8 g + i
+  values          [a][D / 32: c][g: 4][m: 16][u: 2][b][r: 4], dim 32 c + 16 u + m
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+
+def listed():
+    return [
+        # the toy float32 model, a few sequences: the smallest call, all launches and host work
+        {"name": "attn_f32_b3_p200", "kind": "attn", "dtype": "f32", "code": "int8", "b": 3, "t": 1, "h": 4, "hkv": 4,
+         "d": 32, "rows": 32, "p": 200, "tree": False, "window": 0, "sinks": 0},
+        # one decoding step of 32 sequences as long as the benchmark's longest context
+        {"name": "attn_b32_p2048", "kind": "attn", "dtype": "bf16", "code": "int8", "b": 32, "t": 1, "h": 20,
+         "hkv": 20, "d": 64, "rows": 32, "p": 2048, "tree": False, "window": 0, "sinks": 0},
+        # a tree of five speculated tokens for each of 48 sequences, grouped heads: the most bytes and products
+        {"name": "attn_gqa_b48_t5_p8191", "kind": "attn", "dtype": "bf16", "code": "e4m3", "b": 48, "t": 5, "h": 32,
+         "hkv": 8, "d": 128, "rows": 64, "p": 8191, "tree": True, "window": 0, "sinks": 0},
+        # a draft that looks at the last rows of long documents and the first few
+        {"name": "attn_window_b4_t8_p100000", "kind": "attn", "dtype": "bf16", "code": "int8", "b": 4, "t": 8,
+         "h": 20, "hkv": 20, "d": 64, "rows": 64, "p": 100000, "tree": False, "window": 4000, "sinks": 4},
+        # the toy's prompt
+        {"name": "admit_f32_p100", "kind": "admit", "dtype": "f32", "code": "int8", "layers": 2, "hkv": 4, "d": 32,
+         "rows": 32, "p": 100, "b": 4, "cols": 8, "pool": 64},
+        # a prompt of the benchmark's longest context, all layers
+        {"name": "admit_l36_p2047", "kind": "admit", "dtype": "bf16", "code": "int8", "layers": 36, "hkv": 20, "d": 64,
+         "rows": 32, "p": 2047, "b": 8, "cols": 80, "pool": 400},
+        # the toy's step of a tree of 15 nodes
+        {"name": "commit_f32_b3_t15", "kind": "commit", "dtype": "f32", "code": "int8", "layers": 2, "b": 3, "t": 15,
+         "hkv": 4, "d": 32, "rows": 32, "cols": 8, "pool": 64, "window": 0, "sinks": 0},
+        # a step of 48 sequences with 16 nodes each, all layers; pages behind the window are given back
+        {"name": "commit_l36_b48_t16", "kind": "commit", "dtype": "bf16", "code": "int8", "layers": 36, "b": 48,
+         "t": 16, "hkv": 20, "d": 64, "rows": 32, "cols": 24, "pool": 1216, "window": 300, "sinks": 4},
+        # the toy's prompt into more samples of it
+        {"name": "fork_f32_b6", "kind": "fork", "dtype": "f32", "layers": 2, "b": 6, "hkv": 4, "d": 32, "rows": 32,
+         "tail": 47, "cols": 8, "pool": 64},
+        # 64 samples of a few prompts, some of them ended
+        {"name": "fork_l36_b64", "kind": "fork", "dtype": "bf16", "layers": 36, "b": 64, "hkv": 20, "d": 64,
+         "rows": 32, "tail": 48, "cols": 256, "pool": 8000},
+        # a small pool, half of it free
+        {"name": "compact_l2_p64", "kind": "compact", "layers": 2, "hkv": 4, "d": 32, "rows": 32, "b": 4, "cols": 8,
+         "pool": 64},
+        # a pool of 20,000 rows of all layers, half of it free in pieces
+        {"name": "compact_l36_p625", "kind": "compact", "layers": 36, "hkv": 20, "d": 64, "rows": 32, "b": 16,
+         "cols": 64, "pool": 625},
+    ]
+
+
+def _log_int(rng, lo, hi):
+    lo, hi = min(lo, hi), max(lo, hi)
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+HEADS = [(4, 4, 32), (20, 20, 64), (20, 20, 64), (25, 25, 64), (16, 2, 64), (32, 8, 128)]
+
+
+def draw(rng):
+    kind = rng.choice(["attn", "attn", "attn", "admit", "commit", "commit", "fork", "compact"])
+    h, hkv, d = rng.choice(HEADS)
+    rows = rng.choice([32, 32, 64, 128])
+    code = rng.choice(["int8", "int8", "e4m3"])
+    dtype = rng.choice(["f32", "bf16"]) if d == 32 else rng.choice(["bf16", "bf16", "bf16", "f32"])
+    es = BYTES[dtype]
+    if kind == "attn":
+        t = rng.choice([1, 1, 1, 2, 5, 8, 13, 32, 64])
+        b = _log_int(rng, 1, 64)
+        # no more rows than leave the products and the bytes below the listed cases'
+        most = min(100000, 60_000_000 // (b * t * h), 600_000_000 // (2 * b * hkv * d))
+        p = _log_int(rng, 1, most)
+        window = rng.choice([0, 0, _log_int(rng, t, 8000)])
+        return {"kind": "attn", "dtype": dtype, "code": code, "b": b, "t": t, "h": h, "hkv": hkv, "d": d, "rows": rows,
+                "p": p, "tree": rng.random() < 0.4, "window": window,
+                "sinks": rng.choice([0, 1, 4, 100]) if window else 0}
+    layers = rng.choice([1, 2, 12, 36])
+    if kind == "admit":
+        p = _log_int(rng, rows, max(rows, min(8191, 190_000_000 // (2 * layers * hkv * d))))
+        pages = p // rows
+        return {"kind": "admit", "dtype": dtype, "code": code, "layers": layers, "hkv": hkv, "d": d, "rows": rows,
+                "p": p, "b": rng.randint(1, 16), "cols": pages + rng.randint(0, 40), "pool": 2 * pages + rng.randint(0, 60)}
+    if kind == "commit":
+        t = rng.choice([1, 1, 2, 5, 8, 16, 33, 64])
+        b = _log_int(rng, 1, max(1, min(64, 290_000_000 // (2 * layers * hkv * d * (rows + 2 * t) * es))))
+        cols = _log_int(rng, 4, max(4, min(128, 4_000_000_000 // (b * layers * hkv * 2 * rows * d) - 3)))
+        window = rng.choice([0, 0, _log_int(rng, t, cols * rows)])
+        return {"kind": "commit", "dtype": dtype, "code": code, "layers": layers, "b": b, "t": t, "hkv": hkv, "d": d,
+                "rows": rows, "cols": cols, "pool": b * (cols + 3), "window": window,
+                "sinks": rng.choice([0, 4]) if window else 0}
+    if kind == "fork":
+        tail = rows + rng.randint(0, 32)
+        b = _log_int(rng, 1, max(1, min(256, 700_000_000 // (2 * layers * hkv * d * tail * es))))
+        cols = _log_int(rng, 2, 1000)
+        return {"kind": "fork", "dtype": dtype, "layers": layers, "b": b, "hkv": hkv, "d": d, "rows": rows,
+                "tail": tail, "cols": cols, "pool": b * cols // 2 + rng.randint(1, 50)}
+    pool = _log_int(rng, 10, max(10, min(50000, 1_100_000_000 // (layers * hkv * d * rows * 2))))
+    b = rng.randint(1, 32)
+    return {"kind": "compact", "layers": layers, "hkv": hkv, "d": d, "rows": rows, "b": b, "cols": max(2, pool // b),
+            "pool": pool}
+
+
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+BYTES = {"f32": 4, "bf16": 2}
+MOST = {"int8": 127.0, "e4m3": 448.0}  # the largest code
+
+
+def _pool_pages(case):
+    """Pages and columns of the table that an attention case takes."""
+    cols = max(1, -(-(case["p"] + 2 * case["rows"]) // case["rows"]))
+    return case["b"] * cols + 3, cols
+
+
+def _tail_rows(case):
+    return case["rows"] + case["t"]
+
+
+def prepare(case, seed):
+    gen = torch.Generator("cuda").manual_seed(seed)
+    rand = lambda *s: torch.rand(s, generator=gen, device="cuda")  # noqa: E731
+    randn = lambda *s: torch.randn(s, generator=gen, device="cuda")  # noqa: E731
+    return {"attn": _prepare_attn, "admit": _prepare_admit, "commit": _prepare_commit, "fork": _prepare_fork,
+            "compact": _prepare_compact}[case["kind"]](case, gen, rand, randn)
+
+
+def _random_pages(case, layers, pool, gen, randn, rand):
+    """Pages as stored rows leave them: normal codes, scales that differ by block."""
+    size = case["rows"] * case["d"]
+    data = torch.empty((layers, pool, case["hkv"], 2, size), dtype=torch.uint8, device="cuda")
+    flat, top = data.view(-1), MOST[case.get("code", "int8")]
+    step = 1 << 26
+    for i in range(0, flat.numel(), step):
+        x = (randn(min(step, flat.numel() - i)) * (top / 4)).clamp(-top, top)
+        flat[i:i + step] = (x.round() + 128).to(torch.uint8) if case.get("code", "int8") == "int8" else \
+            x.to(torch.float8_e4m3fn).view(torch.uint8)
+    scale = (0.7 * 4 / top) * (0.6 + 0.8 * rand(layers, pool, case["hkv"], 2))
+    return data, scale
+
+
+def _random_tables(b, cols, pool, held, gen):
+    """Tables whose slot i holds held[i] pages, anywhere in the pool."""
+    table = torch.full((b, cols), -1, dtype=torch.int32, device="cuda")
+    ids = torch.randperm(pool, generator=gen, device="cuda").to(torch.int32)
+    at = 0
+    for i, n in enumerate(held):
+        table[i, :n] = ids[at:at + n]
+        at += n
+    refs = torch.zeros(pool, dtype=torch.int32, device="cuda")
+    refs[ids[:at].long()] = 1
+    return table, refs
+
+
+def _prepare_attn(case, gen, rand, randn):
+    dt, b, t, h, hkv, d, p = (DTYPES[case["dtype"]],) + tuple(case[k] for k in ("b", "t", "h", "hkv", "d", "p"))
+    pool, cols = _pool_pages(case)
+    state = {"case": case}
+    state["data"], state["scale"] = _random_pages(case, 1, pool, gen, randn, rand)
+    # every sequence is somewhere else
+    length = (p - (rand(b) * (p // 4 + 1)).floor()).to(torch.int32).clamp(min=0)
+    held = [int(x) // case["rows"] for x in length.tolist()]
+    table, _ = _random_tables(b, cols, pool, held, gen)
+    if case["window"]:  # pages behind the window were given back
+        first = (length.view(b, 1) - case["window"] + 1)
+        col = torch.arange(cols, device="cuda").view(1, cols)
+        gone = ((col + 1) * case["rows"] <= first) & (col * case["rows"] >= case["sinks"])
+        table = torch.where(gone, torch.full_like(table, -1), table)
+    if b > 4:  # one slot of the batch that holds no sequence
+        length[b // 3] = -1
+    if case["tree"]:  # a node's parent is any node before it
+        anc = torch.zeros((b, t), dtype=torch.int64)
+        up = torch.rand((b, t), generator=torch.Generator().manual_seed(int(length.sum()) + t))
+        for j in range(t):
+            own_bit = torch.full((b,), 1 << j if j < 63 else -(1 << 63), dtype=torch.int64)
+            anc[:, j] = own_bit if j == 0 else anc.gather(1, (up[:, j:j + 1] * j).long()).squeeze(1) | own_bit
+        state["anc"] = anc.cuda()
+    state.update(table=table, length=length, q=(2.0 * randn(b, t, h, d)).to(dt))
+    for name, shape in (("k_tail", (b, hkv, _tail_rows(case), d)), ("v_tail", (b, hkv, _tail_rows(case), d)),
+                        ("k_new", (b, t, hkv, d)), ("v_new", (b, t, hkv, d))):
+        state[name] = (0.7 * randn(*shape)).to(dt)
+    return state
+
+
+def _prepare_admit(case, gen, rand, randn):
+    layers, hkv, d, p, b, cols = (case[k] for k in ("layers", "hkv", "d", "p", "b", "cols"))
+    n = p // case["rows"]
+    free = case["pool"] - n - 2
+    held = [min(cols, max(0, free // (2 * b)))] * b
+    state = {"case": case, "slot": b // 2}
+    held[state["slot"]] = 0
+    state["table0"], state["refs0"] = _random_tables(b, cols, case["pool"], held, gen)
+    state["length0"] = torch.tensor(held, dtype=torch.int32, device="cuda") * case["rows"]
+    state["length0"][state["slot"]] = -1
+    state["count"] = torch.full((b,), -1, dtype=torch.int32, device="cuda")
+    state["count"][state["slot"]] = n
+    for x in ("table", "refs", "length"):
+        state[x] = state[x + "0"].clone()
+    state["data"], state["scale"] = _empty_pages(case, layers, case["pool"])
+    for name in ("k", "v"):  # a cache as the verification pass keeps it
+        x = torch.empty((layers, hkv, p, d), dtype=DTYPES[case["dtype"]], device="cuda")
+        for layer in range(layers):  # (some dims of the keys are larger than others)
+            x[layer] = ((randn(hkv, p, d) + 0.2) * (0.5 + 2.0 * rand(hkv, 1, d) ** 4)).to(x.dtype)
+        state[name] = x
+    return state
+
+
+def _empty_pages(case, layers, pool):
+    return (torch.zeros((layers, pool, case["hkv"], 2, case["rows"] * case["d"]), dtype=torch.uint8, device="cuda"),
+            torch.zeros((layers, pool, case["hkv"], 2), device="cuda"))
+
+
+def _prepare_commit(case, gen, rand, randn):
+    layers, b, t, hkv, d, rows, cols = (case[k] for k in ("layers", "b", "t", "hkv", "d", "rows", "cols"))
+    dt = DTYPES[case["dtype"]]
+    length = (rand(b) * (cols * rows)).to(torch.int32)
+    held = [int(x) // rows for x in length.tolist()]
+    state = {"case": case}
+    state["table0"], state["refs0"] = _random_tables(b, cols, case["pool"], held, gen)
+    if case["window"]:
+        col = torch.arange(cols, device="cuda").view(1, cols)
+        first = length.view(b, 1) - case["window"] + 1
+        gone = ((col + 1) * rows <= first) & (col * rows >= case["sinks"])
+        at = state["table0"][gone & (state["table0"] >= 0)].long()
+        state["refs0"][at] = 0
+        state["table0"] = torch.where(gone, torch.full_like(state["table0"], -1), state["table0"])
+    if b > 4:
+        length[b // 3] = -1
+    state["length0"] = length
+    for x in ("table", "refs", "length"):
+        state[x] = state[x + "0"].clone()
+    # the root is always kept, then fewer and fewer
+    keep = torch.rand((b, t), generator=gen, device="cuda") < 0.55
+    keep[:, 0] = True
+    state["path_len"] = keep.sum(1).to(torch.int32)
+    state["path"] = torch.argsort((~keep).to(torch.int32), dim=1, stable=True).to(torch.int32)
+    for name, shape in (("k_tail", (layers, b, hkv, rows + t, d)), ("v_tail", (layers, b, hkv, rows + t, d)),
+                        ("k_new", (layers, b, t, hkv, d)), ("v_new", (layers, b, t, hkv, d))):
+        x = torch.empty(shape, dtype=dt, device="cuda")
+        for layer in range(layers):
+            x[layer] = (0.7 * randn(*shape[1:])).to(dt)
+        state[name] = x
+    state["data"], state["scale"] = _empty_pages(case, layers, case["pool"])
+    return state
+
+
+def _prepare_fork(case, gen, rand, randn):
+    layers, b, hkv, d, rows, cols = (case[k] for k in ("layers", "b", "hkv", "d", "rows", "cols"))
+    dt = DTYPES[case["dtype"]]
+    most = min(cols, case["pool"] // b)
+    length = (rand(b) * (most + 1) * rows).to(torch.int32).clamp(max=most * rows + rows - 1)
+    state = {"case": case, "length": length}
+    state["table"], state["refs"] = _random_tables(b, cols, case["pool"], [int(x) // rows for x in length.tolist()], gen)
+    # every eighth slot is a prompt, the others become samples of one of them, or end
+    prompt = torch.arange(b, device="cuda") // 8 * 8
+    parents = (rand(b) * ((b + 7) // 8)).long() * 8
+    parents = torch.where(rand(b) < 0.1, torch.full_like(parents, -1), parents)
+    state["parents"] = torch.where(prompt == torch.arange(b, device="cuda"), prompt, parents).to(torch.int32)
+    for name in ("k_tail", "v_tail"):
+        x = torch.empty((layers, b, hkv, case["tail"], d), dtype=dt, device="cuda")
+        for layer in range(layers):
+            x[layer] = randn(*x.shape[1:]).to(dt)
+        state[name] = x
+    return state
+
+
+def _prepare_compact(case, gen, rand, randn):
+    layers, pool, b, cols = (case[k] for k in ("layers", "pool", "b", "cols"))
+    state = {"case": case}
+    held = [min(cols, int(x)) for x in (rand(b) * (pool / b)).tolist()]  # half of the pool
+    state["table0"], state["refs0"] = _random_tables(b, cols, pool, held, gen)
+    if b > 1:  # two sequences that share their first page
+        state["table0"][1, 0] = state["table0"][0, 0]
+        state["refs0"] = torch.bincount(state["table0"][state["table0"] >= 0].view(-1), minlength=pool).to(torch.int32)
+    state["table"], state["refs"] = state["table0"].clone(), state["refs0"].clone()
+    state["data"], state["scale"] = _random_pages(case, layers, pool, gen, randn, rand)
+    return state
+
+
+def run(state):
+    kind = state["case"]["kind"]
+    if own:
+        return {"attn": _attn_own, "admit": _admit_own, "commit": _commit_own, "fork": _fork_own,
+                "compact": _compact_own}[kind](state["case"], state)
+    return {"attn": _attn_plain, "admit": _admit_plain, "commit": _commit_plain, "fork": _fork_plain,
+            "compact": _compact_plain}[kind](state["case"], state)
+
+
+# ---------------------------------------------------------------- the package's operators
+
+def _pages(case, s):
+    from paper_2308_04623_amd import paged
+    if "pages" not in s:  # (the cache's object: a user's program keeps it beside its tensors)
+        s["pages"] = paged.Pages(s["data"], s["scale"], case["rows"], case.get("code", "int8"))
+    return paged, s["pages"]
+
+
+def _attn_own(case, s):
+    paged, pages = _pages(case, s)
+    return paged.paged_attention(s["q"], pages, s["table"], s["length"], s["k_tail"], s["v_tail"], s["k_new"],
+                                 s["v_new"], layer=0, anc=s.get("anc"), window=case["window"], sinks=case["sinks"])
+
+
+def _again(s, *names):
+    """The state before the pass: what a pass changes in place."""
+    for x in names:
+        s[x].copy_(s[x + "0"])
+
+
+def _admit_own(case, s):
+    paged, pages = _pages(case, s)
+    _again(s, "refs", "table", "length")
+    n, rows = case["p"] // case["rows"], case["rows"]
+    got = paged.pages_take(pages, s["refs"], s["table"], s["length"], s["count"])
+    ids = s["table"][s["slot"], :n]
+    k, v = (x[:, :, :n * rows].unflatten(2, (n, rows)).transpose(1, 2) for x in (s["k"], s["v"]))
+    paged.pages_store(pages, ids, k, v)
+    k, v = paged.pages_load(pages, ids, dtype=s["k"].dtype)
+    return {"got": got, "refs": s["refs"], "table": s["table"], "length": s["length"], "k": k, "v": v}
+
+
+def _commit_own(case, s):
+    paged, pages = _pages(case, s)
+    _again(s, "refs", "table", "length")
+    full = paged.pages_commit(pages, s["refs"], s["table"], s["length"], s["k_tail"], s["v_tail"], s["k_new"],
+                              s["v_new"], s["path"], s["path_len"], window=case["window"], sinks=case["sinks"])
+    k, v = paged.pages_load(pages, _last_page(case, s["table"], s["length"], full), dtype=s["k_tail"].dtype)
+    return {"full": full, "refs": s["refs"], "table": s["table"], "length": s["length"], "k_tail": s["k_tail"],
+            "v_tail": s["v_tail"], "k": k, "v": v}
+
+
+def _last_page(case, table, length, full):
+    """The last page that each sequence filled, -1 where there is none."""
+    col = length // case["rows"] - 1
+    last = table.gather(1, col.clamp(min=0).long().view(-1, 1)).squeeze(1)
+    return torch.where(full > 0, last, torch.full_like(last, -1))
+
+
+def _fork_own(case, s):
+    from paper_2308_04623_amd import paged
+    paged.pages_fork(s["refs"], s["table"], s["length"], s["parents"], s["k_tail"], s["v_tail"], case["rows"])
+    return {x: s[x] for x in ("refs", "table", "length", "k_tail", "v_tail")}
+
+
+def _compact_own(case, s):
+    paged, pages = _pages(case, s)
+    _again(s, "refs", "table")
+    used = paged.pages_compact(pages, s["refs"], s["table"])
+    # (pages are moved as they are: their bytes)
+    return {"used": used, "refs": s["refs"], "table": s["table"], "data": s["data"], "scale": s["scale"]}
+
+
+# ---------------------------------------------------------------- plain forms
+
+def _codes(x, case):
+    return x.float() - 128.0 if case.get("code", "int8") == "int8" else x.view(torch.float8_e4m3fn).float()
+
+
+def _rows_of(data, scale, case):
+    """(keys, values) float32 [...][rows][d] of pages [...][2][rows d] and scales [...][2]."""
+    rows, d, lead = case["rows"], case["d"], tuple(data.shape[:-2])
+    x = _codes(data, case) * scale.unsqueeze(-1)
+    k, v = x[..., 0, :].reshape(-1, rows * d), x[..., 1, :].reshape(-1, rows * d)
+    a = rows // 32
+    if d == 32:
+        k = k.view(-1, a, 4, 16, 2, 8).permute(0, 1, 4, 3, 2, 5)
+    else:
+        k = k.view(-1, a, 2, d // 64, 4, 16, 16).permute(0, 1, 2, 5, 3, 4, 6)
+    v = v.view(-1, a, d // 32, 4, 16, 2, 2, 4).permute(0, 1, 6, 3, 7, 2, 5, 4)
+    return k.reshape(*lead, rows, d), v.reshape(*lead, rows, d)
+
+
+def _quantized(x, case):
+    """(codes, scales) of blocks [...][rows][d]: scale * code is what stands for an element."""
+    top = MOST[case["code"]]
+    a = x.float().abs().amax((-1, -2), keepdim=True)
+    zero, most = a < 2.0 ** -100, torch.full_like(a, top)  # (a division by or of a number is not the rounded quotient)
+    r = torch.where(zero, torch.zeros_like(a), torch.div(most, torch.where(zero, torch.ones_like(a), a)))
+    y = (x.float() * r).clamp(-top, top)
+    code = y.round() if case["code"] == "int8" else y.to(torch.float8_e4m3fn).float()
+    return code, torch.where(zero, torch.zeros_like(a), torch.div(a, most))
+
+
+def _seen(case, s, cols):
+    """bool [b][t][rows of the pages], [b][t][tail rows], [b][t][new rows]."""
+    b, t, rows, length = case["b"], case["t"], case["rows"], s["length"].long()
+    dev = length.device
+    bit = torch.arange(t, device=dev)
+    if "anc" in s:
+        new = (s["anc"].view(b, t, 1) >> bit) & 1 > 0
+    else:
+        new = (bit.view(1, 1, t) <= bit.view(1, t, 1)).expand(b, t, t)
+    position = length.view(b, 1) + (new.sum(2) - 1).clamp(min=0)  # of the queries
+    first = position - case["window"] + 1 if case["window"] else torch.zeros_like(position)
+
+    def old(j, held):  # j: positions [b][n]
+        return held.unsqueeze(1) & ((j.unsqueeze(1) >= first.unsqueeze(2)) | (j.unsqueeze(1) < case["sinks"]))
+
+    n_paged = length.clamp(min=0) // rows * rows
+    j = torch.arange(cols * rows, device=dev).expand(b, -1)
+    paged = old(j, (j < n_paged.view(b, 1)) & (s["table"] >= 0).repeat_interleave(rows, 1))
+    x = torch.arange(rows, device=dev).expand(b, -1)
+    tail = old(n_paged.view(b, 1) + x, x < (length - n_paged).view(b, 1))
+    return paged, tail, new & (length >= 0).view(b, 1, 1), (n_paged.view(b, 1) + x) % _tail_rows(case)
+
+
+def _attn_plain(case, s):
+    b, t, h, hkv, d = (case[k] for k in ("b", "t", "h", "hkv", "d"))
+    g, cols = h // hkv, s["table"].shape[1]
+    paged, tail, new, slot = _seen(case, s, cols)
+    ids = s["table"].clamp(min=0).long()
+    kp, vp = _rows_of(s["data"][0][ids], s["scale"][0][ids], case)  # [b][cols][hkv][rows][d]
+    at = slot.view(b, 1, -1, 1).expand(-1, hkv, -1, d)
+    parts = []
+    for p, x, y in ((kp, s["k_tail"], s["k_new"]), (vp, s["v_tail"], s["v_new"])):
+        parts.append(torch.cat([p.transpose(1, 2).reshape(b, hkv, -1, d), x.float().gather(2, at),
+                                y.float().transpose(1, 2)], 2).reshape(b * hkv, -1, d))
+    k, v = parts
+    q = s["q"].float().view(b, t, hkv, g, d).transpose(1, 2).reshape(b * hkv, t * g, d)
+    x = torch.bmm(q, k.transpose(1, 2).contiguous()).view(b, hkv, t, g, -1) * (1.0 / math.sqrt(d))
+    seen = torch.cat([paged, tail, new], 2).view(b, 1, t, 1, -1)
+    x = x.masked_fill(~seen, -math.inf)
+    top = x.amax(4, keepdim=True)
+    e = torch.exp(x - torch.where(top == -math.inf, torch.zeros_like(top), top))
+    total = e.sum(4, keepdim=True)
+    w = torch.where(total > 0, e / total, torch.zeros_like(e))
+    o = torch.bmm(w.view(b * hkv, t * g, -1), v).view(b, hkv, t, g, d)
+    return o.transpose(1, 2).reshape(b, t, h, d).to(s["q"].dtype)
+
+
+def _taken(refs, need, can):
+    """The lowest free pages for slots that need some, in order: (ids [b][most], slots that get theirs)."""
+    free = torch.nonzero(refs == 0).squeeze(1)
+    want = torch.where(can, need, torch.zeros_like(need))
+    first = torch.cumsum(want, 0) - want
+    ok = can & ((want == 0) | (first + want <= free.numel()))
+    most = int(need.max()) if need.numel() else 0
+    at = first.view(-1, 1) + torch.arange(max(most, 1), device=refs.device)
+    ids = free[at.clamp(max=max(free.numel() - 1, 0))] if free.numel() else torch.zeros_like(at)
+    return ids, ok
+
+
+def _admit_plain(case, s):
+    rows, n = case["rows"], case["p"] // case["rows"]
+    refs, table, length = s["refs0"].clone(), s["table0"].clone(), s["length0"].clone()
+    asked = s["count"] >= 0
+    col = length.clamp(min=0) // rows
+    can = asked & (length.clamp(min=0) % rows == 0) & (col + s["count"] <= case["cols"])
+    ids, ok = _taken(refs, s["count"].clamp(min=0).long(), can)
+    got = torch.where(ok, s["count"], torch.full_like(s["count"], -1))
+    j = torch.arange(ids.shape[1], device=refs.device)
+    put = ok.view(-1, 1) & (j < s["count"].view(-1, 1))
+    slot, x = torch.nonzero(put, as_tuple=True)
+    table[slot, col[slot].long() + x] = ids[put].to(torch.int32)
+    refs[ids[put]] = 1
+    length = torch.where(ok, length.clamp(min=0) + got * rows, length)
+    out = {"got": got, "refs": refs, "table": table, "length": length}
+    for name in ("k", "v"):
+        x = s[name][:, :, :n * rows].unflatten(2, (n, rows)).transpose(1, 2)
+        code, scale = _quantized(x, case)
+        out[name] = (code * scale).to(x.dtype)
+    return out
+
+
+def _commit_plain(case, s):
+    rows, b, t, cols = case["rows"], case["b"], case["t"], case["cols"]
+    refs, table, length = s["refs0"].clone(), s["table0"].clone(), s["length0"].long()
+    ring = rows + t
+    live = length >= 0
+    n = torch.where(live, s["path_len"].long(), torch.zeros_like(length))
+    before, after = length.clamp(min=0) // rows, (length.clamp(min=0) + n) // rows
+    need = after - before
+    ids, ok = _taken(refs, need, live & (after <= cols))
+    n = torch.where(ok, n, torch.zeros_like(n))
+    total = torch.where(ok, length + n, length)
+    full = torch.where(ok | ~live, torch.where(ok, need, torch.zeros_like(need)), torch.full_like(need, -1))
+    j = torch.arange(ids.shape[1], device=refs.device)
+    put = ok.view(b, 1) & (j < need.view(b, 1))
+    slot, x = torch.nonzero(put, as_tuple=True)
+    table[slot, before[slot] + x] = ids[put].to(torch.int32)
+    refs[ids[put]] = 1
+    if case["window"]:
+        col = torch.arange(cols, device=refs.device).view(1, cols)
+        gone = ((col + 1) * rows <= total.view(b, 1) - case["window"] + 1) & (col * rows >= case["sinks"])
+        gone = gone & ok.view(b, 1) & (table >= 0)
+        refs.index_add_(0, table[gone].long(), torch.full((int(gone.sum()),), -1, dtype=torch.int32, device=refs.device))
+        table = torch.where(gone, torch.full_like(table, -1), table)
+    out = {"full": full.to(torch.int32), "refs": refs, "table": table, "length": total.to(torch.int32)}
+    # the rows of the last page that got full: from the tail up to `length`, from the new rows behind
+    last = (after - 1).clamp(min=0) * rows
+    pos = last.view(b, 1) + torch.arange(rows, device=refs.device)
+    from_tail = pos < length.view(b, 1)
+    step = s["path"].long().gather(1, (pos - length.view(b, 1)).clamp(0, t - 1))
+    moved = torch.arange(t, device=refs.device)
+    keep = (moved < n.view(b, 1)) & (length.view(b, 1) + moved >= (after * rows).view(b, 1))
+    bi, mi = torch.nonzero(keep, as_tuple=True)
+    for name in ("k", "v"):
+        tail, new = s[name + "_tail"], s[name + "_new"]
+        layers, _, hkv, _, d = tail.shape
+        a = tail.gather(3, (pos % ring).view(1, b, 1, rows, 1).expand(layers, -1, hkv, -1, d))
+        c = new.transpose(2, 3).gather(3, step.view(1, b, 1, rows, 1).expand(layers, -1, hkv, -1, d))
+        code, scale = _quantized(torch.where(from_tail.view(1, b, 1, rows, 1), a, c), case)
+        # (a page given back at once, behind a short window, is not read)
+        there = (full > 0) & (table.gather(1, (after - 1).clamp(min=0).view(b, 1)).squeeze(1) >= 0)
+        out[name] = torch.where(there.view(1, b, 1, 1, 1), code * scale, torch.zeros_like(code)).to(tail.dtype)
+        tail = tail.clone()
+        tail[:, bi, :, (length[bi] + mi) % ring] = new[:, bi, s["path"].long()[bi, mi]].transpose(0, 1)
+        out[name + "_tail"] = tail
+    return {x: out[x] for x in ("full", "refs", "table", "length", "k_tail", "v_tail", "k", "v")}
+
+
+def _fork_plain(case, s):
+    rows, b, cols = case["rows"], case["b"], case["cols"]
+    here = torch.arange(b, device=s["length"].device)
+    parent = s["parents"].long()
+    kept = (parent >= 0) & (parent < b)
+    kept = kept & (parent[parent.clamp(0, b - 1)] == parent)
+    src = torch.where(kept, parent, here)
+    none = (~kept).view(b, 1)
+    table = torch.where(none, torch.full_like(s["table"], -1), s["table"][src])
+    length = torch.where(kept, s["length"][src], torch.full_like(s["length"], -1))
+    refs = s["refs"].clone()
+    for x, by in ((s["table"], -1), (table, 1)):
+        at = x[x >= 0].long()
+        refs.index_add_(0, at, torch.full((at.numel(),), by, dtype=torch.int32, device=refs.device))
+    out = {"refs": refs, "table": table, "length": length}
+    ring = case["tail"]
+    start = length.clamp(min=0).long() // rows * rows
+    x = torch.arange(rows, device=refs.device)
+    moved = (x < (length.clamp(min=0).long() - start).view(b, 1)) & (src != here).view(b, 1)
+    bi, xi = torch.nonzero(moved, as_tuple=True)
+    slot = (start[bi] + xi) % ring
+    for name in ("k_tail", "v_tail"):
+        tail = s[name].clone()
+        tail[:, bi, :, slot] = s[name][:, src[bi], :, slot]
+        out[name] = tail
+    return out
+
+
+def _compact_plain(case, s):
+    refs, table = s["refs0"].clone(), s["table0"].clone()
+    used = torch.nonzero(refs > 0).squeeze(1)
+    u = used.numel()
+    front = torch.arange(refs.numel(), device=refs.device) < u
+    holes, movers = torch.nonzero(front & (refs == 0)).squeeze(1), torch.nonzero(~front & (refs > 0)).squeeze(1)
+    to = torch.arange(refs.numel(), device=refs.device)
+    to[movers] = holes
+    table = torch.where(table >= 0, to[table.clamp(min=0).long()].to(torch.int32), table)
+    refs[holes] = refs[movers]
+    refs[movers] = 0
+    data, scale = s["data"].clone(), s["scale"].clone()
+    data[:, holes] = data[:, movers]
+    scale[:, holes] = scale[:, movers]
+    return {"used": torch.tensor([u], dtype=torch.int32, device=refs.device), "refs": refs, "table": table, "data": data,
+            "scale": scale}
+
+
+# ---------------------------------------------------------------- what a pass cannot do without
+
+def work(case):
+    kind, hkv, d, rows = case["kind"], case["hkv"], case["d"], case["rows"]
+    es = BYTES[case.get("dtype", "f32")]
+    if kind == "attn":
+        b, t, h, p = (case[k] for k in ("b", "t", "h", "p"))
+        live = b - (b > 4)
+        mean = max(0.0, p - 0.5 * (p // 4))
+        if case["window"]:
+            mean = min(mean, case["window"] + case["sinks"])
+        old = max(0.0, mean - rows / 2)
+        own_rows = min(mean, rows / 2) + t
+        return {"bytes": live * (2 * hkv * (d * old + 4 * old / rows + es * d * own_rows) + 2 * es * t * h * d),
+                "flops": 4.0 * d * h * t * live * (mean + (t + 1) / 2)}
+    layers = case["layers"]
+    if kind == "admit":
+        n = case["p"] // rows
+        entries = 2 * layers * n * hkv * rows * d
+        return {"bytes": entries * (es + 1 + 1 + es), "flops": 2.0 * entries}
+    if kind == "commit":
+        b, t = case["b"] - (case["b"] > 4), case["t"]
+        kept = 1 + 0.55 * (t - 1)  # rows of a sequence
+        pages = kept / rows
+        entries = 2 * layers * b * hkv * d
+        # kept rows are read and written, full pages' rows read, their codes written; those, and zeros, read back
+        return {"bytes": entries * (kept * es * 2 + pages * rows * (es + 1) + pages * rows + rows * es),
+                "flops": 2.0 * entries * pages * rows}
+    if kind == "fork":
+        b = case["b"]
+        moved = 0.9 * (b - (b + 7) // 8)
+        return {"bytes": moved * (2 * 2 * layers * hkv * d * es * rows / 2) + 8 * b * case["cols"], "flops": 0.0}
+    moved = case["pool"] / 4  # half of the used half
+    return {"bytes": 2 * moved * layers * hkv * 2 * (rows * d + 4) + 8 * case["pool"], "flops": 0.0}
+
+
+# ---------------------------------------------------------------- the definition in 64 bits
+
+def exact(case, seed):
+    if case["kind"] == "attn":
+        return _attn_exact(case, prepare(case, seed))
+    if case["kind"] == "admit":
+        s = prepare(case, seed)
+        n = case["p"] // case["rows"]
+        out = {"got": None, "refs": None, "table": None, "length": None}
+        for name in ("k", "v"):
+            out[name] = torch.empty((case["layers"], n, case["hkv"], case["rows"], case["d"]), dtype=torch.float64,
+                                    device="cuda")
+            for i in range(n):
+                out[name][:, i] = _values_exact(s[name][:, :, i * case["rows"]:(i + 1) * case["rows"]], case)
+        return out
+    if case["kind"] == "commit":
+        return _commit_exact(case, prepare(case, seed))
+    return None  # whole numbers and rows that are moved as they are
+
+
+def _values_exact(x, case):
+    """Blocks' values; which code stands for an element is decided in float32 by definition."""
+    top = torch.tensor(MOST[case["code"]], device=x.device)
+    flat = x.float().flatten(-2)
+    a = flat.abs().max(-1).values
+    code = flat * torch.div(top, a).unsqueeze(-1)
+    code = torch.clamp(code.double(), -MOST[case["code"]], MOST[case["code"]])
+    if case["code"] == "int8":
+        code = torch.round(code)
+    else:  # 3 bits behind the leading one, steps of 2^-9 at the least
+        step = torch.exp2((torch.frexp(code)[1].double() - 1).clamp(min=-6) - 3)
+        code = torch.round(code / step) * step
+    return (code * torch.div(a, top).double().unsqueeze(-1)).view(x.shape)
+
+
+def _byte_places(rows, d, device):
+    """Places of element (row, dim) in a page's keys and values."""
+    j = torch.arange(rows, device=device).view(-1, 1)
+    i = torch.arange(d, device=device).view(1, -1)
+    if d == 32:
+        k = (j // 32) * 1024 + (i // 8) * 256 + (j % 16) * 16 + (j // 16 % 2) * 8 + i % 8
+    else:
+        k = (j // 16) * (16 * d) + (i // 64) * 1024 + (i // 16 % 4) * 256 + (j % 16) * 16 + i % 16
+    v = (j // 32) * (32 * d) + (i // 32) * 1024 + (j // 4 % 4) * 256 + (i % 16) * 16 + (i // 16 % 2) * 8 + \
+        (j // 16 % 2) * 4 + j % 4
+    return k.reshape(-1), v.reshape(-1)
+
+
+def _attn_exact(case, s):
+    b, t, h, hkv, d, rows = (case[k] for k in ("b", "t", "h", "hkv", "d", "rows"))
+    g, ring = h // hkv, _tail_rows(case)
+    out = torch.zeros((b, t, h, d), dtype=torch.float64, device="cuda")
+    places = _byte_places(rows, d, "cuda")
+    for i, n in enumerate(s["length"].tolist()):
+        if n < 0:
+            continue
+        masks = [int(m) & (2 ** 64 - 1) for m in s["anc"][i].tolist()] if "anc" in s else \
+            [(2 << j) - 1 for j in range(t)]
+        cols = [c for c in range(n // rows) if int(s["table"][i, c]) >= 0] if not case["window"] else \
+            [c for c, x in enumerate(s["table"][i, :n // rows].tolist()) if x >= 0]
+        ids = s["table"][i, cols].long()
+        at = torch.tensor([c * rows for c in cols], dtype=torch.long, device="cuda").view(-1, 1) + \
+            torch.arange(rows, device="cuda")
+        behind = torch.arange(n // rows * rows, n, device="cuda")
+        pos = torch.cat([at.view(-1), behind])
+        for kv in range(hkv):
+            both = []
+            for which, tail, new in ((0, "k_tail", "k_new"), (1, "v_tail", "v_new")):
+                x = s["data"][0, ids, kv, which][:, places[which]]
+                x = (x.double() - 128 if case["code"] == "int8" else x.view(torch.float8_e4m3fn).double())
+                x = (x * s["scale"][0, ids, kv, which].double().view(-1, 1)).view(-1, d)
+                both.append(torch.cat([x, s[tail][i, kv, behind % ring].double(), s[new][i, :, kv].double()]))
+            k, v = both
+            q = s["q"][i, :, kv * g:(kv + 1) * g].double()
+            scores = (q.reshape(t * g, d) @ k.T / math.sqrt(d)).view(t, g, -1)
+            for j in range(t):
+                seen = torch.ones(len(k), dtype=torch.bool, device="cuda")
+                if case["window"]:
+                    last = n + max(bin(masks[j]).count("1") - 1, 0)
+                    seen[:len(pos)] = (pos > last - case["window"]) | (pos < case["sinks"])
+                seen[len(pos):] = torch.tensor([bool(masks[j] >> x & 1) for x in range(t)], device="cuda")
+                if bool(seen.any()):
+                    out[i, j, kv * g:(kv + 1) * g] = torch.softmax(scores[j][:, seen], 1) @ v[seen]
+    return out
+
+
+def _commit_exact(case, s):
+    """The values of the pages that got full, sequence by sequence; rows of the tails as they are."""
+    rows, ring, hkv, d = case["rows"], case["rows"] + case["t"], case["hkv"], case["d"]
+    free = int((s["refs0"] == 0).sum())
+    out = {x: None for x in ("full", "refs", "table", "length", "k_tail", "v_tail")}
+    for name in ("k", "v"):
+        out[name] = torch.zeros((case["layers"], case["b"], hkv, rows, d), dtype=torch.float64, device="cuda")
+    for i, (n, m) in enumerate(zip(s["length0"].tolist(), s["path_len"].tolist())):
+        need = (n + m) // rows - n // rows
+        if n < 0 or (n + m) // rows > case["cols"]:
+            continue
+        free -= need  # (a slot that finds too few takes none, and leaves none to those behind it)
+        end = (n + m) // rows * rows
+        released = case["window"] and end <= n + m - case["window"] + 1 and end - rows >= case["sinks"]
+        if free < 0 or need == 0 or released:
+            continue
+        path = s["path"][i].tolist()
+        for name in ("k", "v"):
+            x = [s[name + "_tail"][:, i, :, p % ring] if p < n else s[name + "_new"][:, i, path[p - n]]
+                 for p in range(end - rows, end)]
+            out[name][:, i] = _values_exact(torch.stack(x, 2), case)
+    return out
