@@ -6,7 +6,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 SOURCES = [os.path.join(HERE, "csrc", n) for n in ("kernels.hip", "fused.hip", "runtime.hip", "ops_attn.hip",
-                                                    "ops_distill.hip", "ops_embed.hip")]
+                                                    "ops_distill.hip", "ops_embed.hip", "ops_pages.hip",
+                                                    "ops_pages_attn.hip")]
 OUT = os.path.join(HERE, "libssd.so")
 
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -1,0 +1,918 @@
+// The paged cache of ssd_pages.h, but for its attention: blocks of rows into 8-bit codes and
+// back, and the sequences' tables.
+#include <algorithm>
+#include <type_traits>
+
+#include "ops_pages.h"
+
+namespace ssd {
+namespace {
+
+constexpr int kThreads = 256, kWaveCount = kThreads / 64;
+constexpr int kPlan = 1024, kPer = 4;  // threads of the kernels that give out pages, slots for each
+static_assert(kPlan * kPer >= 4096, "a thread for every four slots");
+
+// ---------------------------------------------------------------- codes
+
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float* x);
+template <>
+__device__ __forceinline__ void load8<float>(const float* p, float* x) {
+  const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
+}
+template <>
+__device__ __forceinline__ void load8<bf16_t>(const bf16_t* p, float* x) {
+  const u32x4 a = *(const u32x4*)p;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(a[i] << 16);
+    x[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void store8(float* p, const float* x) {
+  *(f32x4*)p = (f32x4){x[0], x[1], x[2], x[3]};
+  *(f32x4*)(p + 4) = (f32x4){x[4], x[5], x[6], x[7]};
+}
+__device__ __forceinline__ void store8(bf16_t* p, const float* x) {
+  u32x4 a;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    a[i] = (unsigned)__builtin_bit_cast(uint16_t, (__bf16)x[2 * i]) |
+           (unsigned)__builtin_bit_cast(uint16_t, (__bf16)x[2 * i + 1]) << 16;
+  *(u32x4*)p = a;
+}
+
+// How a block is coded (see ssd_pages.h), from the bits of its largest magnitude: as
+// whole numbers those of infinities and NaN are larger than all finite ones'.
+struct Coding {
+  float r, scale;
+  bool live;  // else: codes 0
+};
+template <int CODE>
+__device__ __forceinline__ Coding coding(unsigned bits) {
+  constexpr float top = CODE == SSD_PAGE_INT8 ? 127.f : 448.f;
+  const float a = __uint_as_float(bits);
+  if (bits >= 0x7f800000u) return {0.f, __uint_as_float(0x7fc00000u), false};
+  if (a < 0x1p-100f) return {0.f, 0.f, false};
+  return {top / a, a / top, true};
+}
+// Four codes, the first in the lowest byte.  (x r is rounded by itself: the clamp lies between
+// it and the sum whose last bits are the nearest whole number's, ties to even.)
+template <int CODE>
+__device__ __forceinline__ unsigned code4(const float* x, int step, const Coding& c) {
+  constexpr float top = CODE == SSD_PAGE_INT8 ? 127.f : 448.f;
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = c.live ? fminf(fmaxf(x[i * step] * c.r, -top), top) : 0.f;
+  if constexpr (CODE == SSD_PAGE_INT8) {
+    unsigned u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = __float_as_uint(y[i] + 12583040.f);  // 1.5 2^23 + 128
+    return __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400u) | __builtin_amdgcn_perm(u[3], u[2], 0x04000c0cu);
+  } else {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+    return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+  }
+}
+template <int CODE>
+__device__ __forceinline__ void values4(unsigned w, float scale, float* x, int step) {
+  if constexpr (CODE == SSD_PAGE_INT8) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i * step] = ((float)(w >> 8 * i & 255u) - 128.f) * scale;
+  } else {
+    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+    x[0] = lo[0] * scale;
+    x[step] = lo[1] * scale;
+    x[2 * step] = hi[0] * scale;
+    x[3 * step] = hi[1] * scale;
+  }
+}
+
+// A wave's part of a block: 32 rows.
+//   Keys: a lane has chunks q < D / 16 of 8 dims, of row k_row(q) at k_dim(q), in the order of
+// its bytes: chunks 2 s and 2 s + 1 are the 16 bytes at 1024 s + 16 lane.
+//   Values: a lane has, for i < V, the four rows 4 (p / (D / 8)) .. at the 8 dims 8 (p mod (D / 8)), p = lane + 64 i
+// (D = 32: 32 lanes do); four rows at a dim are one 4-byte word, placed through LDS.
+template <int D>
+struct Part {
+  static constexpr int KEYS = D / 16, VALUES = D == 128 ? 2 : 1, BYTES = 32 * D;
+  static __device__ __forceinline__ int k_row(int lane, int q) {
+    return (lane & 15) + 16 * (D == 32 ? q : q / (D / 32));
+  }
+  static __device__ __forceinline__ int k_dim(int lane, int q) {
+    return D == 32 ? 8 * (lane >> 4) : 64 * (q / 2 % (D / 64)) + 16 * (lane >> 4) + 8 * (q & 1);
+  }
+  static __device__ __forceinline__ bool v_mine(int lane) { return D > 32 || lane < 32; }
+  static __device__ __forceinline__ int v_row(int lane, int i) { return 4 * ((lane + 64 * i) / (D / 8)); }
+  static __device__ __forceinline__ int v_dim(int lane, int i) { return 8 * ((lane + 64 * i) % (D / 8)); }
+  // the word of rows v_row .. + 3 at dim d
+  static __device__ __forceinline__ int v_word(int row, int d) {
+    return d / 32 * 1024 + (row / 4 % 4 * 16 + d % 16) * 16 + d / 16 % 2 * 8 + row / 16 * 4;
+  }
+};
+
+// The part's elements, row r at row(r), and the bits of the largest magnitude of the lane's.
+template <int D>
+constexpr int kHeld = D == 32 ? 32 : D / 2;  // elements of a lane
+template <typename T, int D, typename Row>
+__device__ __forceinline__ unsigned take_rows(bool values, int lane, Row row, float (&x)[kHeld<D>]) {
+  typedef Part<D> P;
+  if (!values) {
+#pragma unroll
+    for (int q = 0; q < P::KEYS; ++q) load8<T>(row(P::k_row(lane, q)) + P::k_dim(lane, q), x + 8 * q);
+#pragma unroll
+    for (int i = 8 * P::KEYS; i < kHeld<D>; ++i) x[i] = 0.f;
+  } else {
+    const int mine = P::v_mine(lane) ? lane : lane - 32;
+#pragma unroll
+    for (int i = 0; i < P::VALUES; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) load8<T>(row(P::v_row(mine, i) + r) + P::v_dim(mine, i), x + 32 * i + 8 * r);
+  }
+  unsigned most = 0;
+#pragma unroll
+  for (int i = 0; i < kHeld<D>; ++i) most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);
+#pragma unroll
+  for (int o = 32; o; o >>= 1) most = max(most, (unsigned)__shfl_xor((int)most, o));
+  return most;
+}
+// Their codes to the part at dst; lds: Part::BYTES of the wave's own.
+template <int D, int CODE>
+__device__ __forceinline__ void put_codes(bool values, int lane, const float (&x)[kHeld<D>], const Coding& c,
+                                          uint8_t* dst, uint8_t* lds) {
+  typedef Part<D> P;
+  if (!values) {
+#pragma unroll
+    for (int s = 0; s < P::KEYS / 2; ++s) {
+      u32x4 w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = code4<CODE>(x + 16 * s + 4 * i, 1, c);
+      *(u32x4*)(dst + 1024 * s + 16 * lane) = w;
+    }
+    return;
+  }
+  if (P::v_mine(lane)) {
+#pragma unroll
+    for (int i = 0; i < P::VALUES; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        *(unsigned*)(lds + P::v_word(P::v_row(lane, i), P::v_dim(lane, i) + j)) = code4<CODE>(x + 32 * i + j, 8, c);
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int s = 0; s < P::BYTES / 1024; ++s)
+    *(u32x4*)(dst + 1024 * s + 16 * lane) = *(const u32x4*)(lds + 1024 * s + 16 * lane);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+// The values that the part at src stands for, to row(r); the wave's lds as above.
+template <typename T, int D, int CODE, typename Row>
+__device__ __forceinline__ void put_values(bool values, int lane, const uint8_t* src, float scale, Row row,
+                                           uint8_t* lds) {
+  typedef Part<D> P;
+  float x[kHeld<D>];
+  if (!values) {
+#pragma unroll
+    for (int s = 0; s < P::KEYS / 2; ++s) {
+      const u32x4 w = *(const u32x4*)(src + 1024 * s + 16 * lane);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) values4<CODE>(w[i], scale, x + 16 * s + 4 * i, 1);
+    }
+#pragma unroll
+    for (int q = 0; q < P::KEYS; ++q) store8(row(P::k_row(lane, q)) + P::k_dim(lane, q), x + 8 * q);
+    return;
+  }
+#pragma unroll
+  for (int s = 0; s < P::BYTES / 1024; ++s)
+    *(u32x4*)(lds + 1024 * s + 16 * lane) = *(const u32x4*)(src + 1024 * s + 16 * lane);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  if (P::v_mine(lane)) {
+#pragma unroll
+    for (int i = 0; i < P::VALUES; ++i) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        values4<CODE>(*(const unsigned*)(lds + P::v_word(P::v_row(lane, i), P::v_dim(lane, i) + j)), scale,
+                      x + 32 * i + j, 8);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) store8(row(P::v_row(lane, i) + r) + P::v_dim(lane, i), x + 32 * i + 8 * r);
+    }
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// The waves of a workgroup take blocks, page_rows / 32 waves one.  The block's scale comes
+// from all of its rows, so waves of one block meet once.
+template <typename T, int D, int CODE, typename Row>
+__device__ __forceinline__ void code_block(const ssd_page_pool& p, bool there, int64_t block, bool values, Row row,
+                                           uint8_t (*lds)[Part<D>::BYTES], unsigned (&most)[kWaveCount]) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = p.page_rows / 32, part = wave % waves;
+  float x[kHeld<D>];
+  unsigned bits = 0;
+  if (there) bits = take_rows<T, D>(values, lane, [&](int r) { return row(32 * part + r); }, x);
+  if (waves > 1) {
+    if (lane == 0) most[wave] = bits;
+    __syncthreads();
+    for (int w = 0; w < waves; ++w) bits = max(bits, most[wave - part + w]);
+    __syncthreads();
+  }
+  if (!there) return;
+  const Coding c = coding<CODE>(bits);
+  put_codes<D, CODE>(values, lane, x, c, (uint8_t*)p.data + block * block_bytes(p) + part * Part<D>::BYTES, lds[wave]);
+  if (part == 0 && lane == 0) p.scale[block] = c.scale;
+}
+
+// ---------------------------------------------------------------- rows into pages, and back
+
+struct BlockArgs {
+  ssd_page_pool p;
+  ssd_rows_desc d;
+  const int* ids;
+  char *k, *v;
+  int n, first_layer;
+  int64_t blocks;  // 2 (keys, values) for each head, page and layer
+};
+struct BlockAt {
+  int64_t block, rows;  // the block's number in the pool, its rows' first element
+  bool values, there;
+};
+__device__ __forceinline__ BlockAt block_at(const BlockArgs& a, int64_t i) {
+  BlockAt x;
+  x.there = i < a.blocks;
+  if (!x.there) i = 0;
+  x.values = i & 1;
+  i >>= 1;
+  const int g = (int)(i % a.p.n_kv_head);
+  i /= a.p.n_kv_head;
+  const int n = (int)(i % a.n), l = (int)(i / a.n);
+  const int id = a.ids[n];
+  if (id < 0 || id >= a.p.n_page) {
+    x.block = -1;
+  } else {
+    x.block = ((((int64_t)(a.first_layer + l) * a.p.n_page + id) * a.p.n_kv_head + g) << 1) + x.values;
+  }
+  x.rows = l * a.d.layer + n * a.d.seq + g * a.d.head;
+  return x;
+}
+
+// Bound: memory.
+template <typename T, int D, int CODE>
+__global__ __launch_bounds__(kThreads) void store_kernel(BlockArgs a) {
+  __shared__ __align__(16) uint8_t lds[kWaveCount][Part<D>::BYTES];
+  __shared__ unsigned most[kWaveCount];
+  const int waves = a.p.page_rows / 32, units = kWaveCount / waves, unit = (threadIdx.x >> 6) / waves;
+  for (int64_t first = (int64_t)blockIdx.x * units; first < a.blocks; first += (int64_t)gridDim.x * units) {
+    const BlockAt at = block_at(a, first + unit);
+    const T* base = (const T*)(at.values ? a.v : a.k) + at.rows;
+    code_block<T, D, CODE>(a.p, at.there && at.block >= 0, at.block, at.values,
+                           [&](int r) { return base + r * a.d.row; }, lds, most);
+  }
+}
+template <typename T, int D, int CODE>
+__global__ __launch_bounds__(kThreads) void load_kernel(BlockArgs a) {
+  __shared__ __align__(16) uint8_t lds[kWaveCount][Part<D>::BYTES];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = a.p.page_rows / 32, units = kWaveCount / waves,
+            unit = wave / waves, part = wave % waves;
+  for (int64_t first = (int64_t)blockIdx.x * units; first < a.blocks; first += (int64_t)gridDim.x * units) {
+    const BlockAt at = block_at(a, first + unit);
+    if (!at.there) continue;
+    T* base = (T*)(at.values ? a.v : a.k) + at.rows;
+    auto row = [&](int r) { return base + (32 * part + r) * a.d.row; };
+    if (at.block < 0) {
+      const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      for (int q = 0; q < Part<D>::KEYS; ++q) store8(row(Part<D>::k_row(lane, q)) + Part<D>::k_dim(lane, q), zero);
+    } else {
+      put_values<T, D, CODE>(at.values, lane, (const uint8_t*)a.p.data + at.block * block_bytes(a.p) + part * Part<D>::BYTES,
+                             a.p.scale[at.block], row, lds[wave]);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- giving out pages
+
+struct Work {  // the workspace
+  int *head;            // [0]: pages that get full, [1]: pages to move, [2]: pages in use
+  int4* slot;           // [n_seq] (length before, rows appended, pages that get full, whether it is served)
+  int4* jobs;           // [2 n_seq] (slot, column, page, -) of those pages
+  int *a, *b, *to;      // [n_page]
+};
+Work work_at(void* w, int n_seq, int n_page) {
+  Work x;
+  x.head = (int*)w;
+  x.slot = (int4*)(x.head + 16);
+  x.jobs = x.slot + n_seq;
+  x.a = (int*)(x.jobs + 2 * n_seq);
+  x.b = x.a + n_page;
+  x.to = x.b + n_page;
+  return x;
+}
+size_t work_bytes(int n_seq, int n_page) { return 64 + 48 * (size_t)n_seq + 12 * (size_t)n_page; }
+
+// sums over the threads before this one, and over all
+__device__ __forceinline__ long long scan(long long x, long long* sums, long long& all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  long long in = x;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const long long y = __shfl_up(in, o);
+    if (lane >= o) in += y;
+  }
+  if (lane == 63) sums[wave] = in;
+  __syncthreads();
+  long long before = 0;
+  all = 0;
+#pragma unroll
+  for (int w = 0; w < kPlan / 64; ++w) {
+    if (w < wave) before += sums[w];
+    all += sums[w];
+  }
+  __syncthreads();
+  return before + in - x;
+}
+// Writes the first `most` pages p in [from, to) whose refs are as asked to list, in order; how many there
+// are, up to those with which the search ended.
+constexpr int kLook = 16;  // refs a thread looks at
+__device__ __forceinline__ int find_pages(const int* refs, int from, int to, bool in_use, int* list, long long most,
+                                          long long* sums) {
+  long long found = 0;
+  for (int base = from; base < to && found < most; base += kPlan * kLook) {
+    const int at = base + (int)threadIdx.x * kLook;
+    unsigned mask = 0;
+#pragma unroll
+    for (int i = 0; i < kLook; ++i)
+      if (at + i < to && (refs[at + i] > 0) == in_use) mask |= 1u << i;
+    long long all;
+    long long rank = found + scan(__popc(mask), sums, all);
+    for (; mask; mask &= mask - 1, ++rank)
+      if (rank < most) list[rank] = at + __ffs(mask) - 1;
+    found += all;
+  }
+  return (int)found;
+}
+
+struct PlanArgs {
+  ssd_page_seqs s;
+  Work w;
+  int n_page, page_rows;
+  const int* count;           // take
+  int* got;                   // take: pages that a slot got, commit: that got full
+  const int *path, *path_len; // commit
+  int64_t path_ld;
+  int max_path, n_new;
+};
+
+// Which slots get how many pages, and which: one workgroup, since pages are given out in the order of the
+// slots.  Bound: latency, a chain of some ten loads and meetings.
+template <bool COMMIT>
+__global__ __launch_bounds__(kPlan) void plan_kernel(PlanArgs a) {
+  __shared__ int want[4096], first[4096];
+  __shared__ long long sums[kPlan / 64];
+  __shared__ int rows[COMMIT ? 4096 : 1], jobs;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n_seq = a.s.n_seq;
+  if (threadIdx.x == 0) jobs = 0;
+  if constexpr (COMMIT) {
+    for (int b = wave; b < n_seq; b += kPlan / 64) {  // rows up to the path's first that is none
+      const int n = min(a.path_len[b], a.max_path);
+      bool bad = lane >= n;
+      if (!bad) {
+        const int t = a.path[b * a.path_ld + lane];
+        bad = t < 0 || t >= a.n_new;
+      }
+      const unsigned long long bads = __ballot(bad);
+      if (lane == 0) rows[b] = bads ? __ffsll(bads) - 1 : 64;
+    }
+  }
+  __syncthreads();
+  int col[kPer], need[kPer], len[kPer];
+  bool can[kPer];
+  long long sum = 0;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int b = threadIdx.x * kPer + i;
+    can[i] = false;
+    need[i] = col[i] = len[i] = 0;
+    if (b >= n_seq) continue;
+    len[i] = a.s.length[b];
+    if constexpr (COMMIT) {
+      can[i] = len[i] >= 0;
+      col[i] = len[i] / a.page_rows;
+      const int64_t after = ((int64_t)len[i] + rows[b]) / a.page_rows;
+      can[i] = can[i] && after <= a.s.n_col;
+      need[i] = can[i] ? (int)after - col[i] : 0;
+    } else {
+      const int n = a.count[b], from = max(len[i], 0);
+      col[i] = from / a.page_rows;
+      can[i] = n >= 0 && from % a.page_rows == 0 && (int64_t)col[i] + n <= a.s.n_col;
+      need[i] = can[i] ? n : 0;
+    }
+    sum += need[i];
+  }
+  long long all;
+  long long rank = scan(sum, sums, all);
+  long long free = 0;
+  if (all > 0) {
+    free = find_pages(a.s.refs, 0, a.n_page, false, a.w.a, all < a.n_page ? all : a.n_page, sums);
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int b = threadIdx.x * kPer + i;
+    if (b >= n_seq) continue;
+    const bool ok = can[i] && (need[i] == 0 || rank + need[i] <= free);
+    want[b] = ok ? need[i] : 0;
+    first[b] = ok && need[i] ? (int)rank : 0;
+    rank += need[i];
+    if constexpr (COMMIT) {
+      const int n = ok ? rows[b] : 0;
+      a.w.slot[b] = make_int4(len[i], n, want[b], ok);
+      a.got[b] = ok ? need[i] : len[i] < 0 ? 0 : -1;
+      if (n) a.s.length[b] = len[i] + n;
+    } else {
+      a.got[b] = ok ? need[i] : -1;
+      if (ok) a.s.length[b] = max(len[i], 0) + need[i] * a.page_rows;
+    }
+  }
+  __syncthreads();
+  for (int b = wave; b < n_seq; b += kPlan / 64) {
+    const int n = want[b];
+    if (n == 0) continue;
+    const int c = COMMIT ? a.w.slot[b].x / a.page_rows : a.s.length[b] / a.page_rows - n;
+    int job = 0;
+    if (COMMIT && lane == 0) job = atomicAdd(&jobs, n);  // (their order in the list changes no result)
+    job = __shfl(job, 0);
+    for (int j = lane; j < n; j += 64) {
+      const int page = a.w.a[first[b] + j];
+      a.s.table[b * a.s.table_ld + c + j] = page;
+      a.s.refs[page] = 1;
+      if (COMMIT) a.w.jobs[job + j] = make_int4(b, c + j, page, 0);
+    }
+  }
+  if (COMMIT) {
+    __syncthreads();
+    if (threadIdx.x == 0) a.w.head[0] = jobs;
+  }
+}
+
+// ---------------------------------------------------------------- commit
+
+struct CommitArgs {
+  ssd_page_pool p;
+  ssd_page_seqs s;
+  Work w;
+  ssd_rows_desc tail, fresh;
+  char *kt, *vt;
+  const char *kn, *vn;
+  const int* path;
+  int64_t path_ld;
+  int window, sinks;
+  int fill;  // workgroups that fill pages
+};
+
+// items 16 bytes each, of `heads` heads' `rows` rows, four a thread under way: src(head, row), dst(head, row)
+// the row's first byte
+template <typename Src, typename Dst>
+__device__ __forceinline__ void copy_rows(int heads, int rows, int row_bytes, bool rows_outer, Src src, Dst dst) {
+  const int vec = row_bytes / 16, total = heads * rows * vec, inner = rows_outer ? heads : rows;
+  constexpr int U = 4;
+  for (int i0 = threadIdx.x; i0 < total; i0 += U * kThreads) {
+    u32x4 x[U];
+    char* to[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * kThreads;
+      if (i >= total) break;
+      const int v = i % vec, hr = i / vec, in = hr % inner, out = hr / inner;
+      const int h = rows_outer ? in : out, r = rows_outer ? out : in;
+      x[u] = *(const u32x4*)(src(h, r) + 16 * v);
+      to[u] = dst(h, r) + 16 * v;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i0 + u * kThreads < total) *(u32x4*)to[u] = x[u];
+  }
+}
+
+// Workgroups: first `fill` that make the pages that got full, wave by wave; then for each slot one that
+// gives back what is behind the window, and for each layer and keys or values one that moves rows into the tail.
+// (Rows that are moved go to other places of the tail than those of the page: its positions are less
+// than tail_rows apart.)  Bound: memory, and for few rows the launch.
+template <typename T, int D, int CODE>
+__global__ __launch_bounds__(kThreads) void commit_kernel(CommitArgs a) {
+  __shared__ __align__(16) uint8_t lds[kWaveCount][Part<D>::BYTES];
+  __shared__ unsigned most[kWaveCount];
+  const int R0 = a.p.page_rows, G = a.p.n_kv_head;
+  if ((int)blockIdx.x < a.fill) {
+    const int waves = R0 / 32, units = kWaveCount / waves, unit = (threadIdx.x >> 6) / waves;
+    const int64_t blocks = (int64_t)a.w.head[0] * a.p.n_layer * G * 2;
+    for (int64_t at = (int64_t)blockIdx.x * units; at < blocks; at += (int64_t)a.fill * units) {
+      int64_t i = at + unit;
+      const bool there = i < blocks;
+      if (!there) i = 0;
+      const bool values = i & 1;
+      i >>= 1;
+      const int g = (int)(i % G);
+      i /= G;
+      const int l = (int)(i % a.p.n_layer);
+      const int4 job = a.w.jobs[i / a.p.n_layer];
+      const int b = job.x, len = a.w.slot[b].x;
+      const int64_t block = ((((int64_t)l * a.p.n_page + job.z) * G + g) << 1) + values;
+      const T* old = (const T*)(values ? a.vt : a.kt) + l * a.tail.layer + b * a.tail.seq + g * a.tail.head;
+      const T* add = (const T*)(values ? a.vn : a.kn) + l * a.fresh.layer + b * a.fresh.seq + g * a.fresh.head;
+      code_block<T, D, CODE>(
+          a.p, there, block, values,
+          [&](int r) {
+            const int pos = job.y * R0 + r;
+            return pos < len ? old + pos % a.tail.rows * a.tail.row
+                             : add + a.path[b * a.path_ld + pos - len] * a.fresh.row;
+          },
+          lds, most);
+    }
+    return;
+  }
+  const int each = 1 + 2 * a.p.n_layer, at = (int)blockIdx.x - a.fill, b = at / each, part = at % each;
+  const int4 slot = a.w.slot[b];
+  if (part == 0) {
+    if (a.window <= 0 || !slot.w) return;
+    // pages whose rows are all at sinks or behind, and at most length - window
+    const int64_t end = (int64_t)slot.x + slot.y - a.window + 1;
+    const int from = (int)(((int64_t)a.sinks + R0 - 1) / R0), to = (int)min((int64_t)a.s.n_col, end > 0 ? end / R0 : 0);
+    for (int c = from + threadIdx.x; c < to; c += kThreads) {
+      int* entry = a.s.table + b * a.s.table_ld + c;
+      const int page = *entry;
+      if (page < 0) continue;
+      *entry = -1;
+      if (page < a.p.n_page) atomicSub(a.s.refs + page, 1);
+    }
+    return;
+  }
+  const int l = (part - 1) >> 1;
+  const bool values = (part - 1) & 1;
+  // rows behind the last page that got full
+  const int start = max(0, (slot.x / R0 + slot.z) * R0 - slot.x), n = slot.y - start;
+  if (n <= 0) return;
+  char* old = (values ? a.vt : a.kt) + (l * a.tail.layer + b * a.tail.seq) * (int)sizeof(T);
+  const char* add = (values ? a.vn : a.kn) + (l * a.fresh.layer + b * a.fresh.seq) * (int)sizeof(T);
+  const int* path = a.path + b * a.path_ld + start;
+  const int pos = slot.x + start;
+  copy_rows(
+      G, n, D * (int)sizeof(T), true,
+      [&](int g, int r) { return add + (path[r] * a.fresh.row + g * a.fresh.head) * (int)sizeof(T); },
+      [&](int g, int r) { return old + ((pos + r) % a.tail.rows * a.tail.row + g * a.tail.head) * (int)sizeof(T); });
+}
+
+// ---------------------------------------------------------------- fork
+
+struct ForkArgs {
+  ssd_page_seqs s;
+  ssd_rows_desc tail;
+  int n_page, page_rows, n_layer, n_kv_head, row_bytes;
+  const int* parents;
+  char *kt, *vt;
+};
+// blockIdx.y: the slot; blockIdx.x: 0 its table, 1 + 2 l + (keys, values) its open rows in layer l.
+// A slot that is copied from stays as it is, so nothing that is read here is written here.
+__global__ __launch_bounds__(kThreads) void fork_kernel(ForkArgs a) {
+  const int b = blockIdx.y, s = a.parents[b];
+  if (s == b) return;
+  const bool kept = s >= 0 && s < a.s.n_seq && a.parents[s] == s;
+  if (blockIdx.x == 0) {
+    int* mine = a.s.table + b * a.s.table_ld;
+    const int* its = a.s.table + s * a.s.table_ld;
+    for (int c = threadIdx.x; c < a.s.n_col; c += kThreads) {
+      const int old = mine[c], now = kept ? its[c] : -1;
+      if (old == now) continue;
+      mine[c] = now;
+      if (now >= 0 && now < a.n_page) atomicAdd(a.s.refs + now, 1);
+      if (old >= 0 && old < a.n_page) atomicSub(a.s.refs + old, 1);
+    }
+    if (threadIdx.x == 0) a.s.length[b] = kept ? a.s.length[s] : -1;
+    return;
+  }
+  if (!kept) return;
+  const int len = a.s.length[s];
+  if (len <= 0) return;
+  const int n = len % a.page_rows, pos = len - n, l = (blockIdx.x - 1) >> 1, es = a.tail.dtype == SSD_F32 ? 4 : 2;
+  char* base = (blockIdx.x - 1 & 1 ? a.vt : a.kt) + l * a.tail.layer * es;
+  auto at = [&](int slot, int g, int r) {
+    return base + (slot * a.tail.seq + g * a.tail.head + (pos + r) % a.tail.rows * a.tail.row) * es;
+  };
+  copy_rows(a.n_kv_head, n, a.row_bytes, false, [&](int g, int r) { return (const char*)at(s, g, r); },
+            [&](int g, int r) { return at(b, g, r); });
+}
+
+// ---------------------------------------------------------------- compaction
+
+struct CompactArgs {
+  ssd_page_pool p;
+  ssd_page_seqs s;
+  Work w;
+  int* used;
+};
+__global__ __launch_bounds__(kPlan) void compact_plan_kernel(CompactArgs a) {
+  __shared__ long long sums[kPlan / 64];
+  const int n = a.p.n_page;
+  int count = 0;
+  for (int p = threadIdx.x; p < n; p += kPlan) count += a.s.refs[p] > 0;
+  long long all;
+  scan(count, sums, all);
+  const int u = (int)all;
+  const int holes = find_pages(a.s.refs, 0, u, false, a.w.a, n, sums);
+  const int movers = find_pages(a.s.refs, u, n, true, a.w.b, n, sums);  // (as many)
+  for (int p = u + threadIdx.x; p < n; p += kPlan) a.w.to[p] = p;
+  __syncthreads();
+  const int moves = min(holes, movers);
+  for (int i = threadIdx.x; i < moves; i += kPlan) {
+    const int to = a.w.a[i], from = a.w.b[i];
+    a.w.to[from] = to;
+    a.s.refs[to] = a.s.refs[from];
+    a.s.refs[from] = 0;
+  }
+  if (threadIdx.x == 0) {
+    a.w.head[1] = moves;
+    a.w.head[2] = u;
+    *a.used = u;
+  }
+}
+// Moves pages, a piece of one layer's at a time, and names them anew.  Pages come from behind
+// `used` and go before it: no piece is read and written.  Bound: memory.
+constexpr int kPiece = 16384;
+__global__ __launch_bounds__(kThreads) void compact_move_kernel(CompactArgs a) {
+  const int moves = a.w.head[1], used = a.w.head[2], n = a.p.n_page, G = a.p.n_kv_head;
+  const int64_t bytes = (int64_t)G * 2 * block_bytes(a.p);
+  const int pieces = (int)((bytes + kPiece - 1) / kPiece);
+  for (int64_t i = blockIdx.x; i < (int64_t)moves * a.p.n_layer * pieces; i += gridDim.x) {
+    const int piece = (int)(i % pieces);
+    const int64_t lm = i / pieces;
+    const int m = (int)(lm % moves), l = (int)(lm / moves);
+    const int64_t from = (int64_t)l * n + a.w.b[m], to = (int64_t)l * n + a.w.a[m];
+    const int64_t at = (int64_t)piece * kPiece;
+    const char* src = (const char*)a.p.data + from * bytes + at;
+    char* dst = (char*)a.p.data + to * bytes + at;
+    const int vec = (int)(min((int64_t)kPiece, bytes - at) / 16);
+    u32x4 x[kPiece / 16 / kThreads];
+#pragma unroll
+    for (int u = 0; u < kPiece / 16 / kThreads; ++u)
+      if ((int)threadIdx.x + u * kThreads < vec) x[u] = *(const u32x4*)(src + 16 * (threadIdx.x + u * kThreads));
+#pragma unroll
+    for (int u = 0; u < kPiece / 16 / kThreads; ++u)
+      if ((int)threadIdx.x + u * kThreads < vec) *(u32x4*)(dst + 16 * (threadIdx.x + u * kThreads)) = x[u];
+    if (piece == 0)
+      for (int j = threadIdx.x; j < 2 * G; j += kThreads) a.p.scale[to * 2 * G + j] = a.p.scale[from * 2 * G + j];
+  }
+  const int64_t entries = (int64_t)a.s.n_seq * a.s.n_col;
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < entries; i += (int64_t)gridDim.x * kThreads) {
+    int* entry = a.s.table + i / a.s.n_col * a.s.table_ld + i % a.s.n_col;
+    const int page = *entry;
+    if (page >= used && page < n) *entry = a.w.to[page];
+  }
+}
+
+// ---------------------------------------------------------------- host
+
+constexpr int kMostBlocks = 1 << 16;  // workgroups of kernels that take more work than that in turns
+
+template <typename F>
+void by_type(ssd_dtype t, int d, int code, F f) {
+  auto with_code = [&](auto dtype, auto dim) {
+    if (code == SSD_PAGE_INT8) f(dtype, dim, std::integral_constant<int, SSD_PAGE_INT8>{});
+    else f(dtype, dim, std::integral_constant<int, SSD_PAGE_E4M3>{});
+  };
+  auto with_dim = [&](auto dtype) {
+    if (d == 32) with_code(dtype, std::integral_constant<int, 32>{});
+    else if (d == 64) with_code(dtype, std::integral_constant<int, 64>{});
+    else with_code(dtype, std::integral_constant<int, 128>{});
+  };
+  if (t == SSD_F32) with_dim(float{});
+  else with_dim(bf16_t{});
+}
+
+ssd_status blocks_args(const ssd_page_pool* pool, const int32_t* ids, int32_t n, int32_t first_layer, int32_t n_layer,
+                       const ssd_rows_desc* d, const void* k, const void* v, bool written, BlockArgs* a) {
+  ssd_status st = check_pool(pool);
+  if (st != SSD_OK) return st;
+  OP_REQUIRE(n >= 0 && n <= (1 << 24), SSD_E_INVALID_ARG, "n outside [0, 2^24]");
+  OP_REQUIRE(first_layer >= 0 && n_layer >= 0 && (int64_t)first_layer + n_layer <= pool->n_layer, SSD_E_INVALID_ARG,
+             "layers outside the pool's");
+  OP_REQUIRE(d, SSD_E_INVALID_ARG, "null rows");
+  a->p = *pool;
+  a->d = *d;
+  a->ids = ids;
+  a->n = n;
+  a->first_layer = first_layer;
+  a->k = (char*)k;
+  a->v = (char*)v;
+  a->blocks = (int64_t)n_layer * n * pool->n_kv_head * 2;
+  if (a->blocks == 0) return SSD_OK;
+  OP_REQUIRE(ids && (uintptr_t)ids % 4 == 0, SSD_E_INVALID_ARG, "ids is null or not aligned");
+  const RowDim dims[4] = {{n_layer, d->layer}, {n, d->seq}, {pool->n_kv_head, d->head}, {pool->page_rows, d->row}};
+  st = check_rows(d->dtype, dims, pool->head_dim, written, k, v);
+  if (st != SSD_OK) return st;
+  const size_t e = rows_extent(d->dtype, dims, pool->head_dim);
+  const size_t held = (size_t)pool->n_layer * pool->n_page * pool->n_kv_head * 2 * block_bytes(*pool);
+  const size_t scales = (size_t)pool->n_layer * pool->n_page * pool->n_kv_head * 8;
+  OP_REQUIRE(!written || !op_overlap(k, e, v, e), SSD_E_INVALID_ARG, "k and v share memory");
+  for (const void* x : {k, v})
+    OP_REQUIRE(!op_overlap(x, e, pool->data, held) && !op_overlap(x, e, pool->scale, scales) &&
+                   (!written || !op_overlap(x, e, ids, (size_t)n * 4)),
+               SSD_E_INVALID_ARG, "rows share memory with the pool or ids");
+  return SSD_OK;
+}
+
+ssd_status check_work(const ssd_page_pool* pool, const ssd_page_seqs* s, const void* w, size_t bytes) {
+  OP_REQUIRE(w, SSD_E_INVALID_ARG, "null workspace");
+  OP_REQUIRE(bytes >= work_bytes(s->n_seq, pool->n_page) && (uintptr_t)w % 16 == 0, SSD_E_CAPACITY,
+             "workspace below ssd_pages_workspace's bytes or not 16-byte aligned");
+  return SSD_OK;
+}
+
+}  // namespace
+}  // namespace ssd
+
+using namespace ssd;
+
+extern "C" ssd_status ssd_pages_store(const ssd_page_pool* pool, const int32_t* ids, int32_t n, int32_t first_layer,
+                                      int32_t n_layer, const ssd_rows_desc* d, const void* k, const void* v,
+                                      void* stream) {
+  BlockArgs a{};
+  const ssd_status st = blocks_args(pool, ids, n, first_layer, n_layer, d, k, v, false, &a);
+  if (st != SSD_OK || a.blocks == 0) return st;
+  by_type(d->dtype, pool->head_dim, pool->code, [&](auto t, auto dim, auto code) {
+    const int64_t units = kWaveCount / (pool->page_rows / 32), want = (a.blocks + units - 1) / units;
+    store_kernel<decltype(t), dim.value, code.value>
+        <<<(unsigned)std::min<int64_t>(want, kMostBlocks), kThreads, 0, (hipStream_t)stream>>>(a);
+  });
+  OP_LAUNCHED();
+  return SSD_OK;
+}
+
+extern "C" ssd_status ssd_pages_load(const ssd_page_pool* pool, const int32_t* ids, int32_t n, int32_t first_layer,
+                                     int32_t n_layer, const ssd_rows_desc* d, void* k, void* v, void* stream) {
+  BlockArgs a{};
+  const ssd_status st = blocks_args(pool, ids, n, first_layer, n_layer, d, k, v, true, &a);
+  if (st != SSD_OK || a.blocks == 0) return st;
+  by_type(d->dtype, pool->head_dim, pool->code, [&](auto t, auto dim, auto code) {
+    const int64_t units = kWaveCount / (pool->page_rows / 32), want = (a.blocks + units - 1) / units;
+    load_kernel<decltype(t), dim.value, code.value>
+        <<<(unsigned)std::min<int64_t>(want, kMostBlocks), kThreads, 0, (hipStream_t)stream>>>(a);
+  });
+  OP_LAUNCHED();
+  return SSD_OK;
+}
+
+extern "C" ssd_status ssd_pages_workspace(const ssd_page_pool* pool, const ssd_page_seqs* seqs, size_t* bytes) {
+  OP_REQUIRE(bytes, SSD_E_INVALID_ARG, "null argument");
+  ssd_status st = check_pool(pool);
+  if (st == SSD_OK) st = check_seqs(seqs, pool->page_rows, true);
+  if (st != SSD_OK) return st;
+  *bytes = work_bytes(seqs->n_seq, pool->n_page);
+  return SSD_OK;
+}
+
+extern "C" ssd_status ssd_pages_take(const ssd_page_pool* pool, const ssd_page_seqs* seqs, const int32_t* count,
+                                     int32_t* got, void* workspace, size_t workspace_bytes, void* stream) {
+  ssd_status st = check_pool(pool);
+  if (st == SSD_OK) st = check_seqs(seqs, pool->page_rows, true);
+  if (st == SSD_OK) st = check_work(pool, seqs, workspace, workspace_bytes);
+  if (st != SSD_OK) return st;
+  OP_REQUIRE(count && got && (uintptr_t)count % 4 == 0 && (uintptr_t)got % 4 == 0, SSD_E_INVALID_ARG,
+             "count or got is null or not aligned");
+  PlanArgs a{};
+  a.s = *seqs;
+  a.w = work_at(workspace, seqs->n_seq, pool->n_page);
+  a.n_page = pool->n_page;
+  a.page_rows = pool->page_rows;
+  a.count = count;
+  a.got = got;
+  plan_kernel<false><<<1, kPlan, 0, (hipStream_t)stream>>>(a);
+  OP_LAUNCHED();
+  return SSD_OK;
+}
+
+extern "C" ssd_status ssd_pages_commit(const ssd_page_pool* pool, const ssd_page_seqs* seqs, const ssd_rows_desc* tail,
+                                       void* k_tail, void* v_tail, const ssd_rows_desc* fresh, const void* k_new,
+                                       const void* v_new, const int32_t* path, int64_t path_ld, int32_t max_path,
+                                       const int32_t* path_len, int32_t window, int32_t sinks, int32_t* full,
+                                       void* workspace, size_t workspace_bytes, void* stream) {
+  ssd_status st = check_pool(pool);
+  if (st == SSD_OK) st = check_seqs(seqs, pool->page_rows, true);
+  if (st == SSD_OK) st = check_work(pool, seqs, workspace, workspace_bytes);
+  if (st != SSD_OK) return st;
+  OP_REQUIRE(tail && fresh, SSD_E_INVALID_ARG, "null rows");
+  OP_REQUIRE(tail->dtype == fresh->dtype, SSD_E_INVALID_ARG, "the tail and the new rows have two types");
+  OP_REQUIRE(fresh->rows >= 1 && fresh->rows <= 64, SSD_E_INVALID_ARG, "new rows outside [1, 64]");
+  OP_REQUIRE(tail->rows >= pool->page_rows + fresh->rows - 1 && tail->rows < (1 << 30), SSD_E_INVALID_ARG,
+             "tail rows below page_rows + new rows - 1, or 2^30");
+  OP_REQUIRE(max_path >= 0 && max_path <= 64 && (seqs->n_seq == 1 || path_ld >= max_path), SSD_E_INVALID_ARG,
+             "max_path outside [0, 64], or path_ld below it");
+  OP_REQUIRE(window >= 0 && sinks >= 0, SSD_E_INVALID_ARG, "window or sinks is negative");
+  OP_REQUIRE((path || max_path == 0) && path_len && full && (uintptr_t)path % 4 == 0 && (uintptr_t)path_len % 4 == 0 &&
+                 (uintptr_t)full % 4 == 0,
+             SSD_E_INVALID_ARG, "path, path_len or full is null or not aligned");
+  const RowDim td[4] = {{pool->n_layer, tail->layer}, {seqs->n_seq, tail->seq}, {pool->n_kv_head, tail->head},
+                        {tail->rows, tail->row}};
+  const RowDim nd[4] = {{pool->n_layer, fresh->layer}, {seqs->n_seq, fresh->seq}, {pool->n_kv_head, fresh->head},
+                        {fresh->rows, fresh->row}};
+  st = check_rows(tail->dtype, td, pool->head_dim, true, k_tail, v_tail);
+  if (st == SSD_OK) st = check_rows(fresh->dtype, nd, pool->head_dim, false, k_new, v_new);
+  if (st != SSD_OK) return st;
+  const size_t te = rows_extent(tail->dtype, td, pool->head_dim), ne = rows_extent(fresh->dtype, nd, pool->head_dim);
+  OP_REQUIRE(!op_overlap(k_tail, te, v_tail, te), SSD_E_INVALID_ARG, "the tail's keys and values share memory");
+  for (const void* t : {(const void*)k_tail, (const void*)v_tail})
+    for (const void* x : {k_new, v_new})
+      OP_REQUIRE(!op_overlap(t, te, x, ne), SSD_E_INVALID_ARG, "the tail shares memory with the new rows");
+  const Work w = work_at(workspace, seqs->n_seq, pool->n_page);
+  PlanArgs p{};
+  p.s = *seqs;
+  p.w = w;
+  p.n_page = pool->n_page;
+  p.page_rows = pool->page_rows;
+  p.got = full;
+  p.path = path;
+  p.path_len = path_len;
+  p.path_ld = path_ld;
+  p.max_path = max_path;
+  p.n_new = fresh->rows;
+  plan_kernel<true><<<1, kPlan, 0, (hipStream_t)stream>>>(p);
+  OP_LAUNCHED();
+  CommitArgs a{};
+  a.p = *pool;
+  a.s = *seqs;
+  a.w = w;
+  a.tail = *tail;
+  a.fresh = *fresh;
+  a.kt = (char*)k_tail;
+  a.vt = (char*)v_tail;
+  a.kn = (const char*)k_new;
+  a.vn = (const char*)v_new;
+  a.path = path;
+  a.path_ld = path_ld;
+  a.window = window;
+  a.sinks = sinks;
+  const int units = kWaveCount / (pool->page_rows / 32);
+  a.fill = (int)std::min<int64_t>(((int64_t)seqs->n_seq * pool->n_layer * pool->n_kv_head * 2 + units - 1) / units, 1024);
+  const int64_t blocks = a.fill + (int64_t)seqs->n_seq * (1 + 2 * pool->n_layer);
+  OP_REQUIRE(blocks < (1 << 24), SSD_E_CAPACITY, "more workgroups than a grid holds");
+  by_type(tail->dtype, pool->head_dim, pool->code, [&](auto t, auto dim, auto code) {
+    commit_kernel<decltype(t), dim.value, code.value><<<(unsigned)blocks, kThreads, 0, (hipStream_t)stream>>>(a);
+  });
+  OP_LAUNCHED();
+  return SSD_OK;
+}
+
+extern "C" ssd_status ssd_pages_fork(const ssd_page_seqs* seqs, int32_t n_page, int32_t page_rows,
+                                     const int32_t* parents, const ssd_rows_desc* tail, int32_t n_layer,
+                                     int32_t n_kv_head, int32_t head_dim, void* k_tail, void* v_tail, void* stream) {
+  OP_REQUIRE(n_page >= 1 && n_page <= kMaxPages, SSD_E_INVALID_ARG, "n_page outside [1, 2^20]");
+  OP_REQUIRE(page_rows == 32 || page_rows == 64 || page_rows == 128, SSD_E_UNSUPPORTED,
+             "page_rows must be 32, 64 or 128");
+  OP_REQUIRE(head_dim == 32 || head_dim == 64 || head_dim == 128, SSD_E_UNSUPPORTED, "head_dim must be 32, 64 or 128");
+  OP_REQUIRE(n_layer >= 1 && n_layer <= 4096 && n_kv_head >= 1 && n_kv_head <= 1024, SSD_E_INVALID_ARG,
+             "n_layer outside [1, 4096] or n_kv_head outside [1, 1024]");
+  ssd_status st = check_seqs(seqs, page_rows, true);
+  if (st != SSD_OK) return st;
+  OP_REQUIRE(parents && (uintptr_t)parents % 4 == 0, SSD_E_INVALID_ARG, "parents is null or not aligned");
+  OP_REQUIRE(tail, SSD_E_INVALID_ARG, "null rows");
+  OP_REQUIRE(tail->rows >= page_rows && tail->rows < (1 << 30), SSD_E_INVALID_ARG, "tail rows below page_rows, or 2^30");
+  const RowDim td[4] = {{n_layer, tail->layer}, {seqs->n_seq, tail->seq}, {n_kv_head, tail->head}, {tail->rows, tail->row}};
+  st = check_rows(tail->dtype, td, head_dim, true, k_tail, v_tail);
+  if (st != SSD_OK) return st;
+  const size_t te = rows_extent(tail->dtype, td, head_dim);
+  OP_REQUIRE(!op_overlap(k_tail, te, v_tail, te), SSD_E_INVALID_ARG, "the tail's keys and values share memory");
+  ForkArgs a{};
+  a.s = *seqs;
+  a.tail = *tail;
+  a.n_page = n_page;
+  a.page_rows = page_rows;
+  a.n_layer = n_layer;
+  a.n_kv_head = n_kv_head;
+  a.row_bytes = head_dim * op_size(tail->dtype);
+  a.parents = parents;
+  a.kt = (char*)k_tail;
+  a.vt = (char*)v_tail;
+  fork_kernel<<<dim3(1 + 2 * n_layer, seqs->n_seq), kThreads, 0, (hipStream_t)stream>>>(a);
+  OP_LAUNCHED();
+  return SSD_OK;
+}
+
+extern "C" ssd_status ssd_pages_compact(const ssd_page_pool* pool, const ssd_page_seqs* seqs, int32_t* used,
+                                        void* workspace, size_t workspace_bytes, void* stream) {
+  ssd_status st = check_pool(pool);
+  if (st == SSD_OK) st = check_seqs(seqs, pool->page_rows, true);
+  if (st == SSD_OK) st = check_work(pool, seqs, workspace, workspace_bytes);
+  if (st != SSD_OK) return st;
+  OP_REQUIRE(used && (uintptr_t)used % 4 == 0, SSD_E_INVALID_ARG, "used is null or not aligned");
+  CompactArgs a{};
+  a.p = *pool;
+  a.s = *seqs;
+  a.w = work_at(workspace, seqs->n_seq, pool->n_page);
+  a.used = used;
+  compact_plan_kernel<<<1, kPlan, 0, (hipStream_t)stream>>>(a);
+  OP_LAUNCHED();
+  compact_move_kernel<<<2048, kThreads, 0, (hipStream_t)stream>>>(a);
+  OP_LAUNCHED();
+  return SSD_OK;
+}
