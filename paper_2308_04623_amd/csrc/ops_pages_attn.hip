@@ -15,6 +15,7 @@
 // parts of 11 bits: bfloat16's 8 bits are one, float32's 24 three.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "ops_pages.h"
 
@@ -26,6 +27,7 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kWaves = 4;
+constexpr float kFar = 4194304.f;
 constexpr float kSlack = 8.f;  // how far a score may lie above the reference before the sums are rescaled
 
 struct Args {
@@ -39,9 +41,12 @@ struct Args {
   const int64_t* anc;
   char* out;
   float* lse;
-  float* o;    // [query][splits][head_dim], query = (sequence, new row, head)
-  float2* ml;  // [query][splits] (m, l)
-  int tiles, splits;
+  float* o;    // [part][tile][query of the tile][head_dim]
+  float2* ml;  // [part][tile][query of the tile] (m, l)
+  int tiles, cols, owners;
+  int parts;     // that there is room for
+  int splits;    // parts of every sequence, 0: see find_part()
+  int round;     // workgroups that those are cut for
   float scale2;  // scale log2 e
 };
 
@@ -92,126 +97,285 @@ __device__ __forceinline__ float group_max(float x) {  // over the lanes of a co
   x = fmaxf(x, __shfl_xor(x, 16));
   return fmaxf(x, __shfl_xor(x, 32));
 }
-
 // a block's bytes of 32 rows: of keys and of values, 16 a lane each
 template <int D>
 struct Codes {
   u32x4 k[D / 32], v[D / 32];
+  // (read once: they pass by the caches)
   __device__ __forceinline__ void load(const uint8_t* keys, const uint8_t* values, int lane) {
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) k[i] = *(const u32x4*)(keys + 1024 * i + 16 * lane);
+    for (int i = 0; i < D / 32; ++i) k[i] = __builtin_nontemporal_load((const u32x4*)(keys + 1024 * i + 16 * lane));
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) v[i] = *(const u32x4*)(values + 1024 * i + 16 * lane);
+    for (int i = 0; i < D / 32; ++i) v[i] = __builtin_nontemporal_load((const u32x4*)(values + 1024 * i + 16 * lane));
+  }
+  // bytes of step st of the product of keys 16 k .. + 15
+  template <int CODE>
+  __device__ __forceinline__ f16x8 keys(int k_, int st) const {
+    const int i = D == 32 ? 0 : k_ * (D / 64) + (st >> 1), h = D == 32 ? k_ : st & 1;
+    return codes8<CODE>(k[i][2 * h], k[i][2 * h + 1]);
+  }
+  // of dims 16 dt .. + 15
+  template <int CODE>
+  __device__ __forceinline__ f16x8 values(int dt) const {
+    return codes8<CODE>(v[dt >> 1][2 * (dt & 1)], v[dt >> 1][2 * (dt & 1) + 1]);
   }
 };
 
-// A wave's queries and results.  Lane 16 g + n has column n of every tile: of scores the rows 4 g + r
-// of 16, of outputs the dims 4 g + r of 16.
-template <typename T, int D, int CODE, int NT>
-struct Wave {
+// What a wave knows of its call, whichever way it takes its queries.  Lane 16 g + n.
+template <typename T, int D, int CODE_>
+struct Base {
+  typedef T Type;
   static constexpr bool F32 = sizeof(T) == 4;
-  static constexpr int NQ = F32 ? 3 : 1, NP = F32 ? 2 : 1, KS = D / 32, DT = D / 16;
+  static constexpr int CODE = CODE_, DIM = D, KS = D / 32, DT = D / 16;
+  static constexpr int NQ = F32 ? 3 : 1, NP = F32 ? 2 : 1;  // parts of a query, of a weight
   const Args& a;
   const int lane, g, n;
-  f16x8 q[NT][KS][NQ];
-  float unit[NT];   // of a product of queries and codes: scale2 and the query's power of two
-  f32x4 o[NT][DT];
-  float m[NT], sub[NT], l[NT];  // reference, what is subtracted (0 for -infinity), this lane's share of the sum
-  float vunit;                  // o is in units of this power of two
-  int seen_from[NT];            // cached rows from here on, and sinks, are seen
-  uint64_t anc[NT];             // new rows that are seen
-  int64_t at[NT];               // the query's first element, -1: none
+  float vunit, vrel;  // o is in units of this power of two; 0: of 1, no page was taken yet; 1 / vunit
+  bool own;           // rows in the model's type were taken
+  bool rounded;       // a reference is far from 0: see weights()
 
-  __device__ __forceinline__ Wave(const Args& args)
-      : a(args), lane(threadIdx.x & 63), g(lane >> 4), n(lane & 15), vunit(0.f) {}
+  __device__ __forceinline__ Base(const Args& args)
+      : a(args), lane(threadIdx.x & 63), g(lane >> 4), n(lane & 15), vunit(0.f), vrel(1.f), own(false), rounded(false) {}
 
   // the 8 dims from here on are what the lane has in step s of a product over dims
   __device__ __forceinline__ int dim_at(int s) const { return D == 32 ? 8 * g : 64 * (s >> 1) + 16 * g + 8 * (s & 1); }
 
-  __device__ __forceinline__ void load(int b, int kv, int tile, int len) {
+  // a query, as it is: its loads are under way when issue() returns
+  struct Query {
+    u32x4 x[KS][F32 ? 2 : 1];
+    int64_t anc;
+    int step;  // its new row, -1: none
+  };
+  __device__ __forceinline__ void issue(Query& q, int b, int kv, int c) {
     const int group = a.d.n_head / a.n_kv_head, cols = a.d.n_query * group;
+    const int t = group == 1 ? c : c / group;
+    q.step = c < cols ? t : -1;
+    const T* p = (const T*)a.q + (c < cols ? b * a.d.q_seq + t * a.d.q_row + (kv * group + c - t * group) * a.d.q_head : 0);
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const int c = (tile * NT + nt) * 16 + n, t = c / group;
-      const bool live = c < cols;
-      at[nt] = live ? b * a.d.q_seq + t * a.d.q_row + (kv * group + c % group) * a.d.q_head : -1;
-      float x[KS][8], top = 0.f;
+    for (int s = 0; s < KS; ++s)
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const T* p = (const T*)a.q + (live ? at[nt] : 0) + dim_at(s);
-        if constexpr (F32) {
-          const f32x4 u = *(const f32x4*)p, v = *(const f32x4*)(p + 4);
+      for (int i = 0; i < (F32 ? 2 : 1); ++i) q.x[s][i] = *(const u32x4*)(p + dim_at(s) + 4 * i);
+    q.anc = a.anc ? a.anc[(int64_t)b * a.d.n_query + max(q.step, 0)] : 0;
+  }
+  // what it sees
+  __device__ __forceinline__ void sees(const Query& q, int len, uint64_t& anc, int& seen_from) const {
+    const int t = q.step;
+    anc = t >= 63 ? ~0ull : (2ull << max(t, 0)) - 1;
+    if (a.anc) anc = (uint64_t)q.anc & (~0ull >> (64 - a.d.n_query));
+    const int depth = a.anc ? max(__popcll(anc) - 1, 0) : max(t, 0);
+    seen_from = a.d.window ? len + depth - a.d.window + 1 : 0;
+  }
+  // its parts for products with codes, and what such a product is multiplied by
+  __device__ __forceinline__ void split(const Query& q, f16x8 (&parts)[KS][NQ], float& unit) const {
+    float x[KS][8], top = 0.f;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[s][i] = u[i], x[s][4 + i] = v[i];
-        } else {
-          const u32x4 u = *(const u32x4*)p;
+    for (int s = 0; s < KS; ++s)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            x[s][2 * i] = __uint_as_float(u[i] << 16);
-            x[s][2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[s][i]));
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (F32) x[s][i] = __uint_as_float(q.x[s][i >> 2][i & 3]);
+        else x[s][i] = __uint_as_float(i & 1 ? q.x[s][0][i >> 1] & 0xffff0000u : q.x[s][0][i >> 1] << 16);
+        top = fmaxf(top, fabsf(x[s][i]));
       }
-      top = group_max(top);
-      // the largest to [2^14, 2^15): what is smaller by up to 2^28 keeps its 11 bits
-      const int e = top < __builtin_inff() ? max((int)(__float_as_uint(top) >> 23) - 127, -100) : 14;
-      const float by = __uint_as_float((unsigned)(min(14 - e, 127) + 127) << 23);
-      unit[nt] = a.scale2 * __uint_as_float((unsigned)(max(e - 14, -126) + 127) << 23);
+    top = group_max(top);
+    // the largest to [2^14, 2^15): what is smaller by up to 2^28 keeps its 11 bits
+    const int e = top < __builtin_inff() ? max((int)(__float_as_uint(top) >> 23) - 127, -100) : 14;
+    const float by = __uint_as_float((unsigned)(min(14 - e, 127) + 127) << 23);
+    unit = fabsf(a.scale2) * __uint_as_float((unsigned)(max(e - 14, -126) + 127) << 23);
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float y = q.step < 0 ? 0.f : x[s][i] * (a.scale2 < 0.f ? -by : by);
+#pragma unroll
+        for (int p = 0; p < NQ; ++p) {
+          parts[s][p][i] = (_Float16)y;
+          y -= (float)parts[s][p][i];
+        }
+      }
+  }
+
+  // The unit of o for values of this scale: whether o has to be multiplied by f.  Weights up to 2^15 are what float16
+  // holds to 2^-32 of the largest there can be.  (Sums of rows in the model's type are far from the largest number: a
+  // unit of 2^-64 at the least.)
+  __device__ __forceinline__ bool new_unit(float size, float& f) {
+    if (!((size > vunit * 0x1p7f || vunit == 0.f) && size > 0.f && size < __builtin_inff())) return false;
+    const unsigned up = (__float_as_uint(size) + 0x7fffffu) & 0x7f800000u;  // the next power of two
+    const unsigned now = max(min(max(up, 9u << 23), 253u << 23) - (7u << 23), own ? 63u << 23 : 0u);
+    const float to = __uint_as_float((254u << 23) - now);
+    f = vunit == 0.f ? to : vunit * to;
+    vunit = __uint_as_float(now);
+    vrel = to;
+    return true;
+  }
+
+  // 32 rows in the model's type: those from x0 on of `tail` open rows, the first at place `slot` of the ring, and of
+  // the new ones behind them; rows past the last are the last again.  Lane (g, n): row 16 k + n of the keys, rows
+  // 16 (i / 4) + 4 g + i mod 4 of the values at dims 16 dt + n.  Loads are under way when issue_own() returns.
+  struct Own {
+    u32x4 k[2][KS][F32 ? 2 : 1];
+    typename std::conditional<F32, float, uint16_t>::type v[DT][8];
+  };
+  template <bool KEYS, bool VALUES>
+  __device__ __forceinline__ void issue_own(Own& rows, int b, int kv, int x0, int tail, int slot) {
+    const int total = tail + a.d.n_query;
+    const int64_t told = b * a.d.tail_seq + kv * a.d.tail_head, tnew = b * a.d.new_seq + kv * a.d.new_head;
+    auto row = [&](const char* old, const char* add, int x) {
+      x = min(x, total - 1);
+      const bool open = x < tail;
+      const int at = slot + x, place = open ? at - (at >= a.d.tail_rows ? a.d.tail_rows : 0) : x - tail;
+      return (const T*)(open ? old : add) + (open ? told : tnew) + place * (open ? a.d.tail_row : a.d.new_row);
+    };
+#pragma unroll
+    for (int k = 0; KEYS && k < 2; ++k) {
+      const T* p = row(a.kt, a.kn, x0 + 16 * k + n);
 #pragma unroll
       for (int s = 0; s < KS; ++s)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          float y = live ? x[s][i] * by : 0.f;
+        for (int i = 0; i < (F32 ? 2 : 1); ++i) rows.k[k][s][i] = *(const u32x4*)(p + dim_at(s) + 4 * i);
+    }
 #pragma unroll
-          for (int p = 0; p < NQ; ++p) {
-            q[nt][s][p][i] = (_Float16)y;
-            y -= (float)q[nt][s][p][i];
-          }
+    for (int i = 0; VALUES && i < 8; ++i) {
+      const T* p = row(a.vt, a.vn, x0 + 16 * (i >> 2) + 4 * g + (i & 3)) + n;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+        rows.v[dt][i] = __builtin_bit_cast(typename std::conditional<F32, float, uint16_t>::type, p[16 * dt]);
+    }
+  }
+  // products over dims of keys 16 k .. and a query
+  __device__ __forceinline__ f32x4 own_scores(const Own& rows, int k, const Query& q) {
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      if constexpr (F32) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float x = __uint_as_float(rows.k[k][s][i >> 2][i & 3]), y = __uint_as_float(q.x[s][i >> 2][i & 3]);
+          sum = product(x, y, sum);
         }
+      } else {
+        const bf16x8 x = __builtin_bit_cast(bf16x8, rows.k[k][s][0]), y = __builtin_bit_cast(bf16x8, q.x[s][0]);
+        sum = product(x, y, sum);
+      }
+    }
+    return sum;
+  }
+  __device__ __forceinline__ bool sees_own(int x, int tail, int start, int seen_from, uint64_t anc) const {
+    if (x < tail) return start + x >= seen_from || start + x < a.d.sinks;
+    return x < tail + a.d.n_query && (anc >> (x - tail & 63) & 1);
+  }
+  static __device__ __forceinline__ bool finite(float x) { return fabsf(x) < __builtin_inff(); }
+  static __device__ __forceinline__ bool finite(uint16_t x) { return (x & 0x7f80u) != 0x7f80u; }
+  __device__ __forceinline__ bool all_finite(const Own& rows) const {
+    bool odd = false;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) odd |= !finite(rows.v[dt][i]);
+    return !__builtin_amdgcn_ballot_w64(odd);
+  }
+  // which of a dim's values are not finite, as 1; they become 0
+  __device__ __forceinline__ bf16x8 take_out(Own& rows, int dt) const {
+    bf16x8 y;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const bool bad = !finite(rows.v[dt][i]);
+      y[i] = (__bf16)(bad ? 1.f : 0.f);
+      if (bad) rows.v[dt][i] = 0;
+    }
+    return y;
+  }
+};
+
+// Up to 16 NT queries as the columns of products with keys and with values: lane 16 g + n has query n of every tile,
+// of scores the rows 4 g + r of 16, of outputs the dims 4 g + r of 16.
+template <typename T, int D, int CODE, int NT_>
+struct Tiles : Base<T, D, CODE> {
+  typedef Base<T, D, CODE> B;
+  using typename B::Own;
+  using B::a, B::g, B::n, B::lane, B::vunit, B::vrel, B::KS, B::DT, B::NQ, B::NP, B::F32;
+  static constexpr int NT = NT_, COLS = 16 * NT;
+  static constexpr bool EARLY = !(D == 128 && (F32 || NT == 2)) && !(F32 && D == 64 && NT == 2);  // see take_own()
+  typename B::Query raw[NT];
+  f16x8 q[NT][KS][NQ];
+  float unit[NT];
+  f32x4 o[NT][DT];
+  float m[NT], sub[NT], l[NT];  // reference, what is subtracted (0 for -infinity), this lane's share of the sum
+  int seen_from[NT];
+  uint64_t anc[NT];
+
+  __device__ __forceinline__ Tiles(const Args& args) : B(args) {}
+  __device__ __forceinline__ void issue(int b, int kv, int tile) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) B::issue(raw[nt], b, kv, (tile * NT + nt) * 16 + n);
+  }
+  __device__ __forceinline__ void begin(int len) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      B::sees(raw[nt], len, anc[nt], seen_from[nt]);
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) o[nt][dt] = (f32x4){0.f, 0.f, 0.f, 0.f};
       m[nt] = -INFINITY;
       sub[nt] = l[nt] = 0.f;
-      anc[nt] = t >= 63 ? ~0ull : (2ull << t) - 1;
-      if (a.anc && live) anc[nt] = (uint64_t)a.anc[(int64_t)b * a.d.n_query + t] & (~0ull >> (64 - a.d.n_query));
-      const int depth = a.anc ? max(__popcll(anc[nt]) - 1, 0) : t;
-      seen_from[nt] = a.d.window ? len + depth - a.d.window + 1 : 0;
     }
   }
+  __device__ __forceinline__ void split() {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) B::split(raw[nt], q[nt], unit[nt]);
+  }
+  __device__ __forceinline__ void scale_o(float f) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[nt][dt] *= f;
+  }
 
-  // x = s unit, masked, in the reference's units; sums rescaled where a score is far above it
+  // s becomes 2^(s by - reference), by >= 0, and 0 where `masked` and not seen(tile, k, r): row 16 k + 4 g + r; the sums are rescaled where a score is far above the reference.  Product
+  // and difference are one operation; from references of 2^22 on, where their rounding counts, they are two.
   template <typename Seen>
-  __device__ __forceinline__ void weights(f32x4 (&s)[NT][2], const float (&by)[NT], bool masked, Seen seen) {
+  __device__ __forceinline__ void weights(f32x4 (&s)[NT][2], float (&by)[NT], bool masked, Seen seen) {
 #pragma clang fp contract(off)
     bool far = false;
     float top[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-      for (int k = 0; k < 2; ++k) s[nt][k] *= by[nt];
       if (masked) {
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (!seen(nt, 16 * k + 4 * g + r)) s[nt][k][r] = -INFINITY;
+            s[nt][k][r] = seen(nt, k, r) ? s[nt][k][r] * by[nt] : -INFINITY;
+        by[nt] = 1.f;
       }
-      top[nt] = fmaxf(fmaxf(fmaxf(s[nt][0][0], s[nt][0][1]), fmaxf(s[nt][0][2], s[nt][0][3])),
-                      fmaxf(fmaxf(s[nt][1][0], s[nt][1][1]), fmaxf(s[nt][1][2], s[nt][1][3])));
+      top[nt] = by[nt] * fmaxf(fmaxf(fmaxf(s[nt][0][0], s[nt][0][1]), fmaxf(s[nt][0][2], s[nt][0][3])),
+                               fmaxf(fmaxf(s[nt][1][0], s[nt][1][1]), fmaxf(s[nt][1][2], s[nt][1][3])));
       far |= top[nt] > m[nt] + kSlack;
     }
     if (__builtin_amdgcn_ballot_w64(far)) {
+      bool large = false;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const float now = fmaxf(m[nt], group_max(top[nt]));
-        const float by = m[nt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[nt] - now);
+        const float f = m[nt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[nt] - now);
         m[nt] = now;
         sub[nt] = now == -INFINITY ? 0.f : now;
-        l[nt] *= by;
+        large |= fabsf(sub[nt]) >= kFar;
+        l[nt] *= f;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) o[nt][dt] *= by;
+        for (int dt = 0; dt < DT; ++dt) o[nt][dt] *= f;
+      }
+      if (__builtin_amdgcn_ballot_w64(large)) this->rounded = true;
+    }
+    if (this->rounded) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            s[nt][k][r] *= by[nt];
+            asm volatile("" : "+v"(s[nt][k][r]));  // (not to be made one operation with what follows)
+          }
+        by[nt] = 1.f;
       }
     }
 #pragma unroll
@@ -219,57 +383,59 @@ struct Wave {
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) s[nt][k][r] = __builtin_amdgcn_exp2f(s[nt][k][r] - sub[nt]);
+        for (int r = 0; r < 4; ++r) s[nt][k][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[nt][k][r], by[nt], -sub[nt]));
       l[nt] += ((s[nt][0][0] + s[nt][0][1]) + (s[nt][0][2] + s[nt][0][3])) +
                ((s[nt][1][0] + s[nt][1][1]) + (s[nt][1][2] + s[nt][1][3]));
     }
   }
 
-  // 32 rows of a page; first: the position of the first; rows: their number that count
+  // 32 rows of a page, the first at position `first`
   __device__ __forceinline__ void take(const Codes<D>& c, float kscale, float vscale, int first, bool masked) {
     f32x4 s[NT][2];
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
+    for (int k = 0; k < 2; ++k) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) s[nt][k] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
-#pragma unroll
       for (int st = 0; st < KS; ++st) {
-        // (bytes of step st of rows 16 k ..: see the order of keys)
-        const int i = D == 32 ? 0 : k * (D / 64) + (st >> 1), h = D == 32 ? k : st & 1;
-        const f16x8 x = codes8<CODE>(c.k[i][2 * h], c.k[i][2 * h + 1]);
+        const f16x8 y = c.template keys<CODE>(k, st);
 #pragma unroll
         for (int p = NQ - 1; p >= 0; --p)
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) s[nt][k] = product(x, q[nt][st][p], s[nt][k]);
+          for (int nt = 0; nt < NT; ++nt) s[nt][k] = product(y, q[nt][st][p], s[nt][k]);
       }
+    }
     complete<2 * NT>(&s[0][0]);
+    if (kscale < 0.f) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) s[nt][0] = -s[nt][0], s[nt][1] = -s[nt][1];
+    }
     float by[NT];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) by[nt] = kscale * unit[nt];
+    for (int nt = 0; nt < NT; ++nt) by[nt] = fabsf(kscale) * unit[nt];
     const int sinks = a.d.sinks;
-    weights(s, by, masked, [&](int nt, int j) { return first + j >= seen_from[nt] || first + j < sinks; });
-    // weights in units of the values' scale, and up to 2^15: float16 holds them to 2^-32 of the largest there can be
-    const float size = fabsf(vscale);
-    if (size > vunit * 0x1p7f && size < __builtin_inff()) {
-      const unsigned up = (__float_as_uint(size) + 0x7fffffu) & 0x7f800000u;  // the next power of two
-      const float now = fmaxf(fminf(__uint_as_float(up), 0x1p127f) * 0x1p-7f, 0x1p-126f);
-      const float f = vunit / now;
+    int mine = first + 4 * g;
+    if (masked) asm volatile("" : "+v"(mine));  // (not to be taken out of the condition, in eight registers)
+    weights(s, by, masked, [&](int nt, int k, int r) {
+      return mine + 16 * k + r >= seen_from[nt] || mine + 16 * k + r < sinks;
+    });
+    float f;
+    if (B::new_unit(fabsf(vscale), f)) scale_o(f);
+    float rel = vscale * vrel;
+    if (masked && !(fabsf(rel) < __builtin_inff())) {  // rows that a query does not see count 0 whatever the scale
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) o[nt][dt] *= f;
-      vunit = now;
+        for (int i = 0; i < 8; ++i)
+          if (s[nt][i >> 2][i & 3] != 0.f) s[nt][i >> 2][i & 3] = __builtin_nanf("");
+      rel = 1.f;
     }
-    const float rel = vunit > 0.f ? vscale / vunit : vscale;
     f16x8 w[NT][NP];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         float y = s[nt][i >> 2][i & 3] * rel;
-        if (masked) y = s[nt][i >> 2][i & 3] == 0.f ? 0.f : y;  // (whatever the scale)
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
           w[nt][p][i] = (_Float16)y;
@@ -277,135 +443,104 @@ struct Wave {
         }
       }
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i)
+    for (int dt = 0; dt < DT; ++dt) {
+      const f16x8 y = c.template values<CODE>(dt);
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const f16x8 x = codes8<CODE>(c.v[i][2 * u], c.v[i][2 * u + 1]);
+      for (int p = NP - 1; p >= 0; --p)
 #pragma unroll
-        for (int p = NP - 1; p >= 0; --p)
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) o[nt][2 * i + u] = product(x, w[nt][p], o[nt][2 * i + u]);
-      }
+        for (int nt = 0; nt < NT; ++nt) o[nt][dt] = product(y, w[nt][p], o[nt][dt]);
+    }
   }
 
-  // 32 rows in the model's type, those from x on of `tail` open rows and the new ones behind them
-  __device__ __forceinline__ void take_own(int b, int kv, int x0, int tail, int start) {
-    const int total = tail + a.d.n_query;
-    const int64_t told = b * a.d.tail_seq + kv * a.d.tail_head, tnew = b * a.d.new_seq + kv * a.d.new_head;
-    auto row = [&](const char* old, const char* add, int x) {
-      x = min(x, total - 1);
-      return x < tail ? (const T*)old + told + (start + x) % a.d.tail_rows * a.d.tail_row
-                      : (const T*)add + tnew + (x - tail) * a.d.new_row;
-    };
+  // (Values come at once where the registers hold them, else when the weights are known.)
+  __device__ __forceinline__ void issue_own(Own& rows, int b, int kv, int x0, int tail, int slot) {
+    B::template issue_own<true, EARLY>(rows, b, kv, x0, tail, slot);
+  }
+  __device__ __forceinline__ void take_own(Own& rows, int b, int kv, int x0, int tail, int start, int slot) {
+    this->own = true;
     f32x4 s[NT][2];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const T* p = row(a.kt, a.kn, x0 + 16 * k + n);
-      if constexpr (F32) {
-        // step i of the products has dims g (D / 4) + i
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
-          const f32x4 y = *(const f32x4*)(p + g * (D / 4) + 4 * i);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            const f32x4 z = *(const f32x4*)((const T*)a.q + max(at[nt], (int64_t)0) + g * (D / 4) + 4 * i);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) s[nt][k] = product(y[j], z[j], s[nt][k]);
-          }
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < KS; ++i) {
-          const bf16x8 y = __builtin_bit_cast(bf16x8, *(const u32x4*)(p + dim_at(i)));
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            const bf16x8 z =
-                __builtin_bit_cast(bf16x8, *(const u32x4*)((const T*)a.q + max(at[nt], (int64_t)0) + dim_at(i)));
-            s[nt][k] = product(y, z, s[nt][k]);
-          }
-        }
-      }
-    }
+      for (int k = 0; k < 2; ++k) s[nt][k] = B::own_scores(rows, k, raw[nt]);
     complete<2 * NT>(&s[0][0]);
+    unsigned bits[NT];  // which of the lane's 8 rows are seen
     float by[NT];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) by[nt] = a.scale2;
-    const int sinks = a.d.sinks;
-    unsigned bits[NT];  // which of the lane's 8 rows are seen
-#pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
+      by[nt] = a.scale2;
       bits[nt] = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int x = x0 + 16 * (i >> 2) + 4 * g + (i & 3), pos = start + x, step = x - tail;
-        const bool old = x < tail && (pos >= seen_from[nt] || pos < sinks);
-        const bool add = x >= tail && x < total && (anc[nt] >> (step & 63) & 1);
-        bits[nt] |= (old || add) ? 1u << i : 0u;
-      }
+      for (int i = 0; i < 8; ++i)
+        bits[nt] |= B::sees_own(x0 + 16 * (i >> 2) + 4 * g + (i & 3), tail, start, seen_from[nt], anc[nt]) ? 1u << i : 0u;
     }
-    weights(s, by, true, [&](int nt, int j) { return (bits[nt] >> ((j >> 4) * 4 + (j & 3)) & 1) != 0; });
-    const T* rows[8];
+    weights(s, by, true, [&](int nt, int k, int r) { return (bits[nt] >> (4 * k + r) & 1) != 0; });
+    if constexpr (!EARLY) B::template issue_own<false, true>(rows, b, kv, x0, tail, slot);
+    // values that are not finite are taken out of the product, and make NaN where they are seen
+    if (!B::all_finite(rows)) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) rows[i] = row(a.vt, a.vn, x0 + 16 * (i >> 2) + 4 * g + (i & 3)) + n;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      // values that are not finite are taken out of the product, and make NaN where they are seen
-      bool odd = false;
-      unsigned odds = 0;
-      if constexpr (F32) {
-        float y[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          y[i] = rows[i][16 * dt];
-          const bool bad = !(fabsf(y[i]) < __builtin_inff());
-          odds |= bad ? 1u << i : 0u;
-          y[i] = bad ? 0.f : y[i];
-        }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) o[nt][dt] = product(y[i], s[nt][i >> 2][i & 3], o[nt][dt]);
-      } else {
-        bf16x8 y;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          unsigned v = rows[i][16 * dt].bits;
-          const bool bad = (v & 0x7f80u) == 0x7f80u;
-          odds |= bad ? 1u << i : 0u;
-          y[i] = __builtin_bit_cast(__bf16, (uint16_t)(bad ? 0 : v));
-        }
+      for (int dt = 0; dt < DT; ++dt) {
+        const bf16x8 y = B::take_out(rows, dt);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          bf16x8 hi, lo;
+          bf16x8 z;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float w = s[nt][i >> 2][i & 3];
-            hi[i] = (__bf16)w;
-            lo[i] = (__bf16)(w - (float)hi[i]);
-          }
-          o[nt][dt] = product(y, lo, o[nt][dt]);
-          o[nt][dt] = product(y, hi, o[nt][dt]);
-        }
-      }
-      odd = odds != 0;
-      if (__builtin_amdgcn_ballot_w64(odd)) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          bf16x8 y, z;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            y[i] = (__bf16)(odds >> i & 1 ? 1.f : 0.f);
-            z[i] = (__bf16)(bits[nt] >> i & 1 ? 1.f : 0.f);
-          }
+          for (int i = 0; i < 8; ++i) z[i] = (__bf16)(bits[nt] >> i & 1 ? 1.f : 0.f);
           f32x4 count = product(y, z, (f32x4){0.f, 0.f, 0.f, 0.f});
           complete<1>(&count);
-          complete<1>(&o[nt][dt]);
 #pragma unroll
           for (int r = 0; r < 4; ++r) o[nt][dt][r] = count[r] > 0.f ? __builtin_nanf("") : o[nt][dt][r];
         }
       }
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      bf16x8 hi, lo;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float w = s[nt][i >> 2][i & 3];
+        hi[i] = (__bf16)w;
+        lo[i] = (__bf16)(w - (float)hi[i]);
+      }
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        if constexpr (F32) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) o[nt][dt] = product(rows.v[dt][i], s[nt][i >> 2][i & 3], o[nt][dt]);
+        } else {
+          bf16x8 y;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) y[i] = __builtin_bit_cast(__bf16, rows.v[dt][i]);
+          o[nt][dt] = product(y, lo, o[nt][dt]);
+          o[nt][dt] = product(y, hi, o[nt][dt]);
+        }
+      }
+    }
+  }
+
+  // the wave's references and sums to ms (COLS each, `apart` from each other), then what it adds to o
+  __device__ __forceinline__ void put_sums(float* ms, int apart) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      float sum = l[nt];
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      if (sum != sum && m[nt] == -INFINITY) m[nt] = 0.f;  // (-infinity says that no row is seen)
+      if (g == 0) {
+        ms[nt * 16 + n] = m[nt];
+        ms[apart + nt * 16 + n] = sum;
+      }
+    }
+  }
+  template <typename Top>
+  __device__ __forceinline__ void put_o(float* os, int width, Top top) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const float f = m[nt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[nt] - top(nt * 16 + n));
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+        *(f32x4*)(os + (nt * 16 + n) * width + 16 * dt + 4 * g) =
+            m[nt] == -INFINITY ? (f32x4){0.f, 0.f, 0.f, 0.f} : o[nt][dt] * f;
     }
   }
 };
@@ -433,206 +568,315 @@ __device__ __forceinline__ void put_query(const Args& a, int b, int t, int h, in
         l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
-template <typename T, int D, int CODE, int NT>
-__global__ __launch_bounds__(64 * kWaves, 2) void paged_attn_kernel(Args a) {
-  extern __shared__ __align__(16) float lds[];
-  // the sequences' workgroups of one head and part run side by side on one XCD (blocks go round
-  // the XCDs): pages that they share are in its L2
-  const int xcd = blockIdx.x & 7;
-  int i = blockIdx.x >> 3;
-  const int tile = i % a.tiles;
-  i /= a.tiles;
-  const int b = i % a.n_seq, hs = (i / a.n_seq) * 8 + xcd;
-  if (hs >= a.n_kv_head * a.splits) return;
-  const int kv = hs % a.n_kv_head, split = hs / a.n_kv_head;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int len = a.length[b], R0 = a.page_rows;
-
-  Wave<T, D, CODE, NT> w(a);
-  w.load(b, kv, tile, len);
-  if (len >= 0) {
-    const int pages = min(len / R0, a.n_col), start = len / R0 * R0;
-    // columns [0, sinks) and [from, pages) are looked at, in parts of 32 rows
-    int sinks = 0, from = 0, first_full = 0;
+// The cached rows that a sequence's queries can see: columns [0, sinks) and those from `from` on of its table, in all
+// `count` parts of 32 rows.  (page_rows is 32 << shift.)
+struct Seen {
+  int sinks, from, count;
+  __device__ __forceinline__ Seen(const Args& a, int len, int shift) : sinks(0), from(0) {
+    const int pages = min(max(len, 0) >> (5 + shift), a.n_col);
     if (a.d.window) {
-      sinks = min((min(a.d.sinks, pages * R0) + R0 - 1) / R0, pages);
-      from = min(max(max(len - a.d.window + 1, 0) / R0, sinks), pages);
-      first_full = len + a.d.n_query - a.d.window;  // all queries see rows from here on
+      const int rows = 32 << shift;
+      sinks = min((min(a.d.sinks, pages << (5 + shift)) + rows - 1) >> (5 + shift), pages);
+      from = min(max(max(len - a.d.window + 1, 0) >> (5 + shift), sinks), pages);
     }
-    const int per = R0 / 32, count = (sinks + pages - from) * per, all = a.splits * kWaves, me = split * kWaves + wave;
-    const int i0 = (int)((int64_t)count * me / all), i1 = (int)((int64_t)count * (me + 1) / all);
-    const int64_t head_bytes = 2 * (int64_t)R0 * D;
-    const int* table = a.table + b * a.table_ld;
-    for (int p0 = i0 / per; p0 * per < i1; p0 += 64) {
-      // lane j: the page of column p0 + j, and its scales
-      int page = -1;
-      float2 sc = {0.f, 0.f};
-      {
-        const int v = p0 + lane, c = v < sinks ? v : v - sinks + from;
-        if (v * per < i1 && c < pages) page = table[c];
-        if (page < 0 || page >= a.n_page) page = -1;
-        else sc = a.scale[(int64_t)page * a.n_kv_head + kv];
+    count = (sinks + pages - from) << shift;
+  }
+};
+
+// Long sequences are cut by their own lengths: each into the nearest number of parts of an equal share of all rows
+// (one at the least), parts of a head side by side, sequence by sequence.  So a batch of one long and many short
+// ones fills the chip too.  (Every wave finds its part by itself: the lengths are in its lanes.)
+constexpr int kLeast = 16;  // 32 rows each of a part: four for each wave
+constexpr int kLong = 512;  // from this many on, sequences are cut by their own lengths
+struct Part {
+  int b, j, n;  // part j of n of sequence b,
+  int at, kv;   // the at-th of all, in kv head kv
+};
+// sums over the lanes up to this one
+__device__ __forceinline__ int scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // 1, 2, 4, 8 lanes before, within 16
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // the last of the 16 before, to every second 16
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31, to the upper 32
+  return x;
+}
+__device__ __forceinline__ int last(int x) { return __builtin_amdgcn_readlane(x, 63); }
+// Part number p (SEQ: the first one of sequence p, and in kv the parts of a head); kv is n_kv_head or more where there is none.
+template <bool SEQ>
+__device__ __forceinline__ Part find_part(const Args& a, int p) {
+  const int lane = threadIdx.x & 63, shift = a.page_rows >> 6;
+  auto count = [&](int b0) { return b0 + lane < a.n_seq ? Seen(a, a.length[b0 + lane], shift).count : 0; };
+  const int first = count(0);
+  int sum = last(scan(first));
+  for (int b0 = 64; b0 < a.n_seq; b0 += 64) sum += last(scan(count(b0)));
+  const int share = max((sum * a.n_kv_head * a.tiles + a.round - 1) / a.round, kLeast);
+  auto parts = [&](int b0) {
+    const int n = b0 == 0 ? first : count(b0);
+    return b0 + lane < a.n_seq ? max((n + (share >> 1)) / share, 1) : 0;
+  };
+  const int upto0 = scan(parts(0));
+  int all = last(upto0);  // parts of a head
+  for (int b0 = 64; b0 < a.n_seq; b0 += 64) all += last(scan(parts(b0)));
+  Part x;
+  x.kv = SEQ ? all : p / all;
+  const int rest = SEQ ? 0 : p - x.kv * all;
+  int before = 0;
+  for (int b0 = 0; b0 < a.n_seq; b0 += 64) {
+    const int upto = b0 == 0 ? upto0 : scan(parts(b0));
+    // the lane whose sequence it is
+    const unsigned long long hit = SEQ ? (p >= b0 && p < b0 + 64 ? 1ull << (p - b0) : 0ull)
+                                       : __builtin_amdgcn_ballot_w64(before + upto > rest);
+    if (hit) {
+      const int s = __builtin_ctzll(hit), to = __builtin_amdgcn_readlane(upto, s);
+      const int from = s ? __builtin_amdgcn_readlane(upto, s - 1) : 0;
+      x.n = to - from;
+      x.b = b0 + s;
+      x.j = SEQ ? 0 : rest - before - from;
+      x.at = SEQ ? before + from : p;
+      return x;
+    }
+    before += last(upto);
+  }
+  x.kv = a.n_kv_head;
+  return x;
+}
+
+// Items, 32 rows of pages each, go to the waves of a part of a sequence (and of its other parts) in turn: wave `me` of `all`
+// has, but for the last `owners` waves, items me + k others for k < early, and then every wave each all-th one.  The last waves,
+// as many as open and new rows can need, take those in place of their early items.  So which columns a wave looks at
+// does not depend on the length (without a window or parts), and the table's entries are under way with it.
+constexpr int kOwnCost = 6;  // what 32 rows in the model's type take, in 32 rows of pages
+
+template <typename W>
+__global__ __launch_bounds__(64 * kWaves, W::DIM == 128 || W::COLS == 32 || W::F32 ? 2 : 3) void paged_attn_kernel(Args a) {
+  typedef typename W::Type T;
+  constexpr int D = W::DIM, COLS = W::COLS;
+  extern __shared__ __align__(16) float lds[];
+  // the sequences' workgroups of one head and part run side by side on one XCD (blocks go round the XCDs), and
+  // so do a part's tiles of queries: pages that they share are in its L2
+  const int xcd = blockIdx.x & 7, tile = blockIdx.x >> 3;
+  int b, kv, split, splits, at;
+  if (a.splits) {
+    const int hs = blockIdx.z * 8 + xcd;
+    if (hs >= a.n_kv_head * a.splits) return;
+    splits = a.splits;
+    split = splits == 1 ? 0 : hs / a.n_kv_head;
+    kv = hs - split * a.n_kv_head;
+    b = blockIdx.y;
+    at = (b * a.n_kv_head + kv) * splits + split;
+  } else {
+    const Part p = find_part<false>(a, (blockIdx.z * gridDim.y + blockIdx.y) * 8 + xcd);
+    if (p.kv >= a.n_kv_head || p.at >= a.parts) return;
+    b = __builtin_amdgcn_readfirstlane(p.b);
+    kv = __builtin_amdgcn_readfirstlane(p.kv);
+    split = __builtin_amdgcn_readfirstlane(p.j);
+    splits = __builtin_amdgcn_readfirstlane(p.n);
+    at = __builtin_amdgcn_readfirstlane(p.at);
+  }
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int R0 = a.page_rows, shift = R0 >> 6, per = 1 << shift, all = splits * kWaves, me = split * kWaves + wave;
+  const int owners = min(a.owners, all), others = all - owners, early = others > 0 ? kOwnCost : 0;
+  const bool owner = me >= others;
+  const int item0 = owner ? early * others + me : me, slow = owner ? 0 : early;
+  auto item = [&](int k) { return item0 + min(k, slow) * others + max(k - slow, 0) * all; };  // the k-th of this wave
+  const int* table = a.table + b * a.table_ld;
+  int entry = -1;
+  if (a.d.window == 0) {
+    const int c = item(lane) >> shift;
+    if (c < a.n_col) entry = table[c];
+  }
+  W w(a);
+  w.issue(b, kv, tile);
+  const int len = a.length[b];
+  if (len < 0) {
+    w.begin(0);
+  } else {
+    const int start = len & -R0, tail = len - start;
+    const Seen look(a, len, shift);
+    const int sinks = look.sinks, from = look.from, count = look.count;
+    const int first_full = a.d.window ? len + a.d.n_query - a.d.window : 0;  // all queries see rows from here on
+    // lane j: the page of item k0 + j of this wave's, and its scales
+    int page = -1;
+    float2 sc = {0.f, 0.f};
+    auto find = [&](int k0) {
+      const int i = item(k0 + lane), v = i >> shift, c = v < sinks ? v : v - sinks + from;
+      page = a.d.window == 0 && k0 == 0 ? entry : i < count ? table[c] : -1;
+      if (i >= count || (unsigned)page >= (unsigned)a.n_page) page = -1;
+      sc = a.scale[(int64_t)max(page, 0) * a.n_kv_head + kv];
+    };
+    find(0);
+    w.begin(len);
+    const int owns = (tail + a.d.n_query + 31) >> 5;
+    if (owner && all - 1 - me < owns) {
+      const int slot = start % a.d.tail_rows;
+      typename W::Own rows;
+      for (int j = all - 1 - me; j < owns; j += owners) {
+        w.issue_own(rows, b, kv, 32 * j, tail, slot);
+        w.take_own(rows, b, kv, 32 * j, tail, start, slot);
       }
-      const int lo = max(i0, p0 * per), hi = min(i1, (p0 + 64) * per);
-      auto fetch = [&](Codes<D>& c, int i) {
-        const int id = max(__builtin_amdgcn_readlane(page, i / per - p0), 0);
-        const uint8_t* block = a.data + ((int64_t)id * a.n_kv_head + kv) * head_bytes + (i % per) * (32 * D);
-        c.load(block, block + R0 * D, lane);
+    }
+    w.split();
+    const int64_t head_bytes = 2 * (int64_t)R0 * D;
+    const int soon = slow * others, rest = count - item0;
+    const int items = rest <= 0 ? 0 : rest <= soon ? (rest + others - 1) / others : slow + (rest - soon + all - 1) / all;
+    for (int k0 = 0; k0 < items; k0 += 64) {
+      if (k0) find(k0);
+      auto fetch = [&](Codes<D>& x, int k) {
+        // (lanes past the last item have no page: page 0, for all waves the same)
+        const int id = max(__builtin_amdgcn_readlane(page, min(k - k0, 63)), 0);
+        const uint8_t* block = a.data + ((int64_t)id * a.n_kv_head + kv) * head_bytes + (item(k) & (per - 1)) * (32 * D);
+        x.load(block, block + R0 * D, lane);
       };
-      auto work = [&](const Codes<D>& c, int i) {
-        const int j = i / per - p0;
+      auto work = [&](const Codes<D>& x, int k) {
+        const int j = k - k0, i = item(k), v = i >> shift, col = v < sinks ? v : v - sinks + from;
         if (__builtin_amdgcn_readlane(page, j) < 0) return;
         const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sc.x), j));
         const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sc.y), j));
-        const int v = i / per, col = v < sinks ? v : v - sinks + from, first = col * R0 + i % per * 32;
-        w.take(c, ks, vs, first, first < first_full && first + 32 > a.d.sinks);
+        const int first = col * R0 + (i & (per - 1)) * 32;
+        w.take(x, ks, vs, first, first < first_full && first + 32 > a.d.sinks);
       };
-      Codes<D> c0, c1;
-      fetch(c0, lo);
-      for (int i = lo; i < hi; i += 2) {
-        if (i + 1 < hi) fetch(c1, i + 1);
-        work(c0, i);
-        if (i + 1 >= hi) break;
-        if (i + 2 < hi) fetch(c0, i + 2);
-        work(c1, i + 1);
-      }
+      // Loads run ST - 1 items ahead, past the last item, too: were they under a condition, the compiler would have to
+      // wait as if they had not been issued, for those of the next items with the item's own.
+      constexpr int ST = 2;
+      Codes<D> x[ST];
+#pragma unroll
+      for (int u = 0; u < ST - 1; ++u) fetch(x[u], k0 + u);
+      const int end = min(k0 + 64, items);
+      for (int k = k0; k < end; k += ST)
+#pragma unroll
+        for (int u = 0; u < ST; ++u) {
+          fetch(x[(u + ST - 1) % ST], k + u + ST - 1);
+          if (k + u < end) work(x[u], k + u);
+        }
     }
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int dt = 0; dt < D / 16; ++dt) w.o[nt][dt] *= w.vunit;
-    const int tail = len - start;
-    for (int j = all - 1 - me; j * 32 < tail + a.d.n_query; j += all) w.take_own(b, kv, 32 * j, tail, start);
+    if (w.vunit != 0.f) w.scale_o(w.vunit);
   }
 
   // the waves' sums, joined
-  float* ms = lds;                         // [wave][column] m, then l
-  float* os = lds + 2 * kWaves * 16 * NT;  // [wave][column][dim]
-  constexpr int W = D + 4;                 // (columns 16 bytes apart in the banks)
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    float l = w.l[nt];
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    if (l != l && w.m[nt] == -INFINITY) w.m[nt] = 0.f;  // (-infinity says that no row is seen)
-    if (w.g == 0) {
-      ms[wave * 16 * NT + nt * 16 + w.n] = w.m[nt];
-      ms[(kWaves + wave) * 16 * NT + nt * 16 + w.n] = l;
-    }
-  }
+  constexpr int WIDTH = D + 4;          // (columns 16 bytes apart in the banks)
+  float* ms = lds;                      // [wave][column] m, then l
+  float* os = lds + 2 * kWaves * COLS;  // [wave][column][dim]
+  w.put_sums(ms + wave * COLS, kWaves * COLS);
   __syncthreads();
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
+  auto top_of = [&](int col) {
     float top = -INFINITY;
 #pragma unroll
-    for (int v = 0; v < kWaves; ++v) top = fmaxf(top, ms[v * 16 * NT + nt * 16 + w.n]);
-    const float by = w.m[nt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(w.m[nt] - top);
-#pragma unroll
-    for (int dt = 0; dt < D / 16; ++dt)
-      *(f32x4*)(os + (wave * 16 * NT + nt * 16 + w.n) * W + 16 * dt + 4 * w.g) =
-          w.m[nt] == -INFINITY ? (f32x4){0.f, 0.f, 0.f, 0.f} : w.o[nt][dt] * by;
-  }
+    for (int v = 0; v < kWaves; ++v) top = fmaxf(top, ms[v * COLS + col]);
+    return top;
+  };
+  w.put_o(os + wave * COLS * WIDTH, WIDTH, top_of);
   __syncthreads();
   const int group = a.d.n_head / a.n_kv_head, cols = a.d.n_query * group;
-  for (int x = threadIdx.x; x < 16 * NT * (D / 4); x += 64 * kWaves) {
-    const int col = x / (D / 4), dim = 4 * (x % (D / 4)), c = tile * NT * 16 + col;
+  for (int x = threadIdx.x; x < COLS * (D / 4); x += 64 * kWaves) {
+    const int col = x / (D / 4), dim = 4 * (x % (D / 4)), c = tile * COLS + col;
     if (c >= cols) break;
-    float top = -INFINITY, l = 0.f;
+    const float top = top_of(col);
+    float l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int v = 0; v < kWaves; ++v) top = fmaxf(top, ms[v * 16 * NT + col]);
-#pragma unroll
     for (int v = 0; v < kWaves; ++v) {
-      const float m = ms[v * 16 * NT + col];
-      if (m != -INFINITY) l += ms[(kWaves + v) * 16 * NT + col] * __builtin_amdgcn_exp2f(m - top);
-      o += *(const f32x4*)(os + (v * 16 * NT + col) * W + dim);
+      const float m = ms[v * COLS + col];
+      if (m != -INFINITY) l += ms[(kWaves + v) * COLS + col] * __builtin_amdgcn_exp2f(m - top);
+      o += *(const f32x4*)(os + (v * COLS + col) * WIDTH + dim);
     }
-    const int t = c / group, h = kv * group + c % group;
-    if (a.splits == 1) {
+    const int t = group == 1 ? c : c / group, h = kv * group + c - t * group;
+    if (splits == 1) {
       put_query<T>(a, b, t, h, dim, o, top, l);
     } else {
-      const int64_t part = (((int64_t)b * a.d.n_query + t) * a.d.n_head + h) * a.splits + split;
-      *(f32x4*)(a.o + part * D + dim) = o;
-      if (dim == 0) a.ml[part] = make_float2(top, l);
+      const int64_t place = ((int64_t)at * a.tiles + tile) * COLS + col;
+      *(f32x4*)(a.o + place * D + dim) = o;
+      if (dim == 0) a.ml[place] = make_float2(top, l);
     }
   }
 }
 
 // A wave per query adds its parts: lane l has dims 4 (l mod (D / 4)) .. + 3 of every (256 / D)-th.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void join_kernel(Args a, int64_t queries) {
+__global__ __launch_bounds__(256) void join_kernel(Args a) {
   constexpr int LD = D / 4, PAR = 64 / LD;
-  const int lane = threadIdx.x & 63, x = lane % LD;
-  const int64_t q = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (q >= queries) return;
-  const float2* ml = a.ml + q * a.splits;
-  const float* po = a.o + q * a.splits * D + 4 * x;
+  const int lane = threadIdx.x & 63, x = lane % LD, b = blockIdx.y;
+  const int query = blockIdx.x * 4 + (threadIdx.x >> 6), t = query / a.d.n_head, h = query - t * a.d.n_head;
+  const int group = a.d.n_head / a.n_kv_head, kv = h / group, c = t * group + h - kv * group;
+  int n = a.splits, part = (b * a.n_kv_head + kv) * n;
+  if (n == 0) {
+    const Part p = find_part<true>(a, b);
+    n = p.n;
+    part = kv * p.kv + p.at;
+    if (n == 1) return;
+  }
+  if (t >= a.d.n_query) return;
+  const int64_t step = (int64_t)a.tiles * a.cols, at = part * step + c;
+  const float2* ml = a.ml + at;
+  const float* po = a.o + at * D + 4 * x;
   float top = -INFINITY, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int i = lane / LD; i < a.splits; i += PAR) {
-    const float2 p = ml[i];
-    const f32x4 y = *(const f32x4*)(po + (int64_t)i * D);
-    const float now = fmaxf(top, p.x);
-    const float c = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - now);
-    const float d = p.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(p.x - now);
-    o = o * c + (p.x == -INFINITY ? (f32x4){0.f, 0.f, 0.f, 0.f} : y * d);
-    l = l * c + (p.x == -INFINITY ? 0.f : p.y * d);
+  for (int i = lane / LD; i < n; i += PAR) {
+    const float2 q = ml[i * step];
+    const f32x4 y = *(const f32x4*)(po + i * step * D);
+    const float now = fmaxf(top, q.x);
+    const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - now);
+    const float d = q.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(q.x - now);
+    o = o * f + (q.x == -INFINITY ? (f32x4){0.f, 0.f, 0.f, 0.f} : y * d);
+    l = l * f + (q.x == -INFINITY ? 0.f : q.y * d);
     top = now;
   }
   float all = top;
 #pragma unroll
   for (int s = 32; s >= LD; s >>= 1) all = fmaxf(all, __shfl_xor(all, s));
-  const float c = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - all);
-  o *= c;
-  l *= c;
+  const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - all);
+  o *= f;
+  l *= f;
 #pragma unroll
   for (int s = 32; s >= LD; s >>= 1) {
     l += __shfl_xor(l, s);
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], s);
   }
-  if (lane < LD) {
-    const int h = (int)(q % a.d.n_head);
-    const int64_t bt = q / a.d.n_head;
-    put_query<T>(a, (int)(bt / a.d.n_query), (int)(bt % a.d.n_query), h, 4 * x, o, all, l);
-  }
+  if (lane < LD) put_query<T>(a, b, t, h, 4 * x, o, all, l);
 }
 
 // ---------------------------------------------------------------- host
 
 struct Plan {
-  int nt, tiles, splits;
-  int64_t blocks, queries;
+  int cols, tiles, splits, round;  // queries of a workgroup, workgroups of a sequence's and head's queries; see Args
+  int64_t parts, blocks;           // parts that there can be, workgroups
   size_t o_bytes, bytes;
 };
 int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-constexpr int kRound = 1024;  // workgroups that are asked for
-
 Plan plan(const ssd_page_pool& p, const ssd_page_seqs& s, const ssd_paged_attn_desc& d) {
   Plan x{};
   const int64_t cols = (int64_t)d.n_query * (d.n_head / p.n_kv_head);
-  x.nt = cols > 16 ? 2 : 1;
-  x.tiles = (int)div_up(cols, 16 * x.nt);
+  x.cols = cols > 16 && !(d.dtype == SSD_F32 && p.head_dim == 128) ? 32 : 16;  // (what the registers hold)
+  x.tiles = (int)div_up(cols, x.cols);
   int64_t pages = s.n_col;
   if (d.window)
     pages = std::min<int64_t>(pages, div_up(std::min<int64_t>(d.sinks, 1 << 30), p.page_rows) + d.window / p.page_rows + 2);
   const int64_t units = (int64_t)s.n_seq * p.n_kv_head * x.tiles, steps = pages * (p.page_rows / 32);
-  x.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kRound / units, div_up(steps, 4 * kWaves)));
-  x.blocks = div_up((int64_t)p.n_kv_head * x.splits, 8) * 8 * s.n_seq * x.tiles;
-  x.queries = (int64_t)s.n_seq * d.n_query * d.n_head;
-  if (x.splits == 1) {
-    x.bytes = 16;  // (not used)
-    return x;
+  const int64_t round = p.head_dim == 128 || x.cols == 32 || d.dtype == SSD_F32 ? 512 : 768;
+  const int64_t heads = (int64_t)s.n_seq * p.n_kv_head;
+  // (numbers of 32 rows of all queries are 32-bit where the device counts them)
+  if (s.n_seq > 1 && steps > kLong && units * steps < (1 << 30)) {
+    x.round = (int)round;
+    x.parts = div_up(heads + div_up(round, x.tiles), 8) * 8;
+    x.blocks = x.parts * x.tiles;
+  } else {
+    x.splits = (int)std::max<int64_t>(1, std::min<int64_t>(round / units, div_up(steps, kLeast)));
+    x.parts = heads * x.splits;
+    x.blocks = div_up((int64_t)p.n_kv_head * x.splits, 8) * 8 * s.n_seq * x.tiles;
   }
-  x.o_bytes = (size_t)x.queries * x.splits * p.head_dim * 4;
-  x.bytes = x.o_bytes + (size_t)x.queries * x.splits * sizeof(float2);
+  x.bytes = 16;  // (not used)
+  if (x.splits == 1) return x;
+  x.o_bytes = (size_t)x.parts * x.tiles * x.cols * p.head_dim * 4;
+  x.bytes = x.o_bytes + (size_t)x.parts * x.tiles * x.cols * sizeof(float2);
   return x;
 }
 
-template <typename T, int D, int CODE, int NT>
+template <typename W>
 hipError_t launch(const Args& a, const Plan& p, hipStream_t s) {
-  constexpr int lds = (2 * kWaves * 16 * NT + kWaves * 16 * NT * (D + 4)) * 4;
+  constexpr int lds = (2 * kWaves * W::COLS + kWaves * W::COLS * (W::DIM + 4)) * 4;
   if constexpr (lds > 65536) {  // has to be asked for, once per kernel and device
     static std::atomic<uint64_t> ready{0};
     int dev = 0;
@@ -640,21 +884,25 @@ hipError_t launch(const Args& a, const Plan& p, hipStream_t s) {
     if (e != hipSuccess) return e;
     const uint64_t bit = dev < 64 ? 1ull << dev : 0;
     if (!(ready.load(std::memory_order_acquire) & bit)) {
-      e = hipFuncSetAttribute((const void*)paged_attn_kernel<T, D, CODE, NT>,
-                              hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+      e = hipFuncSetAttribute((const void*)paged_attn_kernel<W>, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
       if (e != hipSuccess) return e;
       ready.fetch_or(bit, std::memory_order_release);
     }
   }
-  paged_attn_kernel<T, D, CODE, NT><<<(unsigned)p.blocks, 64 * kWaves, lds, s>>>(a);
+  const int64_t rows = 32768;  // (of a grid's dimensions, 65535 at the most)
+  const dim3 grid = p.splits ? dim3(8 * p.tiles, a.n_seq, (unsigned)div_up((int64_t)a.n_kv_head * p.splits, 8))
+                             : dim3(8 * p.tiles, (unsigned)std::min(p.parts / 8, rows), (unsigned)div_up(p.parts / 8, rows));
+  paged_attn_kernel<W><<<grid, 64 * kWaves, lds, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
-  join_kernel<T, D><<<(unsigned)div_up(p.queries, 4), 256, 0, s>>>(a, p.queries);
+  join_kernel<typename W::Type, W::DIM><<<dim3((a.d.n_query * a.d.n_head + 3) / 4, a.n_seq), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 template <typename T, int D, int CODE>
 hipError_t launch(const Args& a, const Plan& p, hipStream_t s) {
-  return p.nt == 2 ? launch<T, D, CODE, 2>(a, p, s) : launch<T, D, CODE, 1>(a, p, s);
+  if constexpr (!(sizeof(T) == 4 && D == 128))
+    if (p.cols == 32) return launch<Tiles<T, D, CODE, 2>>(a, p, s);
+  return launch<Tiles<T, D, CODE, 1>>(a, p, s);
 }
 template <typename T, int D>
 hipError_t launch(const Args& a, const Plan& p, int code, hipStream_t s) {
@@ -696,7 +944,7 @@ extern "C" ssd_status ssd_paged_attn_workspace(const ssd_page_pool* pool, const 
   const ssd_status st = check(pool, seqs, a);
   if (st != SSD_OK) return st;
   const Plan p = plan(*pool, *seqs, *a);
-  OP_REQUIRE(p.blocks <= kMostBlocks && p.queries <= 4 * kMostBlocks, SSD_E_CAPACITY, "more workgroups than a grid holds");
+  OP_REQUIRE(p.blocks <= kMostBlocks, SSD_E_CAPACITY, "more workgroups than a grid holds");
   *bytes = p.bytes;
   return SSD_OK;
 }
@@ -753,7 +1001,11 @@ extern "C" ssd_status ssd_paged_attn(const ssd_page_pool* pool, const ssd_page_s
   x.o = (float*)workspace;
   x.ml = (float2*)((char*)workspace + p.o_bytes);
   x.tiles = p.tiles;
+  x.cols = p.cols;
   x.splits = p.splits;
+  x.round = p.round;
+  x.parts = (int)p.parts;
+  x.owners = (pool->page_rows - 1 + a->n_query + 31) / 32;
   x.scale2 = a->scale * 1.4426950408889634f;
   const hipError_t e = a->dtype == SSD_F32 ? launch<float>(x, p, D, pool->code, (hipStream_t)stream)
                                            : launch<bf16_t>(x, p, D, pool->code, (hipStream_t)stream);

@@ -808,3 +808,61 @@ def test_the_operators_run_on_the_stream_they_are_given(env):
     for n in ("table", "length", "refs", "kt", "vt", "full", "used"):
         assert torch.equal(getattr(a, n), getattr(e, n)), n
     assert torch.equal(a.pages.data, e.pages.data)
+
+
+# ---------------------------------------------------------------- attention, cut by the sequences' lengths
+
+@pytest.mark.parametrize("dtype,code,b,t,h,g,d,rows,lens,kw", [
+    ("bf16", "int8", 3, 1, 2, 1, 64, 32, [3000, 40, 1500], {}),
+    ("bf16", "e4m3", 4, 5, 8, 2, 128, 64, [0, 2500, -1, 777], {"tree": True}),
+    ("f32", "int8", 2, 9, 4, 2, 64, 128, [2222, 1031], {}),
+    ("bf16", "int8", 2, 40, 6, 2, 32, 32, [1800, 64], {}),
+    ("f32", "e4m3", 130, 1, 1, 1, 32, 32, [(37 * i) % 90 if i % 41 else 2600 for i in range(130)], {}),
+    ("bf16", "int8", 70, 2, 2, 2, 64, 32, [-1 if i % 7 == 0 else (53 * i) % 200 if i != 66 else 1900 for i in range(70)], {})])
+def test_batches_of_long_and_short_sequences(env, dtype, code, b, t, h, g, d, rows, lens, kw):
+    """Tables wide enough that sequences are cut by their lengths (more than 512 times 32 rows)."""
+    print(dtype, code, b, t, lens[:4], flush=True)
+    c = Case(env, dtype, code, b, t, h, g, d, rows, lens, cols=600 * 32 // rows + 1, **kw)
+    want = c.check()
+    again = c.run()
+    assert all(env[0].equal(x, y) for x, y in zip(want, again))
+
+
+def test_windows_where_sequences_are_cut_by_their_lengths(env):
+    c = Case(env, "bf16", "int8", 3, 2, 2, 1, 64, 32, [2900, 900, 100], cols=1300)
+    c.check(window=17000, sinks=5)  # (wide enough to be cut so)
+    c.check(window=2000, sinks=16500)
+    c.check(window=1000, sinks=70)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_scores_of_any_size(env, dtype):
+    """Scores around 2^26, 2^45 and 2^90: the row with the largest by far is all that is left of a query's."""
+    for by in (2.0 ** 22, 2.0 ** 41, 2.0 ** 86):
+        c = Case(env, dtype, "int8", 1, 1, 2, 1, 64, 32, [140])
+        c.q = c.q.abs() + 1
+        pk, _ = M.places(32, 64)
+        for row in (3, 77, 127):
+            x = Case(env, dtype, "int8", 1, 1, 2, 1, 64, 32, [140])
+            x.q = (c.q * by).to(x.dt)
+            x.kt.fill_(0.1), x.kn.fill_(0.2)
+            raw = x.data.clone().view(1, -1, 1, 2, 32 * 64)
+            raw[:, :, :, 0] = 128 + 16   # all keys alike ...
+            raw[0, x.table[0, row // 32], 0, 0, pk[row % 32]] = 128 + 120  # ... but one
+            x.data = raw.view(x.data.shape)
+            x.scale[0, :, :, 0] = 0.03
+            out, lse = x.run()
+            v = x.host()[1][x.table[0, row // 32], 0, row % 32]
+            got = out[0, 0].double().cpu().numpy()
+            assert np.abs(got - v[None]).max() <= np.abs(v).max() * (2.0 ** -8 if dtype == "bf16" else 2.0 ** -21)
+            assert lse.isfinite().all()
+
+
+def test_scales_below_zero(env):
+    """(Stored pages have none.)"""
+    for dtype in ("f32", "bf16"):
+        c = Case(env, dtype, "e4m3", 2, 2, 4, 2, 64, 32, [200, 321])
+        c.scale[0, ::3, :, 0] *= -1
+        c.scale[0, ::4, :, 1] *= -1
+        c.check()
+        c.check(scale=-0.2)
