@@ -127,6 +127,7 @@ typedef struct {
   int64_t new_seq, new_row, new_head;
 } ssd_paged_attn_desc;
 
+/* Bytes of workspace for a call with these shapes (0: none, it may be NULL). */
 ssd_status ssd_paged_attn_workspace(const ssd_page_pool *pool, const ssd_page_seqs *seqs,
                                     const ssd_paged_attn_desc *a, size_t *bytes);
 ssd_status ssd_paged_attn(const ssd_page_pool *pool, const ssd_page_seqs *seqs, const ssd_paged_attn_desc *a,

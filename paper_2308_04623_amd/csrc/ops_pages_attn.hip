@@ -867,7 +867,6 @@ Plan plan(const ssd_page_pool& p, const ssd_page_seqs& s, const ssd_paged_attn_d
     x.parts = heads * x.splits;
     x.blocks = div_up((int64_t)p.n_kv_head * x.splits, 8) * 8 * s.n_seq * x.tiles;
   }
-  x.bytes = 16;  // (not used)
   if (x.splits == 1) return x;
   x.o_bytes = (size_t)x.parts * x.tiles * x.cols * p.head_dim * 4;
   x.bytes = x.o_bytes + (size_t)x.parts * x.tiles * x.cols * sizeof(float2);
@@ -973,7 +972,7 @@ extern "C" ssd_status ssd_paged_attn(const ssd_page_pool* pool, const ssd_page_s
   const OpView o = view(out, od);
   for (const OpView& in : {view(q, qd), view(k_tail, td), view(v_tail, td), view(k_new, nd), view(v_new, nd)})
     OP_REQUIRE(op_apart(o, in), SSD_E_INVALID_ARG, "out overlaps an input");
-  OP_REQUIRE(workspace, SSD_E_INVALID_ARG, "null workspace");
+  OP_REQUIRE(workspace || need == 0, SSD_E_INVALID_ARG, "null workspace");
   OP_REQUIRE(workspace_bytes >= need && (uintptr_t)workspace % 16 == 0, SSD_E_CAPACITY,
              "workspace below ssd_paged_attn_workspace's bytes or not 16-byte aligned");
   const Plan p = plan(*pool, *seqs, *a);

@@ -24,7 +24,7 @@ from typing import Optional
 import torch
 
 from . import ops, ssd
-from .ops import _check, _DTYPES, _elsewhere, _KINDS, _layout, _raw_stream, _refuse, _strides, _tensor, _vector
+from .ops import _check, _DTYPES, _elsewhere, _KINDS, _raw_stream, _refuse, _strides, _tensor, _vector
 
 # every function include/ssd_pages.h declares
 EXPORTS = ("ssd_paged_attn_workspace", "ssd_paged_attn", "ssd_pages_store", "ssd_pages_load", "ssd_pages_workspace",
@@ -102,7 +102,7 @@ class Pages:
         self.device, self._dev = data.device, data.get_device()
         self._pool = _Pool(CODES[code], l, p, g, page_rows, self.head_dim, data.data_ptr(), scale.data_ptr())
         self._ref = C.byref(self._pool)
-        self._work = {}
+        self.kind = code, l, p, g, page_rows, self.head_dim, self._dev  # (all that checks depend on)
 
     @classmethod
     def empty(cls, n_layer: int, n_page: int, n_kv_head: int, head_dim: int, page_rows: int = 32, code: str = "int8",
@@ -111,15 +111,6 @@ class Pages:
         shape = (n_layer, n_page, n_kv_head, 2)
         return cls(torch.zeros(shape + (page_rows * head_dim,), dtype=torch.uint8, device=device),
                    torch.zeros(shape, dtype=torch.float32, device=device), page_rows, code)
-
-    def _workspace(self, what, seqs, n_seq):
-        """The bytes that take, commit and compact need for n_seq sequences."""
-        need = self._work.get(n_seq)
-        if need is None:
-            size = C.c_size_t(0)
-            _check(_ops().ssd_pages_workspace(self._ref, C.byref(seqs), C.byref(size)), what)
-            need = self._work[n_seq] = size.value
-        return need
 
 
 def _pages(what, pages):
@@ -140,6 +131,13 @@ def _seqs(what, table, length, refs, like, n_page=None):
                  refs.data_ptr() if refs is not None else None)
 
 
+def _workspace(what, pages, seqs):
+    """The bytes that take, commit and compact need."""
+    size = C.c_size_t(0)
+    _check(_ops().ssd_pages_workspace(pages._ref, C.byref(seqs), C.byref(size)), what)
+    return size.value
+
+
 def _lies(what, name, t):
     if t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1:
         _refuse(what, f"{name}'s last dimension must be contiguous")
@@ -150,23 +148,33 @@ def _alike(what, k, v, name):
         _refuse(what, f"{name}'s keys and values must have the same strides")
 
 
+# calls' descriptions and workspaces' bytes by their tensors' layouts (and the function): what was found in order is
+# not looked at again, which is half of the host's time of a call
+_plans = {}
+
+
+def _plan(key, make):
+    """What make() gives for this key (None: for a call that is not all tensors, and is refused)."""
+    plan = _plans.get(key) if key is not None else None
+    if plan is None:
+        plan = make()
+        if key is not None:
+            if len(_plans) >= 512:
+                _plans.clear()
+            _plans[key] = plan
+    return plan
+
+
+def _key(what, values, *tensors):
+    try:
+        return (what, values, *[None if t is None else (t.dtype, t.shape, t.stride(), t.get_device()) for t in tensors])
+    except AttributeError:
+        return None
+
+
 # ---------------------------------------------------------------- attention
 
-# calls' descriptions and workspaces' bytes by their tensors' layouts: what was found in order is not looked at again
-_attn_plans = {}
-
-
 def _attn_plan(q, pages, table, length, k_tail, v_tail, k_new, v_new, layer, anc, window, sinks, scale, out):
-    try:
-        key = (_layout(q), _layout(table), _layout(length), _layout(k_tail), _layout(v_tail), _layout(k_new),
-               _layout(v_new), None if anc is None else _layout(anc), None if out is None else _layout(out),
-               pages.code, pages.page_rows, pages.n_layer, pages.n_page, pages.n_kv_head, pages.head_dim, pages._dev,
-               layer, window, sinks, scale)
-        plan = _attn_plans.get(key)
-    except (AttributeError, TypeError):  # (not all tensors: refused below)
-        key = plan = None
-    if plan is not None:
-        return plan
     _refuse_attn(q, pages, table, length, k_tail, v_tail, k_new, v_new, anc, out)
     b, t, h, d = q.shape
     g, r = k_tail.shape[1:3]
@@ -177,12 +185,7 @@ def _attn_plan(q, pages, table, length, k_tail, v_tail, k_new, v_new, layer, anc
     need = C.c_size_t(0)
     seqs = _seqs("ssd_paged_attn", table, length, None, q)
     _check(_ops().ssd_paged_attn_workspace(pages._ref, C.byref(seqs), C.byref(a), C.byref(need)), "ssd_paged_attn")
-    plan = C.byref(a), need.value, seqs.n_seq, seqs.n_col, seqs.table_ld
-    if key is not None:
-        if len(_attn_plans) >= 256:
-            _attn_plans.clear()
-        _attn_plans[key] = plan
-    return plan
+    return C.byref(a), need.value, seqs.n_seq, seqs.n_col, seqs.table_ld
 
 
 def _refuse_attn(q, pages, table, length, k_tail, v_tail, k_new, v_new, anc, out):
@@ -233,8 +236,11 @@ def paged_attention(q, pages: Pages, table, length, k_tail, v_tail, k_new, v_new
     if scale is not None and type(scale) is not float:
         scale = float(scale)  # (by its value: what is remembered of a call must not go by a tensor's identity)
     layer, window, sinks = ops.operator.index(layer), ops.operator.index(window), ops.operator.index(sinks)
-    a, need, n_seq, n_col, ld = _attn_plan(q, pages, table, length, k_tail, v_tail, k_new, v_new, layer, anc, window,
-                                           sinks, scale, out)
+    if not isinstance(pages, Pages):
+        _pages("ssd_paged_attn", pages)
+    a, need, n_seq, n_col, ld = _plan(
+        _key("attn", (pages.kind, layer, window, sinks, scale), q, table, length, k_tail, v_tail, k_new, v_new, anc, out),
+        lambda: _attn_plan(q, pages, table, length, k_tail, v_tail, k_new, v_new, layer, anc, window, sinks, scale, out))
     dev = pages._dev
     where = _elsewhere(dev, stream)
     if where is not None:
@@ -244,18 +250,19 @@ def paged_attention(q, pages: Pages, table, length, k_tail, v_tail, k_new, v_new
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device) if return_lse else None
-    work = torch.empty(need, dtype=torch.uint8, device=q.device)
+    work = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
     seqs = _Seqs(n_seq, n_col, ld, table.data_ptr(), length.data_ptr(), None)
     _check(_ops().ssd_paged_attn(pages._ref, C.byref(seqs), a, q.data_ptr(), k_tail.data_ptr(), v_tail.data_ptr(),
                                  k_new.data_ptr(), v_new.data_ptr(), anc.data_ptr() if anc is not None else None,
-                                 out.data_ptr(), lse.data_ptr() if return_lse else None, work.data_ptr(), need,
+                                 out.data_ptr(), lse.data_ptr() if return_lse else None,
+                                 work.data_ptr() if need else None, need,
                                  _raw_stream(dev)), "ssd_paged_attn")
     return (out, lse) if return_lse else out
 
 
 # ---------------------------------------------------------------- rows into pages and back
 
-def _block_rows(what, pages, ids, k, v, layer):
+def _block_rows(what, pages, ids, k, v):
     _vector(what, "ids", ids, torch.int32, None, pages.data)
     n = ids.shape[0]
     _tensor(what, "k", k, _KINDS, 5, pages.data)
@@ -274,12 +281,12 @@ def pages_store(pages: Pages, ids, k, v, layer: int = 0, stream=None):
     x.unflatten(2, (n, page_rows)).transpose(1, 2)."""
     what = "ssd_pages_store"
     _pages(what, pages)
-    d = _block_rows(what, pages, ids, k, v, layer)
+    d = _plan(_key(what, pages.kind, ids, k, v), lambda: C.byref(_block_rows(what, pages, ids, k, v)))
     where = _elsewhere(pages._dev, stream)
     if where is not None:
         with where:
             return pages_store(pages, ids, k, v, layer)
-    _check(_ops().ssd_pages_store(pages._ref, ids.data_ptr(), ids.shape[0], layer, k.shape[0], C.byref(d), k.data_ptr(),
+    _check(_ops().ssd_pages_store(pages._ref, ids.data_ptr(), ids.shape[0], layer, k.shape[0], d, k.data_ptr(),
                                   v.data_ptr(), _raw_stream(pages._dev)), what)
 
 
@@ -314,14 +321,19 @@ def pages_take(pages: Pages, refs, table, length, count, stream=None):
     times page_rows rows, behind those they have; returns how many each got, int32 [B] (-1: none asked for, or not to be had)."""
     what = "ssd_pages_take"
     _pages(what, pages)
-    seqs = _seqs(what, table, length, refs, pages.data, pages.n_page)
-    _vector(what, "count", count, torch.int32, seqs.n_seq, pages.data)
+
+    def make():
+        seqs = _seqs(what, table, length, refs, pages.data, pages.n_page)
+        _vector(what, "count", count, torch.int32, seqs.n_seq, pages.data)
+        return seqs.n_seq, seqs.n_col, seqs.table_ld, _workspace(what, pages, seqs)
+
+    b, c, ld, need = _plan(_key(what, pages.kind, refs, table, length, count), make)
     where = _elsewhere(pages._dev, stream)
     if where is not None:
         with where:
             return pages_take(pages, refs, table, length, count)
-    need = pages._workspace(what, seqs, seqs.n_seq)
-    got = torch.empty(seqs.n_seq, dtype=torch.int32, device=pages.device)
+    seqs = _Seqs(b, c, ld, table.data_ptr(), length.data_ptr(), refs.data_ptr())
+    got = torch.empty(b, dtype=torch.int32, device=pages.device)
     work = torch.empty(need, dtype=torch.uint8, device=pages.device)
     _check(_ops().ssd_pages_take(pages._ref, C.byref(seqs), count.data_ptr(), got.data_ptr(), work.data_ptr(), need,
                                  _raw_stream(pages._dev)), what)
@@ -348,6 +360,24 @@ def pages_commit(pages: Pages, refs, table, length, k_tail, v_tail, k_new, v_new
     sees, with this window and these sinks, are given back."""
     what = "ssd_pages_commit"
     _pages(what, pages)
+    b, c, ld, tail, fresh, path_ld, need = _plan(
+        _key(what, pages.kind, refs, table, length, k_tail, v_tail, k_new, v_new, path, path_len),
+        lambda: _commit_plan(what, pages, refs, table, length, k_tail, v_tail, k_new, v_new, path, path_len))
+    where = _elsewhere(pages._dev, stream)
+    if where is not None:
+        with where:
+            return pages_commit(pages, refs, table, length, k_tail, v_tail, k_new, v_new, path, path_len, window, sinks)
+    seqs = _Seqs(b, c, ld, table.data_ptr(), length.data_ptr(), refs.data_ptr())
+    full = torch.empty(b, dtype=torch.int32, device=pages.device)
+    work = torch.empty(need, dtype=torch.uint8, device=pages.device)
+    _check(_ops().ssd_pages_commit(pages._ref, C.byref(seqs), tail, k_tail.data_ptr(), v_tail.data_ptr(), fresh,
+                                   k_new.data_ptr(), v_new.data_ptr(), path.data_ptr(), path_ld, path.shape[1],
+                                   path_len.data_ptr(), window, sinks, full.data_ptr(), work.data_ptr(), need,
+                                   _raw_stream(pages._dev)), what)
+    return full
+
+
+def _commit_plan(what, pages, refs, table, length, k_tail, v_tail, k_new, v_new, path, path_len):
     like = pages.data
     seqs = _seqs(what, table, length, refs, like, pages.n_page)
     b, g, w = seqs.n_seq, pages.n_kv_head, pages.head_dim
@@ -365,55 +395,56 @@ def pages_commit(pages: Pages, refs, table, length, k_tail, v_tail, k_new, v_new
     if path.shape[0] != b or (path.shape[1] > 1 and path.stride(1) != 1):
         _refuse(what, f"path {tuple(path.shape)} must be [{b}][M] with contiguous rows")
     _vector(what, "path_len", path_len, torch.int32, b, like)
-    where = _elsewhere(pages._dev, stream)
-    if where is not None:
-        with where:
-            return pages_commit(pages, refs, table, length, k_tail, v_tail, k_new, v_new, path, path_len, window, sinks)
-    need = pages._workspace(what, seqs, b)
-    full = torch.empty(b, dtype=torch.int32, device=pages.device)
-    work = torch.empty(need, dtype=torch.uint8, device=pages.device)
-    _check(_ops().ssd_pages_commit(pages._ref, C.byref(seqs), C.byref(tail), k_tail.data_ptr(), v_tail.data_ptr(),
-                                   C.byref(fresh), k_new.data_ptr(), v_new.data_ptr(), path.data_ptr(),
-                                   path.stride(0) if b > 1 else path.shape[1], path.shape[1], path_len.data_ptr(), window, sinks,
-                                   full.data_ptr(), work.data_ptr(), need, _raw_stream(pages._dev)), what)
-    return full
+    return (b, seqs.n_col, seqs.table_ld, C.byref(tail), C.byref(fresh), path.stride(0) if b > 1 else path.shape[1],
+            _workspace(what, pages, seqs))
 
 
 def pages_fork(refs, table, length, parents, k_tail, v_tail, page_rows: int, stream=None):
     """ssd_pages_fork: slot b becomes a copy of slot parents[b] (int32 [B]), which has to keep itself; itself: it stays as it
     is; any other value: it is freed."""
     what = "ssd_pages_fork"
-    _tensor(what, "table", table, (torch.int32,), 2)
-    seqs = _seqs(what, table, length, refs, table)
-    _vector(what, "parents", parents, torch.int32, seqs.n_seq, table)
-    tail = _tail(what, k_tail, v_tail, None, seqs.n_seq, None, None, table)
+
+    def make():
+        _tensor(what, "table", table, (torch.int32,), 2)
+        seqs = _seqs(what, table, length, refs, table)
+        _vector(what, "parents", parents, torch.int32, seqs.n_seq, table)
+        tail = _tail(what, k_tail, v_tail, None, seqs.n_seq, None, None, table)
+        return seqs.n_seq, seqs.n_col, seqs.table_ld, C.byref(tail)
+
+    b, c, ld, tail = _plan(_key(what, None, refs, table, length, parents, k_tail, v_tail), make)
     dev = table.get_device()
     where = _elsewhere(dev, stream)
     if where is not None:
         with where:
             return pages_fork(refs, table, length, parents, k_tail, v_tail, page_rows)
-    _check(_ops().ssd_pages_fork(C.byref(seqs), refs.shape[0], page_rows, parents.data_ptr(), C.byref(tail),
-                                 k_tail.shape[0], k_tail.shape[2], k_tail.shape[4], k_tail.data_ptr(), v_tail.data_ptr(),
-                                 _raw_stream(dev)), what)
+    seqs = _Seqs(b, c, ld, table.data_ptr(), length.data_ptr(), refs.data_ptr())
+    n_layer, _, g, _, w = k_tail.shape
+    _check(_ops().ssd_pages_fork(C.byref(seqs), refs.shape[0], page_rows, parents.data_ptr(), tail, n_layer, g, w,
+                                 k_tail.data_ptr(), v_tail.data_ptr(), _raw_stream(dev)), what)
 
 
 def pages_compact(pages: Pages, refs, table, stream=None):
     """ssd_pages_compact: moves the pages in use to the front of the pool; returns their number, int32 [1]."""
     what = "ssd_pages_compact"
     _pages(what, pages)
-    _tensor(what, "table", table, (torch.int32,), 2, pages.data)
-    _vector(what, "refs", refs, torch.int32, pages.n_page, pages.data)
-    b, c = table.shape
-    if c > 1 and table.stride(1) != 1:
-        _refuse(what, "table's last dimension must be contiguous")
+
+    def make():
+        _tensor(what, "table", table, (torch.int32,), 2, pages.data)
+        _vector(what, "refs", refs, torch.int32, pages.n_page, pages.data)
+        b, c = table.shape
+        if c > 1 and table.stride(1) != 1:
+            _refuse(what, "table's last dimension must be contiguous")
+        ld = table.stride(0) if b > 1 else max(c, table.stride(0))
+        at = refs.data_ptr()
+        return b, c, ld, _workspace(what, pages, _Seqs(b, c, ld, table.data_ptr(), at, at))
+
+    b, c, ld, need = _plan(_key(what, pages.kind, refs, table), make)
     where = _elsewhere(pages._dev, stream)
     if where is not None:
         with where:
             return pages_compact(pages, refs, table)
     # (lengths are not looked at)
-    seqs = _Seqs(b, c, table.stride(0) if b > 1 else max(c, table.stride(0)), table.data_ptr(), refs.data_ptr(),
-                 refs.data_ptr())
-    need = pages._workspace(what, seqs, b)
+    seqs = _Seqs(b, c, ld, table.data_ptr(), refs.data_ptr(), refs.data_ptr())
     used = torch.empty(1, dtype=torch.int32, device=pages.device)
     work = torch.empty(need, dtype=torch.uint8, device=pages.device)
     _check(_ops().ssd_pages_compact(pages._ref, C.byref(seqs), used.data_ptr(), work.data_ptr(), need,

@@ -117,9 +117,9 @@ def test_attention_refuses_shapes(kw, status):
 
 @pytest.mark.parametrize("kw,status", [
     (dict(q=None), INVALID), (dict(kt=None), INVALID), (dict(vt=None), INVALID), (dict(kn=None), INVALID), (dict(vn=None), INVALID),
-    (dict(out=None), INVALID), (dict(work=None), INVALID), (dict(q=MB + 8), UNSUPPORTED), (dict(vn=5 * MB + 2), UNSUPPORTED),
+    (dict(out=None), INVALID), (dict(work=None, s=seqs(n_col=500, table_ld=500)), INVALID), (dict(q=MB + 8), UNSUPPORTED), (dict(vn=5 * MB + 2), UNSUPPORTED),
     (dict(out=6 * MB + 4), UNSUPPORTED), (dict(anc=7 * MB + 4), INVALID), (dict(lse=7 * MB + 2), INVALID),
-    (dict(size=0), CAPACITY), (dict(work=16 * MB + 4), CAPACITY), (dict(out=MB), INVALID), (dict(out=MB + 16), INVALID),
+    (dict(size=0, s=seqs(n_col=500, table_ld=500)), CAPACITY), (dict(work=16 * MB + 4), CAPACITY), (dict(out=MB), INVALID), (dict(out=MB + 16), INVALID),
     (dict(out=2 * MB + 16 * 64), INVALID), (dict(out=5 * MB - 16), INVALID), (dict(out=3 * MB), INVALID)])
 def test_attention_refuses_buffers(kw, status):
     assert attn(**kw) == status
@@ -138,9 +138,9 @@ def test_workspaces_grow_with_the_call():
     a, b, L = C.c_size_t(0), C.c_size_t(0), paged._ops()
     assert L.ssd_pages_workspace(ref(pool()), ref(seqs()), C.byref(a)) == ssd.OK and a.value > 0
     assert L.ssd_pages_workspace(ref(pool(n_page=1000)), ref(seqs(n_seq=9)), C.byref(b)) == ssd.OK and b.value > a.value
-    assert L.ssd_paged_attn_workspace(ref(pool()), ref(seqs(n_seq=1)), ref(desc()), C.byref(a)) == ssd.OK and a.value > 0
+    assert L.ssd_paged_attn_workspace(ref(pool()), ref(seqs(n_seq=1)), ref(desc()), C.byref(a)) == ssd.OK
     assert L.ssd_paged_attn_workspace(ref(pool()), ref(seqs(n_seq=1, n_col=2000)), ref(desc()), C.byref(b)) == ssd.OK
-    assert b.value >= a.value
+    assert b.value > a.value
 
 
 # ---------------------------------------------------------------- blocks
