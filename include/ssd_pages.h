@@ -139,7 +139,7 @@ ssd_status ssd_paged_attn(const ssd_page_pool *pool, const ssd_page_seqs *seqs, 
  * first_layer + l, l < n_layer of the call, n < n.  Ids outside the pool are passed over.  A page that
  * ids names twice gets a block of either for each head, and keys or values: name it once.
  * ssd_pages_load is the way back: k and v get the values that the pages stand for, rounded once to
- * dtype; ids outside the pool give zeros.  rows of the desc is not used.  n_layer and n >= 0; 0
+ * dtype; ids outside the pool give zeros.  rows of the desc is not used.  n_layer and n >= 0, n at most 2^20; 0
  * does nothing.  k and v of ssd_pages_load lie apart, one behind the other.
  * Errors: SSD_E_INVALID_ARG, SSD_E_UNSUPPORTED, SSD_E_DEVICE. */
 ssd_status ssd_pages_store(const ssd_page_pool *pool, const int32_t *ids, int32_t n, int32_t first_layer,

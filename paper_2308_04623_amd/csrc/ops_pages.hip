@@ -44,6 +44,26 @@ __device__ __forceinline__ void store8(bf16_t* p, const float* x) {
   *(u32x4*)p = a;
 }
 
+// Sums over the lanes up to this one, and the largest of all, within the registers.
+__device__ __forceinline__ int lane_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // 1, 2, 4, 8 lanes before, within 16
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // the last of the 16 before, to every second 16
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31, to the upper 32
+  return x;
+}
+__device__ __forceinline__ unsigned lane_max(unsigned x) {
+  x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false));
+  x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false));
+  x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false));
+  x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false));
+  x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false));
+  x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false));
+  return (unsigned)__builtin_amdgcn_readlane((int)x, 63);
+}
+
 // How a block is coded (see ssd_pages.h), from the bits of its largest magnitude: as
 // whole numbers those of infinities and NaN are larger than all finite ones'.
 struct Coding {
@@ -134,9 +154,7 @@ __device__ __forceinline__ unsigned take_rows(bool values, int lane, Row row, fl
   unsigned most = 0;
 #pragma unroll
   for (int i = 0; i < kHeld<D>; ++i) most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);
-#pragma unroll
-  for (int o = 32; o; o >>= 1) most = max(most, (unsigned)__shfl_xor((int)most, o));
-  return most;
+  return lane_max(most);
 }
 // Their codes to the part at dst; lds: Part::BYTES of the wave's own.
 template <int D, int CODE>
@@ -210,7 +228,8 @@ __device__ __forceinline__ void put_values(bool values, int lane, const uint8_t*
 template <typename T, int D, int CODE, typename Row>
 __device__ __forceinline__ void code_block(const ssd_page_pool& p, bool there, int64_t block, bool values, Row row,
                                            uint8_t (*lds)[Part<D>::BYTES], unsigned (&most)[kWaveCount]) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = p.page_rows / 32, part = wave % waves;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = p.page_rows >> 5,
+            part = wave % waves;
   float x[kHeld<D>];
   unsigned bits = 0;
   if (there) bits = take_rows<T, D>(values, lane, [&](int r) { return row(32 * part + r); }, x);
@@ -233,29 +252,23 @@ struct BlockArgs {
   ssd_rows_desc d;
   const int* ids;
   char *k, *v;
-  int n, first_layer;
-  int64_t blocks;  // 2 (keys, values) for each head, page and layer
+  int first_layer;
+  unsigned blocks;  // of a layer: 2 (keys, values) for each head and page
 };
 struct BlockAt {
-  int64_t block, rows;  // the block's number in the pool, its rows' first element
+  int64_t block, rows;  // the block's number in the pool (-1: none), its rows' first element
   bool values, there;
 };
-__device__ __forceinline__ BlockAt block_at(const BlockArgs& a, int64_t i) {
+// blockIdx.y: the layer
+__device__ __forceinline__ BlockAt block_at(const BlockArgs& a, unsigned i) {
   BlockAt x;
   x.there = i < a.blocks;
   if (!x.there) i = 0;
-  x.values = i & 1;
-  i >>= 1;
-  const int g = (int)(i % a.p.n_kv_head);
-  i /= a.p.n_kv_head;
-  const int n = (int)(i % a.n), l = (int)(i / a.n);
+  const unsigned heads = 2 * a.p.n_kv_head, n = i / heads, gv = i - n * heads, l = blockIdx.y;
+  x.values = gv & 1;
   const int id = a.ids[n];
-  if (id < 0 || id >= a.p.n_page) {
-    x.block = -1;
-  } else {
-    x.block = ((((int64_t)(a.first_layer + l) * a.p.n_page + id) * a.p.n_kv_head + g) << 1) + x.values;
-  }
-  x.rows = l * a.d.layer + n * a.d.seq + g * a.d.head;
+  x.block = id < 0 || id >= a.p.n_page ? -1 : ((int64_t)(a.first_layer + l) * a.p.n_page + id) * heads + gv;
+  x.rows = l * a.d.layer + n * a.d.seq + (gv >> 1) * a.d.head;
   return x;
 }
 
@@ -264,8 +277,9 @@ template <typename T, int D, int CODE>
 __global__ __launch_bounds__(kThreads) void store_kernel(BlockArgs a) {
   __shared__ __align__(16) uint8_t lds[kWaveCount][Part<D>::BYTES];
   __shared__ unsigned most[kWaveCount];
-  const int waves = a.p.page_rows / 32, units = kWaveCount / waves, unit = (threadIdx.x >> 6) / waves;
-  for (int64_t first = (int64_t)blockIdx.x * units; first < a.blocks; first += (int64_t)gridDim.x * units) {
+  const int waves = a.p.page_rows >> 5, units = kWaveCount / waves,
+            unit = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / waves;
+  for (unsigned first = blockIdx.x * units; first < a.blocks; first += gridDim.x * units) {
     const BlockAt at = block_at(a, first + unit);
     const T* base = (const T*)(at.values ? a.v : a.k) + at.rows;
     code_block<T, D, CODE>(a.p, at.there && at.block >= 0, at.block, at.values,
@@ -275,9 +289,9 @@ __global__ __launch_bounds__(kThreads) void store_kernel(BlockArgs a) {
 template <typename T, int D, int CODE>
 __global__ __launch_bounds__(kThreads) void load_kernel(BlockArgs a) {
   __shared__ __align__(16) uint8_t lds[kWaveCount][Part<D>::BYTES];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = a.p.page_rows / 32, units = kWaveCount / waves,
-            unit = wave / waves, part = wave % waves;
-  for (int64_t first = (int64_t)blockIdx.x * units; first < a.blocks; first += (int64_t)gridDim.x * units) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = a.p.page_rows >> 5,
+            units = kWaveCount / waves, unit = wave / waves, part = wave % waves;
+  for (unsigned first = blockIdx.x * units; first < a.blocks; first += gridDim.x * units) {
     const BlockAt at = block_at(a, first + unit);
     if (!at.there) continue;
     T* base = (T*)(at.values ? a.v : a.k) + at.rows;
@@ -312,46 +326,56 @@ Work work_at(void* w, int n_seq, int n_page) {
 }
 size_t work_bytes(int n_seq, int n_page) { return 64 + 48 * (size_t)n_seq + 12 * (size_t)n_page; }
 
-// sums over the threads before this one, and over all
-__device__ __forceinline__ long long scan(long long x, long long* sums, long long& all) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  long long in = x;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const long long y = __shfl_up(in, o);
-    if (lane >= o) in += y;
-  }
-  if (lane == 63) sums[wave] = in;
+// Sums over the threads before this one, and over all.  A wave's is counted to 2^26 at the most: more than there
+// are pages, so what lies behind it gets none either way.
+__device__ __forceinline__ int scan(int x, int* sums, int& all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, upto = lane_scan(x);
+  if (lane == 63) sums[wave] = min(upto, 1 << 26);
   __syncthreads();
-  long long before = 0;
+  int before = 0;
   all = 0;
 #pragma unroll
   for (int w = 0; w < kPlan / 64; ++w) {
-    if (w < wave) before += sums[w];
-    all += sums[w];
+    const int y = sums[w];
+    before += w < wave ? y : 0;
+    all += y;
   }
   __syncthreads();
-  return before + in - x;
+  return before + upto - x;
 }
 // Writes the first `most` pages p in [from, to) whose refs are as asked to list, in order; how many there
 // are, up to those with which the search ended.
-constexpr int kLook = 16;  // refs a thread looks at
-__device__ __forceinline__ int find_pages(const int* refs, int from, int to, bool in_use, int* list, long long most,
-                                          long long* sums) {
-  long long found = 0;
+constexpr int kLook = 8;  // refs a thread looks at
+struct Refs {
+  int x[kLook];
+  __device__ __forceinline__ void load(const int* refs, int at, int to) {
+    if (at + kLook <= to) {
+      __builtin_memcpy(x, refs + at, sizeof(x));
+    } else {
+#pragma unroll
+      for (int i = 0; i < kLook; ++i) x[i] = at + i < to ? refs[at + i] : -1;
+    }
+  }
+};
+__device__ __forceinline__ int find_pages(const Refs* first, const int* refs, int from, int to, bool in_use, int* list, int most,
+                                          int* sums) {
+  int found = 0;
   for (int base = from; base < to && found < most; base += kPlan * kLook) {
     const int at = base + (int)threadIdx.x * kLook;
+    Refs r;
+    if (first && base == from) r = *first;
+    else r.load(refs, at, to);
     unsigned mask = 0;
 #pragma unroll
     for (int i = 0; i < kLook; ++i)
-      if (at + i < to && (refs[at + i] > 0) == in_use) mask |= 1u << i;
-    long long all;
-    long long rank = found + scan(__popc(mask), sums, all);
+      if (at + i < to && (r.x[i] > 0) == in_use) mask |= 1u << i;
+    int all;
+    int rank = found + scan(__popc(mask), sums, all);
     for (; mask; mask &= mask - 1, ++rank)
       if (rank < most) list[rank] = at + __ffs(mask) - 1;
     found += all;
   }
-  return (int)found;
+  return found;
 }
 
 struct PlanArgs {
@@ -369,53 +393,53 @@ struct PlanArgs {
 // slots.  Bound: latency, a chain of some ten loads and meetings.
 template <bool COMMIT>
 __global__ __launch_bounds__(kPlan) void plan_kernel(PlanArgs a) {
-  __shared__ int want[4096], first[4096];
-  __shared__ long long sums[kPlan / 64];
-  __shared__ int rows[COMMIT ? 4096 : 1], jobs;
+  __shared__ int want[4096], first[4096], col0[4096], sums[kPlan / 64], jobs;
+  __shared__ uint8_t rows[COMMIT ? 4096 : 1];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n_seq = a.s.n_seq;
+  // (what does not depend on anything is under way from the start)
+  Refs refs;
+  refs.load(a.s.refs, threadIdx.x * kLook, a.n_page);
+  int len[kPer], asked[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int b = threadIdx.x * kPer + i;
+    len[i] = b < n_seq ? a.s.length[b] : -1;
+    asked[i] = !COMMIT && b < n_seq ? a.count[b] : -1;
+  }
   if (threadIdx.x == 0) jobs = 0;
   if constexpr (COMMIT) {
     for (int b = wave; b < n_seq; b += kPlan / 64) {  // rows up to the path's first that is none
-      const int n = min(a.path_len[b], a.max_path);
-      bool bad = lane >= n;
-      if (!bad) {
-        const int t = a.path[b * a.path_ld + lane];
-        bad = t < 0 || t >= a.n_new;
-      }
-      const unsigned long long bads = __ballot(bad);
+      const int t = lane < a.max_path ? a.path[b * a.path_ld + lane] : -1, n = min(a.path_len[b], a.max_path);
+      const unsigned long long bads = __ballot(lane >= n || t < 0 || t >= a.n_new);
       if (lane == 0) rows[b] = bads ? __ffsll(bads) - 1 : 64;
     }
+    __syncthreads();
   }
-  __syncthreads();
-  int col[kPer], need[kPer], len[kPer];
+  int need[kPer], sum = 0;
   bool can[kPer];
-  long long sum = 0;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     const int b = threadIdx.x * kPer + i;
     can[i] = false;
-    need[i] = col[i] = len[i] = 0;
+    need[i] = 0;
     if (b >= n_seq) continue;
-    len[i] = a.s.length[b];
+    const int from = max(len[i], 0), col = from / a.page_rows;
     if constexpr (COMMIT) {
-      can[i] = len[i] >= 0;
-      col[i] = len[i] / a.page_rows;
-      const int64_t after = ((int64_t)len[i] + rows[b]) / a.page_rows;
-      can[i] = can[i] && after <= a.s.n_col;
-      need[i] = can[i] ? (int)after - col[i] : 0;
+      const int64_t after = ((int64_t)from + rows[b]) / a.page_rows;
+      can[i] = len[i] >= 0 && after <= a.s.n_col;
+      need[i] = can[i] ? (int)after - col : 0;
     } else {
-      const int n = a.count[b], from = max(len[i], 0);
-      col[i] = from / a.page_rows;
-      can[i] = n >= 0 && from % a.page_rows == 0 && (int64_t)col[i] + n <= a.s.n_col;
-      need[i] = can[i] ? n : 0;
+      can[i] = asked[i] >= 0 && from % a.page_rows == 0 && (int64_t)col + asked[i] <= a.s.n_col;
+      need[i] = can[i] ? asked[i] : 0;
     }
-    sum += need[i];
+    col0[b] = col;
+    sum += min(need[i], kMaxPages + 1);  // (more than there are: as good as any number)
   }
-  long long all;
-  long long rank = scan(sum, sums, all);
-  long long free = 0;
+  int all;
+  int rank = scan(sum, sums, all);
+  int free = 0;
   if (all > 0) {
-    free = find_pages(a.s.refs, 0, a.n_page, false, a.w.a, all < a.n_page ? all : a.n_page, sums);
+    free = find_pages(&refs, a.s.refs, 0, a.n_page, false, a.w.a, min(all, a.n_page), sums);
     __syncthreads();
   }
 #pragma unroll
@@ -424,11 +448,11 @@ __global__ __launch_bounds__(kPlan) void plan_kernel(PlanArgs a) {
     if (b >= n_seq) continue;
     const bool ok = can[i] && (need[i] == 0 || rank + need[i] <= free);
     want[b] = ok ? need[i] : 0;
-    first[b] = ok && need[i] ? (int)rank : 0;
-    rank += need[i];
+    first[b] = rank;
+    rank += min(need[i], kMaxPages + 1);
     if constexpr (COMMIT) {
       const int n = ok ? rows[b] : 0;
-      a.w.slot[b] = make_int4(len[i], n, want[b], ok);
+      a.w.slot[b] = make_int4(len[i], n, ok ? need[i] : 0, ok);
       a.got[b] = ok ? need[i] : len[i] < 0 ? 0 : -1;
       if (n) a.s.length[b] = len[i] + n;
     } else {
@@ -440,7 +464,7 @@ __global__ __launch_bounds__(kPlan) void plan_kernel(PlanArgs a) {
   for (int b = wave; b < n_seq; b += kPlan / 64) {
     const int n = want[b];
     if (n == 0) continue;
-    const int c = COMMIT ? a.w.slot[b].x / a.page_rows : a.s.length[b] / a.page_rows - n;
+    const int c = col0[b];
     int job = 0;
     if (COMMIT && lane == 0) job = atomicAdd(&jobs, n);  // (their order in the list changes no result)
     job = __shfl(job, 0);
@@ -475,8 +499,8 @@ struct CommitArgs {
 // items 16 bytes each, of `heads` heads' `rows` rows, four a thread under way: src(head, row), dst(head, row)
 // the row's first byte
 template <typename Src, typename Dst>
-__device__ __forceinline__ void copy_rows(int heads, int rows, int row_bytes, bool rows_outer, Src src, Dst dst) {
-  const int vec = row_bytes / 16, total = heads * rows * vec, inner = rows_outer ? heads : rows;
+__device__ __forceinline__ void copy_rows(int heads, int rows, int row_shift, bool rows_outer, Src src, Dst dst) {
+  const int total = heads * rows << row_shift, inner = rows_outer ? heads : rows;  // (a row: 2^row_shift times 16 bytes)
   constexpr int U = 4;
   for (int i0 = threadIdx.x; i0 < total; i0 += U * kThreads) {
     u32x4 x[U];
@@ -485,7 +509,8 @@ __device__ __forceinline__ void copy_rows(int heads, int rows, int row_bytes, bo
     for (int u = 0; u < U; ++u) {
       const int i = i0 + u * kThreads;
       if (i >= total) break;
-      const int v = i % vec, hr = i / vec, in = hr % inner, out = hr / inner;
+      const unsigned hr = (unsigned)i >> row_shift;
+      const int v = i & ((1 << row_shift) - 1), out = hr / (unsigned)inner, in = hr - out * inner;
       const int h = rows_outer ? in : out, r = rows_outer ? out : in;
       x[u] = *(const u32x4*)(src(h, r) + 16 * v);
       to[u] = dst(h, r) + 16 * v;
@@ -506,20 +531,19 @@ __global__ __launch_bounds__(kThreads) void commit_kernel(CommitArgs a) {
   __shared__ unsigned most[kWaveCount];
   const int R0 = a.p.page_rows, G = a.p.n_kv_head;
   if ((int)blockIdx.x < a.fill) {
-    const int waves = R0 / 32, units = kWaveCount / waves, unit = (threadIdx.x >> 6) / waves;
-    const int64_t blocks = (int64_t)a.w.head[0] * a.p.n_layer * G * 2;
+    const int waves = R0 >> 5, units = kWaveCount / waves, unit = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / waves;
+    const unsigned heads = 2 * G, each = a.p.n_layer * heads;  // (of a page)
+    const int64_t blocks = (int64_t)a.w.head[0] * each;
     for (int64_t at = (int64_t)blockIdx.x * units; at < blocks; at += (int64_t)a.fill * units) {
       int64_t i = at + unit;
       const bool there = i < blocks;
       if (!there) i = 0;
-      const bool values = i & 1;
-      i >>= 1;
-      const int g = (int)(i % G);
-      i /= G;
-      const int l = (int)(i % a.p.n_layer);
-      const int4 job = a.w.jobs[i / a.p.n_layer];
+      const unsigned which = blocks >> 32 ? (unsigned)(i / each) : (unsigned)i / each, at_page = (unsigned)(i - (int64_t)which * each);
+      const unsigned l = at_page / heads, gv = at_page - l * heads, g = gv >> 1;
+      const bool values = gv & 1;
+      const int4 job = a.w.jobs[which];
       const int b = job.x, len = a.w.slot[b].x;
-      const int64_t block = ((((int64_t)l * a.p.n_page + job.z) * G + g) << 1) + values;
+      const int64_t block = ((int64_t)l * a.p.n_page + job.z) * heads + gv;
       const T* old = (const T*)(values ? a.vt : a.kt) + l * a.tail.layer + b * a.tail.seq + g * a.tail.head;
       const T* add = (const T*)(values ? a.vn : a.kn) + l * a.fresh.layer + b * a.fresh.seq + g * a.fresh.head;
       code_block<T, D, CODE>(
@@ -559,7 +583,7 @@ __global__ __launch_bounds__(kThreads) void commit_kernel(CommitArgs a) {
   const int* path = a.path + b * a.path_ld + start;
   const int pos = slot.x + start;
   copy_rows(
-      G, n, D * (int)sizeof(T), true,
+      G, n, __builtin_ctz(D * sizeof(T) / 16), true,
       [&](int g, int r) { return add + (path[r] * a.fresh.row + g * a.fresh.head) * (int)sizeof(T); },
       [&](int g, int r) { return old + ((pos + r) % a.tail.rows * a.tail.row + g * a.tail.head) * (int)sizeof(T); });
 }
@@ -569,7 +593,7 @@ __global__ __launch_bounds__(kThreads) void commit_kernel(CommitArgs a) {
 struct ForkArgs {
   ssd_page_seqs s;
   ssd_rows_desc tail;
-  int n_page, page_rows, n_layer, n_kv_head, row_bytes;
+  int n_page, page_rows, n_layer, n_kv_head, row_shift;
   const int* parents;
   char *kt, *vt;
 };
@@ -600,7 +624,7 @@ __global__ __launch_bounds__(kThreads) void fork_kernel(ForkArgs a) {
   auto at = [&](int slot, int g, int r) {
     return base + (slot * a.tail.seq + g * a.tail.head + (pos + r) % a.tail.rows * a.tail.row) * es;
   };
-  copy_rows(a.n_kv_head, n, a.row_bytes, false, [&](int g, int r) { return (const char*)at(s, g, r); },
+  copy_rows(a.n_kv_head, n, a.row_shift, false, [&](int g, int r) { return (const char*)at(s, g, r); },
             [&](int g, int r) { return at(b, g, r); });
 }
 
@@ -613,15 +637,18 @@ struct CompactArgs {
   int* used;
 };
 __global__ __launch_bounds__(kPlan) void compact_plan_kernel(CompactArgs a) {
-  __shared__ long long sums[kPlan / 64];
+  __shared__ int sums[kPlan / 64];
   const int n = a.p.n_page;
+  Refs refs;
+  refs.load(a.s.refs, threadIdx.x * kLook, n);
   int count = 0;
-  for (int p = threadIdx.x; p < n; p += kPlan) count += a.s.refs[p] > 0;
-  long long all;
-  scan(count, sums, all);
-  const int u = (int)all;
-  const int holes = find_pages(a.s.refs, 0, u, false, a.w.a, n, sums);
-  const int movers = find_pages(a.s.refs, u, n, true, a.w.b, n, sums);  // (as many)
+#pragma unroll
+  for (int i = 0; i < kLook; ++i) count += refs.x[i] > 0;
+  for (int p = kPlan * kLook + threadIdx.x; p < n; p += kPlan) count += a.s.refs[p] > 0;
+  int u;
+  scan(count, sums, u);
+  const int holes = find_pages(&refs, a.s.refs, 0, u, false, a.w.a, n, sums);
+  const int movers = find_pages(nullptr, a.s.refs, u, n, true, a.w.b, n, sums);  // (as many)
   for (int p = u + threadIdx.x; p < n; p += kPlan) a.w.to[p] = p;
   __syncthreads();
   const int moves = min(holes, movers);
@@ -673,7 +700,7 @@ __global__ __launch_bounds__(kThreads) void compact_move_kernel(CompactArgs a) {
 
 // ---------------------------------------------------------------- host
 
-constexpr int kMostBlocks = 1 << 16;  // workgroups of kernels that take more work than that in turns
+constexpr unsigned kMostBlocks = 1 << 16;  // workgroups of kernels that take more work than that in turns
 
 template <typename F>
 void by_type(ssd_dtype t, int d, int code, F f) {
@@ -694,18 +721,17 @@ ssd_status blocks_args(const ssd_page_pool* pool, const int32_t* ids, int32_t n,
                        const ssd_rows_desc* d, const void* k, const void* v, bool written, BlockArgs* a) {
   ssd_status st = check_pool(pool);
   if (st != SSD_OK) return st;
-  OP_REQUIRE(n >= 0 && n <= (1 << 24), SSD_E_INVALID_ARG, "n outside [0, 2^24]");
+  OP_REQUIRE(n >= 0 && n <= kMaxPages, SSD_E_INVALID_ARG, "n outside [0, 2^20]");
   OP_REQUIRE(first_layer >= 0 && n_layer >= 0 && (int64_t)first_layer + n_layer <= pool->n_layer, SSD_E_INVALID_ARG,
              "layers outside the pool's");
   OP_REQUIRE(d, SSD_E_INVALID_ARG, "null rows");
   a->p = *pool;
   a->d = *d;
   a->ids = ids;
-  a->n = n;
   a->first_layer = first_layer;
   a->k = (char*)k;
   a->v = (char*)v;
-  a->blocks = (int64_t)n_layer * n * pool->n_kv_head * 2;
+  a->blocks = n_layer ? (unsigned)n * pool->n_kv_head * 2 : 0;  // (2^31 at the most)
   if (a->blocks == 0) return SSD_OK;
   OP_REQUIRE(ids && (uintptr_t)ids % 4 == 0, SSD_E_INVALID_ARG, "ids is null or not aligned");
   const RowDim dims[4] = {{n_layer, d->layer}, {n, d->seq}, {pool->n_kv_head, d->head}, {pool->page_rows, d->row}};
@@ -741,9 +767,10 @@ extern "C" ssd_status ssd_pages_store(const ssd_page_pool* pool, const int32_t* 
   const ssd_status st = blocks_args(pool, ids, n, first_layer, n_layer, d, k, v, false, &a);
   if (st != SSD_OK || a.blocks == 0) return st;
   by_type(d->dtype, pool->head_dim, pool->code, [&](auto t, auto dim, auto code) {
-    const int64_t units = kWaveCount / (pool->page_rows / 32), want = (a.blocks + units - 1) / units;
+    const unsigned units = kWaveCount / (pool->page_rows / 32), want = (a.blocks + units - 1) / units;
+    const dim3 grid(std::min(want, kMostBlocks), n_layer);
     store_kernel<decltype(t), dim.value, code.value>
-        <<<(unsigned)std::min<int64_t>(want, kMostBlocks), kThreads, 0, (hipStream_t)stream>>>(a);
+        <<<grid, kThreads, 0, (hipStream_t)stream>>>(a);
   });
   OP_LAUNCHED();
   return SSD_OK;
@@ -755,9 +782,10 @@ extern "C" ssd_status ssd_pages_load(const ssd_page_pool* pool, const int32_t* i
   const ssd_status st = blocks_args(pool, ids, n, first_layer, n_layer, d, k, v, true, &a);
   if (st != SSD_OK || a.blocks == 0) return st;
   by_type(d->dtype, pool->head_dim, pool->code, [&](auto t, auto dim, auto code) {
-    const int64_t units = kWaveCount / (pool->page_rows / 32), want = (a.blocks + units - 1) / units;
+    const unsigned units = kWaveCount / (pool->page_rows / 32), want = (a.blocks + units - 1) / units;
+    const dim3 grid(std::min(want, kMostBlocks), n_layer);
     load_kernel<decltype(t), dim.value, code.value>
-        <<<(unsigned)std::min<int64_t>(want, kMostBlocks), kThreads, 0, (hipStream_t)stream>>>(a);
+        <<<grid, kThreads, 0, (hipStream_t)stream>>>(a);
   });
   OP_LAUNCHED();
   return SSD_OK;
@@ -889,7 +917,7 @@ extern "C" ssd_status ssd_pages_fork(const ssd_page_seqs* seqs, int32_t n_page, 
   a.page_rows = page_rows;
   a.n_layer = n_layer;
   a.n_kv_head = n_kv_head;
-  a.row_bytes = head_dim * op_size(tail->dtype);
+  a.row_shift = __builtin_ctz(head_dim * op_size(tail->dtype) / 16);
   a.parents = parents;
   a.kt = (char*)k_tail;
   a.vt = (char*)v_tail;

@@ -295,21 +295,27 @@ def pages_load(pages: Pages, ids, dtype=torch.float32, layer: int = 0, n_layer: 
     `layer` on (default: all), as the values that the pages stand for; ids outside the pool give zeros."""
     what = "ssd_pages_load"
     _pages(what, pages)
-    _vector(what, "ids", ids, torch.int32, None, pages.data)
-    if dtype not in _DTYPES:
-        _refuse(what, f"dtype must be torch.float32 or torch.bfloat16, not {dtype}")
     if n_layer is None:
         n_layer = pages.n_layer - layer
-    if not 0 <= layer <= layer + n_layer <= pages.n_layer:
-        _refuse(what, f"layers {layer} .. {layer + n_layer} are not the pool's {pages.n_layer}")
+
+    def make():
+        _vector(what, "ids", ids, torch.int32, None, pages.data)
+        if dtype not in _DTYPES:
+            _refuse(what, f"dtype must be torch.float32 or torch.bfloat16, not {dtype}")
+        if not 0 <= layer <= layer + n_layer <= pages.n_layer:
+            _refuse(what, f"layers {layer} .. {layer + n_layer} are not the pool's {pages.n_layer}")
+        shape = n_layer, ids.shape[0], pages.n_kv_head, pages.page_rows, pages.head_dim
+        _, n, g, r, w = shape
+        return shape, C.byref(_Rows(_DTYPES[dtype], r, n * g * r * w, g * r * w, r * w, w))
+
+    shape, d = _plan(_key(what, (pages.kind, dtype, layer, n_layer), ids), make)
     where = _elsewhere(pages._dev, stream)
     if where is not None:
         with where:
             return pages_load(pages, ids, dtype, layer, n_layer)
-    n, g, r, w = ids.shape[0], pages.n_kv_head, pages.page_rows, pages.head_dim
-    k, v = torch.empty((2, n_layer, n, g, r, w), dtype=dtype, device=pages.device)
-    d = _Rows(_DTYPES[dtype], r, n * g * r * w, g * r * w, r * w, w)
-    _check(_ops().ssd_pages_load(pages._ref, ids.data_ptr(), n, layer, n_layer, C.byref(d), k.data_ptr(), v.data_ptr(),
+    k = torch.empty(shape, dtype=dtype, device=pages.device)
+    v = torch.empty(shape, dtype=dtype, device=pages.device)
+    _check(_ops().ssd_pages_load(pages._ref, ids.data_ptr(), shape[1], layer, n_layer, d, k.data_ptr(), v.data_ptr(),
                                  _raw_stream(pages._dev)), what)
     return k, v
 

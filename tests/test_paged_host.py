@@ -147,7 +147,7 @@ def test_workspaces_grow_with_the_call():
 
 @pytest.mark.parametrize("load", [False, True])
 @pytest.mark.parametrize("kw,status", [
-    (dict(n=-1), INVALID), (dict(n=(1 << 24) + 1), INVALID), (dict(first=-1), INVALID), (dict(layers=-1), INVALID),
+    (dict(n=-1), INVALID), (dict(n=(1 << 20) + 1), INVALID), (dict(first=-1), INVALID), (dict(layers=-1), INVALID),
     (dict(first=1), INVALID), (dict(first=2**31 - 1), INVALID), (dict(d=None), INVALID), (dict(ids=None), INVALID),
     (dict(ids=MB + 2), INVALID), (dict(k=None), INVALID), (dict(v=None), INVALID), (dict(k=2 * MB + 8), UNSUPPORTED),
     (dict(d=rows("pages", dtype=5)), INVALID), (dict(d=rows("pages", row=-64)), INVALID),
