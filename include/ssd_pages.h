@@ -99,7 +99,8 @@ typedef struct {
  * Head h reads the keys and values of head h / (n_head / n_kv_head).  out is the softmax of scale
  * q.k over the seen rows times their values; a query that sees no row (anc 0 and
  * nothing cached), or of a slot without a sequence, gives 0, and lse -infinity.  Rows that no query of
- * a sequence sees may hold anything, and a cached row whose table entry is no page of the
+ * a sequence sees may hold anything (in pages of which it sees other rows, anything but e4m3's codes of NaN, which
+ * ssd_pages_store never writes), and a cached row whose table entry is no page of the
  * pool is not seen.  A row whose score is -infinity counts as one that is not seen; a score
  * that is NaN or +infinity makes the query's out and lse NaN; an element that is not finite
  * among the values of a seen row makes that element of out NaN.
@@ -171,7 +172,8 @@ ssd_status ssd_pages_take(const ssd_page_pool *pool, const ssd_page_seqs *seqs, 
  * are given back: their entries become -1.
  * Tail and new rows have one dtype; tail rows >= page_rows + new rows - 1; 1 <= new rows <= 64;
  * layers are the pool's.  Buffers share no bytes.
- * Errors: SSD_E_INVALID_ARG, SSD_E_CAPACITY (workspace), SSD_E_UNSUPPORTED, SSD_E_DEVICE. */
+ * Errors: SSD_E_INVALID_ARG, SSD_E_CAPACITY (workspace, or slots and layers for 2^24 workgroups), SSD_E_UNSUPPORTED,
+ * SSD_E_DEVICE. */
 ssd_status ssd_pages_commit(const ssd_page_pool *pool, const ssd_page_seqs *seqs, const ssd_rows_desc *tail,
                             void *k_tail, void *v_tail, const ssd_rows_desc *fresh, const void *k_new,
                             const void *v_new, const int32_t *path, int64_t path_ld, int32_t max_path,

@@ -496,6 +496,9 @@ struct CommitArgs {
   int fill;  // workgroups that fill pages
 };
 
+// the place of a row that lies less than a ring's `rows` behind its start
+__device__ __forceinline__ int64_t ring(int at, int rows) { return at >= rows ? at - rows : at; }
+
 // items 16 bytes each, of `heads` heads' `rows` rows, four a thread under way: src(head, row), dst(head, row)
 // the row's first byte
 template <typename Src, typename Dst>
@@ -546,12 +549,12 @@ __global__ __launch_bounds__(kThreads) void commit_kernel(CommitArgs a) {
       const int64_t block = ((int64_t)l * a.p.n_page + job.z) * heads + gv;
       const T* old = (const T*)(values ? a.vt : a.kt) + l * a.tail.layer + b * a.tail.seq + g * a.tail.head;
       const T* add = (const T*)(values ? a.vn : a.kn) + l * a.fresh.layer + b * a.fresh.seq + g * a.fresh.head;
+      const int pos = job.y * R0, place = pos % a.tail.rows;
+      const int* path = a.path + b * a.path_ld - (len - pos);
       code_block<T, D, CODE>(
           a.p, there, block, values,
           [&](int r) {
-            const int pos = job.y * R0 + r;
-            return pos < len ? old + pos % a.tail.rows * a.tail.row
-                             : add + a.path[b * a.path_ld + pos - len] * a.fresh.row;
+            return r < len - pos ? old + ring(place + r, a.tail.rows) * a.tail.row : add + path[r] * a.fresh.row;
           },
           lds, most);
     }
@@ -581,11 +584,11 @@ __global__ __launch_bounds__(kThreads) void commit_kernel(CommitArgs a) {
   char* old = (values ? a.vt : a.kt) + (l * a.tail.layer + b * a.tail.seq) * (int)sizeof(T);
   const char* add = (values ? a.vn : a.kn) + (l * a.fresh.layer + b * a.fresh.seq) * (int)sizeof(T);
   const int* path = a.path + b * a.path_ld + start;
-  const int pos = slot.x + start;
+  const int place = (slot.x + start) % a.tail.rows;
   copy_rows(
       G, n, __builtin_ctz(D * sizeof(T) / 16), true,
       [&](int g, int r) { return add + (path[r] * a.fresh.row + g * a.fresh.head) * (int)sizeof(T); },
-      [&](int g, int r) { return old + ((pos + r) % a.tail.rows * a.tail.row + g * a.tail.head) * (int)sizeof(T); });
+      [&](int g, int r) { return old + (ring(place + r, a.tail.rows) * a.tail.row + g * a.tail.head) * (int)sizeof(T); });
 }
 
 // ---------------------------------------------------------------- fork
@@ -619,10 +622,10 @@ __global__ __launch_bounds__(kThreads) void fork_kernel(ForkArgs a) {
   if (!kept) return;
   const int len = a.s.length[s];
   if (len <= 0) return;
-  const int n = len % a.page_rows, pos = len - n, l = (blockIdx.x - 1) >> 1, es = a.tail.dtype == SSD_F32 ? 4 : 2;
+  const int n = len % a.page_rows, place = (len - n) % a.tail.rows, l = (blockIdx.x - 1) >> 1, es = a.tail.dtype == SSD_F32 ? 4 : 2;
   char* base = (blockIdx.x - 1 & 1 ? a.vt : a.kt) + l * a.tail.layer * es;
   auto at = [&](int slot, int g, int r) {
-    return base + (slot * a.tail.seq + g * a.tail.head + (pos + r) % a.tail.rows * a.tail.row) * es;
+    return base + (slot * a.tail.seq + g * a.tail.head + ring(place + r, a.tail.rows) * a.tail.row) * es;
   };
   copy_rows(a.n_kv_head, n, a.row_shift, false, [&](int g, int r) { return (const char*)at(s, g, r); },
             [&](int g, int r) { return at(b, g, r); });
@@ -852,6 +855,10 @@ extern "C" ssd_status ssd_pages_commit(const ssd_page_pool* pool, const ssd_page
   for (const void* t : {(const void*)k_tail, (const void*)v_tail})
     for (const void* x : {k_new, v_new})
       OP_REQUIRE(!op_overlap(t, te, x, ne), SSD_E_INVALID_ARG, "the tail shares memory with the new rows");
+  const int units = kWaveCount / (pool->page_rows / 32);
+  const int fill = (int)std::min<int64_t>(((int64_t)seqs->n_seq * pool->n_layer * pool->n_kv_head * 2 + units - 1) / units, 1024);
+  const int64_t blocks = fill + (int64_t)seqs->n_seq * (1 + 2 * pool->n_layer);
+  OP_REQUIRE(blocks < (1 << 24), SSD_E_CAPACITY, "more workgroups than a grid holds");
   const Work w = work_at(workspace, seqs->n_seq, pool->n_page);
   PlanArgs p{};
   p.s = *seqs;
@@ -880,10 +887,7 @@ extern "C" ssd_status ssd_pages_commit(const ssd_page_pool* pool, const ssd_page
   a.path_ld = path_ld;
   a.window = window;
   a.sinks = sinks;
-  const int units = kWaveCount / (pool->page_rows / 32);
-  a.fill = (int)std::min<int64_t>(((int64_t)seqs->n_seq * pool->n_layer * pool->n_kv_head * 2 + units - 1) / units, 1024);
-  const int64_t blocks = a.fill + (int64_t)seqs->n_seq * (1 + 2 * pool->n_layer);
-  OP_REQUIRE(blocks < (1 << 24), SSD_E_CAPACITY, "more workgroups than a grid holds");
+  a.fill = fill;
   by_type(tail->dtype, pool->head_dim, pool->code, [&](auto t, auto dim, auto code) {
     commit_kernel<decltype(t), dim.value, code.value><<<(unsigned)blocks, kThreads, 0, (hipStream_t)stream>>>(a);
   });

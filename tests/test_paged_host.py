@@ -201,6 +201,13 @@ def test_commit_refuses(kw, status):
     assert commit(**kw) == status
 
 
+def test_commit_refuses_more_workgroups_than_a_grid_holds():
+    big = dict(p=pool(n_layer=4096), s=seqs(n_seq=4096), tail=rows("tail", layer=4096 * 4 * 39 * 64),
+               fresh=rows("new", layer=4096 * 8 * 256), kt=1 << 44, vt=1 << 45, kn=1 << 46, vn=1 << 47)
+    assert commit(**big) == CAPACITY
+    assert b"grid" in paged._ops().ssd_last_error()
+
+
 @pytest.mark.parametrize("kw", [dict(count=None), dict(got=None), dict(count=MB + 1), dict(got=MB + 2)])
 def test_take_refuses(kw):
     v = dict(count=MB, got=2 * MB)
