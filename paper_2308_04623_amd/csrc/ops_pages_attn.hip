@@ -121,6 +121,16 @@ struct Codes {
   }
 };
 
+// the largest of eight, NaN passed over (one instruction for three: fmaxf would have each operand made quiet first)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float x;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(x) : "v"(a), "v"(b), "v"(c));
+  return x;
+}
+__device__ __forceinline__ float largest(f32x4 a, f32x4 b) {
+  return max3(max3(a[0], a[1], a[2]), max3(a[3], b[0], b[1]), max3(b[2], b[3], b[3]));
+}
+
 // What a wave knows of its call, whichever way it takes its queries.  Lane 16 g + n.
 template <typename T, int D, int CODE_>
 struct Base {
@@ -346,8 +356,7 @@ struct Tiles : Base<T, D, CODE> {
             s[nt][k][r] = seen(nt, k, r) ? s[nt][k][r] * by[nt] : -INFINITY;
         by[nt] = 1.f;
       }
-      top[nt] = by[nt] * fmaxf(fmaxf(fmaxf(s[nt][0][0], s[nt][0][1]), fmaxf(s[nt][0][2], s[nt][0][3])),
-                               fmaxf(fmaxf(s[nt][1][0], s[nt][1][1]), fmaxf(s[nt][1][2], s[nt][1][3])));
+      top[nt] = by[nt] * largest(s[nt][0], s[nt][1]);
       far |= top[nt] > m[nt] + kSlack;
     }
     if (__builtin_amdgcn_ballot_w64(far)) {
@@ -407,6 +416,7 @@ struct Tiles : Base<T, D, CODE> {
     }
     complete<2 * NT>(&s[0][0]);
     if (kscale < 0.f) {
+      asm volatile("");  // (a branch, not selects: stored pages have no such scale)
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) s[nt][0] = -s[nt][0], s[nt][1] = -s[nt][1];
     }
@@ -421,27 +431,28 @@ struct Tiles : Base<T, D, CODE> {
     });
     float f;
     if (B::new_unit(fabsf(vscale), f)) scale_o(f);
-    float rel = vscale * vrel;
+    const float rel = vscale * vrel;
+    f16x8 w[NT][NP];
     if (masked && !(fabsf(rel) < __builtin_inff())) {  // rows that a query does not see count 0 whatever the scale
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (s[nt][i >> 2][i & 3] != 0.f) s[nt][i >> 2][i & 3] = __builtin_nanf("");
-      rel = 1.f;
-    }
-    f16x8 w[NT][NP];
+        for (int p = 0; p < NP; ++p)
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+          for (int i = 0; i < 8; ++i) w[nt][p][i] = (_Float16)(s[nt][i >> 2][i & 3] == 0.f ? 0.f : __builtin_nanf(""));
+    } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float y = s[nt][i >> 2][i & 3] * rel;
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int p = 0; p < NP; ++p) {
-          w[nt][p][i] = (_Float16)y;
-          y -= (float)w[nt][p][i];
+        for (int i = 0; i < 8; ++i) {
+          float y = s[nt][i >> 2][i & 3] * rel;
+#pragma unroll
+          for (int p = 0; p < NP; ++p) {
+            w[nt][p][i] = (_Float16)y;
+            y -= (float)w[nt][p][i];
+          }
         }
-      }
+    }
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
       const f16x8 y = c.template values<CODE>(dt);
@@ -586,7 +597,8 @@ struct Seen {
 // Long sequences are cut by their own lengths: each into the nearest number of parts of an equal share of all rows
 // (one at the least), parts of a head side by side, sequence by sequence.  So a batch of one long and many short
 // ones fills the chip too.  (Every wave finds its part by itself: the lengths are in its lanes.)
-constexpr int kLeast = 16;  // 32 rows each of a part: four for each wave
+constexpr int kLeast = 24;  // 32 rows each of a part: six for each wave
+constexpr int kRound = 512;  // workgroups that sequences are cut for: two a CU
 constexpr int kLong = 512;  // from this many on, sequences are cut by their own lengths
 struct Part {
   int b, j, n;  // part j of n of sequence b,
@@ -654,20 +666,20 @@ __global__ __launch_bounds__(64 * kWaves, W::DIM == 128 || W::COLS == 32 || W::F
   typedef typename W::Type T;
   constexpr int D = W::DIM, COLS = W::COLS;
   extern __shared__ __align__(16) float lds[];
-  // the sequences' workgroups of one head and part run side by side on one XCD (blocks go round the XCDs), and
-  // so do a part's tiles of queries: pages that they share are in its L2
-  const int xcd = blockIdx.x & 7, tile = blockIdx.x >> 3;
+  // Blocks go round the XCDs: a part's tiles of queries run side by side on one of them, so that its pages are
+  // read once into that L2, and the parts are spread evenly.
+  const int xcd = blockIdx.x & 7, tile = blockIdx.x >> 3, unit = (blockIdx.z * gridDim.y + blockIdx.y) * 8 + xcd;
   int b, kv, split, splits, at;
   if (a.splits) {
-    const int hs = blockIdx.z * 8 + xcd;
-    if (hs >= a.n_kv_head * a.splits) return;
     splits = a.splits;
-    split = splits == 1 ? 0 : hs / a.n_kv_head;
-    kv = hs - split * a.n_kv_head;
-    b = blockIdx.y;
+    const int rest = unit / a.n_kv_head;
+    kv = unit - rest * a.n_kv_head;
+    split = splits == 1 ? 0 : rest / a.n_seq;
+    b = rest - split * a.n_seq;
+    if (split >= splits || b >= a.n_seq) return;
     at = (b * a.n_kv_head + kv) * splits + split;
   } else {
-    const Part p = find_part<false>(a, (blockIdx.z * gridDim.y + blockIdx.y) * 8 + xcd);
+    const Part p = find_part<false>(a, unit);
     if (p.kv >= a.n_kv_head || p.at >= a.parts) return;
     b = __builtin_amdgcn_readfirstlane(p.b);
     kv = __builtin_amdgcn_readfirstlane(p.kv);
@@ -697,14 +709,18 @@ __global__ __launch_bounds__(64 * kWaves, W::DIM == 128 || W::COLS == 32 || W::F
     const Seen look(a, len, shift);
     const int sinks = look.sinks, from = look.from, count = look.count;
     const int first_full = a.d.window ? len + a.d.n_query - a.d.window : 0;  // all queries see rows from here on
-    // lane j: the page of item k0 + j of this wave's, and its scales
-    int page = -1;
+    // lane j, of item k0 + j of this wave's: its page, the page's scales, where its bytes begin and its first row's position
+    int page = -1, first = 0;
     float2 sc = {0.f, 0.f};
+    int64_t bytes = 0;
     auto find = [&](int k0) {
-      const int i = item(k0 + lane), v = i >> shift, c = v < sinks ? v : v - sinks + from;
+      const int i = item(k0 + lane), v = i >> shift, c = v < sinks ? v : v - sinks + from, row = 32 * (i & (per - 1));
       page = a.d.window == 0 && k0 == 0 ? entry : i < count ? table[c] : -1;
       if (i >= count || (unsigned)page >= (unsigned)a.n_page) page = -1;
-      sc = a.scale[(int64_t)max(page, 0) * a.n_kv_head + kv];
+      const int64_t block = (int64_t)max(page, 0) * a.n_kv_head + kv;  // (without one: page 0, for all waves the same)
+      sc = a.scale[block];
+      bytes = block * (2 * R0 * D) + row * D;
+      first = c * R0 + row;
     };
     find(0);
     w.begin(len);
@@ -718,24 +734,23 @@ __global__ __launch_bounds__(64 * kWaves, W::DIM == 128 || W::COLS == 32 || W::F
       }
     }
     w.split();
-    const int64_t head_bytes = 2 * (int64_t)R0 * D;
     const int soon = slow * others, rest = count - item0;
     const int items = rest <= 0 ? 0 : rest <= soon ? (rest + others - 1) / others : slow + (rest - soon + all - 1) / all;
     for (int k0 = 0; k0 < items; k0 += 64) {
       if (k0) find(k0);
       auto fetch = [&](Codes<D>& x, int k) {
-        // (lanes past the last item have no page: page 0, for all waves the same)
-        const int id = max(__builtin_amdgcn_readlane(page, min(k - k0, 63)), 0);
-        const uint8_t* block = a.data + ((int64_t)id * a.n_kv_head + kv) * head_bytes + (item(k) & (per - 1)) * (32 * D);
+        const int j = min(k - k0, 63);
+        const uint8_t* block = a.data + ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)bytes, j) |
+                                         (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(bytes >> 32), j) << 32);
         x.load(block, block + R0 * D, lane);
       };
       auto work = [&](const Codes<D>& x, int k) {
-        const int j = k - k0, i = item(k), v = i >> shift, col = v < sinks ? v : v - sinks + from;
+        const int j = k - k0;
         if (__builtin_amdgcn_readlane(page, j) < 0) return;
         const float ks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sc.x), j));
         const float vs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sc.y), j));
-        const int first = col * R0 + (i & (per - 1)) * 32;
-        w.take(x, ks, vs, first, first < first_full && first + 32 > a.d.sinks);
+        const int at = __builtin_amdgcn_readlane(first, j);
+        w.take(x, ks, vs, at, at < first_full && at + 32 > a.d.sinks);
       };
       // Loads run ST - 1 items ahead, past the last item, too: were they under a condition, the compiler would have to
       // wait as if they had not been issued, for those of the next items with the item's own.
@@ -855,18 +870,17 @@ Plan plan(const ssd_page_pool& p, const ssd_page_seqs& s, const ssd_paged_attn_d
   if (d.window)
     pages = std::min<int64_t>(pages, div_up(std::min<int64_t>(d.sinks, 1 << 30), p.page_rows) + d.window / p.page_rows + 2);
   const int64_t units = (int64_t)s.n_seq * p.n_kv_head * x.tiles, steps = pages * (p.page_rows / 32);
-  const int64_t round = p.head_dim == 128 || x.cols == 32 || d.dtype == SSD_F32 ? 512 : 768;
+  const int64_t round = kRound;
   const int64_t heads = (int64_t)s.n_seq * p.n_kv_head;
   // (numbers of 32 rows of all queries are 32-bit where the device counts them)
   if (s.n_seq > 1 && steps > kLong && units * steps < (1 << 30)) {
     x.round = (int)round;
     x.parts = div_up(heads + div_up(round, x.tiles), 8) * 8;
-    x.blocks = x.parts * x.tiles;
   } else {
     x.splits = (int)std::max<int64_t>(1, std::min<int64_t>(round / units, div_up(steps, kLeast)));
-    x.parts = heads * x.splits;
-    x.blocks = div_up((int64_t)p.n_kv_head * x.splits, 8) * 8 * s.n_seq * x.tiles;
+    x.parts = div_up(heads * x.splits, 8) * 8;
   }
+  x.blocks = x.parts * x.tiles;
   if (x.splits == 1) return x;
   x.o_bytes = (size_t)x.parts * x.tiles * x.cols * p.head_dim * 4;
   x.bytes = x.o_bytes + (size_t)x.parts * x.tiles * x.cols * sizeof(float2);
@@ -889,8 +903,7 @@ hipError_t launch(const Args& a, const Plan& p, hipStream_t s) {
     }
   }
   const int64_t rows = 32768;  // (of a grid's dimensions, 65535 at the most)
-  const dim3 grid = p.splits ? dim3(8 * p.tiles, a.n_seq, (unsigned)div_up((int64_t)a.n_kv_head * p.splits, 8))
-                             : dim3(8 * p.tiles, (unsigned)std::min(p.parts / 8, rows), (unsigned)div_up(p.parts / 8, rows));
+  const dim3 grid(8 * p.tiles, (unsigned)std::min(p.parts / 8, rows), (unsigned)div_up(p.parts / 8, rows));
   paged_attn_kernel<W><<<grid, 64 * kWaves, lds, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;

@@ -127,11 +127,11 @@ def test_attention_refuses_buffers(kw, status):
 
 def test_attention_refuses_more_workgroups_than_a_grid_holds():
     n = C.c_size_t(0)
-    p, s = pool(n_kv_head=1), seqs(n_seq=4096)
-    big = desc(n_query=64, n_head=1024)
-    assert paged._ops().ssd_paged_attn_workspace(ref(p), ref(s), ref(big), C.byref(n)) == CAPACITY
-    assert attn(p, s, big) == CAPACITY
-    assert paged._ops().ssd_paged_attn_workspace(ref(p), ref(s), ref(desc(n_query=16, n_head=64)), C.byref(n)) == ssd.OK
+    p, s = pool(n_kv_head=1, head_dim=128), seqs(n_seq=4096)
+    big = dict(n_query=64, n_head=1024, dtype=ssd.F32)  # 4096 tiles of 16 queries for each sequence
+    assert paged._ops().ssd_paged_attn_workspace(ref(p), ref(s), ref(desc(**big)), C.byref(n)) == CAPACITY
+    assert attn(p, s, desc(**big)) == CAPACITY
+    assert paged._ops().ssd_paged_attn_workspace(ref(p), ref(s), ref(desc(**{**big, "n_query": 63})), C.byref(n)) == ssd.OK
 
 
 def test_workspaces_grow_with_the_call():
