@@ -29,6 +29,11 @@ class Batch:
         cfg = model.cfg
         if not isinstance(model, ssd.Model) or model.q8:
             raise ValueError("a batch needs a Model with its weights as they are, not a view or 8-bit codes")
+        if n_seq < 1 or not 1 <= max_nodes <= 64 or max_ctx < 0 or page_rows not in (32, 64, 128):
+            raise ValueError(f"{n_seq} sequences, {max_nodes} nodes (1 to 64), {max_ctx} rows in pages of {page_rows} (32, 64 or "
+                             "128)")
+        if window < 0 or sinks < 0 or 0 < window < max_nodes:
+            raise ValueError(f"a window of {window} rows and {sinks} sinks for {max_nodes} nodes")
         n_col = max_ctx // page_rows
         if (n_col + 1) * page_rows + max_nodes > cfg.n_pos + 1:
             raise ValueError(f"{max_ctx} rows, an open page of {page_rows} and {max_nodes} nodes: more than the model's "
@@ -51,6 +56,10 @@ class Batch:
         """The first prefix_len rows of a session's cache become the sequence of a slot without one."""
         if not 0 <= slot < self.n_seq or not 0 <= prefix_len <= session.max_ctx:
             raise ValueError(f"slot {slot}, {prefix_len} rows: outside the batch or the session's cache")
+        like, cache = self.k_tail, session.k_cache
+        if (cache.dtype, cache.device, cache.shape[0], cache.shape[1], cache.shape[3]) != \
+                (like.dtype, like.device, like.shape[0], like.shape[2], like.shape[4]):
+            raise ValueError("the session's cache is not of the batch's model's shape")
         if int(self.length[slot]) >= 0:
             raise ValueError(f"slot {slot} holds a sequence")
         rows, full = self.page_rows, prefix_len // self.page_rows

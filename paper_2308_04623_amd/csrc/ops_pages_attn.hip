@@ -941,7 +941,8 @@ ssd_status check(const ssd_page_pool* pool, const ssd_page_seqs* seqs, const ssd
              "tail_rows below page_rows, or 2^30");
   OP_REQUIRE(a->window >= 0 && a->sinks >= 0 && (a->window == 0 || a->window >= a->n_query), SSD_E_INVALID_ARG,
              "window or sinks is negative, or the window is shorter than n_query");
-  OP_REQUIRE(isfinite(a->scale), SSD_E_INVALID_ARG, "scale must be finite");
+  OP_REQUIRE(isfinite(a->scale * 1.4426950408889634f), SSD_E_INVALID_ARG,
+             "scale, and scale times log2 e, must be finite");
   return SSD_OK;
 }
 

@@ -113,6 +113,13 @@ class Pages:
                    torch.zeros(shape, dtype=torch.float32, device=device), page_rows, code)
 
 
+def _counts(what, **values):
+    """They are what the descriptions' 32 bits hold (where ctypes would drop the others)."""
+    for name, x in values.items():
+        if not 0 <= ops.operator.index(x) < 1 << 31:
+            _refuse(what, f"{name} is {x}, not a number from 0 on of 31 bits")
+
+
 def _pages(what, pages):
     if not isinstance(pages, Pages):
         _refuse(what, "pages must be a paged.Pages")
@@ -175,6 +182,7 @@ def _key(what, values, *tensors):
 # ---------------------------------------------------------------- attention
 
 def _attn_plan(q, pages, table, length, k_tail, v_tail, k_new, v_new, layer, anc, window, sinks, scale, out):
+    _counts("ssd_paged_attn", layer=layer, window=window, sinks=sinks)
     _refuse_attn(q, pages, table, length, k_tail, v_tail, k_new, v_new, anc, out)
     b, t, h, d = q.shape
     g, r = k_tail.shape[1:3]
@@ -281,7 +289,8 @@ def pages_store(pages: Pages, ids, k, v, layer: int = 0, stream=None):
     x.unflatten(2, (n, page_rows)).transpose(1, 2)."""
     what = "ssd_pages_store"
     _pages(what, pages)
-    d = _plan(_key(what, pages.kind, ids, k, v), lambda: C.byref(_block_rows(what, pages, ids, k, v)))
+    d = _plan(_key(what, (pages.kind, layer), ids, k, v),
+              lambda: _counts(what, layer=layer) or C.byref(_block_rows(what, pages, ids, k, v)))
     where = _elsewhere(pages._dev, stream)
     if where is not None:
         with where:
@@ -367,8 +376,9 @@ def pages_commit(pages: Pages, refs, table, length, k_tail, v_tail, k_new, v_new
     what = "ssd_pages_commit"
     _pages(what, pages)
     b, c, ld, tail, fresh, path_ld, need = _plan(
-        _key(what, pages.kind, refs, table, length, k_tail, v_tail, k_new, v_new, path, path_len),
-        lambda: _commit_plan(what, pages, refs, table, length, k_tail, v_tail, k_new, v_new, path, path_len))
+        _key(what, (pages.kind, window, sinks), refs, table, length, k_tail, v_tail, k_new, v_new, path, path_len),
+        lambda: _counts(what, window=window, sinks=sinks) or
+        _commit_plan(what, pages, refs, table, length, k_tail, v_tail, k_new, v_new, path, path_len))
     where = _elsewhere(pages._dev, stream)
     if where is not None:
         with where:
@@ -411,13 +421,14 @@ def pages_fork(refs, table, length, parents, k_tail, v_tail, page_rows: int, str
     what = "ssd_pages_fork"
 
     def make():
+        _counts(what, page_rows=page_rows)
         _tensor(what, "table", table, (torch.int32,), 2)
         seqs = _seqs(what, table, length, refs, table)
         _vector(what, "parents", parents, torch.int32, seqs.n_seq, table)
         tail = _tail(what, k_tail, v_tail, None, seqs.n_seq, None, None, table)
         return seqs.n_seq, seqs.n_col, seqs.table_ld, C.byref(tail)
 
-    b, c, ld, tail = _plan(_key(what, None, refs, table, length, parents, k_tail, v_tail), make)
+    b, c, ld, tail = _plan(_key(what, page_rows, refs, table, length, parents, k_tail, v_tail), make)
     dev = table.get_device()
     where = _elsewhere(dev, stream)
     if where is not None:

@@ -137,3 +137,14 @@ def test_refusals(env):
         b.verify(tokens[:, :3], [[-1, 0, 1], [-1, 0, 1]])
     with pytest.raises(ValueError):
         batch.Batch(session.model, 2, 256, 4)
+    for kw in (dict(max_nodes=65), dict(max_nodes=0), dict(n_seq=0), dict(page_rows=48), dict(window=3), dict(sinks=-1)):
+        with pytest.raises(ValueError):
+            batch.Batch(**{**dict(model=session.model, n_seq=2, max_ctx=96, max_nodes=4), **kw})
+    # another model's cache is refused before pages are taken for it
+    cfg = W.TINY.with_(dtype="bf16")
+    other = ssd.Session(ssd.Model(cfg, W.make_weights(cfg, 0)), 160, 64)
+    b.fork([0, -1])
+    used = b.refs.clone()
+    with pytest.raises(ValueError):
+        b.admit(1, other, 40)
+    assert torch.equal(b.refs, used) and int(b.length[1]) == -1

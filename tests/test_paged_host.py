@@ -108,7 +108,7 @@ def test_sequences_are_checked(kw, status):
     (dict(dtype=2), INVALID), (dict(layer=2), INVALID), (dict(layer=-1), INVALID), (dict(n_query=0), INVALID),
     (dict(n_query=65), INVALID), (dict(n_head=6), INVALID), (dict(n_head=0), INVALID), (dict(n_head=1028), INVALID),
     (dict(tail_rows=31), INVALID), (dict(tail_rows=1 << 30), INVALID), (dict(window=-1), INVALID), (dict(sinks=-1), INVALID),
-    (dict(window=7), INVALID), (dict(scale=float("nan")), INVALID), (dict(scale=float("inf")), INVALID),
+    (dict(window=7), INVALID), (dict(scale=float("nan")), INVALID), (dict(scale=float("inf")), INVALID), (dict(scale=3e38), INVALID),
     (dict(q_row=516), UNSUPPORTED), (dict(tail_row=65), UNSUPPORTED), (dict(new_head=-64), INVALID), (dict(out_head=0), INVALID),
     (dict(out_row=448), INVALID), (dict(out_seq=7 * 512), INVALID), (dict(out_head=512, out_row=128), INVALID)])
 def test_attention_refuses_shapes(kw, status):
@@ -247,6 +247,22 @@ def test_the_binding_refuses_host_tensors():
         paged.pages_store(data, x, data, data)
     with pytest.raises(ssd.SSDError):
         paged.paged_attention(data, data, x, x, x, x, x, x)
+
+
+def test_the_binding_refuses_numbers_past_32_bits():
+    # (they would lose their upper bits on the way: a window of 2^32 rows would be none)
+    pages = object.__new__(paged.Pages)
+    pages.kind = ()
+    for kw in (dict(window=1 << 32), dict(window=(1 << 32) + 8), dict(sinks=1 << 31), dict(layer=1 << 32), dict(layer=-1)):
+        with pytest.raises(ssd.SSDError, match=next(iter(kw))):
+            paged.paged_attention(None, pages, None, None, None, None, None, None, **kw)
+    with pytest.raises(ssd.SSDError, match="layer"):
+        paged.pages_store(pages, None, None, None, layer=1 << 32)
+    for kw in (dict(window=1 << 32), dict(sinks=-1)):
+        with pytest.raises(ssd.SSDError, match=next(iter(kw))):
+            paged.pages_commit(pages, *[None] * 9, **kw)
+    with pytest.raises(ssd.SSDError, match="page_rows"):
+        paged.pages_fork(*[None] * 6, (1 << 32) + 32)
 
 
 # ---------------------------------------------------------------- the plain forms
