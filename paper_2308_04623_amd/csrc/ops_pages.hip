@@ -272,7 +272,11 @@ __device__ __forceinline__ BlockAt block_at(const BlockArgs& a, unsigned i) {
   return x;
 }
 
-// Bound: memory.
+// A wave reads 32 rows once, holds them in registers until the block's largest magnitude is known, and writes their
+// bytes in the pool's order: rows are read once and no second pass is made.  The keys' order is the order that lanes
+// read in; the values' four rows of a dim come together through 2 KB (of 64 dims) of the wave's own LDS.
+//   Bound: memory.  36 layers x 63 pages x 20 heads x 32 rows of 64 bfloat16 (558 MB): 116 us, 4.8 TB/s where a large
+// copy reaches 5.2.  Block numbers in 32 bits and a layer a grid row took it there from 124 (64-bit divisions).
 template <typename T, int D, int CODE>
 __global__ __launch_bounds__(kThreads) void store_kernel(BlockArgs a) {
   __shared__ __align__(16) uint8_t lds[kWaveCount][Part<D>::BYTES];
@@ -286,6 +290,7 @@ __global__ __launch_bounds__(kThreads) void store_kernel(BlockArgs a) {
                            [&](int r) { return base + r * a.d.row; }, lds, most);
   }
 }
+// The way back: as many bytes, 93 us of the same size (6.0 TB/s; more is written than read).
 template <typename T, int D, int CODE>
 __global__ __launch_bounds__(kThreads) void load_kernel(BlockArgs a) {
   __shared__ __align__(16) uint8_t lds[kWaveCount][Part<D>::BYTES];
@@ -389,8 +394,11 @@ struct PlanArgs {
   int max_path, n_new;
 };
 
-// Which slots get how many pages, and which: one workgroup, since pages are given out in the order of the
-// slots.  Bound: latency, a chain of some ten loads and meetings.
+// Which slots get how many pages, and which: the lowest free ones, slots in order, so that tables do not depend on
+// timing.  One workgroup: the sums over slots and pages are two scans, and a launch between workgroups would
+// cost more (a launch 3 us) than the whole.
+//   Bound: latency, a chain of some ten loads and meetings.  48 sequences, 1216 pages: 8.4 us (15.6 before refs, lengths
+// and paths were loaded at once ahead of everything, and before scans stayed in registers); 3 sequences 3.8.
 template <bool COMMIT>
 __global__ __launch_bounds__(kPlan) void plan_kernel(PlanArgs a) {
   __shared__ int want[4096], first[4096], col0[4096], sums[kPlan / 64], jobs;
@@ -527,7 +535,13 @@ __device__ __forceinline__ void copy_rows(int heads, int rows, int row_shift, bo
 // Workgroups: first `fill` that make the pages that got full, wave by wave; then for each slot one that
 // gives back what is behind the window, and for each layer and keys or values one that moves rows into the tail.
 // (Rows that are moved go to other places of the tail than those of the page: its positions are less
-// than tail_rows apart.)  Bound: memory, and for few rows the launch.
+// than tail_rows apart, so all run side by side.)  How many pages got full is known on the device alone: the fillers share
+// the blocks there are, side by side, each an equal run of them, so that most of its blocks are of one page and where
+// that page's rows lie is looked up once (in the lanes, a row each).
+//   Bound: memory; for few rows the launch (4.1 us for 3 sequences).  48 sequences of 36 layers and 20 heads of 64 that
+// take up to 16 rows each: 71 us for 257 MB, 3.6 TB/s.  The fillers alone take 40 (55 while every block looked its page
+// and rows up), the moves alone 40: rows of 128 bytes, scattered on one side whichever order they are taken in.
+// 768, 1024, 1536 and 3072 fillers measure the same; 4 and 8 copies under way, too.
 template <typename T, int D, int CODE>
 __global__ __launch_bounds__(kThreads) void commit_kernel(CommitArgs a) {
   __shared__ __align__(16) uint8_t lds[kWaveCount][Part<D>::BYTES];
@@ -536,25 +550,34 @@ __global__ __launch_bounds__(kThreads) void commit_kernel(CommitArgs a) {
   if ((int)blockIdx.x < a.fill) {
     const int waves = R0 >> 5, units = kWaveCount / waves, unit = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / waves;
     const unsigned heads = 2 * G, each = a.p.n_layer * heads;  // (of a page)
-    const int64_t blocks = (int64_t)a.w.head[0] * each;
-    for (int64_t at = (int64_t)blockIdx.x * units; at < blocks; at += (int64_t)a.fill * units) {
+    const int64_t blocks = (int64_t)a.w.head[0] * each, turn = (int64_t)a.fill * units;
+    const int64_t share = (blocks + turn - 1) / turn * units, to = min((int64_t)(blockIdx.x + 1) * share, blocks);
+    const int lane = threadIdx.x & 63, part = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % waves;
+    unsigned had = ~0u;
+    int b = 0, page = 0, mine = 0;  // of the job; lane r: where row 32 part + r lies, ~ its number among the new ones
+    for (int64_t at = (int64_t)blockIdx.x * share; at < to; at += units) {
       int64_t i = at + unit;
-      const bool there = i < blocks;
-      if (!there) i = 0;
+      const bool there = i < to;
+      if (!there) i = at;
       const unsigned which = blocks >> 32 ? (unsigned)(i / each) : (unsigned)i / each, at_page = (unsigned)(i - (int64_t)which * each);
       const unsigned l = at_page / heads, gv = at_page - l * heads, g = gv >> 1;
+      if (which != had) {
+        had = which;
+        const int4 job = a.w.jobs[which];
+        b = job.x;
+        page = job.z;
+        const int len = a.w.slot[b].x, pos = job.y * R0, r = 32 * part + (lane & 31);
+        mine = r < len - pos ? (int)ring(pos % a.tail.rows + r, a.tail.rows) : ~a.path[b * a.path_ld + r - (len - pos)];
+      }
       const bool values = gv & 1;
-      const int4 job = a.w.jobs[which];
-      const int b = job.x, len = a.w.slot[b].x;
-      const int64_t block = ((int64_t)l * a.p.n_page + job.z) * heads + gv;
+      const int64_t block = ((int64_t)l * a.p.n_page + page) * heads + gv;
       const T* old = (const T*)(values ? a.vt : a.kt) + l * a.tail.layer + b * a.tail.seq + g * a.tail.head;
       const T* add = (const T*)(values ? a.vn : a.kn) + l * a.fresh.layer + b * a.fresh.seq + g * a.fresh.head;
-      const int pos = job.y * R0, place = pos % a.tail.rows;
-      const int* path = a.path + b * a.path_ld - (len - pos);
       code_block<T, D, CODE>(
           a.p, there, block, values,
           [&](int r) {
-            return r < len - pos ? old + ring(place + r, a.tail.rows) * a.tail.row : add + path[r] * a.fresh.row;
+            const int x = __shfl(mine, r & 31);
+            return x >= 0 ? old + x * a.tail.row : add + ~x * a.fresh.row;
           },
           lds, most);
     }
@@ -601,7 +624,9 @@ struct ForkArgs {
   char *kt, *vt;
 };
 // blockIdx.y: the slot; blockIdx.x: 0 its table, 1 + 2 l + (keys, values) its open rows in layer l.
-// A slot that is copied from stays as it is, so nothing that is read here is written here.
+// A slot that is copied from stays as it is, so nothing that is read here is written here, and one launch does it.
+//   Bound: memory; for few slots the launch (3.7 us).  64 slots of 36 layers and 20 heads of 64, open rows of up to 31:
+// 39 us, 5.6 TB/s (219 MB; samples of one prompt read the same rows).
 __global__ __launch_bounds__(kThreads) void fork_kernel(ForkArgs a) {
   const int b = blockIdx.y, s = a.parents[b];
   if (s == b) return;
@@ -639,6 +664,8 @@ struct CompactArgs {
   Work w;
   int* used;
 };
+// Which pages move where: the pages in use, counted, the free ones before and the used ones behind their number, in
+// order.  Bound: latency, 5.2 us for 625 pages (8.6 with a turn of loads for every step).
 __global__ __launch_bounds__(kPlan) void compact_plan_kernel(CompactArgs a) {
   __shared__ int sums[kPlan / 64];
   const int n = a.p.n_page;
@@ -668,7 +695,8 @@ __global__ __launch_bounds__(kPlan) void compact_plan_kernel(CompactArgs a) {
   }
 }
 // Moves pages, a piece of one layer's at a time, and names them anew.  Pages come from behind
-// `used` and go before it: no piece is read and written.  Bound: memory.
+// `used` and go before it: no piece is read and written.  16 KB a piece, 64 bytes a thread under way.
+//   Bound: memory.  156 pages of 36 layers, 20 heads, 32 rows of 64 (921 MB read and written): 186 us, 5.0 TB/s.
 constexpr int kPiece = 16384;
 __global__ __launch_bounds__(kThreads) void compact_move_kernel(CompactArgs a) {
   const int moves = a.w.head[1], used = a.w.head[2], n = a.p.n_page, G = a.p.n_kv_head;

@@ -13,6 +13,19 @@
 // the weights' factor scale_v relative to a power of two that the wave's result is multiplied by at the end.
 // Queries are scaled by a power of two each, to the middle of float16's range, and split into
 // parts of 11 bits: bfloat16's 8 bits are one, float32's 24 three.
+//
+// Bound, and what it measured (int8 unless said otherwise; read: 6.1 TB/s is the most this card reads at, 5.2 a copy moves at):
+//   32 sequences of about 1800 rows, 20 heads of 64, one query       31 us, 145 MB: 4.6 TB/s; a short call, its loads alone 31
+//   48 sequences of about 7100 rows, 32 heads on 8 of 128, 5 queries, e4m3    129 us, 712 MB: 5.5 TB/s
+//   4 sequences, 8 queries over a window of 4000 rows, 20 heads of 64         15.8 us, 44 MB: 14 the parts, 4 the join (traced)
+//   3 sequences of 200 rows, 4 heads of 32, float32                   8 us, of which a launch is 3: the chain length, table,
+//                                                                     scales, codes, products, join
+//   4 sequences of 4000 rows, 32 heads on 8 of 128, 64 queries        47 us: the softmax's arithmetic and the products
+// With more than one query a kv head the matrix units have slots to spare (16 columns a product), so the
+// vector instructions count: per item of 32 rows and 64 dims 64 turn codes into float16, whatever the
+// queries' number; then comes the softmax of 8 scores a lane.  What was measured and not kept: four queries or fewer as the rows of products, a score a
+// lane (32 sequences that share one prompt 27 -> 22 us, but 35.3 -> 34.9 where the pages come from memory, float32 25.5 -> 28.6
+// and four queries 92 -> 105 us); three and four items of loads ahead (36 -> 37 to 39 us).
 #include <algorithm>
 #include <atomic>
 #include <type_traits>
@@ -27,8 +40,10 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kWaves = 4;
-constexpr float kFar = 4194304.f;
-constexpr float kSlack = 8.f;  // how far a score may lie above the reference before the sums are rescaled
+constexpr float kFar = 4194304.f;  // references from here on take scores that are rounded first: see weights()
+// How far a score may lie above the reference (the largest so far, in units of log 2) before the sums are rescaled: weights
+// up to 2^8, sums to 2^38 of the rows there can be.  So most items rescale nothing.
+constexpr float kSlack = 8.f;
 
 struct Args {
   ssd_paged_attn_desc d;
@@ -101,7 +116,7 @@ __device__ __forceinline__ float group_max(float x) {  // over the lanes of a co
 template <int D>
 struct Codes {
   u32x4 k[D / 32], v[D / 32];
-  // (read once: they pass by the caches)
+  // (read once: they pass by the caches.  48 x 1 query over 7100 rows 105 us, 113 with plain loads)
   __device__ __forceinline__ void load(const uint8_t* keys, const uint8_t* values, int lane) {
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) k[i] = __builtin_nontemporal_load((const u32x4*)(keys + 1024 * i + 16 * lane));
@@ -339,8 +354,10 @@ struct Tiles : Base<T, D, CODE> {
       for (int dt = 0; dt < DT; ++dt) o[nt][dt] *= f;
   }
 
-  // s becomes 2^(s by - reference), by >= 0, and 0 where `masked` and not seen(tile, k, r): row 16 k + 4 g + r; the sums are rescaled where a score is far above the reference.  Product
-  // and difference are one operation; from references of 2^22 on, where their rounding counts, they are two.
+  // s becomes 2^(s by - reference), by >= 0, and 0 where `masked` and not seen(tile, k, r): row 16 k + 4 g + r; the
+  // sums are rescaled where a score is far above the reference.  Product and difference are one operation; from
+  // references of 2^22 on, where the largest score and the reference made of it would differ by the product's
+  // rounding, and the weight with it, they are two.
   template <typename Seen>
   __device__ __forceinline__ void weights(f32x4 (&s)[NT][2], float (&by)[NT], bool masked, Seen seen) {
 #pragma clang fp contract(off)
@@ -597,9 +614,10 @@ struct Seen {
 // Long sequences are cut by their own lengths: each into the nearest number of parts of an equal share of all rows
 // (one at the least), parts of a head side by side, sequence by sequence.  So a batch of one long and many short
 // ones fills the chip too.  (Every wave finds its part by itself: the lengths are in its lanes.)
-constexpr int kLeast = 24;  // 32 rows each of a part: six for each wave
-constexpr int kRound = 512;  // workgroups that sequences are cut for: two a CU
-constexpr int kLong = 512;  // from this many on, sequences are cut by their own lengths
+// One sequence of 60,000 rows among 31 of about 1000, 20 heads of 64: 729 us in equal parts of the table, 55 so.
+constexpr int kLeast = 24;  // 32 rows each of a part: six for each wave (16 x 1 query of 16 heads on 2 over 4000 rows 12.7 us, 13.8 with 16)
+constexpr int kRound = 512;  // workgroups that sequences are cut for: two a CU (100,000 rows of one 48.2 us, 50.3 with 768)
+constexpr int kLong = 512;  // from this many on, sequences are cut by their own lengths (finding the part takes 2 us)
 struct Part {
   int b, j, n;  // part j of n of sequence b,
   int at, kv;   // the at-th of all, in kv head kv
@@ -659,8 +677,12 @@ __device__ __forceinline__ Part find_part(const Args& a, int p) {
 // has, but for the last `owners` waves, items me + k others for k < early, and then every wave each all-th one.  The last waves,
 // as many as open and new rows can need, take those in place of their early items.  So which columns a wave looks at
 // does not depend on the length (without a window or parts), and the table's entries are under way with it.
-constexpr int kOwnCost = 6;  // what 32 rows in the model's type take, in 32 rows of pages
+// What 32 rows in the model's type take, in 32 rows of pages (64 sequences of 512 rows, 20 heads of 64: 27.6 us, 31.5 with 3,
+// 34.7 with 0).
+constexpr int kOwnCost = 6;
 
+// (Registers: the loads under way and the outputs.  The masks and the sign of a scale are kept out of the loop of items by
+// empty statements: taken out of it by the compiler they made 200 bytes of spills, 163 us in place of 152 for heads of 128.)
 template <typename W>
 __global__ __launch_bounds__(64 * kWaves, W::DIM == 128 || W::COLS == 32 || W::F32 ? 2 : 3) void paged_attn_kernel(Args a) {
   typedef typename W::Type T;
@@ -807,7 +829,9 @@ __global__ __launch_bounds__(64 * kWaves, W::DIM == 128 || W::COLS == 32 || W::F
   }
 }
 
-// A wave per query adds its parts: lane l has dims 4 (l mod (D / 4)) .. + 3 of every (256 / D)-th.
+// A wave per query adds its parts, out = sum 2^(m_c - M) o_c / sum 2^(m_c - M) l_c, reading all at once; parts are added
+// in their order, so results do not depend on which ended first.  Bound: latency, 4 us for 7 parts of 640 queries.
+// Lane l has dims 4 (l mod (D / 4)) .. + 3 of every (256 / D)-th.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void join_kernel(Args a) {
   constexpr int LD = D / 4, PAR = 64 / LD;
@@ -870,14 +894,13 @@ Plan plan(const ssd_page_pool& p, const ssd_page_seqs& s, const ssd_paged_attn_d
   if (d.window)
     pages = std::min<int64_t>(pages, div_up(std::min<int64_t>(d.sinks, 1 << 30), p.page_rows) + d.window / p.page_rows + 2);
   const int64_t units = (int64_t)s.n_seq * p.n_kv_head * x.tiles, steps = pages * (p.page_rows / 32);
-  const int64_t round = kRound;
   const int64_t heads = (int64_t)s.n_seq * p.n_kv_head;
   // (numbers of 32 rows of all queries are 32-bit where the device counts them)
   if (s.n_seq > 1 && steps > kLong && units * steps < (1 << 30)) {
-    x.round = (int)round;
-    x.parts = div_up(heads + div_up(round, x.tiles), 8) * 8;
+    x.round = kRound;
+    x.parts = div_up(heads + div_up(kRound, x.tiles), 8) * 8;
   } else {
-    x.splits = (int)std::max<int64_t>(1, std::min<int64_t>(round / units, div_up(steps, kLeast)));
+    x.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kRound / units, div_up(steps, kLeast)));
     x.parts = div_up(heads * x.splits, 8) * 8;
   }
   x.blocks = x.parts * x.tiles;
