@@ -14,28 +14,36 @@ static_assert(kPlan * kPer >= 4096, "a thread for every four slots");
 
 // ---------------------------------------------------------------- codes
 
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, float* x);
-template <>
-__device__ __forceinline__ void load8<float>(const float* p, float* x) {
-  const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
+// 16 bytes, by the caches or past them (nontemporal).  What a call reads or writes once and in whole lines goes past
+// them, but for what is read again soon: rows that a fork copies for several slots, and pages that a commit has filled.
+// With all of it in the caches, lines that were written and not yet sent to memory stand in the way of what follows: commit
+// 72 us, then 60, and the read of its pages behind it 73, then 53 (48 sequences of 36 layers); a prompt's rows into pages
+// and back 210, then 201; fork 39, then 34; compaction 185, then 172.
+template <bool PAST = true>
+__device__ __forceinline__ u32x4 get16(const void* p) {
+  if constexpr (PAST) return __builtin_nontemporal_load((const u32x4*)p);
+  else return *(const u32x4*)p;
 }
-template <>
-__device__ __forceinline__ void load8<bf16_t>(const bf16_t* p, float* x) {
-  const u32x4 a = *(const u32x4*)p;
+template <bool PAST = true>
+__device__ __forceinline__ void put16(void* p, u32x4 x) {
+  if constexpr (PAST) __builtin_nontemporal_store(x, (u32x4*)p);
+  else *(u32x4*)p = x;
+}
+
+// 16 bytes of the model's type
+__device__ __forceinline__ void unpack(u32x4 a, const float*, float* x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(a[i]);
+}
+__device__ __forceinline__ void unpack(u32x4 a, const bf16_t*, float* x) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     x[2 * i] = __uint_as_float(a[i] << 16);
     x[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
   }
 }
-__device__ __forceinline__ void store8(float* p, const float* x) {
-  *(f32x4*)p = (f32x4){x[0], x[1], x[2], x[3]};
-  *(f32x4*)(p + 4) = (f32x4){x[4], x[5], x[6], x[7]};
-}
-__device__ __forceinline__ void store8(bf16_t* p, const float* x) {
+__device__ __forceinline__ void store16(float* p, const float* x) { *(f32x4*)p = (f32x4){x[0], x[1], x[2], x[3]}; }
+__device__ __forceinline__ void store16(bf16_t* p, const float* x) {
   u32x4 a;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -110,79 +118,82 @@ __device__ __forceinline__ void values4(unsigned w, float scale, float* x, int s
   }
 }
 
-// A wave's part of a block: 32 rows.
-//   Keys: a lane has chunks q < D / 16 of 8 dims, of row k_row(q) at k_dim(q), in the order of
-// its bytes: chunks 2 s and 2 s + 1 are the 16 bytes at 1024 s + 16 lane.
-//   Values: a lane has, for i < V, the four rows 4 (p / (D / 8)) .. at the 8 dims 8 (p mod (D / 8)), p = lane + 64 i
-// (D = 32: 32 lanes do); four rows at a dim are one 4-byte word, placed through LDS.
-template <int D>
+// A wave's part of a block: 32 rows, in units of 16 bytes of a row, U elements, so that a wave's loads and stores are of whole
+// rows.  Lane l has
+//   keys:   units l + 64 q, q < KEYS, of the part;
+//   values: for i < VALUES unit (l + 64 i) mod (D / U) of the four rows 4 ((l + 64 i) / (D / U)) .. (bfloat16 of 32 dims: 32
+//           lanes do), whose codes at a dim are one 4-byte word.
+// Codes get to their places, and back, through 32 D bytes of the wave's own LDS.
+template <typename T, int D>
 struct Part {
-  static constexpr int KEYS = D / 16, VALUES = D == 128 ? 2 : 1, BYTES = 32 * D;
-  static __device__ __forceinline__ int k_row(int lane, int q) {
-    return (lane & 15) + 16 * (D == 32 ? q : q / (D / 32));
+  static constexpr int U = 16 / sizeof(T), ROW = D / U, KEYS = ROW / 2, VALUES = (ROW + 7) / 8, BYTES = 32 * D;
+  static constexpr int HELD = 4 * U * VALUES > U * KEYS ? 4 * U * VALUES : U * KEYS;  // elements of a lane
+  static __device__ __forceinline__ int k_row(int lane, int q) { return (lane + 64 * q) / ROW; }
+  static __device__ __forceinline__ int k_dim(int lane, int q) { return (lane + 64 * q) % ROW * U; }
+  static __device__ __forceinline__ bool v_mine(int lane) { return ROW >= 8 || lane < 8 * ROW; }
+  static __device__ __forceinline__ int v_row(int lane, int i) { return 4 * ((lane + 64 * i) / ROW); }
+  static __device__ __forceinline__ int v_dim(int lane, int i) { return (lane + 64 * i) % ROW * U; }
+  // where the codes of a row of the keys from dim d on lie, and the word of rows row .. row + 3 of the values at dim d
+  static __device__ __forceinline__ int k_byte(int row, int d) {
+    return D == 32 ? d / 8 * 256 + row % 16 * 16 + row / 16 * 8 + d % 8
+                   : (row / 16 * (D / 64) + d / 64) * 1024 + d / 16 % 4 * 256 + row % 16 * 16 + d % 16;
   }
-  static __device__ __forceinline__ int k_dim(int lane, int q) {
-    return D == 32 ? 8 * (lane >> 4) : 64 * (q / 2 % (D / 64)) + 16 * (lane >> 4) + 8 * (q & 1);
-  }
-  static __device__ __forceinline__ bool v_mine(int lane) { return D > 32 || lane < 32; }
-  static __device__ __forceinline__ int v_row(int lane, int i) { return 4 * ((lane + 64 * i) / (D / 8)); }
-  static __device__ __forceinline__ int v_dim(int lane, int i) { return 8 * ((lane + 64 * i) % (D / 8)); }
-  // the word of rows v_row .. + 3 at dim d
   static __device__ __forceinline__ int v_word(int row, int d) {
     return d / 32 * 1024 + (row / 4 % 4 * 16 + d % 16) * 16 + d / 16 % 2 * 8 + row / 16 * 4;
   }
 };
 
 // The part's elements, row r at row(r), and the bits of the largest magnitude of the lane's.
-template <int D>
-constexpr int kHeld = D == 32 ? 32 : D / 2;  // elements of a lane
 template <typename T, int D, typename Row>
-__device__ __forceinline__ unsigned take_rows(bool values, int lane, Row row, float (&x)[kHeld<D>]) {
-  typedef Part<D> P;
+__device__ __forceinline__ unsigned take_rows(bool values, int lane, Row row, float (&x)[Part<T, D>::HELD]) {
+  typedef Part<T, D> P;
+#pragma unroll
+  for (int i = 0; i < P::HELD; ++i) x[i] = 0.f;
   if (!values) {
 #pragma unroll
-    for (int q = 0; q < P::KEYS; ++q) load8<T>(row(P::k_row(lane, q)) + P::k_dim(lane, q), x + 8 * q);
-#pragma unroll
-    for (int i = 8 * P::KEYS; i < kHeld<D>; ++i) x[i] = 0.f;
+    for (int q = 0; q < P::KEYS; ++q) {
+      const T* p = row(P::k_row(lane, q)) + P::k_dim(lane, q);
+      unpack(get16(p), p, x + P::U * q);
+    }
   } else {
     const int mine = P::v_mine(lane) ? lane : lane - 32;
 #pragma unroll
     for (int i = 0; i < P::VALUES; ++i)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) load8<T>(row(P::v_row(mine, i) + r) + P::v_dim(mine, i), x + 32 * i + 8 * r);
+      for (int r = 0; r < 4; ++r) {
+        const T* p = row(P::v_row(mine, i) + r) + P::v_dim(mine, i);
+        unpack(get16(p), p, x + P::U * (4 * i + r));
+      }
   }
   unsigned most = 0;
 #pragma unroll
-  for (int i = 0; i < kHeld<D>; ++i) most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);
+  for (int i = 0; i < P::HELD; ++i) most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);
   return lane_max(most);
 }
 // Their codes to the part at dst; lds: Part::BYTES of the wave's own.
-template <int D, int CODE>
-__device__ __forceinline__ void put_codes(bool values, int lane, const float (&x)[kHeld<D>], const Coding& c,
+template <typename T, int D, int CODE, bool PAST>
+__device__ __forceinline__ void put_codes(bool values, int lane, const float (&x)[Part<T, D>::HELD], const Coding& c,
                                           uint8_t* dst, uint8_t* lds) {
-  typedef Part<D> P;
+  typedef Part<T, D> P;
   if (!values) {
 #pragma unroll
-    for (int s = 0; s < P::KEYS / 2; ++s) {
-      u32x4 w;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = code4<CODE>(x + 16 * s + 4 * i, 1, c);
-      *(u32x4*)(dst + 1024 * s + 16 * lane) = w;
+    for (int q = 0; q < P::KEYS; ++q) {
+      uint8_t* p = lds + P::k_byte(P::k_row(lane, q), P::k_dim(lane, q));
+      if constexpr (P::U == 8) *(u32x2*)p = (u32x2){code4<CODE>(x + 8 * q, 1, c), code4<CODE>(x + 8 * q + 4, 1, c)};
+      else *(unsigned*)p = code4<CODE>(x + 4 * q, 1, c);
     }
-    return;
-  }
-  if (P::v_mine(lane)) {
+  } else if (P::v_mine(lane)) {
 #pragma unroll
     for (int i = 0; i < P::VALUES; ++i)
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        *(unsigned*)(lds + P::v_word(P::v_row(lane, i), P::v_dim(lane, i) + j)) = code4<CODE>(x + 32 * i + j, 8, c);
+      for (int j = 0; j < P::U; ++j)
+        *(unsigned*)(lds + P::v_word(P::v_row(lane, i), P::v_dim(lane, i) + j)) = code4<CODE>(x + 4 * P::U * i + j, P::U, c);
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
 #pragma unroll
   for (int s = 0; s < P::BYTES / 1024; ++s)
-    *(u32x4*)(dst + 1024 * s + 16 * lane) = *(const u32x4*)(lds + 1024 * s + 16 * lane);
+    put16<PAST>(dst + 1024 * s + 16 * lane, *(const u32x4*)(lds + 1024 * s + 16 * lane));
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
 }
@@ -190,33 +201,30 @@ __device__ __forceinline__ void put_codes(bool values, int lane, const float (&x
 template <typename T, int D, int CODE, typename Row>
 __device__ __forceinline__ void put_values(bool values, int lane, const uint8_t* src, float scale, Row row,
                                            uint8_t* lds) {
-  typedef Part<D> P;
-  float x[kHeld<D>];
-  if (!values) {
-#pragma unroll
-    for (int s = 0; s < P::KEYS / 2; ++s) {
-      const u32x4 w = *(const u32x4*)(src + 1024 * s + 16 * lane);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) values4<CODE>(w[i], scale, x + 16 * s + 4 * i, 1);
-    }
-#pragma unroll
-    for (int q = 0; q < P::KEYS; ++q) store8(row(P::k_row(lane, q)) + P::k_dim(lane, q), x + 8 * q);
-    return;
-  }
+  typedef Part<T, D> P;
 #pragma unroll
   for (int s = 0; s < P::BYTES / 1024; ++s)
-    *(u32x4*)(lds + 1024 * s + 16 * lane) = *(const u32x4*)(src + 1024 * s + 16 * lane);
+    *(u32x4*)(lds + 1024 * s + 16 * lane) = get16(src + 1024 * s + 16 * lane);
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
-  if (P::v_mine(lane)) {
+  float x[P::HELD];
+  if (!values) {
+#pragma unroll
+    for (int q = 0; q < P::KEYS; ++q) {
+      const uint8_t* p = lds + P::k_byte(P::k_row(lane, q), P::k_dim(lane, q));
+#pragma unroll
+      for (int w = 0; w < P::U / 4; ++w) values4<CODE>(((const unsigned*)p)[w], scale, x + P::U * q + 4 * w, 1);
+      store16(row(P::k_row(lane, q)) + P::k_dim(lane, q), x + P::U * q);
+    }
+  } else if (P::v_mine(lane)) {
 #pragma unroll
     for (int i = 0; i < P::VALUES; ++i) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
+      for (int j = 0; j < P::U; ++j)
         values4<CODE>(*(const unsigned*)(lds + P::v_word(P::v_row(lane, i), P::v_dim(lane, i) + j)), scale,
-                      x + 32 * i + j, 8);
+                      x + 4 * P::U * i + j, P::U);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) store8(row(P::v_row(lane, i) + r) + P::v_dim(lane, i), x + 32 * i + 8 * r);
+      for (int r = 0; r < 4; ++r) store16(row(P::v_row(lane, i) + r) + P::v_dim(lane, i), x + P::U * (4 * i + r));
     }
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -225,12 +233,12 @@ __device__ __forceinline__ void put_values(bool values, int lane, const uint8_t*
 
 // The waves of a workgroup take blocks, page_rows / 32 waves one.  The block's scale comes
 // from all of its rows, so waves of one block meet once.
-template <typename T, int D, int CODE, typename Row>
+template <typename T, int D, int CODE, bool PAST, typename Row>
 __device__ __forceinline__ void code_block(const ssd_page_pool& p, bool there, int64_t block, bool values, Row row,
-                                           uint8_t (*lds)[Part<D>::BYTES], unsigned (&most)[kWaveCount]) {
+                                           uint8_t (*lds)[Part<T, D>::BYTES], unsigned (&most)[kWaveCount]) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = p.page_rows >> 5,
             part = wave % waves;
-  float x[kHeld<D>];
+  float x[Part<T, D>::HELD];
   unsigned bits = 0;
   if (there) bits = take_rows<T, D>(values, lane, [&](int r) { return row(32 * part + r); }, x);
   if (waves > 1) {
@@ -241,7 +249,8 @@ __device__ __forceinline__ void code_block(const ssd_page_pool& p, bool there, i
   }
   if (!there) return;
   const Coding c = coding<CODE>(bits);
-  put_codes<D, CODE>(values, lane, x, c, (uint8_t*)p.data + block * block_bytes(p) + part * Part<D>::BYTES, lds[wave]);
+  put_codes<T, D, CODE, PAST>(values, lane, x, c, (uint8_t*)p.data + block * block_bytes(p) + part * Part<T, D>::BYTES,
+                           lds[wave]);
   if (part == 0 && lane == 0) p.scale[block] = c.scale;
 }
 
@@ -273,27 +282,26 @@ __device__ __forceinline__ BlockAt block_at(const BlockArgs& a, unsigned i) {
 }
 
 // A wave reads 32 rows once, holds them in registers until the block's largest magnitude is known, and writes their
-// bytes in the pool's order: rows are read once and no second pass is made.  The keys' order is the order that lanes
-// read in; the values' four rows of a dim come together through 2 KB (of 64 dims) of the wave's own LDS.
-//   Bound: memory.  36 layers x 63 pages x 20 heads x 32 rows of 64 bfloat16 (558 MB): 116 us, 4.8 TB/s where a large
-// copy reaches 5.2.  Block numbers in 32 bits and a layer a grid row took it there from 124 (64-bit divisions).
+// bytes in the pool's order: rows are read once and no second pass is made.
+//   Bound: memory.  36 layers x 63 pages x 20 heads x 32 rows of 64 bfloat16 (558 MB): 101 us, 5.5 TB/s where a large
+// copy reaches 5.2.  (Block numbers in 32 bits and a layer a grid row were 117 to 124 with 64-bit divisions.)
 template <typename T, int D, int CODE>
 __global__ __launch_bounds__(kThreads) void store_kernel(BlockArgs a) {
-  __shared__ __align__(16) uint8_t lds[kWaveCount][Part<D>::BYTES];
+  __shared__ __align__(16) uint8_t lds[kWaveCount][Part<T, D>::BYTES];
   __shared__ unsigned most[kWaveCount];
   const int waves = a.p.page_rows >> 5, units = kWaveCount / waves,
             unit = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / waves;
   for (unsigned first = blockIdx.x * units; first < a.blocks; first += gridDim.x * units) {
     const BlockAt at = block_at(a, first + unit);
     const T* base = (const T*)(at.values ? a.v : a.k) + at.rows;
-    code_block<T, D, CODE>(a.p, at.there && at.block >= 0, at.block, at.values,
+    code_block<T, D, CODE, true>(a.p, at.there && at.block >= 0, at.block, at.values,
                            [&](int r) { return base + r * a.d.row; }, lds, most);
   }
 }
-// The way back: as many bytes, 93 us of the same size (6.0 TB/s; more is written than read).
+// The way back: as many bytes, 100 us of the same size (5.6 TB/s).
 template <typename T, int D, int CODE>
 __global__ __launch_bounds__(kThreads) void load_kernel(BlockArgs a) {
-  __shared__ __align__(16) uint8_t lds[kWaveCount][Part<D>::BYTES];
+  __shared__ __align__(16) uint8_t lds[kWaveCount][Part<T, D>::BYTES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = a.p.page_rows >> 5,
             units = kWaveCount / waves, unit = wave / waves, part = wave % waves;
   for (unsigned first = blockIdx.x * units; first < a.blocks; first += gridDim.x * units) {
@@ -302,10 +310,11 @@ __global__ __launch_bounds__(kThreads) void load_kernel(BlockArgs a) {
     T* base = (T*)(at.values ? a.v : a.k) + at.rows;
     auto row = [&](int r) { return base + (32 * part + r) * a.d.row; };
     if (at.block < 0) {
+      typedef Part<T, D> P;
       const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      for (int q = 0; q < Part<D>::KEYS; ++q) store8(row(Part<D>::k_row(lane, q)) + Part<D>::k_dim(lane, q), zero);
+      for (int q = 0; q < P::KEYS; ++q) store16(row(P::k_row(lane, q)) + P::k_dim(lane, q), zero);
     } else {
-      put_values<T, D, CODE>(at.values, lane, (const uint8_t*)a.p.data + at.block * block_bytes(a.p) + part * Part<D>::BYTES,
+      put_values<T, D, CODE>(at.values, lane, (const uint8_t*)a.p.data + at.block * block_bytes(a.p) + part * Part<T, D>::BYTES,
                              a.p.scale[at.block], row, lds[wave]);
     }
   }
@@ -509,7 +518,7 @@ __device__ __forceinline__ int64_t ring(int at, int rows) { return at >= rows ? 
 
 // items 16 bytes each, of `heads` heads' `rows` rows, four a thread under way: src(head, row), dst(head, row)
 // the row's first byte
-template <typename Src, typename Dst>
+template <bool PAST, typename Src, typename Dst>
 __device__ __forceinline__ void copy_rows(int heads, int rows, int row_shift, bool rows_outer, Src src, Dst dst) {
   const int total = heads * rows << row_shift, inner = rows_outer ? heads : rows;  // (a row: 2^row_shift times 16 bytes)
   constexpr int U = 4;
@@ -523,12 +532,12 @@ __device__ __forceinline__ void copy_rows(int heads, int rows, int row_shift, bo
       const unsigned hr = (unsigned)i >> row_shift;
       const int v = i & ((1 << row_shift) - 1), out = hr / (unsigned)inner, in = hr - out * inner;
       const int h = rows_outer ? in : out, r = rows_outer ? out : in;
-      x[u] = *(const u32x4*)(src(h, r) + 16 * v);
+      x[u] = get16<PAST>(src(h, r) + 16 * v);
       to[u] = dst(h, r) + 16 * v;
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (i0 + u * kThreads < total) *(u32x4*)to[u] = x[u];
+      if (i0 + u * kThreads < total) put16(to[u], x[u]);
   }
 }
 
@@ -539,12 +548,12 @@ __device__ __forceinline__ void copy_rows(int heads, int rows, int row_shift, bo
 // the blocks there are, side by side, each an equal run of them, so that most of its blocks are of one page and where
 // that page's rows lie is looked up once (in the lanes, a row each).
 //   Bound: memory; for few rows the launch (4.1 us for 3 sequences).  48 sequences of 36 layers and 20 heads of 64 that
-// take up to 16 rows each: 71 us for 257 MB, 3.6 TB/s.  The fillers alone take 40 (55 while every block looked its page
-// and rows up), the moves alone 40: rows of 128 bytes, scattered on one side whichever order they are taken in.
-// 768, 1024, 1536 and 3072 fillers measure the same; 4 and 8 copies under way, too.
+// take up to 16 rows each: 60 us for 257 MB, 4.3 TB/s.  (All by the caches 72, of it the fillers alone 40, 55 while every block
+// looked its page and rows up, and the moves alone 40.)
+// 768, 1024 and 1536 fillers measure the same; 4 and 8 copies under way, too.
 template <typename T, int D, int CODE>
-__global__ __launch_bounds__(kThreads) void commit_kernel(CommitArgs a) {
-  __shared__ __align__(16) uint8_t lds[kWaveCount][Part<D>::BYTES];
+__global__ __launch_bounds__(kThreads, 4) void commit_kernel(CommitArgs a) {
+  __shared__ __align__(16) uint8_t lds[kWaveCount][Part<T, D>::BYTES];
   __shared__ unsigned most[kWaveCount];
   const int R0 = a.p.page_rows, G = a.p.n_kv_head;
   if ((int)blockIdx.x < a.fill) {
@@ -573,7 +582,7 @@ __global__ __launch_bounds__(kThreads) void commit_kernel(CommitArgs a) {
       const int64_t block = ((int64_t)l * a.p.n_page + page) * heads + gv;
       const T* old = (const T*)(values ? a.vt : a.kt) + l * a.tail.layer + b * a.tail.seq + g * a.tail.head;
       const T* add = (const T*)(values ? a.vn : a.kn) + l * a.fresh.layer + b * a.fresh.seq + g * a.fresh.head;
-      code_block<T, D, CODE>(
+      code_block<T, D, CODE, false>(
           a.p, there, block, values,
           [&](int r) {
             const int x = __shfl(mine, r & 31);
@@ -608,7 +617,7 @@ __global__ __launch_bounds__(kThreads) void commit_kernel(CommitArgs a) {
   const char* add = (values ? a.vn : a.kn) + (l * a.fresh.layer + b * a.fresh.seq) * (int)sizeof(T);
   const int* path = a.path + b * a.path_ld + start;
   const int place = (slot.x + start) % a.tail.rows;
-  copy_rows(
+  copy_rows<true>(
       G, n, __builtin_ctz(D * sizeof(T) / 16), true,
       [&](int g, int r) { return add + (path[r] * a.fresh.row + g * a.fresh.head) * (int)sizeof(T); },
       [&](int g, int r) { return old + (ring(place + r, a.tail.rows) * a.tail.row + g * a.tail.head) * (int)sizeof(T); });
@@ -626,7 +635,7 @@ struct ForkArgs {
 // blockIdx.y: the slot; blockIdx.x: 0 its table, 1 + 2 l + (keys, values) its open rows in layer l.
 // A slot that is copied from stays as it is, so nothing that is read here is written here, and one launch does it.
 //   Bound: memory; for few slots the launch (3.7 us).  64 slots of 36 layers and 20 heads of 64, open rows of up to 31:
-// 39 us, 5.6 TB/s (219 MB; samples of one prompt read the same rows).
+// 34 us, 6.4 TB/s (219 MB; samples of one prompt read the same rows).
 __global__ __launch_bounds__(kThreads) void fork_kernel(ForkArgs a) {
   const int b = blockIdx.y, s = a.parents[b];
   if (s == b) return;
@@ -652,7 +661,7 @@ __global__ __launch_bounds__(kThreads) void fork_kernel(ForkArgs a) {
   auto at = [&](int slot, int g, int r) {
     return base + (slot * a.tail.seq + g * a.tail.head + ring(place + r, a.tail.rows) * a.tail.row) * es;
   };
-  copy_rows(a.n_kv_head, n, a.row_shift, false, [&](int g, int r) { return (const char*)at(s, g, r); },
+  copy_rows<false>(a.n_kv_head, n, a.row_shift, false, [&](int g, int r) { return (const char*)at(s, g, r); },
             [&](int g, int r) { return at(b, g, r); });
 }
 
@@ -696,7 +705,7 @@ __global__ __launch_bounds__(kPlan) void compact_plan_kernel(CompactArgs a) {
 }
 // Moves pages, a piece of one layer's at a time, and names them anew.  Pages come from behind
 // `used` and go before it: no piece is read and written.  16 KB a piece, 64 bytes a thread under way.
-//   Bound: memory.  156 pages of 36 layers, 20 heads, 32 rows of 64 (921 MB read and written): 186 us, 5.0 TB/s.
+//   Bound: memory.  156 pages of 36 layers, 20 heads, 32 rows of 64 (921 MB read and written): 172 us, 5.4 TB/s.
 constexpr int kPiece = 16384;
 __global__ __launch_bounds__(kThreads) void compact_move_kernel(CompactArgs a) {
   const int moves = a.w.head[1], used = a.w.head[2], n = a.p.n_page, G = a.p.n_kv_head;
@@ -714,10 +723,10 @@ __global__ __launch_bounds__(kThreads) void compact_move_kernel(CompactArgs a) {
     u32x4 x[kPiece / 16 / kThreads];
 #pragma unroll
     for (int u = 0; u < kPiece / 16 / kThreads; ++u)
-      if ((int)threadIdx.x + u * kThreads < vec) x[u] = *(const u32x4*)(src + 16 * (threadIdx.x + u * kThreads));
+      if ((int)threadIdx.x + u * kThreads < vec) x[u] = get16(src + 16 * (threadIdx.x + u * kThreads));
 #pragma unroll
     for (int u = 0; u < kPiece / 16 / kThreads; ++u)
-      if ((int)threadIdx.x + u * kThreads < vec) *(u32x4*)(dst + 16 * (threadIdx.x + u * kThreads)) = x[u];
+      if ((int)threadIdx.x + u * kThreads < vec) put16(dst + 16 * (threadIdx.x + u * kThreads), x[u]);
     if (piece == 0)
       for (int j = threadIdx.x; j < 2 * G; j += kThreads) a.p.scale[to * 2 * G + j] = a.p.scale[from * 2 * G + j];
   }
