@@ -14,21 +14,17 @@ static_assert(kPlan * kPer >= 4096, "a thread for every four slots");
 
 // ---------------------------------------------------------------- codes
 
-// 16 bytes, by the caches or past them (nontemporal).  What a call reads or writes once and in whole lines goes past
-// them, but for what is read again soon: rows that a fork copies for several slots, and pages that a commit has filled.
-// With all of it in the caches, lines that were written and not yet sent to memory stand in the way of what follows: commit
-// 72 us, then 60, and the read of its pages behind it 73, then 53 (48 sequences of 36 layers); a prompt's rows into pages
-// and back 210, then 201; fork 39, then 34; compaction 185, then 172.
+// 16 bytes, by the caches or past them (nontemporal).  Rows, which a call reads or writes once, go past them, whole rows at a
+// time (in halves of a line they are fetched twice); codes that are made stay in them for the attention that reads them, and so do
+// rows that a fork reads for several slots.  With all of it in the caches, lines that wait there for their way to memory
+// stand in the way of what follows: 48 sequences of 36 layers, commit 72 us (here 51) and the read of their pages behind it 73
+// (61); a prompt's rows into pages and back 210 (178); fork 39 (34); compaction 185 (172).
 template <bool PAST = true>
 __device__ __forceinline__ u32x4 get16(const void* p) {
   if constexpr (PAST) return __builtin_nontemporal_load((const u32x4*)p);
   else return *(const u32x4*)p;
 }
-template <bool PAST = true>
-__device__ __forceinline__ void put16(void* p, u32x4 x) {
-  if constexpr (PAST) __builtin_nontemporal_store(x, (u32x4*)p);
-  else *(u32x4*)p = x;
-}
+__device__ __forceinline__ void put16(void* p, u32x4 x) { __builtin_nontemporal_store(x, (u32x4*)p); }
 
 // 16 bytes of the model's type
 __device__ __forceinline__ void unpack(u32x4 a, const float*, float* x) {
@@ -42,14 +38,16 @@ __device__ __forceinline__ void unpack(u32x4 a, const bf16_t*, float* x) {
     x[2 * i + 1] = __uint_as_float(a[i] & 0xffff0000u);
   }
 }
-__device__ __forceinline__ void store16(float* p, const float* x) { *(f32x4*)p = (f32x4){x[0], x[1], x[2], x[3]}; }
+__device__ __forceinline__ void store16(float* p, const float* x) {
+  put16(p, __builtin_bit_cast(u32x4, (f32x4){x[0], x[1], x[2], x[3]}));
+}
 __device__ __forceinline__ void store16(bf16_t* p, const float* x) {
   u32x4 a;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     a[i] = (unsigned)__builtin_bit_cast(uint16_t, (__bf16)x[2 * i]) |
            (unsigned)__builtin_bit_cast(uint16_t, (__bf16)x[2 * i + 1]) << 16;
-  *(u32x4*)p = a;
+  put16(p, a);
 }
 
 // Sums over the lanes up to this one, and the largest of all, within the registers.
@@ -171,7 +169,7 @@ __device__ __forceinline__ unsigned take_rows(bool values, int lane, Row row, fl
   return lane_max(most);
 }
 // Their codes to the part at dst; lds: Part::BYTES of the wave's own.
-template <typename T, int D, int CODE, bool PAST>
+template <typename T, int D, int CODE>
 __device__ __forceinline__ void put_codes(bool values, int lane, const float (&x)[Part<T, D>::HELD], const Coding& c,
                                           uint8_t* dst, uint8_t* lds) {
   typedef Part<T, D> P;
@@ -193,7 +191,7 @@ __device__ __forceinline__ void put_codes(bool values, int lane, const float (&x
   __builtin_amdgcn_wave_barrier();
 #pragma unroll
   for (int s = 0; s < P::BYTES / 1024; ++s)
-    put16<PAST>(dst + 1024 * s + 16 * lane, *(const u32x4*)(lds + 1024 * s + 16 * lane));
+    *(u32x4*)(dst + 1024 * s + 16 * lane) = *(const u32x4*)(lds + 1024 * s + 16 * lane);
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
 }
@@ -233,7 +231,7 @@ __device__ __forceinline__ void put_values(bool values, int lane, const uint8_t*
 
 // The waves of a workgroup take blocks, page_rows / 32 waves one.  The block's scale comes
 // from all of its rows, so waves of one block meet once.
-template <typename T, int D, int CODE, bool PAST, typename Row>
+template <typename T, int D, int CODE, typename Row>
 __device__ __forceinline__ void code_block(const ssd_page_pool& p, bool there, int64_t block, bool values, Row row,
                                            uint8_t (*lds)[Part<T, D>::BYTES], unsigned (&most)[kWaveCount]) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = p.page_rows >> 5,
@@ -249,7 +247,7 @@ __device__ __forceinline__ void code_block(const ssd_page_pool& p, bool there, i
   }
   if (!there) return;
   const Coding c = coding<CODE>(bits);
-  put_codes<T, D, CODE, PAST>(values, lane, x, c, (uint8_t*)p.data + block * block_bytes(p) + part * Part<T, D>::BYTES,
+  put_codes<T, D, CODE>(values, lane, x, c, (uint8_t*)p.data + block * block_bytes(p) + part * Part<T, D>::BYTES,
                            lds[wave]);
   if (part == 0 && lane == 0) p.scale[block] = c.scale;
 }
@@ -283,7 +281,7 @@ __device__ __forceinline__ BlockAt block_at(const BlockArgs& a, unsigned i) {
 
 // A wave reads 32 rows once, holds them in registers until the block's largest magnitude is known, and writes their
 // bytes in the pool's order: rows are read once and no second pass is made.
-//   Bound: memory.  36 layers x 63 pages x 20 heads x 32 rows of 64 bfloat16 (558 MB): 101 us, 5.5 TB/s where a large
+//   Bound: memory.  36 layers x 63 pages x 20 heads x 32 rows of 64 bfloat16 (558 MB): 96 us, 5.8 TB/s where a large
 // copy reaches 5.2.  (Block numbers in 32 bits and a layer a grid row were 117 to 124 with 64-bit divisions.)
 template <typename T, int D, int CODE>
 __global__ __launch_bounds__(kThreads) void store_kernel(BlockArgs a) {
@@ -294,11 +292,11 @@ __global__ __launch_bounds__(kThreads) void store_kernel(BlockArgs a) {
   for (unsigned first = blockIdx.x * units; first < a.blocks; first += gridDim.x * units) {
     const BlockAt at = block_at(a, first + unit);
     const T* base = (const T*)(at.values ? a.v : a.k) + at.rows;
-    code_block<T, D, CODE, true>(a.p, at.there && at.block >= 0, at.block, at.values,
+    code_block<T, D, CODE>(a.p, at.there && at.block >= 0, at.block, at.values,
                            [&](int r) { return base + r * a.d.row; }, lds, most);
   }
 }
-// The way back: as many bytes, 100 us of the same size (5.6 TB/s).
+// The way back: as many bytes, 82 us of the same size (6.8 TB/s).
 template <typename T, int D, int CODE>
 __global__ __launch_bounds__(kThreads) void load_kernel(BlockArgs a) {
   __shared__ __align__(16) uint8_t lds[kWaveCount][Part<T, D>::BYTES];
@@ -548,9 +546,9 @@ __device__ __forceinline__ void copy_rows(int heads, int rows, int row_shift, bo
 // the blocks there are, side by side, each an equal run of them, so that most of its blocks are of one page and where
 // that page's rows lie is looked up once (in the lanes, a row each).
 //   Bound: memory; for few rows the launch (4.1 us for 3 sequences).  48 sequences of 36 layers and 20 heads of 64 that
-// take up to 16 rows each: 60 us for 257 MB, 4.3 TB/s.  (All by the caches 72, of it the fillers alone 40, 55 while every block
+// take up to 16 rows each: 51 us for 257 MB, 5.0 TB/s.  (All by the caches 72, of it the fillers alone 40, 55 while every block
 // looked its page and rows up, and the moves alone 40.)
-// 768, 1024 and 1536 fillers measure the same; 4 and 8 copies under way, too.
+// 768, 1024 and 1536 fillers measured the same; 4 and 8 copies under way, too.
 template <typename T, int D, int CODE>
 __global__ __launch_bounds__(kThreads, 4) void commit_kernel(CommitArgs a) {
   __shared__ __align__(16) uint8_t lds[kWaveCount][Part<T, D>::BYTES];
@@ -582,7 +580,7 @@ __global__ __launch_bounds__(kThreads, 4) void commit_kernel(CommitArgs a) {
       const int64_t block = ((int64_t)l * a.p.n_page + page) * heads + gv;
       const T* old = (const T*)(values ? a.vt : a.kt) + l * a.tail.layer + b * a.tail.seq + g * a.tail.head;
       const T* add = (const T*)(values ? a.vn : a.kn) + l * a.fresh.layer + b * a.fresh.seq + g * a.fresh.head;
-      code_block<T, D, CODE, false>(
+      code_block<T, D, CODE>(
           a.p, there, block, values,
           [&](int r) {
             const int x = __shfl(mine, r & 31);
@@ -635,7 +633,7 @@ struct ForkArgs {
 // blockIdx.y: the slot; blockIdx.x: 0 its table, 1 + 2 l + (keys, values) its open rows in layer l.
 // A slot that is copied from stays as it is, so nothing that is read here is written here, and one launch does it.
 //   Bound: memory; for few slots the launch (3.7 us).  64 slots of 36 layers and 20 heads of 64, open rows of up to 31:
-// 34 us, 6.4 TB/s (219 MB; samples of one prompt read the same rows).
+// 34 us, 6.2 TB/s (210 MB; samples of one prompt read the same rows).
 __global__ __launch_bounds__(kThreads) void fork_kernel(ForkArgs a) {
   const int b = blockIdx.y, s = a.parents[b];
   if (s == b) return;
