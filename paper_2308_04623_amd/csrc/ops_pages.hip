@@ -550,7 +550,7 @@ __device__ __forceinline__ void copy_rows(int heads, int rows, int row_shift, bo
 // looked its page and rows up, and the moves alone 40.)
 // 768, 1024 and 1536 fillers measured the same; 4 and 8 copies under way, too.
 template <typename T, int D, int CODE>
-__global__ __launch_bounds__(kThreads, 4) void commit_kernel(CommitArgs a) {
+__global__ __launch_bounds__(kThreads) void commit_kernel(CommitArgs a) {
   __shared__ __align__(16) uint8_t lds[kWaveCount][Part<T, D>::BYTES];
   __shared__ unsigned most[kWaveCount];
   const int R0 = a.p.page_rows, G = a.p.n_kv_head;
