@@ -162,8 +162,8 @@ ssd_status ssd_pages_take(const ssd_page_pool *pool, const ssd_page_seqs *seqs, 
                           void *workspace, size_t workspace_bytes, void *stream);
 
 /* Appends accepted new rows: rows path[b][0 .. path_len[b]-1] (device; path_ld entries from row to row, at
- * most max_path of them count, and none from the first outside [0, k_new's rows) on) of
- * sequence b become its rows length[b] .., in every layer, and length[b] grows by their number (n).
+ * most max_path of them, and no more than k_new has rows, count, and none from the first outside [0, k_new's rows)
+ * on) of sequence b become its rows length[b] .., in every layer, and length[b] grows by their number (n).
  * Pages that get full by it are taken as by ssd_pages_take and made from the tail's and the new
  * rows; rows behind them join the tail, whose other rows stay as they are.  full[b] (device): how many pages got full;
  * -1 where pages or columns of the table did not suffice, and nothing of the sequence changes; 0 for a slot without one.

@@ -423,8 +423,10 @@ __global__ __launch_bounds__(kPlan) void plan_kernel(PlanArgs a) {
   }
   if (threadIdx.x == 0) jobs = 0;
   if constexpr (COMMIT) {
-    for (int b = wave; b < n_seq; b += kPlan / 64) {  // rows up to the path's first that is none
-      const int t = lane < a.max_path ? a.path[b * a.path_ld + lane] : -1, n = min(a.path_len[b], a.max_path);
+    // rows up to the path's first that is none, and no more than there are (a path can name one twice): a sequence then
+    // grows by less than the tail has rows behind its open page, which the kernel behind this one relies on
+    for (int b = wave; b < n_seq; b += kPlan / 64) {
+      const int t = lane < a.max_path ? a.path[b * a.path_ld + lane] : -1, n = min(min(a.path_len[b], a.max_path), a.n_new);
       const unsigned long long bads = __ballot(lane >= n || t < 0 || t >= a.n_new);
       if (lane == 0) rows[b] = bads ? __ffsll(bads) - 1 : 64;
     }
@@ -541,8 +543,8 @@ __device__ __forceinline__ void copy_rows(int heads, int rows, int row_shift, bo
 
 // Workgroups: first `fill` that make the pages that got full, wave by wave; then for each slot one that
 // gives back what is behind the window, and for each layer and keys or values one that moves rows into the tail.
-// (Rows that are moved go to other places of the tail than those of the page: its positions are less
-// than tail_rows apart, so all run side by side.)  How many pages got full is known on the device alone: the fillers share
+// (Rows that are moved go to other places of the tail than those of the page: from the open page's first row to the last
+// new one are page_rows + new rows - 1 at the most, and tail_rows is no less, so all run side by side.)  How many pages got full is known on the device alone: the fillers share
 // the blocks there are, side by side, each an equal run of them, so that most of its blocks are of one page and where
 // that page's rows lie is looked up once (in the lanes, a row each).
 //   Bound: memory; for few rows the launch (4.1 us for 3 sequences).  48 sequences of 36 layers and 20 heads of 64 that

@@ -370,7 +370,7 @@ def _tail(what, k, v, n_layer, n_seq, g, d, like):
 def pages_commit(pages: Pages, refs, table, length, k_tail, v_tail, k_new, v_new, path, path_len, window: int = 0,
                  sinks: int = 0, stream=None):
     """ssd_pages_commit: rows path[b][:path_len[b]] of k_new, v_new [L][B][T][G][D] become sequence b's next
-    rows.  path int32 [B][M], path_len int32 [B].  Returns how many pages of each sequence got full, int32 [B]
+    rows (at most T of them).  path int32 [B][M], path_len int32 [B].  Returns how many pages of each sequence got full, int32 [B]
     (-1: pages did not suffice, and nothing of the sequence changed).  window > 0: pages that no later row
     sees, with this window and these sinks, are given back."""
     what = "ssd_pages_commit"
