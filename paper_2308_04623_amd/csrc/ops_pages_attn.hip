@@ -1,16 +1,17 @@
 // Attention over a paged cache in 8 bits (ssd_paged_attn of ssd_pages.h).
 //
 // With x_j the scaled score of row j, in units of log 2, and a set c of rows:
-//   m_c >= max x_j - 8,  l_c = sum 2^(x_j - m_c),  o_c = sum 2^(x_j - m_c) v_j;
+//   m_c >= max x_j - 23,  l_c = sum 2^(x_j - m_c),  o_c = sum 2^(x_j - m_c) v_j;
 // out = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c with M the largest m_c.
 //
 // A workgroup of four waves takes up to 16 NT queries of one sequence and kv head (its new rows' and the
 // group's heads) and every splits-th part of the rows; a wave takes 32 rows at a time, and never
 // waits for another until the end.  Codes go from memory to registers in operand order (see
 // ops_pages.h), 16 bytes a lane, are made float16 there (exactly: whole numbers up to 127, or
-// 4 bits), and their scales multiply scores and weights:
-//   x = (code_k . q) scale_k scale,   o += code_v (2^(x - m) scale_v),
-// the weights' factor scale_v relative to a power of two that the wave's result is multiplied by at the end.
+// 4 bits), and their scales multiply scores and products:
+//   x = (code_k . q) scale_k scale,   o += (code_v 2^(x - r)) 2^(r - m) scale_v,   r = max x - 15 of the 32 rows and a query.
+// So a weight is rounded by what it is among its own 32 rows, which share a scale, whatever scales and weights other rows
+// have, and o is float32 throughout.
 // Queries are scaled by a power of two each, to the middle of float16's range, and split into
 // parts of 11 bits: bfloat16's 8 bits are one, float32's 24 three.
 //
@@ -40,10 +41,16 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kWaves = 4;
-constexpr float kFar = 4194304.f;  // references from here on take scores that are rounded first: see weights()
-// How far a score may lie above the reference (the largest so far, in units of log 2) before the sums are rescaled: weights
-// up to 2^8, sums to 2^38 of the rows there can be.  So most items rescale nothing.
+constexpr float kFar = 4194304.f - 256.f;  // references from here on take scores that are rounded first: see weights()
+// Weights are up to 2^kUp where their reference is made, so that float16 holds them to 2^-11 of their own or 2^-40 of the
+// largest of their 32 rows.
+constexpr float kUp = 15.f;
+// How far a score may rise from there before the sums are rescaled (weights up to 2^23).  So most items rescale nothing.
 constexpr float kSlack = 8.f;
+// Sums of 2^30 rows with weights up to 2^23 and values up to 2^128 would not be finite where their quotient is.  From finite values
+// of 2^80, or scales of 2^48, on a wave's references are made larger by so much, and its weights smaller.
+constexpr float kLift = 56.f;
+constexpr unsigned kLarge = 127 + 80, kLargeScale = 127 + 48;  // (exponents, as float32 and bfloat16 hold them)
 
 struct Args {
   ssd_paged_attn_desc d;
@@ -108,9 +115,11 @@ __device__ __forceinline__ f32x4 product(bf16x8 a, bf16x8 b, f32x4 c) {
 __device__ __forceinline__ f32x4 product(float a, float b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
-__device__ __forceinline__ float group_max(float x) {  // over the lanes of a column
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
+__device__ __forceinline__ float group_max(float x) {  // over the lanes of a column, within the registers
+  const u32x2 a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const u32x2 b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 // a block's bytes of 32 rows: of keys and of values, 16 a lane each
 template <int D>
@@ -155,12 +164,11 @@ struct Base {
   static constexpr int NQ = F32 ? 3 : 1, NP = F32 ? 2 : 1;  // parts of a query, of a weight
   const Args& a;
   const int lane, g, n;
-  float vunit, vrel;  // o is in units of this power of two; 0: of 1, no page was taken yet; 1 / vunit
-  bool own;           // rows in the model's type were taken
-  bool rounded;       // a reference is far from 0: see weights()
+  float up;      // a reference is so far below the score that it is made of: kUp, or kUp - kLift
+  bool rounded;  // a reference is far from 0: see weights()
 
   __device__ __forceinline__ Base(const Args& args)
-      : a(args), lane(threadIdx.x & 63), g(lane >> 4), n(lane & 15), vunit(0.f), vrel(1.f), own(false), rounded(false) {}
+      : a(args), lane(threadIdx.x & 63), g(lane >> 4), n(lane & 15), up(kUp), rounded(false) {}
 
   // the 8 dims from here on are what the lane has in step s of a product over dims
   __device__ __forceinline__ int dim_at(int s) const { return D == 32 ? 8 * g : 64 * (s >> 1) + 16 * g + 8 * (s & 1); }
@@ -217,20 +225,6 @@ struct Base {
           y -= (float)parts[s][p][i];
         }
       }
-  }
-
-  // The unit of o for values of this scale: whether o has to be multiplied by f.  Weights up to 2^15 are what float16
-  // holds to 2^-32 of the largest there can be.  (Sums of rows in the model's type are far from the largest number: a
-  // unit of 2^-64 at the least.)
-  __device__ __forceinline__ bool new_unit(float size, float& f) {
-    if (!((size > vunit * 0x1p7f || vunit == 0.f) && size > 0.f && size < __builtin_inff())) return false;
-    const unsigned up = (__float_as_uint(size) + 0x7fffffu) & 0x7f800000u;  // the next power of two
-    const unsigned now = max(min(max(up, 9u << 23), 253u << 23) - (7u << 23), own ? 63u << 23 : 0u);
-    const float to = __uint_as_float((254u << 23) - now);
-    f = vunit == 0.f ? to : vunit * to;
-    vunit = __uint_as_float(now);
-    vrel = to;
-    return true;
   }
 
   // 32 rows in the model's type: those from x0 on of `tail` open rows, the first at place `slot` of the ring, and of
@@ -298,6 +292,19 @@ struct Base {
       for (int i = 0; i < 8; ++i) odd |= !finite(rows.v[dt][i]);
     return !__builtin_amdgcn_ballot_w64(odd);
   }
+  // whether |x| is 2^(from - 127) or more, and finite
+  static __device__ __forceinline__ bool large(float x, unsigned from) {
+    return (__float_as_uint(x) >> 23 & 255u) - from < 255u - from;
+  }
+  static __device__ __forceinline__ bool large(uint16_t x, unsigned from) { return (x >> 7 & 255u) - from < 255u - from; }
+  __device__ __forceinline__ bool any_large(const Own& rows) const {
+    bool odd = false;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) odd |= large(rows.v[dt][i], kLarge);
+    return __builtin_amdgcn_ballot_w64(odd);
+  }
   // which of a dim's values are not finite, as 1; they become 0
   __device__ __forceinline__ bf16x8 take_out(Own& rows, int dt) const {
     bf16x8 y;
@@ -317,14 +324,14 @@ template <typename T, int D, int CODE, int NT_>
 struct Tiles : Base<T, D, CODE> {
   typedef Base<T, D, CODE> B;
   using typename B::Own;
-  using B::a, B::g, B::n, B::lane, B::vunit, B::vrel, B::KS, B::DT, B::NQ, B::NP, B::F32;
+  using B::a, B::g, B::n, B::lane, B::KS, B::DT, B::NQ, B::NP, B::F32;
   static constexpr int NT = NT_, COLS = 16 * NT;
   static constexpr bool EARLY = !(D == 128 && (F32 || NT == 2)) && !(F32 && D == 64 && NT == 2);  // see take_own()
   typename B::Query raw[NT];
   f16x8 q[NT][KS][NQ];
   float unit[NT];
   f32x4 o[NT][DT];
-  float m[NT], sub[NT], l[NT];  // reference, what is subtracted (0 for -infinity), this lane's share of the sum
+  float m[NT], l[NT];  // reference, this lane's share of the sum
   int seen_from[NT];
   uint64_t anc[NT];
 
@@ -340,29 +347,19 @@ struct Tiles : Base<T, D, CODE> {
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) o[nt][dt] = (f32x4){0.f, 0.f, 0.f, 0.f};
       m[nt] = -INFINITY;
-      sub[nt] = l[nt] = 0.f;
+      l[nt] = 0.f;
     }
   }
   __device__ __forceinline__ void split() {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) B::split(raw[nt], q[nt], unit[nt]);
   }
-  __device__ __forceinline__ void scale_o(float f) {
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) o[nt][dt] *= f;
-  }
 
-  // s becomes 2^(s by - reference), by >= 0, and 0 where `masked` and not seen(tile, k, r): row 16 k + 4 g + r; the
-  // sums are rescaled where a score is far above the reference.  Product and difference are one operation; from
-  // references of 2^22 on, where the largest score and the reference made of it would differ by the product's
-  // rounding, and the weight with it, they are two.
+  // s by (by >= 0) are the scores of 32 rows; what is `masked` and not seen(tile, k, r): row 16 k + 4 g + r, becomes
+  // -infinity, by then 1.  top: the largest of a column.  The sums are rescaled where it is far above the reference.
   template <typename Seen>
-  __device__ __forceinline__ void weights(f32x4 (&s)[NT][2], float (&by)[NT], bool masked, Seen seen) {
-#pragma clang fp contract(off)
+  __device__ __forceinline__ void meet(f32x4 (&s)[NT][2], float (&by)[NT], float (&top)[NT], bool masked, Seen seen) {
     bool far = false;
-    float top[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       if (masked) {
@@ -373,24 +370,29 @@ struct Tiles : Base<T, D, CODE> {
             s[nt][k][r] = seen(nt, k, r) ? s[nt][k][r] * by[nt] : -INFINITY;
         by[nt] = 1.f;
       }
-      top[nt] = by[nt] * largest(s[nt][0], s[nt][1]);
-      far |= top[nt] > m[nt] + kSlack;
+      top[nt] = group_max(by[nt] * largest(s[nt][0], s[nt][1]));
+      far |= top[nt] > m[nt] + (kSlack + this->up);
     }
     if (__builtin_amdgcn_ballot_w64(far)) {
       bool large = false;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        const float now = fmaxf(m[nt], group_max(top[nt]));
+        const float now = fmaxf(m[nt], top[nt] - this->up);
         const float f = m[nt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[nt] - now);
         m[nt] = now;
-        sub[nt] = now == -INFINITY ? 0.f : now;
-        large |= fabsf(sub[nt]) >= kFar;
+        large |= fabsf(now) >= kFar && now != -INFINITY;
         l[nt] *= f;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[nt][dt] *= f;
       }
       if (__builtin_amdgcn_ballot_w64(large)) this->rounded = true;
     }
+  }
+  // s becomes 2^(s by - ref), and sum what the lane has of its sum.  Product and difference are one operation; from
+  // references of 2^22 on, where the largest score and the reference made of it would differ by the product's
+  // rounding, and the weight with it, they are two.
+  __device__ __forceinline__ void weights(f32x4 (&s)[NT][2], float (&by)[NT], const float (&ref)[NT], float (&sum)[NT]) {
+#pragma clang fp contract(off)
     if (this->rounded) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
@@ -409,9 +411,9 @@ struct Tiles : Base<T, D, CODE> {
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) s[nt][k][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[nt][k][r], by[nt], -sub[nt]));
-      l[nt] += ((s[nt][0][0] + s[nt][0][1]) + (s[nt][0][2] + s[nt][0][3])) +
-               ((s[nt][1][0] + s[nt][1][1]) + (s[nt][1][2] + s[nt][1][3]));
+        for (int r = 0; r < 4; ++r) s[nt][k][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[nt][k][r], by[nt], -ref[nt]));
+      sum[nt] = ((s[nt][0][0] + s[nt][0][1]) + (s[nt][0][2] + s[nt][0][3])) +
+                ((s[nt][1][0] + s[nt][1][1]) + (s[nt][1][2] + s[nt][1][3]));
     }
   }
 
@@ -443,40 +445,46 @@ struct Tiles : Base<T, D, CODE> {
     const int sinks = a.d.sinks;
     int mine = first + 4 * g;
     if (masked) asm volatile("" : "+v"(mine));  // (not to be taken out of the condition, in eight registers)
-    weights(s, by, masked, [&](int nt, int k, int r) {
+    float top[NT], ref[NT], f[NT], sum[NT];
+    meet(s, by, top, masked, [&](int nt, int k, int r) {
       return mine + 16 * k + r >= seen_from[nt] || mine + 16 * k + r < sinks;
     });
-    float f;
-    if (B::new_unit(fabsf(vscale), f)) scale_o(f);
-    const float rel = vscale * vrel;
+    const float below = this->rounded ? 0.f : kUp;  // (where the difference would be rounded, weights might exceed float16)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      // (no further below the query's reference than where f is 0 all the same: `rounded` goes by that)
+      const bool none = top[nt] == -INFINITY;
+      ref[nt] = none ? 0.f : fmaxf(top[nt] - below, m[nt] - 200.f);
+      f[nt] = none ? 0.f : __builtin_amdgcn_exp2f(ref[nt] - m[nt]);
+    }
+    weights(s, by, ref, sum);
     f16x8 w[NT][NP];
-    if (masked && !(fabsf(rel) < __builtin_inff())) {  // rows that a query does not see count 0 whatever the scale
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+    for (int nt = 0; nt < NT; ++nt) {
+      l[nt] += f[nt] * sum[nt];
 #pragma unroll
-        for (int p = 0; p < NP; ++p)
+      for (int i = 0; i < 8; ++i) {
+        float y = s[nt][i >> 2][i & 3];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) w[nt][p][i] = (_Float16)(s[nt][i >> 2][i & 3] == 0.f ? 0.f : __builtin_nanf(""));
-    } else {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          float y = s[nt][i >> 2][i & 3] * rel;
-#pragma unroll
-          for (int p = 0; p < NP; ++p) {
-            w[nt][p][i] = (_Float16)y;
-            y -= (float)w[nt][p][i];
-          }
+        for (int p = 0; p < NP; ++p) {
+          w[nt][p][i] = (_Float16)y;
+          y -= (float)w[nt][p][i];
         }
+      }
+      f[nt] = top[nt] == -INFINITY ? 0.f : f[nt] * vscale;  // rows that a query does not see count 0 whatever the scale
     }
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
       const f16x8 y = c.template values<CODE>(dt);
+      f32x4 part[NT];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) part[nt] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int p = NP - 1; p >= 0; --p)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) o[nt][dt] = product(y, w[nt][p], o[nt][dt]);
+        for (int nt = 0; nt < NT; ++nt) part[nt] = product(y, w[nt][p], part[nt]);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) o[nt][dt] += part[nt] * f[nt];
     }
   }
 
@@ -485,14 +493,14 @@ struct Tiles : Base<T, D, CODE> {
     B::template issue_own<true, EARLY>(rows, b, kv, x0, tail, slot);
   }
   __device__ __forceinline__ void take_own(Own& rows, int b, int kv, int x0, int tail, int start, int slot) {
-    this->own = true;
     f32x4 s[NT][2];
+    unsigned bits[NT];  // which of the lane's 8 rows are seen
+    if (EARLY && B::any_large(rows)) this->up = kUp - kLift;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int k = 0; k < 2; ++k) s[nt][k] = B::own_scores(rows, k, raw[nt]);
     complete<2 * NT>(&s[0][0]);
-    unsigned bits[NT];  // which of the lane's 8 rows are seen
     float by[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -502,8 +510,29 @@ struct Tiles : Base<T, D, CODE> {
       for (int i = 0; i < 8; ++i)
         bits[nt] |= B::sees_own(x0 + 16 * (i >> 2) + 4 * g + (i & 3), tail, start, seen_from[nt], anc[nt]) ? 1u << i : 0u;
     }
-    weights(s, by, true, [&](int nt, int k, int r) { return (bits[nt] >> (4 * k + r) & 1) != 0; });
-    if constexpr (!EARLY) B::template issue_own<false, true>(rows, b, kv, x0, tail, slot);
+    float top[NT], ref[NT], sum[NT];
+    meet(s, by, top, true, [&](int nt, int k, int r) { return (bits[nt] >> (4 * k + r) & 1) != 0; });
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) ref[nt] = m[nt] == -INFINITY ? 0.f : m[nt];
+    weights(s, by, ref, sum);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) l[nt] += sum[nt];
+    if constexpr (!EARLY) {
+      B::template issue_own<false, true>(rows, b, kv, x0, tail, slot);
+      if (this->up == kUp && B::any_large(rows)) {
+        this->up = kUp - kLift;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const float now = m[nt] + kLift, f = fabsf(now) < __builtin_inff() ? __builtin_amdgcn_exp2f(m[nt] - now) : 1.f;
+          m[nt] = now;
+          l[nt] *= f;
+          s[nt][0] *= f;
+          s[nt][1] *= f;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) o[nt][dt] *= f;
+        }
+      }
+    }
     // values that are not finite are taken out of the product, and make NaN where they are seen
     if (!B::all_finite(rows)) {
 #pragma unroll
@@ -760,6 +789,7 @@ __global__ __launch_bounds__(64 * kWaves, W::DIM == 128 || W::COLS == 32 || W::F
     const int items = rest <= 0 ? 0 : rest <= soon ? (rest + others - 1) / others : slow + (rest - soon + all - 1) / all;
     for (int k0 = 0; k0 < items; k0 += 64) {
       if (k0) find(k0);
+      if (__builtin_amdgcn_ballot_w64(page >= 0 && W::large(sc.y, kLargeScale))) w.up = kUp - kLift;
       auto fetch = [&](Codes<D>& x, int k) {
         const int j = min(k - k0, 63);
         const uint8_t* block = a.data + ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)bytes, j) |
@@ -788,7 +818,6 @@ __global__ __launch_bounds__(64 * kWaves, W::DIM == 128 || W::COLS == 32 || W::F
           if (k + u < end) work(x[u], k + u);
         }
     }
-    if (w.vunit != 0.f) w.scale_o(w.vunit);
   }
 
   // the waves' sums, joined

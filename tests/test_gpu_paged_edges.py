@@ -32,3 +32,155 @@ def test_paths_that_name_rows_twice(env, dtype, code, rows, d, t):
         batch.step(path, [64, 40 + t, 64, max(t - 1, 1)])
     batch.open_rows()
     assert batch.host.length[0] == (3 * rows // t + 2) * t
+
+
+# ---------------------------------------------------------------- attention
+
+def sized(c, **kw):
+    """(out, sum of weights times |values|) in 64 bits, and the largest sum of |q_i k_i| scale."""
+    f = lambda x: x.double().numpy()  # noqa: E731
+    hk, hv = c.host()
+    call = lambda g: M.attention(f(c.q), c.table, c.lens, (hk, g(hv)), (f(c.kt), g(f(c.vt))), (f(c.kn), g(f(c.vn))),  # noqa: E731
+                                 c.rows, c.anc, **kw)
+    ref, _, big, _ = call(lambda x: x)
+    return ref, call(np.abs)[0], big
+
+
+def agrees(c, **kw):
+    """Every element of out against its own terms' size: weights are off by twice a score's error, the sums' roundings and
+    their own rounding (2^-11 or 2^-22), the result by its type's.  (As in test_gpu_paged; weights of the
+    same 32 rows are near each other here, so that what is lost of those far below the largest does not count.)"""
+    out, _ = c.run(**kw)
+    ref, size, big = sized(c, **kw)
+    off = size * (2 * P.EPS * (3 * c.d + 8) * big + 64 * P.EPS + (2.0 ** -11 if c.dtype == "bf16" else 2.0 ** -22))
+    if c.dtype == "bf16":
+        off = off + 2.0 ** -8 * (np.abs(ref) + off)
+    got = out.double().cpu().numpy()
+    assert np.isfinite(got).all()
+    worst = (np.abs(got - ref) / np.maximum(off, 1e-300)).max()
+    assert worst <= 1, worst
+
+
+def alike(env, dtype, code, pages, seed=0):
+    """One sequence of `pages` full pages of 32 rows and an open one, whose scores lie near each other.  (Every third of
+    the first 18 pages is the same wave's.)"""
+    c = P.Case(env, dtype, code, 1, 1, 2, 1, 64, 32, [32 * pages + 5], seed=seed, cols=pages + 1)
+    assert pages < 24
+    c.q *= 0.1
+    return c
+
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_pages_of_large_values_without_weight_take_no_bits_from_others(env, dtype, code):
+    """Value scales 2^30 apart; the pages of the large ones have scores far below the others'."""
+    for first in (0, 1):
+        c = alike(env, dtype, code, 18)
+        c.q = c.q.abs() + 0.1
+        raw = c.data.view(1, -1, 1, 2, 32 * 64)
+        for col in range(18):
+            if (col // 3 + first) % 2 == 0:
+                page = c.table[0, col]
+                raw[0, page, 0, 0] = int(M.to_bytes(np.array([-120.0]), code)[0])
+                c.scale[0, page, 0, 0] = 1.0
+                c.scale[0, page, 0, 1] *= 2.0 ** 30
+        # (small rows of the model's type, too)
+        c.vt *= 2.0 ** -6
+        c.vn *= 2.0 ** -6
+        agrees(c)
+
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_values_behind_the_window_take_no_bits_from_others(env, dtype, code):
+    """The first page's scale is 2^30 times the others', for a row behind the window; its other rows are 0."""
+    c = alike(env, dtype, code, 18)
+    _, pv = M.places(32, 64)
+    page = c.table[0, 0]
+    zero, top = (int(M.to_bytes(np.array([x]), code)[0]) for x in (0.0, M.TOP[code]))
+    raw = c.data.view(1, -1, 1, 2, 32 * 64)
+    raw[0, page, 0, 1] = zero
+    raw[0, page, 0, 1, pv[0]] = top
+    c.scale[0, page, 0, 1] *= 2.0 ** 30
+    agrees(c, window=c.lens[0])  # (row 0 is not seen)
+
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_pages_whose_values_are_powers_apart(env, dtype, code):
+    """Each page's rows count to their own size: a page of values 2^-30 of its neighbours', in dims where those are 0."""
+    c = alike(env, dtype, code, 18)
+    _, pv = M.places(32, 64)
+    zero = int(M.to_bytes(np.array([0.0]), code)[0])
+    raw = c.data.view(1, -1, 1, 2, 32 * 64)
+    for col in range(18):
+        page, small = c.table[0, col], col // 3 % 2
+        raw[0, page, 0, 1, (pv[:, :32] if small else pv[:, 32:]).reshape(-1)] = zero
+        if not small:
+            c.scale[0, page, 0, 1] *= 2.0 ** 30
+    c.vt[..., 32:] = 0
+    c.vn[..., 32:] = 0
+    agrees(c)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("own,scale", [(2.0 ** 110, 0.022), (2.0 ** 80, 1e-14), (2.0 ** 66, 1e-20), (2.0 ** 66, 1e-38)])
+def test_large_open_and_new_rows_beside_pages(env, dtype, own, scale):
+    """(The wave that takes the open and new rows takes a page, too, from the 22nd on.)"""
+    c = alike(env, dtype, "int8", 23)
+    c.scale[0, :, :, 1] = scale
+    c.vt *= own
+    c.vn *= own
+    c.check()
+    # as many digits where the large ones are of other dims
+    c.vt[..., 32:] = 0
+    c.vn[..., 32:] = 0
+    agrees(c)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_nan_in_pages_at_the_windows_edge(env, dtype):
+    """Rows of next to no weight in a page whose value scale is NaN: NaN where one of them is seen."""
+    c = P.Case(env, dtype, "int8", 1, 2, 2, 1, 64, 32, [70])
+    c.q = c.q.abs() + 1
+    page = c.table[0, 0]
+    c.data.view(1, -1, 1, 2, 32 * 64)[0, page, 0, 0] = 8
+    c.scale[0, page, 0, 0] = 1.0
+    c.scale[0, page, 0, 1] = math.nan
+    for window, nan in ((70, [True, True]), (60, [True, True]), (40, [True, False]), (39, [False, False])):
+        out, lse = c.run(window=window)
+        assert lse.isfinite().all()
+        assert [bool(out[0, t].isnan().all()) for t in (0, 1)] == nan, window
+        assert [bool(out[0, t].isfinite().all()) for t in (0, 1)] == [not x for x in nan], window
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_nan_at_the_windows_edge_behind_rows_of_more_weight(env, dtype):
+    """(40 queries leave the first pages to one wave: the first rows' page, then the one at the window's edge.)"""
+    c = P.Case(env, dtype, "int8", 1, 40, 2, 1, 64, 32, [300])
+    c.q = c.q.abs() + 1
+    page = c.table[0, 1]
+    c.data.view(1, -1, 1, 2, 32 * 64)[0, page, 0, 0] = 8
+    c.scale[0, page, 0, 0] = 1.0
+    c.scale[0, page, 0, 1] = math.nan
+    out, lse = c.run(window=260, sinks=1)  # query t sees rows from 41 + t on: of page 1 up to t = 22
+    assert lse.isfinite().all() and out[0, :23].isnan().all() and out[0, 23:].isfinite().all()
+
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("t,d,lens", [(1, 64, [740, 37]), (3, 128, [740, 64]), (40, 64, [100, 0]), (17, 128, [20, 740]),
+                                      (2, 32, [9000]), (33, 128, [3000])])
+def test_values_up_to_the_largest(env, dtype, code, t, d, lens):
+    """Results are finite where values are, whatever their sums were: open and new rows, pages, or both near the type's
+    largest, in one part of a sequence and in many."""
+    print(dtype, code, t, d, lens, flush=True)
+    for own, top in ((2.0 ** 125, 0.0), (1.0, 2.0 ** 120), (2.0 ** 125, 2.0 ** 120)):
+        c = P.Case(env, dtype, code, len(lens), t, 4, 2, d, 32, lens)
+        c.q *= 0.2
+        c.vt *= own
+        c.vn *= own
+        assert c.vt.isfinite().all() and c.vn.isfinite().all()
+        if top:
+            c.scale[0, ::2, :, 1] *= top / P.M.TOP[code]
+        c.check()
