@@ -42,8 +42,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kWaves = 4;
 constexpr float kFar = 4194304.f - 256.f;  // references from here on take scores that are rounded first: see weights()
-// Weights are up to 2^kUp where their reference is made, so that float16 holds them to 2^-11 of their own or 2^-40 of the
-// largest of their 32 rows.
+// Weights are up to 2^kUp where their reference is made, so that two float16 parts hold them to 20 bits and more of their own,
+// or 2^-39 of the largest of their 32 rows.
 constexpr float kUp = 15.f;
 // How far a score may rise from there before the sums are rescaled (weights up to 2^23).  So most items rescale nothing.
 constexpr float kSlack = 8.f;
@@ -121,6 +121,24 @@ __device__ __forceinline__ float group_max(float x) {  // over the lanes of a co
   const u32x2 b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
+// Eight weights in two float16 parts each, cut off: 20 bits.  (One part, 11 bits, moved a bfloat16 result by half a step in
+// one of 20 elements; the second is a product more and the time of one in 33 where queries are many: 48 x 5 queries over
+// 7100 rows 155.5 -> 161 us, one query and short calls the same.  Rounded parts, 21 bits, took 164.)
+__device__ __forceinline__ void halves(const f32x4 (&s)[2], f16x8& hi, f16x8& lo) {
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) {
+    const float a = s[i >> 2][i & 3], b = s[i >> 2][(i & 3) + 1];
+    const f16x2 h = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(a, b));
+    float x, y;  // a and b less those, in one operation each
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(x) : "v"(h), "v"(a));
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(y) : "v"(h), "v"(b));
+    const f16x2 r = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(x, y));
+    hi[i] = h[0];
+    hi[i + 1] = h[1];
+    lo[i] = r[0];
+    lo[i + 1] = r[1];
+  }
+}
 // a block's bytes of 32 rows: of keys and of values, 16 a lane each
 template <int D>
 struct Codes {
@@ -161,7 +179,7 @@ struct Base {
   typedef T Type;
   static constexpr bool F32 = sizeof(T) == 4;
   static constexpr int CODE = CODE_, DIM = D, KS = D / 32, DT = D / 16;
-  static constexpr int NQ = F32 ? 3 : 1, NP = F32 ? 2 : 1;  // parts of a query, of a weight
+  static constexpr int NQ = F32 ? 3 : 1, NP = 2;  // parts of a query, of a weight
   const Args& a;
   const int lane, g, n;
   float up;      // a reference is so far below the score that it is made of: kUp, or kUp - kLift
@@ -462,13 +480,17 @@ struct Tiles : Base<T, D, CODE> {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       l[nt] += f[nt] * sum[nt];
+      if constexpr (!F32) {
+        halves(s[nt], w[nt][0], w[nt][1]);
+      } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float y = s[nt][i >> 2][i & 3];
+        for (int i = 0; i < 8; ++i) {
+          float y = s[nt][i >> 2][i & 3];
 #pragma unroll
-        for (int p = 0; p < NP; ++p) {
-          w[nt][p][i] = (_Float16)y;
-          y -= (float)w[nt][p][i];
+          for (int p = 0; p < NP; ++p) {
+            w[nt][p][i] = (_Float16)y;
+            y -= (float)w[nt][p][i];
+          }
         }
       }
       f[nt] = top[nt] == -INFINITY ? 0.f : f[nt] * vscale;  // rows that a query does not see count 0 whatever the scale

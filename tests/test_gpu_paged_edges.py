@@ -184,3 +184,20 @@ def test_values_up_to_the_largest(env, dtype, code, t, d, lens):
         if top:
             c.scale[0, ::2, :, 1] *= top / P.M.TOP[code]
         c.check()
+
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+def test_bfloat16_results_are_off_by_their_own_rounding(env, code):
+    """What a result near 0 shows: weights of cached rows hold 20 bits (cut off, so off by 2^-19), twice that where their sum
+    divides them.  Scores are small, so they add next to nothing."""
+    for t, h, g, d in ((4, 8, 8, 64), (3, 16, 4, 128), (9, 16, 4, 32)):
+        c = P.Case(env, "bf16", code, 2, t, h, g, d, 32, [96, 64])
+        c.q *= 0.02
+        c.kn *= 0.1
+        c.vn *= 0.1
+        out, _ = c.run()
+        ref, size, big = sized(c)
+        off = size * (2 * P.EPS * (3 * d + 8) * big + 64 * P.EPS + 2 * 2.0 ** -19)
+        off = off + 2.0 ** -8 * (np.abs(ref) + off)
+        worst = (np.abs(out.double().cpu().numpy() - ref) / off).max()
+        assert worst <= 1, (t, worst)
