@@ -191,7 +191,8 @@ struct Base {
   // the 8 dims from here on are what the lane has in step s of a product over dims
   __device__ __forceinline__ int dim_at(int s) const { return D == 32 ? 8 * g : 64 * (s >> 1) + 16 * g + 8 * (s & 1); }
 
-  // a query, as it is: its loads are under way when issue() returns
+  // A query, as it is: its loads are under way when issue() returns.  Columns behind the last query load the first of all, see
+  // nothing, and have a reference that no score is above: what they hold decides nothing for the others.
   struct Query {
     u32x4 x[KS][F32 ? 2 : 1];
     int64_t anc;
@@ -364,7 +365,7 @@ struct Tiles : Base<T, D, CODE> {
       B::sees(raw[nt], len, anc[nt], seen_from[nt]);
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) o[nt][dt] = (f32x4){0.f, 0.f, 0.f, 0.f};
-      m[nt] = -INFINITY;
+      m[nt] = raw[nt].step < 0 ? INFINITY : -INFINITY;
       l[nt] = 0.f;
     }
   }
@@ -398,7 +399,7 @@ struct Tiles : Base<T, D, CODE> {
         const float now = fmaxf(m[nt], top[nt] - this->up);
         const float f = m[nt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[nt] - now);
         m[nt] = now;
-        large |= fabsf(now) >= kFar && now != -INFINITY;
+        large |= fabsf(now) >= kFar && fabsf(now) < INFINITY;
         l[nt] *= f;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[nt][dt] *= f;
@@ -530,7 +531,7 @@ struct Tiles : Base<T, D, CODE> {
       bits[nt] = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        bits[nt] |= B::sees_own(x0 + 16 * (i >> 2) + 4 * g + (i & 3), tail, start, seen_from[nt], anc[nt]) ? 1u << i : 0u;
+        bits[nt] |= raw[nt].step >= 0 && B::sees_own(x0 + 16 * (i >> 2) + 4 * g + (i & 3), tail, start, seen_from[nt], anc[nt]) ? 1u << i : 0u;
     }
     float top[NT], ref[NT], sum[NT];
     meet(s, by, top, true, [&](int nt, int k, int r) { return (bits[nt] >> (4 * k + r) & 1) != 0; });

@@ -201,3 +201,20 @@ def test_bfloat16_results_are_off_by_their_own_rounding(env, code):
         off = off + 2.0 ** -8 * (np.abs(ref) + off)
         worst = (np.abs(out.double().cpu().numpy() - ref) / off).max()
         assert worst <= 1, (t, worst)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("t,h,g", [(3, 2, 2), (1, 4, 4), (5, 8, 2), (9, 4, 2)])
+def test_results_depend_on_no_other_sequence(env, dtype, t, h, g):
+    """Bitwise: fewer queries than a tile has columns, a wave that takes open rows and pages behind them, and a first
+    sequence whose first query scores those rows from far below to far above the others'."""
+    c = P.Case(env, dtype, "int8", 2, t, h, g, 64, 32, [5, 740], cols=24)
+    c.kt = c.kt.abs()
+    c.kn = c.kn.abs()
+    c.scale[0, :, :, 0] *= 4
+    want = None
+    for q in (0.0, -100.0, 100.0, 1e30, math.inf, math.nan):
+        c.q[0, 0, 0] = q
+        got = [x[1] for x in c.run()]
+        want = want or got
+        assert all(c.torch.equal(x, y) for x, y in zip(got, want)), q
