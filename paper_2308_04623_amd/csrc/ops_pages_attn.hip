@@ -536,7 +536,12 @@ struct Tiles : Base<T, D, CODE> {
     float top[NT], ref[NT], sum[NT];
     meet(s, by, top, true, [&](int nt, int k, int r) { return (bits[nt] >> (4 * k + r) & 1) != 0; });
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) ref[nt] = m[nt] == -INFINITY ? 0.f : m[nt];
+    for (int nt = 0; nt < NT; ++nt) {
+      ref[nt] = m[nt] == -INFINITY ? 0.f : m[nt];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (s[nt][i >> 2][i & 3] == -INFINITY) bits[nt] &= ~(1u << i);  // (counts as one that is not seen)
+    }
     weights(s, by, ref, sum);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) l[nt] += sum[nt];

@@ -218,3 +218,19 @@ def test_results_depend_on_no_other_sequence(env, dtype, t, h, g):
         got = [x[1] for x in c.run()]
         want = want or got
         assert all(c.torch.equal(x, y) for x, y in zip(got, want)), q
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_values_of_rows_whose_score_is_minus_infinity(env, dtype, bad):
+    """Such a row counts as one that is not seen, so its value may be anything."""
+    c = P.Case(env, dtype, "int8", 1, 2, 2, 1, 64, 32, [40])
+    c.q = c.q.abs() + 1
+    c.kt[0, 0, 33 % c.kt.shape[2]] = -math.inf
+    c.kn[0, 0, 0] = -math.inf
+    want = c.run()
+    assert all(x.isfinite().all() for x in want)
+    c.vt[0, 0, 33 % c.kt.shape[2]] = bad
+    c.vn[0, 0, 0, 5:9] = bad
+    got = c.run()
+    assert all(c.torch.equal(x, y) for x, y in zip(got, want))
