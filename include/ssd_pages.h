@@ -103,7 +103,7 @@ typedef struct {
  * ssd_pages_store never writes), and a cached row whose table entry is no page of the
  * pool is not seen.  A row whose score is -infinity counts as one that is not seen; a score
  * that is NaN or +infinity makes the query's out and lse NaN; an element that is not finite
- * among the values of a seen row makes that element of out NaN.
+ * among the values of a seen row makes that element of out NaN.  A page's scale that is not finite reads as NaN.
  * lse, if not NULL: float32 [n_seq][n_query][n_head], the log of the sum of exponentials of
  * the seen scores.
  *   q, out: element (b, t, h, i) at b seq + t row + h head + i.  dtype, of q, tail, new rows and

@@ -531,7 +531,8 @@ struct Tiles : Base<T, D, CODE> {
       bits[nt] = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        bits[nt] |= raw[nt].step >= 0 && B::sees_own(x0 + 16 * (i >> 2) + 4 * g + (i & 3), tail, start, seen_from[nt], anc[nt]) ? 1u << i : 0u;
+        bits[nt] |= B::sees_own(x0 + 16 * (i >> 2) + 4 * g + (i & 3), tail, start, seen_from[nt], anc[nt]) ? 1u << i : 0u;
+      if (raw[nt].step < 0) bits[nt] = 0;
     }
     float top[NT], ref[NT], sum[NT];
     meet(s, by, top, true, [&](int nt, int k, int r) { return (bits[nt] >> (4 * k + r) & 1) != 0; });
@@ -817,7 +818,6 @@ __global__ __launch_bounds__(64 * kWaves, W::DIM == 128 || W::COLS == 32 || W::F
     const int items = rest <= 0 ? 0 : rest <= soon ? (rest + others - 1) / others : slow + (rest - soon + all - 1) / all;
     for (int k0 = 0; k0 < items; k0 += 64) {
       if (k0) find(k0);
-      if (__builtin_amdgcn_ballot_w64(page >= 0 && W::large(sc.y, kLargeScale))) w.up = kUp - kLift;
       auto fetch = [&](Codes<D>& x, int k) {
         const int j = min(k - k0, 63);
         const uint8_t* block = a.data + ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)bytes, j) |
@@ -838,6 +838,9 @@ __global__ __launch_bounds__(64 * kWaves, W::DIM == 128 || W::COLS == 32 || W::F
       Codes<D> x[ST];
 #pragma unroll
       for (int u = 0; u < ST - 1; ++u) fetch(x[u], k0 + u);
+      sc.x = W::finite(sc.x) ? sc.x : __builtin_nanf("");  // (infinity times a code is infinity or NaN: all of the page is NaN)
+      sc.y = W::finite(sc.y) ? sc.y : __builtin_nanf("");
+      if (__builtin_amdgcn_ballot_w64(page >= 0 && W::large(sc.y, kLargeScale))) w.up = kUp - kLift;
       const int end = min(k0 + 64, items);
       for (int k = k0; k < end; k += ST)
 #pragma unroll

@@ -234,3 +234,20 @@ def test_values_of_rows_whose_score_is_minus_infinity(env, dtype, bad):
     c.vn[0, 0, 0, 5:9] = bad
     got = c.run()
     assert all(c.torch.equal(x, y) for x, y in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_page_scales_that_are_not_finite(env, dtype, code, bad):
+    """All of a head's keys (out and lse) or values (out) of the page are NaN for queries that see a row of it."""
+    for which in (0, 1):
+        c = P.Case(env, dtype, code, 1, 2, 4, 2, 64, 32, [740], cols=24)
+        c.data[0, :, 1, 0] = int(M.to_bytes(np.array([-4.0]), code)[0])  # (scores of one sign: with infinity all -infinity)
+        c.q = c.q.abs() + 1
+        want, lse = c.run()
+        c.scale[0, c.table[0, 21], 1, which] = bad
+        got, l2 = c.run()
+        assert got[0, :, 2:].isnan().all() and c.torch.equal(got[0, :, :2], want[0, :, :2])
+        assert l2[0, :, 2:].isnan().all() if which == 0 else c.torch.equal(l2, lse)
+        assert c.torch.equal(l2[0, :, :2], lse[0, :, :2])
