@@ -226,11 +226,11 @@ struct Base {
       for (int i = 0; i < 8; ++i) {
         if constexpr (F32) x[s][i] = __uint_as_float(q.x[s][i >> 2][i & 3]);
         else x[s][i] = __uint_as_float(i & 1 ? q.x[s][0][i >> 1] & 0xffff0000u : q.x[s][0][i >> 1] << 16);
-        top = fmaxf(top, fabsf(x[s][i]));
+        top = fmaxf(top, finite(x[s][i]) ? fabsf(x[s][i]) : 0.f);
       }
     top = group_max(top);
-    // the largest to [2^14, 2^15): what is smaller by up to 2^28 keeps its 11 bits
-    const int e = top < __builtin_inff() ? max((int)(__float_as_uint(top) >> 23) - 127, -100) : 14;
+    // the largest finite one to [2^14, 2^15): what is smaller by up to 2^28 keeps its 11 bits
+    const int e = max((int)(__float_as_uint(top) >> 23) - 127, -100);
     const float by = __uint_as_float((unsigned)(min(14 - e, 127) + 127) << 23);
     unit = fabsf(a.scale2) * __uint_as_float((unsigned)(max(e - 14, -126) + 127) << 23);
 #pragma unroll
@@ -241,7 +241,7 @@ struct Base {
 #pragma unroll
         for (int p = 0; p < NQ; ++p) {
           parts[s][p][i] = (_Float16)y;
-          y -= (float)parts[s][p][i];
+          y = finite(y) ? y - (float)parts[s][p][i] : 0.f;  // (infinity is one part)
         }
       }
   }

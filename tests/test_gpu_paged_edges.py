@@ -251,3 +251,27 @@ def test_page_scales_that_are_not_finite(env, dtype, code, bad):
         assert got[0, :, 2:].isnan().all() and c.torch.equal(got[0, :, :2], want[0, :, :2])
         assert l2[0, :, 2:].isnan().all() if which == 0 else c.torch.equal(l2, lse)
         assert c.torch.equal(l2[0, :, :2], lse[0, :, :2])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("others", [1.0, 2.0 ** 30])
+def test_queries_with_infinite_elements(env, dtype, code, others):
+    """Every score is infinite, of the sign that the key's element gives it, or NaN."""
+    c = P.Case(env, dtype, code, 1, 3, 2, 1, 64, 32, [100])
+    raw = c.data.view(1, -1, 1, 2, 32 * 64)
+    pk, _ = M.places(32, 64)
+    for x in (c.kt, c.kn):
+        x[..., 3] = 2.0
+    for page in c.table[0, :3]:
+        raw[0, page, 0, 0, pk[:, 3]] = int(M.to_bytes(np.array([5.0]), code)[0])
+    c.q *= others
+    want, lse = c.run()
+    assert want.isfinite().all()
+    c.q[0, 0, 0, 3] = -math.inf           # all rows' scores -infinity: no row is seen
+    c.q[0, 1, 0, 3] = math.inf            # all +infinity
+    c.q[0, 2, 0, 2:4] = math.inf          # some +infinity, some NaN
+    got, l2 = c.run()
+    assert not got[0, 0, 0].any() and l2[0, 0, 0] == -math.inf
+    assert got[0, 1:, 0].isnan().all() and l2[0, 1:, 0].isnan().all()
+    assert c.torch.equal(got[:, :, 1], want[:, :, 1]) and c.torch.equal(l2[:, :, 1], lse[:, :, 1])
