@@ -83,7 +83,8 @@ def _ops():
 
 
 class Pages:
-    """The pool: data uint8 [L][P][G][2][page_rows * D], scale float32 [L][P][G][2], contiguous."""
+    """The pool: data uint8 [L][P][G][2][page_rows * D], scale float32 [L][P][G][2], contiguous.  It stays the pool of these
+    tensors: their contents change, its attributes do not (other tensors: another Pages)."""
 
     def __init__(self, data, scale, page_rows: int, code: str = "int8"):
         what = "Pages"
@@ -103,6 +104,14 @@ class Pages:
         self._pool = _Pool(CODES[code], l, p, g, page_rows, self.head_dim, data.data_ptr(), scale.data_ptr())
         self._ref = C.byref(self._pool)
         self.kind = code, l, p, g, page_rows, self.head_dim, self._dev  # (all that checks depend on)
+
+    def __setattr__(self, name, value):
+        if "kind" in self.__dict__:  # (set last; the calls hold the tensors' addresses)
+            _refuse("Pages", f"{name} cannot be replaced; make another Pages")
+        super().__setattr__(name, value)
+
+    def __delattr__(self, name):
+        _refuse("Pages", f"{name} cannot be taken away")
 
     @classmethod
     def empty(cls, n_layer: int, n_page: int, n_kv_head: int, head_dim: int, page_rows: int = 32, code: str = "int8",
