@@ -82,11 +82,11 @@ class Batch:
         paged.pages_fork(self.refs, self.table, self.length, p, self.k_tail, self.v_tail, self.page_rows)
 
     def masks(self, parents) -> torch.Tensor:
-        """int64 [n_seq][max_nodes] of trees parents [n_seq][max_nodes]: -1 a root, below -1 no node."""
+        """int64 [n_seq][max_nodes] of trees parents [n_seq][max_nodes]: -1 a root, below -1 no node (and no node's parent)."""
         anc = np.zeros(parents.shape, np.uint64)
         for b, row in enumerate(parents):
             for i, p in enumerate(row):
-                if p >= i:
+                if p >= i or p >= 0 and row[p] < -1:
                     raise ValueError(f"node {i} of sequence {b} has parent {p}")
                 if p >= -1:
                     anc[b, i] = (anc[b, p] if p >= 0 else np.uint64(0)) | np.uint64(1 << i)
