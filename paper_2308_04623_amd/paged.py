@@ -298,6 +298,7 @@ def pages_store(pages: Pages, ids, k, v, layer: int = 0, stream=None):
     x.unflatten(2, (n, page_rows)).transpose(1, 2)."""
     what = "ssd_pages_store"
     _pages(what, pages)
+    layer = ops.operator.index(layer)
     d = _plan(_key(what, (pages.kind, layer), ids, k, v),
               lambda: _counts(what, layer=layer) or C.byref(_block_rows(what, pages, ids, k, v)))
     where = _elsewhere(pages._dev, stream)
@@ -313,8 +314,8 @@ def pages_load(pages: Pages, ids, dtype=torch.float32, layer: int = 0, n_layer: 
     `layer` on (default: all), as the values that the pages stand for; ids outside the pool give zeros."""
     what = "ssd_pages_load"
     _pages(what, pages)
-    if n_layer is None:
-        n_layer = pages.n_layer - layer
+    layer = ops.operator.index(layer)
+    n_layer = pages.n_layer - layer if n_layer is None else ops.operator.index(n_layer)
 
     def make():
         _vector(what, "ids", ids, torch.int32, None, pages.data)
@@ -384,6 +385,7 @@ def pages_commit(pages: Pages, refs, table, length, k_tail, v_tail, k_new, v_new
     sees, with this window and these sinks, are given back."""
     what = "ssd_pages_commit"
     _pages(what, pages)
+    window, sinks = ops.operator.index(window), ops.operator.index(sinks)
     b, c, ld, tail, fresh, path_ld, need = _plan(
         _key(what, (pages.kind, window, sinks), refs, table, length, k_tail, v_tail, k_new, v_new, path, path_len),
         lambda: _counts(what, window=window, sinks=sinks) or
@@ -428,6 +430,7 @@ def pages_fork(refs, table, length, parents, k_tail, v_tail, page_rows: int, str
     """ssd_pages_fork: slot b becomes a copy of slot parents[b] (int32 [B]), which has to keep itself; itself: it stays as it
     is; any other value: it is freed."""
     what = "ssd_pages_fork"
+    page_rows = ops.operator.index(page_rows)
 
     def make():
         _counts(what, page_rows=page_rows)

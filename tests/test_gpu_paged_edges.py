@@ -275,3 +275,34 @@ def test_queries_with_infinite_elements(env, dtype, code, others):
     assert not got[0, 0, 0].any() and l2[0, 0, 0] == -math.inf
     assert got[0, 1:, 0].isnan().all() and l2[0, 1:, 0].isnan().all()
     assert c.torch.equal(got[:, :, 1], want[:, :, 1]) and c.torch.equal(l2[:, :, 1], lse[:, :, 1])
+
+
+# ---------------------------------------------------------------- the binding
+
+def test_numbers_count_by_their_value(env):
+    """Whole numbers of any kind, a tensor's entry whose value changes between calls among them."""
+    torch, paged, _ = env
+    batch = P.grown(env)
+    ids = batch.i32([0, 1])
+    like = paged.pages_load(batch.pages, ids, layer=1)
+    which = torch.tensor(1)
+    for layer in (np.int64(1), which):
+        assert all(torch.equal(x, y) for x, y in zip(paged.pages_load(batch.pages, ids, layer=layer, n_layer=np.int32(1)), like))
+    which.zero_()
+    for x, y in zip(paged.pages_load(batch.pages, ids, layer=which, n_layer=1), paged.pages_load(batch.pages, ids, layer=0)):
+        assert torch.equal(x[:1], y[:1])
+    before = batch.pages.data.clone()
+    paged.pages_store(batch.pages, ids.flip(0), *like, layer=np.int64(1))
+    assert torch.equal(batch.pages.data[0], before[0]) and torch.equal(batch.pages.data[1, 1], before[1, 0])
+    parents = batch.i32([0, 0, 2, 3, 4, 5, 6, 7])
+    paged.pages_fork(*batch.seqs(), parents, batch.kt, batch.vt, np.int64(32))
+    batch.host.fork(parents.tolist())
+    batch.same()
+    kn = torch.zeros((2, 8, 8, 2, 64), device="cuda").bfloat16()
+    paged.pages_commit(batch.pages, *batch.seqs(), batch.kt, batch.vt, kn, kn, batch.i32([[0, 1]] * 8), batch.i32([2] * 8),
+                       window=np.int64(40), sinks=np.int16(1))
+    batch.host.commit([[0, 1]] * 8, [2] * 8, 8, 40, 1)
+    batch.same()
+    for bad in (1.0, "1", None):
+        with pytest.raises(TypeError):
+            paged.pages_store(batch.pages, ids, *like, layer=bad)
