@@ -287,6 +287,8 @@ def _prepare_fork(case, gen, rand, randn):
         for layer in range(layers):
             x[layer] = randn(*x.shape[1:]).to(dt)
         state[name] = x
+    for x in ("refs", "table", "length"):
+        state[x + "0"] = state[x].clone()
     return state
 
 
@@ -364,6 +366,7 @@ def _last_page(case, table, length, full):
 
 def _fork_own(case, s):
     from paper_2308_04623_amd import paged
+    _again(s, "refs", "table", "length")  # (else every pass but the first finds its tables as it would leave them)
     paged.pages_fork(s["refs"], s["table"], s["length"], s["parents"], s["k_tail"], s["v_tail"], case["rows"])
     return {x: s[x] for x in ("refs", "table", "length", "k_tail", "v_tail")}
 
