@@ -530,7 +530,8 @@ def _commit_plain(case, s):
         c = new.transpose(2, 3).gather(3, step.view(1, b, 1, rows, 1).expand(layers, -1, hkv, -1, d))
         code, scale = _quantized(torch.where(from_tail.view(1, b, 1, rows, 1), a, c), case)
         # (a page given back at once, behind a short window, is not read)
-        there = (full > 0) & (table.gather(1, (after - 1).clamp(min=0).view(b, 1)).squeeze(1) >= 0)
+        # (nor one behind the table's last column, of a sequence that was not served)
+        there = (full > 0) & (table.gather(1, (after - 1).clamp(0, cols - 1).view(b, 1)).squeeze(1) >= 0)
         out[name] = torch.where(there.view(1, b, 1, 1, 1), code * scale, torch.zeros_like(code)).to(tail.dtype)
         tail = tail.clone()
         tail[:, bi, :, (length[bi] + mi) % ring] = new[:, bi, s["path"].long()[bi, mi]].transpose(0, 1)
