@@ -111,11 +111,10 @@ typedef struct {
  * 1024; tail_rows >= page_rows; pointers and strides as ssd_rows_desc says; out shares no
  * element with an input (it may lie between its rows, heads or tokens, where a step that divides the larger
  * ones of both tells them apart).  window and sinks >= 0.
- * Scores, softmax and sums are float32; 8-bit codes are multiplied exactly.  bfloat16 calls hold
- * the weights exp(x - max) in 20 bits for the product with the cached values (16 for that with others); float32 calls
- * hold queries in 33 bits and weights in 22 for theirs; both to 2^-39 of the largest weight of the same 32 rows
- * (32 a .. 32 a + 31; 2^-24 from scores of 2^21 on), and products of a row's weight and its page's scale to 2^-149.  So no
- * page takes bits from another's, whatever its scale.  Sums are finite where their quotient is (up to scores of 2^29).
+ * Scores, softmax and sums are float32; 8-bit codes are multiplied exactly.  For the product with the cached values bfloat16 calls
+ * hold the weights exp(x - max) in 20 bits or to 2^-24 of the largest weight of the same 32 rows (32 a .. 32 a + 31), float32
+ * calls in 22 bits or to 2^-39 of it, and queries in 33 bits; for that with other values bfloat16 calls hold them in 16 bits.
+ * No page takes bits from another's, whatever its scale.  Sums are finite where their quotient is (up to scores of 2^29).
  * Errors: SSD_E_INVALID_ARG, SSD_E_CAPACITY (workspace too small or not 16-byte aligned, or more than 2^24 workgroups),
  * SSD_E_UNSUPPORTED (page_rows, head_dim, alignment), SSD_E_DEVICE. */
 typedef struct {

@@ -1,7 +1,7 @@
 // Attention over a paged cache in 8 bits (ssd_paged_attn of ssd_pages.h).
 //
 // With x_j the scaled score of row j, in units of log 2, and a set c of rows:
-//   m_c >= max x_j - 23,  l_c = sum 2^(x_j - m_c),  o_c = sum 2^(x_j - m_c) v_j;
+//   m_c >= max x_j - 8,  l_c = sum 2^(x_j - m_c),  o_c = sum 2^(x_j - m_c) v_j;
 // out = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c with M the largest m_c.
 //
 // A workgroup of four waves takes up to 16 NT queries of one sequence and kv head (its new rows' and the
@@ -9,7 +9,7 @@
 // waits for another until the end.  Codes go from memory to registers in operand order (see
 // ops_pages.h), 16 bytes a lane, are made float16 there (exactly: whole numbers up to 127, or
 // 4 bits), and their scales multiply scores and products:
-//   x = (code_k . q) scale_k scale,   o += (code_v 2^(x - r)) 2^(r - m) scale_v,   r = max x - 15 of the 32 rows and a query.
+//   x = (code_k . q) scale_k scale,   o += (code_v 2^(x - r)) 2^(r - m) scale_v,   r = max x of the 32 rows and a query.
 // So a weight is rounded by what it is among its own 32 rows, which share a scale, whatever scales and weights other rows
 // have, and o is float32 throughout.
 // Queries are scaled by a power of two each, to the middle of float16's range, and split into
@@ -42,11 +42,12 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kWaves = 4;
 constexpr float kFar = 4194304.f - 256.f;  // references from here on take scores that are rounded first: see weights()
-// Weights are up to 2^kUp where their reference is made, so that two float16 parts hold them to 20 bits and more of their own,
-// or 2^-39 of the largest of their 32 rows.
-constexpr float kUp = 15.f;
-// How far a score may rise from there before the sums are rescaled (weights up to 2^23).  So most items rescale nothing.
+// How far a score may lie above the reference (the largest so far, in units of log 2) before the sums are rescaled: weights
+// up to 2^8.  So most items rescale nothing.
 constexpr float kSlack = 8.f;
+// float32 calls hold all weights, and with them l and o, multiplied by 2^kUp: so the lower ones of two float16 parts are not
+// below what float16 holds to 11 bits.  (By the reference instead, exponents would be rounded as numbers around 15.)
+constexpr float kUp = 15.f;
 // Sums of 2^30 rows with weights up to 2^23 and values up to 2^128 would not be finite where their quotient is.  From finite values
 // of 2^80, or scales of 2^48, on a wave's references are made larger by so much, and its weights smaller.
 constexpr float kLift = 56.f;
@@ -121,7 +122,7 @@ __device__ __forceinline__ float group_max(float x) {  // over the lanes of a co
   const u32x2 b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
-// Eight weights in two float16 parts each, cut off: 20 bits.  (One part, 11 bits, moved a bfloat16 result by half a step in
+// Eight weights (1 the largest) in two float16 parts each, cut off: 20 bits from 2^-4 on, and to 2^-24.  (One part, 11 bits, moved a bfloat16 result by half a step in
 // one of 20 elements; the second is a product more and the time of one in 33 where queries are many: 48 x 5 queries over
 // 7100 rows 155.5 -> 161 us, one query and short calls the same.  Rounded parts, 21 bits, took 164.)
 __device__ __forceinline__ void halves(const f32x4 (&s)[2], f16x8& hi, f16x8& lo) {
@@ -182,11 +183,11 @@ struct Base {
   static constexpr int NQ = F32 ? 3 : 1, NP = 2;  // parts of a query, of a weight
   const Args& a;
   const int lane, g, n;
-  float up;      // a reference is so far below the score that it is made of: kUp, or kUp - kLift
+  float lift;    // a reference is so far above the score that it is made of: 0 or kLift
   bool rounded;  // a reference is far from 0: see weights()
 
   __device__ __forceinline__ Base(const Args& args)
-      : a(args), lane(threadIdx.x & 63), g(lane >> 4), n(lane & 15), up(kUp), rounded(false) {}
+      : a(args), lane(threadIdx.x & 63), g(lane >> 4), n(lane & 15), lift(0.f), rounded(false) {}
 
   // the 8 dims from here on are what the lane has in step s of a product over dims
   __device__ __forceinline__ int dim_at(int s) const { return D == 32 ? 8 * g : 64 * (s >> 1) + 16 * g + 8 * (s & 1); }
@@ -390,13 +391,13 @@ struct Tiles : Base<T, D, CODE> {
         by[nt] = 1.f;
       }
       top[nt] = group_max(by[nt] * largest(s[nt][0], s[nt][1]));
-      far |= top[nt] > m[nt] + (kSlack + this->up);
+      far |= top[nt] > m[nt] + (kSlack - this->lift);
     }
     if (__builtin_amdgcn_ballot_w64(far)) {
       bool large = false;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        const float now = fmaxf(m[nt], top[nt] - this->up);
+        const float now = fmaxf(m[nt], top[nt] + this->lift);
         const float f = m[nt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[nt] - now);
         m[nt] = now;
         large |= fabsf(now) >= kFar && fabsf(now) < INFINITY;
@@ -407,7 +408,7 @@ struct Tiles : Base<T, D, CODE> {
       if (__builtin_amdgcn_ballot_w64(large)) this->rounded = true;
     }
   }
-  // s becomes 2^(s by - ref), and sum what the lane has of its sum.  Product and difference are one operation; from
+  // s becomes 2^(s by - ref) (float32: 2^kUp times that), and sum what the lane has of its sum.  Product and difference are one operation; from
   // references of 2^22 on, where the largest score and the reference made of it would differ by the product's
   // rounding, and the weight with it, they are two.
   __device__ __forceinline__ void weights(f32x4 (&s)[NT][2], float (&by)[NT], const float (&ref)[NT], float (&sum)[NT]) {
@@ -430,7 +431,10 @@ struct Tiles : Base<T, D, CODE> {
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) s[nt][k][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[nt][k][r], by[nt], -ref[nt]));
+        for (int r = 0; r < 4; ++r) {
+          s[nt][k][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[nt][k][r], by[nt], -ref[nt]));
+          if constexpr (F32) s[nt][k][r] *= 1 << (int)kUp;
+        }
       sum[nt] = ((s[nt][0][0] + s[nt][0][1]) + (s[nt][0][2] + s[nt][0][3])) +
                 ((s[nt][1][0] + s[nt][1][1]) + (s[nt][1][2] + s[nt][1][3]));
     }
@@ -468,12 +472,11 @@ struct Tiles : Base<T, D, CODE> {
     meet(s, by, top, masked, [&](int nt, int k, int r) {
       return mine + 16 * k + r >= seen_from[nt] || mine + 16 * k + r < sinks;
     });
-    const float below = this->rounded ? 0.f : kUp;  // (where the difference would be rounded, weights might exceed float16)
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       // (no further below the query's reference than where f is 0 all the same: `rounded` goes by that)
       const bool none = top[nt] == -INFINITY;
-      ref[nt] = none ? 0.f : fmaxf(top[nt] - below, m[nt] - 200.f);
+      ref[nt] = none ? 0.f : fmaxf(top[nt], m[nt] - 200.f);
       f[nt] = none ? 0.f : __builtin_amdgcn_exp2f(ref[nt] - m[nt]);
     }
     weights(s, by, ref, sum);
@@ -518,7 +521,7 @@ struct Tiles : Base<T, D, CODE> {
   __device__ __forceinline__ void take_own(Own& rows, int b, int kv, int x0, int tail, int start, int slot) {
     f32x4 s[NT][2];
     unsigned bits[NT];  // which of the lane's 8 rows are seen
-    if (EARLY && B::any_large(rows)) this->up = kUp - kLift;
+    if (EARLY && B::any_large(rows)) this->lift = kLift;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -548,8 +551,8 @@ struct Tiles : Base<T, D, CODE> {
     for (int nt = 0; nt < NT; ++nt) l[nt] += sum[nt];
     if constexpr (!EARLY) {
       B::template issue_own<false, true>(rows, b, kv, x0, tail, slot);
-      if (this->up == kUp && B::any_large(rows)) {
-        this->up = kUp - kLift;
+      if (this->lift == 0.f && B::any_large(rows)) {
+        this->lift = kLift;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           const float now = m[nt] + kLift, f = fabsf(now) < __builtin_inff() ? __builtin_amdgcn_exp2f(m[nt] - now) : 1.f;
@@ -651,7 +654,7 @@ __device__ __forceinline__ void put_query(const Args& a, int b, int t, int h, in
   put4((T*)a.out + b * a.d.out_seq + t * a.d.out_row + h * a.d.out_head + dim, l == 0.f ? (f32x4){0.f, 0.f, 0.f, 0.f} : o * by);
   if (a.lse && dim == 0)
     a.lse[((int64_t)b * a.d.n_query + t) * a.d.n_head + h] =
-        l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+        l == 0.f ? -INFINITY : (m + (__builtin_amdgcn_logf(l) - (sizeof(T) == 4 ? kUp : 0.f))) * 0.6931471805599453f;
 }
 
 // The cached rows that a sequence's queries can see: columns [0, sinks) and those from `from` on of its table, in all
@@ -840,7 +843,7 @@ __global__ __launch_bounds__(64 * kWaves, W::DIM == 128 || W::COLS == 32 || W::F
       for (int u = 0; u < ST - 1; ++u) fetch(x[u], k0 + u);
       sc.x = W::finite(sc.x) ? sc.x : __builtin_nanf("");  // (infinity times a code is infinity or NaN: all of the page is NaN)
       sc.y = W::finite(sc.y) ? sc.y : __builtin_nanf("");
-      if (__builtin_amdgcn_ballot_w64(page >= 0 && W::large(sc.y, kLargeScale))) w.up = kUp - kLift;
+      if (__builtin_amdgcn_ballot_w64(page >= 0 && W::large(sc.y, kLargeScale))) w.lift = kLift;
       const int end = min(k0 + 64, items);
       for (int k = k0; k < end; k += ST)
 #pragma unroll
