@@ -306,3 +306,40 @@ def test_numbers_count_by_their_value(env):
     for bad in (1.0, "1", None):
         with pytest.raises(TypeError):
             paged.pages_store(batch.pages, ids, *like, layer=bad)
+
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+def test_pages_past_32_bits_are_the_ones_that_are_named(env, code):
+    """A pool of 6 GB whose last page of the last layer, 4 GB and more from the first, and first page get rows of their own:
+    written, read back and attended to, each to half a code of its own largest magnitude."""
+    torch, paged, _ = env
+    g, rows, d, n = 2, 32, 64, 370_000
+    data = torch.zeros((2, n, g, 2, rows * d), dtype=torch.uint8, device="cuda")
+    scale = torch.zeros((2, n, g, 2), device="cuda")
+    pages = paged.Pages(data, scale, rows, code)
+    assert data[1, n - 1].data_ptr() - data.data_ptr() > 1 << 32
+    k, v = P.blocks(torch, "bf16", 2, 2, g, rows, d, seed=5)
+    ids = torch.tensor([n - 1, 0], dtype=torch.int32, device="cuda")
+    paged.pages_store(pages, ids, k.cuda(), v.cuda())
+    wanted, scales = P.host_pages(k, v, code)
+    at = [n - 1, 0]
+    assert np.array_equal(M.from_bytes(data[:, at].cpu().numpy(), code), M.from_bytes(wanted, code))
+    assert np.array_equal(scale[:, at].cpu().numpy(), scales)
+    assert (scale.count_nonzero(dim=(2, 3)) > 0).sum() == 4  # (no other page)
+    kk, vv = paged.pages_load(pages, ids, torch.float32)
+    for x, y, p in ((kk, k, 0), (vv, v, 1)):
+        host = M.page_values(wanted, scales, rows, d, code)[p]
+        assert torch.equal(x.cpu(), torch.from_numpy(host.astype(np.float32)))
+        top = y.float().abs().amax((3, 4), keepdim=True)
+        # (half a code, or half of e4m3's step at the top, 16 of 448; and the roundings of r, x r and the value)
+        half = top / 254 if code == "int8" else top * 16 / 448
+        assert ((x.cpu() - y.float()).abs() <= half * (1 + 2.0 ** -10)).all()
+    # attention over the last layer's last page gives what a pool of this page alone gives
+    c = P.Case(env, "bf16", code, 1, 2, 2, g, d, rows, [rows])
+    x = [getattr(c, w).cuda() for w in ("kt", "vt", "kn", "vn")]
+    length = torch.tensor([rows], dtype=torch.int32, device="cuda")
+    for i, page in enumerate(at):
+        small = paged.Pages(data[1:, page:page + 1].contiguous(), scale[1:, page:page + 1].contiguous(), rows, code)
+        outs = [paged.paged_attention(c.q.cuda(), p, torch.tensor([[where, -1]], dtype=torch.int32, device="cuda"), length, *x,
+                                      layer=layer) for p, where, layer in ((pages, page, 1), (small, 0, 0))]
+        assert outs[0].isfinite().all() and torch.equal(*outs), page
