@@ -405,7 +405,8 @@ struct PlanArgs {
 // timing.  One workgroup: the sums over slots and pages are two scans, and a launch between workgroups would
 // cost more (a launch 3 us) than the whole.
 //   Bound: latency, a chain of some ten loads and meetings.  48 sequences, 1216 pages: 8.4 us (15.6 before refs, lengths
-// and paths were loaded at once ahead of everything, and before scans stayed in registers); 3 sequences 3.8.
+// and paths were loaded at once ahead of everything, and before scans stayed in registers); 3 sequences 3.8.  Paths take
+// a turn for 16 slots: a commit of one layer takes 14 us for 512 sequences and 84 for 4096.
 template <bool COMMIT>
 __global__ __launch_bounds__(kPlan) void plan_kernel(PlanArgs a) {
   __shared__ int want[4096], first[4096], col0[4096], sums[kPlan / 64], jobs;
@@ -548,7 +549,7 @@ __device__ __forceinline__ void copy_rows(int heads, int rows, int row_shift, bo
 // the blocks there are, side by side, each an equal run of them, so that most of its blocks are of one page and where
 // that page's rows lie is looked up once (in the lanes, a row each).
 //   Bound: memory; for few rows the launch (4.1 us for 3 sequences).  48 sequences of 36 layers and 20 heads of 64 that
-// take up to 16 rows each: 51 us for 257 MB, 5.0 TB/s.  (All by the caches 72, of it the fillers alone 40, 55 while every block
+// take up to 16 rows each: 50 us for 257 MB, 5.1 TB/s.  (All by the caches 72, of it the fillers alone 40, 55 while every block
 // looked its page and rows up, and the moves alone 40.)
 // 768, 1024 and 1536 fillers measured the same; 4 and 8 copies under way, too.
 template <typename T, int D, int CODE>
@@ -635,7 +636,7 @@ struct ForkArgs {
 // blockIdx.y: the slot; blockIdx.x: 0 its table, 1 + 2 l + (keys, values) its open rows in layer l.
 // A slot that is copied from stays as it is, so nothing that is read here is written here, and one launch does it.
 //   Bound: memory; for few slots the launch (3.7 us).  64 slots of 36 layers and 20 heads of 64, open rows of up to 31:
-// 34 us, 6.2 TB/s (210 MB; samples of one prompt read the same rows).
+// 35 us, 6.0 TB/s (210 MB; samples of one prompt read the same rows).
 __global__ __launch_bounds__(kThreads) void fork_kernel(ForkArgs a) {
   const int b = blockIdx.y, s = a.parents[b];
   if (s == b) return;

@@ -16,15 +16,17 @@
 // parts of 11 bits: bfloat16's 8 bits are one, float32's 24 three.
 //
 // Bound, and what it measured (int8 unless said otherwise; read: 6.1 TB/s is the most this card reads at, 5.2 a copy moves at):
-//   32 sequences of about 1800 rows, 20 heads of 64, one query       31 us, 145 MB: 4.6 TB/s; a short call, its loads alone 31
-//   48 sequences of about 7100 rows, 32 heads on 8 of 128, 5 queries, e4m3    129 us, 712 MB: 5.5 TB/s
-//   4 sequences, 8 queries over a window of 4000 rows, 20 heads of 64         15.8 us, 44 MB: 14 the parts, 4 the join (traced)
+//   32 sequences of about 1800 rows, 20 heads of 64, one query       31 us, 145 MB: 4.7 TB/s; a short call, its loads alone 31
+//   48 sequences of about 7100 rows, 32 heads on 8 of 128, 5 queries, e4m3    139 us, 712 MB: 5.1 TB/s
+//   4 sequences, 8 queries over a window of 4000 rows, 20 heads of 64         16 us, 44 MB: 14 the parts, 4 the join (traced)
 //   3 sequences of 200 rows, 4 heads of 32, float32                   8 us, of which a launch is 3: the chain length, table,
 //                                                                     scales, codes, products, join
-//   4 sequences of 4000 rows, 32 heads on 8 of 128, 64 queries        47 us: the softmax's arithmetic and the products
+//   4 sequences of 4000 rows, 32 heads on 8 of 128, 64 queries        54 us: the softmax's arithmetic and the products
 // With more than one query a kv head the matrix units have slots to spare (16 columns a product), so the
 // vector instructions count: per item of 32 rows and 64 dims 64 turn codes into float16, whatever the
-// queries' number; then comes the softmax of 8 scores a lane.  What was measured and not kept: four queries or fewer as the rows of products, a score a
+// queries' number; then comes the softmax of 8 scores a lane, its weights' two parts, and 16 operations a tile that add what
+// the 32 rows add (one card, 48 x 5 queries: 152 us without either, 155 with the adding, 160 with both).
+// What was measured and not kept: four queries or fewer as the rows of products, a score a
 // lane (32 sequences that share one prompt 27 -> 22 us, but 35.3 -> 34.9 where the pages come from memory, float32 25.5 -> 28.6
 // and four queries 92 -> 105 us); three and four items of loads ahead (36 -> 37 to 39 us).
 #include <algorithm>
@@ -122,7 +124,7 @@ __device__ __forceinline__ float group_max(float x) {  // over the lanes of a co
   const u32x2 b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
-// Eight weights (1 the largest) in two float16 parts each, cut off: 20 bits from 2^-4 on, and to 2^-24.  (One part, 11 bits, moved a bfloat16 result by half a step in
+// Eight weights (1 the largest) in two float16 parts each, cut off: 20 bits from 2^-4 on, and to 2^-24.  (One part, 11 bits, moved a bfloat16 result by a step in
 // one of 20 elements; the second is a product more and the time of one in 33 where queries are many: 48 x 5 queries over
 // 7100 rows 155.5 -> 161 us, one query and short calls the same.  Rounded parts, 21 bits, took 164.)
 __device__ __forceinline__ void halves(const f32x4 (&s)[2], f16x8& hi, f16x8& lo) {
@@ -678,7 +680,10 @@ struct Seen {
 // One sequence of 60,000 rows among 31 of about 1000, 20 heads of 64: 729 us in equal parts of the table, 55 so.
 constexpr int kLeast = 24;  // 32 rows each of a part: six for each wave (16 x 1 query of 16 heads on 2 over 4000 rows 12.7 us, 13.8 with 16)
 constexpr int kRound = 512;  // workgroups that sequences are cut for: two a CU (100,000 rows of one 48.2 us, 50.3 with 768)
-constexpr int kLong = 512;  // from this many on, sequences are cut by their own lengths (finding the part takes 2 us)
+// From this many 32 rows of a table's row on, sequences are cut by their own lengths: finding the part takes 2 us (32 sequences
+// of 1500 rows of 20 heads of 64 take 30 in equal parts).  Below, equal parts, so the longest sequence sets the time: 31 of
+// 1000 rows and one of 16,000 take 85 us, one of 17,000 cut by lengths 37, one of 8191 in equal parts 53.
+constexpr int kLong = 512;
 struct Part {
   int b, j, n;  // part j of n of sequence b,
   int at, kv;   // the at-th of all, in kv head kv
