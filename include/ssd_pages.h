@@ -114,7 +114,8 @@ typedef struct {
  * Scores, softmax and sums are float32; 8-bit codes are multiplied exactly.  For the product with the cached values bfloat16 calls
  * hold the weights exp(x - max) in 20 bits or to 2^-24 of the largest weight of the same 32 rows (32 a .. 32 a + 31), float32
  * calls in 22 bits or to 2^-39 of it, and queries in 33 bits; for that with other values bfloat16 calls hold them in 16 bits.
- * No page takes bits from another's, whatever its scale.  Sums are finite where their quotient is (up to scores of 2^29).
+ * No page takes bits from another's, whatever its scale.  Sums are finite where their quotient is (up to scores of 2^29;
+ * beside seen values of 2^80 or scales of 2^48, weights are held in 19 bits).
  * Errors: SSD_E_INVALID_ARG, SSD_E_CAPACITY (workspace too small or not 16-byte aligned, or more than 2^24 workgroups),
  * SSD_E_UNSUPPORTED (page_rows, head_dim, alignment), SSD_E_DEVICE. */
 typedef struct {

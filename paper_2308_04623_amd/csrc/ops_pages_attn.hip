@@ -51,7 +51,8 @@ constexpr float kSlack = 8.f;
 // below what float16 holds to 11 bits.  (By the reference instead, exponents would be rounded as numbers around 15.)
 constexpr float kUp = 15.f;
 // Sums of 2^30 rows with weights up to 2^23 and values up to 2^128 would not be finite where their quotient is.  From finite values
-// of 2^80, or scales of 2^48, on a wave's references are made larger by so much, and its weights smaller.
+// of 2^80 of rows that are seen, or scales of 2^48, on a wave's references are made larger by so much, and its weights
+// smaller (their exponents are rounded as numbers around 56 then: 19 bits).
 constexpr float kLift = 56.f;
 constexpr unsigned kLarge = 127 + 80, kLargeScale = 127 + 48;  // (exponents, as float32 and bfloat16 hold them)
 
@@ -319,12 +320,21 @@ struct Base {
     return (__float_as_uint(x) >> 23 & 255u) - from < 255u - from;
   }
   static __device__ __forceinline__ bool large(uint16_t x, unsigned from) { return (x >> 7 & 255u) - from < 255u - from; }
-  __device__ __forceinline__ bool any_large(const Own& rows) const {
+  // whether one of the values is so of a row that a query of the wave sees (bits: the lane's of its column's)
+  __device__ __forceinline__ bool any_large(const Own& rows, unsigned bits) const {
     bool odd = false;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
       for (int i = 0; i < 8; ++i) odd |= large(rows.v[dt][i], kLarge);
+    if (!__builtin_amdgcn_ballot_w64(odd)) return false;
+    odd = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const bool seen = __builtin_amdgcn_ballot_w64(bits >> i & 1) >> (16 * g) & 0xffff;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) odd |= seen && large(rows.v[dt][i], kLarge);
+    }
     return __builtin_amdgcn_ballot_w64(odd);
   }
   // which of a dim's values are not finite, as 1; they become 0
@@ -523,13 +533,8 @@ struct Tiles : Base<T, D, CODE> {
   __device__ __forceinline__ void take_own(Own& rows, int b, int kv, int x0, int tail, int start, int slot) {
     f32x4 s[NT][2];
     unsigned bits[NT];  // which of the lane's 8 rows are seen
-    if (EARLY && B::any_large(rows)) this->lift = kLift;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int k = 0; k < 2; ++k) s[nt][k] = B::own_scores(rows, k, raw[nt]);
-    complete<2 * NT>(&s[0][0]);
     float by[NT];
+    unsigned all = 0;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       by[nt] = a.scale2;
@@ -538,7 +543,14 @@ struct Tiles : Base<T, D, CODE> {
       for (int i = 0; i < 8; ++i)
         bits[nt] |= B::sees_own(x0 + 16 * (i >> 2) + 4 * g + (i & 3), tail, start, seen_from[nt], anc[nt]) ? 1u << i : 0u;
       if (raw[nt].step < 0) bits[nt] = 0;
+      all |= bits[nt];
     }
+    if (EARLY && B::any_large(rows, all)) this->lift = kLift;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) s[nt][k] = B::own_scores(rows, k, raw[nt]);
+    complete<2 * NT>(&s[0][0]);
     float top[NT], ref[NT], sum[NT];
     meet(s, by, top, true, [&](int nt, int k, int r) { return (bits[nt] >> (4 * k + r) & 1) != 0; });
 #pragma unroll
@@ -553,7 +565,7 @@ struct Tiles : Base<T, D, CODE> {
     for (int nt = 0; nt < NT; ++nt) l[nt] += sum[nt];
     if constexpr (!EARLY) {
       B::template issue_own<false, true>(rows, b, kv, x0, tail, slot);
-      if (this->lift == 0.f && B::any_large(rows)) {
+      if (this->lift == 0.f && B::any_large(rows, all)) {
         this->lift = kLift;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {

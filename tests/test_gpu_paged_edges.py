@@ -277,6 +277,25 @@ def test_queries_with_infinite_elements(env, dtype, code, others):
     assert c.torch.equal(got[:, :, 1], want[:, :, 1]) and c.torch.equal(l2[:, :, 1], lse[:, :, 1])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("t,d,code", [(4, 64, "int8"), (20, 64, "e4m3"), (20, 128, "int8")])
+def test_large_values_that_are_not_seen_change_nothing(env, dtype, t, d, code):
+    """Bitwise: a padded place's rows, and those of the ring that are not the sequence's."""
+    c = P.Case(env, dtype, code, 2, t, 4, 2, d, 32, [740, 95], tree=True, cols=24)
+    for row in c.anc:
+        row[t - 1] = 0
+    want = c.run()
+    for bad in (2.0 ** 100, -(2.0 ** 127)):
+        c.kn[:, t - 1] = bad
+        c.vn[:, t - 1] = bad
+        ring = c.kt.shape[2]
+        for i, n in enumerate(c.lens):
+            for p in range(ring):
+                if p not in {j % ring for j in range(n // 32 * 32, n)}:
+                    c.kt[i, :, p] = c.vt[i, :, p] = bad
+        assert all(c.torch.equal(x, y) for x, y in zip(c.run(), want)), bad
+
+
 # ---------------------------------------------------------------- the binding
 
 def test_numbers_count_by_their_value(env):
