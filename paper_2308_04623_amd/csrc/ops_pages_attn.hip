@@ -17,7 +17,7 @@
 //
 // Bound, and what it measured (int8 unless said otherwise; read: 6.1 TB/s is the most this card reads at, 5.2 a copy moves at):
 //   32 sequences of about 1800 rows, 20 heads of 64, one query       31 us, 145 MB: 4.7 TB/s; a short call, its loads alone 31
-//   48 sequences of about 7100 rows, 32 heads on 8 of 128, 5 queries, e4m3    139 us, 712 MB: 5.1 TB/s
+//   48 sequences of about 7100 rows, 32 heads on 8 of 128, 5 queries, e4m3    140 us, 712 MB: 5.1 TB/s
 //   4 sequences, 8 queries over a window of 4000 rows, 20 heads of 64         16 us, 44 MB: 14 the parts, 4 the join (traced)
 //   3 sequences of 200 rows, 4 heads of 32, float32                   8 us, of which a launch is 3: the chain length, table,
 //                                                                     scales, codes, products, join
